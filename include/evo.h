@@ -287,6 +287,77 @@ evo_status evo_es_gradient_static(const float* d_u, const float* d_eps, uint32_t
                                   uint32_t param_dim, size_t ld_eps, float sigma,
                                   float* d_gradient, void* cuda_stream);
 
+/*
+ * ---- matrix operators -----------------------------------------------------------------------------
+ * Calls without a solver (the paper has no counterpart): what an orthogonalised update is made of, and the
+ * policy's get_actions for callers that run the task themselves.  They keep nothing between calls: all
+ * that they use is in their arguments, so any number of them may be in flight on different streams, each with
+ * a workspace of its own, and they can be captured into CUDA graphs.  The device that owns the buffers must
+ * be current.  A workspace is 256-byte aligned device memory of at least the number of bytes that the
+ * matching _bytes call gives (0: NULL is fine); it holds nothing before or after the call.
+ */
+enum { EVO_F32 = 0, EVO_BF16 = 1, EVO_F16 = 2 };
+
+/* `batch` matrices: element (k, r, c) is data[k * batch_stride + r * row_stride + c], row_stride >= cols;
+ * type EVO_F32 / EVO_BF16 / EVO_F16.  rows and cols up to 2^20. */
+typedef struct evo_matrices {
+    void*    data;                 /* device */
+    uint32_t type, batch, rows, cols;
+    size_t   batch_stride, row_stride;       /* in elements */
+} evo_matrices;
+
+/* The iteration x <- a x + b (x x') x + c (x x')^2 x from x = g / (|g|_F + eps), which moves the singular values
+ * of g towards 1 and keeps its singular vectors.  0 selects 5 steps of (3.4445, -4.7750, 2.0315), eps 1e-7. */
+typedef struct evo_newton_schulz {
+    uint32_t struct_size;          /* sizeof(evo_newton_schulz), checked */
+    uint32_t steps;                /* <= 64                              */
+    float    a, b, c;              /* all three 0: the default           */
+    float    eps;                  /* >= 1e-30                           */
+} evo_newton_schulz;
+
+/*
+ * Orthogonalise every matrix of a batch: out = the result of the iteration above, in out's type (x's).  The sums
+ * are kept in fp32, x in pairs of fp16 numbers (22 bits) whatever the type.  out may be x itself (same pointer
+ * and strides); else the two must not overlap.  ns NULL selects the defaults.  A matrix of zeros stays
+ * zero; one with an infinity or a NaN becomes NaN throughout, and no other matrix does.
+ * Errors: INVALID_ARG, WORKSPACE, UNSUPPORTED (coefficients whose iteration grows a singular value of [0, 1] beyond
+ * 64), CUDA.
+ */
+evo_status evo_orthogonalize_bytes(uint32_t batch, uint32_t rows, uint32_t cols, size_t* bytes);
+evo_status evo_orthogonalize(const evo_newton_schulz* ns, const evo_matrices* x, const evo_matrices* out,
+                             void* d_workspace, size_t workspace_bytes, void* cuda_stream);
+
+/* A weight matrix [rows][cols] inside a flat parameter vector. */
+typedef struct evo_matrix { uint64_t offset; uint32_t rows, cols; } evo_matrix;
+
+typedef struct evo_muon {
+    uint32_t struct_size;          /* sizeof(evo_muon), checked                                         */
+    uint32_t plain_momentum;       /* 1: u = m' below, 0: Nesterov's                                    */
+    double   lr;                   /* (doubles: 1 - beta2 is a difference)                              */
+    double   momentum;             /* mu, 0 <= mu < 1                                                   */
+    double   weight_decay;         /* >= 0                                                              */
+    double   beta1, beta2, adam_eps;   /* 0 selects 0.9 / 0.999 / 1e-8                                  */
+    evo_newton_schulz newton_schulz;
+} evo_muon;
+
+/*
+ * One Muon step (ascent) of a parameter vector of param_dim elements.  For the `n` matrices of `list` (ascending,
+ * not overlapping):
+ *   m' = mu m + (1 - mu) g;  u = mu m' + (1 - mu) g  (plain_momentum: m');  O = orthogonalised u
+ *   center' = (1 - lr weight_decay) center + lr 0.2 sqrt(max(rows, cols)) O;  v' = v
+ * (the factor gives O the root mean square of an Adam step, so one lr serves both), and for everything else Adam
+ * with the same decay, `step` being the number of this step from 1 on:
+ *   m' = b1 m + (1 - b1) g;  v' = b2 v + (1 - b2) g^2
+ *   center' = (1 - lr weight_decay) center + lr (m' / (1 - b1^step)) / (sqrt(v' / (1 - b2^step)) + adam_eps)
+ * Each output may be its own input; otherwise the outputs must not overlap anything.
+ * Errors: INVALID_ARG, WORKSPACE, UNSUPPORTED (as above), CUDA.
+ */
+evo_status evo_muon_bytes(const evo_matrix* list, uint32_t n, uint64_t param_dim, size_t* bytes);
+evo_status evo_muon_step(const evo_muon* cfg, const evo_matrix* list, uint32_t n, uint64_t param_dim, uint32_t step,
+                         const float* d_center, const float* d_m, const float* d_v, const float* d_gradient,
+                         float* d_center_out, float* d_m_out, float* d_v_out,
+                         void* d_workspace, size_t workspace_bytes, void* cuda_stream);
+
 const char* evo_status_string(evo_status st);
 uint32_t    evo_version(void);            /* major*10000 + minor*100 + patch: 1.1.0 = 10100 */
 

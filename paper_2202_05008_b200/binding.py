@@ -103,11 +103,37 @@ def load_library(debug: bool = False):
         getattr(L, name).restype = C.c_int
     L.evo_debug_check.argtypes = [vp, C.POINTER(C.c_int32), u32p, C.POINTER(C.c_uint64)]
     L.evo_debug_check.restype = C.c_int
+    L.evo_orthogonalize_bytes.argtypes = [C.c_uint32, C.c_uint32, C.c_uint32, szp]
+    L.evo_orthogonalize.argtypes = [vp, vp, vp, vp, C.c_size_t, vp]
+    L.evo_muon_bytes.argtypes = [vp, C.c_uint32, C.c_uint64, szp]
+    L.evo_muon_step.argtypes = [vp, vp, C.c_uint32, C.c_uint64, C.c_uint32] + [vp] * 8 + [C.c_size_t, vp]
+    for name in ("evo_orthogonalize_bytes", "evo_orthogonalize", "evo_muon_bytes", "evo_muon_step"):
+        getattr(L, name).restype = C.c_int
     if debug:
         _lib_debug = L
     else:
         _lib = L
     return L
+
+
+class Matrices(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("type", C.c_uint32), ("batch", C.c_uint32), ("rows", C.c_uint32), ("cols", C.c_uint32),
+                ("batch_stride", C.c_size_t), ("row_stride", C.c_size_t)]
+
+
+class NewtonSchulz(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("steps", C.c_uint32), ("a", C.c_float), ("b", C.c_float), ("c", C.c_float),
+                ("eps", C.c_float)]
+
+
+class Matrix(C.Structure):
+    _fields_ = [("offset", C.c_uint64), ("rows", C.c_uint32), ("cols", C.c_uint32)]
+
+
+class Muon(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("plain_momentum", C.c_uint32), ("lr", C.c_double), ("momentum", C.c_double),
+                ("weight_decay", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("adam_eps", C.c_double),
+                ("newton_schulz", NewtonSchulz)]
 
 
 def make_config(w: W.Workload, *, trace_steps: int = 0, rollout_kernel: int = ROLLOUT_AUTO,

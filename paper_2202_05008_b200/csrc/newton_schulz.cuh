@@ -1,0 +1,153 @@
+// Device code that both Newton-Schulz kernels use: how a matrix element is read and written, and the fp16 pairs.
+//
+// The iteration (the odd quintic that Muon made common): X = G / (|G|_F + eps), then `steps` times
+//     A = X X',   B = b A + c A^2,   X <- a X + B X.
+// Its products run on tcgen05 with fp16 operands and fp32 sums, and keep fp32's accuracy: a matrix is a pair of fp16 matrices
+// hi + lo (22 bits) times a power of two, and a product is hi hi' + hi lo' + lo hi' (lo lo' is below 2^-22 of it).
+// Singular values of an estimated gradient are small against the Frobenius norm, and a step multiplies the small ones, and
+// whatever rounding left beside them, by a (3.4): with 11 bits alone a matrix of low rank would come back with some percent of noise in
+// its null space.  The scales are powers of two found on the host from the largest singular value that the steps can reach
+// (an element is never larger), so nothing overflows; what lies below fp16's normal range is below 2^-29 of the largest, and
+// its last bit below 2^-39.
+//
+// All matrices of the iteration are kept in panels: element (i, j) of a matrix with mp rows is half (j / 8 * mp + i) * 8 + j % 8.  A
+// panel's 8 x 8 squares are the core matrices of an unswizzled tcgen05 operand both ways: with j as the contracted index (K-major) and
+// with i (MN-major), so B X and X X' read the same X, and any tile is a set of contiguous runs.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "internal.h"
+#include "newton_schulz.h"
+#include "umma.cuh"
+
+namespace evo {
+namespace ns {
+
+// kind::f16, fp16 x fp16 -> fp32, A K-major; B K-major or MN-major
+__host__ __device__ constexpr uint32_t idesc_f16(uint32_t M, uint32_t N, bool b_mn)
+{
+    return (1u << 4) | (b_mn ? 1u << 16 : 0u) | ((N >> 3) << 17) | ((M >> 4) << 24);
+}
+
+// Waits of a kernel without a status block of its own: after one that ran out all others return at once.
+struct Waits {
+    volatile int* abort;
+    const uint32_t* limit;               // log2 of the clocks (shared memory)
+    uint32_t* sticky;
+    __device__ __forceinline__ void wait(uint32_t bar, uint32_t parity) const
+    {
+        if (mbar_try_wait(bar, parity) || *abort) return;
+        if (!mbar_wait_bounded(bar, parity, limit)) {
+            *abort = 1;
+            if (sticky) atomicOr(sticky, 1u << EVO_ERR_TIMEOUT);
+        }
+    }
+};
+
+// (1 - mu) g and mu m' are rounded once each
+template <uint32_t SRC>
+__device__ __forceinline__ float load(const Args& a, uint64_t at, float* momentum)
+{
+    if constexpr (SRC == kF32) return static_cast<const float*>(a.in)[at];
+    if constexpr (SRC == kBf16) return __bfloat162float(static_cast<const __nv_bfloat16*>(a.in)[at]);
+    if constexpr (SRC == kF16) return __half2float(static_cast<const __half*>(a.in)[at]);
+    if constexpr (SRC == kMuon) {
+        const float g = a.s.rest * static_cast<const float*>(a.in)[at];
+        const float m = fmaf(a.s.mu, a.m_in[at], g);
+        *momentum = m;
+        return a.s.nesterov ? fmaf(a.s.mu, m, g) : m;
+    }
+}
+
+// the momentum of a matrix element, and its second moment as it was (Adam's, which matrices do not use)
+__device__ __forceinline__ void store_moments(const Args& a, uint64_t at, float momentum)
+{
+    a.m_out[at] = momentum;
+    if (a.v_out != a.v_in) a.v_out[at] = a.v_in[at];
+}
+
+template <uint32_t SRC>
+__device__ __forceinline__ void store(const Args& a, uint64_t at, float x, float gain)
+{
+    if constexpr (SRC == kF32) static_cast<float*>(a.out)[at] = x;
+    if constexpr (SRC == kBf16) static_cast<__nv_bfloat16*>(a.out)[at] = __float2bfloat16_rn(x);
+    if constexpr (SRC == kF16) static_cast<__half*>(a.out)[at] = __float2half_rn(x);
+    if constexpr (SRC == kMuon) static_cast<float*>(a.out)[at] = fmaf(gain, x, a.s.keep * a.c_in[at]);
+}
+
+// element (i, j) of the m x n matrix in the source or the result
+__device__ __forceinline__ uint64_t in_index(const Group& g, uint32_t which, uint32_t i, uint32_t j)
+{
+    const uint32_t r = g.tall ? j : i, c = g.tall ? i : j;
+    return g.in + which * g.in_stride + static_cast<uint64_t>(r) * g.in_ld + c;
+}
+__device__ __forceinline__ uint64_t out_index(const Group& g, uint32_t which, uint32_t i, uint32_t j)
+{
+    const uint32_t r = g.tall ? j : i, c = g.tall ? i : j;
+    return g.out + which * g.out_stride + static_cast<uint64_t>(r) * g.out_ld + c;
+}
+
+// What the elements are multiplied with.  A matrix with an infinity or a NaN has no direction: the result is NaN throughout.
+// One whose norm is not far above eps starts with small singular values; it is carried times a further 2^lift, so that fp16 pairs hold
+// it as well, and a step takes `growth` back from that until nothing is left (see lift_at).
+__device__ __forceinline__ double first_scale(const Scalars& s, double sum_of_squares, uint32_t* lift)
+{
+    *lift = 0u;
+    if (!isfinite(sum_of_squares)) return __longlong_as_double(0x7FF8000000000000ll);
+    const double norm = sqrt(sum_of_squares), f = norm / (norm + static_cast<double>(s.eps));
+    if (f > 0.0 && f < 0.5) *lift = static_cast<uint32_t>(min(-1 - ilogb(f), 100));
+    return ldexp(static_cast<double>(s.s_x) / (norm + static_cast<double>(s.eps)), static_cast<int>(*lift));
+}
+// lift of X in step k
+__device__ __forceinline__ uint32_t lift_at(const Scalars& s, uint32_t first, uint32_t k)
+{
+    return first > k * s.growth ? first - k * s.growth : 0u;
+}
+__device__ __forceinline__ float power_of_two(int e) { return __int_as_float(e < -126 ? 0 : (e + 127) << 23); }
+
+// x and y as pairs, packed
+__device__ __forceinline__ void split2(float x, float y, uint32_t& hi, uint32_t& lo)
+{
+    const __half2 h = __floats2half2_rn(x, y);
+    const float2 f = __half22float2(h);
+    const __half2 l = __floats2half2_rn(x - f.x, y - f.y);
+    hi = *reinterpret_cast<const uint32_t*>(&h);
+    lo = *reinterpret_cast<const uint32_t*>(&l);
+}
+__device__ __forceinline__ void split8(const float (&x)[8], uint4& hi, uint4& lo)
+{
+    split2(x[0], x[1], hi.x, lo.x);
+    split2(x[2], x[3], hi.y, lo.y);
+    split2(x[4], x[5], hi.z, lo.z);
+    split2(x[6], x[7], hi.w, lo.w);
+}
+__device__ __forceinline__ void join8(const uint4& hi, const uint4& lo, float (&x)[8])
+{
+    const uint32_t h[4] = { hi.x, hi.y, hi.z, hi.w }, l[4] = { lo.x, lo.y, lo.z, lo.w };
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&h[i]));
+        const float2 b = __half22float2(*reinterpret_cast<const __half2*>(&l[i]));
+        x[2 * i] = a.x + b.x;
+        x[2 * i + 1] = a.y + b.y;
+    }
+}
+
+// fixed-order sum over a block of T threads; every thread gets it
+template <uint32_t T>
+__device__ __forceinline__ double block_sum(double x, double* red)
+{
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) x += __shfl_xor_sync(0xffffffffu, x, off);
+    if ((threadIdx.x & 31u) == 0u) red[threadIdx.x >> 5] = x;
+    __syncthreads();
+    double t = 0.0;
+#pragma unroll
+    for (uint32_t w = 0; w < T / 32u; ++w) t += red[w];
+    __syncthreads();
+    return t;
+}
+
+}  // namespace ns
+}  // namespace evo
