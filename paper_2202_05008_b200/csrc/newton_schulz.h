@@ -8,11 +8,13 @@
 namespace evo {
 namespace ns {
 
-// The tensor core cuts its sums off instead of rounding them, 4e-8 of the sum per MMA on average, and always downwards: 2048^2
-// came out 1.6e-5 off with all products in one accumulator (a chain of fp32 torch products: 3.6e-6).  So the small products
-// have an accumulator of their own, and the large ones' is taken out and added up in registers every 256 of the contracted index
-// (2.1e-6).
+// The tensor core cuts its sums off instead of rounding them, always towards zero: sums of squares come out short by kCut per MMA
+// (A X of random matrices, one step: -6.1e-8 with one MMA a sum, -4.6e-7 with 8, -9.4e-7 with 16; 2048^2 was 1.6e-5 off after five
+// steps with all products in one accumulator, a chain of fp32 torch products 3.6e-6).  So the small products have an accumulator of
+// their own, the large ones' is taken out and added up in registers every kChunk of the contracted index, and what A's sums lack on
+// average is given back.
 constexpr uint32_t kChunk = 256;
+constexpr float kCut = 5.7e-8f;
 
 // What a matrix is made from, and what becomes of the result: a plain matrix of one of three types, or the gradient of a flat
 // parameter vector (its momentum is updated on the way in, the centre on the way out).

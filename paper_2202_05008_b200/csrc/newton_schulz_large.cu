@@ -273,6 +273,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) k_ns_gemm(const __grid_consta
             const uint32_t width = MODE == kApply ? min(kTile, g.np - t.j0) : kTile;
             float sum[2][4][8];
             for (uint32_t k = 0; k < t.k; k += kChunk) {
+                const float cut = MODE == kGram ? kCut * static_cast<float>(min(kChunk, t.k - k) / 16u) : 0.f;
                 waits.wait(smem_u32(&done[acc]), acc_phase);
                 tc_fence_after();
 #pragma unroll
@@ -287,7 +288,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) k_ns_gemm(const __grid_consta
                     for (int c = 0; c < 4; ++c)
 #pragma unroll
                         for (int e = 0; e < 8; ++e) {
-                            const float x = __uint_as_float(u[c][e]) + __uint_as_float(v[c][e]);
+                            const float x = __uint_as_float(u[c][e]) + fmaf(cut, __uint_as_float(u[c][e]), __uint_as_float(v[c][e]));
                             sum[h][c][e] = k == 0u ? x : sum[h][c][e] + x;
                         }
                 }

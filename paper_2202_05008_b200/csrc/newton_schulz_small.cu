@@ -98,7 +98,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_small(const __grid_constant_
             umma_bf16(tmem, ph, rh, idesc, k != 0u);
             umma_bf16(tmem + half_cols, ph, rl, idesc, k != 0u);
             umma_bf16(tmem + half_cols, pl, rh, idesc, 1u);
-            umma_bf16(tmem + half_cols, pl, rl, idesc, 1u);      // (the squares on A's diagonal all miss it: 1 x 1 was 1.3e-6 off, now NEW)
+            umma_bf16(tmem + half_cols, pl, rl, idesc, 1u);      // (the squares on A's diagonal would all miss it)
         }
         umma_commit(smem_u32(&bar));
     };
@@ -116,7 +116,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_small(const __grid_constant_
     };
     const uint32_t row = (warp & 3u) * 32u + lane, lanes = (warp & 3u) << 21, part = warp >> 2;      // four warps share a quarter of the lanes
     const bool rows_live = (warp & 3u) * 32u < mp, row_live = row < mp;
-    auto sums8 = [&](uint32_t c, float (&x)[8]) {
+    auto sums8 = [&](uint32_t c, float (&x)[8], float cut = 0.f) {
         uint32_t u[8], v[8];
         tmem_ld8_issue(tmem + lanes + c * 8u, u);
         tmem_ld8_issue(tmem + half_cols + lanes + c * 8u, v);
@@ -124,7 +124,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_small(const __grid_constant_
                      : "+r"(u[0]), "+r"(u[1]), "+r"(u[2]), "+r"(u[3]), "+r"(u[4]), "+r"(u[5]), "+r"(u[6]), "+r"(u[7]),
                        "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]) :: "memory");
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = __uint_as_float(u[e]) + __uint_as_float(v[e]);
+        for (int e = 0; e < 8; ++e) x[e] = __uint_as_float(u[e]) + fmaf(cut, __uint_as_float(u[e]), __uint_as_float(v[e]));
     };
     auto put_q = [&](uint32_t c, const float (&x)[8]) {
         uint4 hi, lo;
@@ -155,7 +155,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_small(const __grid_constant_
                 for (uint32_t c = 0; c < 4u; ++c)
                     if (part + 4u * c < mp / 8u) {
                         float x[8];
-                        sums8(part + 4u * c, x);
+                        sums8(part + 4u * c, x, kCut * static_cast<float>(min(kChunk, np - k0) / 16u));
 #pragma unroll
                         for (int e = 0; e < 8; ++e) gram[c][e] = k0 == 0u ? x[e] : gram[c][e] + x[e];
                     }
