@@ -358,6 +358,54 @@ evo_status evo_muon_step(const evo_muon* cfg, const evo_matrix* list, uint32_t n
                          float* d_center_out, float* d_m_out, float* d_v_out,
                          void* d_workspace, size_t workspace_bytes, void* cuda_stream);
 
+/*
+ * Product grouped by member (or expert), with bias and activation:
+ *   y[r] = scale act(W_g x[r] + b_g)   for the rows offsets[g] <= r < offsets[g + 1] of each of `groups` groups.
+ * x[rows][n_in], y[rows][n_out], W_g[n_out][n_in] at weight + g weight_stride, b_g at bias + g bias_stride (bias NULL:
+ * none); all of one type, any pitch and alignment; a layer of every row of theta is such a set of weights.
+ * offsets[groups + 1] (int32, or int64 with offsets_64) lies on the device and does not fall; groups may be empty.  Rows of y
+ * that belong to no group are left as they are.  (Offsets that fall or leave [0, rows] give wrong rows, but nothing
+ * outside the arrays is touched.)  Sums in fp32; fp32 operands count with 21 bits and more.  y may not overlap anything.
+ * Errors: INVALID_ARG, UNSUPPORTED (more than 2^31 blocks), CUDA.
+ */
+enum { EVO_ACT_NONE = 0, EVO_ACT_TANH = 1, EVO_ACT_RELU = 2 };
+typedef struct evo_grouped {
+    uint32_t struct_size;          /* sizeof(evo_grouped), checked */
+    uint32_t type, groups, n_in, n_out;      /* n_in, n_out up to 2^20 */
+    uint32_t activation;           /* EVO_ACT_*                    */
+    float    scale;
+    uint32_t offsets_64;
+    uint64_t rows;
+    const void* d_x;       size_t ld_x;
+    const void* d_weight;  size_t ld_weight, weight_stride;
+    const void* d_bias;    size_t bias_stride;
+    const void* d_offsets;
+    void*       d_y;       size_t ld_y;
+} evo_grouped;
+evo_status evo_grouped_linear(const evo_grouped* p, void* cuda_stream);
+
+/*
+ * The MLP policy's get_actions (paper Section 4, PolicyNetwork.get_actions) for callers that run the task themselves:
+ * rows offsets[m] <= r < offsets[m + 1] of the observations are member m's (episodes that have ended need no row), and
+ *   actions[r] = action_scale tanh(W_L ... tanh(W_1 observations[r] + b_1) ... + b_L)
+ * with the parameters theta[m] (fp32, pitch ld_theta: a multiple of 4 floats, rows 16-byte aligned) in the
+ * layout of evo_ask.  Offsets and rows without a member as above.
+ * Errors: INVALID_ARG, WORKSPACE, UNSUPPORTED, CUDA.  Workspace 0 unless a member's parameters exceed a block's shared memory.
+ */
+typedef struct evo_actions {
+    uint32_t struct_size;          /* sizeof(evo_actions), checked */
+    uint32_t members, n_layers, layer_sizes[EVO_MAX_LAYERS + 1];
+    float    action_scale;
+    uint32_t offsets_64;
+    uint64_t rows;
+    const float* d_theta;         size_t ld_theta;
+    const float* d_observations;  size_t ld_observations;
+    const void*  d_offsets;
+    float*       d_actions;       size_t ld_actions;
+} evo_actions;
+evo_status evo_mlp_actions_bytes(const evo_actions* p, size_t* bytes);
+evo_status evo_mlp_actions(const evo_actions* p, void* d_workspace, size_t workspace_bytes, void* cuda_stream);
+
 const char* evo_status_string(evo_status st);
 uint32_t    evo_version(void);            /* major*10000 + minor*100 + patch: 1.1.0 = 10100 */
 

@@ -4,5 +4,5 @@
 configurations and seeded input generators; ``build`` compiles the CUDA sources.
 """
 from .binding import EvoConfig, EvoError, Solver, load_library  # noqa: F401
-from .operators import muon_step, orthogonalize  # noqa: F401
+from .operators import grouped_linear, mlp_actions, muon_step, orthogonalize  # noqa: F401
 from . import workloads  # noqa: F401

@@ -107,7 +107,11 @@ def load_library(debug: bool = False):
     L.evo_orthogonalize.argtypes = [vp, vp, vp, vp, C.c_size_t, vp]
     L.evo_muon_bytes.argtypes = [vp, C.c_uint32, C.c_uint64, szp]
     L.evo_muon_step.argtypes = [vp, vp, C.c_uint32, C.c_uint64, C.c_uint32] + [vp] * 8 + [C.c_size_t, vp]
-    for name in ("evo_orthogonalize_bytes", "evo_orthogonalize", "evo_muon_bytes", "evo_muon_step"):
+    L.evo_grouped_linear.argtypes = [vp, vp]
+    L.evo_mlp_actions_bytes.argtypes = [vp, szp]
+    L.evo_mlp_actions.argtypes = [vp, vp, C.c_size_t, vp]
+    for name in ("evo_orthogonalize_bytes", "evo_orthogonalize", "evo_muon_bytes", "evo_muon_step", "evo_grouped_linear",
+                 "evo_mlp_actions_bytes", "evo_mlp_actions"):
         getattr(L, name).restype = C.c_int
     if debug:
         _lib_debug = L
@@ -134,6 +138,21 @@ class Muon(C.Structure):
     _fields_ = [("struct_size", C.c_uint32), ("plain_momentum", C.c_uint32), ("lr", C.c_double), ("momentum", C.c_double),
                 ("weight_decay", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("adam_eps", C.c_double),
                 ("newton_schulz", NewtonSchulz)]
+
+
+class Grouped(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("type", C.c_uint32), ("groups", C.c_uint32), ("n_in", C.c_uint32), ("n_out", C.c_uint32),
+                ("activation", C.c_uint32), ("scale", C.c_float), ("offsets_64", C.c_uint32), ("rows", C.c_uint64),
+                ("d_x", C.c_void_p), ("ld_x", C.c_size_t), ("d_weight", C.c_void_p), ("ld_weight", C.c_size_t),
+                ("weight_stride", C.c_size_t), ("d_bias", C.c_void_p), ("bias_stride", C.c_size_t), ("d_offsets", C.c_void_p),
+                ("d_y", C.c_void_p), ("ld_y", C.c_size_t)]
+
+
+class Actions(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("members", C.c_uint32), ("n_layers", C.c_uint32),
+                ("layer_sizes", C.c_uint32 * (EVO_MAX_LAYERS + 1)), ("action_scale", C.c_float), ("offsets_64", C.c_uint32),
+                ("rows", C.c_uint64), ("d_theta", C.c_void_p), ("ld_theta", C.c_size_t), ("d_observations", C.c_void_p),
+                ("ld_observations", C.c_size_t), ("d_offsets", C.c_void_p), ("d_actions", C.c_void_p), ("ld_actions", C.c_size_t)]
 
 
 def make_config(w: W.Workload, *, trace_steps: int = 0, rollout_kernel: int = ROLLOUT_AUTO,
@@ -191,13 +210,15 @@ class Solver:
         self.P, self.D = (2 * self.cfg.shard_pairs if self.cfg.shard_pairs else workload.pop_size), workload.param_dim
         self.ldD = (self.D + 31) // 32 * 32
         self._batch = None
+        self._theta = None
 
     # -- the five calls ------------------------------------------------------------------
     def ask(self) -> torch.Tensor:
         """theta[P][D] as a strided view (row pitch ldD) of the workspace."""
         p, ld = C.c_void_p(), C.c_size_t()
         _check(self.lib.evo_ask(self._h, C.byref(p), C.byref(ld)), "evo_ask")
-        return self._view_f32(p.value, self.P, ld.value)[:, :self.D]
+        self._theta = self._view_f32(p.value, self.P, ld.value)[:, :self.D]
+        return self._theta
 
     def rollout(self, theta: Optional[torch.Tensor] = None, fitness: Optional[torch.Tensor] = None,
                 trace: Optional[torch.Tensor] = None) -> torch.Tensor:
@@ -232,6 +253,20 @@ class Solver:
 
     def tell_end(self) -> None:
         _check(self.lib.evo_tell_end(self._h), "evo_tell_end")
+
+    def actions(self, observations: torch.Tensor, offsets: torch.Tensor, theta: Optional[torch.Tensor] = None,
+                out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """The MLP policy's get_actions for a task outside the library: rows offsets[m] .. offsets[m + 1] of the
+        observations belong to member m of ``theta`` (by default the matrix of the last ask).  See ``mlp_actions``."""
+        from .operators import mlp_actions
+        if self.workload.policy_kind != W.POLICY_MLP:
+            raise EvoError(7, "actions")
+        if theta is None:
+            if self._theta is None:
+                raise EvoError(2, "actions")
+            theta = self._theta
+        return mlp_actions(theta, self.workload.layer_sizes, observations, offsets, action_scale=self.workload.action_scale, out=out,
+                           stream=self.stream)
 
     def capture_generation(self, fitness: torch.Tensor) -> "torch.cuda.CUDAGraph":
         """Captures ask -> rollout -> tell into a CUDA graph; every ``replay()`` is one generation

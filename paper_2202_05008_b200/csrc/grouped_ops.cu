@@ -1,0 +1,136 @@
+// C entry points of the products grouped by member and of the policy's actions.
+#include <cmath>
+#include <cstring>
+
+#include "grouped.h"
+#include "mlp_actions.h"
+
+using namespace evo;
+
+namespace {
+
+bool overlap(const void* p, uint64_t n, const void* q, uint64_t m)
+{
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
+    return a < b + m && b < a + n;
+}
+uint64_t span(uint64_t rows, uint64_t ld, uint64_t cols) { return rows ? (rows - 1u) * ld + cols : 0u; }
+
+constexpr uint64_t kMost = 1ull << 40;       // elements of a pitch or a stride, and rows: their products stay inside 64 bits
+
+// rows of the layers between the first and the last, twice, for a policy that one block does not hold
+size_t layers_bytes(const evo_actions& a)
+{
+    uint64_t widest = 0;
+    for (uint32_t l = 1; l < a.n_layers; ++l) widest = a.layer_sizes[l] > widest ? a.layer_sizes[l] : widest;
+    return static_cast<size_t>(2u * a.rows * ((widest + 3u) / 4u * 4u) * sizeof(float));
+}
+
+evo_status check_actions(const evo_actions* a)
+{
+    if (!a || a->struct_size != sizeof(evo_actions) || a->members < 1u || a->n_layers < 1u || a->n_layers > EVO_MAX_LAYERS) return EVO_ERR_INVALID_ARG;
+    uint64_t dim = 0;
+    for (uint32_t l = 0; l <= a->n_layers; ++l)
+        if (a->layer_sizes[l] < 1u || a->layer_sizes[l] > (1u << 20)) return EVO_ERR_INVALID_ARG;
+    for (uint32_t l = 0; l < a->n_layers; ++l) dim += static_cast<uint64_t>(a->layer_sizes[l] + 1u) * a->layer_sizes[l + 1];
+    if (dim > kMaxParamDim || a->ld_theta < dim || a->ld_theta > kMost || (a->ld_theta & 3u)) return EVO_ERR_INVALID_ARG;
+    if (a->rows > kMost || a->members > 0x7FFFFFFFu || a->offsets_64 > 1u || !std::isfinite(a->action_scale)) return EVO_ERR_INVALID_ARG;
+    return EVO_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+evo_status evo_grouped_linear(const evo_grouped* p, void* cuda_stream)
+{
+    if (!p || p->struct_size != sizeof(evo_grouped) || p->type > EVO_F16 || p->activation > EVO_ACT_RELU || p->offsets_64 > 1u) return EVO_ERR_INVALID_ARG;
+    if (p->groups < 1u || p->groups > 0x7FFFFFFFu || p->n_in < 1u || p->n_out < 1u || p->n_in > (1u << 20) || p->n_out > (1u << 20)) return EVO_ERR_INVALID_ARG;
+    if (p->rows > kMost || p->ld_x > kMost || p->ld_y > kMost || p->ld_weight > kMost || p->weight_stride > kMost || p->bias_stride > kMost) return EVO_ERR_INVALID_ARG;
+    if (!std::isfinite(p->scale)) return EVO_ERR_INVALID_ARG;
+    if (p->rows == 0u) return EVO_OK;
+    const uint64_t size = p->type == EVO_F32 ? 4u : 2u;
+    const uintptr_t bits = reinterpret_cast<uintptr_t>(p->d_x) | reinterpret_cast<uintptr_t>(p->d_weight) | reinterpret_cast<uintptr_t>(p->d_bias) |
+                           reinterpret_cast<uintptr_t>(p->d_y);
+    if (!p->d_x || !p->d_weight || !p->d_y || !p->d_offsets || (bits & (size - 1u))) return EVO_ERR_INVALID_ARG;
+    if (reinterpret_cast<uintptr_t>(p->d_offsets) & (p->offsets_64 ? 7u : 3u)) return EVO_ERR_INVALID_ARG;
+    if ((p->rows > 1u && (p->ld_x < p->n_in || p->ld_y < p->n_out)) || (p->n_out > 1u && p->ld_weight < p->n_in)) return EVO_ERR_INVALID_ARG;
+    // (weights and biases may be shared by groups: stride 0)
+    const uint64_t y_bytes = span(p->rows, p->ld_y, p->n_out) * size;
+    if (overlap(p->d_y, y_bytes, p->d_x, span(p->rows, p->ld_x, p->n_in) * size) ||
+        overlap(p->d_y, y_bytes, p->d_weight, ((p->groups - 1u) * static_cast<uint64_t>(p->weight_stride) + span(p->n_out, p->ld_weight, p->n_in)) * size) ||
+        (p->d_bias && overlap(p->d_y, y_bytes, p->d_bias, ((p->groups - 1u) * static_cast<uint64_t>(p->bias_stride) + p->n_out) * size)) ||
+        overlap(p->d_y, y_bytes, p->d_offsets, (p->groups + 1ull) * (p->offsets_64 ? 8u : 4u)))
+        return EVO_ERR_INVALID_ARG;
+    GroupedArgs a;
+    std::memset(&a, 0, sizeof(a));
+    a.x = p->d_x; a.w = p->d_weight; a.b = p->d_bias; a.y = p->d_y; a.offsets = p->d_offsets; a.wide_offsets = p->offsets_64;
+    a.groups = p->groups; a.n_in = p->n_in; a.n_out = p->n_out; a.activation = p->activation; a.scale = p->scale;
+    // a pitch that is never taken may be anything
+    a.rows = p->rows; a.ld_x = p->rows > 1u ? p->ld_x : 0u; a.ld_y = p->ld_y; a.ld_w = p->n_out > 1u ? p->ld_weight : 0u;
+    a.stride_w = p->groups > 1u ? p->weight_stride : 0u; a.stride_b = p->bias_stride;
+    const int n = launch_grouped(static_cast<cudaStream_t>(cuda_stream), p->type, a);
+    return n == -2 ? EVO_ERR_UNSUPPORTED : n < 0 ? EVO_ERR_CUDA : EVO_OK;
+}
+
+evo_status evo_mlp_actions_bytes(const evo_actions* p, size_t* bytes)
+{
+    const evo_status st = check_actions(p);
+    if (st != EVO_OK || !bytes) return EVO_ERR_INVALID_ARG;
+    ActionsArgs a;
+    size_t smem = 0;
+    *bytes = actions_plan(p->layer_sizes, p->n_layers, &a, &smem) ? 0u : layers_bytes(*p);
+    return EVO_OK;
+}
+
+evo_status evo_mlp_actions(const evo_actions* p, void* d_workspace, size_t workspace_bytes, void* cuda_stream)
+{
+    size_t need = 0;
+    const evo_status st = evo_mlp_actions_bytes(p, &need);
+    if (st != EVO_OK) return st;
+    const uint32_t n_in = p->layer_sizes[0], n_out = p->layer_sizes[p->n_layers];
+    if (p->rows == 0u) return EVO_OK;
+    if (!p->d_theta || !p->d_observations || !p->d_actions || !p->d_offsets || (reinterpret_cast<uintptr_t>(p->d_theta) & 15u)) return EVO_ERR_INVALID_ARG;
+    if ((reinterpret_cast<uintptr_t>(p->d_observations) | reinterpret_cast<uintptr_t>(p->d_actions)) & 3u) return EVO_ERR_INVALID_ARG;
+    if (reinterpret_cast<uintptr_t>(p->d_offsets) & (p->offsets_64 ? 7u : 3u)) return EVO_ERR_INVALID_ARG;
+    if (p->ld_observations > kMost || p->ld_actions > kMost || (p->rows > 1u && (p->ld_observations < n_in || p->ld_actions < n_out))) return EVO_ERR_INVALID_ARG;
+    const uint64_t out_bytes = span(p->rows, p->ld_actions, n_out) * 4u;
+    if (overlap(p->d_actions, out_bytes, p->d_observations, span(p->rows, p->ld_observations, n_in) * 4u) ||
+        overlap(p->d_actions, out_bytes, p->d_theta, static_cast<uint64_t>(p->members) * p->ld_theta * 4u) ||
+        overlap(p->d_actions, out_bytes, p->d_offsets, (p->members + 1ull) * (p->offsets_64 ? 8u : 4u)))
+        return EVO_ERR_INVALID_ARG;
+    if (need && (!d_workspace || (reinterpret_cast<uintptr_t>(d_workspace) & 255u))) return EVO_ERR_INVALID_ARG;
+    if (workspace_bytes < need) return EVO_ERR_WORKSPACE;
+    const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    ActionsArgs a;
+    std::memset(&a, 0, sizeof(a));
+    size_t smem = 0;
+    const bool whole = actions_plan(p->layer_sizes, p->n_layers, &a, &smem);
+    a.theta = p->d_theta; a.ld_theta = p->ld_theta;
+    GroupedArgs& g = a.g;
+    g.x = p->d_observations; g.y = p->d_actions; g.offsets = p->d_offsets; g.wide_offsets = p->offsets_64; g.groups = p->members; g.rows = p->rows;
+    g.ld_x = p->rows > 1u ? p->ld_observations : 0u; g.ld_y = p->ld_actions; g.activation = EVO_ACT_TANH; g.scale = p->action_scale;
+    if (whole) {
+        const int n = launch_actions(stream, a, smem);
+        return n == -2 ? EVO_ERR_UNSUPPORTED : n < 0 ? EVO_ERR_CUDA : EVO_OK;
+    }
+    // a launch per layer, hidden rows in the workspace
+    float* const hidden[2] = { static_cast<float*>(d_workspace), static_cast<float*>(d_workspace) + need / 8u };
+    uint64_t at = 0;
+    for (uint32_t l = 0; l < p->n_layers; ++l) {
+        const bool last = l + 1u == p->n_layers;
+        GroupedArgs b = g;
+        b.n_in = p->layer_sizes[l]; b.n_out = p->layer_sizes[l + 1];
+        if (l) { b.x = hidden[l & 1u]; b.ld_x = (b.n_in + 3u) / 4u * 4u; }
+        if (!last) { b.y = hidden[(l + 1u) & 1u]; b.ld_y = (b.n_out + 3u) / 4u * 4u; b.scale = 1.f; }
+        b.w = p->d_theta + at; b.ld_w = b.n_in; b.stride_w = p->ld_theta;
+        at += static_cast<uint64_t>(b.n_in) * b.n_out;
+        b.b = p->d_theta + at; b.stride_b = p->ld_theta;
+        at += b.n_out;
+        const int n = launch_grouped(stream, EVO_F32, b);
+        if (n < 0) return n == -2 ? EVO_ERR_UNSUPPORTED : EVO_ERR_CUDA;
+    }
+    return EVO_OK;
+}
+
+}  // extern "C"

@@ -11,10 +11,11 @@ from typing import Optional, Sequence, Tuple
 
 import torch
 
-from .binding import EvoError, Matrices, Matrix, Muon, NewtonSchulz, _check, load_library
+from .binding import EVO_MAX_LAYERS, Actions, EvoError, Grouped, Matrices, Matrix, Muon, NewtonSchulz, _check, load_library
 
 TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 INVALID_ARG = 1
+ACTIVATIONS = {"none": 0, "tanh": 1, "relu": 2}
 COEFFICIENTS = (3.4445, -4.7750, 2.0315)
 
 
@@ -111,3 +112,75 @@ def muon_step(center: torch.Tensor, m: torch.Tensor, v: torch.Tensor, gradient: 
                                  gradient.data_ptr(), out[0].data_ptr(), out[1].data_ptr(), out[2].data_ptr(),
                                  None if work is None else work.data_ptr(), need.value, st), where)
     return tuple(out)
+
+
+def _rows(x: torch.Tensor, dtype: torch.dtype, like: torch.Tensor) -> bool:
+    return x.is_cuda and x.device == like.device and x.dtype == dtype and x.dim() == 2 and (x.shape[1] <= 1 or x.stride(1) == 1)
+
+
+def _ragged(offsets: torch.Tensor, groups: int, like: torch.Tensor, where: str) -> int:
+    _require(offsets.device == like.device and offsets.dtype in (torch.int32, torch.int64) and offsets.dim() == 1 and
+             offsets.numel() == groups + 1 and offsets.is_contiguous(), where, "offsets: int32 or int64 on the same GPU, one more than groups")
+    return 1 if offsets.dtype == torch.int64 else 0
+
+
+def _out(out: Optional[torch.Tensor], x: torch.Tensor, cols: int, where: str) -> torch.Tensor:
+    if out is None:
+        return torch.empty(x.shape[0], cols, dtype=x.dtype, device=x.device)
+    _require(_rows(out, x.dtype, x) and out.shape == (x.shape[0], cols), where, "out does not match")
+    return out
+
+
+def grouped_linear(x: torch.Tensor, weight: torch.Tensor, offsets: torch.Tensor, bias: Optional[torch.Tensor] = None, *,
+                   activation: str = "none", scale: float = 1.0, out: Optional[torch.Tensor] = None,
+                   stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """``evo_grouped_linear``: ``y[r] = scale * act(weight[g] @ x[r] + bias[g])`` for the rows ``offsets[g] <= r < offsets[g + 1]``.
+    x [rows, n_in], weight [groups, n_out, n_in], bias [groups, n_out]; fp32, bf16 or fp16; unit stride in the last dimension, any
+    other strides (a layer of theta is ``theta[:, a:b].unflatten(1, (n_out, n_in))``; an expanded weight is shared).  Rows outside all
+    groups are left as they are in ``out``, and undefined without one."""
+    lib, where = load_library(), "grouped_linear"
+    _require(x.is_cuda and x.dtype in TYPES and _rows(x, x.dtype, x), where, "x: fp32, bf16 or fp16 rows on a GPU")
+    _require(weight.device == x.device and weight.dtype == x.dtype and weight.dim() == 3 and weight.shape[0] >= 1 and
+             weight.shape[2] == x.shape[1] and (weight.shape[2] <= 1 or weight.stride(2) == 1), where, "weight does not match x")
+    groups, n_out, n_in = weight.shape
+    _require(n_out >= 1 and n_in >= 1 and activation in ACTIVATIONS, where, "sizes or activation")
+    _require(weight.stride(0) >= 0 and weight.stride(1) >= 0, where, "weight strides")
+    if bias is not None:
+        _require(_rows(bias, x.dtype, x) and bias.shape == (groups, n_out) and (n_out == 1 or bias.stride(1) == 1), where, "bias does not match")
+    wide = _ragged(offsets, groups, x, where)
+    with _On(x.device, stream) as st:
+        y = _out(out, x, n_out, where)
+        p = Grouped(C.sizeof(Grouped), TYPES[x.dtype], groups, n_in, n_out, ACTIVATIONS[activation], scale, wide, x.shape[0],
+                    x.data_ptr(), x.stride(0), weight.data_ptr(), weight.stride(1) if n_out > 1 else n_in, weight.stride(0),
+                    None if bias is None else bias.data_ptr(), 0 if bias is None else bias.stride(0), offsets.data_ptr(), y.data_ptr(),
+                    y.stride(0))
+        _check(lib.evo_grouped_linear(C.byref(p), st), where)
+    return y
+
+
+def mlp_actions(theta: torch.Tensor, layer_sizes: Sequence[int], observations: torch.Tensor, offsets: torch.Tensor, *,
+                action_scale: float = 1.0, out: Optional[torch.Tensor] = None,
+                stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """``evo_mlp_actions``: the MLP policy's actions for rows of observations, ``offsets[m] <= r < offsets[m + 1]`` being member m's.
+    theta [members, >= parameters] fp32 as ``Solver.ask`` returns it (row pitch a multiple of 4, rows 16-byte aligned),
+    layer_sizes the widths, input first.  Rows without a member are left as they are in ``out``, and undefined without one."""
+    lib, where = load_library(), "mlp_actions"
+    sizes = tuple(layer_sizes)
+    _require(2 <= len(sizes) <= EVO_MAX_LAYERS + 1 and min(sizes) >= 1, where, "layer_sizes")
+    _require(observations.is_cuda and _rows(observations, torch.float32, observations) and observations.shape[1] == sizes[0], where,
+             "observations: fp32 rows of the first layer's width on a GPU")
+    dim = sum((a + 1) * b for a, b in zip(sizes[:-1], sizes[1:]))
+    _require(_rows(theta, torch.float32, observations) and theta.shape[0] >= 1 and theta.shape[1] >= dim, where, "theta does not match")
+    members = theta.shape[0]
+    wide = _ragged(offsets, members, observations, where)
+    with _On(observations.device, stream) as st:
+        y = _out(out, observations, sizes[-1], where)
+        pitch = theta.stride(0) if members > 1 else -(-max(dim, theta.stride(0)) // 4) * 4
+        p = Actions(C.sizeof(Actions), members, len(sizes) - 1, (C.c_uint32 * (EVO_MAX_LAYERS + 1))(*sizes), action_scale, wide,
+                    observations.shape[0], theta.data_ptr(), pitch, observations.data_ptr(), observations.stride(0), offsets.data_ptr(),
+                    y.data_ptr(), y.stride(0))
+        need = C.c_size_t()
+        _check(lib.evo_mlp_actions_bytes(C.byref(p), C.byref(need)), where)
+        work = torch.empty(need.value, dtype=torch.uint8, device=observations.device) if need.value else None
+        _check(lib.evo_mlp_actions(C.byref(p), None if work is None else work.data_ptr(), need.value, st), where)
+    return y

@@ -5,7 +5,7 @@ import ctypes as C
 import pytest
 
 from paper_2202_05008_b200 import build as B
-from paper_2202_05008_b200.binding import Matrices, Matrix, Muon, NewtonSchulz, load_library
+from paper_2202_05008_b200.binding import Actions, Grouped, Matrices, Matrix, Muon, NewtonSchulz, load_library
 
 OK, INVALID, WORKSPACE, UNSUPPORTED = 0, 1, 3, 7
 FAR = 1 << 40          # addresses far apart: 1 FAR, 2 FAR, ...
@@ -125,3 +125,50 @@ def test_muon_step_refusals(lib):
     assert call(ptrs=apart[:4] + [apart[0] + 4] + apart[5:]) == INVALID
     assert call(work=None) == INVALID and call(work=FAR * 9 + 8) == INVALID and call(size=1024) == WORKSPACE
     assert lib.evo_muon_step(None, items, n, 90010, 1, *apart, FAR * 9, 1 << 40, None) == INVALID
+
+
+def _grouped(**kw):
+    p = Grouped(C.sizeof(Grouped), 0, 4, 10, 20, 1, 1.0, 0, 100, FAR, 10, 2 * FAR, 10, 200, 3 * FAR, 20, 4 * FAR, 5 * FAR, 20)
+    for k, v in kw.items():
+        setattr(p, k, v)
+    return p
+
+
+@pytest.mark.parametrize("bad", [dict(struct_size=8), dict(type=3), dict(groups=0), dict(n_in=0), dict(n_out=0), dict(n_in=(1 << 20) + 1), dict(activation=3),
+                                 dict(scale=float("inf")), dict(offsets_64=2), dict(rows=1 << 41), dict(d_x=None), dict(d_weight=None), dict(d_y=None),
+                                 dict(d_offsets=None), dict(d_x=FAR + 2), dict(d_bias=3 * FAR + 1), dict(d_offsets=4 * FAR + 2),
+                                 dict(offsets_64=1, d_offsets=4 * FAR + 4), dict(ld_x=9), dict(ld_y=19), dict(ld_weight=9), dict(weight_stride=1 << 41),
+                                 dict(d_y=FAR + 4), dict(d_y=2 * FAR - 4), dict(d_y=3 * FAR), dict(d_y=4 * FAR), dict(groups=1 << 31)])
+def test_grouped_refusals(lib, bad):
+    assert lib.evo_grouped_linear(C.byref(_grouped(**bad)), None) == INVALID
+
+
+def test_grouped_without_rows_is_nothing_to_do(lib):
+    assert lib.evo_grouped_linear(C.byref(_grouped(rows=0, d_x=None, d_y=None)), None) == OK
+    assert lib.evo_grouped_linear(None, None) == INVALID
+    assert lib.evo_grouped_linear(C.byref(_grouped(groups=(1 << 31) - 1, n_out=1 << 20, weight_stride=0, ld_y=1 << 20, d_y=FAR * 64)), None) in (INVALID, UNSUPPORTED)
+
+
+def _actions(sizes=(5, 16, 16, 1), **kw):
+    p = Actions(C.sizeof(Actions), 4, len(sizes) - 1, (C.c_uint32 * 9)(*sizes), 1.0, 0, 100, FAR, 416, 2 * FAR, sizes[0], 3 * FAR, 4 * FAR, sizes[-1])
+    for k, v in kw.items():
+        setattr(p, k, v)
+    return p
+
+
+def test_actions_refusals(lib):
+    n = C.c_size_t(9)
+    assert lib.evo_mlp_actions_bytes(C.byref(_actions()), C.byref(n)) == OK and n.value == 0
+    wide = _actions((40, 700, 700, 3), ld_theta=700 * 41 + 700 * 701 + 3 * 701 + 1)
+    wide.ld_theta = (wide.ld_theta + 3) // 4 * 4
+    assert lib.evo_mlp_actions_bytes(C.byref(wide), C.byref(n)) == OK and n.value == 2 * 100 * 700 * 4
+    assert lib.evo_mlp_actions(C.byref(wide), FAR * 8, n.value - 1, None) == WORKSPACE
+    assert lib.evo_mlp_actions(C.byref(wide), None, n.value, None) == INVALID
+    for bad in (dict(struct_size=4), dict(members=0), dict(n_layers=0), dict(n_layers=9), dict(ld_theta=384), dict(ld_theta=387),
+                dict(action_scale=float("nan")), dict(offsets_64=7), dict(rows=1 << 41)):
+        assert lib.evo_mlp_actions_bytes(C.byref(_actions(**bad)), C.byref(n)) == INVALID, bad
+    for bad in (dict(d_theta=None), dict(d_theta=FAR + 8), dict(d_observations=None), dict(d_observations=2 * FAR + 2), dict(d_offsets=None),
+                dict(d_actions=None), dict(ld_observations=4), dict(d_actions=FAR), dict(d_actions=2 * FAR + 4), dict(d_actions=3 * FAR)):
+        assert lib.evo_mlp_actions(C.byref(_actions(**bad)), None, 0, None) == INVALID, bad
+    assert lib.evo_mlp_actions(C.byref(_actions(rows=0, d_actions=None)), None, 0, None) == OK
+    assert lib.evo_mlp_actions_bytes(C.byref(_actions((5, 0, 1))), C.byref(n)) == INVALID
