@@ -58,7 +58,7 @@ enum { EVO_TASK_NONE = 0, EVO_TASK_CARTPOLE = 1, EVO_TASK_TANH_LINEAR = 2, EVO_T
  * of one to four hidden layers of up to 128 units in registers (but where only some of the layers are wide
  * and the population large), those of any other policy in shared memory as long as they fit; else GENERIC. */
 enum { EVO_ROLLOUT_AUTO = 0, EVO_ROLLOUT_GENERIC = 1, EVO_ROLLOUT_TILED = 2 };
-enum { EVO_OPT_ADAM = 0, EVO_OPT_CLIPUP = 1 };
+enum { EVO_OPT_ADAM = 0, EVO_OPT_CLIPUP = 1, EVO_OPT_MUON = 2 };
 enum { EVO_SIGMA_CONSTANT = 0, EVO_SIGMA_PGPE = 1 };
 /* evo_config.debug_flags.  DROP_COMPLETION: the roll-out kernels leave out the asynchronous
  * completion their first bounded wait depends on (the copy of a member's parameters; in the
@@ -111,6 +111,12 @@ typedef struct evo_config {
     uint32_t wait_cycles_log2;     /* a device-side wait gives up after 2^n SM clocks and raises
                                       EVO_ERR_TIMEOUT; 0 selects 31 (about a second), else 10..40 */
     uint32_t debug_flags;          /* EVO_DEBUG_* bits, 0 in production                          */
+    uint32_t reserved;             /* not read                                                   */
+    /* (a configuration that ends here, struct_size included, is taken too: all below is 0 then) */
+    float    muon_momentum;        /* Muon: 0 selects 0.95                                        */
+    float    muon_weight_decay;    /* Muon: >= 0                                                  */
+    uint32_t muon_steps;           /* Muon: Newton-Schulz steps, 0 selects 5, at most 64          */
+    uint32_t muon_plain_momentum;  /* Muon: 1: without Nesterov's look-ahead                      */
 } evo_config;
 
 /* Bytes of device workspace a solver with this configuration needs.  Pure host function. */
@@ -166,6 +172,8 @@ evo_status evo_rollout(evo_solver* s, const float* d_theta, float* d_fitness, fl
  * optimizer = EVO_OPT_CLIPUP replaces the Adam lines by ClipUp (the optimiser the paper's PGPE
  * reference pairs it with, Section 5): vel = momentum vel + lr g/|g|; if |vel| > max_speed it is
  * scaled back to that length; center += vel (vel lives in the first-moment buffer).
+ * optimizer = EVO_OPT_MUON takes the step of evo_muon_step (below) with the weight matrices of the policy (MLP, CNN or
+ * LSTM; with task NONE an MLP whose layer_sizes make param_dim) and Adam's constants for the biases.
  * sigma_mode = EVO_SIGMA_PGPE also adapts sigma (PGPE with symmetric sampling, Section 5):
  *   gs[d] = (sigma[d]/H) * sum_j ((u[2j] + u[2j+1])/2) * (eps[j][d]^2 - 1)
  *   sigma[d] += sigma_lr * gs[d], limited to a relative change of +-sigma_max_change per tell.
@@ -349,7 +357,8 @@ typedef struct evo_muon {
  * with the same decay, `step` being the number of this step from 1 on:
  *   m' = b1 m + (1 - b1) g;  v' = b2 v + (1 - b2) g^2
  *   center' = (1 - lr weight_decay) center + lr (m' / (1 - b1^step)) / (sqrt(v' / (1 - b2^step)) + adam_eps)
- * Each output may be its own input; otherwise the outputs must not overlap anything.
+ * Each output may be its own input; otherwise the outputs must not overlap anything.  The evo_tell of a solver
+ * with EVO_OPT_MUON takes this step.
  * Errors: INVALID_ARG, WORKSPACE, UNSUPPORTED (as above), CUDA.
  */
 evo_status evo_muon_bytes(const evo_matrix* list, uint32_t n, uint64_t param_dim, size_t* bytes);

@@ -40,6 +40,8 @@ class EvoConfig(C.Structure):
         ("sigma_mode", C.c_uint32), ("sigma_lr", C.c_float), ("sigma_max_change", C.c_float),
         ("shard_first_pair", C.c_uint32), ("shard_pairs", C.c_uint32),
         ("wait_cycles_log2", C.c_uint32), ("debug_flags", C.c_uint32),
+        ("reserved", C.c_uint32), ("muon_momentum", C.c_float), ("muon_weight_decay", C.c_float), ("muon_steps", C.c_uint32),
+        ("muon_plain_momentum", C.c_uint32),
     ]
 
 
@@ -173,6 +175,8 @@ def make_config(w: W.Workload, *, trace_steps: int = 0, rollout_kernel: int = RO
     for i, v in enumerate(w.task_param):
         c.task_param[i] = v
     c.optimizer, c.clipup_momentum, c.clipup_max_speed = w.optimizer, w.clipup_momentum, w.clipup_max_speed
+    c.muon_momentum, c.muon_weight_decay, c.muon_steps = w.muon_momentum, w.muon_weight_decay, w.muon_steps
+    c.muon_plain_momentum = 1 if w.muon_plain_momentum else 0
     c.sigma_mode, c.sigma_lr, c.sigma_max_change = w.sigma_mode, w.sigma_lr, w.sigma_max_change
     c.shard_first_pair, c.shard_pairs = shard_first_pair, shard_pairs
     c.wait_cycles_log2, c.debug_flags = wait_cycles_log2, debug_flags

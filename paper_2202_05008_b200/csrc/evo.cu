@@ -2,6 +2,7 @@
 // kernel launches.  No device memory is allocated here; nothing synchronises except
 // evo_sync_status / evo_get_counters.
 #include "internal.h"
+#include "matrix_ops.h"
 
 #include <cmath>
 #include <cstring>
@@ -27,15 +28,51 @@ struct evo_solver {
     uint32_t     k0, k1;
     S2sSplit     s2s;              // how the queries of a seq2seq roll-out are split
     bool         deep;             // the control policy runs on k_rollout_mlp_deep
+    evo_matrix   matrices[EVO_MAX_LAYERS];   // Muon: the policy's weight matrices
+    uint32_t     n_matrices;
     bool         rollout_prepared;  // per-kernel attributes are set by the solver's first roll-out only
 };
 
 static size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 constexpr int kCanaryByte = 0xA5;
 
+// The configuration as it was before Muon's fields were added to its end
+constexpr size_t kFirstConfigBytes = offsetof(evo_config, muon_momentum);
+static_assert(kFirstConfigBytes % alignof(evo_config) == 0, "the first configuration had no padding at its end");
+static bool read_config(const evo_config* in, evo_config* out)
+{
+    std::memset(out, 0, sizeof(*out));
+    if (!in || (in->struct_size != sizeof(evo_config) && in->struct_size != kFirstConfigBytes)) return false;
+    std::memcpy(out, in, in->struct_size);
+    out->struct_size = sizeof(evo_config);
+    return true;
+}
+
+// Muon needs the weight matrices of the policy, which tasks check; without a task the layers have to make the parameter vector
+static evo_status check_muon(const evo_config* c)
+{
+    if (!(c->muon_momentum >= 0.f && c->muon_momentum < 1.f) || !(c->muon_weight_decay >= 0.f) || !std::isfinite(c->muon_weight_decay) ||
+        c->muon_steps > 64u || c->muon_plain_momentum > 1u)
+        return EVO_ERR_INVALID_ARG;
+    if (c->optimizer != EVO_OPT_MUON) return EVO_OK;
+    if (c->task_kind == EVO_TASK_NONE && c->policy_kind == EVO_POLICY_MLP) {
+        if (c->n_layers < 1u || c->n_layers > EVO_MAX_LAYERS) return EVO_ERR_INVALID_ARG;
+        uint64_t n = 0;
+        for (uint32_t l = 0; l < c->n_layers; ++l) {
+            const uint64_t in = c->layer_sizes[l], out = c->layer_sizes[l + 1];
+            if (in < 1u || out < 1u || in > (1u << 20) || out > (1u << 20)) return EVO_ERR_INVALID_ARG;
+            n += (in + 1u) * out;
+        }
+        if (n != c->param_dim) return EVO_ERR_INVALID_ARG;
+    } else if (c->task_kind == EVO_TASK_NONE || c->policy_kind == EVO_POLICY_NONE) {
+        return EVO_ERR_UNSUPPORTED;
+    }
+    return EVO_OK;
+}
+
 static evo_status check_config(const evo_config* c)
 {
-    if (!c || c->struct_size != sizeof(evo_config)) return EVO_ERR_INVALID_ARG;
+    if (!c) return EVO_ERR_INVALID_ARG;
     if (c->pop_size < 2 || (c->pop_size & 1u) || c->param_dim < 1) return EVO_ERR_INVALID_ARG;
     if (c->param_dim > kMaxParamDim) return EVO_ERR_INVALID_ARG;      // the row pitch must fit 32 bits
     if (!(c->sigma > 0.f) || !std::isfinite(c->sigma) || !std::isfinite(c->lr)) return EVO_ERR_INVALID_ARG;
@@ -43,7 +80,7 @@ static evo_status check_config(const evo_config* c)
     if (c->beta1 < 0.f || c->beta1 >= 1.f || c->beta2 < 0.f || c->beta2 >= 1.f || c->adam_eps < 0.f)
         return EVO_ERR_INVALID_ARG;
     if (c->rollout_kernel > EVO_ROLLOUT_TILED) return EVO_ERR_INVALID_ARG;
-    if (c->optimizer > EVO_OPT_CLIPUP || c->sigma_mode > EVO_SIGMA_PGPE) return EVO_ERR_INVALID_ARG;
+    if (c->optimizer > EVO_OPT_MUON || c->sigma_mode > EVO_SIGMA_PGPE) return EVO_ERR_INVALID_ARG;
     if (c->clipup_momentum < 0.f || c->clipup_momentum >= 1.f || c->clipup_max_speed < 0.f) return EVO_ERR_INVALID_ARG;
     if (c->sigma_lr < 0.f || c->sigma_max_change < 0.f || c->sigma_max_change >= 1.f) return EVO_ERR_INVALID_ARG;
     if (c->wait_cycles_log2 != 0 && (c->wait_cycles_log2 < 10 || c->wait_cycles_log2 > 40)) return EVO_ERR_INVALID_ARG;
@@ -92,7 +129,7 @@ static evo_status check_config(const evo_config* c)
         }
         default: return EVO_ERR_INVALID_ARG;
     }
-    return EVO_OK;
+    return check_muon(c);
 }
 
 static evo_status make_layout(const evo_config& c, Layout* L)
@@ -143,6 +180,13 @@ static evo_status make_layout(const evo_config& c, Layout* L)
         cnn = paint_scratch_bytes(static_cast<uint32_t>(Pl), static_cast<uint32_t>(c.task_param[EVO_PAINT_WIDTH]),
                                   static_cast<uint32_t>(c.task_param[EVO_PAINT_HEIGHT]));
     L->cnn_scratch = take(cnn);                                 // scratch of the single-step tasks
+    L->muon = 0;
+    if (c.optimizer == EVO_OPT_MUON) {
+        evo_matrix list[EVO_MAX_LAYERS];
+        const size_t bytes = muon_workspace_bytes(list, policy_matrices(c, list));
+        if (bytes == ~static_cast<size_t>(0)) return EVO_ERR_UNSUPPORTED;
+        L->muon = take(bytes);
+    }
     L->theta = take(row * Pl);
     L->eps = take(c.noise_mode == EVO_NOISE_STORED ? row * Hl : 0);
     L->total = off;
@@ -153,11 +197,13 @@ extern "C" {
 
 evo_status evo_workspace_bytes(const evo_config* cfg, size_t* bytes)
 {
-    if (!bytes) return EVO_ERR_INVALID_ARG;
-    evo_status st = check_config(cfg);
+    evo_config c;
+    if (!bytes || !read_config(cfg, &c)) return EVO_ERR_INVALID_ARG;
+    evo_status st = check_config(&c);
     if (st != EVO_OK) return st;
     Layout L;
-    make_layout(*cfg, &L);
+    st = make_layout(c, &L);
+    if (st != EVO_OK) return st;
     *bytes = L.total;
     return EVO_OK;
 }
@@ -167,12 +213,14 @@ evo_status evo_create(const evo_config* cfg_in, void* d_workspace, size_t worksp
 {
     if (!out) return EVO_ERR_INVALID_ARG;
     *out = nullptr;
-    evo_status st = check_config(cfg_in);
+    evo_config c;
+    if (!read_config(cfg_in, &c)) return EVO_ERR_INVALID_ARG;
+    evo_status st = check_config(&c);
     if (st != EVO_OK) return st;
     if (!d_workspace || (reinterpret_cast<uintptr_t>(d_workspace) & 255u)) return EVO_ERR_INVALID_ARG;
     evo_solver* s = new (std::nothrow) evo_solver();
     if (!s) return EVO_ERR_INVALID_ARG;
-    s->cfg = *cfg_in;
+    s->cfg = c;
     if (s->cfg.beta1 == 0.f) s->cfg.beta1 = 0.9f;
     if (s->cfg.beta2 == 0.f) s->cfg.beta2 = 0.999f;
     if (s->cfg.adam_eps == 0.f) s->cfg.adam_eps = 1e-8f;
@@ -181,7 +229,11 @@ evo_status evo_create(const evo_config* cfg_in, void* d_workspace, size_t worksp
     if (s->cfg.sigma_lr == 0.f) s->cfg.sigma_lr = 0.1f;
     if (s->cfg.sigma_max_change == 0.f) s->cfg.sigma_max_change = 0.2f;
     if (s->cfg.wait_cycles_log2 == 0) s->cfg.wait_cycles_log2 = 31;       // ~1 s at 2 GHz
-    make_layout(s->cfg, &s->lay);
+    if (s->cfg.muon_momentum == 0.f) s->cfg.muon_momentum = 0.95f;
+    if (s->cfg.muon_steps == 0u) s->cfg.muon_steps = 5u;
+    st = make_layout(s->cfg, &s->lay);
+    if (st != EVO_OK) { delete s; return st; }
+    s->n_matrices = s->cfg.optimizer == EVO_OPT_MUON ? policy_matrices(s->cfg, s->matrices) : 0u;
     if (workspace_bytes < s->lay.total) { delete s; return EVO_ERR_WORKSPACE; }
     s->ws = static_cast<char*>(d_workspace);
     s->stream = static_cast<cudaStream_t>(cuda_stream);
@@ -375,6 +427,30 @@ static TellArgs tell_args(evo_solver* s, const float* d_fitness)
     return t;
 }
 
+// Muon's step from the gradient that the kernels of the tell have left (nothing for the other optimisers)
+static int muon_after_tell(evo_solver* s)
+{
+    const evo_config& c = s->cfg;
+    if (c.optimizer != EVO_OPT_MUON) return 0;
+    const Layout& L = s->lay;
+    MuonArgs a;
+    std::memset(&a, 0, sizeof(a));
+    a.center_out = reinterpret_cast<float*>(s->ws + L.center); a.center = a.center_out;
+    a.m_out = reinterpret_cast<float*>(s->ws + L.m); a.m = a.m_out;
+    a.v_out = reinterpret_cast<float*>(s->ws + L.v); a.v = a.v_out;
+    a.g = reinterpret_cast<const float*>(s->ws + L.g);
+    a.dim = c.param_dim;
+    DeviceStatus* const status = reinterpret_cast<DeviceStatus*>(s->ws + L.status);
+    a.d_step = &status->adam_step;                              // (advanced already)
+    a.skip = reinterpret_cast<const double*>(s->ws + L.norms);
+    a.lr = c.lr; a.mu = c.muon_momentum; a.decay = c.muon_weight_decay; a.beta1 = c.beta1; a.beta2 = c.beta2; a.adam_eps = c.adam_eps;
+    a.nesterov = c.muon_plain_momentum ? 0u : 1u; a.ns_steps = c.muon_steps;
+    a.a = kNsA; a.b = kNsB; a.c = kNsC; a.ns_eps = kNsEps;
+    a.work = s->ws + L.muon;
+    a.sticky = &status->sticky; a.wait_log2 = c.wait_cycles_log2;
+    return launch_muon(s->stream, s->matrices, s->n_matrices, a);
+}
+
 evo_status evo_tell(evo_solver* s, const float* d_fitness)
 {
     if (!s || !d_fitness) return EVO_ERR_INVALID_ARG;
@@ -383,6 +459,9 @@ evo_status evo_tell(evo_solver* s, const float* d_fitness)
     const int n = launch_gradient_update(s->stream, tell_args(s, d_fitness));
     if (n < 0) return EVO_ERR_CUDA;
     s->launches += n;
+    const int k = muon_after_tell(s);
+    if (k < 0) return EVO_ERR_CUDA;
+    s->launches += k;
     s->asked = false;
     s->generation += 1;
     return EVO_OK;
@@ -419,6 +498,9 @@ evo_status evo_tell_end(evo_solver* s)
                                           reinterpret_cast<float*>(s->ws + L.sigma_sum));
     if (n < 0) return EVO_ERR_CUDA;
     s->launches += n;
+    const int k = muon_after_tell(s);
+    if (k < 0) return EVO_ERR_CUDA;
+    s->launches += k;
     s->telling = false;
     s->asked = false;
     s->generation += 1;

@@ -81,7 +81,7 @@ struct RolloutMlpArgs {
 struct Layout {                  // byte offsets into the workspace
     size_t status, center, m, v, g, sigma, theta, eps, u, rank, grad_partial, sigma_partial, grad_sum,
            sigma_sum, norms, counters,
-           fit_partial, task_const, cnn_scratch, total;
+           fit_partial, task_const, cnn_scratch, muon, total;
     uint32_t ldD, grad_splits, n_eb, EB;
     size_t canary[kMaxRegions];  // checked build: offset of the guard words behind each region, in layout order
     int    n_canaries;
@@ -105,7 +105,7 @@ struct TellArgs {
     uint32_t pair0, P;            // first global pair of the shard; global population size
     double* partial;              // [splits][ldD] fp64 partial sums of the centre gradient
     float*  sigma_partial;        // [splits][ldD] fp32 partial sums of the sigma gradient, or NULL
-    double* norms;                // scratch for ClipUp's two vector norms
+    double* norms;                // scratch for ClipUp's two vector norms; Muon: whether to take the step
     float*  sigma_vec;            // [ldD]
     float   lr, beta1, beta2, adam_eps;
     uint32_t optimizer;

@@ -153,9 +153,11 @@ static std::vector<ns::Matrix> muon_list(const evo_matrix* list, size_t n, doubl
 }
 
 size_t muon_workspace_bytes(const evo_matrix* list, size_t n)
-{
+try {
     const std::vector<ns::Matrix> m = muon_list(list, n, 0.0);
     return ns::workspace_bytes(m.data(), m.size());
+} catch (const std::bad_alloc&) {
+    return ~static_cast<size_t>(0);
 }
 
 bool muon_scalars(const MuonArgs& a, ns::Scalars* s)
@@ -167,7 +169,7 @@ bool muon_scalars(const MuonArgs& a, ns::Scalars* s)
 }
 
 int launch_muon(cudaStream_t st, const evo_matrix* list, size_t n, const MuonArgs& a)
-{
+try {
     ns::Args args;
     std::memset(&args, 0, sizeof(args));
     if (!muon_scalars(a, &args.s)) return -1;
@@ -202,18 +204,20 @@ int launch_muon(cudaStream_t st, const evo_matrix* list, size_t n, const MuonArg
         ++launches;
     }
     return launches;
+} catch (const std::bad_alloc&) {
+    return -1;
 }
 
-std::vector<evo_matrix> policy_matrices(const evo_config& c)
+uint32_t policy_matrices(const evo_config& c, evo_matrix (&out)[EVO_MAX_LAYERS])
 {
-    std::vector<evo_matrix> out;
     uint64_t at = 0;
+    uint32_t n = 0;
     auto layer = [&](uint32_t rows, uint32_t cols, uint32_t bias) {
-        out.push_back(evo_matrix{ at, rows, cols });
+        out[n++] = evo_matrix{ at, rows, cols };
         at += static_cast<uint64_t>(rows) * cols + bias;
     };
     if (c.policy_kind == EVO_POLICY_MLP) {
-        for (uint32_t l = 0; l < c.n_layers; ++l) layer(c.layer_sizes[l + 1], c.layer_sizes[l], c.layer_sizes[l + 1]);
+        for (uint32_t l = 0; l < c.n_layers && l < EVO_MAX_LAYERS; ++l) layer(c.layer_sizes[l + 1], c.layer_sizes[l], c.layer_sizes[l + 1]);
     } else if (c.policy_kind == EVO_POLICY_CNN_28) {
         layer(8, 25, 8);
         layer(16, 200, 16);
@@ -226,7 +230,7 @@ std::vector<evo_matrix> policy_matrices(const evo_config& c)
         }
         layer(12, h, 12);
     }
-    return out;
+    return n;
 }
 
 }  // namespace evo
@@ -235,7 +239,7 @@ using namespace evo;
 
 static bool default_ns(const evo_newton_schulz* in, evo_newton_schulz* out)
 {
-    *out = evo_newton_schulz{ sizeof(evo_newton_schulz), 5u, 3.4445f, -4.7750f, 2.0315f, 1e-7f };
+    *out = evo_newton_schulz{ sizeof(evo_newton_schulz), 5u, kNsA, kNsB, kNsC, kNsEps };
     if (!in) return true;
     if (in->struct_size != sizeof(evo_newton_schulz)) return false;
     if (in->steps) out->steps = in->steps;
@@ -319,13 +323,9 @@ evo_status evo_muon_bytes(const evo_matrix* list, uint32_t n, uint64_t param_dim
     if (!bytes) return EVO_ERR_INVALID_ARG;
     const evo_status st = check_list(list, n, param_dim);
     if (st != EVO_OK) return st;
-    try {
-        const size_t need = muon_workspace_bytes(list, n);
-        if (need == ~static_cast<size_t>(0)) return EVO_ERR_UNSUPPORTED;
-        *bytes = need;
-    } catch (const std::bad_alloc&) {
-        return EVO_ERR_INVALID_ARG;
-    }
+    const size_t need = muon_workspace_bytes(list, n);
+    if (need == ~static_cast<size_t>(0)) return EVO_ERR_UNSUPPORTED;
+    *bytes = need;
     return EVO_OK;
 }
 
@@ -364,11 +364,7 @@ evo_status evo_muon_step(const evo_muon* cfg, const evo_matrix* list, uint32_t n
     if (workspace_bytes < need) return EVO_ERR_WORKSPACE;
     a.center = d_center; a.m = d_m; a.v = d_v; a.g = d_gradient; a.center_out = d_center_out; a.m_out = d_m_out; a.v_out = d_v_out;
     a.dim = param_dim; a.step = step; a.work = static_cast<char*>(d_workspace); a.wait_log2 = 31u;
-    try {
-        return launch_muon(static_cast<cudaStream_t>(cuda_stream), list, n, a) < 0 ? EVO_ERR_CUDA : EVO_OK;
-    } catch (const std::bad_alloc&) {
-        return EVO_ERR_INVALID_ARG;
-    }
+    return launch_muon(static_cast<cudaStream_t>(cuda_stream), list, n, a) < 0 ? EVO_ERR_CUDA : EVO_OK;
 }
 
 }  // extern "C"

@@ -25,6 +25,9 @@ int launch(cudaStream_t st, uint32_t source, const Matrix* list, size_t n, const
 
 }  // namespace ns
 
+// the quintic and the eps that 0 selects
+constexpr float kNsA = 3.4445f, kNsB = -4.7750f, kNsC = 2.0315f, kNsEps = 1e-7f;
+
 struct MuonArgs {
     const float *center, *m, *v, *g;
     float *center_out, *m_out, *v_out;
@@ -42,7 +45,7 @@ struct MuonArgs {
 bool muon_scalars(const MuonArgs& a, ns::Scalars* s);       // false: an iteration that grows beyond fp16 pairs
 size_t muon_workspace_bytes(const evo_matrix* list, size_t n);
 int launch_muon(cudaStream_t st, const evo_matrix* list, size_t n, const MuonArgs& a);
-// weight matrices of a solver's policy inside its parameter vector
-std::vector<evo_matrix> policy_matrices(const evo_config& c);
+// weight matrices of a solver's policy inside its parameter vector; returns how many
+uint32_t policy_matrices(const evo_config& c, evo_matrix (&out)[EVO_MAX_LAYERS]);
 
 }  // namespace evo

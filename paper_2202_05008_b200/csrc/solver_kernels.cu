@@ -292,7 +292,7 @@ __device__ __forceinline__ double power(double b, uint32_t n)
     return r;
 }
 
-enum : uint32_t { kStepAdam = 0, kStepClipup = 1, kStepSums = 2 };
+enum : uint32_t { kStepAdam = 0, kStepClipup = 1, kStepSums = 2, kStepMuon = 3 };    // (kStepMuon: the gradient and sigma; the centre follows in kernels of its own)
 
 struct StepArgs {
     uint32_t mode, ldD;
@@ -349,7 +349,7 @@ __device__ __forceinline__ void quad_step(const StepArgs& a, uint32_t quad, cons
         reinterpret_cast<float4*>(a.v)[quad] = make_float4(vv[0], vv[1], vv[2], vv[3]);
         if (EVO_IN_BOUNDS(a.status, EVO_SITE_UPDATE, 4u * quad + 3u, a.ldD))
             reinterpret_cast<float4*>(a.center)[quad] = make_float4(cc[0], cc[1], cc[2], cc[3]);
-    } else {
+    } else if (a.mode == kStepClipup) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             dots[0] += static_cast<double>(mm[i]) * mm[i];
@@ -425,6 +425,8 @@ __device__ __forceinline__ void close_tell(const StepArgs& a, uint32_t n_blocks,
         }
     } else if (a.mode == kStepClipup && threadIdx.x == 0) {
         a.norms[3u * n_blocks + 2u] = 0.0;                   // the step is left out
+    } else if (a.mode == kStepMuon && threadIdx.x == 0) {
+        a.norms[0] = skip ? 0.0 : 1.0;
     }
     if (threadIdx.x == 0) {
         if (skip) {
@@ -773,9 +775,14 @@ static int launch_tell(cudaStream_t st, const TellArgs& a, uint32_t mode, double
     return launches;
 }
 
+static uint32_t step_mode(const TellArgs& a)
+{
+    return a.optimizer == EVO_OPT_ADAM ? kStepAdam : a.optimizer == EVO_OPT_MUON ? kStepMuon : kStepClipup;
+}
+
 int launch_gradient_update(cudaStream_t st, const TellArgs& a)
 {
-    return launch_tell(st, a, a.optimizer == EVO_OPT_ADAM ? kStepAdam : kStepClipup, nullptr, nullptr);
+    return launch_tell(st, a, step_mode(a), nullptr, nullptr);
 }
 
 int launch_gradient_sums(cudaStream_t st, const TellArgs& a, double* grad_sum, float* sigma_sum)
@@ -785,7 +792,7 @@ int launch_gradient_sums(cudaStream_t st, const TellArgs& a, double* grad_sum, f
 
 int launch_update_from_sums(cudaStream_t st, const TellArgs& a, double* grad_sum, float* sigma_sum)
 {
-    const uint32_t mode = a.optimizer == EVO_OPT_ADAM ? kStepAdam : kStepClipup;
+    const uint32_t mode = step_mode(a);
     const StepArgs s = step_args(a, mode, grad_sum, sigma_sum);
     const uint32_t nb = (a.ldD / 4u + 255u) / 256u;
     if (launch_dependent(k_step_from_sums, dim3(nb), dim3(256), 0, st, a.counters, a.sigma_partial != nullptr, s) != cudaSuccess) return -1;

@@ -51,13 +51,15 @@ def main(argv: Optional[List[str]] = None) -> None:
     ap.add_argument("--workload", default="cfg2", choices=sorted(W.CONFIGS))
     ap.add_argument("--generations", type=int, default=100)
     ap.add_argument("--log-every", type=int, default=10)
-    ap.add_argument("--clipup", action="store_true", help="ClipUp instead of Adam")
+    optimizer = ap.add_mutually_exclusive_group()
+    optimizer.add_argument("--clipup", action="store_true", help="ClipUp instead of Adam")
+    optimizer.add_argument("--muon", action="store_true", help="Muon instead of Adam")
     ap.add_argument("--adapt-sigma", action="store_true", help="PGPE sigma update")
     a = ap.parse_args(argv)
     w = W.CONFIGS[a.workload]
     if w.task_kind == W.TASK_NONE:
         raise SystemExit("this workload has no task to train on")
-    w = w.with_(optimizer=W.OPT_CLIPUP if a.clipup else W.OPT_ADAM,
+    w = w.with_(optimizer=W.OPT_CLIPUP if a.clipup else W.OPT_MUON if a.muon else W.OPT_ADAM,
                 sigma_mode=W.SIGMA_PGPE if a.adapt_sigma else W.SIGMA_CONSTANT)
     t0 = time.perf_counter()
     _, hist = run(w, a.generations, log_every=a.log_every)

@@ -15,7 +15,7 @@ import numpy as np
 NOISE_STORED, NOISE_REGENERATED = 0, 1
 POLICY_NONE, POLICY_MLP, POLICY_CNN_28, POLICY_LSTM_SEQ2SEQ = 0, 1, 2, 3
 TASK_NONE, TASK_CARTPOLE, TASK_TANH_LINEAR, TASK_SUPERVISED, TASK_SEQ2SEQ_ADD, TASK_PAINT = 0, 1, 2, 3, 4, 5
-OPT_ADAM, OPT_CLIPUP = 0, 1
+OPT_ADAM, OPT_CLIPUP, OPT_MUON = 0, 1, 2
 SIGMA_CONSTANT, SIGMA_PGPE = 0, 1
 
 CNN_PARAMS = 5994
@@ -46,6 +46,10 @@ class Workload:
     sigma_mode: int = SIGMA_CONSTANT
     sigma_lr: float = 0.0                 # 0 = library default (0.1)
     sigma_max_change: float = 0.0         # 0 = library default (0.2)
+    muon_momentum: float = 0.0            # 0 = library default (0.95)
+    muon_weight_decay: float = 0.0
+    muon_steps: int = 0                   # 0 = library default (5)
+    muon_plain_momentum: bool = False
 
     @property
     def env_steps_per_generation(self) -> int:

@@ -172,3 +172,29 @@ def test_actions_refusals(lib):
         assert lib.evo_mlp_actions(C.byref(_actions(**bad)), None, 0, None) == INVALID, bad
     assert lib.evo_mlp_actions(C.byref(_actions(rows=0, d_actions=None)), None, 0, None) == OK
     assert lib.evo_mlp_actions_bytes(C.byref(_actions((5, 0, 1))), C.byref(n)) == INVALID
+
+
+def test_a_configuration_without_the_fields_of_muon_is_still_taken(lib):
+    from paper_2202_05008_b200 import workloads as W
+    from paper_2202_05008_b200.binding import EvoConfig, make_config
+    first = EvoConfig.muon_momentum.offset
+    a, b = C.c_size_t(), C.c_size_t()
+    cfg = make_config(W.CFG4)
+    assert cfg.struct_size == C.sizeof(EvoConfig) and lib.evo_workspace_bytes(C.byref(cfg), C.byref(a)) == OK
+    cfg.struct_size, cfg.muon_momentum, cfg.muon_steps = first, 7.0, 1000        # what lies behind it is not read
+    assert lib.evo_workspace_bytes(C.byref(cfg), C.byref(b)) == OK and a.value == b.value
+    cfg.struct_size = first + 4
+    assert lib.evo_workspace_bytes(C.byref(cfg), C.byref(b)) == INVALID
+
+
+def test_muon_solvers_have_their_workspace(lib):
+    from paper_2202_05008_b200 import workloads as W
+    from paper_2202_05008_b200.binding import make_config
+    n, m = C.c_size_t(), C.c_size_t()
+    for w, large in ((W.CFG4, False), (W.CFG3, False), (W.SEQ2SEQ, True),
+                     (W.Workload("x", 4, 300 * 201 + 201 * 5, 1, policy_kind=W.POLICY_MLP, layer_sizes=(200, 300, 3)), True)):
+        w = w.with_(param_dim=W.mlp_param_count(w.layer_sizes)) if w.name == "x" else w
+        assert lib.evo_workspace_bytes(C.byref(make_config(w)), C.byref(n)) == OK
+        assert lib.evo_workspace_bytes(C.byref(make_config(w.with_(optimizer=W.OPT_MUON))), C.byref(m)) == OK
+        assert (m.value > n.value) == large, w.name
+    assert lib.evo_workspace_bytes(C.byref(make_config(W.CFG5.with_(optimizer=W.OPT_MUON))), C.byref(m)) == UNSUPPORTED
