@@ -31,7 +31,7 @@ static bool gather_large(const Matrix* list, size_t n, size_t* at, Args* a, size
     uint64_t blocks = 0, pairs = 0, tiles = 0, matrices = 0;
     size_t off = 0;
     a->groups = 0;
-    for (; *at < n && a->groups < kMaxGroups; ++*at) {
+    for (; *at < n && a->groups < kMaxLarge; ++*at) {
         if (small(list[*at])) continue;
         Group g = group_for(list[*at], false);
         const uint64_t rows = g.mp / kTile;

@@ -21,6 +21,7 @@ constexpr float kCut = 5.7e-8f;
 enum Source : uint32_t { kF32 = 0, kBf16 = 1, kF16 = 2, kMuon = 3 };
 
 constexpr uint32_t kMaxGroups = 32;      // groups of a launch; longer lists take several
+constexpr uint32_t kMaxLarge = 16;       // ... of large matrices (each comes with its tensor maps)
 constexpr uint32_t kTile = 128;          // rows and columns of a tile of the kernels for large matrices
 constexpr uint32_t kPieceCols = 64;      // columns of a piece of the kernels that read the matrix (128 rows)
 

@@ -2,10 +2,12 @@
 //
 // k_ns_norm sums the squares of pieces of 128 x 64 elements, k_ns_split writes X in panels (zero in the padding, and so is all
 // that is made of it), k_ns_gemm<kGram / kPoly / kApply> is one of the three products of a step.  A block of k_ns_gemm walks over
-// 128 x 128 tiles: a warp copies operands into a ring of three stages (64 of the contracted index: two pairs of 128 x 64
-// matrices, 64 KB, every panel's run one bulk copy), a thread issues the MMAs, and eight warps take the sums out of tensor memory and
+// 128 x 128 tiles: a thread copies operands into a ring of three stages (64 of the contracted index: two pairs of 128 x 64
+// matrices, 64 KB in four TMA boxes of 8 runs of 2 KB or 16 of 1 KB), another issues the MMAs, and eight warps take the sums out of tensor memory and
 // turn them into fp16 pairs while the next ones are under way (two sets of accumulators).  A and B are symmetric: tiles on
 // and under the diagonal only, written twice.
+#include <cuda.h>
+
 #include "newton_schulz.cuh"
 
 namespace evo {
@@ -136,15 +138,18 @@ __device__ __forceinline__ Tile tile_at(const Args& a, uint32_t at)
     return t;
 }
 
-// bytes from global to shared memory; the arrival with the expected number of them is made elsewhere
-__device__ __forceinline__ void copy_run(uint32_t dst, const char* src, uint32_t bytes, uint32_t bar)
+// A box of a buffer's panels to shared memory: runs of a panel (8-byte elements), panels, matrix of the group
+__device__ __forceinline__ void copy_box(uint32_t dst, const CUtensorMap* map, uint32_t row, uint32_t panel, uint32_t which, uint32_t bar)
 {
-    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                 :: "r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+    asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+                 :: "r"(dst), "l"(map), "r"(bar), "r"(2u * row), "r"(panel), "r"(which) : "memory");
 }
 
+// The operands of a product: kGram: X, kPoly: A (the same for both); kApply: B and X
+struct Maps { CUtensorMap first[kMaxLarge], second[kMaxLarge]; };
+
 template <uint32_t MODE, uint32_t SRC>
-__global__ void __launch_bounds__(kGemmThreads, 1) k_ns_gemm(const __grid_constant__ Args a, uint32_t step)
+__global__ void __launch_bounds__(kGemmThreads, 1) k_ns_gemm(const __grid_constant__ Args a, const __grid_constant__ Maps maps, uint32_t step)
 {
     const uint32_t cur = step & 1u;                              // which of the two X buffers holds X
     const bool last = step + 1u == a.s.steps;
@@ -176,29 +181,25 @@ __global__ void __launch_bounds__(kGemmThreads, 1) k_ns_gemm(const __grid_consta
         uint32_t stage = 0, phase = 0, filled = 0;
         for (uint32_t at = blockIdx.x; at < total; at += gridDim.x) {
             const Tile t = tile_at<MODE>(a, at);
-            const Group& g = *t.g;
-            const size_t half = static_cast<size_t>(g.mp) * (MODE == kGram ? g.np : g.mp) * 2u, x_half = static_cast<size_t>(g.mp) * g.np * 2u;
-            const char* const p = buffer(a, g, t.which, MODE == kGram ? cur : MODE == kPoly ? 2u : 3u);
-            const char* const x = buffer(a, g, t.which, cur);
-            const uint32_t panels = MODE == kApply ? min(16u, g.np / 8u - t.j0 / 8u) : 8u;
-            const bool twice = MODE != kApply && t.i0 != t.j0;
-            const uint32_t bytes = 2u * kOperand + (MODE == kApply ? panels * 2048u : twice ? 2u * kOperand : 0u);
+            const uint32_t gi = static_cast<uint32_t>(t.g - a.g), lo = (MODE == kGram ? t.g->np : t.g->mp) / 8u, x_lo = t.g->np / 8u;
+            const bool twice = MODE == kApply || t.i0 != t.j0;
             for (uint32_t k = 0; k < t.k; k += 64u) {
                 waits.wait(smem_u32(&empty[stage]), phase ^ 1u);
                 if (__any_sync(0xffffffffu, abort_flag)) break;
-                const uint32_t bar = smem_u32(&full[stage]), to = smem_u32(smem) + stage * kStage;
-                if (lane == 0) asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" :: "r"(bar), "r"(bytes) : "memory");
-                __syncwarp();
-                const uint32_t c = lane & 7u, lo = lane >> 3 & 1u;
-                const size_t run = (static_cast<size_t>(k / 8u + c) * g.mp) * 16u + lo * half;
-                if (lane < 16u) copy_run(to + lo * kOperand + c * 2048u, p + run + t.i0 * 16u, 2048u, bar);
-                if constexpr (MODE == kApply) {                 // 64 rows of X by up to 16 panels
-                    const uint32_t c2 = lane & 15u, lo2 = lane >> 4;
-                    if (c2 < panels)
-                        copy_run(to + (2u + lo2) * kOperand + c2 * 1024u, x + (static_cast<size_t>(t.j0 / 8u + c2) * g.mp + k) * 16u + lo2 * x_half, 1024u, bar);
-                } else if (twice && lane >= 16u) {
-                    copy_run(to + (2u + lo) * kOperand + c * 2048u, p + run + t.j0 * 16u, 2048u, bar);
+                if (lane == 0) {
+                    const uint32_t bar = smem_u32(&full[stage]), to = smem_u32(smem) + stage * kStage;
+                    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" :: "r"(bar), "r"(twice ? kStage : kStage / 2u) : "memory");
+                    copy_box(to, &maps.first[gi], t.i0, k / 8u, t.which, bar);
+                    copy_box(to + kOperand, &maps.first[gi], t.i0, k / 8u + lo, t.which, bar);
+                    if constexpr (MODE == kApply) {             // 64 rows of X by 16 panels (those beyond the last are not looked at)
+                        copy_box(to + 2u * kOperand, &maps.second[gi], k, t.j0 / 8u, t.which, bar);
+                        copy_box(to + 3u * kOperand, &maps.second[gi], k, t.j0 / 8u + x_lo, t.which, bar);
+                    } else if (twice) {
+                        copy_box(to + 2u * kOperand, &maps.first[gi], t.j0, k / 8u, t.which, bar);
+                        copy_box(to + 3u * kOperand, &maps.first[gi], t.j0, k / 8u + lo, t.which, bar);
+                    }
                 }
+                __syncwarp();
                 ++filled;
                 if (++stage == kStages) { stage = 0; phase ^= 1u; }
             }
@@ -369,6 +370,29 @@ __global__ void __launch_bounds__(kGemmThreads, 1) k_ns_gemm(const __grid_consta
     }
 }
 
+typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+static EncodeTiled encoder()
+{
+    static std::atomic<void*> known{ nullptr };
+    void* f = known.load(std::memory_order_relaxed);
+    if (!f) {
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess) return nullptr;
+        known.store(f, std::memory_order_relaxed);
+    }
+    return reinterpret_cast<EncodeTiled>(f);
+}
+
+// boxes of `rows` x `panels` of a buffer (high and low parts: twice cols / 8 panels) of all matrices of a group
+static bool encode(EncodeTiled f, CUtensorMap* map, char* base, const Group& g, uint32_t cols, uint32_t rows, uint32_t panels)
+{
+    const cuuint64_t dims[3] = { 2ull * g.mp, cols / 4u, g.count }, strides[2] = { 16ull * g.mp, large_bytes(g.mp, g.np) };
+    const cuuint32_t box[3] = { 2u * rows, panels, 1u }, steps[3] = { 1u, 1u, 1u };
+    return f(map, CU_TENSOR_MAP_DATA_TYPE_INT64, 3, base, dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE,
+             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <uint32_t SRC>
 static int launch_list(cudaStream_t st, const Args& a)
 {
@@ -377,15 +401,27 @@ static int launch_list(cudaStream_t st, const Args& a)
                                reinterpret_cast<const void*>(k_ns_gemm<kApply, SRC>) };
     for (const void* k : kernels)
         if (cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kGemmSmem) != cudaSuccess) return -1;
+    const EncodeTiled f = encoder();
+    if (!f) return -1;
+    Maps gram[2], poly, apply[2];
+    for (uint32_t i = 0; i < a.groups; ++i) {
+        const Group& g = a.g[i];
+        const size_t x = x_bytes(g.mp, g.np), q = a_bytes(g.mp);
+        char* const base = a.work + g.work;
+        bool ok = encode(f, &poly.first[i], base + 2u * x, g, g.mp, kTile, 8u) && encode(f, &apply[0].first[i], base + 2u * x + q, g, g.mp, kTile, 8u);
+        for (uint32_t b = 0; ok && b < 2u; ++b)
+            ok = encode(f, &gram[b].first[i], base + b * x, g, g.np, kTile, 8u) && encode(f, &apply[b].second[i], base + b * x, g, g.np, 64u, 16u);
+        if (!ok) return -1;
+        apply[1].first[i] = apply[0].first[i];
+    }
     if (launch_dependent(k_ns_norm<SRC>, dim3(a.blocks), dim3(256), 0, st, a) != cudaSuccess) return -1;
     if (launch_dependent(k_ns_split<SRC>, dim3(a.blocks), dim3(256), 0, st, a) != cudaSuccess) return -1;
     const dim3 pairs(a.pairs < kSms ? a.pairs : kSms), tiles(a.tiles < kSms ? a.tiles : kSms);
-    for (uint32_t step = 0; step < a.s.steps; ++step) {
-        if (launch_dependent(k_ns_gemm<kGram, kF32>, pairs, dim3(kGemmThreads), kGemmSmem, st, a, step) != cudaSuccess ||
-            launch_dependent(k_ns_gemm<kPoly, kF32>, pairs, dim3(kGemmThreads), kGemmSmem, st, a, step) != cudaSuccess ||
-            launch_dependent(k_ns_gemm<kApply, SRC>, tiles, dim3(kGemmThreads), kGemmSmem, st, a, step) != cudaSuccess)
+    for (uint32_t step = 0; step < a.s.steps; ++step)
+        if (launch_dependent(k_ns_gemm<kGram, kF32>, pairs, dim3(kGemmThreads), kGemmSmem, st, a, gram[step & 1u], step) != cudaSuccess ||
+            launch_dependent(k_ns_gemm<kPoly, kF32>, pairs, dim3(kGemmThreads), kGemmSmem, st, a, poly, step) != cudaSuccess ||
+            launch_dependent(k_ns_gemm<kApply, SRC>, tiles, dim3(kGemmThreads), kGemmSmem, st, a, apply[step & 1u], step) != cudaSuccess)
             return -1;
-    }
     return 2 + 3 * static_cast<int>(a.s.steps);
 }
 
