@@ -231,6 +231,7 @@ int launch_type(cudaStream_t st, const GroupedArgs& a)
 
 int launch_grouped(cudaStream_t st, uint32_t type, const GroupedArgs& a)
 {
+    if (grouped_tc_takes(type, a)) return launch_grouped_tc(st, type, a);
     return type == EVO_F32 ? launch_type<float>(st, a) : type == EVO_BF16 ? launch_type<__nv_bfloat16>(st, a) : launch_type<__half>(st, a);
 }
 

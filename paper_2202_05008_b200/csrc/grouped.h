@@ -33,5 +33,8 @@ __device__ __forceinline__ void group_rows(const GroupedArgs& a, uint32_t g, uin
 }
 
 int launch_grouped(cudaStream_t st, uint32_t type, const GroupedArgs& a);
+// grouped_tc.cu: 16-bit types whose rows TMA can address
+bool grouped_tc_takes(uint32_t type, const GroupedArgs& a);
+int launch_grouped_tc(cudaStream_t st, uint32_t type, const GroupedArgs& a);
 
 }  // namespace evo

@@ -1,0 +1,265 @@
+// Products grouped by member of 16-bit operands on tcgen05: y[r] = scale act(W_g x[r] + b_g).
+//
+// The weights are the MMA's first operand, 128 outputs, and a group's rows the second, as many as it has (16 .. 256 a tile): a group
+// of one row costs one pass over its weights and hardly any tensor time, a long one runs at the tensor core's pace, and no row
+// count is padded beyond 16.  Blocks stay and walk over (group, row tile, 128 outputs), the outputs of a row tile side by side, so
+// that its rows are read from L2.  A thread copies 64 of the contracted index a stage by TMA (weights 128 x 64, rows in boxes of 32), another
+// issues the MMAs, eight warps take the sums of one tile out of tensor memory while the next tile's are under way.
+#include <type_traits>
+
+#include "grouped.h"
+#include "grouped_mma.cuh"
+#include "tma.h"
+#include "umma.cuh"
+
+namespace evo {
+namespace {
+
+constexpr uint32_t kStages = 4;
+constexpr uint32_t kMostRows = 256;                          // of a tile
+constexpr uint32_t kBox = 32;                                // rows of a copy
+constexpr uint32_t kWBytes = 128u * 128u, kXBytes = kMostRows * 128u;
+constexpr uint32_t kSmem = kStages * (kWBytes + kXBytes) + 1024u;
+constexpr uint32_t kThreads = 320;
+
+struct TcArgs {
+    GroupedArgs g;
+    CUtensorMap w, x;
+    uint32_t out_tiles, shared_w;                            // shared_w: one set of weights for all groups
+};
+
+// K-major operand of rows of 128 bytes with the 128-byte swizzle, groups of 8 rows side by side
+__device__ __forceinline__ uint64_t desc_sw128(uint32_t addr)
+{
+    return static_cast<uint64_t>((addr & 0x3FFFFu) >> 4) | static_cast<uint64_t>(1) << 16 | static_cast<uint64_t>(64) << 32 |
+           static_cast<uint64_t>(1) << 46 | static_cast<uint64_t>(2) << 61;
+}
+template <typename T>
+__device__ __forceinline__ uint32_t idesc(uint32_t n)
+{
+    const uint32_t type = std::is_same<T, __half>::value ? 0u : 1u;
+    return (1u << 4) | (type << 7) | (type << 10) | ((n >> 3) << 17) | ((128u >> 4) << 24);
+}
+
+__device__ __forceinline__ void copy2(uint32_t dst, const CUtensorMap* map, uint32_t c0, uint32_t c1, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+                 :: "r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1) : "memory");
+}
+__device__ __forceinline__ void copy3(uint32_t dst, const CUtensorMap* map, uint32_t c0, uint32_t c1, uint32_t c2, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+                 :: "r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2) : "memory");
+}
+
+// Walks a warp over the tiles of all groups.  Row tiles of a group: as few as can be, equal up to 16 rows.
+struct Walk {
+    uint32_t base = 0;                                       // groups [base, base + 32): a lane each
+    uint64_t before = 0, first = 0, end = 0;                 // row tiles of earlier groups; the lane's rows
+    uint32_t tiles = 0, upto = 0;                            // the lane's row tiles, and the running sum
+
+    __device__ __forceinline__ void fill(const GroupedArgs& a)
+    {
+        const uint32_t lane = threadIdx.x & 31u;
+        first = end = 0;
+        if (base + lane < a.groups) group_rows(a, base + lane, &first, &end);
+        tiles = static_cast<uint32_t>((end - first + kMostRows - 1u) / kMostRows);
+        upto = tiles;
+#pragma unroll
+        for (uint32_t d = 1; d < 32u; d <<= 1) {
+            const uint32_t v = __shfl_up_sync(0xffffffffu, upto, d);
+            if (lane >= d) upto += v;
+        }
+    }
+    // row tile `at`: its group, first row and rows; false behind the last
+    __device__ __forceinline__ bool find(const GroupedArgs& a, uint64_t at, uint32_t* group, uint64_t* row, uint32_t* rows)
+    {
+        for (;;) {
+            const uint32_t here = __shfl_sync(0xffffffffu, upto, 31);
+            if (at - before < here) break;
+            before += here;
+            base += 32u;
+            if (base >= a.groups) return false;
+            fill(a);
+        }
+        const uint32_t local = static_cast<uint32_t>(at - before);
+        const uint32_t lane = __ffs(__ballot_sync(0xffffffffu, upto > local)) - 1;
+        const uint32_t n = __shfl_sync(0xffffffffu, tiles, lane), nth = local - (__shfl_sync(0xffffffffu, upto, lane) - n);
+        const uint64_t f = __shfl_sync(0xffffffffu, first, lane), e = __shfl_sync(0xffffffffu, end, lane);
+        const uint64_t per = ((e - f + n - 1u) / n + 15u) / 16u * 16u;        // (n tiles of `per` may be one too many: then the last has no rows)
+        *group = base + lane;
+        *row = f + nth * per;
+        *rows = *row >= e ? 0u : static_cast<uint32_t>(min(per, e - *row));
+        return true;
+    }
+};
+
+template <typename T>
+__global__ void __launch_bounds__(kThreads, 1) k_grouped_tc(const __grid_constant__ TcArgs p)
+{
+    extern __shared__ uint8_t raw[];
+    __shared__ __align__(8) uint64_t full[kStages], empty[kStages], done[2], taken[2], drain;
+    __shared__ uint32_t slot, limit;
+    __shared__ volatile int abort_flag;
+    const GroupedArgs& a = p.g;
+    const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31u;
+    const uint32_t smem = (smem_u32(raw) + 1023u) / 1024u * 1024u;
+    if (tid == 0) {
+        for (uint32_t s = 0; s < kStages; ++s) { mbar_init(smem_u32(&full[s]), 1); mbar_init(smem_u32(&empty[s]), 1); }
+        for (uint32_t b = 0; b < 2u; ++b) { mbar_init(smem_u32(&done[b]), 1); mbar_init(smem_u32(&taken[b]), 8); }
+        mbar_init(smem_u32(&drain), 1);
+        mbar_init_fence();
+        limit = 31u;
+        abort_flag = 0;
+    }
+    dep_wait();
+    dep_trigger();
+    if (warp == 1) tmem_alloc(smem_u32(&slot), 512);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = slot, steps = (a.n_in + 63u) / 64u;
+    auto wait = [&](uint64_t* bar, uint32_t parity) {
+        if (mbar_try_wait(smem_u32(bar), parity) || abort_flag) return;
+        if (!mbar_wait_bounded(smem_u32(bar), parity, &limit)) abort_flag = 1;
+    };
+    auto aborted = [&] { return __any_sync(0xffffffffu, abort_flag) != 0; };
+    Walk walk;
+    walk.fill(a);
+    uint32_t group, rows, stage = 0, phase = 0, acc = 0, acc_phase = 0, filled = 0;
+    uint64_t row;
+
+    if (warp == 0) {
+        for (uint64_t at = blockIdx.x; walk.find(a, at / p.out_tiles, &group, &row, &rows); at += gridDim.x) {
+            if (rows == 0u) continue;
+            const uint32_t o0 = static_cast<uint32_t>(at % p.out_tiles) * 128u, boxes = (rows + kBox - 1u) / kBox;
+            for (uint32_t k = 0; k < steps; ++k) {
+                wait(&empty[stage], phase ^ 1u);
+                if (aborted()) break;
+                if (lane == 0) {
+                    const uint32_t bar = smem_u32(&full[stage]), to = smem + stage * (kWBytes + kXBytes);
+                    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" :: "r"(bar), "r"(kWBytes + boxes * kBox * 128u) : "memory");
+                    copy3(to, &p.w, k * 64u, o0, p.shared_w ? 0u : group, bar);
+                    for (uint32_t b = 0; b < boxes; ++b) copy2(to + kWBytes + b * kBox * 128u, &p.x, k * 64u, static_cast<uint32_t>(row) + b * kBox, bar);
+                }
+                __syncwarp();
+                ++filled;
+                if (++stage == kStages) { stage = 0; phase ^= 1u; }
+            }
+            if (aborted()) break;
+        }
+        if (aborted())                                       // nothing may land after the block has gone
+            for (uint32_t s = 0; s < min(filled, kStages); ++s) {
+                const uint32_t nth = filled - 1u - s;
+                mbar_wait_bounded(smem_u32(&full[nth % kStages]), nth / kStages & 1u, &limit);
+            }
+    } else if (warp == 1) {
+        for (uint64_t at = blockIdx.x; walk.find(a, at / p.out_tiles, &group, &row, &rows); at += gridDim.x) {
+            if (rows == 0u) continue;
+            const uint32_t d = tmem + acc * kMostRows, id = idesc<T>((rows + 15u) / 16u * 16u);
+            wait(&taken[acc], acc_phase ^ 1u);
+            for (uint32_t k = 0; k < steps; ++k) {
+                wait(&full[stage], phase);
+                tc_fence_after();
+                if (aborted()) break;
+                if (lane == 0) {
+                    const uint32_t w = smem + stage * (kWBytes + kXBytes);
+#pragma unroll
+                    for (uint32_t s = 0; s < 4u; ++s) umma_bf16(d, desc_sw128(w + s * 32u), desc_sw128(w + kWBytes + s * 32u), id, k + s != 0u);
+                    umma_commit(smem_u32(&empty[stage]));
+                    if (k + 1u == steps) umma_commit(smem_u32(&done[acc]));
+                }
+                __syncwarp();
+                if (++stage == kStages) { stage = 0; phase ^= 1u; }
+            }
+            if (aborted()) break;
+            acc ^= 1u;
+            if (acc == 0u) acc_phase ^= 1u;
+        }
+        if (aborted()) {                                     // nor may an MMA write after its tensor memory is freed
+            if (lane == 0) umma_commit(smem_u32(&drain));
+            __syncwarp();
+            mbar_wait_bounded(smem_u32(&drain), 0u, &limit);
+        }
+    } else {
+        const uint32_t quarter = warp & 3u, half = (warp - 2u) >> 2;
+        for (uint64_t at = blockIdx.x; walk.find(a, at / p.out_tiles, &group, &row, &rows); at += gridDim.x) {
+            if (rows == 0u) continue;
+            const uint32_t o = static_cast<uint32_t>(at % p.out_tiles) * 128u + quarter * 32u + lane;
+            const bool live = o < a.n_out;
+            float bias = 0.f;
+            if (a.b && live) {
+                const T b = static_cast<const T*>(a.b)[group * a.stride_b + o];
+                if constexpr (std::is_same<T, __half>::value) bias = __half2float(b); else bias = __bfloat162float(b);
+            }
+            T* const y = static_cast<T*>(a.y) + row * a.ld_y + o;
+            wait(&done[acc], acc_phase);
+            tc_fence_after();
+            // the halves take every other 32 rows
+            for (uint32_t c = half * 32u; c < rows; c += 64u) {
+                uint32_t u[4][8];
+                tmem_ld32_issue(tmem + acc * kMostRows + (quarter << 21) + c, u);
+                tmem_ld8x4_fence(u[0], u[1], u[2], u[3]);
+                if (live)
+#pragma unroll
+                    for (uint32_t i = 0; i < 32u; ++i)
+                        if (c + i < rows) {
+                            float v = __uint_as_float(u[i / 8u][i % 8u]) + bias;
+                            if (a.activation == EVO_ACT_TANH) v = tanhf(v);
+                            if (a.activation == EVO_ACT_RELU) v = v < 0.f ? 0.f : v;
+                            v = abort_flag ? __int_as_float(0x7FC00000) : a.scale * v;
+                            if constexpr (std::is_same<T, __half>::value) y[(c + i) * a.ld_y] = __float2half_rn(v);
+                            else y[(c + i) * a.ld_y] = __float2bfloat16_rn(v);
+                        }
+                __syncwarp();
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&taken[acc]));
+            acc ^= 1u;
+            if (acc == 0u) acc_phase ^= 1u;
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        tc_fence_after();
+        tmem_dealloc(tmem, 512);
+    }
+}
+
+}  // namespace
+
+bool grouped_tc_takes(uint32_t type, const GroupedArgs& a)
+{
+    if (type == EVO_F32 || ((reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.w)) & 15u)) return false;
+    if ((a.ld_x | a.ld_w | a.stride_w) & 7u) return false;
+    return a.rows < (1ull << 31) && a.ld_x < (1ull << 38) && a.ld_w < (1ull << 38) && a.stride_w < (1ull << 38);
+}
+
+int launch_grouped_tc(cudaStream_t st, uint32_t type, const GroupedArgs& a)
+{
+    const EncodeTiled f = tensor_map_encoder();
+    if (!f) return -1;
+    TcArgs p;
+    p.g = a;
+    p.out_tiles = (a.n_out + 127u) / 128u;
+    p.shared_w = a.groups > 1u && a.stride_w == 0u;
+    const CUtensorMapDataType t = type == EVO_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+    // (a pitch of 0 is one that is never taken: any valid one stands in for it)
+    const uint64_t own = (a.n_in + 7ull) / 8ull * 8ull;
+    const cuuint64_t wd[3] = { a.n_in, a.n_out, p.shared_w ? 1u : a.groups }, ws[2] = { 2u * (a.ld_w ? a.ld_w : own), 2u * (a.stride_w ? a.stride_w : own) };
+    const cuuint64_t xd[2] = { a.n_in, a.rows }, xs[1] = { 2u * (a.ld_x ? a.ld_x : own) };
+    const cuuint32_t wb[3] = { 64u, 128u, 1u }, xb[2] = { 64u, kBox }, one[3] = { 1u, 1u, 1u };
+    if (f(&p.w, t, 3, const_cast<void*>(a.w), wd, ws, wb, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+          CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS ||
+        f(&p.x, t, 2, const_cast<void*>(a.x), xd, xs, xb, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+          CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+        return -1;
+    const uint64_t used = a.rows < a.groups ? a.rows : a.groups, most = (a.rows / kMostRows + used) * p.out_tiles;
+    auto kernel = type == EVO_F16 ? k_grouped_tc<__half> : k_grouped_tc<__nv_bfloat16>;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) != cudaSuccess) return -1;
+    return launch_dependent(kernel, dim3(most < kSms ? static_cast<uint32_t>(most) : kSms), dim3(kThreads), kSmem, st, p) == cudaSuccess ? 1 : -1;
+}
+
+}  // namespace evo

@@ -6,9 +6,8 @@
 // matrices, 64 KB in four TMA boxes of 8 runs of 2 KB or 16 of 1 KB), another issues the MMAs, and eight warps take the sums out of tensor memory and
 // turn them into fp16 pairs while the next ones are under way (two sets of accumulators).  A and B are symmetric: tiles on
 // and under the diagonal only, written twice.
-#include <cuda.h>
-
 #include "newton_schulz.cuh"
+#include "tma.h"
 
 namespace evo {
 namespace ns {
@@ -370,20 +369,6 @@ __global__ void __launch_bounds__(kGemmThreads, 1) k_ns_gemm(const __grid_consta
     }
 }
 
-typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
-                                const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-static EncodeTiled encoder()
-{
-    static std::atomic<void*> known{ nullptr };
-    void* f = known.load(std::memory_order_relaxed);
-    if (!f) {
-        cudaDriverEntryPointQueryResult found;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess) return nullptr;
-        known.store(f, std::memory_order_relaxed);
-    }
-    return reinterpret_cast<EncodeTiled>(f);
-}
-
 // boxes of `rows` x `panels` of a buffer (high and low parts: twice cols / 8 panels) of all matrices of a group
 static bool encode(EncodeTiled f, CUtensorMap* map, char* base, const Group& g, uint32_t cols, uint32_t rows, uint32_t panels)
 {
@@ -401,7 +386,7 @@ static int launch_list(cudaStream_t st, const Args& a)
                                reinterpret_cast<const void*>(k_ns_gemm<kApply, SRC>) };
     for (const void* k : kernels)
         if (cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kGemmSmem) != cudaSuccess) return -1;
-    const EncodeTiled f = encoder();
+    const EncodeTiled f = tensor_map_encoder();
     if (!f) return -1;
     Maps gram[2], poly, apply[2];
     for (uint32_t i = 0; i < a.groups; ++i) {
