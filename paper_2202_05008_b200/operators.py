@@ -7,6 +7,7 @@ take raise ``EvoError``; there is no fallback.
 from __future__ import annotations
 
 import ctypes as C
+from functools import lru_cache
 from typing import Optional, Sequence, Tuple
 
 import torch
@@ -26,34 +27,63 @@ def _require(condition: bool, where: str, what: str) -> None:
         raise error
 
 
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)      # the handle without a Stream object (2 us)
+
+
 class _On:
-    """The tensors' device, and the stream the call goes to, as the current ones (allocations belong to that stream)."""
+    """The tensors' device, and the stream the call goes to, as the current ones (allocations belong to that stream).  Entering
+    gives the stream's handle; nothing is switched where both are current already (6 us of a small call)."""
+    __slots__ = ("device", "stream", "guard")
 
     def __init__(self, device: torch.device, stream: Optional[torch.cuda.Stream]):
-        self.guard = torch.cuda.device(device) if stream is None else torch.cuda.stream(stream)
-        self.device = device
-        self.stream = stream
+        self.device, self.stream, self.guard = device, stream, None
 
     def __enter__(self) -> int:
-        self.guard.__enter__()
-        return (self.stream if self.stream is not None else torch.cuda.current_stream(self.device)).cuda_stream
+        if self.stream is not None:
+            self.guard = torch.cuda.stream(self.stream)
+        elif self.device.index != torch.cuda.current_device():
+            self.guard = torch.cuda.device(self.device)
+        if self.guard is not None:
+            self.guard.__enter__()
+        if self.stream is not None:
+            return self.stream.cuda_stream
+        return _raw_stream(self.device.index) if _raw_stream else torch.cuda.current_stream(self.device).cuda_stream
 
     def __exit__(self, *exc):
-        return self.guard.__exit__(*exc)
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
 
 
-def _newton_schulz(steps: int, coefficients: Sequence[float], eps: float, where: str) -> NewtonSchulz:
+@lru_cache(maxsize=256)
+def _newton_schulz(steps: int, coefficients: Tuple[float, ...], eps: float, where: str) -> NewtonSchulz:
     _require(1 <= steps <= 64 and len(coefficients) == 3 and any(coefficients) and eps > 0, where, "steps, coefficients or eps")
     return NewtonSchulz(C.sizeof(NewtonSchulz), steps, *coefficients, eps)
 
 
-def _matrices(x: torch.Tensor) -> Matrices:
-    batched = x.dim() == 3
-    rows, cols = x.shape[-2:]
+@lru_cache(maxsize=1024)
+def _orthogonalize_bytes(batch: int, rows: int, cols: int) -> int:
+    need = C.c_size_t()
+    _check(load_library().evo_orthogonalize_bytes(batch, rows, cols, C.byref(need)), "orthogonalize")
+    return need.value
+
+
+@lru_cache(maxsize=256)
+def _matrix_list(matrices: Tuple[Tuple[int, int, int], ...], dim: int):
+    """(array of evo_matrix, how many, bytes of workspace)"""
+    where = "muon_step"
+    _require(all(o >= 0 and 1 <= r <= 1 << 20 and 1 <= c <= 1 << 20 for o, r, c in matrices), where, "matrices are (offset, rows, cols)")
+    n = len(matrices)
+    items, need = (Matrix * max(n, 1))(*(Matrix(o, r, c) for o, r, c in matrices)), C.c_size_t()
+    _check(load_library().evo_muon_bytes(items, n, dim, C.byref(need)), where)
+    return items, n, need.value
+
+
+def _matrices(x: torch.Tensor, shape, strides) -> Matrices:
+    rows, cols = shape[-2:]
     # a stride that is never taken may be anything
-    row_stride = x.stride(-2) if rows > 1 else cols
-    batch = x.shape[0] if batched else 1
-    return Matrices(x.data_ptr(), TYPES[x.dtype], batch, rows, cols, x.stride(0) if batch > 1 else rows * row_stride, row_stride)
+    row_stride = strides[-2] if rows > 1 else cols
+    batch = shape[0] if len(shape) == 3 else 1
+    return Matrices(x.data_ptr(), TYPES[x.dtype], batch, rows, cols, strides[0] if batch > 1 else rows * row_stride, row_stride)
 
 
 def orthogonalize(x: torch.Tensor, out: Optional[torch.Tensor] = None, *, steps: int = 5,
@@ -64,19 +94,21 @@ def orthogonalize(x: torch.Tensor, out: Optional[torch.Tensor] = None, *, steps:
     lib, where = load_library(), "orthogonalize"
     _require(x.is_cuda and x.dtype in TYPES and x.dim() in (2, 3), where, "a fp32, bf16 or fp16 matrix or batch on a GPU")
     _require(x.shape[-1] == 1 or x.stride(-1) == 1, where, "the columns of x need unit stride")
-    with _On(x.device, stream) as st:
+    ns = _newton_schulz(steps, tuple(coefficients), eps, where)
+    shape, device = x.shape, x.device
+    with _On(device, stream) as st:
         if out is None:
-            out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        _require(out.device == x.device and out.dtype == x.dtype and out.shape == x.shape, where, "out must match x")
-        _require(out.shape[-1] == 1 or out.stride(-1) == 1, where, "the columns of out need unit stride")
-        if x.numel() == 0:
+            out = torch.empty(shape, dtype=x.dtype, device=device)
+        else:
+            _require(out.device == device and out.dtype == x.dtype and out.shape == shape, where, "out must match x")
+            _require(shape[-1] == 1 or out.stride(-1) == 1, where, "the columns of out need unit stride")
+        if 0 in shape:
             return out
-        ns = _newton_schulz(steps, coefficients, eps, where)
-        a, b, need = _matrices(x), _matrices(out), C.c_size_t()
-        _check(lib.evo_orthogonalize_bytes(a.batch, a.rows, a.cols, C.byref(need)), where)
-        work = torch.empty(need.value, dtype=torch.uint8, device=x.device) if need.value else None
-        _check(lib.evo_orthogonalize(C.byref(ns), C.byref(a), C.byref(b), None if work is None else work.data_ptr(), need.value, st),
-               where)
+        a, b = _matrices(x, shape, x.stride()), _matrices(out, shape, out.stride())
+        need = _orthogonalize_bytes(a.batch, a.rows, a.cols)
+        work = torch.empty(need, dtype=torch.uint8, device=device) if need else None
+        code = lib.evo_orthogonalize(C.byref(ns), C.byref(a), C.byref(b), None if work is None else work.data_ptr(), need, st)
+    _check(code, where)
     return out
 
 
@@ -94,40 +126,38 @@ def muon_step(center: torch.Tensor, m: torch.Tensor, v: torch.Tensor, gradient: 
     for x in vectors:
         _require(x.is_cuda and x.device == center.device and x.dtype == torch.float32 and x.dim() == 1 and x.is_contiguous() and
                  x.numel() == center.numel(), where, "contiguous fp32 vectors of one length on one GPU")
-    ns = _newton_schulz(ns_steps, coefficients, eps, where)
+    ns = _newton_schulz(ns_steps, tuple(coefficients), eps, where)
     cfg = Muon(C.sizeof(Muon), 0 if nesterov else 1, lr, momentum, weight_decay, beta1, beta2, adam_eps, ns)
-    _require(all(o >= 0 and 1 <= r <= 1 << 20 and 1 <= c <= 1 << 20 for o, r, c in matrices) and step >= 1, where,
-             "matrices are (offset, rows, cols), the step counts from 1")
-    n, dim = len(matrices), center.numel()
-    items = (Matrix * max(n, 1))(*(Matrix(o, r, c) for o, r, c in matrices))
+    _require(step >= 1, where, "the step counts from 1")
+    dim = center.numel()
+    items, n, need = _matrix_list(tuple(map(tuple, matrices)), dim)
     with _On(center.device, stream) as st:
         if out is None:
             out = (torch.empty_like(center), torch.empty_like(m), torch.empty_like(v))
         if dim == 0:
             return tuple(out)
-        need = C.c_size_t()
-        _check(lib.evo_muon_bytes(items, n, dim, C.byref(need)), where)
-        work = torch.empty(need.value, dtype=torch.uint8, device=center.device) if need.value else None
-        _check(lib.evo_muon_step(C.byref(cfg), items, n, dim, step, center.data_ptr(), m.data_ptr(), v.data_ptr(),
-                                 gradient.data_ptr(), out[0].data_ptr(), out[1].data_ptr(), out[2].data_ptr(),
-                                 None if work is None else work.data_ptr(), need.value, st), where)
+        work = torch.empty(need, dtype=torch.uint8, device=center.device) if need else None
+        code = lib.evo_muon_step(C.byref(cfg), items, n, dim, step, center.data_ptr(), m.data_ptr(), v.data_ptr(), gradient.data_ptr(),
+                                 out[0].data_ptr(), out[1].data_ptr(), out[2].data_ptr(), None if work is None else work.data_ptr(), need, st)
+    _check(code, where)
     return tuple(out)
 
 
-def _rows(x: torch.Tensor, dtype: torch.dtype, like: torch.Tensor) -> bool:
-    return x.is_cuda and x.device == like.device and x.dtype == dtype and x.dim() == 2 and (x.shape[1] <= 1 or x.stride(1) == 1)
+def _rows(x: torch.Tensor, dtype: torch.dtype, device: torch.device) -> bool:
+    return x.device == device and x.dtype == dtype and x.dim() == 2 and (x.stride(1) == 1 or x.shape[1] <= 1)
 
 
-def _ragged(offsets: torch.Tensor, groups: int, like: torch.Tensor, where: str) -> int:
-    _require(offsets.device == like.device and offsets.dtype in (torch.int32, torch.int64) and offsets.dim() == 1 and
-             offsets.numel() == groups + 1 and offsets.is_contiguous(), where, "offsets: int32 or int64 on the same GPU, one more than groups")
-    return 1 if offsets.dtype == torch.int64 else 0
+def _ragged(offsets: torch.Tensor, groups: int, device: torch.device, where: str) -> int:
+    dtype = offsets.dtype
+    _require(offsets.device == device and (dtype == torch.int32 or dtype == torch.int64) and offsets.shape == (groups + 1,) and
+             offsets.is_contiguous(), where, "offsets: int32 or int64 on the same GPU, one more than groups")
+    return 1 if dtype == torch.int64 else 0
 
 
-def _out(out: Optional[torch.Tensor], x: torch.Tensor, cols: int, where: str) -> torch.Tensor:
+def _out(out: Optional[torch.Tensor], x: torch.Tensor, rows: int, cols: int, where: str) -> torch.Tensor:
     if out is None:
-        return torch.empty(x.shape[0], cols, dtype=x.dtype, device=x.device)
-    _require(_rows(out, x.dtype, x) and out.shape == (x.shape[0], cols), where, "out does not match")
+        return torch.empty((rows, cols), dtype=x.dtype, device=x.device)
+    _require(_rows(out, x.dtype, x.device) and out.shape == (rows, cols), where, "out does not match")
     return out
 
 
@@ -138,24 +168,34 @@ def grouped_linear(x: torch.Tensor, weight: torch.Tensor, offsets: torch.Tensor,
     x [rows, n_in], weight [groups, n_out, n_in], bias [groups, n_out]; fp32, bf16 or fp16; unit stride in the last dimension, any
     other strides (a layer of theta is ``theta[:, a:b].unflatten(1, (n_out, n_in))``; an expanded weight is shared).  Rows outside all
     groups are left as they are in ``out``, and undefined without one."""
-    lib, where = load_library(), "grouped_linear"
-    _require(x.is_cuda and x.dtype in TYPES and _rows(x, x.dtype, x), where, "x: fp32, bf16 or fp16 rows on a GPU")
-    _require(weight.device == x.device and weight.dtype == x.dtype and weight.dim() == 3 and weight.shape[0] >= 1 and
-             weight.shape[2] == x.shape[1] and (weight.shape[2] <= 1 or weight.stride(2) == 1), where, "weight does not match x")
+    lib, where, device, dtype = load_library(), "grouped_linear", x.device, x.dtype
+    _require(x.is_cuda and dtype in TYPES and _rows(x, dtype, device), where, "x: fp32, bf16 or fp16 rows on a GPU")
+    _require(weight.device == device and weight.dtype == dtype and weight.dim() == 3, where, "weight does not match x")
     groups, n_out, n_in = weight.shape
-    _require(n_out >= 1 and n_in >= 1 and activation in ACTIVATIONS, where, "sizes or activation")
-    _require(weight.stride(0) >= 0 and weight.stride(1) >= 0, where, "weight strides")
+    rows = x.shape[0]
+    stride, pitch, one = weight.stride()
+    _require(groups >= 1 and n_out >= 1 and n_in >= 1 and n_in == x.shape[1] and (n_in == 1 or one == 1) and stride >= 0 and pitch >= 0, where,
+             "weight does not match x")
+    _require(activation in ACTIVATIONS, where, "activation")
     if bias is not None:
-        _require(_rows(bias, x.dtype, x) and bias.shape == (groups, n_out) and (n_out == 1 or bias.stride(1) == 1), where, "bias does not match")
-    wide = _ragged(offsets, groups, x, where)
-    with _On(x.device, stream) as st:
-        y = _out(out, x, n_out, where)
-        p = Grouped(C.sizeof(Grouped), TYPES[x.dtype], groups, n_in, n_out, ACTIVATIONS[activation], scale, wide, x.shape[0],
-                    x.data_ptr(), x.stride(0), weight.data_ptr(), weight.stride(1) if n_out > 1 else n_in, weight.stride(0),
+        _require(_rows(bias, dtype, device) and bias.shape == (groups, n_out), where, "bias does not match")
+    wide = _ragged(offsets, groups, device, where)
+    with _On(device, stream) as st:
+        y = _out(out, x, rows, n_out, where)
+        p = Grouped(C.sizeof(Grouped), TYPES[dtype], groups, n_in, n_out, ACTIVATIONS[activation], scale, wide, rows,
+                    x.data_ptr(), x.stride(0), weight.data_ptr(), pitch if n_out > 1 else n_in, stride,
                     None if bias is None else bias.data_ptr(), 0 if bias is None else bias.stride(0), offsets.data_ptr(), y.data_ptr(),
                     y.stride(0))
-        _check(lib.evo_grouped_linear(C.byref(p), st), where)
+        code = lib.evo_grouped_linear(C.byref(p), st)
+    _check(code, where)
     return y
+
+
+@lru_cache(maxsize=256)
+def _layers(sizes: Tuple[int, ...]):
+    """(parameters, the widths as evo_actions has them)"""
+    _require(2 <= len(sizes) <= EVO_MAX_LAYERS + 1 and min(sizes) >= 1 and max(sizes) <= 1 << 20, "mlp_actions", "layer_sizes")
+    return sum((a + 1) * b for a, b in zip(sizes[:-1], sizes[1:])), (C.c_uint32 * (EVO_MAX_LAYERS + 1))(*sizes)
 
 
 def mlp_actions(theta: torch.Tensor, layer_sizes: Sequence[int], observations: torch.Tensor, offsets: torch.Tensor, *,
@@ -164,23 +204,22 @@ def mlp_actions(theta: torch.Tensor, layer_sizes: Sequence[int], observations: t
     """``evo_mlp_actions``: the MLP policy's actions for rows of observations, ``offsets[m] <= r < offsets[m + 1]`` being member m's.
     theta [members, >= parameters] fp32 as ``Solver.ask`` returns it (row pitch a multiple of 4, rows 16-byte aligned),
     layer_sizes the widths, input first.  Rows without a member are left as they are in ``out``, and undefined without one."""
-    lib, where = load_library(), "mlp_actions"
+    lib, where, device = load_library(), "mlp_actions", observations.device
     sizes = tuple(layer_sizes)
-    _require(2 <= len(sizes) <= EVO_MAX_LAYERS + 1 and min(sizes) >= 1, where, "layer_sizes")
-    _require(observations.is_cuda and _rows(observations, torch.float32, observations) and observations.shape[1] == sizes[0], where,
+    dim, widths = _layers(sizes)
+    _require(observations.is_cuda and _rows(observations, torch.float32, device) and observations.shape[1] == sizes[0], where,
              "observations: fp32 rows of the first layer's width on a GPU")
-    dim = sum((a + 1) * b for a, b in zip(sizes[:-1], sizes[1:]))
-    _require(_rows(theta, torch.float32, observations) and theta.shape[0] >= 1 and theta.shape[1] >= dim, where, "theta does not match")
-    members = theta.shape[0]
-    wide = _ragged(offsets, members, observations, where)
-    with _On(observations.device, stream) as st:
-        y = _out(out, observations, sizes[-1], where)
+    members, rows = theta.shape[0], observations.shape[0]
+    _require(_rows(theta, torch.float32, device) and members >= 1 and theta.shape[1] >= dim, where, "theta does not match")
+    wide = _ragged(offsets, members, device, where)
+    with _On(device, stream) as st:
+        y = _out(out, observations, rows, sizes[-1], where)
         pitch = theta.stride(0) if members > 1 else -(-max(dim, theta.stride(0)) // 4) * 4
-        p = Actions(C.sizeof(Actions), members, len(sizes) - 1, (C.c_uint32 * (EVO_MAX_LAYERS + 1))(*sizes), action_scale, wide,
-                    observations.shape[0], theta.data_ptr(), pitch, observations.data_ptr(), observations.stride(0), offsets.data_ptr(),
-                    y.data_ptr(), y.stride(0))
+        p = Actions(C.sizeof(Actions), members, len(sizes) - 1, widths, action_scale, wide, rows, theta.data_ptr(), pitch,
+                    observations.data_ptr(), observations.stride(0), offsets.data_ptr(), y.data_ptr(), y.stride(0))
         need = C.c_size_t()
         _check(lib.evo_mlp_actions_bytes(C.byref(p), C.byref(need)), where)
-        work = torch.empty(need.value, dtype=torch.uint8, device=observations.device) if need.value else None
-        _check(lib.evo_mlp_actions(C.byref(p), None if work is None else work.data_ptr(), need.value, st), where)
+        work = torch.empty(need.value, dtype=torch.uint8, device=device) if need.value else None
+        code = lib.evo_mlp_actions(C.byref(p), None if work is None else work.data_ptr(), need.value, st)
+    _check(code, where)
     return y
