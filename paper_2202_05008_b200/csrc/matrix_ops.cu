@@ -10,20 +10,21 @@ namespace ns {
 
 static uint32_t up(uint32_t x, uint32_t a) { return (x + a - 1u) / a * a; }
 
-static Group group_for(const Matrix& x, bool small)
+// blocks: of the cluster that takes a small matrix, 0: a large one
+static Group group_for(const Matrix& x, uint32_t blocks)
 {
     Group g = {};
     g.in = x.in; g.out = x.out; g.in_stride = x.in_stride; g.out_stride = x.out_stride; g.in_ld = x.in_ld; g.out_ld = x.out_ld;
     g.tall = x.rows > x.cols;
     g.m = g.tall ? x.cols : x.rows;
     g.n = g.tall ? x.rows : x.cols;
-    g.mp = up(g.m, small ? 16u : kTile);
-    g.np = up(g.n, small ? 16u : kPieceCols);
+    g.mp = up(g.m, blocks ? 16u : kTile);
+    g.np = blocks ? up((g.n + blocks - 1u) / blocks, 16u) : up(g.n, kPieceCols);
     g.count = x.count;
     g.gain = x.gain;
     return g;
 }
-static bool small(const Matrix& x) { return is_small(std::min(x.rows, x.cols), std::max(x.rows, x.cols)); }
+static uint32_t blocks_of(const Matrix& x) { return small_blocks(std::min(x.rows, x.cols), std::max(x.rows, x.cols)); }
 
 // Lists the large matrices from *at on, as many as a launch takes; advances *at.  False where their numbers do not fit 32 bits.
 static bool gather_large(const Matrix* list, size_t n, size_t* at, Args* a, size_t* bytes)
@@ -32,8 +33,8 @@ static bool gather_large(const Matrix* list, size_t n, size_t* at, Args* a, size
     size_t off = 0;
     a->groups = 0;
     for (; *at < n && a->groups < kMaxLarge; ++*at) {
-        if (small(list[*at])) continue;
-        Group g = group_for(list[*at], false);
+        if (blocks_of(list[*at])) continue;
+        Group g = group_for(list[*at], 0u);
         const uint64_t rows = g.mp / kTile;
         g.first_block = static_cast<uint32_t>(blocks); g.first_pair = static_cast<uint32_t>(pairs); g.first_tile = static_cast<uint32_t>(tiles);
         g.work = off;
@@ -68,25 +69,27 @@ int launch(cudaStream_t st, uint32_t source, const Matrix* list, size_t n, const
 {
     int launches = 0;
     Args a = base;
-    for (size_t at = 0; at < n;) {
-        uint64_t blocks = 0;
-        size_t smem = 0;
-        a.groups = 0;
-        for (; at < n && a.groups < kMaxGroups; ++at) {
-            if (!small(list[at])) continue;
-            Group g = group_for(list[at], true);
-            g.first_block = static_cast<uint32_t>(blocks);
-            blocks += g.count;
-            if (blocks > 0x7FFFFFFFu) return -1;
-            smem = std::max(smem, small_bytes(g.mp, g.np));
-            a.g[a.groups++] = g;
+    for (uint32_t cluster = kMostBlocks; cluster; cluster /= 2u)
+        for (size_t at = 0; at < n;) {
+            uint64_t blocks = 0;
+            size_t smem = 0;
+            a.groups = 0;
+            a.cluster = cluster;
+            for (; at < n && a.groups < kMaxGroups; ++at) {
+                if (blocks_of(list[at]) != cluster) continue;
+                Group g = group_for(list[at], cluster);
+                g.first_block = static_cast<uint32_t>(blocks);
+                blocks += g.count;
+                if (blocks * cluster > 0x7FFFFFFFu) return -1;
+                smem = std::max(smem, small_bytes(g.mp, g.np, cluster));
+                a.g[a.groups++] = g;
+            }
+            a.blocks = static_cast<uint32_t>(blocks);
+            if (a.groups == 0u) continue;
+            const int k = launch_small(st, source, a, smem);
+            if (k < 0) return -1;
+            launches += k;
         }
-        a.blocks = static_cast<uint32_t>(blocks);
-        if (a.groups == 0u) continue;
-        const int k = launch_small(st, source, a, smem);
-        if (k < 0) return -1;
-        launches += k;
-    }
     for (size_t at = 0; at < n;) {
         size_t bytes = 0;
         if (!gather_large(list, n, &at, &a, &bytes)) return -1;

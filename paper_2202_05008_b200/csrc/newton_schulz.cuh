@@ -76,6 +76,43 @@ __device__ __forceinline__ void store(const Args& a, uint64_t at, float x, float
     if constexpr (SRC == kMuon) static_cast<float*>(a.out)[at] = fmaf(gain, x, a.s.keep * a.c_in[at]);
 }
 
+// Eight elements from `at` on, `step` apart, of which `count` exist (the others are 0); what Muon updates on the way is updated.
+template <uint32_t SRC>
+__device__ __forceinline__ void load8(const Args& a, uint64_t at, uint32_t step, uint32_t count, float (&x)[8])
+{
+    if constexpr (SRC == kF32) {
+        const float* const p = static_cast<const float*>(a.in) + at;
+        if (step == 1u && count == 8u && (reinterpret_cast<uintptr_t>(p) & 15u) == 0u) {
+            const float4 u = *reinterpret_cast<const float4*>(p), v = *reinterpret_cast<const float4*>(p + 4);
+            x[0] = u.x; x[1] = u.y; x[2] = u.z; x[3] = u.w; x[4] = v.x; x[5] = v.y; x[6] = v.z; x[7] = v.w;
+            return;
+        }
+    }
+#pragma unroll
+    for (uint32_t e = 0; e < 8u; ++e) {
+        float momentum = 0.f;
+        x[e] = e < count ? load<SRC>(a, at + static_cast<uint64_t>(e) * step, &momentum) : 0.f;
+        if constexpr (SRC == kMuon)
+            if (e < count) store_moments(a, at + static_cast<uint64_t>(e) * step, momentum);
+    }
+}
+// four neighbouring elements of the result, of which `count` (or more) exist
+template <uint32_t SRC>
+__device__ __forceinline__ void store4(const Args& a, uint64_t at, const float4& v, uint32_t count, float gain)
+{
+    if constexpr (SRC == kF32) {
+        float* const p = static_cast<float*>(a.out) + at;
+        if (count >= 4u && (reinterpret_cast<uintptr_t>(p) & 15u) == 0u) {
+            *reinterpret_cast<float4*>(p) = v;
+            return;
+        }
+    }
+    const float x[4] = { v.x, v.y, v.z, v.w };
+#pragma unroll
+    for (uint32_t e = 0; e < 4u; ++e)
+        if (e < count) store<SRC>(a, at + e, x[e], gain);
+}
+
 // element (i, j) of the m x n matrix in the source or the result
 __device__ __forceinline__ uint64_t in_index(const Group& g, uint32_t which, uint32_t i, uint32_t j)
 {
@@ -106,14 +143,14 @@ __device__ __forceinline__ uint32_t lift_at(const Scalars& s, uint32_t first, ui
 }
 __device__ __forceinline__ float power_of_two(int e) { return __int_as_float(e < -126 ? 0 : (e + 127) << 23); }
 
-// x and y as pairs, packed
+// x and y as pairs, packed (the difference to the high part by an instruction that takes it as it is)
 __device__ __forceinline__ void split2(float x, float y, uint32_t& hi, uint32_t& lo)
 {
-    const __half2 h = __floats2half2_rn(x, y);
-    const float2 f = __half22float2(h);
-    const __half2 l = __floats2half2_rn(x - f.x, y - f.y);
-    hi = *reinterpret_cast<const uint32_t*>(&h);
-    lo = *reinterpret_cast<const uint32_t*>(&l);
+    float u, v;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(hi) : "f"(y), "f"(x));
+    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tadd.rn.f32.f16 %0, l, %3;\n\tadd.rn.f32.f16 %1, h, %4;\n\t}"
+        : "=f"(u), "=f"(v) : "r"(hi ^ 0x80008000u), "f"(x), "f"(y));
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(lo) : "f"(v), "f"(u));
 }
 __device__ __forceinline__ void split8(const float (&x)[8], uint4& hi, uint4& lo)
 {

@@ -32,7 +32,7 @@ struct Group {
     uint64_t in_stride, out_stride;      // ... and from one matrix to the next
     uint64_t work;                       // large: byte offset of the first matrix' buffers in the workspace
     uint32_t in_ld, out_ld;              // row pitches
-    uint32_t m, n, mp, np;               // m <= n, and what they are padded to (small: 16 and 16; large: 128 and 64)
+    uint32_t m, n, mp, np;               // m <= n, and what they are padded to (small: 16 and 16, np of a block's share; large: 128 and 64)
     uint32_t tall, count, first_matrix;
     uint32_t first_block;                // of this group among the blocks of the launch (small) or the pieces (large)
     uint32_t first_pair, first_tile;     // large: among the tiles on and under the diagonal, and among those of an m x n matrix
@@ -61,7 +61,7 @@ struct Args {
     uint32_t wait_log2;
     size_t partial_at, lift_at;          // byte offsets of the two in the workspace
     uint32_t* lift;                      // large: per matrix of the launch, see first_scale
-    uint32_t groups, blocks, pairs, tiles;
+    uint32_t groups, blocks, pairs, tiles, cluster;
     Scalars s;
     Group g[kMaxGroups];
 };
@@ -115,17 +115,23 @@ inline bool set_scales(Scalars* s)
     return true;
 }
 
-// The kernel for small matrices holds one in the shared memory of a block: X as a pair of fp16 matrices, and A or B as one
-// (with the rows that a product reads beyond the last).
-constexpr uint32_t kSmallRows = 128;
+// The kernel for small matrices: up to 128 rows, and 128 columns a block of a cluster of 1, 2, 4 or 8.
+constexpr uint32_t kSmallRows = 128, kSmallCols = 128, kMostBlocks = 8;
 constexpr size_t kSmallBytes = 200u * 1024u;
-inline size_t small_bytes(uint32_t mp, uint32_t np)
+// Shared memory of a block: X as a pair of fp16 matrices, A or B as one, the other blocks' parts of A, and what a product reads beyond the last row
+inline size_t small_bytes(uint32_t mp, uint32_t np, uint32_t blocks)
 {
-    return static_cast<size_t>(mp) * np * 4u + static_cast<size_t>(mp) * mp * 4u + 2048u;
+    const size_t eights = mp / 8u;
+    return static_cast<size_t>(mp) * np * 4u + static_cast<size_t>(mp) * mp * 4u +
+           (blocks > 1u ? (eights + blocks - 1u) / blocks * blocks * mp * 32u : 0u) + 2048u;
 }
-inline bool is_small(uint32_t m, uint32_t n)
+// Blocks of the cluster that takes an m x n matrix, 0 where none does.
+inline uint32_t small_blocks(uint32_t m, uint32_t n)
 {
-    return m <= kSmallRows && n <= 8192u && small_bytes((m + 15u) / 16u * 16u, (n + 15u) / 16u * 16u) <= kSmallBytes;
+    if (m > kSmallRows) return 0u;
+    for (uint32_t b = 1; b <= kMostBlocks; b *= 2u)
+        if (n <= b * kSmallCols) return b;
+    return 0u;
 }
 
 // Buffers of a large matrix in the workspace, each a matrix of high parts followed by one of low parts: X, the next X, A, B.

@@ -191,7 +191,7 @@ def test_muon_solvers_have_their_workspace(lib):
     from paper_2202_05008_b200 import workloads as W
     from paper_2202_05008_b200.binding import make_config
     n, m = C.c_size_t(), C.c_size_t()
-    for w, large in ((W.CFG4, False), (W.CFG3, False), (W.SEQ2SEQ, True),
+    for w, large in ((W.CFG4, False), (W.CFG3, False), (W.SEQ2SEQ, False),
                      (W.Workload("x", 4, 300 * 201 + 201 * 5, 1, policy_kind=W.POLICY_MLP, layer_sizes=(200, 300, 3)), True)):
         w = w.with_(param_dim=W.mlp_param_count(w.layer_sizes)) if w.name == "x" else w
         assert lib.evo_workspace_bytes(C.byref(make_config(w)), C.byref(n)) == OK
