@@ -24,7 +24,7 @@ static Group group_for(const Matrix& x, uint32_t blocks)
     g.gain = x.gain;
     return g;
 }
-static uint32_t blocks_of(const Matrix& x) { return small_blocks(std::min(x.rows, x.cols), std::max(x.rows, x.cols)); }
+static Choice choice_of(const Matrix& x) { return choose(std::min(x.rows, x.cols), std::max(x.rows, x.cols)); }
 
 // Lists the large matrices from *at on, as many as a launch takes; advances *at.  False where their numbers do not fit 32 bits.
 static bool gather_large(const Matrix* list, size_t n, size_t* at, Args* a, size_t* bytes)
@@ -33,7 +33,7 @@ static bool gather_large(const Matrix* list, size_t n, size_t* at, Args* a, size
     size_t off = 0;
     a->groups = 0;
     for (; *at < n && a->groups < kMaxLarge; ++*at) {
-        if (blocks_of(list[*at])) continue;
+        if (choice_of(list[*at]).kind != kLarge) continue;
         Group g = group_for(list[*at], 0u);
         const uint64_t rows = g.mp / kTile;
         g.first_block = static_cast<uint32_t>(blocks); g.first_pair = static_cast<uint32_t>(pairs); g.first_tile = static_cast<uint32_t>(tiles);
@@ -69,27 +69,32 @@ int launch(cudaStream_t st, uint32_t source, const Matrix* list, size_t n, const
 {
     int launches = 0;
     Args a = base;
-    for (uint32_t cluster = kMostBlocks; cluster; cluster /= 2u)
-        for (size_t at = 0; at < n;) {
-            uint64_t blocks = 0;
-            size_t smem = 0;
-            a.groups = 0;
-            a.cluster = cluster;
-            for (; at < n && a.groups < kMaxGroups; ++at) {
-                if (blocks_of(list[at]) != cluster) continue;
-                Group g = group_for(list[at], cluster);
-                g.first_block = static_cast<uint32_t>(blocks);
-                blocks += g.count;
-                if (blocks * cluster > 0x7FFFFFFFu) return -1;
-                smem = std::max(smem, small_bytes(g.mp, g.np, cluster));
-                a.g[a.groups++] = g;
+    // the longest first: a launch for each kernel and size of cluster that the list needs
+    for (int kind = kSmall; kind >= static_cast<int>(kTiny16); --kind)
+        for (uint32_t cluster = kMostBlocks; cluster; cluster /= 2u)
+            for (size_t at = 0; at < n;) {
+                uint64_t blocks = 0;
+                size_t smem = 0;
+                uint32_t columns = 0;
+                a.groups = 0;
+                a.cluster = cluster;
+                for (; at < n && a.groups < kMaxGroups; ++at) {
+                    const Choice c = choice_of(list[at]);
+                    if (static_cast<int>(c.kind) != kind || c.blocks != cluster) continue;
+                    Group g = group_for(list[at], cluster);
+                    g.first_block = static_cast<uint32_t>(blocks);
+                    blocks += g.count;
+                    if (blocks * cluster > 0x7FFFFFFFu) return -1;
+                    smem = std::max(smem, small_bytes(g.mp, g.np, cluster));
+                    columns = std::max(columns, g.np);
+                    a.g[a.groups++] = g;
+                }
+                a.blocks = static_cast<uint32_t>(blocks);
+                if (a.groups == 0u) continue;
+                const int k = kind == kSmall ? launch_small(st, source, a, smem) : launch_tiny(st, source, a, kind + 1u, std::min(16u, columns / 16u));
+                if (k < 0) return -1;
+                launches += k;
             }
-            a.blocks = static_cast<uint32_t>(blocks);
-            if (a.groups == 0u) continue;
-            const int k = launch_small(st, source, a, smem);
-            if (k < 0) return -1;
-            launches += k;
-        }
     for (size_t at = 0; at < n;) {
         size_t bytes = 0;
         if (!gather_large(list, n, &at, &a, &bytes)) return -1;

@@ -15,6 +15,7 @@ struct Matrix {
     float gain;
 };
 
+int launch_tiny(cudaStream_t st, uint32_t source, const Args& a, uint32_t row_tiles, uint32_t warps);
 int launch_small(cudaStream_t st, uint32_t source, const Args& a, size_t smem);
 int launch_large(cudaStream_t st, uint32_t source, const Args& a);
 
