@@ -4,10 +4,12 @@
 // takes 16 outputs and reads their weight rows once, straight into the MMA's operand registers; the group's rows are the
 // MMA's columns (8, or 32 where more are left).  Where there are too few such tiles to fill the GPU the four warps of a block
 // share one and split the contracted index.
+#include <cstring>
 #include <type_traits>
 
 #include "grouped.h"
 #include "grouped_mma.cuh"
+#include "member_stream.h"
 
 namespace evo {
 namespace {
@@ -232,6 +234,17 @@ int launch_type(cudaStream_t st, const GroupedArgs& a)
 int launch_grouped(cudaStream_t st, uint32_t type, const GroupedArgs& a)
 {
     if (grouped_tc_takes(type, a)) return launch_grouped_tc(st, type, a);
+    // fp32 weights whose rows follow one another, members 16 bytes aligned: streamed
+    if (type == EVO_F32 && (a.ld_w == a.n_in || a.n_out == 1u) && (reinterpret_cast<uintptr_t>(a.w) & 15u) == 0u && a.stride_w % 4u == 0u) {
+        StreamArgs s;
+        std::memset(&s, 0, sizeof(s));
+        s.g = a;
+        s.w = static_cast<const float*>(a.w); s.b = static_cast<const float*>(a.b); s.stride_w = a.stride_w; s.stride_b = a.stride_b;
+        s.w_end = static_cast<uint64_t>(a.n_in) * a.n_out;
+        s.n_layers = 1u; s.sizes[0] = a.n_in; s.sizes[1] = a.n_out;
+        size_t bytes = 0;
+        if (stream_plan(&s, &bytes)) return launch_stream(st, s, bytes);
+    }
     return type == EVO_F32 ? launch_type<float>(st, a) : type == EVO_BF16 ? launch_type<__nv_bfloat16>(st, a) : launch_type<__half>(st, a);
 }
 

@@ -3,7 +3,7 @@
 #include <cstring>
 
 #include "grouped.h"
-#include "mlp_actions.h"
+#include "member_stream.h"
 
 using namespace evo;
 
@@ -17,6 +17,23 @@ bool overlap(const void* p, uint64_t n, const void* q, uint64_t m)
 uint64_t span(uint64_t rows, uint64_t ld, uint64_t cols) { return rows ? (rows - 1u) * ld + cols : 0u; }
 
 constexpr uint64_t kMost = 1ull << 40;       // elements of a pitch or a stride, and rows: their products stay inside 64 bits
+
+// the layers of a policy as the streaming kernel takes them
+void policy_layers(const evo_actions& p, StreamArgs* a)
+{
+    uint64_t at = 0;
+    a->n_layers = p.n_layers;
+    for (uint32_t l = 0; l <= p.n_layers; ++l) a->sizes[l] = p.layer_sizes[l];
+    for (uint32_t l = 0; l < p.n_layers; ++l) {
+        a->w_at[l] = static_cast<uint32_t>(at);
+        at += static_cast<uint64_t>(p.layer_sizes[l]) * p.layer_sizes[l + 1];
+        a->b_at[l] = static_cast<uint32_t>(at);
+        at += p.layer_sizes[l + 1];
+    }
+    a->w_end = at;
+    a->g.rows = p.rows;
+    a->g.groups = p.members;
+}
 
 // rows of the layers between the first and the last, twice, for a policy that one block does not hold
 size_t layers_bytes(const evo_actions& a)
@@ -77,9 +94,11 @@ evo_status evo_mlp_actions_bytes(const evo_actions* p, size_t* bytes)
 {
     const evo_status st = check_actions(p);
     if (st != EVO_OK || !bytes) return EVO_ERR_INVALID_ARG;
-    ActionsArgs a;
+    StreamArgs a;
+    std::memset(&a, 0, sizeof(a));
+    policy_layers(*p, &a);
     size_t smem = 0;
-    *bytes = actions_plan(p->layer_sizes, p->n_layers, &a, &smem) ? 0u : layers_bytes(*p);
+    *bytes = stream_plan(&a, &smem) ? 0u : layers_bytes(*p);
     return EVO_OK;
 }
 
@@ -102,16 +121,16 @@ evo_status evo_mlp_actions(const evo_actions* p, void* d_workspace, size_t works
     if (need && (!d_workspace || (reinterpret_cast<uintptr_t>(d_workspace) & 255u))) return EVO_ERR_INVALID_ARG;
     if (workspace_bytes < need) return EVO_ERR_WORKSPACE;
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    ActionsArgs a;
+    StreamArgs a;
     std::memset(&a, 0, sizeof(a));
-    size_t smem = 0;
-    const bool whole = actions_plan(p->layer_sizes, p->n_layers, &a, &smem);
-    a.theta = p->d_theta; a.ld_theta = p->ld_theta;
+    policy_layers(*p, &a);
+    a.w = p->d_theta; a.b = p->d_theta; a.stride_w = a.stride_b = p->ld_theta;
     GroupedArgs& g = a.g;
-    g.x = p->d_observations; g.y = p->d_actions; g.offsets = p->d_offsets; g.wide_offsets = p->offsets_64; g.groups = p->members; g.rows = p->rows;
+    g.x = p->d_observations; g.y = p->d_actions; g.offsets = p->d_offsets; g.wide_offsets = p->offsets_64;
     g.ld_x = p->rows > 1u ? p->ld_observations : 0u; g.ld_y = p->ld_actions; g.activation = EVO_ACT_TANH; g.scale = p->action_scale;
-    if (whole) {
-        const int n = launch_actions(stream, a, smem);
+    size_t smem = 0;
+    if (stream_plan(&a, &smem)) {
+        const int n = launch_stream(stream, a, smem);
         return n == -2 ? EVO_ERR_UNSUPPORTED : n < 0 ? EVO_ERR_CUDA : EVO_OK;
     }
     // a launch per layer, hidden rows in the workspace

@@ -146,7 +146,7 @@ def test_grouped_refusals(lib, bad):
 def test_grouped_without_rows_is_nothing_to_do(lib):
     assert lib.evo_grouped_linear(C.byref(_grouped(rows=0, d_x=None, d_y=None)), None) == OK
     assert lib.evo_grouped_linear(None, None) == INVALID
-    assert lib.evo_grouped_linear(C.byref(_grouped(groups=(1 << 31) - 1, n_out=1 << 20, weight_stride=0, ld_y=1 << 20, d_y=FAR * 64)), None) in (INVALID, UNSUPPORTED)
+    assert lib.evo_grouped_linear(C.byref(_grouped(groups=(1 << 31) - 1, n_out=1 << 20, ld_weight=12, weight_stride=0, ld_y=1 << 20, d_y=FAR * 64)), None) in (INVALID, UNSUPPORTED)
 
 
 def _actions(sizes=(5, 16, 16, 1), **kw):
