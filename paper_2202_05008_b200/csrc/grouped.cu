@@ -9,7 +9,7 @@
 
 #include "grouped.h"
 #include "grouped_mma.cuh"
-#include "member_stream.h"
+#include "member_rows.h"
 
 namespace evo {
 namespace {
@@ -234,16 +234,14 @@ int launch_type(cudaStream_t st, const GroupedArgs& a)
 int launch_grouped(cudaStream_t st, uint32_t type, const GroupedArgs& a)
 {
     if (grouped_tc_takes(type, a)) return launch_grouped_tc(st, type, a);
-    // fp32 weights whose rows follow one another, members 16 bytes aligned: streamed
-    if (type == EVO_F32 && (a.ld_w == a.n_in || a.n_out == 1u) && (reinterpret_cast<uintptr_t>(a.w) & 15u) == 0u && a.stride_w % 4u == 0u) {
-        StreamArgs s;
-        std::memset(&s, 0, sizeof(s));
-        s.g = a;
-        s.w = static_cast<const float*>(a.w); s.b = static_cast<const float*>(a.b); s.stride_w = a.stride_w; s.stride_b = a.stride_b;
-        s.w_end = static_cast<uint64_t>(a.n_in) * a.n_out;
-        s.n_layers = 1u; s.sizes[0] = a.n_in; s.sizes[1] = a.n_out;
-        size_t bytes = 0;
-        if (stream_plan(&s, &bytes)) return launch_stream(st, s, bytes);
+    // fp32 rows that a warp can keep: each weight is read once and goes to all rows of a pass
+    if (type == EVO_F32 && a.ld_w < (1ull << 31)) {
+        MemberArgs m;
+        std::memset(&m, 0, sizeof(m));
+        m.g = a;
+        m.w = static_cast<const float*>(a.w); m.b = static_cast<const float*>(a.b); m.stride_w = a.stride_w; m.stride_b = a.stride_b;
+        m.n_layers = 1u; m.sizes[0] = a.n_in; m.sizes[1] = a.n_out; m.ld_w[0] = static_cast<uint32_t>(a.ld_w);
+        if (member_plan(&m)) return launch_member_rows(st, m);
     }
     return type == EVO_F32 ? launch_type<float>(st, a) : type == EVO_BF16 ? launch_type<__nv_bfloat16>(st, a) : launch_type<__half>(st, a);
 }

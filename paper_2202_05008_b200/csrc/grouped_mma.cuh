@@ -31,14 +31,34 @@ __device__ __forceinline__ void mma_16(float (&c)[4], const uint32_t (&a)[4], ui
             : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// Of an infinity the low part is a NaN, which only reaches the small products' sums: they do not count where the large ones' sum is
-// no finite number, and then it is what the plain product would be.  (Numbers above 3.4011e38 round to an infinity.)
+// hi is rounded to nearest by hand (cvt.rna.tf32 is a sequence of instructions: 4,096 members of 28-128-128-8 took 62 million warp
+// instructions with it and SPLIT_NOTE without).  Of an infinity the low part is a NaN, which only reaches the small products' sums: they do not
+// count where the large ones' sum is no finite number, and then it is what the plain product would be.  A NaN that rounds to something else stays one
+// in its low part.  (Numbers above 3.4011e38 round to an infinity.)
 __device__ __forceinline__ void split(float x, uint32_t& hi, uint32_t& lo)
 {
-    asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(hi) : "f"(x));
+    hi = (__float_as_uint(x) + 0x1000u) & 0xFFFFE000u;
     lo = __float_as_uint(x - __uint_as_float(hi));
 }
 __device__ __forceinline__ float join(float large, float small) { return isfinite(large) ? large + small : large; }
+
+// tanh without branches: up to 1/2 the series of tanh to x^13 (what is left out is below 1e-7 of the result), beyond it
+// 1 - 2 / (e^2|x| + 1) with the hardware's exponential (2^-22 relative): 2e-7 of the result at worst
+__device__ __forceinline__ float tanh32(float x)
+{
+    const float a = fabsf(x), s = x * x;
+    float p = 21844.0f / 6081075.0f;
+    p = fmaf(p, s, -1382.0f / 155925.0f);
+    p = fmaf(p, s, 62.0f / 2835.0f);
+    p = fmaf(p, s, -17.0f / 315.0f);
+    p = fmaf(p, s, 2.0f / 15.0f);
+    p = fmaf(p, s, -1.0f / 3.0f);
+    const float near = fmaf(x * s, p, x);
+    float e, r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(a * 2.885390082f));      // 2 log2(e)
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(e + 1.0f));
+    return a < 0.5f ? near : copysignf(fmaf(-2.0f, r, 1.0f), x);
+}
 
 }  // namespace gm
 }  // namespace evo

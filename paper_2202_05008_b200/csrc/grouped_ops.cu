@@ -3,7 +3,7 @@
 #include <cstring>
 
 #include "grouped.h"
-#include "member_stream.h"
+#include "member_rows.h"
 
 using namespace evo;
 
@@ -18,19 +18,19 @@ uint64_t span(uint64_t rows, uint64_t ld, uint64_t cols) { return rows ? (rows -
 
 constexpr uint64_t kMost = 1ull << 40;       // elements of a pitch or a stride, and rows: their products stay inside 64 bits
 
-// the layers of a policy as the streaming kernel takes them
-void policy_layers(const evo_actions& p, StreamArgs* a)
+// the layers of a policy as the kernel for rows and layers takes them
+void policy_layers(const evo_actions& p, MemberArgs* a)
 {
     uint64_t at = 0;
     a->n_layers = p.n_layers;
     for (uint32_t l = 0; l <= p.n_layers; ++l) a->sizes[l] = p.layer_sizes[l];
     for (uint32_t l = 0; l < p.n_layers; ++l) {
         a->w_at[l] = static_cast<uint32_t>(at);
+        a->ld_w[l] = p.layer_sizes[l];
         at += static_cast<uint64_t>(p.layer_sizes[l]) * p.layer_sizes[l + 1];
         a->b_at[l] = static_cast<uint32_t>(at);
         at += p.layer_sizes[l + 1];
     }
-    a->w_end = at;
     a->g.rows = p.rows;
     a->g.groups = p.members;
 }
@@ -94,11 +94,10 @@ evo_status evo_mlp_actions_bytes(const evo_actions* p, size_t* bytes)
 {
     const evo_status st = check_actions(p);
     if (st != EVO_OK || !bytes) return EVO_ERR_INVALID_ARG;
-    StreamArgs a;
+    MemberArgs a;
     std::memset(&a, 0, sizeof(a));
     policy_layers(*p, &a);
-    size_t smem = 0;
-    *bytes = stream_plan(&a, &smem) ? 0u : layers_bytes(*p);
+    *bytes = member_plan(&a) ? 0u : layers_bytes(*p);
     return EVO_OK;
 }
 
@@ -121,16 +120,15 @@ evo_status evo_mlp_actions(const evo_actions* p, void* d_workspace, size_t works
     if (need && (!d_workspace || (reinterpret_cast<uintptr_t>(d_workspace) & 255u))) return EVO_ERR_INVALID_ARG;
     if (workspace_bytes < need) return EVO_ERR_WORKSPACE;
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    StreamArgs a;
+    MemberArgs a;
     std::memset(&a, 0, sizeof(a));
     policy_layers(*p, &a);
     a.w = p->d_theta; a.b = p->d_theta; a.stride_w = a.stride_b = p->ld_theta;
     GroupedArgs& g = a.g;
     g.x = p->d_observations; g.y = p->d_actions; g.offsets = p->d_offsets; g.wide_offsets = p->offsets_64;
     g.ld_x = p->rows > 1u ? p->ld_observations : 0u; g.ld_y = p->ld_actions; g.activation = EVO_ACT_TANH; g.scale = p->action_scale;
-    size_t smem = 0;
-    if (stream_plan(&a, &smem)) {
-        const int n = launch_stream(stream, a, smem);
+    if (member_plan(&a)) {
+        const int n = launch_member_rows(stream, a);
         return n == -2 ? EVO_ERR_UNSUPPORTED : n < 0 ? EVO_ERR_CUDA : EVO_OK;
     }
     // a launch per layer, hidden rows in the workspace
