@@ -48,26 +48,32 @@ __device__ __forceinline__ void tile_sums(const T* w0, const T* w1, const T* con
 {
     const uint32_t q = threadIdx.x & 3u;
     if constexpr (std::is_same<T, float>::value) {
-        float small[NT][4];
+        constexpr uint32_t kAhead = NT == 1u ? 8u : 4u;          // sixteens whose weights are asked for together
+        float small[NT][4], less[NT][4];
 #pragma unroll
         for (uint32_t t = 0; t < NT; ++t)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) c[t][i] = small[t][i] = 0.f;
-        for (uint32_t k = k0; k < k1; k += 64u) {
+            for (int i = 0; i < 4; ++i) c[t][i] = small[t][i] = less[t][i] = 0.f;
+        for (uint32_t k = k0; k < k1; k += 16u * kAhead) {
             float large[NT][4];
 #pragma unroll
             for (uint32_t t = 0; t < NT; ++t)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) large[t][i] = 0.f;
-            uint4 u[4], v[4];
+            uint4 u[kAhead], v[kAhead];
 #pragma unroll
-            for (uint32_t s = 0; s < 4u; ++s) {
+            for (uint32_t s = 0; s < kAhead; ++s) {
                 u[s] = load16<T, VEC>(w0, k + 16u * s + 4u * q, n_in);
                 v[s] = load16<T, VEC>(w1, k + 16u * s + 4u * q, n_in);
             }
 #pragma unroll
-            for (uint32_t s = 0; s < 4u; ++s) {
+            for (uint32_t s = 0; s < kAhead; ++s) {
                 if (k + 16u * s >= k1) break;
+                if (s == 4u)
+#pragma unroll
+                    for (uint32_t t = 0; t < NT; ++t)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) { c[t][i] += large[t][i]; large[t][i] = 0.f; }
                 const uint32_t wu[4] = { u[s].x, u[s].y, u[s].z, u[s].w }, wv[4] = { v[s].x, v[s].y, v[s].z, v[s].w };
                 uint32_t hi[2][4], lo[2][4];
 #pragma unroll
@@ -88,7 +94,7 @@ __device__ __forceinline__ void tile_sums(const T* w0, const T* w1, const T* con
                     for (int h = 0; h < 2; ++h) {
                         gm::mma_tf32(large[t], hi[h], xh[2 * h], xh[2 * h + 1]);
                         gm::mma_tf32(small[t], hi[h], xl[2 * h], xl[2 * h + 1]);
-                        gm::mma_tf32(small[t], lo[h], xh[2 * h], xh[2 * h + 1]);
+                        gm::mma_tf32(less[t], lo[h], xh[2 * h], xh[2 * h + 1]);
                     }
                 }
             }
@@ -100,7 +106,7 @@ __device__ __forceinline__ void tile_sums(const T* w0, const T* w1, const T* con
 #pragma unroll
         for (uint32_t t = 0; t < NT; ++t)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) c[t][i] = gm::join(c[t][i], small[t][i]);
+            for (int i = 0; i < 4; ++i) c[t][i] = gm::join(c[t][i], small[t][i] + less[t][i]);
     } else {
 #pragma unroll
         for (uint32_t t = 0; t < NT; ++t)
@@ -130,7 +136,7 @@ __device__ __forceinline__ void tile_sums(const T* w0, const T* w1, const T* con
 
 __device__ __forceinline__ float activate(float x, uint32_t activation, float scale)
 {
-    if (activation == EVO_ACT_TANH) x = tanhf(x);
+    if (activation == EVO_ACT_TANH) x = gm::tanh32(x);
     if (activation == EVO_ACT_RELU) x = x < 0.f ? 0.f : x;                   // (a NaN stays one)
     return scale * x;
 }
@@ -191,6 +197,79 @@ __device__ __forceinline__ void tile(const GroupedArgs& a, uint32_t group, uint3
     }
 }
 
+// fp32, at most 128 of the contracted index, aligned; up to 8 rows: the weights and biases are asked for first, then the rows, which the block's warps
+// share through shared memory: one latency for all of them
+constexpr uint32_t kShort = 128;
+__device__ __forceinline__ void short_tile(const GroupedArgs& a, uint32_t group, uint32_t o0, uint64_t r, uint64_t end, float (*rows)[kShort + 4])
+{
+    const uint32_t lane = threadIdx.x & 31u, g = lane >> 2, q = lane & 3u;
+    const float* const w = static_cast<const float*>(a.w) + group * a.stride_w;
+    const float* const w0 = w + static_cast<uint64_t>(min(o0 + g, a.n_out - 1u)) * a.ld_w;
+    const float* const w1 = w + static_cast<uint64_t>(min(o0 + g + 8u, a.n_out - 1u)) * a.ld_w;
+    const float* const b = a.b ? static_cast<const float*>(a.b) + group * a.stride_b : nullptr;
+    uint4 u[8], v[8];
+#pragma unroll
+    for (uint32_t s = 0; s < 8u; ++s) {
+        u[s] = load16<float, true>(w0, 16u * s + 4u * q, a.n_in);
+        v[s] = load16<float, true>(w1, 16u * s + 4u * q, a.n_in);
+    }
+    const float b0 = b && o0 + g < a.n_out ? b[o0 + g] : 0.f, b1 = b && o0 + g + 8u < a.n_out ? b[o0 + g + 8u] : 0.f;
+#pragma unroll
+    for (uint32_t t = 0; t < 2u; ++t) {
+        const uint32_t x = threadIdx.x + 128u * t, row = x >> 5, k = (x & 31u) * 4u;
+        const uint64_t from = r + row < end ? r + row : end - 1u;
+        *reinterpret_cast<uint4*>(&rows[row][k]) = load16<float, true>(static_cast<const float*>(a.x) + from * a.ld_x, k, a.n_in);
+    }
+    __syncthreads();
+    float large[4] = {}, small[4] = {}, less[4] = {}, sum[4] = {};
+#pragma unroll
+    for (uint32_t s = 0; s < 8u; ++s) {
+        if (16u * s >= a.n_in) break;
+        if (s == 4u)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { sum[i] = large[i]; large[i] = 0.f; }
+        const uint32_t wu[4] = { u[s].x, u[s].y, u[s].z, u[s].w }, wv[4] = { v[s].x, v[s].y, v[s].z, v[s].w };
+        const float4 z = *reinterpret_cast<const float4*>(&rows[g][16u * s + 4u * q]);
+        uint32_t xh[4], xl[4];
+        gm::split(z.x, xh[0], xl[0]); gm::split(z.y, xh[1], xl[1]); gm::split(z.z, xh[2], xl[2]); gm::split(z.w, xh[3], xl[3]);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            uint32_t hi[4], lo[4];
+            gm::split(__uint_as_float(wu[2 * h]), hi[0], lo[0]);
+            gm::split(__uint_as_float(wv[2 * h]), hi[1], lo[1]);
+            gm::split(__uint_as_float(wu[2 * h + 1]), hi[2], lo[2]);
+            gm::split(__uint_as_float(wv[2 * h + 1]), hi[3], lo[3]);
+            gm::mma_tf32(large, hi, xh[2 * h], xh[2 * h + 1]);
+            gm::mma_tf32(small, hi, xl[2 * h], xl[2 * h + 1]);
+            gm::mma_tf32(less, lo, xh[2 * h], xh[2 * h + 1]);
+        }
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < 4u; ++i) {
+        const uint32_t o = o0 + g + 8u * (i >> 1);
+        const uint64_t row = r + 2u * q + (i & 1u);
+        if (o >= a.n_out || row >= end) continue;
+        float y = gm::join(sum[i] + large[i], small[i] + less[i]) + (i >> 1 ? b1 : b0);
+        if (a.activation == EVO_ACT_TANH) y = gm::tanh32(y);
+        if (a.activation == EVO_ACT_RELU) y = y < 0.f ? 0.f : y;
+        static_cast<float*>(a.y)[row * a.ld_y + o] = a.scale * y;
+    }
+}
+__global__ void __launch_bounds__(kWarps * 32, 5) k_grouped_short(const __grid_constant__ GroupedArgs a)
+{
+    __shared__ float rows[8][kShort + 4];
+    dep_wait();
+    dep_trigger();
+    const uint32_t per = (a.n_out + 16u * kWarps - 1u) / (16u * kWarps);
+    const uint32_t group = blockIdx.x / per, o0 = blockIdx.x % per * 16u * kWarps + (threadIdx.x >> 5) * 16u;
+    uint64_t r, end;
+    group_rows(a, group, &r, &end);
+    for (; r < end; r += 8u) {
+        short_tile(a, group, o0, r, end, rows);              // (a warp without outputs works on the last one's weights and stores nothing)
+        __syncthreads();
+    }
+}
+
 template <typename T, bool VEC, bool SPLIT>
 __global__ void __launch_bounds__(kWarps * 32) k_grouped(const __grid_constant__ GroupedArgs a)
 {
@@ -213,6 +292,9 @@ int launch(cudaStream_t st, const GroupedArgs& a, bool split)
 {
     const uint64_t per = split ? (a.n_out + 15u) / 16u : (a.n_out + 16u * kWarps - 1u) / (16u * kWarps), blocks = per * a.groups;
     if (blocks > 0x7FFFFFFFull) return -2;
+    if constexpr (std::is_same<T, float>::value && VEC)
+        if (!split && a.n_in <= kShort && a.rows <= 8ull * a.groups)
+            return launch_dependent(k_grouped_short, dim3(static_cast<uint32_t>(blocks)), dim3(kWarps * 32), 0, st, a) == cudaSuccess ? 1 : -1;
     auto kernel = split ? k_grouped<T, VEC, true> : k_grouped<T, VEC, false>;
     return launch_dependent(kernel, dim3(static_cast<uint32_t>(blocks)), dim3(kWarps * 32), 0, st, a) == cudaSuccess ? 1 : -1;
 }
@@ -234,8 +316,9 @@ int launch_type(cudaStream_t st, const GroupedArgs& a)
 int launch_grouped(cudaStream_t st, uint32_t type, const GroupedArgs& a)
 {
     if (grouped_tc_takes(type, a)) return launch_grouped_tc(st, type, a);
-    // fp32 rows that a warp can keep: each weight is read once and goes to all rows of a pass
-    if (type == EVO_F32 && a.ld_w < (1ull << 31)) {
+    // Many fp32 rows a group: kept in shared memory while the weights pass by (8 groups of 500 rows, 500 x 1,000: 184 us against 452; 1,000 of 20 rows,
+    // 200 x 300: 251 against 139)
+    if (type == EVO_F32 && a.rows > 24ull * a.groups && a.ld_w < (1ull << 31)) {
         MemberArgs m;
         std::memset(&m, 0, sizeof(m));
         m.g = a;

@@ -32,7 +32,7 @@ __device__ __forceinline__ void mma_16(float (&c)[4], const uint32_t (&a)[4], ui
 }
 
 // hi is rounded to nearest by hand (cvt.rna.tf32 is a sequence of instructions: 4,096 members of 28-128-128-8 took 62 million warp
-// instructions with it and SPLIT_NOTE without).  Of an infinity the low part is a NaN, which only reaches the small products' sums: they do not
+// instructions with it and 53 without).  Of an infinity the low part is a NaN, which only reaches the small products' sums: they do not
 // count where the large ones' sum is no finite number, and then it is what the plain product would be.  A NaN that rounds to something else stays one
 // in its low part.  (Numbers above 3.4011e38 round to an infinity.)
 __device__ __forceinline__ void split(float x, uint32_t& hi, uint32_t& lo)

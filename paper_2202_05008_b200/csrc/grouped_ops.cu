@@ -43,6 +43,22 @@ size_t layers_bytes(const evo_actions& a)
     return static_cast<size_t>(2u * a.rows * ((widest + 3u) / 4u * 4u) * sizeof(float));
 }
 
+// Whether a launch per layer is the faster way: few rows a member and many weights, in layers that the kernel for one short layer takes (it reads
+// them at 5.1 TB/s, the one for all layers at 2.5).  All layers / one after the other: 28-128-128-8, 300 members of 4 rows 15.5 / 19.6 us, 1,000 59.9 / 30.9,
+// 4,096 140 / 107; 28-64-64-64-64-8, 1,000 47.8 / 31.6, 4,000 of 6 rows 112 / 99.5; 5-64-64-1, 1,000 28.4 / 21.8; 9-179-38-13 (not aligned), 4,000 145 / 177.
+bool by_layers(const evo_actions& p)
+{
+    uint64_t dim = 0, at = 0;
+    bool simple = p.n_layers > 1u;
+    for (uint32_t l = 0; l < p.n_layers; ++l) {
+        const uint64_t in = p.layer_sizes[l], out = p.layer_sizes[l + 1];
+        if (in > 16u && (in > 128u || (in | at) % 4u)) simple = false;
+        dim += in * out;
+        at += (in + 1u) * out;
+    }
+    return simple && p.rows <= 8ull * p.members && dim * p.members >= (1u << 22);
+}
+
 evo_status check_actions(const evo_actions* a)
 {
     if (!a || a->struct_size != sizeof(evo_actions) || a->members < 1u || a->n_layers < 1u || a->n_layers > EVO_MAX_LAYERS) return EVO_ERR_INVALID_ARG;
@@ -97,7 +113,7 @@ evo_status evo_mlp_actions_bytes(const evo_actions* p, size_t* bytes)
     MemberArgs a;
     std::memset(&a, 0, sizeof(a));
     policy_layers(*p, &a);
-    *bytes = member_plan(&a) ? 0u : layers_bytes(*p);
+    *bytes = member_plan(&a) && !by_layers(*p) ? 0u : layers_bytes(*p);
     return EVO_OK;
 }
 
@@ -127,7 +143,7 @@ evo_status evo_mlp_actions(const evo_actions* p, void* d_workspace, size_t works
     GroupedArgs& g = a.g;
     g.x = p->d_observations; g.y = p->d_actions; g.offsets = p->d_offsets; g.wide_offsets = p->offsets_64;
     g.ld_x = p->rows > 1u ? p->ld_observations : 0u; g.ld_y = p->ld_actions; g.activation = EVO_ACT_TANH; g.scale = p->action_scale;
-    if (member_plan(&a)) {
+    if (need == 0u && member_plan(&a)) {
         const int n = launch_member_rows(stream, a);
         return n == -2 ? EVO_ERR_UNSUPPORTED : n < 0 ? EVO_ERR_CUDA : EVO_OK;
     }

@@ -205,7 +205,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_grouped_tc(const __grid_constan
                     for (uint32_t i = 0; i < 32u; ++i)
                         if (c + i < rows) {
                             float v = __uint_as_float(u[i / 8u][i % 8u]) + bias;
-                            if (a.activation == EVO_ACT_TANH) v = tanhf(v);
+                            if (a.activation == EVO_ACT_TANH) v = gm::tanh32(v);
                             if (a.activation == EVO_ACT_RELU) v = v < 0.f ? 0.f : v;
                             v = abort_flag ? __int_as_float(0x7FC00000) : a.scale * v;
                             if constexpr (std::is_same<T, __half>::value) y[(c + i) * a.ld_y] = __float2half_rn(v);

@@ -215,6 +215,33 @@ def test_actions(sizes, lengths):
     assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("members,rows,sizes", [(700, 2500, (28, 128, 128, 8)), (1100, 5000, (5, 64, 64, 1)), (2000, 30000, (20, 100, 60, 4)), (300, 9000, (28, 96, 40, 8)),
+                                                (3, 4000, (28, 128, 128, 8)), (40, 60, (60, 200, 200, 200, 200, 9)), (64, 64, (28, 512, 300, 8))])
+def test_actions_of_populations(members, rows, sizes):
+    """Sizes at which other kernels are chosen: a launch per layer, a warp and eight warps an item."""
+    theta = theta_for(members, sizes)
+    gen = torch.Generator(device="cuda").manual_seed(rows)
+    cuts = torch.sort(torch.randint(0, rows + 1, (members - 1,), generator=gen, device="cuda")).values
+    off = torch.cat([torch.zeros(1, dtype=torch.int64, device="cuda"), cuts, torch.full((1,), rows, device="cuda")]).int()
+    obs = torch.randn(rows, sizes[0], generator=gen, device="cuda")
+    got = mlp_actions(theta, sizes, obs, off, action_scale=2.0)
+    want, bound = actions_exact(theta, sizes, obs, off, 2.0)
+    assert ((got.double() - want).abs() <= bound).all(), float(((got.double() - want).abs() / bound).max())
+    assert torch.equal(mlp_actions(theta, sizes, obs, off, action_scale=2.0), got)
+
+
+@pytest.mark.parametrize("groups,rows,n_in,n_out,dtype", [(500, 1500, 128, 130, F32), (500, 1500, 100, 64, F32), (40, 9000, 500, 200, F32), (3, 3, 4000, 70, F32), (20, 2000, 36, 1000, F32),
+                                                          (2000, 4000, 64, 40, BF16), (3, 2000, 520, 384, F16), (1, 5000, 128, 128, BF16)])
+def test_grouped_populations(groups, rows, n_in, n_out, dtype):
+    gen = torch.Generator(device="cuda").manual_seed(rows + n_in)
+    cuts = torch.sort(torch.randint(0, rows + 1, (groups - 1,), generator=gen, device="cuda")).values
+    off = torch.cat([torch.zeros(1, dtype=torch.int64, device="cuda"), cuts, torch.full((1,), rows, device="cuda")])
+    x = torch.randn(rows, n_in, generator=gen, device="cuda").to(dtype)
+    w = (torch.randn(groups, n_out, n_in, generator=gen, device="cuda") / math.sqrt(n_in)).to(dtype)
+    b = torch.randn(groups, n_out, generator=gen, device="cuda").to(dtype)
+    check(grouped_linear(x, w, off, b, activation="tanh"), x, w, off, b, "tanh")
+
+
 def test_actions_layer_by_layer_are_the_same_policy():
     """The products grouped by member, one after the other over the layers of theta, as a user composes them."""
     sizes, lengths = (28, 128, 128, 8), [4, 0, 7, 3, 1]

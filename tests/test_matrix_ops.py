@@ -198,3 +198,12 @@ def test_muon_solvers_have_their_workspace(lib):
         assert lib.evo_workspace_bytes(C.byref(make_config(w.with_(optimizer=W.OPT_MUON))), C.byref(m)) == OK
         assert (m.value > n.value) == large, w.name
     assert lib.evo_workspace_bytes(C.byref(make_config(W.CFG5.with_(optimizer=W.OPT_MUON))), C.byref(m)) == UNSUPPORTED
+
+
+def test_policies_that_go_layer_by_layer_need_room_for_hidden_rows(lib):
+    n = C.c_size_t()
+    sizes, ld = (28, 128, 128, 8), 21280
+    for members, rows, layers in ((4096, 16384, True), (100, 400, False), (4096, 40000, False)):
+        p = _actions(sizes, members=members, rows=rows, ld_theta=ld)
+        assert lib.evo_mlp_actions_bytes(C.byref(p), C.byref(n)) == OK
+        assert n.value == (2 * rows * 128 * 4 if layers else 0), (members, rows)
