@@ -375,7 +375,8 @@ evo_status evo_muon_step(const evo_muon* cfg, const evo_matrix* list, uint32_t n
  * offsets[groups + 1] (int32, or int64 with offsets_64) lies on the device and does not fall; groups may be empty.  Rows of y
  * that belong to no group are left as they are.  (Offsets that fall or leave [0, rows] give wrong rows, but nothing
  * outside the arrays is touched.)  Sums in fp32; fp32 operands count with 21 bits and more.  y may not overlap anything.
- * Errors: INVALID_ARG, UNSUPPORTED (more than 2^31 blocks), CUDA.
+ * Errors: INVALID_ARG, WORKSPACE, UNSUPPORTED (more than 2^31 blocks), CUDA.  Workspace 0 unless there are many rows a group in a
+ * type or at addresses that have to be laid out anew for the tensor cores.
  */
 enum { EVO_ACT_NONE = 0, EVO_ACT_TANH = 1, EVO_ACT_RELU = 2 };
 typedef struct evo_grouped {
@@ -391,7 +392,8 @@ typedef struct evo_grouped {
     const void* d_offsets;
     void*       d_y;       size_t ld_y;
 } evo_grouped;
-evo_status evo_grouped_linear(const evo_grouped* p, void* cuda_stream);
+evo_status evo_grouped_linear_bytes(const evo_grouped* p, size_t* bytes);
+evo_status evo_grouped_linear(const evo_grouped* p, void* d_workspace, size_t workspace_bytes, void* cuda_stream);
 
 /*
  * The MLP policy's get_actions (paper Section 4, PolicyNetwork.get_actions) for callers that run the task themselves:

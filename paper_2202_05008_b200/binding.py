@@ -109,10 +109,11 @@ def load_library(debug: bool = False):
     L.evo_orthogonalize.argtypes = [vp, vp, vp, vp, C.c_size_t, vp]
     L.evo_muon_bytes.argtypes = [vp, C.c_uint32, C.c_uint64, szp]
     L.evo_muon_step.argtypes = [vp, vp, C.c_uint32, C.c_uint64, C.c_uint32] + [vp] * 8 + [C.c_size_t, vp]
-    L.evo_grouped_linear.argtypes = [vp, vp]
+    L.evo_grouped_linear_bytes.argtypes = [vp, szp]
+    L.evo_grouped_linear.argtypes = [vp, vp, C.c_size_t, vp]
     L.evo_mlp_actions_bytes.argtypes = [vp, szp]
     L.evo_mlp_actions.argtypes = [vp, vp, C.c_size_t, vp]
-    for name in ("evo_orthogonalize_bytes", "evo_orthogonalize", "evo_muon_bytes", "evo_muon_step", "evo_grouped_linear",
+    for name in ("evo_orthogonalize_bytes", "evo_orthogonalize", "evo_muon_bytes", "evo_muon_step", "evo_grouped_linear_bytes", "evo_grouped_linear",
                  "evo_mlp_actions_bytes", "evo_mlp_actions"):
         getattr(L, name).restype = C.c_int
     if debug:

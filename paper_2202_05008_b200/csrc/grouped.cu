@@ -94,7 +94,7 @@ __device__ __forceinline__ void tile_sums(const T* w0, const T* w1, const T* con
                     for (int h = 0; h < 2; ++h) {
                         gm::mma_tf32(large[t], hi[h], xh[2 * h], xh[2 * h + 1]);
                         gm::mma_tf32(small[t], hi[h], xl[2 * h], xl[2 * h + 1]);
-                        gm::mma_tf32(less[t], lo[h], xh[2 * h], xh[2 * h + 1]);
+                        gm::mma_tf32(NT == 1u ? less[t] : small[t], lo[h], xh[2 * h], xh[2 * h + 1]);      // (32 rows have no registers for a third sum)
                     }
                 }
             }
@@ -313,9 +313,11 @@ int launch_type(cudaStream_t st, const GroupedArgs& a)
 
 }  // namespace
 
-int launch_grouped(cudaStream_t st, uint32_t type, const GroupedArgs& a)
+size_t grouped_bytes(uint32_t type, const GroupedArgs& a) { return grouped_tc_takes(type, a) ? 0u : grouped_tc_bytes(type, a); }
+
+int launch_grouped(cudaStream_t st, uint32_t type, const GroupedArgs& a, void* work)
 {
-    if (grouped_tc_takes(type, a)) return launch_grouped_tc(st, type, a);
+    if (work || grouped_tc_takes(type, a)) return launch_grouped_tc(st, type, a, work);
     // Many fp32 rows a group: kept in shared memory while the weights pass by (8 groups of 500 rows, 500 x 1,000: 184 us against 452; 1,000 of 20 rows,
     // 200 x 300: 251 against 139)
     if (type == EVO_F32 && a.rows > 24ull * a.groups && a.ld_w < (1ull << 31)) {

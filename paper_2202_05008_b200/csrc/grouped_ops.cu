@@ -75,26 +75,18 @@ evo_status check_actions(const evo_actions* a)
 
 extern "C" {
 
-evo_status evo_grouped_linear(const evo_grouped* p, void* cuda_stream)
+static evo_status check_grouped(const evo_grouped* p)
 {
     if (!p || p->struct_size != sizeof(evo_grouped) || p->type > EVO_F16 || p->activation > EVO_ACT_RELU || p->offsets_64 > 1u) return EVO_ERR_INVALID_ARG;
     if (p->groups < 1u || p->groups > 0x7FFFFFFFu || p->n_in < 1u || p->n_out < 1u || p->n_in > (1u << 20) || p->n_out > (1u << 20)) return EVO_ERR_INVALID_ARG;
     if (p->rows > kMost || p->ld_x > kMost || p->ld_y > kMost || p->ld_weight > kMost || p->weight_stride > kMost || p->bias_stride > kMost) return EVO_ERR_INVALID_ARG;
     if (!std::isfinite(p->scale)) return EVO_ERR_INVALID_ARG;
-    if (p->rows == 0u) return EVO_OK;
-    const uint64_t size = p->type == EVO_F32 ? 4u : 2u;
-    const uintptr_t bits = reinterpret_cast<uintptr_t>(p->d_x) | reinterpret_cast<uintptr_t>(p->d_weight) | reinterpret_cast<uintptr_t>(p->d_bias) |
-                           reinterpret_cast<uintptr_t>(p->d_y);
-    if (!p->d_x || !p->d_weight || !p->d_y || !p->d_offsets || (bits & (size - 1u))) return EVO_ERR_INVALID_ARG;
-    if (reinterpret_cast<uintptr_t>(p->d_offsets) & (p->offsets_64 ? 7u : 3u)) return EVO_ERR_INVALID_ARG;
     if ((p->rows > 1u && (p->ld_x < p->n_in || p->ld_y < p->n_out)) || (p->n_out > 1u && p->ld_weight < p->n_in)) return EVO_ERR_INVALID_ARG;
-    // (weights and biases may be shared by groups: stride 0)
-    const uint64_t y_bytes = span(p->rows, p->ld_y, p->n_out) * size;
-    if (overlap(p->d_y, y_bytes, p->d_x, span(p->rows, p->ld_x, p->n_in) * size) ||
-        overlap(p->d_y, y_bytes, p->d_weight, ((p->groups - 1u) * static_cast<uint64_t>(p->weight_stride) + span(p->n_out, p->ld_weight, p->n_in)) * size) ||
-        (p->d_bias && overlap(p->d_y, y_bytes, p->d_bias, ((p->groups - 1u) * static_cast<uint64_t>(p->bias_stride) + p->n_out) * size)) ||
-        overlap(p->d_y, y_bytes, p->d_offsets, (p->groups + 1ull) * (p->offsets_64 ? 8u : 4u)))
-        return EVO_ERR_INVALID_ARG;
+    return EVO_OK;
+}
+
+static GroupedArgs grouped_args(const evo_grouped* p)
+{
     GroupedArgs a;
     std::memset(&a, 0, sizeof(a));
     a.x = p->d_x; a.w = p->d_weight; a.b = p->d_bias; a.y = p->d_y; a.offsets = p->d_offsets; a.wide_offsets = p->offsets_64;
@@ -102,7 +94,39 @@ evo_status evo_grouped_linear(const evo_grouped* p, void* cuda_stream)
     // a pitch that is never taken may be anything
     a.rows = p->rows; a.ld_x = p->rows > 1u ? p->ld_x : 0u; a.ld_y = p->ld_y; a.ld_w = p->n_out > 1u ? p->ld_weight : 0u;
     a.stride_w = p->groups > 1u ? p->weight_stride : 0u; a.stride_b = p->bias_stride;
-    const int n = launch_grouped(static_cast<cudaStream_t>(cuda_stream), p->type, a);
+    return a;
+}
+
+evo_status evo_grouped_linear_bytes(const evo_grouped* p, size_t* bytes)
+{
+    const evo_status st = check_grouped(p);
+    if (st != EVO_OK || !bytes) return EVO_ERR_INVALID_ARG;
+    *bytes = p->rows ? grouped_bytes(p->type, grouped_args(p)) : 0u;
+    return EVO_OK;
+}
+
+evo_status evo_grouped_linear(const evo_grouped* p, void* d_workspace, size_t workspace_bytes, void* cuda_stream)
+{
+    const evo_status st = check_grouped(p);
+    if (st != EVO_OK) return st;
+    if (p->rows == 0u) return EVO_OK;
+    const uint64_t size = p->type == EVO_F32 ? 4u : 2u;
+    const uintptr_t bits = reinterpret_cast<uintptr_t>(p->d_x) | reinterpret_cast<uintptr_t>(p->d_weight) | reinterpret_cast<uintptr_t>(p->d_bias) |
+                           reinterpret_cast<uintptr_t>(p->d_y);
+    if (!p->d_x || !p->d_weight || !p->d_y || !p->d_offsets || (bits & (size - 1u))) return EVO_ERR_INVALID_ARG;
+    if (reinterpret_cast<uintptr_t>(p->d_offsets) & (p->offsets_64 ? 7u : 3u)) return EVO_ERR_INVALID_ARG;
+    // (weights and biases may be shared by groups: stride 0)
+    const uint64_t y_bytes = span(p->rows, p->ld_y, p->n_out) * size;
+    if (overlap(p->d_y, y_bytes, p->d_x, span(p->rows, p->ld_x, p->n_in) * size) ||
+        overlap(p->d_y, y_bytes, p->d_weight, ((p->groups - 1u) * static_cast<uint64_t>(p->weight_stride) + span(p->n_out, p->ld_weight, p->n_in)) * size) ||
+        (p->d_bias && overlap(p->d_y, y_bytes, p->d_bias, ((p->groups - 1u) * static_cast<uint64_t>(p->bias_stride) + p->n_out) * size)) ||
+        overlap(p->d_y, y_bytes, p->d_offsets, (p->groups + 1ull) * (p->offsets_64 ? 8u : 4u)))
+        return EVO_ERR_INVALID_ARG;
+    const GroupedArgs a = grouped_args(p);
+    const size_t need = grouped_bytes(p->type, a);
+    if (need && (!d_workspace || (reinterpret_cast<uintptr_t>(d_workspace) & 255u))) return EVO_ERR_INVALID_ARG;
+    if (workspace_bytes < need) return EVO_ERR_WORKSPACE;
+    const int n = launch_grouped(static_cast<cudaStream_t>(cuda_stream), p->type, a, need ? d_workspace : nullptr);
     return n == -2 ? EVO_ERR_UNSUPPORTED : n < 0 ? EVO_ERR_CUDA : EVO_OK;
 }
 
@@ -160,7 +184,7 @@ evo_status evo_mlp_actions(const evo_actions* p, void* d_workspace, size_t works
         at += static_cast<uint64_t>(b.n_in) * b.n_out;
         b.b = p->d_theta + at; b.stride_b = p->ld_theta;
         at += b.n_out;
-        const int n = launch_grouped(stream, EVO_F32, b);
+        const int n = launch_grouped(stream, EVO_F32, b, nullptr);
         if (n < 0) return n == -2 ? EVO_ERR_UNSUPPORTED : EVO_ERR_CUDA;
     }
     return EVO_OK;

@@ -1,4 +1,8 @@
-// Products grouped by member of 16-bit operands on tcgen05: y[r] = scale act(W_g x[r] + b_g).
+// Products grouped by member on tcgen05: y[r] = scale act(W_g x[r] + b_g).
+//
+// 16-bit operands are taken as they lie where TMA can address their rows; where it cannot (a contracted index that is no multiple of 8, an odd start), and
+// fp32 ones, they are first laid out in the workspace, fp32 numbers as three bf16 numbers each (24 bits, no exponent is lost): of their nine
+// products the six down to 2^-16 of the largest are made, the small ones first, by running through the contracted index six times.
 //
 // The weights are the MMA's first operand, 128 outputs, and a group's rows the second, as many as it has (16 .. 256 a tile): a group
 // of one row costs one pass over its weights and hardly any tensor time, a long one runs at the tensor core's pace, and no row
@@ -26,7 +30,10 @@ struct TcArgs {
     GroupedArgs g;
     CUtensorMap w, x;
     uint32_t out_tiles, shared_w;                            // shared_w: one set of weights for all groups
+    uint32_t passes, pitch;                                  // passes through the contracted index; from one part of an operand to the next
 };
+// fp32: which parts (0 the largest) of the weights and of the rows a pass multiplies
+__constant__ uint8_t kPartW[6] = { 0, 2, 1, 0, 1, 0 }, kPartX[6] = { 2, 0, 1, 1, 0, 0 };
 
 // K-major operand of rows of 128 bytes with the 128-byte swizzle, groups of 8 rows side by side
 __device__ __forceinline__ uint64_t desc_sw128(uint32_t addr)
@@ -94,7 +101,8 @@ struct Walk {
     }
 };
 
-template <typename T>
+// T: type of the operands, O: of bias and result
+template <typename T, typename O>
 __global__ void __launch_bounds__(kThreads, 1) k_grouped_tc(const __grid_constant__ TcArgs p)
 {
     extern __shared__ uint8_t raw[];
@@ -118,7 +126,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_grouped_tc(const __grid_constan
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = slot, steps = (a.n_in + 63u) / 64u;
+    const uint32_t tmem = slot, chunks = (a.n_in + 63u) / 64u, steps = chunks * p.passes;
     auto wait = [&](uint64_t* bar, uint32_t parity) {
         if (mbar_try_wait(smem_u32(bar), parity) || abort_flag) return;
         if (!mbar_wait_bounded(smem_u32(bar), parity, &limit)) abort_flag = 1;
@@ -133,15 +141,18 @@ __global__ void __launch_bounds__(kThreads, 1) k_grouped_tc(const __grid_constan
         for (uint64_t at = blockIdx.x; walk.find(a, at / p.out_tiles, &group, &row, &rows); at += gridDim.x) {
             if (rows == 0u) continue;
             const uint32_t o0 = static_cast<uint32_t>(at % p.out_tiles) * 128u, boxes = (rows + kBox - 1u) / kBox;
+            uint32_t pass = 0, chunk = 0;
             for (uint32_t k = 0; k < steps; ++k) {
                 wait(&empty[stage], phase ^ 1u);
                 if (aborted()) break;
                 if (lane == 0) {
                     const uint32_t bar = smem_u32(&full[stage]), to = smem + stage * (kWBytes + kXBytes);
                     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" :: "r"(bar), "r"(kWBytes + boxes * kBox * 128u) : "memory");
-                    copy3(to, &p.w, k * 64u, o0, p.shared_w ? 0u : group, bar);
-                    for (uint32_t b = 0; b < boxes; ++b) copy2(to + kWBytes + b * kBox * 128u, &p.x, k * 64u, static_cast<uint32_t>(row) + b * kBox, bar);
+                    const uint32_t kw = chunk * 64u + (p.passes > 1u ? kPartW[pass] * p.pitch : 0u), kx = chunk * 64u + (p.passes > 1u ? kPartX[pass] * p.pitch : 0u);
+                    copy3(to, &p.w, kw, o0, p.shared_w ? 0u : group, bar);
+                    for (uint32_t b = 0; b < boxes; ++b) copy2(to + kWBytes + b * kBox * 128u, &p.x, kx, static_cast<uint32_t>(row) + b * kBox, bar);
                 }
+                if (++chunk == chunks) { chunk = 0; ++pass; }
                 __syncwarp();
                 ++filled;
                 if (++stage == kStages) { stage = 0; phase ^= 1u; }
@@ -189,10 +200,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_grouped_tc(const __grid_constan
             const bool live = o < a.n_out;
             float bias = 0.f;
             if (a.b && live) {
-                const T b = static_cast<const T*>(a.b)[group * a.stride_b + o];
-                if constexpr (std::is_same<T, __half>::value) bias = __half2float(b); else bias = __bfloat162float(b);
+                const O b = static_cast<const O*>(a.b)[group * a.stride_b + o];
+                if constexpr (std::is_same<O, __half>::value) bias = __half2float(b);
+                else if constexpr (std::is_same<O, float>::value) bias = b;
+                else bias = __bfloat162float(b);
             }
-            T* const y = static_cast<T*>(a.y) + row * a.ld_y + o;
+            O* const y = static_cast<O*>(a.y) + row * a.ld_y + o;
             wait(&done[acc], acc_phase);
             tc_fence_after();
             // the halves take every other 32 rows
@@ -208,7 +221,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_grouped_tc(const __grid_constan
                             if (a.activation == EVO_ACT_TANH) v = gm::tanh32(v);
                             if (a.activation == EVO_ACT_RELU) v = v < 0.f ? 0.f : v;
                             v = abort_flag ? __int_as_float(0x7FC00000) : a.scale * v;
-                            if constexpr (std::is_same<T, __half>::value) y[(c + i) * a.ld_y] = __float2half_rn(v);
+                            if constexpr (std::is_same<O, __half>::value) y[(c + i) * a.ld_y] = __float2half_rn(v);
+                            else if constexpr (std::is_same<O, float>::value) y[(c + i) * a.ld_y] = v;
                             else y[(c + i) * a.ld_y] = __float2bfloat16_rn(v);
                         }
                 __syncwarp();
@@ -228,6 +242,51 @@ __global__ void __launch_bounds__(kThreads, 1) k_grouped_tc(const __grid_constan
     }
 }
 
+// Lays rows out for TMA: 16-bit ones as they are, fp32 ones as three bf16 parts, `pitch` apart and filled up with zeros.  Weight rows of groups that have
+// rows; or, where n_out is 0, the rows themselves.
+template <typename T>
+__global__ void __launch_bounds__(256) k_lay_out(const __grid_constant__ GroupedArgs a, const T* __restrict__ from, uint64_t stride, uint64_t ld, uint32_t n_out, uint16_t* __restrict__ to, uint32_t pitch)
+{
+    constexpr uint32_t kParts = std::is_same<T, float>::value ? 3u : 1u;
+    dep_wait();
+    dep_trigger();
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
+    uint64_t row = static_cast<uint64_t>(blockIdx.x) * 8u + warp, count = a.rows;      // a row a warp
+    const T* src = from;
+    if (n_out) {
+        const uint32_t per = (n_out + 7u) / 8u, group = blockIdx.x / per, o = blockIdx.x % per * 8u + warp;
+        uint64_t first = 0, end = 1;
+        if (stride || a.groups == 1u) group_rows(a, group, &first, &end);
+        if (first == end || o >= n_out) return;
+        src += group * stride + o * ld;
+        row = static_cast<uint64_t>(group) * n_out + o;
+        count = row + 1u;
+    } else {
+        src += row * ld;
+    }
+    if (row >= count) return;
+    uint16_t* const dst = to + row * kParts * pitch;
+    if constexpr (kParts == 1u) {                            // (the pitch is even; a number behind the last is written and never read)
+        const uint16_t* const s = reinterpret_cast<const uint16_t*>(src);
+        for (uint32_t k = 2u * lane; k < a.n_in; k += 64u)
+            *reinterpret_cast<uint32_t*>(dst + k) = s[k] | (k + 1u < a.n_in ? static_cast<uint32_t>(s[k + 1u]) << 16 : 0u);
+        return;
+    }
+    for (uint32_t k = lane; k < pitch; k += 32u) {
+        if constexpr (kParts == 3u) {
+            // (an infinity, and what rounds to one, has no further parts: their product with a zero would be NaN)
+            float x = k < a.n_in ? src[k] : 0.f;
+#pragma unroll
+            for (uint32_t p = 0; p < 3u; ++p) {
+                const __nv_bfloat16 b = __float2bfloat16_rn(x);
+                const float back = __bfloat162float(b);
+                dst[p * pitch + k] = __bfloat16_as_ushort(b);
+                x = isfinite(back) ? x - back : 0.f;
+            }
+        }
+    }
+}
+
 }  // namespace
 
 bool grouped_tc_takes(uint32_t type, const GroupedArgs& a)
@@ -237,19 +296,58 @@ bool grouped_tc_takes(uint32_t type, const GroupedArgs& a)
     return a.rows < (1ull << 31) && a.ld_x < (1ull << 38) && a.ld_w < (1ull << 38) && a.stride_w < (1ull << 38);
 }
 
-int launch_grouped_tc(cudaStream_t st, uint32_t type, const GroupedArgs& a)
+static uint32_t pitch_for(uint32_t type, uint32_t n_in) { return type == EVO_F32 ? (n_in + 63u) / 64u * 64u : (n_in + 7u) / 8u * 8u; }
+
+// Bytes for rows laid out anew where that pays (0: it does not): the weights are read, written and read again.  16-bit ones: against loads of single
+// numbers, from two rows a group on (6 groups, 3,774 rows, 207 -> 379: 364 us without, LAY_NOTE with).  fp32: against LAY32_NOTE
+size_t grouped_tc_bytes(uint32_t type, const GroupedArgs& a)
+{
+    const uint64_t pitch = pitch_for(type, a.n_in), parts = type == EVO_F32 ? 3u : 1u;
+    const bool shared = a.groups > 1u && a.stride_w == 0u;
+    if (a.rows >= (1ull << 31) || a.rows < (type == EVO_F32 ? 40ull : 4ull) * a.groups || (shared ? 1ull : a.groups) * a.n_out >= (1ull << 31)) return 0;
+    const uint64_t rows = (shared ? 1ull : a.groups) * a.n_out + a.rows;
+    return static_cast<size_t>(rows * parts * pitch * 2u + 256u);
+}
+
+int launch_grouped_tc(cudaStream_t st, uint32_t type, const GroupedArgs& in, void* work)
 {
     const EncodeTiled f = tensor_map_encoder();
     if (!f) return -1;
     TcArgs p;
-    p.g = a;
+    p.g = in;
+    GroupedArgs& a = p.g;
     p.out_tiles = (a.n_out + 127u) / 128u;
     p.shared_w = a.groups > 1u && a.stride_w == 0u;
+    p.passes = type == EVO_F32 ? 6u : 1u;
+    p.pitch = pitch_for(type, a.n_in);
+    int launches = 1;
+    uint64_t span = a.n_in;                                  // of the contracted index, all parts
+    if (work) {
+        const uint32_t parts = type == EVO_F32 ? 3u : 1u, sets = p.shared_w ? 1u : a.groups;
+        uint16_t* const w = static_cast<uint16_t*>(work);
+        uint16_t* const x = w + (static_cast<uint64_t>(sets) * a.n_out * parts * p.pitch + 127u) / 128u * 128u;
+        const uint64_t w_blocks = static_cast<uint64_t>(sets) * ((a.n_out + 7u) / 8u), x_blocks = (a.rows + 7u) / 8u;
+        if (w_blocks > 0x7FFFFFFFull || x_blocks > 0x7FFFFFFFull) return -2;
+        cudaError_t e;
+        if (type == EVO_F32) {
+            e = launch_dependent(k_lay_out<float>, dim3(static_cast<uint32_t>(w_blocks)), dim3(256), 0, st, a, static_cast<const float*>(a.w), a.stride_w, a.ld_w, a.n_out, w, p.pitch);
+            if (e == cudaSuccess) e = launch_dependent(k_lay_out<float>, dim3(static_cast<uint32_t>(x_blocks)), dim3(256), 0, st, a, static_cast<const float*>(a.x), 0ull, a.ld_x, 0u, x, p.pitch);
+        } else {
+            e = launch_dependent(k_lay_out<__half>, dim3(static_cast<uint32_t>(w_blocks)), dim3(256), 0, st, a, static_cast<const __half*>(a.w), a.stride_w, a.ld_w, a.n_out, w, p.pitch);
+            if (e == cudaSuccess) e = launch_dependent(k_lay_out<__half>, dim3(static_cast<uint32_t>(x_blocks)), dim3(256), 0, st, a, static_cast<const __half*>(a.x), 0ull, a.ld_x, 0u, x, p.pitch);
+        }
+        if (e != cudaSuccess) return -1;
+        launches = 3;
+        a.w = w; a.x = x;
+        a.ld_w = a.ld_x = static_cast<uint64_t>(parts) * p.pitch;
+        a.stride_w = p.shared_w ? 0u : a.ld_w * a.n_out;
+        if (type == EVO_F32) span = a.ld_w;
+    }
     const CUtensorMapDataType t = type == EVO_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
     // (a pitch of 0 is one that is never taken: any valid one stands in for it)
-    const uint64_t own = (a.n_in + 7ull) / 8ull * 8ull;
-    const cuuint64_t wd[3] = { a.n_in, a.n_out, p.shared_w ? 1u : a.groups }, ws[2] = { 2u * (a.ld_w ? a.ld_w : own), 2u * (a.stride_w ? a.stride_w : own) };
-    const cuuint64_t xd[2] = { a.n_in, a.rows }, xs[1] = { 2u * (a.ld_x ? a.ld_x : own) };
+    const uint64_t own = (span + 7ull) / 8ull * 8ull;
+    const cuuint64_t wd[3] = { span, a.n_out, p.shared_w ? 1u : a.groups }, ws[2] = { 2u * (a.ld_w ? a.ld_w : own), 2u * (a.stride_w ? a.stride_w : own) };
+    const cuuint64_t xd[2] = { span, a.rows }, xs[1] = { 2u * (a.ld_x ? a.ld_x : own) };
     const cuuint32_t wb[3] = { 64u, 128u, 1u }, xb[2] = { 64u, kBox }, one[3] = { 1u, 1u, 1u };
     if (f(&p.w, t, 3, const_cast<void*>(a.w), wd, ws, wb, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
           CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS ||
@@ -257,9 +355,9 @@ int launch_grouped_tc(cudaStream_t st, uint32_t type, const GroupedArgs& a)
           CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
         return -1;
     const uint64_t used = a.rows < a.groups ? a.rows : a.groups, most = (a.rows / kMostRows + used) * p.out_tiles;
-    auto kernel = type == EVO_F16 ? k_grouped_tc<__half> : k_grouped_tc<__nv_bfloat16>;
+    auto kernel = type == EVO_F16 ? k_grouped_tc<__half, __half> : type == EVO_BF16 ? k_grouped_tc<__nv_bfloat16, __nv_bfloat16> : k_grouped_tc<__nv_bfloat16, float>;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) != cudaSuccess) return -1;
-    return launch_dependent(kernel, dim3(most < kSms ? static_cast<uint32_t>(most) : kSms), dim3(kThreads), kSmem, st, p) == cudaSuccess ? 1 : -1;
+    return launch_dependent(kernel, dim3(most < kSms ? static_cast<uint32_t>(most) : kSms), dim3(kThreads), kSmem, st, p) == cudaSuccess ? launches : -1;
 }
 
 }  // namespace evo

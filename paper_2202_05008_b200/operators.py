@@ -186,7 +186,10 @@ def grouped_linear(x: torch.Tensor, weight: torch.Tensor, offsets: torch.Tensor,
                     x.data_ptr(), x.stride(0), weight.data_ptr(), pitch if n_out > 1 else n_in, stride,
                     None if bias is None else bias.data_ptr(), 0 if bias is None else bias.stride(0), offsets.data_ptr(), y.data_ptr(),
                     y.stride(0))
-        code = lib.evo_grouped_linear(C.byref(p), st)
+        need = C.c_size_t()
+        _check(lib.evo_grouped_linear_bytes(C.byref(p), C.byref(need)), where)
+        work = torch.empty(need.value, dtype=torch.uint8, device=device) if need.value else None
+        code = lib.evo_grouped_linear(C.byref(p), None if work is None else work.data_ptr(), need.value, st)
     _check(code, where)
     return y
 

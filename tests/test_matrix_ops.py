@@ -140,13 +140,31 @@ def _grouped(**kw):
                                  dict(offsets_64=1, d_offsets=4 * FAR + 4), dict(ld_x=9), dict(ld_y=19), dict(ld_weight=9), dict(weight_stride=1 << 41),
                                  dict(d_y=FAR + 4), dict(d_y=2 * FAR - 4), dict(d_y=3 * FAR), dict(d_y=4 * FAR), dict(groups=1 << 31)])
 def test_grouped_refusals(lib, bad):
-    assert lib.evo_grouped_linear(C.byref(_grouped(**bad)), None) == INVALID
+    assert lib.evo_grouped_linear(C.byref(_grouped(**bad)), FAR * 32, 1 << 40, None) == INVALID
 
 
 def test_grouped_without_rows_is_nothing_to_do(lib):
-    assert lib.evo_grouped_linear(C.byref(_grouped(rows=0, d_x=None, d_y=None)), None) == OK
-    assert lib.evo_grouped_linear(None, None) == INVALID
-    assert lib.evo_grouped_linear(C.byref(_grouped(groups=(1 << 31) - 1, n_out=1 << 20, ld_weight=12, weight_stride=0, ld_y=1 << 20, d_y=FAR * 64)), None) in (INVALID, UNSUPPORTED)
+    assert lib.evo_grouped_linear(C.byref(_grouped(rows=0, d_x=None, d_y=None)), None, 0, None) == OK
+    assert lib.evo_grouped_linear(None, None, 0, None) == INVALID
+    assert lib.evo_grouped_linear(C.byref(_grouped(groups=(1 << 31) - 1, n_out=1 << 20, ld_weight=12, weight_stride=0, ld_y=1 << 20, d_y=FAR * 64)), None, 0, None) in (INVALID, UNSUPPORTED)
+
+
+def test_grouped_workspace(lib):
+    n = C.c_size_t()
+
+    def need(**kw):
+        assert lib.evo_grouped_linear_bytes(C.byref(_grouped(**kw)), C.byref(n)) == OK, kw
+        return n.value
+    assert need() == 0 and need(rows=0) == 0                                    # few rows a group
+    many = dict(rows=4000, n_in=48, ld_x=48, ld_weight=48, weight_stride=960, n_out=20)
+    assert need(type=1, **many) == 0                                            # aligned 16-bit rows are taken as they lie
+    assert need(type=1, **dict(many, ld_x=49)) >= 2 * 48 * (4 * 20 + 4000)
+    assert need(type=0, **many) >= 3 * 2 * 48 * (4 * 20 + 4000)
+    p = _grouped(**many)
+    assert lib.evo_grouped_linear(C.byref(p), FAR * 32, n.value - 1, None) == WORKSPACE
+    assert lib.evo_grouped_linear(C.byref(p), FAR * 32 + 16, 1 << 40, None) == INVALID
+    assert lib.evo_grouped_linear(C.byref(p), None, 1 << 40, None) == INVALID
+    assert lib.evo_grouped_linear_bytes(C.byref(p), None) == INVALID
 
 
 def _actions(sizes=(5, 16, 16, 1), **kw):
