@@ -299,7 +299,9 @@ bool grouped_tc_takes(uint32_t type, const GroupedArgs& a)
 static uint32_t pitch_for(uint32_t type, uint32_t n_in) { return type == EVO_F32 ? (n_in + 63u) / 64u * 64u : (n_in + 7u) / 8u * 8u; }
 
 // Bytes for rows laid out anew where that pays (0: it does not): the weights are read, written and read again.  16-bit ones: against loads of single
-// numbers, from two rows a group on (6 groups, 3,774 rows, 207 -> 379: 364 us without, LAY_NOTE with).  fp32: against LAY32_NOTE
+// numbers, from four rows a group on (6 groups, 3,774 rows, 207 -> 379: 364 us without, 22 with).  fp32: three bf16 parts of each
+// number and six products, against pairs in tf32 with mma.sync, from 40 rows a group on (8 groups, 4,000 rows, 1,000 -> 500: 184 us
+// without, 88 with; with fewer rows the laying out costs more than the products).
 size_t grouped_tc_bytes(uint32_t type, const GroupedArgs& a)
 {
     const uint64_t pitch = pitch_for(type, a.n_in), parts = type == EVO_F32 ? 3u : 1u;

@@ -3,7 +3,7 @@
 //
 // A block holds up to 128 columns of X, as a pair of fp16 matrices in shared memory for the tensor core and in fp32 in the registers
 // of the threads that update them.  A step is three products, each followed by what turns its sums into operands, and nothing of it
-// overlaps: it is bound by that chain (128 x 128: CHAIN).
+// overlaps: it is bound by that chain (128 x 128: 38 us, 5.75 a step; 64 x 64: 21 us).
 // Blocks of a cluster each make the part of A that their columns give.  The parts go to their owners (block r adds up the r-th
 // share of A's columns, all parts in the order of the blocks) and the sums, as fp16 pairs, to everybody, both as bulk copies between
 // the blocks' shared memories; A^2 is then made by every block, B X for its own columns.  (Loads of the other blocks' parts by the

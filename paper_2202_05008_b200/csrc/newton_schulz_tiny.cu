@@ -5,7 +5,8 @@
 // g + 8, g = lane / 4).  Packed, that is the first operand of X X' and, rows 0-7 and 8-15 apart, also the second; transposed within
 // the warp (movmatrix) it is the second operand of B X, whose result comes out in the layout that X has.  The warps' parts of A are
 // added up in their order through shared memory, the blocks' of a cluster over distributed shared memory; then every warp has all of
-// A and makes A^2 and B for itself.  A step is two barriers and a few dozen MMAs long: TINY_TIME
+// A and makes A^2 and B for itself.  A step is two barriers and a few dozen MMAs long
+// and bound by the latency of its instructions (16 x 16: 1.46 us a step; 12 x 512, five steps: 16.9 us with its launch).
 #include "grouped_mma.cuh"
 #include "newton_schulz.cuh"
 

@@ -128,7 +128,7 @@ def muon_step(center: torch.Tensor, m: torch.Tensor, v: torch.Tensor, gradient: 
                  x.numel() == center.numel(), where, "contiguous fp32 vectors of one length on one GPU")
     ns = _newton_schulz(ns_steps, tuple(coefficients), eps, where)
     cfg = Muon(C.sizeof(Muon), 0 if nesterov else 1, lr, momentum, weight_decay, beta1, beta2, adam_eps, ns)
-    _require(step >= 1, where, "the step counts from 1")
+    _require(1 <= step < 1 << 32, where, "the step counts from 1")
     dim = center.numel()
     items, n, need = _matrix_list(tuple(map(tuple, matrices)), dim)
     with _On(center.device, stream) as st:
