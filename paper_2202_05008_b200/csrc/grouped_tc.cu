@@ -7,8 +7,11 @@
 // The weights are the MMA's first operand, 128 outputs, and a group's rows the second, as many as it has (16 .. 256 a tile): a group
 // of one row costs one pass over its weights and hardly any tensor time, a long one runs at the tensor core's pace, and no row
 // count is padded beyond 16.  Blocks stay and walk over (group, row tile, 128 outputs), the outputs of a row tile side by side, so
-// that its rows are read from L2.  A thread copies 64 of the contracted index a stage by TMA (weights 128 x 64, rows in boxes of 32), another
+// that its rows are read from L2.  A thread copies 64 of the contracted index a stage by TMA (weights 128 x 64, rows in boxes of 128, 64 and 32), another
 // issues the MMAs, eight warps take the sums of one tile out of tensor memory while the next tile's are under way.
+// 8,192 even rows of 4 groups, 4,096 -> 4,096: 225 us, 1,220 TFLOP/s; of 32 groups, 1,024 -> 4,096: 82 us (the weights alone are 41 from
+// memory).  What is left is the first loads, the last wave and, in ragged groups, tiles of few rows.
+#include <cmath>
 #include <type_traits>
 
 #include "grouped.h"
@@ -19,17 +22,17 @@
 namespace evo {
 namespace {
 
-constexpr uint32_t kStages = 4;
-constexpr uint32_t kMostRows = 256;                          // of a tile
-constexpr uint32_t kBox = 32;                                // rows of a copy
-constexpr uint32_t kWBytes = 128u * 128u, kXBytes = kMostRows * 128u;
-constexpr uint32_t kSmem = kStages * (kWBytes + kXBytes) + 1024u;
+constexpr uint32_t kMostStages = 8;
+constexpr uint32_t kMostRows = 256;                          // of a tile, at most
+constexpr uint32_t kWBytes = 128u * 128u;                    // of a stage; and as many for every 128 rows of a tile
+constexpr uint32_t kRing = 216u * 1024u, kSmem = kRing + 1024u;
 constexpr uint32_t kThreads = 320;
 
 struct TcArgs {
     GroupedArgs g;
-    CUtensorMap w, x;
+    CUtensorMap w, x[3];                                     // the rows in boxes of 32, 64 and 128
     uint32_t out_tiles, shared_w;                            // shared_w: one set of weights for all groups
+    uint32_t most_rows, stages;                              // of a tile (a multiple of 32); as many as the ring has room for
     uint32_t passes, pitch;                                  // passes through the contracted index; from one part of an operand to the next
 };
 // fp32: which parts (0 the largest) of the weights and of the rows a pass multiplies
@@ -65,12 +68,13 @@ struct Walk {
     uint64_t before = 0, first = 0, end = 0;                 // row tiles of earlier groups; the lane's rows
     uint32_t tiles = 0, upto = 0;                            // the lane's row tiles, and the running sum
 
-    __device__ __forceinline__ void fill(const GroupedArgs& a)
+    __device__ __forceinline__ void fill(const TcArgs& p)
     {
+        const GroupedArgs& a = p.g;
         const uint32_t lane = threadIdx.x & 31u;
         first = end = 0;
         if (base + lane < a.groups) group_rows(a, base + lane, &first, &end);
-        tiles = static_cast<uint32_t>((end - first + kMostRows - 1u) / kMostRows);
+        tiles = static_cast<uint32_t>((end - first + p.most_rows - 1u) / p.most_rows);
         upto = tiles;
 #pragma unroll
         for (uint32_t d = 1; d < 32u; d <<= 1) {
@@ -79,15 +83,15 @@ struct Walk {
         }
     }
     // row tile `at`: its group, first row and rows; false behind the last
-    __device__ __forceinline__ bool find(const GroupedArgs& a, uint64_t at, uint32_t* group, uint64_t* row, uint32_t* rows)
+    __device__ __forceinline__ bool find(const TcArgs& p, uint64_t at, uint32_t* group, uint64_t* row, uint32_t* rows)
     {
         for (;;) {
             const uint32_t here = __shfl_sync(0xffffffffu, upto, 31);
             if (at - before < here) break;
             before += here;
             base += 32u;
-            if (base >= a.groups) return false;
-            fill(a);
+            if (base >= p.g.groups) return false;
+            fill(p);
         }
         const uint32_t local = static_cast<uint32_t>(at - before);
         const uint32_t lane = __ffs(__ballot_sync(0xffffffffu, upto > local)) - 1;
@@ -106,14 +110,14 @@ template <typename T, typename O>
 __global__ void __launch_bounds__(kThreads, 1) k_grouped_tc(const __grid_constant__ TcArgs p)
 {
     extern __shared__ uint8_t raw[];
-    __shared__ __align__(8) uint64_t full[kStages], empty[kStages], done[2], taken[2], drain;
+    __shared__ __align__(8) uint64_t full[kMostStages], empty[kMostStages], done[2], taken[2], drain;
     __shared__ uint32_t slot, limit;
     __shared__ volatile int abort_flag;
     const GroupedArgs& a = p.g;
     const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31u;
     const uint32_t smem = (smem_u32(raw) + 1023u) / 1024u * 1024u;
     if (tid == 0) {
-        for (uint32_t s = 0; s < kStages; ++s) { mbar_init(smem_u32(&full[s]), 1); mbar_init(smem_u32(&empty[s]), 1); }
+        for (uint32_t s = 0; s < kMostStages; ++s) { mbar_init(smem_u32(&full[s]), 1); mbar_init(smem_u32(&empty[s]), 1); }
         for (uint32_t b = 0; b < 2u; ++b) { mbar_init(smem_u32(&done[b]), 1); mbar_init(smem_u32(&taken[b]), 8); }
         mbar_init(smem_u32(&drain), 1);
         mbar_init_fence();
@@ -126,46 +130,52 @@ __global__ void __launch_bounds__(kThreads, 1) k_grouped_tc(const __grid_constan
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = slot, chunks = (a.n_in + 63u) / 64u, steps = chunks * p.passes;
+    const uint32_t tmem = slot, chunks = (a.n_in + 63u) / 64u, steps = chunks * p.passes, stages = p.stages;
+    const uint32_t stage_bytes = kWBytes + p.most_rows * 128u;
     auto wait = [&](uint64_t* bar, uint32_t parity) {
         if (mbar_try_wait(smem_u32(bar), parity) || abort_flag) return;
         if (!mbar_wait_bounded(smem_u32(bar), parity, &limit)) abort_flag = 1;
     };
     auto aborted = [&] { return __any_sync(0xffffffffu, abort_flag) != 0; };
     Walk walk;
-    walk.fill(a);
+    walk.fill(p);
     uint32_t group, rows, stage = 0, phase = 0, acc = 0, acc_phase = 0, filled = 0;
     uint64_t row;
 
     if (warp == 0) {
-        for (uint64_t at = blockIdx.x; walk.find(a, at / p.out_tiles, &group, &row, &rows); at += gridDim.x) {
+        for (uint64_t at = blockIdx.x; walk.find(p, at / p.out_tiles, &group, &row, &rows); at += gridDim.x) {
             if (rows == 0u) continue;
-            const uint32_t o0 = static_cast<uint32_t>(at % p.out_tiles) * 128u, boxes = (rows + kBox - 1u) / kBox;
+            const uint32_t o0 = static_cast<uint32_t>(at % p.out_tiles) * 128u, read = (rows + 31u) / 32u * 32u;
             uint32_t pass = 0, chunk = 0;
             for (uint32_t k = 0; k < steps; ++k) {
                 wait(&empty[stage], phase ^ 1u);
                 if (aborted()) break;
                 if (lane == 0) {
-                    const uint32_t bar = smem_u32(&full[stage]), to = smem + stage * (kWBytes + kXBytes);
-                    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" :: "r"(bar), "r"(kWBytes + boxes * kBox * 128u) : "memory");
+                    const uint32_t bar = smem_u32(&full[stage]), to = smem + stage * stage_bytes;
+                    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" :: "r"(bar), "r"(kWBytes + read * 128u) : "memory");
                     const uint32_t kw = chunk * 64u + (p.passes > 1u ? kPartW[pass] * p.pitch : 0u), kx = chunk * 64u + (p.passes > 1u ? kPartX[pass] * p.pitch : 0u);
                     copy3(to, &p.w, kw, o0, p.shared_w ? 0u : group, bar);
-                    for (uint32_t b = 0; b < boxes; ++b) copy2(to + kWBytes + b * kBox * 128u, &p.x, kx, static_cast<uint32_t>(row) + b * kBox, bar);
+                    // (as few copies as make up the rows: 8,192 of 4 groups, 4,096 -> 4,096, 323 us with 32 rows each, 242 with 128)
+                    for (uint32_t b = 0; b < read;) {
+                        const uint32_t box = read - b >= 128u ? 2u : read - b >= 64u ? 1u : 0u;
+                        copy2(to + kWBytes + b * 128u, &p.x[box], kx, static_cast<uint32_t>(row) + b, bar);
+                        b += 32u << box;
+                    }
                 }
                 if (++chunk == chunks) { chunk = 0; ++pass; }
                 __syncwarp();
                 ++filled;
-                if (++stage == kStages) { stage = 0; phase ^= 1u; }
+                if (++stage == stages) { stage = 0; phase ^= 1u; }
             }
             if (aborted()) break;
         }
         if (aborted())                                       // nothing may land after the block has gone
-            for (uint32_t s = 0; s < min(filled, kStages); ++s) {
+            for (uint32_t s = 0; s < min(filled, stages); ++s) {
                 const uint32_t nth = filled - 1u - s;
-                mbar_wait_bounded(smem_u32(&full[nth % kStages]), nth / kStages & 1u, &limit);
+                mbar_wait_bounded(smem_u32(&full[nth % stages]), nth / stages & 1u, &limit);
             }
     } else if (warp == 1) {
-        for (uint64_t at = blockIdx.x; walk.find(a, at / p.out_tiles, &group, &row, &rows); at += gridDim.x) {
+        for (uint64_t at = blockIdx.x; walk.find(p, at / p.out_tiles, &group, &row, &rows); at += gridDim.x) {
             if (rows == 0u) continue;
             const uint32_t d = tmem + acc * kMostRows, id = idesc<T>((rows + 15u) / 16u * 16u);
             wait(&taken[acc], acc_phase ^ 1u);
@@ -174,14 +184,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_grouped_tc(const __grid_constan
                 tc_fence_after();
                 if (aborted()) break;
                 if (lane == 0) {
-                    const uint32_t w = smem + stage * (kWBytes + kXBytes);
+                    const uint32_t w = smem + stage * stage_bytes;
 #pragma unroll
                     for (uint32_t s = 0; s < 4u; ++s) umma_bf16(d, desc_sw128(w + s * 32u), desc_sw128(w + kWBytes + s * 32u), id, k + s != 0u);
                     umma_commit(smem_u32(&empty[stage]));
                     if (k + 1u == steps) umma_commit(smem_u32(&done[acc]));
                 }
                 __syncwarp();
-                if (++stage == kStages) { stage = 0; phase ^= 1u; }
+                if (++stage == stages) { stage = 0; phase ^= 1u; }
             }
             if (aborted()) break;
             acc ^= 1u;
@@ -194,7 +204,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_grouped_tc(const __grid_constan
         }
     } else {
         const uint32_t quarter = warp & 3u, half = (warp - 2u) >> 2;
-        for (uint64_t at = blockIdx.x; walk.find(a, at / p.out_tiles, &group, &row, &rows); at += gridDim.x) {
+        for (uint64_t at = blockIdx.x; walk.find(p, at / p.out_tiles, &group, &row, &rows); at += gridDim.x) {
             if (rows == 0u) continue;
             const uint32_t o = static_cast<uint32_t>(at % p.out_tiles) * 128u + quarter * 32u + lane;
             const bool live = o < a.n_out;
@@ -208,23 +218,33 @@ __global__ void __launch_bounds__(kThreads, 1) k_grouped_tc(const __grid_constan
             O* const y = static_cast<O*>(a.y) + row * a.ld_y + o;
             wait(&done[acc], acc_phase);
             tc_fence_after();
+            const float scale = abort_flag ? __int_as_float(0x7FC00000) : a.scale;
             // the halves take every other 32 rows
             for (uint32_t c = half * 32u; c < rows; c += 64u) {
                 uint32_t u[4][8];
                 tmem_ld32_issue(tmem + acc * kMostRows + (quarter << 21) + c, u);
                 tmem_ld8x4_fence(u[0], u[1], u[2], u[3]);
-                if (live)
+                float v[32];
 #pragma unroll
-                    for (uint32_t i = 0; i < 32u; ++i)
-                        if (c + i < rows) {
-                            float v = __uint_as_float(u[i / 8u][i % 8u]) + bias;
-                            if (a.activation == EVO_ACT_TANH) v = gm::tanh32(v);
-                            if (a.activation == EVO_ACT_RELU) v = v < 0.f ? 0.f : v;
-                            v = abort_flag ? __int_as_float(0x7FC00000) : a.scale * v;
-                            if constexpr (std::is_same<O, __half>::value) y[(c + i) * a.ld_y] = __float2half_rn(v);
-                            else if constexpr (std::is_same<O, float>::value) y[(c + i) * a.ld_y] = v;
-                            else y[(c + i) * a.ld_y] = __float2bfloat16_rn(v);
-                        }
+                for (uint32_t i = 0; i < 32u; ++i) v[i] = __uint_as_float(u[i / 8u][i % 8u]) + bias;
+                if (a.activation == EVO_ACT_TANH) {
+#pragma unroll
+                    for (uint32_t i = 0; i < 32u; ++i) v[i] = gm::tanh32(v[i]);
+                } else if (a.activation == EVO_ACT_RELU) {
+#pragma unroll
+                    for (uint32_t i = 0; i < 32u; ++i) v[i] = v[i] < 0.f ? 0.f : v[i];
+                }
+                O* to = y + c * a.ld_y;
+                const uint32_t count = live ? min(32u, rows - c) : 0u;
+#pragma unroll
+                for (uint32_t i = 0; i < 32u; ++i) {
+                    if (i < count) {
+                        if constexpr (std::is_same<O, __half>::value) *to = __float2half_rn(scale * v[i]);
+                        else if constexpr (std::is_same<O, float>::value) *to = scale * v[i];
+                        else *to = __float2bfloat16_rn(scale * v[i]);
+                    }
+                    to += a.ld_y;
+                }
                 __syncwarp();
             }
             tc_fence_before();
@@ -270,10 +290,8 @@ __global__ void __launch_bounds__(256) k_lay_out(const __grid_constant__ Grouped
         const uint16_t* const s = reinterpret_cast<const uint16_t*>(src);
         for (uint32_t k = 2u * lane; k < a.n_in; k += 64u)
             *reinterpret_cast<uint32_t*>(dst + k) = s[k] | (k + 1u < a.n_in ? static_cast<uint32_t>(s[k + 1u]) << 16 : 0u);
-        return;
-    }
-    for (uint32_t k = lane; k < pitch; k += 32u) {
-        if constexpr (kParts == 3u) {
+    } else {
+        for (uint32_t k = lane; k < pitch; k += 32u) {
             // (an infinity, and what rounds to one, has no further parts: their product with a zero would be NaN)
             float x = k < a.n_in ? src[k] : 0.f;
 #pragma unroll
@@ -301,7 +319,7 @@ static uint32_t pitch_for(uint32_t type, uint32_t n_in) { return type == EVO_F32
 // Bytes for rows laid out anew where that pays (0: it does not): the weights are read, written and read again.  16-bit ones: against loads of single
 // numbers, from four rows a group on (6 groups, 3,774 rows, 207 -> 379: 364 us without, 22 with).  fp32: three bf16 parts of each
 // number and six products, against pairs in tf32 with mma.sync, from 40 rows a group on (8 groups, 4,000 rows, 1,000 -> 500: 184 us
-// without, 88 with; with fewer rows the laying out costs more than the products).
+// without, 75 with; with fewer rows the laying out costs more than the products).
 size_t grouped_tc_bytes(uint32_t type, const GroupedArgs& a)
 {
     const uint64_t pitch = pitch_for(type, a.n_in), parts = type == EVO_F32 ? 3u : 1u;
@@ -309,6 +327,22 @@ size_t grouped_tc_bytes(uint32_t type, const GroupedArgs& a)
     if (a.rows >= (1ull << 31) || a.rows < (type == EVO_F32 ? 40ull : 4ull) * a.groups || (shared ? 1ull : a.groups) * a.n_out >= (1ull << 31)) return 0;
     const uint64_t rows = (shared ? 1ull : a.groups) * a.n_out + a.rows;
     return static_cast<size_t>(rows * parts * pitch * 2u + 256u);
+}
+
+// Rows of a tile, at most.  The groups' sizes are on the device, so their tiles are guessed at (a tile for every so many rows and half a one
+// more a group); a tile takes as long as its operands, 128 rows of weights and its own rows, and the blocks take tiles in waves.  64 / 128 / 192 /
+// 256 rows: 8,192 even rows of 32 groups, 1,024 -> 4,096, 209 / 119 / 118 / 82 us; 3,774 of 6, 1,207 -> 2,379, 103 / 81 / 69 / 73;
+// 3,000 of 100, 1,024 -> 1,024, 55 / 59 / 59 / 64 (fewer rows a stage are more stages in flight).
+static uint32_t rows_of_a_tile(const GroupedArgs& a, uint32_t out_tiles)
+{
+    uint32_t best = kMostRows;
+    double least = 1e300;
+    for (uint32_t most = 64u; most <= kMostRows; most += 64u) {
+        const double used = static_cast<double>(a.rows < a.groups ? a.rows : a.groups), guess = static_cast<double>(a.rows) / most + 0.5 * used;
+        const double tiles = guess > used ? guess : used, time = std::ceil(tiles * out_tiles / kSms) * (128.0 + a.rows / tiles);
+        if (time < least * 0.999) { least = time; best = most; }
+    }
+    return best;
 }
 
 int launch_grouped_tc(cudaStream_t st, uint32_t type, const GroupedArgs& in, void* work)
@@ -350,13 +384,18 @@ int launch_grouped_tc(cudaStream_t st, uint32_t type, const GroupedArgs& in, voi
     const uint64_t own = (span + 7ull) / 8ull * 8ull;
     const cuuint64_t wd[3] = { span, a.n_out, p.shared_w ? 1u : a.groups }, ws[2] = { 2u * (a.ld_w ? a.ld_w : own), 2u * (a.stride_w ? a.stride_w : own) };
     const cuuint64_t xd[2] = { span, a.rows }, xs[1] = { 2u * (a.ld_x ? a.ld_x : own) };
-    const cuuint32_t wb[3] = { 64u, 128u, 1u }, xb[2] = { 64u, kBox }, one[3] = { 1u, 1u, 1u };
+    const cuuint32_t wb[3] = { 64u, 128u, 1u }, xb[3][2] = { { 64u, 32u }, { 64u, 64u }, { 64u, 128u } }, one[3] = { 1u, 1u, 1u };
     if (f(&p.w, t, 3, const_cast<void*>(a.w), wd, ws, wb, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-          CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS ||
-        f(&p.x, t, 2, const_cast<void*>(a.x), xd, xs, xb, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
           CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
         return -1;
-    const uint64_t used = a.rows < a.groups ? a.rows : a.groups, most = (a.rows / kMostRows + used) * p.out_tiles;
+    for (int box = 0; box < 3; ++box)
+        if (f(&p.x[box], t, 2, const_cast<void*>(a.x), xd, xs, xb[box], one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+            return -1;
+    p.most_rows = rows_of_a_tile(a, p.out_tiles);
+    p.stages = kRing / (kWBytes + p.most_rows * 128u);
+    if (p.stages > kMostStages) p.stages = kMostStages;
+    const uint64_t used = a.rows < a.groups ? a.rows : a.groups, most = (a.rows / p.most_rows + used) * p.out_tiles;
     auto kernel = type == EVO_F16 ? k_grouped_tc<__half, __half> : type == EVO_BF16 ? k_grouped_tc<__nv_bfloat16, __nv_bfloat16> : k_grouped_tc<__nv_bfloat16, float>;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) != cudaSuccess) return -1;
     return launch_dependent(kernel, dim3(most < kSms ? static_cast<uint32_t>(most) : kSms), dim3(kThreads), kSmem, st, p) == cudaSuccess ? launches : -1;

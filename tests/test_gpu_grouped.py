@@ -71,6 +71,15 @@ def test_sizes_and_types(groups, lengths, n_in, n_out, dtype):
     check(grouped_linear(x, w, off, b, activation="tanh", scale=2.5), x, w, off, b, "tanh", 2.5)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("n_in,n_out", [(72, 130), (648, 500), (264, 1200), (1032, 1500)])      # tiles of up to 64, 128, 192 and 256 rows
+def test_groups_of_every_part_of_a_tile(n_in, n_out, dtype):
+    x, w, b, off = make(18, [1, 31, 33, 0, 63, 65, 97, 129, 161, 191, 193, 225, 255, 257, 300, 511, 513, 7], n_in, n_out, dtype, tail=3)
+    y = torch.full((x.shape[0], n_out), 7.0, dtype=dtype, device="cuda")
+    check(grouped_linear(x, w, off, b, activation="relu", scale=0.5, out=y), x, w, off, b, "relu", 0.5)
+    assert (y[-3:] == 7).all()
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("n_in,n_out,shift", [(64, 48, 0), (64, 48, 1), (61, 48, 0), (256, 136, 3), (256, 136, 8)])
 def test_strides_alignment_and_rows_outside_of_the_groups(dtype, n_in, n_out, shift):
