@@ -318,13 +318,14 @@ static uint32_t pitch_for(uint32_t type, uint32_t n_in) { return type == EVO_F32
 
 // Bytes for rows laid out anew where that pays (0: it does not): the weights are read, written and read again.  16-bit ones: against loads of single
 // numbers, from four rows a group on (6 groups, 3,774 rows, 207 -> 379: 364 us without, 22 with).  fp32: three bf16 parts of each
-// number and six products, against pairs in tf32 with mma.sync, from 40 rows a group on (8 groups, 4,000 rows, 1,000 -> 500: 184 us
-// without, 75 with; with fewer rows the laying out costs more than the products).
+// number and six products, against pairs in tf32 with mma.sync, from 28 rows a group on (without / with:
+// 8 groups, 4,000 rows, 1,000 -> 500, 184 / 75 us; 300 of 9,000, 128 -> 128, 135 / 46; 100 of 3,000, 512 -> 512, 170 / 124, of 2,000 100 / 124;
+// 50 of 1,500, 1,000 -> 1,000, 178 / 224).
 size_t grouped_tc_bytes(uint32_t type, const GroupedArgs& a)
 {
     const uint64_t pitch = pitch_for(type, a.n_in), parts = type == EVO_F32 ? 3u : 1u;
     const bool shared = a.groups > 1u && a.stride_w == 0u;
-    if (a.rows >= (1ull << 31) || a.rows < (type == EVO_F32 ? 40ull : 4ull) * a.groups || (shared ? 1ull : a.groups) * a.n_out >= (1ull << 31)) return 0;
+    if (a.rows >= (1ull << 31) || a.rows < (type == EVO_F32 ? 28ull : 4ull) * a.groups || (shared ? 1ull : a.groups) * a.n_out >= (1ull << 31)) return 0;
     const uint64_t rows = (shared ? 1ull : a.groups) * a.n_out + a.rows;
     return static_cast<size_t>(rows * parts * pitch * 2u + 256u);
 }
