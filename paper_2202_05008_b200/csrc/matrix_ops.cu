@@ -91,6 +91,7 @@ int launch(cudaStream_t st, uint32_t source, const Matrix* list, size_t n, const
                 }
                 a.blocks = static_cast<uint32_t>(blocks);
                 if (a.groups == 0u) continue;
+                a.late = launches > 0;
                 const int k = kind == kSmall ? launch_small(st, source, a, smem) : launch_tiny(st, source, a, kind + 1u, std::min(16u, columns / 16u));
                 if (k < 0) return -1;
                 launches += k;
@@ -120,18 +121,16 @@ struct GapArgs {
     float *c_out, *m_out, *v_out;
     const double* skip;
     const uint32_t* d_step;
-    uint32_t step, gaps;
+    uint32_t step, gaps, late;           // late: as in Args
     double beta1, beta2;
     float lr, keep, b1, b2, rest1, rest2, eps;      // (rest = 1 - beta)
     uint64_t start[kMaxGaps];
     uint64_t before[kMaxGaps + 1];       // elements of the gaps before this one
 };
 
-__global__ void __launch_bounds__(256) k_muon_rest(const __grid_constant__ GapArgs a)
+__device__ __forceinline__ void muon_rest(const GapArgs& a)
 {
-    dep_wait();
-    dep_trigger();
-    if (a.skip && *a.skip == 0.0) return;
+    if (a.skip && __ldcg(a.skip) == 0.0) return;
     const uint64_t at = static_cast<uint64_t>(blockIdx.x) * 256u + threadIdx.x;
     if (at >= a.before[a.gaps]) return;
     uint32_t lo = 0, hi = a.gaps - 1u;                          // the last gap that starts at or before `at`
@@ -140,13 +139,21 @@ __global__ void __launch_bounds__(256) k_muon_rest(const __grid_constant__ GapAr
         if (a.before[mid] <= at) lo = mid; else hi = mid - 1u;
     }
     const uint64_t d = a.start[lo] + (at - a.before[lo]);
-    const double t = a.d_step ? *a.d_step : a.step;
+    const double t = a.d_step ? __ldcg(a.d_step) : a.step;
     const float corr1 = static_cast<float>(1.0 / (1.0 - pow(a.beta1, t)));
     const float corr2 = static_cast<float>(1.0 / (1.0 - pow(a.beta2, t)));
-    const float g = a.g[d], m = a.b1 * a.m[d] + a.rest1 * g, v = a.b2 * a.v[d] + a.rest2 * g * g;
+    const float g = __ldcg(a.g + d), m = a.b1 * __ldcg(a.m + d) + a.rest1 * g, v = a.b2 * __ldcg(a.v + d) + a.rest2 * g * g;
     a.m_out[d] = m;
     a.v_out[d] = v;
-    a.c_out[d] = a.keep * a.c[d] + a.lr * (m * corr1) / (sqrtf(v * corr2) + a.eps);
+    a.c_out[d] = a.keep * __ldcg(a.c + d) + a.lr * (m * corr1) / (sqrtf(v * corr2) + a.eps);
+}
+
+__global__ void __launch_bounds__(256) k_muon_rest(const __grid_constant__ GapArgs a)
+{
+    if (!a.late) dep_wait();
+    dep_trigger();
+    muon_rest(a);
+    if (a.late) dep_wait();
 }
 
 static std::vector<ns::Matrix> muon_list(const evo_matrix* list, size_t n, double lr)
@@ -208,6 +215,7 @@ try {
         }
         if (r.gaps == 0u) continue;
         const uint64_t blocks = (r.before[r.gaps] + 255u) / 256u;
+        r.late = launches > 0;
         if (launch_dependent(k_muon_rest, dim3(static_cast<uint32_t>(blocks)), dim3(256), 0, st, r) != cudaSuccess) return -1;
         ++launches;
     }

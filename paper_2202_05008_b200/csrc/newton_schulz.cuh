@@ -45,39 +45,49 @@ struct Waits {
     }
 };
 
+// LATE: from L2, see Args
+template <bool LATE, typename T>
+__device__ __forceinline__ T fetch(const T* p)
+{
+    if constexpr (LATE) return __ldcg(p);
+    else return *p;
+}
+
 // (1 - mu) g and mu m' are rounded once each
-template <uint32_t SRC>
+__device__ __forceinline__ float muon_direction(const Args& a, float gradient, float m, float* momentum)
+{
+    const float g = a.s.rest * gradient;
+    *momentum = fmaf(a.s.mu, m, g);
+    return a.s.nesterov ? fmaf(a.s.mu, *momentum, g) : *momentum;
+}
+template <uint32_t SRC, bool LATE>
 __device__ __forceinline__ float load(const Args& a, uint64_t at, float* momentum)
 {
     if constexpr (SRC == kF32) return static_cast<const float*>(a.in)[at];
     if constexpr (SRC == kBf16) return __bfloat162float(static_cast<const __nv_bfloat16*>(a.in)[at]);
     if constexpr (SRC == kF16) return __half2float(static_cast<const __half*>(a.in)[at]);
-    if constexpr (SRC == kMuon) {
-        const float g = a.s.rest * static_cast<const float*>(a.in)[at];
-        const float m = fmaf(a.s.mu, a.m_in[at], g);
-        *momentum = m;
-        return a.s.nesterov ? fmaf(a.s.mu, m, g) : m;
-    }
+    if constexpr (SRC == kMuon) return muon_direction(a, fetch<LATE>(static_cast<const float*>(a.in) + at), fetch<LATE>(a.m_in + at), momentum);
 }
 
 // the momentum of a matrix element, and its second moment as it was (Adam's, which matrices do not use)
+template <bool LATE>
 __device__ __forceinline__ void store_moments(const Args& a, uint64_t at, float momentum)
 {
     a.m_out[at] = momentum;
-    if (a.v_out != a.v_in) a.v_out[at] = a.v_in[at];
+    if (a.v_out != a.v_in) a.v_out[at] = fetch<LATE>(a.v_in + at);
 }
 
-template <uint32_t SRC>
+template <uint32_t SRC, bool LATE>
 __device__ __forceinline__ void store(const Args& a, uint64_t at, float x, float gain)
 {
     if constexpr (SRC == kF32) static_cast<float*>(a.out)[at] = x;
     if constexpr (SRC == kBf16) static_cast<__nv_bfloat16*>(a.out)[at] = __float2bfloat16_rn(x);
     if constexpr (SRC == kF16) static_cast<__half*>(a.out)[at] = __float2half_rn(x);
-    if constexpr (SRC == kMuon) static_cast<float*>(a.out)[at] = fmaf(gain, x, a.s.keep * a.c_in[at]);
+    if constexpr (SRC == kMuon) static_cast<float*>(a.out)[at] = fmaf(gain, x, a.s.keep * fetch<LATE>(a.c_in + at));
 }
 
-// Eight elements from `at` on, `step` apart, of which `count` exist (the others are 0); what Muon updates on the way is updated.
-template <uint32_t SRC>
+// Eight elements from `at` on, `step` apart, of which `count` exist (the others are 0).  UPDATE: what Muon updates on the way is updated.
+template <uint32_t SRC, bool LATE, bool UPDATE>
 __device__ __forceinline__ void load8(const Args& a, uint64_t at, uint32_t step, uint32_t count, float (&x)[8])
 {
     if constexpr (SRC == kF32) {
@@ -88,16 +98,49 @@ __device__ __forceinline__ void load8(const Args& a, uint64_t at, uint32_t step,
             return;
         }
     }
+    float momentum[8];
+    if constexpr (SRC == kMuon) {
+        const float* const g = static_cast<const float*>(a.in) + at;
+        const float* const m = a.m_in + at;
+        if (step == 1u && count == 8u && ((reinterpret_cast<uintptr_t>(g) | reinterpret_cast<uintptr_t>(m) | reinterpret_cast<uintptr_t>(a.m_out + at)) & 15u) == 0u) {
 #pragma unroll
-    for (uint32_t e = 0; e < 8u; ++e) {
-        float momentum = 0.f;
-        x[e] = e < count ? load<SRC>(a, at + static_cast<uint64_t>(e) * step, &momentum) : 0.f;
-        if constexpr (SRC == kMuon)
-            if (e < count) store_moments(a, at + static_cast<uint64_t>(e) * step, momentum);
+            for (uint32_t h = 0; h < 8u; h += 4u) {
+                const float4 u = fetch<LATE>(reinterpret_cast<const float4*>(g + h)), v = fetch<LATE>(reinterpret_cast<const float4*>(m + h));
+                x[h] = muon_direction(a, u.x, v.x, &momentum[h]);
+                x[h + 1u] = muon_direction(a, u.y, v.y, &momentum[h + 1u]);
+                x[h + 2u] = muon_direction(a, u.z, v.z, &momentum[h + 2u]);
+                x[h + 3u] = muon_direction(a, u.w, v.w, &momentum[h + 3u]);
+            }
+#pragma unroll
+            for (uint32_t h = 0; UPDATE && h < 8u; h += 4u)
+                *reinterpret_cast<float4*>(a.m_out + at + h) = make_float4(momentum[h], momentum[h + 1u], momentum[h + 2u], momentum[h + 3u]);
+            if (UPDATE && a.v_out != a.v_in) {
+                const float4* const v4 = reinterpret_cast<const float4*>(a.v_in + at);
+                if (((reinterpret_cast<uintptr_t>(v4) | reinterpret_cast<uintptr_t>(a.v_out + at)) & 15u) == 0u) {
+                    const float4 p = fetch<LATE>(v4), q = fetch<LATE>(v4 + 1);
+                    *reinterpret_cast<float4*>(a.v_out + at) = p;
+                    *reinterpret_cast<float4*>(a.v_out + at + 4u) = q;
+                    return;
+                }
+                float v[8];
+#pragma unroll
+                for (uint32_t e = 0; e < 8u; ++e) v[e] = fetch<LATE>(a.v_in + at + e);
+#pragma unroll
+                for (uint32_t e = 0; e < 8u; ++e) a.v_out[at + e] = v[e];
+            }
+            return;
+        }
+    }
+#pragma unroll
+    for (uint32_t e = 0; e < 8u; ++e) x[e] = e < count ? load<SRC, LATE>(a, at + static_cast<uint64_t>(e) * step, &momentum[e]) : 0.f;
+    if constexpr (SRC == kMuon && UPDATE) {
+#pragma unroll
+        for (uint32_t e = 0; e < 8u; ++e)
+            if (e < count) store_moments<LATE>(a, at + static_cast<uint64_t>(e) * step, momentum[e]);
     }
 }
 // four neighbouring elements of the result, of which `count` (or more) exist
-template <uint32_t SRC>
+template <uint32_t SRC, bool LATE>
 __device__ __forceinline__ void store4(const Args& a, uint64_t at, const float4& v, uint32_t count, float gain)
 {
     if constexpr (SRC == kF32) {
@@ -107,10 +150,19 @@ __device__ __forceinline__ void store4(const Args& a, uint64_t at, const float4&
             return;
         }
     }
+    if constexpr (SRC == kMuon) {
+        float* const p = static_cast<float*>(a.out) + at;
+        if (count >= 4u && ((reinterpret_cast<uintptr_t>(p) | reinterpret_cast<uintptr_t>(a.c_in + at)) & 15u) == 0u) {
+            const float4 c = fetch<LATE>(reinterpret_cast<const float4*>(a.c_in + at));
+            *reinterpret_cast<float4*>(p) = make_float4(fmaf(gain, v.x, a.s.keep * c.x), fmaf(gain, v.y, a.s.keep * c.y),
+                                                        fmaf(gain, v.z, a.s.keep * c.z), fmaf(gain, v.w, a.s.keep * c.w));
+            return;
+        }
+    }
     const float x[4] = { v.x, v.y, v.z, v.w };
 #pragma unroll
     for (uint32_t e = 0; e < 4u; ++e)
-        if (e < count) store<SRC>(a, at + e, x[e], gain);
+        if (e < count) store<SRC, LATE>(a, at + e, x[e], gain);
 }
 
 // element (i, j) of the m x n matrix in the source or the result

@@ -8,8 +8,8 @@
 // through the ring as well.  An MMA of 128 x 128 is bound by its operands' way out of shared memory (104 clocks instead of 64), so the high
 // parts of the first operand meet the high and low parts of the second, which lie side by side, in one MMA of 128 x 256.
 // A and B are symmetric: tiles on and under the diagonal only, written twice.
-// 2048 x 2048, five steps: 0.63 ms, of which 9 us a launch are its start, its first loads and its last tile; the three passes of fp16
-// would take 0.31 ms at the rate of a large library product.  256 x 256 and 32 of 512 x 1,408 are mostly starts and ends: 150 us, 1.0 ms.
+// 2048 x 2048, five steps: 0.64 ms, of which 9 us a launch are its start, its first loads and its last tile; the three passes of fp16
+// would take 0.31 ms at the rate of a large library product.  256 x 256 and 32 of 512 x 1,408 are mostly starts and ends: 150 us, 1 ms.
 #include <algorithm>
 
 #include "newton_schulz.cuh"
@@ -63,12 +63,11 @@ __global__ void __launch_bounds__(256) k_ns_norm(const __grid_constant__ Args a)
     for (uint32_t t = threadIdx.x; t < kTile * 8u; t += 256u) {
         uint32_t i, jc;
         piece_place(g, t, i, jc);
+        const uint32_t j = j0 + jc * 8u, count = i0 + i < g.m && j < g.n ? min(8u, g.n - j) : 0u;
+        float x[8];
+        load8<SRC, false, false>(a, in_index(g, which, i0 + i, j), g.tall ? g.in_ld : 1u, count, x);
 #pragma unroll
-        for (uint32_t e = 0; e < 8u; ++e) {
-            float unused;
-            const double x = i0 + i < g.m && j0 + jc * 8u + e < g.n ? load<SRC>(a, in_index(g, which, i0 + i, j0 + jc * 8u + e), &unused) : 0.f;
-            sum += x * x;
-        }
+        for (uint32_t e = 0; e < 8u; ++e) sum += static_cast<double>(x[e]) * x[e];
     }
     sum = block_sum<256>(sum, red);
     if (threadIdx.x == 0) a.partial[blockIdx.x] = sum;
@@ -95,16 +94,10 @@ __global__ void __launch_bounds__(256) k_ns_split(const __grid_constant__ Args a
         uint32_t i, jc;
         piece_place(g, t, i, jc);
         float x[8];
+        const uint32_t j = j0 + jc * 8u, count = i0 + i < g.m && j < g.n ? min(8u, g.n - j) : 0u;
+        load8<SRC, false, true>(a, in_index(g, which, i0 + i, j), g.tall ? g.in_ld : 1u, count, x);
 #pragma unroll
-        for (uint32_t e = 0; e < 8u; ++e) {
-            x[e] = 0.f;
-            if (i0 + i < g.m && j0 + jc * 8u + e < g.n) {
-                const uint64_t from = in_index(g, which, i0 + i, j0 + jc * 8u + e);
-                float momentum;
-                x[e] = static_cast<float>(scale * load<SRC>(a, from, &momentum));
-                if constexpr (SRC == kMuon) store_moments(a, from, momentum);
-            }
-        }
+        for (uint32_t e = 0; e < 8u; ++e) x[e] = static_cast<float>(scale * x[e]);
         uint4 hi, lo;
         split8(x, hi, lo);
         const size_t to = (static_cast<size_t>(j0 / 8u + jc) * g.mp + i0 + i) * 16u;
@@ -316,13 +309,23 @@ __device__ __forceinline__ void turn_sums(const Args& a, Shared& sh, const Waits
                 // neighbouring lanes are neighbours in memory: rows of the source where the matrix lies as it is, columns where it is transposed
                 __syncwarp();
                 const uint32_t i0 = t.i0 + quarter * 32u, j0 = t.j0 + c0;
-                if (g.tall) {
-                    if (i0 + lane < g.m)
-                        for (uint32_t e = 0; e < min(32u, g.n > j0 ? g.n - j0 : 0u); ++e)
-                            store<SRC>(a, out_index(g, t.which, i0 + lane, j0 + e), __uint_as_float(turn[e * 33u + lane]), g.gain);
-                } else if (j0 + lane < g.n) {
-                    for (uint32_t e = 0; e < min(32u, g.m > i0 ? g.m - i0 : 0u); ++e)
-                        store<SRC>(a, out_index(g, t.which, i0 + e, j0 + lane), __uint_as_float(turn[lane * 33u + e]), g.gain);
+                const uint32_t left = g.tall ? (g.n > j0 ? g.n - j0 : 0u) : (g.m > i0 ? g.m - i0 : 0u);
+                const uint32_t count = (g.tall ? i0 + lane < g.m : j0 + lane < g.n) ? min(32u, left) : 0u;
+                const uint64_t to = g.tall ? out_index(g, t.which, i0 + lane, j0) : out_index(g, t.which, i0, j0 + lane);
+                const uint32_t from = g.tall ? lane : lane * 33u, hop = g.tall ? 33u : 1u;
+                for (uint32_t e0 = 0; e0 < count; e0 += 8u) {
+                    float centre[8];                             // all asked for before the first store (Muon, 784-1536-1536-1000: 144 us a launch without, 82 with)
+                    if constexpr (SRC == kMuon)
+#pragma unroll
+                        for (uint32_t e = 0; e < 8u; ++e) centre[e] = e0 + e < count ? a.c_in[to + static_cast<uint64_t>(e0 + e) * g.out_ld] : 0.f;
+#pragma unroll
+                    for (uint32_t e = 0; e < 8u; ++e)
+                        if (e0 + e < count) {
+                            const uint64_t at_e = to + static_cast<uint64_t>(e0 + e) * g.out_ld;
+                            const float x = __uint_as_float(turn[from + (e0 + e) * hop]);
+                            if constexpr (SRC == kMuon) static_cast<float*>(a.out)[at_e] = fmaf(g.gain, x, a.s.keep * centre[e]);
+                            else store<SRC, false>(a, at_e, x, g.gain);
+                        }
                 }
                 __syncwarp();
             }

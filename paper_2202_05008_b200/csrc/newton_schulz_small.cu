@@ -52,9 +52,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_small(const __grid_constant_
     __shared__ uint32_t slot, limit;
     __shared__ volatile int abort_flag;
     __shared__ double red[kThreads / 32], total;
-    dep_wait();
+    const bool late = SRC == kMuon && a.late;
+    if (!late) dep_wait();
     dep_trigger();
-    if (SRC == kMuon && a.skip && *a.skip == 0.0) return;
+    if (SRC == kMuon && a.skip && __ldcg(a.skip) == 0.0) {
+        if (late) dep_wait();
+        return;
+    }
     const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31u;
     const uint32_t blocks = CLUSTER ? a.cluster : 1u, rank = CLUSTER ? blockIdx.x % blocks : 0u, at_block = blockIdx.x / blocks;
     uint32_t gi = 0;
@@ -102,7 +106,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_small(const __grid_constant_
         uint32_t i, jc;
         place(t, i, jc);
         const uint32_t j = jc * 8u, count = t < items && i < m && j < n ? min(8u, n - j) : 0u;
-        load8<SRC>(a, in_index(g, which, i, j_first + j), g.tall ? g.in_ld : 1u, count, kept[c]);
+        load8<SRC, true, true>(a, in_index(g, which, i, j_first + j), g.tall ? g.in_ld : 1u, count, kept[c]);
     }
 #pragma unroll
     for (uint32_t c = 0; c < kItems; ++c)
@@ -324,7 +328,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_small(const __grid_constant_
             for (uint32_t c = 0; c < kItems; ++c)
 #pragma unroll
                 for (uint32_t e = 0; e < 8u; ++e)
-                    if (mine(c) < jcs && mine(c) * 8u + e < n) store<SRC>(a, out_index(g, which, row, j_first + mine(c) * 8u + e), x[c][e] * back, g.gain);
+                    if (mine(c) < jcs && mine(c) * 8u + e < n) store<SRC, true>(a, out_index(g, which, row, j_first + mine(c) * 8u + e), x[c][e] * back, g.gain);
     } else {
         // by way of shared memory, where the pairs were: floats 0-3 of an eight in place of its high parts, 4-7 of the low ones; then 8 rows by 64
         // bytes a warp
@@ -340,7 +344,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_small(const __grid_constant_
         for (uint32_t t = warp; t < sixteens * (mp / 8u); t += kThreads / 32u) {
             const uint32_t i = t / sixteens * 8u + (lane & 7u), q = lane >> 3, jc = t % sixteens * 2u + (q >> 1), j = jc * 8u + (q & 1u) * 4u;
             const float4 v = *reinterpret_cast<const float4*>((q & 1u ? x_lo : x_hi) + jc * panel + i * 16u);
-            if (i < m && j < n) store4<SRC>(a, out_index(g, which, i, j_first + j), v, n - j, g.gain);
+            if (i < m && j < n) store4<SRC, true>(a, out_index(g, which, i, j_first + j), v, n - j, g.gain);
         }
     }
     if (abort_flag) {                                                      // no MMA may write after its tensor memory is freed
@@ -354,6 +358,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_small(const __grid_constant_
     __syncthreads();
     if (warp == 0) tmem_dealloc(tmem, 2u * half_cols);
     if constexpr (CLUSTER) cluster_sync();                                 // no copy between the blocks is left when one goes
+    if (late) dep_wait();
 }
 
 template <bool CLUSTER>

@@ -63,9 +63,13 @@ __global__ void __launch_bounds__(512) k_ns_tiny(const __grid_constant__ Args a)
     extern __shared__ __align__(16) float parts[];                                  // [warps][V][32]
     __shared__ float sums[2][V][32];                                                // of a step and of the next (cluster)
     __shared__ double squares[16], total;
-    dep_wait();
+    const bool late = SRC == kMuon && a.late;
+    if (!late) dep_wait();
     dep_trigger();
-    if (SRC == kMuon && a.skip && *a.skip == 0.0) return;
+    if (SRC == kMuon && a.skip && __ldcg(a.skip) == 0.0) {
+        if (late) dep_wait();
+        return;
+    }
     const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31u, warps = blockDim.x >> 5, r = lane >> 2, q = lane & 3u;
     const uint32_t blocks = CLUSTER ? a.cluster : 1u, rank = CLUSTER ? blockIdx.x % blocks : 0u, at_block = blockIdx.x / blocks;
     uint32_t gi = 0;
@@ -90,8 +94,8 @@ __global__ void __launch_bounds__(512) k_ns_tiny(const __grid_constant__ Args a)
                     if (i < m && j < n) {
                         const uint64_t at = in_index(g, which, i, j_first + j);
                         float momentum;
-                        x[mt][kt][h][c] = load<SRC>(a, at, &momentum);
-                        if constexpr (SRC == kMuon) store_moments(a, at, momentum);
+                        x[mt][kt][h][c] = load<SRC, true>(a, at, &momentum);
+                        if constexpr (SRC == kMuon) store_moments<true>(a, at, momentum);
                     }
                 }
 #pragma unroll
@@ -241,9 +245,10 @@ __global__ void __launch_bounds__(512) k_ns_tiny(const __grid_constant__ Args a)
 #pragma unroll
                 for (uint32_t c = 0; c < 4u; ++c) {
                     const uint32_t i = 16u * mt + r + 8u * (c >> 1), j = 16u * (warp + warps * kt) + 8u * h + 2u * q + (c & 1u);
-                    if (i < m && j < n) store<SRC>(a, out_index(g, which, i, j_first + j), back * x[mt][kt][h][c], g.gain);
+                    if (i < m && j < n) store<SRC, true>(a, out_index(g, which, i, j_first + j), back * x[mt][kt][h][c], g.gain);
                 }
     if constexpr (CLUSTER) cluster_sync_all();                                      // nobody reads a block's sums after it has gone
+    if (late) dep_wait();
 }
 
 template <uint32_t MT, bool CLUSTER>

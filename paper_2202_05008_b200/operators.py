@@ -1,7 +1,8 @@
 """The matrix operators of ``include/evo.h``: calls on torch tensors that need no solver.
 
 All of them enqueue their work on ``stream`` (the current stream of the tensors' device if it is None), allocate their
-outputs and workspaces through torch on that stream, and return without waiting.  Arguments that the library cannot
+outputs and workspaces through torch on that stream, and return without waiting.  Where that is not the stream on which an argument
+was made, ordering the two and keeping the argument until the work is done are the caller's.  Arguments that the library cannot
 take raise ``EvoError``; there is no fallback.
 """
 from __future__ import annotations

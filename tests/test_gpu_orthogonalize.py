@@ -219,3 +219,29 @@ def test_muon_refusals_in_python():
         muon_step(*x, [], 1, lr=0.1, out=(x[1], x[0], x[2]))
     with pytest.raises(EvoError):
         muon_step(*x, [], 1, lr=0.1, momentum=1.0)
+
+
+def test_muon_steps_in_place_keep_their_order():
+    """The launches of a step overlap; steps after one another, and what writes their inputs, do not."""
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    sizes, at = [(128, 28), (128, 128), (100, 700), (12, 300), (200, 160), (8, 128), (40, 40)], 5
+    matrices = []
+    for rows, cols in sizes:
+        matrices.append((at, rows, cols))
+        at += rows * cols + rows
+    first = [torch.randn(at, generator=gen, device="cuda") for _ in range(3)]
+    first[2].square_()
+    gradients = torch.randn(24, at, generator=gen, device="cuda")
+    results = []
+    for wait in (False, True):
+        state, g = [x.clone() for x in first], torch.empty(at, device="cuda")
+        for step in range(1, 25):
+            torch.mul(gradients[step - 1], state[0].abs() + 0.5, out=g)
+            if wait:
+                torch.cuda.synchronize()
+            muon_step(*state, g, matrices, step, lr=0.05, weight_decay=0.01, out=tuple(state))
+            if wait:
+                torch.cuda.synchronize()
+        results.append(state)
+    for x, y in zip(*results):
+        assert torch.isfinite(x).all() and torch.equal(x, y)
