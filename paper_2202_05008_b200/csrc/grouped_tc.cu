@@ -28,6 +28,11 @@ constexpr uint32_t kWBytes = 128u * 128u;                    // of a stage; and 
 constexpr uint32_t kRing = 216u * 1024u, kSmem = kRing + 1024u;
 constexpr uint32_t kThreads = 320;
 
+// The tensor core cuts its sums off: fp32 rows 1e-6 off per 1,000 of the contracted index.  So the last pass (the large products; the others lie in
+// front of its first chunks) is added up in parts of 8 chunks of 64, in fp32 in y (2,060
+// numbers 2.1e-6 off in one part).
+constexpr uint32_t kSegment = 8;
+
 struct TcArgs {
     GroupedArgs g;
     CUtensorMap w, x[3];                                     // the rows in boxes of 32, 64 and 128
@@ -136,6 +141,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_grouped_tc(const __grid_constan
         if (mbar_try_wait(smem_u32(bar), parity) || abort_flag) return;
         if (!mbar_wait_bounded(smem_u32(bar), parity, &limit)) abort_flag = 1;
     };
+    // the step behind the part of a sum that begins at step k
+    const uint32_t small_steps = steps - chunks;
+    auto part_end = [&](uint32_t k) { return p.passes > 1u ? min(steps, max(k, small_steps) + kSegment) : steps; };
     auto aborted = [&] { return __any_sync(0xffffffffu, abort_flag) != 0; };
     Walk walk;
     walk.fill(p);
@@ -177,25 +185,29 @@ __global__ void __launch_bounds__(kThreads, 1) k_grouped_tc(const __grid_constan
     } else if (warp == 1) {
         for (uint64_t at = blockIdx.x; walk.find(p, at / p.out_tiles, &group, &row, &rows); at += gridDim.x) {
             if (rows == 0u) continue;
-            const uint32_t d = tmem + acc * kMostRows, id = idesc<T>((rows + 15u) / 16u * 16u);
-            wait(&taken[acc], acc_phase ^ 1u);
-            for (uint32_t k = 0; k < steps; ++k) {
-                wait(&full[stage], phase);
-                tc_fence_after();
-                if (aborted()) break;
-                if (lane == 0) {
-                    const uint32_t w = smem + stage * stage_bytes;
+            const uint32_t id = idesc<T>((rows + 15u) / 16u * 16u);
+            for (uint32_t k = 0; k < steps && !aborted();) {
+                const uint32_t d = tmem + acc * kMostRows, first = k, end = part_end(k);
+                wait(&taken[acc], acc_phase ^ 1u);
+                for (; k < end; ++k) {
+                    wait(&full[stage], phase);
+                    tc_fence_after();
+                    if (aborted()) break;
+                    if (lane == 0) {
+                        const uint32_t w = smem + stage * stage_bytes;
 #pragma unroll
-                    for (uint32_t s = 0; s < 4u; ++s) umma_bf16(d, desc_sw128(w + s * 32u), desc_sw128(w + kWBytes + s * 32u), id, k + s != 0u);
-                    umma_commit(smem_u32(&empty[stage]));
-                    if (k + 1u == steps) umma_commit(smem_u32(&done[acc]));
+                        for (uint32_t s = 0; s < 4u; ++s) umma_bf16(d, desc_sw128(w + s * 32u), desc_sw128(w + kWBytes + s * 32u), id, k - first + s != 0u);
+                        umma_commit(smem_u32(&empty[stage]));
+                        if (k + 1u == end) umma_commit(smem_u32(&done[acc]));
+                    }
+                    __syncwarp();
+                    if (++stage == stages) { stage = 0; phase ^= 1u; }
                 }
-                __syncwarp();
-                if (++stage == stages) { stage = 0; phase ^= 1u; }
+                if (aborted()) break;
+                acc ^= 1u;
+                if (acc == 0u) acc_phase ^= 1u;
             }
             if (aborted()) break;
-            acc ^= 1u;
-            if (acc == 0u) acc_phase ^= 1u;
         }
         if (aborted()) {                                     // nor may an MMA write after its tensor memory is freed
             if (lane == 0) umma_commit(smem_u32(&drain));
@@ -216,42 +228,60 @@ __global__ void __launch_bounds__(kThreads, 1) k_grouped_tc(const __grid_constan
                 else bias = __bfloat162float(b);
             }
             O* const y = static_cast<O*>(a.y) + row * a.ld_y + o;
-            wait(&done[acc], acc_phase);
-            tc_fence_after();
-            const float scale = abort_flag ? __int_as_float(0x7FC00000) : a.scale;
-            // the halves take every other 32 rows
-            for (uint32_t c = half * 32u; c < rows; c += 64u) {
-                uint32_t u[4][8];
-                tmem_ld32_issue(tmem + acc * kMostRows + (quarter << 21) + c, u);
-                tmem_ld8x4_fence(u[0], u[1], u[2], u[3]);
-                float v[32];
+            for (uint32_t first = 0, end = 0; end < steps; first = end) {
+                end = part_end(first);
+                wait(&done[acc], acc_phase);
+                tc_fence_after();
+                const float scale = abort_flag ? __int_as_float(0x7FC00000) : a.scale;
+                // the halves take every other 32 rows
+                for (uint32_t c = half * 32u; c < rows; c += 64u) {
+                    uint32_t u[4][8];
+                    tmem_ld32_issue(tmem + acc * kMostRows + (quarter << 21) + c, u);
+                    tmem_ld8x4_fence(u[0], u[1], u[2], u[3]);
+                    O* to = y + c * a.ld_y;
+                    const uint32_t count = live ? min(32u, rows - c) : 0u;
+                    float v[32];
 #pragma unroll
-                for (uint32_t i = 0; i < 32u; ++i) v[i] = __uint_as_float(u[i / 8u][i % 8u]) + bias;
-                if (a.activation == EVO_ACT_TANH) {
+                    for (uint32_t i = 0; i < 32u; ++i) v[i] = __uint_as_float(u[i / 8u][i % 8u]);
+                    if constexpr (std::is_same<O, float>::value) {
+                        if (first != 0u) {
 #pragma unroll
-                    for (uint32_t i = 0; i < 32u; ++i) v[i] = gm::tanh32(v[i]);
-                } else if (a.activation == EVO_ACT_RELU) {
+                            for (uint32_t i = 0; i < 32u; ++i) v[i] += i < count ? to[i * a.ld_y] : 0.f;
+                        }
+                        if (end != steps) {
 #pragma unroll
-                    for (uint32_t i = 0; i < 32u; ++i) v[i] = v[i] < 0.f ? 0.f : v[i];
-                }
-                O* to = y + c * a.ld_y;
-                const uint32_t count = live ? min(32u, rows - c) : 0u;
-#pragma unroll
-                for (uint32_t i = 0; i < 32u; ++i) {
-                    if (i < count) {
-                        if constexpr (std::is_same<O, __half>::value) *to = __float2half_rn(scale * v[i]);
-                        else if constexpr (std::is_same<O, float>::value) *to = scale * v[i];
-                        else *to = __float2bfloat16_rn(scale * v[i]);
+                            for (uint32_t i = 0; i < 32u; ++i)
+                                if (i < count) to[i * a.ld_y] = v[i];
+                            __syncwarp();
+                            continue;
+                        }
                     }
-                    to += a.ld_y;
+#pragma unroll
+                    for (uint32_t i = 0; i < 32u; ++i) v[i] += bias;
+                    if (a.activation == EVO_ACT_TANH) {
+#pragma unroll
+                        for (uint32_t i = 0; i < 32u; ++i) v[i] = gm::tanh32(v[i]);
+                    } else if (a.activation == EVO_ACT_RELU) {
+#pragma unroll
+                        for (uint32_t i = 0; i < 32u; ++i) v[i] = v[i] < 0.f ? 0.f : v[i];
+                    }
+#pragma unroll
+                    for (uint32_t i = 0; i < 32u; ++i) {
+                        if (i < count) {
+                            if constexpr (std::is_same<O, __half>::value) *to = __float2half_rn(scale * v[i]);
+                            else if constexpr (std::is_same<O, float>::value) *to = scale * v[i];
+                            else *to = __float2bfloat16_rn(scale * v[i]);
+                        }
+                        to += a.ld_y;
+                    }
+                    __syncwarp();
                 }
+                tc_fence_before();
                 __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&taken[acc]));
+                acc ^= 1u;
+                if (acc == 0u) acc_phase ^= 1u;
             }
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&taken[acc]));
-            acc ^= 1u;
-            if (acc == 0u) acc_phase ^= 1u;
         }
     }
     tc_fence_before();
