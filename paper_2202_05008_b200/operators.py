@@ -8,6 +8,7 @@ take raise ``EvoError``; there is no fallback.
 from __future__ import annotations
 
 import ctypes as C
+import math
 from functools import lru_cache
 from typing import Optional, Sequence, Tuple
 
@@ -19,6 +20,7 @@ TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 INVALID_ARG = 1
 ACTIVATIONS = {"none": 0, "tanh": 1, "relu": 2}
 COEFFICIENTS = (3.4445, -4.7750, 2.0315)
+_LEAST = math.ulp(0.0)
 
 
 def _require(condition: bool, where: str, what: str) -> None:
@@ -120,7 +122,8 @@ def muon_step(center: torch.Tensor, m: torch.Tensor, v: torch.Tensor, gradient: 
               adam_eps: float = 1e-8, out: Optional[Tuple[torch.Tensor, torch.Tensor, torch.Tensor]] = None,
               stream: Optional[torch.cuda.Stream] = None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
     """``evo_muon_step`` on flat fp32 vectors; ``matrices`` lists (offset, rows, cols) of the weight matrices.  Returns
-    the new (center, m, v); ``out=(center, m, v)`` takes the step in place."""
+    the new (center, m, v); ``out=(center, m, v)`` takes the step in place.  ``beta1``, ``beta2`` and ``adam_eps`` are taken as they
+    are, 0 included."""
     lib, where = load_library(), "muon_step"
     vectors = (center, m, v, gradient) + (tuple(out) if out is not None else ())
     _require(len(vectors) in (4, 7), where, "out needs three vectors")
@@ -128,6 +131,8 @@ def muon_step(center: torch.Tensor, m: torch.Tensor, v: torch.Tensor, gradient: 
         _require(x.is_cuda and x.device == center.device and x.dtype == torch.float32 and x.dim() == 1 and x.is_contiguous() and
                  x.numel() == center.numel(), where, "contiguous fp32 vectors of one length on one GPU")
     ns = _newton_schulz(ns_steps, tuple(coefficients), eps, where)
+    # 0 selects a default in the structure; here it is the caller's: the smallest double instead, which is 0 in the kernel's fp32 (and 1 - beta is 1)
+    beta1, beta2, adam_eps = (x if x != 0 else _LEAST for x in (beta1, beta2, adam_eps))
     cfg = Muon(C.sizeof(Muon), 0 if nesterov else 1, lr, momentum, weight_decay, beta1, beta2, adam_eps, ns)
     _require(1 <= step < 1 << 32, where, "the step counts from 1")
     dim = center.numel()
