@@ -262,7 +262,8 @@ int launch_tiny(cudaStream_t st, uint32_t source, const Args& a, uint32_t row_ti
     auto kernel = a.cluster > 1u ? (row_tiles == 1u ? kernel_for<1, true>(source) : kernel_for<2, true>(source))
                                  : (row_tiles == 1u ? kernel_for<1, false>(source) : kernel_for<2, false>(source));
     const size_t smem = static_cast<size_t>(warps) * row_tiles * row_tiles * 8u * 32u * sizeof(float);
-    if (smem > 48u * 1024u && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 64 * 1024) != cudaSuccess) return -1;
+    // (48 KB without this is what a block may have in all, the 8 KB of its sums included)
+    if (smem > 32u * 1024u && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 64 * 1024) != cudaSuccess) return -1;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(a.blocks * a.cluster); cfg.blockDim = dim3(warps * 32u); cfg.dynamicSmemBytes = smem; cfg.stream = st;
     cudaLaunchAttribute attr[2];
