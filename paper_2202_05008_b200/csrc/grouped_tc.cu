@@ -322,11 +322,13 @@ __global__ void __launch_bounds__(256) k_lay_out(const __grid_constant__ Grouped
             *reinterpret_cast<uint32_t*>(dst + k) = s[k] | (k + 1u < a.n_in ? static_cast<uint32_t>(s[k + 1u]) << 16 : 0u);
     } else {
         for (uint32_t k = lane; k < pitch; k += 32u) {
-            // (an infinity, and what rounds to one, has no further parts: their product with a zero would be NaN)
+            // (an infinity has no further parts: their product with a zero would be NaN.  A number that would round to one is cut off instead: above
+            // 3.396e38)
             float x = k < a.n_in ? src[k] : 0.f;
 #pragma unroll
             for (uint32_t p = 0; p < 3u; ++p) {
-                const __nv_bfloat16 b = __float2bfloat16_rn(x);
+                __nv_bfloat16 b = __float2bfloat16_rn(x);
+                if (p == 0u && isinf(__bfloat162float(b)) && !isinf(x)) b = __float2bfloat16_rz(x);
                 const float back = __bfloat162float(b);
                 dst[p * pitch + k] = __bfloat16_as_ushort(b);
                 x = isfinite(back) ? x - back : 0.f;
