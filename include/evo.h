@@ -63,7 +63,8 @@ enum { EVO_SIGMA_CONSTANT = 0, EVO_SIGMA_PGPE = 1 };
 /* evo_config.debug_flags.  DROP_COMPLETION: the roll-out kernels leave out the asynchronous
  * completion their first bounded wait depends on (the copy of a member's parameters; in the
  * tensor-core CNN the copy of a block's first group of activations), so that wait must run out: every block raises
- * EVO_ERR_TIMEOUT, reports NaN as its return and leaves by itself, with nothing left in flight.  It exists so that the time-out path can be tested without disturbing
+ * EVO_ERR_TIMEOUT, reports NaN as its return and leaves by itself, with nothing left in flight.  In a Muon step the first block of every launch
+ * that waits for tensor cores leaves out the first completion: the matrix that it works on becomes NaN throughout.  It exists so that the time-out path can be tested without disturbing
  * the device. */
 enum { EVO_DEBUG_DROP_COMPLETION = 1 };
 

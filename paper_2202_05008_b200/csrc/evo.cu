@@ -447,7 +447,7 @@ static int muon_after_tell(evo_solver* s)
     a.nesterov = c.muon_plain_momentum ? 0u : 1u; a.ns_steps = c.muon_steps;
     a.a = kNsA; a.b = kNsB; a.c = kNsC; a.ns_eps = kNsEps;
     a.work = s->ws + L.muon;
-    a.sticky = &status->sticky; a.wait_log2 = c.wait_cycles_log2;
+    a.sticky = &status->sticky; a.wait_log2 = c.wait_cycles_log2; a.drop = c.debug_flags & EVO_DEBUG_DROP_COMPLETION;
     return launch_muon(s->stream, s->matrices, s->n_matrices, a);
 }
 

@@ -190,7 +190,7 @@ try {
     if (!muon_scalars(a, &args.s)) return -1;
     args.in = a.g; args.out = a.center_out;
     args.m_in = a.m; args.m_out = a.m_out; args.v_in = a.v; args.v_out = a.v_out; args.c_in = a.center;
-    args.skip = a.skip; args.sticky = a.sticky; args.wait_log2 = a.wait_log2;
+    args.skip = a.skip; args.sticky = a.sticky; args.wait_log2 = a.wait_log2; args.drop = a.drop;
     const std::vector<ns::Matrix> m = muon_list(list, n, a.lr);
     int launches = ns::launch(st, ns::kMuon, m.data(), n, args, a.work);
     if (launches < 0) return -1;

@@ -41,7 +41,7 @@ struct MuonArgs {
     float a, b, c, ns_eps;
     char* work;
     uint32_t* sticky;
-    uint32_t wait_log2;
+    uint32_t wait_log2, drop;
 };
 bool muon_scalars(const MuonArgs& a, ns::Scalars* s);       // false: an iteration that grows beyond fp16 pairs
 size_t muon_workspace_bytes(const evo_matrix* list, size_t n);

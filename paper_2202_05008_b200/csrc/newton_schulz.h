@@ -62,8 +62,9 @@ struct Args {
     uint32_t late;
     char* work;
     double* partial;                     // large: sums of squares per piece
-    uint32_t* sticky;                    // where a wait that ran out is noted (NULL: nowhere; the result is NaN in any case)
+    uint32_t* sticky;                    // where a wait that ran out is noted (NULL: nowhere; what depends on it is NaN in any case)
     uint32_t wait_log2;
+    uint32_t drop;                       // EVO_DEBUG_DROP_COMPLETION: block 0 leaves out the first commit that it waits for
     size_t partial_at, lift_at;          // byte offsets of the two in the workspace
     uint32_t* lift;                      // large: per matrix of the launch, see first_scale
     uint32_t groups, blocks, pairs, tiles, cluster;

@@ -197,9 +197,10 @@ __device__ __forceinline__ void copy_operands(const Args& a, const Maps& maps, S
 }
 
 template <uint32_t MODE>
-__device__ __forceinline__ void issue_products(const Args& a, Shared& sh, const Waits& waits, uint32_t ring, uint32_t tmem, Place& at)
+__device__ __forceinline__ void issue_products(const Args& a, Shared& sh, const Waits& waits, uint32_t ring, uint32_t tmem, Place& at, uint32_t step)
 {
     const uint32_t lane = threadIdx.x & 31u, total = MODE == kApply ? a.tiles : a.pairs;
+    const bool drop = MODE == kGram && a.drop && blockIdx.x == 0u && step == 0u;
     for (uint32_t tile = blockIdx.x; tile < total; tile += gridDim.x) {
         const Tile t = tile_at<MODE>(a, tile);
         constexpr uint32_t wide = idesc_f16(128, 256, MODE == kApply), narrow = idesc_f16(128, 128, MODE == kApply);
@@ -222,7 +223,7 @@ __device__ __forceinline__ void issue_products(const Args& a, Shared& sh, const 
                     ph += 512u; pl += 512u; qq += hop;
                 }
                 umma_commit(smem_u32(&sh.empty[at.stage]));
-                if (ends) umma_commit(smem_u32(&sh.done[at.acc]));
+                if (ends && !drop) umma_commit(smem_u32(&sh.done[at.acc]));
             }
             __syncwarp();
             at.next_stage();
@@ -392,7 +393,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) k_ns_gemm(const __grid_consta
     uint32_t* const turn = reinterpret_cast<uint32_t*>(smem + kStages * kStage) + (warp - 2u) * 32u * 33u;
     Place at;
     if (warp == 0) copy_operands<MODE>(a, maps, sh, waits, ring, at, step);
-    else if (warp == 1) issue_products<MODE>(a, sh, waits, ring, tmem, at);
+    else if (warp == 1) issue_products<MODE>(a, sh, waits, ring, tmem, at, step);
     else turn_sums<MODE, SRC>(a, sh, waits, ring, turn, tmem, at, step);
     if (warp == 0 && aborted(sh))                                // nothing may land after the block has gone
         for (uint32_t s = 0; s < min(at.filled, kStages); ++s) {

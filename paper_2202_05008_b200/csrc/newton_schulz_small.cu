@@ -161,7 +161,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_small(const __grid_constant_
     const uint64_t q_k_hi = umma_smem_desc(smem_u32(q_hi), panel, 128u), q_k_lo = umma_smem_desc(smem_u32(q_lo), panel, 128u);
     const uint32_t k_step = panel / 8u, m_step = 16u;
     // (128 x N) = sum over K of the products of two pairs
-    auto product = [&](uint32_t idesc, uint64_t ph, uint64_t pl, uint32_t p_step, uint64_t rh, uint64_t rl, uint32_t r_step, uint32_t K) {
+    auto product = [&](uint32_t idesc, uint64_t ph, uint64_t pl, uint32_t p_step, uint64_t rh, uint64_t rl, uint32_t r_step, uint32_t K, bool drop = false) {
         if (abort_flag) return;
 #pragma unroll 4
         for (uint32_t k = 0; k < K / 16u; ++k) {
@@ -170,8 +170,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_small(const __grid_constant_
             umma_bf16(tmem + half_cols, pl, rh, idesc, 1u);
             ph += p_step; pl += p_step; rh += r_step; rl += r_step;
         }
-        umma_commit(smem_u32(&bar));
+        if (!drop) umma_commit(smem_u32(&bar));
     };
+    // After a wait that ran out nothing is multiplied any more: what a block has in hand then, and what it sends to the others, is not a number.
+    // (What the others have by the last exchange, and make of it, does not depend on this block any further.)
+    auto sound = [&] { return abort_flag ? __int_as_float(0x7FC00000) : 1.0f; };
     const uint32_t row = (warp & 3u) * 32u + lane, lanes = (warp & 3u) << 21, part = warp >> 2;      // four warps share a quarter of the lanes
     const bool rows_live = (warp & 3u) * 32u < mp, row_live = row < mp;
     // this thread's eights of columns: 2 part + 8 t and the next, t = 0, 1, of A as of X
@@ -216,8 +219,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_small(const __grid_constant_
         const float unlift = power_of_two(-2 * static_cast<int>(lift)), to_a = unlift * (a.s.s_a / (a.s.s_x * a.s.s_x));
         const float poly_b = a.s.b * a.s.s_b / a.s.s_a;
         const float drop = power_of_two(static_cast<int>(next_lift) - static_cast<int>(lift)), next_a = drop * a.s.a, next_bx = drop / a.s.s_b;
-        if (tid == 0) product(idesc_f16(128, mp, false), x_k_hi, x_k_lo, k_step, x_k_hi, x_k_lo, k_step, np);
+        if (tid == 0) product(idesc_f16(128, mp, false), x_k_hi, x_k_lo, k_step, x_k_hi, x_k_lo, k_step, np, a.drop && blockIdx.x == 0u && step == 0u);
         finish();
+        const float scale_a = to_a * sound();
         float gram[kItems][8];                                             // A times s_a
         if (rows_live)
 #pragma unroll
@@ -227,8 +231,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_small(const __grid_constant_
                     sums(c, true, s, cut);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
-                        gram[c][e] = to_a * s[0][e];
-                        gram[c + 1u][e] = to_a * s[1][e];
+                        gram[c][e] = scale_a * s[0][e];
+                        gram[c + 1u][e] = scale_a * s[1][e];
                     }
                 }
         if constexpr (!CLUSTER) {
@@ -260,8 +264,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_small(const __grid_constant_
             waits.wait(smem_u32(&parts_bar), step & 1u);
             // this block's share: the parts in the order of the blocks, and the sum as a pair to where this block's own part would be
             uint8_t* const stage = parts + rank * share;
+            const float fill = sound() - 1.0f;                             // 0 or NaN
             for (uint32_t t = tid; t < owned(rank) * mp; t += kThreads) {
-                float s[8] = {};
+                float s[8] = { fill, fill, fill, fill, fill, fill, fill, fill };
                 for (uint32_t r = 0; r < blocks; ++r) {
                     const float4* const p = reinterpret_cast<const float4*>((r == rank ? q_hi + rank * share : parts + r * share) + t * 32u);
                     const float4 u = p[0], v = p[1];
@@ -320,7 +325,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_small(const __grid_constant_
                 }
         hand_over();
     }
-    const float back = abort_flag ? __int_as_float(0x7FC00000) : power_of_two(-static_cast<int>(lift_at(a.s, first_lift, a.s.steps))) / a.s.s_x;
+    const float back = sound() * power_of_two(-static_cast<int>(lift_at(a.s, first_lift, a.s.steps))) / a.s.s_x;
     if (g.tall) {
         // neighbouring lanes are neighbours in memory
         if (rows_live && row < m)
