@@ -9,14 +9,7 @@ using namespace evo;
 
 namespace {
 
-bool overlap(const void* p, uint64_t n, const void* q, uint64_t m)
-{
-    const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
-    return a < b + m && b < a + n;
-}
-uint64_t span(uint64_t rows, uint64_t ld, uint64_t cols) { return rows ? (rows - 1u) * ld + cols : 0u; }
-
-constexpr uint64_t kMost = 1ull << 40;       // elements of a pitch or a stride, and rows: their products stay inside 64 bits
+constexpr uint64_t kMost = 1ull << 40;       // elements of a pitch or a stride, and rows
 
 // the layers of a policy as the kernel for rows and layers takes them
 void policy_layers(const evo_actions& p, MemberArgs* a)
@@ -116,10 +109,12 @@ evo_status evo_grouped_linear(const evo_grouped* p, void* d_workspace, size_t wo
     if (!p->d_x || !p->d_weight || !p->d_y || !p->d_offsets || (bits & (size - 1u))) return EVO_ERR_INVALID_ARG;
     if (reinterpret_cast<uintptr_t>(p->d_offsets) & (p->offsets_64 ? 7u : 3u)) return EVO_ERR_INVALID_ARG;
     // (weights and biases may be shared by groups: stride 0)
-    const uint64_t y_bytes = span(p->rows, p->ld_y, p->n_out) * size;
-    if (overlap(p->d_y, y_bytes, p->d_x, span(p->rows, p->ld_x, p->n_in) * size) ||
-        overlap(p->d_y, y_bytes, p->d_weight, ((p->groups - 1u) * static_cast<uint64_t>(p->weight_stride) + span(p->n_out, p->ld_weight, p->n_in)) * size) ||
-        (p->d_bias && overlap(p->d_y, y_bytes, p->d_bias, ((p->groups - 1u) * static_cast<uint64_t>(p->bias_stride) + p->n_out) * size)) ||
+    uint64_t x_bytes, y_bytes, set, w_bytes, b_bytes = 0;
+    if (!extent(p->rows, p->ld_x, p->n_in, size, &x_bytes) || !extent(p->rows, p->ld_y, p->n_out, size, &y_bytes) ||
+        !extent(p->n_out, p->ld_weight, p->n_in, 1u, &set) || !extent(p->groups, p->weight_stride, set, size, &w_bytes) ||
+        (p->d_bias && !extent(p->groups, p->bias_stride, p->n_out, size, &b_bytes)))
+        return EVO_ERR_INVALID_ARG;
+    if (overlap(p->d_y, y_bytes, p->d_x, x_bytes) || overlap(p->d_y, y_bytes, p->d_weight, w_bytes) || (p->d_bias && overlap(p->d_y, y_bytes, p->d_bias, b_bytes)) ||
         overlap(p->d_y, y_bytes, p->d_offsets, (p->groups + 1ull) * (p->offsets_64 ? 8u : 4u)))
         return EVO_ERR_INVALID_ARG;
     const GroupedArgs a = grouped_args(p);
@@ -152,9 +147,12 @@ evo_status evo_mlp_actions(const evo_actions* p, void* d_workspace, size_t works
     if ((reinterpret_cast<uintptr_t>(p->d_observations) | reinterpret_cast<uintptr_t>(p->d_actions)) & 3u) return EVO_ERR_INVALID_ARG;
     if (reinterpret_cast<uintptr_t>(p->d_offsets) & (p->offsets_64 ? 7u : 3u)) return EVO_ERR_INVALID_ARG;
     if (p->ld_observations > kMost || p->ld_actions > kMost || (p->rows > 1u && (p->ld_observations < n_in || p->ld_actions < n_out))) return EVO_ERR_INVALID_ARG;
-    const uint64_t out_bytes = span(p->rows, p->ld_actions, n_out) * 4u;
-    if (overlap(p->d_actions, out_bytes, p->d_observations, span(p->rows, p->ld_observations, n_in) * 4u) ||
-        overlap(p->d_actions, out_bytes, p->d_theta, static_cast<uint64_t>(p->members) * p->ld_theta * 4u) ||
+    uint64_t dim = 0, in_bytes, out_bytes, theta_bytes;
+    for (uint32_t l = 0; l < p->n_layers; ++l) dim += (p->layer_sizes[l] + 1ull) * p->layer_sizes[l + 1];
+    if (!extent(p->rows, p->ld_observations, n_in, 4u, &in_bytes) || !extent(p->rows, p->ld_actions, n_out, 4u, &out_bytes) ||
+        !extent(p->members, p->ld_theta, dim, 4u, &theta_bytes))
+        return EVO_ERR_INVALID_ARG;
+    if (overlap(p->d_actions, out_bytes, p->d_observations, in_bytes) || overlap(p->d_actions, out_bytes, p->d_theta, theta_bytes) ||
         overlap(p->d_actions, out_bytes, p->d_offsets, (p->members + 1ull) * (p->offsets_64 ? 8u : 4u)))
         return EVO_ERR_INVALID_ARG;
     if (need && (!d_workspace || (reinterpret_cast<uintptr_t>(d_workspace) & 255u))) return EVO_ERR_INVALID_ARG;

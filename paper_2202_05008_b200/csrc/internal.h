@@ -57,6 +57,20 @@ constexpr uint32_t kTlNa = 8;    // tanh-linear task: action width
 constexpr uint32_t kCnnParams = 5994;
 constexpr uint32_t kMaxParamDim = 1u << 30;   // keeps ldD = round_up(D, 32) and 4 * ldD inside 32 bits
 
+// Bytes from the first of `count` runs of `elements`, `stride` apart, to the end of the last.  False where that is no array: beyond it sums of addresses and the
+// kernels' 64-bit indices would wrap.
+inline bool extent(uint64_t count, uint64_t stride, uint64_t elements, uint64_t size, uint64_t* bytes)
+{
+    const unsigned __int128 n = count ? (static_cast<unsigned __int128>(count - 1u) * stride + elements) * size : 0u;
+    *bytes = static_cast<uint64_t>(n);
+    return n <= (1ull << 60);
+}
+inline bool overlap(const void* p, uint64_t n, const void* q, uint64_t m)
+{
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
+    return a <= b ? b - a < n : a - b < m;
+}
+
 struct RolloutMlpArgs {
     const float* theta;          // [P][ldD]
     float*       fit_partial;    // [P][n_episode_blocks] sums of episode returns

@@ -264,11 +264,6 @@ static bool default_ns(const evo_newton_schulz* in, evo_newton_schulz* out)
     return out->steps <= 64u && out->eps >= 1e-30f && std::isfinite(out->eps);
 }
 
-static uint64_t elements(const evo_matrices& x)
-{
-    return (x.batch - 1u) * static_cast<uint64_t>(x.batch_stride) + (x.rows - 1u) * static_cast<uint64_t>(x.row_stride) + x.cols;
-}
-
 static evo_status check_matrices(const evo_matrices* x)
 {
     if (!x || x->type > EVO_F16 || x->batch < 1u || x->rows < 1u || x->cols < 1u) return EVO_ERR_INVALID_ARG;
@@ -302,9 +297,12 @@ evo_status evo_orthogonalize(const evo_newton_schulz* ns_in, const evo_matrices*
     if (st != EVO_OK) return st;
     if (out->type != x->type || out->batch != x->batch || out->rows != x->rows || out->cols != x->cols) return EVO_ERR_INVALID_ARG;
     const size_t width = x->type == EVO_F32 ? 4u : 2u;
-    const uintptr_t x0 = reinterpret_cast<uintptr_t>(x->data), o0 = reinterpret_cast<uintptr_t>(out->data);
-    const bool same = x0 == o0 && (x->rows == 1u || x->row_stride == out->row_stride) && (x->batch == 1u || x->batch_stride == out->batch_stride);
-    if (!same && x0 < o0 + elements(*out) * width && o0 < x0 + elements(*x) * width) return EVO_ERR_INVALID_ARG;
+    uint64_t one, x_bytes, out_bytes;
+    if (!extent(x->rows, x->row_stride, x->cols, 1u, &one) || !extent(x->batch, x->batch_stride, one, width, &x_bytes) ||
+        !extent(out->rows, out->row_stride, out->cols, 1u, &one) || !extent(out->batch, out->batch_stride, one, width, &out_bytes))
+        return EVO_ERR_INVALID_ARG;
+    const bool same = x->data == out->data && (x->rows == 1u || x->row_stride == out->row_stride) && (x->batch == 1u || x->batch_stride == out->batch_stride);
+    if (!same && overlap(x->data, x_bytes, out->data, out_bytes)) return EVO_ERR_INVALID_ARG;
     ns::Args a;
     std::memset(&a, 0, sizeof(a));
     a.s.a = p.a; a.s.b = p.b; a.s.c = p.c; a.s.eps = p.eps; a.s.steps = p.steps;
