@@ -379,7 +379,8 @@ evo_status evo_muon_step(const evo_muon* cfg, const evo_matrix* list, uint32_t n
  * goes into is an infinity or NaN, and nothing else is, unless the sum leaves fp32's range (with many rows of fp32 it may be NaN where an infinity is due; with
  * few rows fp32 numbers above 3.4011e38 count as infinities).  y may not overlap anything.
  * Errors: INVALID_ARG, WORKSPACE, UNSUPPORTED (more than 2^31 blocks), CUDA.  Workspace 0 unless there are many rows a group in a
- * type or at addresses that have to be laid out anew for the tensor cores.
+ * type or at addresses that have to be laid out anew for the tensor cores: the size depends on the addresses and pitches of x and the weights, and with
+ * d_x or d_weight NULL is enough for any addresses.
  */
 enum { EVO_ACT_NONE = 0, EVO_ACT_TANH = 1, EVO_ACT_RELU = 2 };
 typedef struct evo_grouped {

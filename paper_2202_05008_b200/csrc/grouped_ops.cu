@@ -94,7 +94,9 @@ evo_status evo_grouped_linear_bytes(const evo_grouped* p, size_t* bytes)
 {
     const evo_status st = check_grouped(p);
     if (st != EVO_OK || !bytes) return EVO_ERR_INVALID_ARG;
-    *bytes = p->rows ? grouped_bytes(p->type, grouped_args(p)) : 0u;
+    // (before the buffers exist: as much as they need wherever they lie)
+    const GroupedArgs a = grouped_args(p);
+    *bytes = p->rows == 0u ? 0u : p->d_x && p->d_weight ? grouped_bytes(p->type, a) : grouped_tc_bytes(p->type, a);
     return EVO_OK;
 }
 
