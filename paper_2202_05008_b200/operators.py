@@ -34,12 +34,13 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)      # the ha
 
 
 class _On:
-    """The tensors' device, and the stream the call goes to, as the current ones (allocations belong to that stream).  Entering
+    """The tensors' device, and the stream the call goes to (one of that device), as the current ones (allocations belong to that stream).  Entering
     gives the stream's handle; nothing is switched where both are current already (6 us of a small call)."""
     __slots__ = ("device", "stream", "guard")
 
-    def __init__(self, device: torch.device, stream: Optional[torch.cuda.Stream]):
+    def __init__(self, device: torch.device, stream: Optional[torch.cuda.Stream], where: str):
         self.device, self.stream, self.guard = device, stream, None
+        _require(stream is None or stream.device == device, where, "a stream of another device")
 
     def __enter__(self) -> int:
         if self.stream is not None:
@@ -99,7 +100,7 @@ def orthogonalize(x: torch.Tensor, out: Optional[torch.Tensor] = None, *, steps:
     _require(x.shape[-1] == 1 or x.stride(-1) == 1, where, "the columns of x need unit stride")
     ns = _newton_schulz(steps, tuple(coefficients), eps, where)
     shape, device = x.shape, x.device
-    with _On(device, stream) as st:
+    with _On(device, stream, where) as st:
         if out is None:
             out = torch.empty(shape, dtype=x.dtype, device=device)
         else:
@@ -137,7 +138,7 @@ def muon_step(center: torch.Tensor, m: torch.Tensor, v: torch.Tensor, gradient: 
     _require(1 <= step < 1 << 32, where, "the step counts from 1")
     dim = center.numel()
     items, n, need = _matrix_list(tuple(map(tuple, matrices)), dim)
-    with _On(center.device, stream) as st:
+    with _On(center.device, stream, where) as st:
         if out is None:
             out = (torch.empty_like(center), torch.empty_like(m), torch.empty_like(v))
         if dim == 0:
@@ -186,7 +187,7 @@ def grouped_linear(x: torch.Tensor, weight: torch.Tensor, offsets: torch.Tensor,
     if bias is not None:
         _require(_rows(bias, dtype, device) and bias.shape == (groups, n_out), where, "bias does not match")
     wide = _ragged(offsets, groups, device, where)
-    with _On(device, stream) as st:
+    with _On(device, stream, where) as st:
         y = _out(out, x, rows, n_out, where)
         p = Grouped(C.sizeof(Grouped), TYPES[dtype], groups, n_in, n_out, ACTIVATIONS[activation], scale, wide, rows,
                     x.data_ptr(), x.stride(0), weight.data_ptr(), pitch if n_out > 1 else n_in, stride,
@@ -221,7 +222,7 @@ def mlp_actions(theta: torch.Tensor, layer_sizes: Sequence[int], observations: t
     members, rows = theta.shape[0], observations.shape[0]
     _require(_rows(theta, torch.float32, device) and members >= 1 and theta.shape[1] >= dim, where, "theta does not match")
     wide = _ragged(offsets, members, device, where)
-    with _On(device, stream) as st:
+    with _On(device, stream, where) as st:
         y = _out(out, observations, rows, sizes[-1], where)
         pitch = theta.stride(0) if members > 1 else -(-max(dim, theta.stride(0)) // 4) * 4
         p = Actions(C.sizeof(Actions), members, len(sizes) - 1, widths, action_scale, wide, rows, theta.data_ptr(), pitch,
