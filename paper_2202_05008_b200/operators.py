@@ -60,7 +60,9 @@ class _On:
 
 @lru_cache(maxsize=256)
 def _newton_schulz(steps: int, coefficients: Tuple[float, ...], eps: float, where: str) -> NewtonSchulz:
-    _require(1 <= steps <= 64 and len(coefficients) == 3 and any(coefficients) and eps > 0, where, "steps, coefficients or eps")
+    # (the structure takes zeros, and what fp32 rounds to zero, for its defaults)
+    _require(1 <= steps <= 64 and len(coefficients) == 3 and any(C.c_float(x).value for x in coefficients) and C.c_float(eps).value > 0, where,
+             "steps, coefficients or eps")
     return NewtonSchulz(C.sizeof(NewtonSchulz), steps, *coefficients, eps)
 
 
