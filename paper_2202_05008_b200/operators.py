@@ -3,7 +3,8 @@
 All of them enqueue their work on ``stream`` (the current stream of the tensors' device if it is None), allocate their
 outputs and workspaces through torch on that stream, and return without waiting.  Where that is not the stream on which an argument
 was made, ordering the two and keeping the argument until the work is done are the caller's.  Arguments that the library cannot
-take raise ``EvoError``; there is no fallback.
+take raise ``EvoError``; there is no fallback.  None of them has a backward pass: while torch records gradients, tensors that require one are
+refused (detach them, or call under ``torch.no_grad()``).
 """
 from __future__ import annotations
 
@@ -28,6 +29,11 @@ def _require(condition: bool, where: str, what: str) -> None:
         error = EvoError(INVALID_ARG, where)
         error.args = (f"{error.args[0]}: {what}",)
         raise error
+
+
+def _require_no_gradient(where: str, *tensors: Optional[torch.Tensor]) -> None:
+    if torch.is_grad_enabled():
+        _require(not any(x is not None and x.requires_grad for x in tensors), where, "a tensor requires a gradient, and there is no backward pass")
 
 
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)      # the handle without a Stream object (2 us)
@@ -98,6 +104,7 @@ def orthogonalize(x: torch.Tensor, out: Optional[torch.Tensor] = None, *, steps:
     """``evo_orthogonalize``: every matrix of ``x`` ([rows, cols] or [batch, rows, cols]; fp32, bf16 or fp16; unit
     column stride) with its singular values moved towards 1 by Newton-Schulz steps.  ``out`` may be ``x``."""
     lib, where = load_library(), "orthogonalize"
+    _require_no_gradient(where, x, out)
     _require(x.is_cuda and x.dtype in TYPES and x.dim() in (2, 3), where, "a fp32, bf16 or fp16 matrix or batch on a GPU")
     _require(x.shape[-1] == 1 or x.stride(-1) == 1, where, "the columns of x need unit stride")
     ns = _newton_schulz(steps, tuple(coefficients), eps, where)
@@ -130,6 +137,7 @@ def muon_step(center: torch.Tensor, m: torch.Tensor, v: torch.Tensor, gradient: 
     lib, where = load_library(), "muon_step"
     vectors = (center, m, v, gradient) + (tuple(out) if out is not None else ())
     _require(len(vectors) in (4, 7), where, "out needs three vectors")
+    _require_no_gradient(where, *vectors)
     for x in vectors:
         _require(x.is_cuda and x.device == center.device and x.dtype == torch.float32 and x.dim() == 1 and x.is_contiguous() and
                  x.numel() == center.numel(), where, "contiguous fp32 vectors of one length on one GPU")
@@ -178,6 +186,7 @@ def grouped_linear(x: torch.Tensor, weight: torch.Tensor, offsets: torch.Tensor,
     other strides (a layer of theta is ``theta[:, a:b].unflatten(1, (n_out, n_in))``; an expanded weight is shared).  Rows outside all
     groups are left as they are in ``out``, and undefined without one."""
     lib, where, device, dtype = load_library(), "grouped_linear", x.device, x.dtype
+    _require_no_gradient(where, x, weight, bias, out)
     _require(x.is_cuda and dtype in TYPES and _rows(x, dtype, device), where, "x: fp32, bf16 or fp16 rows on a GPU")
     _require(weight.device == device and weight.dtype == dtype and weight.dim() == 3, where, "weight does not match x")
     groups, n_out, n_in = weight.shape
@@ -217,6 +226,7 @@ def mlp_actions(theta: torch.Tensor, layer_sizes: Sequence[int], observations: t
     theta [members, >= parameters] fp32 as ``Solver.ask`` returns it (row pitch a multiple of 4, rows 16-byte aligned),
     layer_sizes the widths, input first.  Rows without a member are left as they are in ``out``, and undefined without one."""
     lib, where, device = load_library(), "mlp_actions", observations.device
+    _require_no_gradient(where, theta, observations, out)
     sizes = tuple(layer_sizes)
     dim, widths = _layers(sizes)
     _require(observations.is_cuda and _rows(observations, torch.float32, device) and observations.shape[1] == sizes[0], where,
