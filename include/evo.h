@@ -330,7 +330,7 @@ typedef struct evo_newton_schulz {
  * and strides); else the two must not overlap.  ns NULL selects the defaults.  A matrix of zeros stays
  * zero; one with an infinity or a NaN becomes NaN throughout, and no other matrix does.
  * Errors: INVALID_ARG, WORKSPACE, UNSUPPORTED (coefficients whose iteration grows a singular value of [0, 1] beyond
- * 64), CUDA.
+ * 64; more than 2^31 blocks, of which a matrix has 1 to 8 or more), CUDA.
  */
 evo_status evo_orthogonalize_bytes(uint32_t batch, uint32_t rows, uint32_t cols, size_t* bytes);
 evo_status evo_orthogonalize(const evo_newton_schulz* ns, const evo_matrices* x, const evo_matrices* out,

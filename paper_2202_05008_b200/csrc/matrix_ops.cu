@@ -58,6 +58,8 @@ size_t workspace_bytes(const Matrix* list, size_t n)
 {
     size_t most = 0, bytes = 0;
     Args a;
+    for (size_t i = 0; i < n; ++i)
+        if (static_cast<uint64_t>(choice_of(list[i]).blocks) * list[i].count > 0x7FFFFFFFu) return ~static_cast<size_t>(0);
     for (size_t at = 0; at < n;) {
         if (!gather_large(list, n, &at, &a, &bytes)) return ~static_cast<size_t>(0);
         most = std::max(most, bytes);

@@ -19,7 +19,7 @@ int launch_tiny(cudaStream_t st, uint32_t source, const Args& a, uint32_t row_ti
 int launch_small(cudaStream_t st, uint32_t source, const Args& a, size_t smem);
 int launch_large(cudaStream_t st, uint32_t source, const Args& a);
 
-// Workspace of a list (0 where all matrices are small); ~0 if it cannot be numbered in 32 bits
+// Workspace of a list (0 where all matrices are small); ~0 if its blocks or tiles cannot be numbered in 32 bits
 size_t workspace_bytes(const Matrix* list, size_t n);
 // All matrices of the list.  `base` holds the pointers and scalars; the rest is filled in here.
 int launch(cudaStream_t st, uint32_t source, const Matrix* list, size_t n, const Args& base, char* work);

@@ -4,7 +4,7 @@ import ctypes as C
 
 import pytest
 
-from test_matrix_ops import FAR, INVALID, WORKSPACE, _actions, _grouped, _ns, _x, lib  # noqa: F401
+from test_matrix_ops import FAR, INVALID, OK, UNSUPPORTED, WORKSPACE, _actions, _grouped, _ns, _x, lib  # noqa: F401
 
 MOST = 1 << 40
 # weights, biases and rows far behind y, below which nothing of the small case lies
@@ -43,3 +43,12 @@ def test_actions_behind_the_last_members_parameters_do_not_overlap(lib):   # noq
         p = _actions(sizes, ld_theta=ld, d_theta=FAR, d_observations=2 * FAR, d_offsets=3 * FAR, d_actions=at, rows=100, ld_actions=3)
         assert lib.evo_mlp_actions(C.byref(p), FAR * 64, 256, None) == code, (at, code)
 
+
+
+def test_more_small_matrices_than_blocks_of_a_launch(lib):             # noqa: F811
+    n = C.c_size_t()
+    for batch, rows, cols in ((1 << 31, 1, 1), (1 << 28, 4, 8000), (1 << 29, 40, 300), ((1 << 32) - 1, 3, 2)):
+        assert lib.evo_orthogonalize_bytes(batch, rows, cols, C.byref(n)) == UNSUPPORTED, (batch, rows, cols)
+        x, out = _x(FAR, type_=1, batch=batch, rows=rows, cols=cols), _x(1 << 55, type_=1, batch=batch, rows=rows, cols=cols)
+        assert lib.evo_orthogonalize(C.byref(_ns()), C.byref(x), C.byref(out), None, 0, None) == UNSUPPORTED
+    assert lib.evo_orthogonalize_bytes((1 << 31) - 1, 1, 1, C.byref(n)) == OK and n.value == 0
