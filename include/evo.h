@@ -307,7 +307,8 @@ evo_status evo_es_gradient_static(const float* d_u, const float* d_eps, uint32_t
  */
 enum { EVO_F32 = 0, EVO_BF16 = 1, EVO_F16 = 2 };
 
-/* `batch` matrices: element (k, r, c) is data[k * batch_stride + r * row_stride + c], row_stride >= cols;
+/* `batch` matrices: element (k, r, c) is data[k * batch_stride + r * row_stride + c], rows and matrices one behind the other:
+ * row_stride >= cols, batch_stride >= (rows - 1) row_stride + cols (a stride that is never taken may be anything);
  * type EVO_F32 / EVO_BF16 / EVO_F16.  rows and cols up to 2^20. */
 typedef struct evo_matrices {
     void*    data;                 /* device */
@@ -327,7 +328,7 @@ typedef struct evo_newton_schulz {
 /*
  * Orthogonalise every matrix of a batch: out = the result of the iteration above, in out's type (x's).  The sums
  * are kept in fp32, x in pairs of fp16 numbers (22 bits) whatever the type.  out may be x itself (same pointer
- * and strides); else the two must not overlap.  ns NULL selects the defaults.  A matrix of zeros stays
+ * and strides); else the two must not overlap, from the first to the last element of each.  ns NULL selects the defaults.  A matrix of zeros stays
  * zero; one with an infinity or a NaN becomes NaN throughout, and no other matrix does.
  * Errors: INVALID_ARG, WORKSPACE, UNSUPPORTED (coefficients whose iteration grows a singular value of [0, 1] beyond
  * 64; more than 2^31 blocks, of which a matrix has 1 to 8 or more), CUDA.
@@ -377,7 +378,8 @@ evo_status evo_muon_step(const evo_muon* cfg, const evo_matrix* list, uint32_t n
  * that belong to no group are left as they are.  (Offsets that fall or leave [0, rows] give wrong rows, but nothing
  * outside the arrays is touched.)  Sums in fp32; fp32 operands count with 21 bits and more (numbers below 1e-31 with fewer).  What an infinity or a NaN of the operands
  * goes into is an infinity or NaN, and nothing else is, unless the sum leaves fp32's range (with many rows of fp32 it may be NaN where an infinity is due; with
- * few rows fp32 numbers above 3.4011e38 count as infinities).  y may not overlap anything.
+ * few rows fp32 numbers above 3.4011e38 count as infinities).  y may not overlap anything, from the first to the last element of each array (columns
+ * of one wider array do).
  * Errors: INVALID_ARG, WORKSPACE, UNSUPPORTED (more than 2^31 blocks), CUDA.  Workspace 0 unless there are many rows a group in a
  * type or at addresses that have to be laid out anew for the tensor cores: the size depends on the addresses and pitches of x and the weights, and with
  * d_x or d_weight NULL is enough for any addresses.
@@ -404,7 +406,7 @@ evo_status evo_grouped_linear(const evo_grouped* p, void* d_workspace, size_t wo
  * rows offsets[m] <= r < offsets[m + 1] of the observations are member m's (episodes that have ended need no row), and
  *   actions[r] = action_scale tanh(W_L ... tanh(W_1 observations[r] + b_1) ... + b_L)
  * with the parameters theta[m] (fp32, pitch ld_theta: a multiple of 4 floats, rows 16-byte aligned) in the
- * layout of evo_ask.  Offsets and rows without a member as above.
+ * layout of evo_ask.  Offsets, rows without a member and overlaps as above.
  * Errors: INVALID_ARG, WORKSPACE, UNSUPPORTED, CUDA.  Workspace: for what a layer leaves to the next where the layers
  * are taken one by one (layers of more than 512, large populations); else 0.  tanh is off by at most 2.5e-7 of its value.
  */

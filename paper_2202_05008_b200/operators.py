@@ -102,7 +102,8 @@ def orthogonalize(x: torch.Tensor, out: Optional[torch.Tensor] = None, *, steps:
                   coefficients: Sequence[float] = COEFFICIENTS, eps: float = 1e-7,
                   stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """``evo_orthogonalize``: every matrix of ``x`` ([rows, cols] or [batch, rows, cols]; fp32, bf16 or fp16; unit
-    column stride) with its singular values moved towards 1 by Newton-Schulz steps.  ``out`` may be ``x``."""
+    column stride, rows and matrices one behind the other at any pitch) with its singular values moved towards 1 by Newton-Schulz steps.  ``out`` may
+    be ``x``."""
     lib, where = load_library(), "orthogonalize"
     _require_no_gradient(where, x, out)
     _require(x.is_cuda and x.dtype in TYPES and x.dim() in (2, 3), where, "a fp32, bf16 or fp16 matrix or batch on a GPU")
@@ -183,8 +184,8 @@ def grouped_linear(x: torch.Tensor, weight: torch.Tensor, offsets: torch.Tensor,
                    stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """``evo_grouped_linear``: ``y[r] = scale * act(weight[g] @ x[r] + bias[g])`` for the rows ``offsets[g] <= r < offsets[g + 1]``.
     x [rows, n_in], weight [groups, n_out, n_in], bias [groups, n_out]; fp32, bf16 or fp16; unit stride in the last dimension, any
-    other strides (a layer of theta is ``theta[:, a:b].unflatten(1, (n_out, n_in))``; an expanded weight is shared).  Rows outside all
-    groups are left as they are in ``out``, and undefined without one."""
+    other strides that keep rows apart (a layer of theta is ``theta[:, a:b].unflatten(1, (n_out, n_in))``; an expanded weight is shared).  Rows outside all
+    groups are left as they are in ``out``, and undefined without one.  ``out`` may not lie between the elements of another argument."""
     lib, where, device, dtype = load_library(), "grouped_linear", x.device, x.dtype
     _require_no_gradient(where, x, weight, bias, out)
     _require(x.is_cuda and dtype in TYPES and _rows(x, dtype, device), where, "x: fp32, bf16 or fp16 rows on a GPU")
