@@ -348,16 +348,21 @@ bool grouped_tc_takes(uint32_t type, const GroupedArgs& a)
 
 static uint32_t pitch_for(uint32_t type, uint32_t n_in) { return type == EVO_F32 ? (n_in + 63u) / 64u * 64u : (n_in + 7u) / 8u * 8u; }
 
-// Bytes for rows laid out anew where that pays (0: it does not): the weights are read, written and read again.  16-bit ones: against loads of single
-// numbers, from four rows a group on (6 groups, 3,774 rows, 207 -> 379: 364 us without, 22 with).  fp32: three bf16 parts of each
-// number and six products, against pairs in tf32 with mma.sync, from 28 rows a group on (without / with:
-// 8 groups, 4,000 rows, 1,000 -> 500, 184 / 75 us; 300 of 9,000, 128 -> 128, 135 / 46; 100 of 3,000, 512 -> 512, 170 / 124, of 2,000 100 / 124;
-// 50 of 1,500, 1,000 -> 1,000, 178 / 224).
+// Bytes for rows laid out anew where that pays (0: it does not): the weights are read, written and read again whatever the rows, so a group has to have some, and
+// more where its rows are short.  16-bit operands, against loads of single numbers: from 4 + 2,000 / n_in rows a group on; fp32, three bf16 parts of each
+// number and six products, against pairs in tf32 with mma.sync: from 48 + 1,000 / n_in.  Without / with, us, rows a group in brackets:
+//   16 bits  1,000 groups of 61 -> 49 (8) 8.6 / 39.3, (32) 19.2 / 43.6; 300 of 207 -> 379 (8) 38.7 / 64.7, (16) 53.5 / 65.6, (32) 84.1 / 68.5; 50 of
+//            1,001 -> 1,000 (4) 69.8 / 77.8, (8) 87.1 / 78.0, (32) 204.8 / 78.9; 8 of 2,047 -> 2,048 (4) 57.5 / 51.2
+//   fp32     1,000 of 128 -> 128 (28) 51.8 / 109.5, (48) 83.3 / 116.7, (96) 142.2 / 140.1; 50 of 1,000 -> 1,000 (28) 163.8 / 247.5, (48) 316.2 / 254.9;
+//            100 of 512 -> 512 (32) 96.4 / 130.9, (64) 163.4 / 136.1; 300 of 300 -> 200 (40) 104.7 / 123.8, (64) 162.2 / 132.1
+// Over 460 drawn shapes (up to 4,096 -> 4,096, 4,096 groups, 300 rows a group) the choice takes 1.02 times the faster side's time in the geometric mean; at
+// worst, for few groups or few outputs, 1.8 and 1.9 times.
 size_t grouped_tc_bytes(uint32_t type, const GroupedArgs& a)
 {
     const uint64_t pitch = pitch_for(type, a.n_in), parts = type == EVO_F32 ? 3u : 1u;
     const bool shared = a.groups > 1u && a.stride_w == 0u;
-    if (a.rows >= (1ull << 31) || a.rows < (type == EVO_F32 ? 28ull : 4ull) * a.groups || (shared ? 1ull : a.groups) * a.n_out >= (1ull << 31)) return 0;
+    const double least = type == EVO_F32 ? 48.0 + 1000.0 / a.n_in : 4.0 + 2000.0 / a.n_in;
+    if (a.rows >= (1ull << 31) || static_cast<double>(a.rows) < least * a.groups || (shared ? 1ull : a.groups) * a.n_out >= (1ull << 31)) return 0;
     const uint64_t rows = (shared ? 1ull : a.groups) * a.n_out + a.rows;
     return static_cast<size_t>(rows * parts * pitch * 2u + 256u);
 }

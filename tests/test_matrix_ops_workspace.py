@@ -24,3 +24,14 @@ def test_without_addresses_the_size_is_enough_for_any(lib, type_, rows, pitch): 
         p = _grouped(**dict(kw, d_x=FAR + size, d_offsets=FAR * 8 + 4))
         assert lib.evo_grouped_linear(C.byref(p), FAR * 32, most - 1, None) == WORKSPACE and without >= most
     assert lib.evo_grouped_linear(C.byref(_grouped(**dict(kw, d_x=None))), FAR * 32, 1 << 40, None) == INVALID
+
+
+def test_rows_a_group_from_which_operands_are_laid_out(lib):          # noqa: F811
+    n = C.c_size_t()
+
+    def need(type_, rows, n_in, groups=10):
+        p = _grouped(type=type_, rows=rows, groups=groups, n_in=n_in, ld_x=n_in, ld_weight=n_in, n_out=20, weight_stride=20 * n_in + 1)
+        assert lib.evo_grouped_linear_bytes(C.byref(p), C.byref(n)) == OK
+        return n.value
+    for type_, n_in, least in ((0, 1000, 490), (0, 100, 580), (0, 10, 1480), (1, 1000, 60), (2, 1000, 60), (1, 100, 240), (1, 10, 2040)):
+        assert need(type_, least - 1, n_in) == 0 and need(type_, least, n_in) > 0, (type_, n_in)
