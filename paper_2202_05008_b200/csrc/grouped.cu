@@ -9,7 +9,6 @@
 
 #include "grouped.h"
 #include "grouped_mma.cuh"
-#include "member_rows.h"
 
 namespace evo {
 namespace {
@@ -318,16 +317,6 @@ size_t grouped_bytes(uint32_t type, const GroupedArgs& a) { return grouped_tc_ta
 int launch_grouped(cudaStream_t st, uint32_t type, const GroupedArgs& a, void* work)
 {
     if (work || grouped_tc_takes(type, a)) return launch_grouped_tc(st, type, a, work);
-    // Many fp32 rows a group: kept in shared memory while the weights pass by (8 groups of 500 rows, 500 x 1,000: 184 us against 452; 1,000 of 20 rows,
-    // 200 x 300: 251 against 139)
-    if (type == EVO_F32 && a.rows > 24ull * a.groups && a.ld_w < (1ull << 31)) {
-        MemberArgs m;
-        std::memset(&m, 0, sizeof(m));
-        m.g = a;
-        m.w = static_cast<const float*>(a.w); m.b = static_cast<const float*>(a.b); m.stride_w = a.stride_w; m.stride_b = a.stride_b;
-        m.n_layers = 1u; m.sizes[0] = a.n_in; m.sizes[1] = a.n_out; m.ld_w[0] = static_cast<uint32_t>(a.ld_w);
-        if (member_plan(&m)) return launch_member_rows(st, m);
-    }
     return type == EVO_F32 ? launch_type<float>(st, a) : type == EVO_BF16 ? launch_type<__nv_bfloat16>(st, a) : launch_type<__half>(st, a);
 }
 

@@ -19,7 +19,6 @@ void policy_layers(const evo_actions& p, MemberArgs* a)
     for (uint32_t l = 0; l <= p.n_layers; ++l) a->sizes[l] = p.layer_sizes[l];
     for (uint32_t l = 0; l < p.n_layers; ++l) {
         a->w_at[l] = static_cast<uint32_t>(at);
-        a->ld_w[l] = p.layer_sizes[l];
         at += static_cast<uint64_t>(p.layer_sizes[l]) * p.layer_sizes[l + 1];
         a->b_at[l] = static_cast<uint32_t>(at);
         at += p.layer_sizes[l + 1];
@@ -163,7 +162,7 @@ evo_status evo_mlp_actions(const evo_actions* p, void* d_workspace, size_t works
     MemberArgs a;
     std::memset(&a, 0, sizeof(a));
     policy_layers(*p, &a);
-    a.w = p->d_theta; a.b = p->d_theta; a.stride_w = a.stride_b = p->ld_theta;
+    a.theta = p->d_theta; a.stride = p->ld_theta;
     GroupedArgs& g = a.g;
     g.x = p->d_observations; g.y = p->d_actions; g.offsets = p->d_offsets; g.wide_offsets = p->offsets_64;
     g.ld_x = p->rows > 1u ? p->ld_observations : 0u; g.ld_y = p->ld_actions; g.activation = EVO_ACT_TANH; g.scale = p->action_scale;

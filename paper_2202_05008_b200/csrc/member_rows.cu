@@ -1,5 +1,4 @@
-// fp32 rows through the layers of the member that they belong to: an MLP policy's get_actions in one launch, or one layer (products
-// grouped by member).
+// fp32 rows through the layers of the member that they belong to: an MLP policy's get_actions in one launch.
 //
 // A population's weights are read once, so their way from memory is the bound.  A warp takes a member (and 8 of its rows, or 16) through
 // all layers by itself, without a barrier: weight rows go from memory straight into the operand registers of mma.sync (grouped_mma.cuh: pairs of tf32
@@ -45,16 +44,15 @@ __global__ void __launch_bounds__(32 * (TEAM == 1u ? kAlone : TEAM), TEAM == 1u 
         const uint32_t member = a.chunks == 1u ? item : item / a.chunks, chunk = a.chunks == 1u ? 0u : item - member * a.chunks;
         uint64_t row, end;
         group_rows(a.g, member, &row, &end);
-        const float* const w = a.w + member * a.stride_w;
-        const float* const b = a.b ? a.b + member * a.stride_b : nullptr;
+        const float* const w = a.theta + member * a.stride;
         // (an item of one layer may have a part of its outputs)
         const uint32_t all = (a.sizes[1] + 15u) / 16u, per = a.chunks == 1u ? all : (all + a.chunks - 1u) / a.chunks;
         const uint32_t tile0 = min(chunk * per, all), tile1 = min(tile0 + per, all);
         auto rows_of = [&](Cursor& c) {                                     // what is beyond the last output is read as the last one, and not used
             const uint32_t o = c.tile * 16u + g, top = a.sizes[c.layer + 1u] - 1u;
             const float* const base = w + a.w_at[c.layer];
-            c.w0 = base + static_cast<uint64_t>(min(o, top)) * a.ld_w[c.layer] + 4u * q;
-            c.w1 = base + static_cast<uint64_t>(min(o + 8u, top)) * a.ld_w[c.layer] + 4u * q;
+            c.w0 = base + static_cast<uint64_t>(min(o, top)) * a.sizes[c.layer] + 4u * q;
+            c.w1 = base + static_cast<uint64_t>(min(o + 8u, top)) * a.sizes[c.layer] + 4u * q;
         };
         auto start = [&](Cursor& c, uint32_t layer) {                       // first tile of this warp in a layer, or in a later one where it has none
             for (c.layer = layer; c.layer < a.n_layers; ++c.layer) {
@@ -158,18 +156,16 @@ __global__ void __launch_bounds__(32 * (TEAM == 1u ? kAlone : TEAM), TEAM == 1u 
                     for (uint32_t h = 0; h < 2u; ++h) {
                         const uint32_t out = now.tile * 16u + g + 8u * h;
                         const bool there = out < a.sizes[layer + 1u];
-                        const float bias = b && there ? __ldg(b + a.b_at[layer] + out) : 0.f;
+                        const float bias = there ? __ldg(w + a.b_at[layer] + out) : 0.f;
 #pragma unroll
                         for (uint32_t c = 0; c < NT; ++c)
 #pragma unroll
                             for (uint32_t i = 0; i < 2u; ++i) {
                                 const uint32_t r = 8u * c + 2u * q + i;
-                                float s = gm::join(sum[c][2u * h + i], small[c][2u * h + i] + less[c][2u * h + i]) + bias;
-                                if (!last_layer || a.g.activation == EVO_ACT_TANH) s = gm::tanh32(s);
+                                const float s = gm::tanh32(gm::join(sum[c][2u * h + i], small[c][2u * h + i] + less[c][2u * h + i]) + bias);
                                 if (!last_layer) {
                                     y[r * a.ld + out] = there ? s : 0.f;                    // (zeros up to 16: the next layer's contracted index)
                                 } else if (there && r < rows) {
-                                    if (a.g.activation == EVO_ACT_RELU) s = s < 0.f ? 0.f : s;
                                     static_cast<float*>(a.g.y)[(row + r) * a.g.ld_y + out] = a.g.scale * s;
                                 }
                             }
@@ -191,7 +187,7 @@ bool member_plan(MemberArgs* a)
     a->aligned = 0;
     for (uint32_t l = 0; l < a->n_layers; ++l) {
         widest = std::max(widest, a->sizes[l]);
-        if ((reinterpret_cast<uintptr_t>(a->w) & 15u) == 0u && (a->w_at[l] | a->sizes[l] | a->ld_w[l] | a->stride_w) % 4u == 0u) a->aligned |= 1u << l;
+        if ((a->w_at[l] | a->sizes[l]) % 4u == 0u) a->aligned |= 1u << l;                   // (rows of theta are aligned)
     }
     if (widest > 512u) return false;
     // 4 more than a multiple of 32 floats: the eight rows of an MMA operand, 16 bytes a lane, fall on different banks
