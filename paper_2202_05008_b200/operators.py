@@ -32,8 +32,9 @@ def _require(condition: bool, where: str, what: str) -> None:
 
 
 def _require_no_gradient(where: str, *tensors: Optional[torch.Tensor]) -> None:
-    if torch.is_grad_enabled():
-        _require(not any(x is not None and x.requires_grad for x in tensors), where, "a tensor requires a gradient, and there is no backward pass")
+    for x in tensors:
+        if x is not None and x.requires_grad and torch.is_grad_enabled():
+            _require(False, where, "a tensor requires a gradient, and there is no backward pass")
 
 
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)      # the handle without a Stream object (2 us)
@@ -46,7 +47,8 @@ class _On:
 
     def __init__(self, device: torch.device, stream: Optional[torch.cuda.Stream], where: str):
         self.device, self.stream, self.guard = device, stream, None
-        _require(stream is None or stream.device == device, where, "a stream of another device")
+        if stream is not None:
+            _require(stream.device == device, where, "a stream of another device")
 
     def __enter__(self) -> int:
         if self.stream is not None:
@@ -144,8 +146,7 @@ def muon_step(center: torch.Tensor, m: torch.Tensor, v: torch.Tensor, gradient: 
                  x.numel() == center.numel(), where, "contiguous fp32 vectors of one length on one GPU")
     ns = _newton_schulz(ns_steps, tuple(coefficients), eps, where)
     # 0 selects a default in the structure; here it is the caller's: the smallest double instead, which is 0 in the kernel's fp32 (and 1 - beta is 1)
-    beta1, beta2, adam_eps = (x if x != 0 else _LEAST for x in (beta1, beta2, adam_eps))
-    cfg = Muon(C.sizeof(Muon), 0 if nesterov else 1, lr, momentum, weight_decay, beta1, beta2, adam_eps, ns)
+    cfg = Muon(C.sizeof(Muon), 0 if nesterov else 1, lr, momentum, weight_decay, beta1 or _LEAST, beta2 or _LEAST, adam_eps or _LEAST, ns)
     _require(1 <= step < 1 << 32, where, "the step counts from 1")
     dim = center.numel()
     items, n, need = _matrix_list(tuple(map(tuple, matrices)), dim)
