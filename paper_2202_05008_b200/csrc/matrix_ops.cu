@@ -24,7 +24,7 @@ static Group group_for(const Matrix& x, uint32_t blocks)
     g.gain = x.gain;
     return g;
 }
-static Choice choice_of(const Matrix& x) { return choose(std::min(x.rows, x.cols), std::max(x.rows, x.cols)); }
+static Choice choice_of(const Matrix& x) { return choose(std::min(x.rows, x.cols), std::max(x.rows, x.cols), x.count); }
 
 // Lists the large matrices from *at on, as many as a launch takes; advances *at.  False where their numbers do not fit 32 bits.
 static bool gather_large(const Matrix* list, size_t n, size_t* at, Args* a, size_t* bytes)

@@ -135,18 +135,28 @@ inline size_t small_bytes(uint32_t mp, uint32_t np, uint32_t blocks)
     return static_cast<size_t>(mp) * np * 4u + static_cast<size_t>(mp) * mp * 4u +
            (blocks > 1u ? (eights + blocks - 1u) / blocks * blocks * mp * 32u : 0u) + 2048u;
 }
-// Which kernel takes an m x n matrix, and how many blocks of a cluster.
+// Which kernel takes `count` m x n matrices, and how many blocks of a cluster each.
 enum Kind : uint32_t { kTiny16 = 0, kTiny32 = 1, kSmall = 2, kLarge = 3 };
 struct Choice { uint32_t kind, blocks; };
-inline Choice choose(uint32_t m, uint32_t n)
+constexpr uint32_t kTogether = 148;      // blocks of the kernel for small matrices that run at the same time, one an SM
+inline Choice cluster_for(uint32_t kind, uint32_t n)
 {
-    // (32 x 32 takes 25 us in registers and 16.6 us in shared memory, 28 x 128 21.5 and 22.2)
-    const uint32_t kind = m <= 16u ? kTiny16 : m <= 32u && n > kSmallCols ? kTiny32 : m <= kSmallRows ? kSmall : kLarge;
     const uint32_t cols = kind == kSmall ? kSmallCols : tiny_columns(kind + 1u);
-    if (kind != kLarge)
-        for (uint32_t b = 1; b <= kMostBlocks; b *= 2u)
-            if (n <= b * cols) return Choice{ kind, b };
+    for (uint32_t b = 1; b <= kMostBlocks; b *= 2u)
+        if (n <= b * cols) return Choice{ kind, b };
     return Choice{ kLarge, 0u };
+}
+inline Choice choose(uint32_t m, uint32_t n, uint32_t count)
+{
+    if (m <= 16u) return cluster_for(kTiny16, n);
+    if (m > kSmallRows) return Choice{ kLarge, 0u };
+    if (m > 32u) return cluster_for(kSmall, n);
+    // 17 to 32 rows in registers / in shared memory, us: 32 x 32 25 / 16.6, 28 x 128 21.6 / 22.1; 20 x 160 27.1 / 30.1, 32 x 256 32.2 / 32.9; 32 x 384 38.9 / 33.0,
+    // 24 x 700 74 / 35, 12 of them 76 / 36, 24 of them 76 / 70.  Blocks of the second hold a quarter of the columns, so it falls behind where they
+    // do not all run at once: 40 of 20 x 300 35.5 / 63.7, 300 of 24 x 600 349 / 682.  Beyond 1,024 columns the other side is a launch per product: 32 x 1,100 95 / 171.
+    const Choice shared = cluster_for(kSmall, n);
+    const bool registers = n > kSmallCols && (n <= 2u * kSmallCols || shared.kind == kLarge || static_cast<uint64_t>(shared.blocks) * count > kTogether);
+    return registers ? cluster_for(kTiny32, n) : shared;
 }
 
 // Buffers of a large matrix in the workspace, each a matrix of high parts followed by one of low parts: X, the next X, A, B.

@@ -87,3 +87,13 @@ def test_orthogonal_matrices_of_17_to_32_rows_stay_close_to_orthogonal():
     want = (u * t) @ vt
     assert float((exact(g) - want).norm() / want.norm()) < 1e-12
     check(orthogonalize(g), g)
+
+
+@pytest.mark.parametrize("count,rows,cols", [(40, 20, 300), (100, 24, 700), (30, 18, 600), (200, 513, 32), (200, 100, 300), (300, 12, 1500)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16])
+def test_more_matrices_than_run_at_once(count, rows, cols, dtype):
+    x = torch.stack([matrix(rows, cols, k, dtype=dtype) for k in range(count)])
+    got = orthogonalize(x)
+    for k in (0, 1, count // 2, count - 1):
+        check(got[k], x[k])
+    assert torch.equal(orthogonalize(x), got)
