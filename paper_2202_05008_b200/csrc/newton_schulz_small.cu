@@ -14,6 +14,7 @@ namespace evo {
 namespace ns {
 
 constexpr uint32_t kThreads = 512;
+constexpr uint32_t kHalfCols = 128;                                        // tensor memory of an accumulator (512 threads of 119 to 128 registers: a block an SM)
 constexpr uint32_t kItems = kSmallCols * kSmallRows / 8u / kThreads;       // eights of elements of a thread
 
 __device__ __forceinline__ void cluster_sync()
@@ -87,10 +88,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_small(const __grid_constant_
         limit = a.wait_log2;
         abort_flag = 0;
     }
-    // two accumulators of a product's columns, the large products' and the small ones'; no more tensor memory than that, so that small
-    // matrices share an SM
-    const uint32_t half_cols = max(mp, np) <= 64u ? 64u : 128u;
-    if (warp == 0) tmem_alloc(smem_u32(&slot), 2u * half_cols);
+    // two accumulators of a product's columns, the large products' and the small ones'
+    if (warp == 0) tmem_alloc(smem_u32(&slot), 2u * kHalfCols);
 
     // an item is eight j of one i; neighbouring lanes read neighbouring elements of the source
     const uint32_t jcs = np / 8u, items = jcs * mp;
@@ -166,8 +165,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_small(const __grid_constant_
 #pragma unroll 4
         for (uint32_t k = 0; k < K / 16u; ++k) {
             umma_bf16(tmem, ph, rh, idesc, k != 0u);
-            umma_bf16(tmem + half_cols, ph, rl, idesc, k != 0u);
-            umma_bf16(tmem + half_cols, pl, rh, idesc, 1u);
+            umma_bf16(tmem + kHalfCols, ph, rl, idesc, k != 0u);
+            umma_bf16(tmem + kHalfCols, pl, rh, idesc, 1u);
             ph += p_step; pl += p_step; rh += r_step; rl += r_step;
         }
         if (!drop) umma_commit(smem_u32(&bar));
@@ -184,10 +183,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_small(const __grid_constant_
         uint32_t u[2][8], v[2][8];
         const uint32_t from = tmem + lanes + mine(c) * 8u;
         tmem_ld8_issue(from, u[0]);
-        tmem_ld8_issue(from + half_cols, v[0]);
+        tmem_ld8_issue(from + kHalfCols, v[0]);
         if (two) {
             tmem_ld8_issue(from + 8u, u[1]);
-            tmem_ld8_issue(from + half_cols + 8u, v[1]);
+            tmem_ld8_issue(from + kHalfCols + 8u, v[1]);
         }
         wait_loads();
 #pragma unroll
@@ -361,7 +360,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_ns_small(const __grid_constant_
         }
     }
     __syncthreads();
-    if (warp == 0) tmem_dealloc(tmem, 2u * half_cols);
+    if (warp == 0) tmem_dealloc(tmem, 2u * kHalfCols);
     if constexpr (CLUSTER) cluster_sync();                                 // no copy between the blocks is left when one goes
     if (late) dep_wait();
 }
