@@ -408,7 +408,7 @@ evo_status evo_grouped_linear(const evo_grouped* p, void* d_workspace, size_t wo
  * with the parameters theta[m] (fp32, pitch ld_theta: a multiple of 4 floats, rows 16-byte aligned) in the
  * layout of evo_ask.  Offsets, rows without a member and overlaps as above.
  * Errors: INVALID_ARG, WORKSPACE, UNSUPPORTED, CUDA.  Workspace: for what a layer leaves to the next where the layers
- * are taken one by one (layers of more than 512, large populations); else 0.  tanh is off by at most 2.5e-7 of its value.
+ * are taken one by one (layers of more than 512, large populations); else 0.  tanh is off by at most 5.5e-7 of its value.
  */
 typedef struct evo_actions {
     uint32_t struct_size;          /* sizeof(evo_actions), checked */

@@ -43,7 +43,8 @@ __device__ __forceinline__ void split(float x, uint32_t& hi, uint32_t& lo)
 __device__ __forceinline__ float join(float large, float small) { return isfinite(large) ? large + small : large; }
 
 // tanh without branches: up to 1/2 the series of tanh to x^13 (what is left out is below 1e-7 of the result), beyond it
-// 1 - 2 / (e^2|x| + 1) with the hardware's exponential (2^-22 relative): 2e-7 of the result at worst
+// 1 - 2 / (e^2|x| + 1) with the hardware's exponential (2^-22 relative) and reciprocal (2^-23): by these bounds 5.5e-7 of the result at worst, at 1/2.
+// Measured over all multiples of 2^-18 up to 16: 2.2e-7, at 0.568
 __device__ __forceinline__ float tanh32(float x)
 {
     const float a = fabsf(x), s = x * x;
