@@ -1,4 +1,4 @@
-// Arguments and launchers of the products grouped by member (grouped.cu, grouped_tc.cu) and of the policy's actions (mlp_actions.cu).
+// Arguments and launchers of the products grouped by member (grouped.cu, grouped_tc.cu).
 #pragma once
 #include "internal.h"
 

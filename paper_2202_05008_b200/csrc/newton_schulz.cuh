@@ -1,4 +1,4 @@
-// Device code that both Newton-Schulz kernels use: how a matrix element is read and written, and the fp16 pairs.
+// Device code that the Newton-Schulz kernels of all sizes use: how a matrix element is read and written, and the fp16 pairs.
 //
 // The iteration (the odd quintic that Muon made common): X = G / (|G|_F + eps), then `steps` times
 //     A = X X',   B = b A + c A^2,   X <- a X + B X.

@@ -1,5 +1,5 @@
-// Newton-Schulz iteration of matrices of up to 32 rows (the shorter side counts as rows): all steps in one launch, everything in
-// registers.
+// Newton-Schulz iteration of matrices of up to 32 rows (the shorter side counts as rows): all steps in one launch, X in registers
+// (of the instances for 17 to 32 rows, 56 bytes a thread are spilled in clusters and 188 without).
 //
 // A warp owns 16 columns of X at a time, in the layout of an mma.sync accumulator (a lane has two neighbouring columns of rows g and
 // g + 8, g = lane / 4).  Packed, that is the first operand of X X' and, rows 0-7 and 8-15 apart, also the second; transposed within
