@@ -112,6 +112,12 @@ __device__ __forceinline__ void tile_sums(const T* w0, const T* w1, const T* con
 #pragma unroll
             for (int i = 0; i < 4; ++i) c[t][i] = 0.f;
         for (uint32_t k = k0; k < k1; k += 128u) {
+            // (taken out of the tensor core, which cuts its sums off, every 128 numbers)
+            float part[NT][4];
+#pragma unroll
+            for (uint32_t t = 0; t < NT; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) part[t][i] = 0.f;
             uint4 u[4], v[4];
 #pragma unroll
             for (uint32_t s = 0; s < 4u; ++s) {
@@ -125,10 +131,14 @@ __device__ __forceinline__ void tile_sums(const T* w0, const T* w1, const T* con
 #pragma unroll
                 for (uint32_t t = 0; t < NT; ++t) {
                     const uint4 r = load16<T, VEC>(x[t], k + 32u * s + 8u * q, n_in);
-                    gm::mma_16<T>(c[t], a0, r.x, r.y);
-                    gm::mma_16<T>(c[t], a1, r.z, r.w);
+                    gm::mma_16<T>(part[t], a0, r.x, r.y);
+                    gm::mma_16<T>(part[t], a1, r.z, r.w);
                 }
             }
+#pragma unroll
+            for (uint32_t t = 0; t < NT; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) c[t][i] += part[t][i];
         }
     }
 }

@@ -30,8 +30,10 @@ constexpr uint32_t kThreads = 320;
 
 // The tensor core cuts its sums off: fp32 rows 1e-6 off per 1,000 of the contracted index.  So the last pass (the large products; the others lie in
 // front of its first chunks) is added up in parts of 8 chunks of 64, in fp32 in y (2,060
-// numbers 2.1e-6 off in one part).
-constexpr uint32_t kSegment = 8;
+// numbers 2.1e-6 off in one part).  Of 16-bit operands 6.6e-9 of a sum of numbers of one sign is lost per number (262,144: 1.6e-3, 1,048,576: 7e-3), which
+// one part may have of 8,192 numbers; longer sums are added up in parts of 64 chunks (2.7e-5) in the registers of the threads that take them out, which hold
+// those of 128 rows.
+constexpr uint32_t kSegment = 8, kLongSegment = 64, kLong = 8192, kLongRows = 128;
 
 struct TcArgs {
     GroupedArgs g;
@@ -110,8 +112,8 @@ struct Walk {
     }
 };
 
-// T: type of the operands, O: of bias and result
-template <typename T, typename O>
+// T: type of the operands, O: of bias and result; LONG: a sum of 16-bit operands in several parts
+template <typename T, typename O, bool LONG>
 __global__ void __launch_bounds__(kThreads, 1) k_grouped_tc(const __grid_constant__ TcArgs p)
 {
     extern __shared__ uint8_t raw[];
@@ -143,7 +145,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_grouped_tc(const __grid_constan
     };
     // the step behind the part of a sum that begins at step k
     const uint32_t small_steps = steps - chunks;
-    auto part_end = [&](uint32_t k) { return p.passes > 1u ? min(steps, max(k, small_steps) + kSegment) : steps; };
+    auto part_end = [&](uint32_t k) { return LONG ? min(steps, k + kLongSegment) : p.passes > 1u ? min(steps, max(k, small_steps) + kSegment) : steps; };
     auto aborted = [&] { return __any_sync(0xffffffffu, abort_flag) != 0; };
     Walk walk;
     walk.fill(p);
@@ -228,13 +230,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_grouped_tc(const __grid_constan
                 else bias = __bfloat162float(b);
             }
             O* const y = static_cast<O*>(a.y) + row * a.ld_y + o;
+            float held[LONG ? kLongRows / 64u : 1u][32];          // the sum of the parts before this one
             for (uint32_t first = 0, end = 0; end < steps; first = end) {
                 end = part_end(first);
                 wait(&done[acc], acc_phase);
                 tc_fence_after();
                 const float scale = abort_flag ? __int_as_float(0x7FC00000) : a.scale;
-                // the halves take every other 32 rows
-                for (uint32_t c = half * 32u; c < rows; c += 64u) {
+                auto take = [&](uint32_t c, float (&so_far)[32]) {
                     uint32_t u[4][8];
                     tmem_ld32_issue(tmem + acc * kMostRows + (quarter << 21) + c, u);
                     tmem_ld8x4_fence(u[0], u[1], u[2], u[3]);
@@ -243,6 +245,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_grouped_tc(const __grid_constan
                     float v[32];
 #pragma unroll
                     for (uint32_t i = 0; i < 32u; ++i) v[i] = __uint_as_float(u[i / 8u][i % 8u]);
+                    if constexpr (LONG) {
+#pragma unroll
+                        for (uint32_t i = 0; i < 32u; ++i) so_far[i] = v[i] = first ? so_far[i] + v[i] : v[i];
+                        if (end != steps) return;
+                    }
                     if constexpr (std::is_same<O, float>::value) {
                         if (first != 0u) {
 #pragma unroll
@@ -253,7 +260,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_grouped_tc(const __grid_constan
                             for (uint32_t i = 0; i < 32u; ++i)
                                 if (i < count) to[i * a.ld_y] = v[i];
                             __syncwarp();
-                            continue;
+                            return;
                         }
                     }
 #pragma unroll
@@ -275,6 +282,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_grouped_tc(const __grid_constan
                         to += a.ld_y;
                     }
                     __syncwarp();
+                };
+                // the halves take every other 32 rows
+                if constexpr (LONG) {
+#pragma unroll
+                    for (uint32_t i = 0; i < kLongRows / 64u; ++i)
+                        if (half * 32u + i * 64u < rows) take(half * 32u + i * 64u, held[i]);
+                } else {
+                    for (uint32_t c = half * 32u; c < rows; c += 64u) take(c, held[0]);
                 }
                 tc_fence_before();
                 __syncwarp();
@@ -371,11 +386,11 @@ size_t grouped_tc_bytes(uint32_t type, const GroupedArgs& a)
 // more a group); a tile takes as long as its operands, 128 rows of weights and its own rows, and the blocks take tiles in waves.  64 / 128 / 192 /
 // 256 rows: 8,192 even rows of 32 groups, 1,024 -> 4,096, 209 / 119 / 118 / 82 us; 3,774 of 6, 1,207 -> 2,379, 103 / 81 / 69 / 73;
 // 3,000 of 100, 1,024 -> 1,024, 55 / 59 / 59 / 64 (fewer rows a stage are more stages in flight).
-static uint32_t rows_of_a_tile(const GroupedArgs& a, uint32_t out_tiles)
+static uint32_t rows_of_a_tile(const GroupedArgs& a, uint32_t out_tiles, uint32_t limit)
 {
-    uint32_t best = kMostRows;
+    uint32_t best = limit;
     double least = 1e300;
-    for (uint32_t most = 64u; most <= kMostRows; most += 64u) {
+    for (uint32_t most = 64u; most <= limit; most += 64u) {
         const double used = static_cast<double>(a.rows < a.groups ? a.rows : a.groups), guess = static_cast<double>(a.rows) / most + 0.5 * used;
         const double tiles = guess > used ? guess : used, time = std::ceil(tiles * out_tiles / kSms) * (128.0 + a.rows / tiles);
         if (time < least * 0.999) { least = time; best = most; }
@@ -430,11 +445,14 @@ int launch_grouped_tc(cudaStream_t st, uint32_t type, const GroupedArgs& in, voi
         if (f(&p.x[box], t, 2, const_cast<void*>(a.x), xd, xs, xb[box], one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
             return -1;
-    p.most_rows = rows_of_a_tile(a, p.out_tiles);
+    const bool parts_held = type != EVO_F32 && a.n_in > kLong;
+    p.most_rows = rows_of_a_tile(a, p.out_tiles, parts_held ? kLongRows : kMostRows);
     p.stages = kRing / (kWBytes + p.most_rows * 128u);
     if (p.stages > kMostStages) p.stages = kMostStages;
     const uint64_t used = a.rows < a.groups ? a.rows : a.groups, most = (a.rows / p.most_rows + used) * p.out_tiles;
-    auto kernel = type == EVO_F16 ? k_grouped_tc<__half, __half> : type == EVO_BF16 ? k_grouped_tc<__nv_bfloat16, __nv_bfloat16> : k_grouped_tc<__nv_bfloat16, float>;
+    auto kernel = type == EVO_F32 ? k_grouped_tc<__nv_bfloat16, float, false>
+                : type == EVO_F16 ? (parts_held ? k_grouped_tc<__half, __half, true> : k_grouped_tc<__half, __half, false>)
+                                  : (parts_held ? k_grouped_tc<__nv_bfloat16, __nv_bfloat16, true> : k_grouped_tc<__nv_bfloat16, __nv_bfloat16, false>);
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) != cudaSuccess) return -1;
     return launch_dependent(kernel, dim3(most < kSms ? static_cast<uint32_t>(most) : kSms), dim3(kThreads), kSmem, st, p) == cudaSuccess ? launches : -1;
 }

@@ -106,3 +106,22 @@ def test_solver_actions_with_a_matrix_of_the_caller():
     assert ((s.actions(obs, off, theta=other).double() - want).abs() <= bound).all()
     assert s.sync_status() == 0
     s.close()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("n_in", [8192, 8200, 20001, 65536, 262144])
+@pytest.mark.parametrize("rows", [(1, 2), (33, 20), (150, 70)])
+def test_sums_of_many_numbers_of_one_sign(n_in, rows, dtype):
+    """The tensor core cuts up to 2^-23 of a running sum off with every 16 numbers of 16 bits (8 of tf32) that it adds.  Sums stay in it for at most 8,192 numbers,
+    2^-14 of the result; longer ones are added up in fp32, a rounding of 2^-24 for every 64 or more numbers.  The result is rounded once.  (fp32: in it for
+    512 numbers at most, 2^-17, and 2^-20 for the operands.)"""
+    gen = torch.Generator(device="cuda").manual_seed(n_in)
+    x = (torch.rand(sum(rows), n_in, generator=gen, device="cuda") * 0.5 + 0.5).to(dtype)
+    w = ((torch.rand(2, 24, n_in, generator=gen, device="cuda") * 0.5 + 0.5) / n_in).to(dtype)
+    off = torch.tensor([0, rows[0], sum(rows)], device="cuda")
+    got = grouped_linear(x, w, off).double()
+    want = exact(x, w, off, None)[0]
+    lost = 2.0 ** -17 + 2.0 ** -20 if dtype == F32 else 2.0 ** -14
+    bound = torch.finfo(dtype).eps / 2 * 1.001 + lost + n_in / 64 * 2.0 ** -24 + (2.0 ** -25 / want if dtype == F16 else 0)
+    err = (got - want).abs() / want
+    assert (err <= bound).all(), float((err / bound).max())
