@@ -322,7 +322,7 @@ int launch_type(cudaStream_t st, const GroupedArgs& a)
 
 }  // namespace
 
-size_t grouped_bytes(uint32_t type, const GroupedArgs& a) { return grouped_tc_takes(type, a) ? 0u : grouped_tc_bytes(type, a); }
+size_t grouped_bytes(uint32_t type, const GroupedArgs& a) { return grouped_tc_addressable(type, a) ? 0u : grouped_tc_bytes(type, a); }
 
 int launch_grouped(cudaStream_t st, uint32_t type, const GroupedArgs& a, void* work)
 {

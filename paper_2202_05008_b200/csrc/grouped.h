@@ -34,7 +34,8 @@ __device__ __forceinline__ void group_rows(const GroupedArgs& a, uint32_t g, uin
 
 size_t grouped_bytes(uint32_t type, const GroupedArgs& a);             // workspace
 int launch_grouped(cudaStream_t st, uint32_t type, const GroupedArgs& a, void* work);
-// grouped_tc.cu: 16-bit types whose rows TMA can address, or (work) rows that are laid out for it first
+// grouped_tc.cu: 16-bit types whose rows TMA can address as they lie, where that pays, or (work) rows that are laid out for it first
+bool grouped_tc_addressable(uint32_t type, const GroupedArgs& a);
 bool grouped_tc_takes(uint32_t type, const GroupedArgs& a);
 size_t grouped_tc_bytes(uint32_t type, const GroupedArgs& a);
 int launch_grouped_tc(cudaStream_t st, uint32_t type, const GroupedArgs& a, void* work);

@@ -125,3 +125,14 @@ def test_sums_of_many_numbers_of_one_sign(n_in, rows, dtype):
     bound = torch.finfo(dtype).eps / 2 * 1.001 + lost + n_in / 64 * 2.0 ** -24 + (2.0 ** -25 / want if dtype == F16 else 0)
     err = (got - want).abs() / want
     assert (err <= bound).all(), float((err / bound).max())
+
+
+@pytest.mark.parametrize("groups,per,n_in,n_out", [(300, 2, 40, 64), (300, 5, 40, 64), (64, 1, 2048, 136), (200, 4, 512, 72), (1, 5, 1024, 264), (1, 40, 1024, 264), (900, 17, 104, 8)])
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_aligned_rows_of_few_and_many_a_group(groups, per, n_in, n_out, dtype):
+    """16-bit operands that both kernels take as they lie, on either side of where the choice changes."""
+    lengths = [per + (g % 3 - 1 if g + 1 < groups else 0) if per > 1 else g % 2 * 2 for g in range(groups)]
+    x, w, b, off = make(groups, lengths, n_in, n_out, dtype, lead=1, tail=3)
+    y = torch.full((x.shape[0], n_out), 7.0, dtype=dtype, device="cuda")
+    check(grouped_linear(x, w, off, b, activation="tanh", scale=0.5, out=y), x, w, off, b, "tanh", 0.5)
+    assert (y[:1] == 7).all() and (y[-3:] == 7).all()
