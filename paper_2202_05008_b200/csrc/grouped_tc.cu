@@ -362,16 +362,17 @@ bool grouped_tc_addressable(uint32_t type, const GroupedArgs& a)
 }
 
 // Whether they pay against mma.sync with 16-byte loads: not with few rows a group where weight rows are short, where every warp's walk over many groups takes longer
-// than the products (26 ns a group), and where a tile for each 128 outputs leaves SMs without one.  us, without / with, rows a group in brackets:
+// than the products (26 ns a group), where a tile for each 128 outputs leaves SMs without one, and where most of a tile's outputs do not exist.  us, without / with, rows
+// a group in brackets:
 //   4,096 of 128 -> 128 (4) 40 / 114, (32) 79 / 118; 200 of 512 -> 512 (4) 30.1 / 31.8, (8) 35.9 / 32.0, (32) 64 / 33; 64 of 2,048 -> 2,048 (1) 96 / 87, (8) 133 / 100;
-//   1 of 4,096 -> 4,096 (8) 18.4 / 29.8, (32) 33.6 / 29.8; 8 of them (1) 55 / 59, (4) 67 / 59; 3,303 of 96 -> 24 (2) 11.6 / 89.
-// Over 284 shapes (220 of them drawn, up to 4,096 -> 4,096, 4,096 groups, 300 rows a group) 1.01 times the faster side's time in the geometric mean, 2.0 at worst;
+//   1 of 4,096 -> 4,096 (8) 18.4 / 29.8, (32) 33.6 / 29.8; 8 of them (1) 55 / 59, (4) 67 / 59; 500 of 2,048 -> 16 (7) 24.7 / 62.5.
+// Over 809 shapes (740 of them drawn, up to 4,096 -> 4,096, 4,096 groups, 300 rows a group) 1.013 times the faster side's time in the geometric mean, 1.85 at worst;
 // with the tensor cores always, 1.45 and 7.7.
 bool grouped_tc_takes(uint32_t type, const GroupedArgs& a)
 {
     if (!grouped_tc_addressable(type, a)) return false;
-    const double rows = static_cast<double>(a.rows), groups = a.groups, tiles = std::fmin(rows, groups) * ((a.n_out + 127u) / 128u);
-    return rows >= groups * (1000.0 / a.n_in + groups / 130.0 + 20.0 * std::fmax(0.0, 1.0 - tiles / kSms));
+    const double rows = static_cast<double>(a.rows), groups = a.groups, out_tiles = (a.n_out + 127u) / 128u, idle = std::fmax(0.0, 1.0 - std::fmin(rows, groups) * out_tiles / kSms);
+    return rows >= groups * (1000.0 / a.n_in + groups / 133.0 + 0.5 * (out_tiles * 128.0 / a.n_out - 1.0) + 24.0 * idle * idle * idle);
 }
 
 static uint32_t pitch_for(uint32_t type, uint32_t n_in) { return type == EVO_F32 ? (n_in + 63u) / 64u * 64u : (n_in + 7u) / 8u * 8u; }
