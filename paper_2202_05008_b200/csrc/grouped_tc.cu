@@ -336,18 +336,19 @@ __global__ void __launch_bounds__(256) k_lay_out(const __grid_constant__ Grouped
         for (uint32_t k = 2u * lane; k < a.n_in; k += 64u)
             *reinterpret_cast<uint32_t*>(dst + k) = s[k] | (k + 1u < a.n_in ? static_cast<uint32_t>(s[k + 1u]) << 16 : 0u);
     } else {
+        // An infinity or a NaN has no further parts (the product of an infinity's with a zero would be NaN); a number that would round to an infinity, from 3.396e38 on, is
+        // cut off instead.  (Without branches, so that the loads of several numbers run ahead: 61 groups of 159 rows, 2,428 -> 5, 169 us, with them 197.)
+#pragma unroll 4
         for (uint32_t k = lane; k < pitch; k += 32u) {
-            // (an infinity has no further parts: their product with a zero would be NaN.  A number that would round to one is cut off instead: above
-            // 3.396e38)
-            float x = k < a.n_in ? src[k] : 0.f;
-#pragma unroll
-            for (uint32_t p = 0; p < 3u; ++p) {
-                __nv_bfloat16 b = __float2bfloat16_rn(x);
-                if (p == 0u && isinf(__bfloat162float(b)) && !isinf(x)) b = __float2bfloat16_rz(x);
-                const float back = __bfloat162float(b);
-                dst[p * pitch + k] = __bfloat16_as_ushort(b);
-                x = isfinite(back) ? x - back : 0.f;
-            }
+            const float x = k < a.n_in ? src[k] : 0.f;
+            uint32_t part = __bfloat16_as_ushort(__float2bfloat16_rn(x));
+            part -= (part & 0x7FFFu) == 0x7F80u && fabsf(x) <= 3.402823466e38f ? 1u : 0u;
+            const float back = __uint_as_float(part << 16);
+            const float rest = fabsf(back) <= 3.402823466e38f ? x - back : 0.f;
+            const __nv_bfloat16 second = __float2bfloat16_rn(rest);
+            dst[k] = static_cast<uint16_t>(part);
+            dst[pitch + k] = __bfloat16_as_ushort(second);
+            dst[2u * pitch + k] = __bfloat16_as_ushort(__float2bfloat16_rn(rest - __bfloat162float(second)));
         }
     }
 }
