@@ -362,6 +362,13 @@ bool grouped_tc_addressable(uint32_t type, const GroupedArgs& a)
     return a.rows < (1ull << 31) && a.ld_x < (1ull << 38) && a.ld_w < (1ull << 38) && a.stride_w < (1ull << 38);
 }
 
+// The SMs that a tile for each 128 outputs of every group with rows leaves without one
+static double idle_share(const GroupedArgs& a)
+{
+    const double tiles = std::fmin(static_cast<double>(a.rows), a.groups) * ((a.n_out + 127u) / 128u);
+    return std::fmax(0.0, 1.0 - tiles / kSms);
+}
+
 // Whether they pay against mma.sync with 16-byte loads: not with few rows a group where weight rows are short, where every warp's walk over many groups takes longer
 // than the products (26 ns a group), where a tile for each 128 outputs leaves SMs without one, and where most of a tile's outputs do not exist.  us, without / with, rows
 // a group in brackets:
@@ -372,26 +379,25 @@ bool grouped_tc_addressable(uint32_t type, const GroupedArgs& a)
 bool grouped_tc_takes(uint32_t type, const GroupedArgs& a)
 {
     if (!grouped_tc_addressable(type, a)) return false;
-    const double rows = static_cast<double>(a.rows), groups = a.groups, out_tiles = (a.n_out + 127u) / 128u, idle = std::fmax(0.0, 1.0 - std::fmin(rows, groups) * out_tiles / kSms);
+    const double rows = static_cast<double>(a.rows), groups = a.groups, out_tiles = (a.n_out + 127u) / 128u, idle = idle_share(a);
     return rows >= groups * (1000.0 / a.n_in + groups / 133.0 + 0.5 * (out_tiles * 128.0 / a.n_out - 1.0) + 24.0 * idle * idle * idle);
 }
 
 static uint32_t pitch_for(uint32_t type, uint32_t n_in) { return type == EVO_F32 ? (n_in + 63u) / 64u * 64u : (n_in + 7u) / 8u * 8u; }
 
 // Bytes for rows laid out anew where that pays (0: it does not): the weights are read, written and read again whatever the rows, so a group has to have some, and
-// more where its rows are short.  16-bit operands, against loads of single numbers: from 4 + 2,000 / n_in rows a group on; fp32, three bf16 parts of each
-// number and six products, against pairs in tf32 with mma.sync: from 48 + 1,000 / n_in.  Without / with, us, rows a group in brackets:
+// more where its rows are short, where there are many groups to walk over, and where a tile for each 128 outputs leaves SMs without one.  16-bit operands, against loads of
+// single numbers; fp32, three bf16 parts of each number and six products, against pairs in tf32 with mma.sync.  Without / with, us, rows a group in brackets:
 //   16 bits  1,000 groups of 61 -> 49 (8) 8.6 / 39.3, (32) 19.2 / 43.6; 300 of 207 -> 379 (8) 38.7 / 64.7, (16) 53.5 / 65.6, (32) 84.1 / 68.5; 50 of
 //            1,001 -> 1,000 (4) 69.8 / 77.8, (8) 87.1 / 78.0, (32) 204.8 / 78.9; 8 of 2,047 -> 2,048 (4) 57.5 / 51.2
-//   fp32     1,000 of 128 -> 128 (28) 51.8 / 109.5, (48) 83.3 / 116.7, (96) 142.2 / 140.1; 50 of 1,000 -> 1,000 (28) 163.8 / 247.5, (48) 316.2 / 254.9;
-//            100 of 512 -> 512 (32) 96.4 / 130.9, (64) 163.4 / 136.1; 300 of 300 -> 200 (40) 104.7 / 123.8, (64) 162.2 / 132.1
-// Over 460 drawn shapes (up to 4,096 -> 4,096, 4,096 groups, 300 rows a group) the choice takes 1.02 times the faster side's time in the geometric mean; at
-// worst, for few groups or few outputs, 1.8 and 1.9 times.
+//   fp32     1,000 of 128 -> 128 (28) 51.8 / 102, (48) 83.3 / 109; 50 of 1,000 -> 1,000 (28) 163.8 / 231, (48) 316 / 237; 100 of 512 -> 512 (32) 96 / 122, (64) 163 / 127;
+//            38 of 1,684 -> 27 (45) 359 / 96
+// Over 1,100 drawn shapes (up to 4,096 -> 4,096, 4,096 groups, 300 rows a group) the choice takes 1.02 times the faster side's time in the geometric mean.
 size_t grouped_tc_bytes(uint32_t type, const GroupedArgs& a)
 {
     const uint64_t pitch = pitch_for(type, a.n_in), parts = type == EVO_F32 ? 3u : 1u;
-    const bool shared = a.groups > 1u && a.stride_w == 0u;
-    const double least = type == EVO_F32 ? 48.0 + 1000.0 / a.n_in : 4.0 + 2000.0 / a.n_in;
+    const bool shared = a.groups > 1u && a.stride_w == 0u, fp32 = type == EVO_F32;
+    const double least = (fp32 ? 24.0 : 4.0) + 1500.0 / a.n_in + std::fmin(a.groups, 400.0) / 50.0 + (fp32 ? 8.0 : 4.0) * idle_share(a);
     if (a.rows >= (1ull << 31) || static_cast<double>(a.rows) < least * a.groups || (shared ? 1ull : a.groups) * a.n_out >= (1ull << 31)) return 0;
     const uint64_t rows = (shared ? 1ull : a.groups) * a.n_out + a.rows;
     return static_cast<size_t>(rows * parts * pitch * 2u + 256u);

@@ -33,5 +33,5 @@ def test_rows_a_group_from_which_operands_are_laid_out(lib):          # noqa: F8
         p = _grouped(type=type_, rows=rows, groups=groups, n_in=n_in, ld_x=n_in, ld_weight=n_in, n_out=20, weight_stride=20 * n_in + 1)
         assert lib.evo_grouped_linear_bytes(C.byref(p), C.byref(n)) == OK
         return n.value
-    for type_, n_in, least in ((0, 1000, 490), (0, 100, 580), (0, 10, 1480), (1, 1000, 60), (2, 1000, 60), (1, 100, 240), (1, 10, 2040)):
+    for type_, n_in, least in ((0, 1000, 332), (0, 100, 467), (0, 10, 1817), (1, 1000, 95), (2, 1000, 95), (1, 100, 230), (1, 10, 1580)):
         assert need(type_, least - 1, n_in) == 0 and need(type_, least, n_in) > 0, (type_, n_in)
