@@ -377,7 +377,7 @@ evo_status evo_muon_step(const evo_muon* cfg, const evo_matrix* list, uint32_t n
  * offsets[groups + 1] (int32, or int64 with offsets_64) lies on the device and does not fall; groups may be empty.  Rows of y
  * that belong to no group are left as they are.  (Offsets that fall or leave [0, rows] give wrong rows, but nothing
  * outside the arrays is touched.)  Sums in fp32, of 16-bit operands cut off by up to 6e-5 (2^-14); fp32 operands count with 21 bits and more (numbers below 1e-31 with fewer).  What an infinity or a NaN of the operands
- * goes into is an infinity or NaN, and nothing else is, unless the sum leaves fp32's range (with many rows of fp32 it may be NaN where an infinity is due; with
+ * goes into is an infinity or NaN, and nothing else is, unless a sum leaves fp32's range or a result its type's (with many rows of fp32 it may be NaN where an infinity is due; with
  * few rows fp32 numbers above 3.4011e38 count as infinities).  y may not overlap anything, from the first to the last element of each array (columns
  * of one wider array do).
  * Errors: INVALID_ARG, WORKSPACE, UNSUPPORTED (more than 2^31 blocks), CUDA.  Workspace 0 unless there are many rows a group in a
