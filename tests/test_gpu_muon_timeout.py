@@ -17,11 +17,11 @@ def _workload(sizes):
 
 @pytest.mark.parametrize("sizes", SIZES, ids=lambda s: "-".join(map(str, s)))
 def test_a_wait_that_runs_out_leaves_nan_in_its_matrix_and_nowhere_else(sizes):
-    """With EVO_DEBUG_DROP_COMPLETION the first block of a launch never hears of its first product, and with a limit of 2^20 clocks gives up after half
-    a millisecond; it and, in a cluster, the blocks that it shares a matrix with return by themselves."""
+    """With EVO_DEBUG_DROP_COMPLETION the first block of a launch never hears of its first product, and with a limit of 2^23 clocks gives up after some
+    four milliseconds; it and, in a cluster, the blocks that it shares a matrix with return by themselves."""
     w = _workload(sizes)
     first = sizes[0] * sizes[1]
-    plain, s = Solver(w), Solver(w, wait_cycles_log2=20, debug_flags=DEBUG_DROP_COMPLETION)
+    plain, s = Solver(w), Solver(w, wait_cycles_log2=23, debug_flags=DEBUG_DROP_COMPLETION)
     fitness = torch.tensor(W.synthetic_fitness(w.seed, 0, w.pop_size), device="cuda")
     for x in (plain, s):
         x.ask()
