@@ -192,10 +192,11 @@ def _policy_rows(logits, actions, old, ref, advantage, weights):
     d = ref - logp
     loss = weights * (-surrogate + KL * (torch.exp(d) - d - 1.0))
     slope = weights * (torch.where(inside, -ratio * advantage, torch.zeros_like(ratio)) + KL * (1.0 - torch.exp(d)))
+    zero = torch.zeros_like(logp)
+    slope = torch.where(live, slope, zero)          # (a padded row's first action may be a forbidden one: 0 times infinity)
     gradient = e.div_(total).mul_(-slope[:, None])
     gradient.scatter_add_(1, a, slope[:, None])
-    zero = torch.zeros_like(logp)
-    return torch.where(live, loss, zero), torch.where(live, logp, zero), gradient.mul_(live[:, None])
+    return torch.where(live, loss, zero), torch.where(live, logp, zero), gradient
 
 
 def run(state):
