@@ -424,6 +424,111 @@ typedef struct evo_actions {
 evo_status evo_mlp_actions_bytes(const evo_actions* p, size_t* bytes);
 evo_status evo_mlp_actions(const evo_actions* p, void* d_workspace, size_t workspace_bytes, void* cuda_stream);
 
+/*
+ * ---- training a mixture of members (or experts) ---------------------------------------------------
+ * What brings rows into the order of the grouped products and back, and the gradients: like the calls above, without a
+ * solver and keeping nothing.  A step is route -> take -> evo_grouped_linear -> combine -> loss, and back the loss's gradient ->
+ * combine_backward -> evo_grouped_linear_backward -> combine (the gradient of take without weights).
+ *
+ * Pairs of a row and one of its `choices` sorted by the member that they choose, stable: pair p = row * choices + choice.
+ *   offsets[g] = pairs whose member is below g      place[p] = offsets[member of p] + earlier pairs of that member
+ *   source[place[p]] = p
+ * A member outside [0, groups) is none: its pair has place -1, and source is -1 from offsets[groups] on.
+ * Errors: INVALID_ARG, WORKSPACE, CUDA.
+ */
+typedef struct evo_routes {
+    uint32_t struct_size;          /* sizeof(evo_routes), checked  */
+    uint32_t groups;               /* 1 .. 2^20                    */
+    uint32_t choices;              /* of a row, >= 1               */
+    uint32_t members_64;           /* 64-bit members               */
+    uint64_t rows;                 /* rows * choices < 2^31        */
+    const void* d_members; size_t ld_members;        /* [rows][choices], int32 (or int64) */
+    int32_t* d_offsets;            /* [groups + 1]                 */
+    int32_t* d_source;             /* [rows * choices], or NULL    */
+    int32_t* d_place;              /* [rows][choices], no pitch    */
+} evo_routes;
+evo_status evo_route_rows_bytes(const evo_routes* p, size_t* bytes);
+evo_status evo_route_rows(const evo_routes* p, void* d_workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * Rows in sorted order and back.  place[rows][choices] as above; a place outside [0, sorted_rows) is none.
+ *   take:              sorted[place[r][j]] = weights[r][j] rows[r]        (weights NULL: 1)
+ *   combine:           rows[r] = sum over j of weights[r][j] sorted[place[r][j]]       (no place at all: zeros)
+ *   combine_backward, rows being the gradient of what combine returned:
+ *                      sorted_gradient[place[r][j]] = weights[r][j] rows[r]
+ *                      weights_gradient[r][j] = rows[r] . sorted[place[r][j]]      (no place: 0)
+ * Sorted rows that no place names are left as they are.  Two pairs with the same place leave one of the two rows there (route_rows
+ * makes none).  Sums in fp32 in the choices' order, weights fp32, all other numbers of one type, any pitch and alignment.  A weight of 0 takes
+ * infinities and NaN of its row along as NaN; a place that is none takes nothing.  Outputs may not overlap anything, from the first to the last element of
+ * each array.
+ * Errors: INVALID_ARG, UNSUPPORTED (more than 2^31 blocks), CUDA.
+ */
+typedef struct evo_row_sets {
+    uint32_t struct_size;          /* sizeof(evo_row_sets), checked          */
+    uint32_t type, choices, cols;  /* choices and cols 1 .. 2^20             */
+    uint64_t rows, sorted_rows;    /* sorted_rows < 2^31                     */
+    const int32_t* d_place;   size_t ld_place;
+    const float*   d_weights; size_t ld_weights;
+    void*          d_rows;    size_t ld_rows;
+    void*          d_sorted;  size_t ld_sorted;
+    void*          d_sorted_gradient;  size_t ld_sorted_gradient;      /* combine_backward alone */
+    float*         d_weights_gradient; size_t ld_weights_gradient;
+} evo_row_sets;
+evo_status evo_take_rows(const evo_row_sets* p, void* cuda_stream);
+evo_status evo_combine_rows(const evo_row_sets* p, void* cuda_stream);
+evo_status evo_combine_rows_backward(const evo_row_sets* p, void* cuda_stream);
+
+/*
+ * The gradients of evo_grouped_linear (its arguments in `forward`, d_y its result, d_bias unused): with dy the gradient of y,
+ *   dz = dy scale act'(z), from y: tanh dy (scale - y^2 / scale), relu dy scale where y / scale > 0 (else 0), none dy scale
+ *   dx[r] = W_g' dz[r]      dweight_g = sum over the group's rows of dz[r] x[r]'      dbias_g = sum of dz[r]
+ * dx, dweight and dbias NULL: not wanted.  x is read for dweight alone, the weights for dx alone, y for activations alone (d_y may be NULL without one).
+ * Rows of dx that belong to no group are left as they are; an empty group's gradients are zeros.  sum_weight / sum_bias: one gradient for all groups
+ * together (weights or biases that the groups share: stride 0).  Types, offsets, sums and infinities as above; of 16-bit types dz counts with 16 bits and more.  With
+ * an activation scale may not be 0.  Outputs may not overlap anything, from the first to the last element of each array (a layer's
+ * gradients inside rows as wide as theta's do not overlap: dweight and dbias may lie between each other's groups).
+ * Errors: INVALID_ARG, WORKSPACE, UNSUPPORTED (more than 2^31 blocks), CUDA.  The workspace with any of the inputs NULL is enough for any addresses.
+ */
+typedef struct evo_grouped_gradient {
+    uint32_t struct_size;          /* sizeof(evo_grouped_gradient), checked */
+    uint32_t sum_weight, sum_bias;
+    const void* d_dy;      size_t ld_dy;
+    void*       d_dx;      size_t ld_dx;
+    void*       d_dweight; size_t ld_dweight, dweight_stride;
+    void*       d_dbias;   size_t dbias_stride;
+} evo_grouped_gradient;
+evo_status evo_grouped_linear_backward_bytes(const evo_grouped* forward, const evo_grouped_gradient* p, size_t* bytes);
+evo_status evo_grouped_linear_backward(const evo_grouped* forward, const evo_grouped_gradient* p, void* d_workspace, size_t workspace_bytes,
+                                       void* cuda_stream);
+
+/*
+ * Clipped policy loss of rows of logits with a penalty for leaving a reference policy, and its gradient:
+ *   logp = logits[action] - log sum exp(logits)      ratio = exp(logp - old_logp)
+ *   L = -min(ratio A, clamp(ratio, 1 - clip_low, 1 + clip_high) A) + kl (exp(ref - logp) - (ref - logp) - 1)
+ *   loss = sum of w L       gradient[v] = w c ([v = action] - p_v),  c = -ratio A (0 where the clamped product is the smaller) + kl (1 - exp(ref - logp))
+ * (w = weights[r], or 1 / rows where weights is NULL; ref NULL: kl has to be 0).  The ratio may lie on a border: A >= 0 and
+ * ratio <= 1 + clip_high, or A < 0 and ratio >= 1 - clip_low, is not clipped.  A row whose action is outside [0, actions) or whose weight is 0 is padding: nothing else of it
+ * is looked at, its logp is 0 and its gradient zeros.  Logits of minus infinity are forbidden actions (probability and gradient 0); a
+ * row with a NaN, an infinity above zero, or nothing but forbidden actions has NaN for logp and gradient, and the loss is NaN.
+ * logits and gradient [rows][actions] of one type, any pitch and alignment; gradient may be logits itself (same pointer and pitch).  loss (one number), logp and gradient NULL: not wanted.  Sums of a
+ * row in fp32, what follows from it and the sum over rows in fp64, in a fixed order.
+ * Errors: INVALID_ARG, WORKSPACE, UNSUPPORTED (more than 2^31 rows), CUDA.
+ */
+typedef struct evo_policy_rows {
+    uint32_t struct_size;          /* sizeof(evo_policy_rows), checked */
+    uint32_t type, actions;        /* actions 1 .. 2^20                */
+    uint32_t actions_64;           /* 64-bit action numbers            */
+    uint64_t rows;
+    double clip_low, clip_high, kl;      /* 0 <= clip_low <= 1, clip_high >= 0, kl >= 0 */
+    const void*  d_logits; size_t ld_logits;
+    const void*  d_action;                           /* [rows] int32 (or int64) */
+    const float* d_old_logp; const float* d_advantage; const float* d_ref_logp; const float* d_weights;      /* [rows] */
+    float* d_loss; float* d_logp;                    /* [1], [rows] */
+    void*  d_gradient;     size_t ld_gradient;
+} evo_policy_rows;
+evo_status evo_policy_loss_bytes(const evo_policy_rows* p, size_t* bytes);
+evo_status evo_policy_loss(const evo_policy_rows* p, void* d_workspace, size_t workspace_bytes, void* cuda_stream);
+
 const char* evo_status_string(evo_status st);
 uint32_t    evo_version(void);            /* major*10000 + minor*100 + patch: 1.1.0 = 10100 */
 

@@ -113,8 +113,18 @@ def load_library(debug: bool = False):
     L.evo_grouped_linear.argtypes = [vp, vp, C.c_size_t, vp]
     L.evo_mlp_actions_bytes.argtypes = [vp, szp]
     L.evo_mlp_actions.argtypes = [vp, vp, C.c_size_t, vp]
+    L.evo_route_rows_bytes.argtypes = [vp, szp]
+    L.evo_route_rows.argtypes = [vp, vp, C.c_size_t, vp]
+    for name in ("evo_take_rows", "evo_combine_rows", "evo_combine_rows_backward"):
+        getattr(L, name).argtypes = [vp, vp]
+    L.evo_grouped_linear_backward_bytes.argtypes = [vp, vp, szp]
+    L.evo_grouped_linear_backward.argtypes = [vp, vp, vp, C.c_size_t, vp]
+    L.evo_policy_loss_bytes.argtypes = [vp, szp]
+    L.evo_policy_loss.argtypes = [vp, vp, C.c_size_t, vp]
     for name in ("evo_orthogonalize_bytes", "evo_orthogonalize", "evo_muon_bytes", "evo_muon_step", "evo_grouped_linear_bytes", "evo_grouped_linear",
-                 "evo_mlp_actions_bytes", "evo_mlp_actions"):
+                 "evo_mlp_actions_bytes", "evo_mlp_actions", "evo_route_rows_bytes", "evo_route_rows", "evo_take_rows", "evo_combine_rows",
+                 "evo_combine_rows_backward", "evo_grouped_linear_backward_bytes", "evo_grouped_linear_backward", "evo_policy_loss_bytes",
+                 "evo_policy_loss"):
         getattr(L, name).restype = C.c_int
     if debug:
         _lib_debug = L
@@ -156,6 +166,33 @@ class Actions(C.Structure):
                 ("layer_sizes", C.c_uint32 * (EVO_MAX_LAYERS + 1)), ("action_scale", C.c_float), ("offsets_64", C.c_uint32),
                 ("rows", C.c_uint64), ("d_theta", C.c_void_p), ("ld_theta", C.c_size_t), ("d_observations", C.c_void_p),
                 ("ld_observations", C.c_size_t), ("d_offsets", C.c_void_p), ("d_actions", C.c_void_p), ("ld_actions", C.c_size_t)]
+
+
+class RoutePairs(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("groups", C.c_uint32), ("choices", C.c_uint32), ("members_64", C.c_uint32), ("rows", C.c_uint64),
+                ("d_members", C.c_void_p), ("ld_members", C.c_size_t), ("d_offsets", C.c_void_p), ("d_source", C.c_void_p),
+                ("d_place", C.c_void_p)]
+
+
+class RowSets(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("type", C.c_uint32), ("choices", C.c_uint32), ("cols", C.c_uint32), ("rows", C.c_uint64),
+                ("sorted_rows", C.c_uint64), ("d_place", C.c_void_p), ("ld_place", C.c_size_t), ("d_weights", C.c_void_p),
+                ("ld_weights", C.c_size_t), ("d_rows", C.c_void_p), ("ld_rows", C.c_size_t), ("d_sorted", C.c_void_p),
+                ("ld_sorted", C.c_size_t), ("d_sorted_gradient", C.c_void_p), ("ld_sorted_gradient", C.c_size_t),
+                ("d_weights_gradient", C.c_void_p), ("ld_weights_gradient", C.c_size_t)]
+
+
+class GroupedGradient(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("sum_weight", C.c_uint32), ("sum_bias", C.c_uint32), ("d_dy", C.c_void_p), ("ld_dy", C.c_size_t),
+                ("d_dx", C.c_void_p), ("ld_dx", C.c_size_t), ("d_dweight", C.c_void_p), ("ld_dweight", C.c_size_t),
+                ("dweight_stride", C.c_size_t), ("d_dbias", C.c_void_p), ("dbias_stride", C.c_size_t)]
+
+
+class PolicyRows(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("type", C.c_uint32), ("actions", C.c_uint32), ("actions_64", C.c_uint32), ("rows", C.c_uint64),
+                ("clip_low", C.c_double), ("clip_high", C.c_double), ("kl", C.c_double), ("d_logits", C.c_void_p), ("ld_logits", C.c_size_t),
+                ("d_action", C.c_void_p), ("d_old_logp", C.c_void_p), ("d_advantage", C.c_void_p), ("d_ref_logp", C.c_void_p),
+                ("d_weights", C.c_void_p), ("d_loss", C.c_void_p), ("d_logp", C.c_void_p), ("d_gradient", C.c_void_p), ("ld_gradient", C.c_size_t)]
 
 
 def make_config(w: W.Workload, *, trace_steps: int = 0, rollout_kernel: int = ROLLOUT_AUTO,

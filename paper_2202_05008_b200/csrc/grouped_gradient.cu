@@ -1,0 +1,329 @@
+// Gradients of the products grouped by member: dx[r] = W_g' dz[r], dW_g = sum_r dz[r] x[r]', db_g = sum_r dz[r]; any type, size, stride and alignment.
+//
+// A group of a population has few rows and weights of its own: dx is bound by the weights' way from memory, dW by its own way there.  k_rows reads
+// a group's weights once for up to 8 rows, which are multiplied in fp32 on the CUDA cores; k_weights makes tiles of 64 x 64 outputs.  Where there are too few tiles for the
+// GPU and many rows, the rows are split and the parts added up in a fixed order.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include <cstring>
+#include <type_traits>
+
+#include "grouped_gradient.h"
+
+namespace evo {
+namespace {
+
+template <typename T> __device__ __forceinline__ float to_float(T x)
+{
+    if constexpr (std::is_same<T, float>::value) return x;
+    else if constexpr (std::is_same<T, __half>::value) return __half2float(x);
+    else return __bfloat162float(x);
+}
+template <typename T> __device__ __forceinline__ T from_float(float x)
+{
+    if constexpr (std::is_same<T, float>::value) return x;
+    else if constexpr (std::is_same<T, __half>::value) return __float2half_rn(x);
+    else return __float2bfloat16_rn(x);
+}
+template <typename T>
+__device__ __forceinline__ float dz_at(const GradientArgs& a, uint64_t row, uint32_t o)
+{
+    const float dy = to_float(static_cast<const T*>(a.dy)[row * a.ld_dy + o]);
+    return dz_of(a, dy, a.f.activation == EVO_ACT_NONE ? 0.f : to_float(static_cast<const T*>(a.f.y)[row * a.f.ld_y + o]));
+}
+
+// ---- dx ----
+// 4 columns a thread, `wide` threads side by side and the others on other weight rows: their sums are added up at the end.
+constexpr uint32_t kRows = 8, kChunk = 256, kThreads = 256;
+
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(kThreads) k_rows(const __grid_constant__ GradientArgs a, uint32_t wide)
+{
+    __shared__ __align__(16) float dz[kChunk][kRows];
+    __shared__ __align__(16) float sums[kThreads][4 * kRows];
+    dep_wait();
+    dep_trigger();
+    const GroupedArgs& f = a.f;
+    const uint32_t n_in = f.n_in, n_out = f.n_out, tiles = (n_in + 4u * wide - 1u) / (4u * wide);
+    const uint32_t group = blockIdx.x / tiles, c0 = blockIdx.x % tiles * 4u * wide, tx = threadIdx.x % wide, ty = threadIdx.x / wide, slices = kThreads / wide;
+    uint64_t first, end;
+    group_rows(f, group, &first, &end);
+    const T* const w = static_cast<const T*>(f.w) + group * f.stride_w;
+    for (uint64_t r = first; r < end; r += kRows) {
+        const uint32_t rows = static_cast<uint32_t>(min(static_cast<uint64_t>(kRows), end - r));
+        float sum[4][kRows];
+#pragma unroll
+        for (uint32_t i = 0; i < 4u; ++i)
+#pragma unroll
+            for (uint32_t k = 0; k < kRows; ++k) sum[i][k] = 0.f;
+        for (uint32_t o0 = 0; o0 < n_out; o0 += kChunk) {
+            const uint32_t count = min(kChunk, n_out - o0);
+            __syncthreads();
+            for (uint32_t i = threadIdx.x; i < kChunk * kRows; i += kThreads) {
+                const uint32_t o = i % kChunk, row = i / kChunk;
+                dz[o][row] = o < count && row < rows ? dz_at<T>(a, r + row, o0 + o) : 0.f;
+            }
+            __syncthreads();
+#pragma unroll 4
+            for (uint32_t o = ty; o < count; o += slices) {
+                const T* const from = w + static_cast<uint64_t>(o0 + o) * f.ld_w;
+                float v[4];
+                if constexpr (VEC) {
+                    T raw[4];
+                    const uint32_t c = c0 + 4u * tx;
+                    if constexpr (sizeof(T) == 4) {
+                        const uint4 u = c < n_in ? *reinterpret_cast<const uint4*>(from + c) : make_uint4(0u, 0u, 0u, 0u);
+                        memcpy(raw, &u, 16);
+                    } else {
+                        const uint2 u = c < n_in ? *reinterpret_cast<const uint2*>(from + c) : make_uint2(0u, 0u);
+                        memcpy(raw, &u, 8);
+                    }
+#pragma unroll
+                    for (uint32_t i = 0; i < 4u; ++i) v[i] = to_float(raw[i]);
+                } else {
+#pragma unroll
+                    for (uint32_t i = 0; i < 4u; ++i) v[i] = c0 + tx + wide * i < n_in ? to_float(from[c0 + tx + wide * i]) : 0.f;
+                }
+                const float4 d0 = *reinterpret_cast<const float4*>(&dz[o][0]), d1 = *reinterpret_cast<const float4*>(&dz[o][4]);
+                const float d[kRows] = { d0.x, d0.y, d0.z, d0.w, d1.x, d1.y, d1.z, d1.w };
+#pragma unroll
+                for (uint32_t i = 0; i < 4u; ++i)
+#pragma unroll
+                    for (uint32_t k = 0; k < kRows; ++k) sum[i][k] = fmaf(v[i], d[k], sum[i][k]);
+            }
+        }
+        // sums[ty][row][column]
+        __syncthreads();
+        float* const flat = &sums[0][0];
+#pragma unroll
+        for (uint32_t k = 0; k < kRows; ++k)
+#pragma unroll
+            for (uint32_t i = 0; i < 4u; ++i) flat[(ty * kRows + k) * 4u * wide + (VEC ? 4u * tx + i : tx + wide * i)] = sum[i][k];
+        __syncthreads();
+        for (uint32_t i = threadIdx.x; i < rows * 4u * wide; i += kThreads) {
+            const uint32_t c = i % (4u * wide), row = i / (4u * wide);
+            float s = 0.f;
+            for (uint32_t y = 0; y < slices; ++y) s += flat[(y * kRows + row) * 4u * wide + c];
+            if (c0 + c < n_in) static_cast<T*>(a.dx)[(r + row) * a.ld_dx + c0 + c] = from_float<T>(s);
+        }
+    }
+}
+
+// ---- dW and db ----
+// Rows of a set (a group, or all of them together), of which split `s` of `splits` has its part, a multiple of 16 rows.
+__device__ __forceinline__ void set_rows(const GradientArgs& a, bool all, uint32_t set, uint32_t split, uint32_t splits, uint64_t* first, uint64_t* end)
+{
+    group_rows(a.f, set, first, end);
+    if (all) {
+        uint64_t p;
+        group_rows(a.f, a.f.groups - 1u, &p, end);
+        if (*end < *first) *end = *first;
+    }
+    const uint64_t per = ((*end - *first + splits - 1u) / splits + 15u) / 16u * 16u;
+    const uint64_t f = *first + split * per;
+    *end = min(*end, f + per);
+    *first = f;                                              // (behind the end: no rows)
+}
+
+struct WeightsArgs {
+    GradientArgs a;
+    uint32_t all, sets, splits, out_tiles, in_tiles;         // in_tiles 0: db alone, as one column of tiles
+    float* part_w; float* part_b;                            // [splits][sets][n_out][n_in], [splits][sets][n_out]
+};
+constexpr uint32_t kTile = 64, kStep = 16;
+
+template <typename T>
+__global__ void __launch_bounds__(256) k_weights(const __grid_constant__ WeightsArgs p)
+{
+    __shared__ __align__(16) float dz[kStep][kTile], xs[kStep][kTile];
+    dep_wait();
+    dep_trigger();
+    const GradientArgs& a = p.a;
+    const uint32_t n_in = a.f.n_in, n_out = a.f.n_out, across = p.in_tiles ? p.in_tiles : 1u;
+    uint64_t at = blockIdx.x;
+    const uint32_t i0 = static_cast<uint32_t>(at % across) * kTile; at /= across;
+    const uint32_t o0 = static_cast<uint32_t>(at % p.out_tiles) * kTile; at /= p.out_tiles;
+    const uint32_t split = static_cast<uint32_t>(at % p.splits), set = static_cast<uint32_t>(at / p.splits);
+    uint64_t r, end;
+    set_rows(a, p.all, set, split, p.splits, &r, &end);
+    const uint32_t tx = threadIdx.x % 16u, ty = threadIdx.x / 16u, col = threadIdx.x % kTile, row0 = threadIdx.x / kTile;
+    const bool bias = a.db && i0 == 0u && threadIdx.x < kTile;
+    float sum[4][4] = {}, sum_b = 0.f;
+    for (; r < end; r += kStep) {
+        __syncthreads();
+#pragma unroll
+        for (uint32_t k = 0; k < kStep; k += 4u) {
+            const uint32_t row = row0 + k;
+            const bool live = r + row < end;
+            dz[row][col] = live && o0 + col < n_out ? dz_at<T>(a, r + row, o0 + col) : 0.f;
+            if (p.in_tiles) xs[row][col] = live && i0 + col < n_in ? to_float(static_cast<const T*>(a.f.x)[(r + row) * a.f.ld_x + i0 + col]) : 0.f;
+        }
+        __syncthreads();
+        if (bias) {
+            float s = 0.f;
+#pragma unroll
+            for (uint32_t k = 0; k < kStep; ++k) s += dz[k][threadIdx.x];
+            sum_b += s;
+        }
+        if (p.in_tiles) {
+            float s[4][4] = {};
+#pragma unroll
+            for (uint32_t k = 0; k < kStep; ++k) {
+                const float4 d = *reinterpret_cast<const float4*>(&dz[k][4u * ty]), x = *reinterpret_cast<const float4*>(&xs[k][4u * tx]);
+                const float dd[4] = { d.x, d.y, d.z, d.w }, xx[4] = { x.x, x.y, x.z, x.w };
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) s[i][j] = fmaf(dd[i], xx[j], s[i][j]);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) sum[i][j] += s[i][j];
+        }
+    }
+    const uint64_t part = static_cast<uint64_t>(split) * p.sets + set;
+    if (bias && o0 + threadIdx.x < n_out) {
+        const uint32_t o = o0 + threadIdx.x;
+        if (p.splits > 1u) p.part_b[part * n_out + o] = sum_b;
+        else static_cast<T*>(a.db)[set * a.stride_db + o] = from_float<T>(sum_b);
+    }
+    if (!p.in_tiles) return;
+#pragma unroll
+    for (uint32_t i = 0; i < 4u; ++i) {
+        const uint32_t o = o0 + 4u * ty + i;
+        if (o >= n_out) break;
+#pragma unroll
+        for (uint32_t j = 0; j < 4u; ++j) {
+            const uint32_t c = i0 + 4u * tx + j;
+            if (c >= n_in) break;
+            if (p.splits > 1u) p.part_w[(part * n_out + o) * n_in + c] = sum[i][j];
+            else static_cast<T*>(a.dw)[set * a.stride_dw + o * a.ld_dw + c] = from_float<T>(sum[i][j]);
+        }
+    }
+}
+
+// The splits' parts, added up in their order: rows of `n` numbers, `rows` of them a set.
+template <typename T>
+__global__ void __launch_bounds__(256) k_add_parts(const float* __restrict__ part, uint32_t splits, uint32_t sets, uint32_t rows, uint32_t n, T* __restrict__ to, uint64_t stride,
+                                                   uint64_t ld)
+{
+    dep_wait();
+    dep_trigger();
+    const uint64_t each = static_cast<uint64_t>(sets) * rows * n;
+    for (uint64_t i = static_cast<uint64_t>(blockIdx.x) * 256u + threadIdx.x; i < each; i += static_cast<uint64_t>(gridDim.x) * 256u) {
+        float s = 0.f;
+        for (uint32_t k = 0; k < splits; ++k) s += part[k * each + i];
+        const uint64_t row = i / n;
+        to[row / rows * stride + row % rows * ld + i % n] = from_float<T>(s);
+    }
+}
+
+// ---- plans ----
+// Splits of the rows: as many as fill the GPU twice, of no fewer than 128 rows on average.
+uint32_t splits_for(const GradientArgs& a, bool all, uint64_t tiles)
+{
+    const uint64_t sets = all ? 1u : a.f.groups, blocks = sets * tiles, rows = a.f.rows / sets;
+    if (blocks >= kSms) return 1u;
+    const uint64_t most = 2u * kSms / blocks, want = rows / 128u;
+    return static_cast<uint32_t>(want < 2u ? 1u : want < most ? want : most);
+}
+struct Plan {
+    bool both;                           // dW and db in one launch
+    uint32_t w_splits, b_splits;
+    size_t w_bytes, b_bytes;
+};
+size_t padded(size_t n) { return (n + 255u) / 256u * 256u; }
+Plan plan_for(const GradientArgs& a)
+{
+    Plan p;
+    const uint64_t out_tiles = (a.f.n_out + kTile - 1u) / kTile, in_tiles = (a.f.n_in + kTile - 1u) / kTile;
+    p.both = a.dw && a.db && a.sum_w == a.sum_b;
+    p.w_splits = a.dw ? splits_for(a, a.sum_w, out_tiles * in_tiles) : 1u;
+    p.b_splits = p.both ? p.w_splits : a.db ? splits_for(a, a.sum_b, out_tiles) : 1u;
+    const uint64_t w_sets = a.sum_w ? 1u : a.f.groups, b_sets = a.sum_b ? 1u : a.f.groups;
+    p.w_bytes = p.w_splits > 1u ? padded(4u * p.w_splits * w_sets * a.f.n_out * a.f.n_in) : 0u;
+    p.b_bytes = p.b_splits > 1u ? padded(4u * p.b_splits * b_sets * a.f.n_out) : 0u;
+    return p;
+}
+
+template <typename T>
+int launch_rows(cudaStream_t st, const GradientArgs& a)
+{
+    const GroupedArgs& f = a.f;
+    uint32_t wide = 8u;                                      // columns of a block: as the row needs, fewer where there are few groups
+    while (wide < 64u && wide * 4u < f.n_in) wide *= 2u;
+    const uint64_t used = f.rows < f.groups ? f.rows : f.groups;
+    while (wide > 8u && used * ((f.n_in + 4u * wide - 1u) / (4u * wide)) < 2u * kSms) wide /= 2u;
+    const uint64_t blocks = static_cast<uint64_t>(f.groups) * ((f.n_in + 4u * wide - 1u) / (4u * wide));
+    if (blocks > 0x7FFFFFFFull) return -2;
+    const bool aligned = (reinterpret_cast<uintptr_t>(f.w) & (4u * sizeof(T) - 1u)) == 0u && ((f.n_in | f.ld_w | f.stride_w) & 3u) == 0u;
+    auto kernel = aligned ? k_rows<T, true> : k_rows<T, false>;
+    return launch_dependent(kernel, dim3(static_cast<uint32_t>(blocks)), dim3(kThreads), 0, st, a, wide) == cudaSuccess ? 1 : -1;
+}
+
+template <typename T>
+int launch_weights(cudaStream_t st, const GradientArgs& in, bool weights, bool bias, uint32_t splits, float* part_w, float* part_b)
+{
+    WeightsArgs p;
+    p.a = in;
+    if (!bias) p.a.db = nullptr;
+    p.all = weights ? in.sum_w : in.sum_b;
+    p.sets = p.all ? 1u : in.f.groups;
+    p.splits = splits;
+    p.out_tiles = (in.f.n_out + kTile - 1u) / kTile;
+    p.in_tiles = weights ? (in.f.n_in + kTile - 1u) / kTile : 0u;
+    p.part_w = part_w; p.part_b = part_b;
+    const uint64_t blocks = static_cast<uint64_t>(p.sets) * splits * p.out_tiles * (p.in_tiles ? p.in_tiles : 1u);
+    if (blocks > 0x7FFFFFFFull) return -2;
+    if (launch_dependent(k_weights<T>, dim3(static_cast<uint32_t>(blocks)), dim3(256), 0, st, p) != cudaSuccess) return -1;
+    if (splits == 1u) return 1;
+    auto add = [&](const float* part, uint32_t rows, uint32_t n, void* to, uint64_t stride, uint64_t ld) {
+        const uint64_t count = (static_cast<uint64_t>(p.sets) * rows * n + 255u) / 256u;
+        return launch_dependent(k_add_parts<T>, dim3(static_cast<uint32_t>(count < 8u * kSms ? count : 8u * kSms)), dim3(256), 0, st, part, splits, p.sets, rows, n,
+                                static_cast<T*>(to), stride, ld) == cudaSuccess;
+    };
+    if (weights && !add(part_w, in.f.n_out, in.f.n_in, in.dw, in.stride_dw, in.ld_dw)) return -1;
+    if (bias && !add(part_b, 1u, in.f.n_out, in.db, in.stride_db, 0u)) return -1;
+    return 2;
+}
+
+template <typename T>
+int launch_type(cudaStream_t st, const GradientArgs& a, void* work)
+{
+    const Plan plan = plan_for(a);
+    float* const part_w = static_cast<float*>(work);
+    float* const part_b = reinterpret_cast<float*>(static_cast<uint8_t*>(work) + plan.w_bytes);
+    int n = 0;
+    if (a.dx && a.f.rows) {
+        n = launch_rows<T>(st, a);
+        if (n < 0) return n;
+    }
+    if (a.dw) {
+        const int k = launch_weights<T>(st, a, true, plan.both, plan.w_splits, part_w, part_b);
+        if (k < 0) return k;
+        n += k;
+    }
+    if (a.db && !plan.both) {
+        const int k = launch_weights<T>(st, a, false, true, plan.b_splits, nullptr, part_b);
+        if (k < 0) return k;
+        n += k;
+    }
+    return n;
+}
+
+}  // namespace
+
+size_t grouped_gradient_bytes(uint32_t, const GradientArgs& a)
+{
+    const Plan p = plan_for(a);
+    return p.w_bytes + p.b_bytes;
+}
+
+int launch_grouped_gradient(cudaStream_t st, uint32_t type, const GradientArgs& a, void* work)
+{
+    return type == EVO_F32 ? launch_type<float>(st, a, work) : type == EVO_BF16 ? launch_type<__nv_bfloat16>(st, a, work) : launch_type<__half>(st, a, work);
+}
+
+}  // namespace evo

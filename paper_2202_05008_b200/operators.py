@@ -3,19 +3,31 @@
 All of them enqueue their work on ``stream`` (the current stream of the tensors' device if it is None), allocate their
 outputs and workspaces through torch on that stream, and return without waiting.  Where that is not the stream on which an argument
 was made, ordering the two and keeping the argument until the work is done are the caller's.  Arguments that the library cannot
-take raise ``EvoError``; there is no fallback.  None of them has a backward pass: while torch records gradients, tensors that require one are
-refused (detach them, or call under ``torch.no_grad()``).
+take raise ``EvoError``; there is no fallback.  None of them has a backward pass that torch records: while torch records gradients, tensors that require one are
+refused (detach them, or call under ``torch.no_grad()``).  Gradients are calls of their own: a training step of a mixture of members (or experts) is
+
+    routes = route_rows(members, groups)                    # members [rows, choices], gates [rows, choices]
+    xs = take_rows(x, routes.place)
+    ys = grouped_linear(xs, weight, routes.offsets, bias, activation="tanh")
+    logits = combine_rows(ys, routes.place, gates)
+    loss, logp, d_logits = policy_loss(logits, actions, old_logp, advantage)
+    d_ys, d_gates = combine_rows_backward(d_logits, ys, routes.place, gates)
+    d_xs, d_weight, d_bias = grouped_linear_backward(d_ys, xs, weight, routes.offsets, ys, activation="tanh")
+    d_x = combine_rows(d_xs, routes.place)
+
+and ``muon_step`` (which ascends: give it the gradient's negative) takes what it gives.
 """
 from __future__ import annotations
 
 import ctypes as C
 import math
 from functools import lru_cache
-from typing import Optional, Sequence, Tuple
+from typing import NamedTuple, Optional, Sequence, Tuple
 
 import torch
 
-from .binding import EVO_MAX_LAYERS, Actions, EvoError, Grouped, Matrices, Matrix, Muon, NewtonSchulz, _check, load_library
+from .binding import (EVO_MAX_LAYERS, Actions, EvoError, Grouped, GroupedGradient, Matrices, Matrix, Muon, NewtonSchulz, PolicyRows, RoutePairs, RowSets, _check,
+                      load_library)
 
 TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 INVALID_ARG = 1
@@ -247,3 +259,198 @@ def mlp_actions(theta: torch.Tensor, layer_sizes: Sequence[int], observations: t
         code = lib.evo_mlp_actions(C.byref(p), None if work is None else work.data_ptr(), need.value, st)
     _check(code, where)
     return y
+
+
+class Routes(NamedTuple):
+    """Pairs of a row and a choice sorted by member: ``offsets`` [groups + 1], ``source`` [pairs] (the pair at each place, -1 behind the last), ``place``
+    (of ``members``' shape, -1 without a member); int32."""
+    offsets: torch.Tensor
+    source: torch.Tensor
+    place: torch.Tensor
+
+
+def _pairs(x: torch.Tensor, dtype: torch.dtype, device: torch.device, shape=None) -> bool:
+    return x.device == device and x.dtype == dtype and x.dim() in (1, 2) and (x.dim() == 1 or x.stride(1) == 1 or x.shape[1] <= 1) and \
+        (shape is None or x.shape == shape)
+
+
+def route_rows(members: torch.Tensor, groups: int, *, stream: Optional[torch.cuda.Stream] = None) -> Routes:
+    """``evo_route_rows``: the stable order by member of the pairs of ``members`` ([rows] or [rows, choices], int32 or int64).  Numbers outside
+    [0, groups) are no member: padded rows, choices that were dropped."""
+    lib, where, device = load_library(), "route_rows", members.device
+    _require(members.is_cuda and members.dtype in (torch.int32, torch.int64) and _pairs(members, members.dtype, device), where,
+             "members: int32 or int64, [rows] or [rows, choices], on a GPU")
+    choices = members.shape[1] if members.dim() == 2 else 1
+    _require(1 <= groups <= 1 << 20 and choices >= 1 and members.numel() < 1 << 31, where, "groups or members")
+    with _On(device, stream, where) as st:
+        n = members.numel()
+        routes = Routes(torch.empty(groups + 1, dtype=torch.int32, device=device), torch.empty(n, dtype=torch.int32, device=device),
+                        torch.empty(members.shape, dtype=torch.int32, device=device))
+        p = RoutePairs(C.sizeof(RoutePairs), groups, choices, 1 if members.dtype == torch.int64 else 0, members.shape[0], members.data_ptr(),
+                       members.stride(0), *(x.data_ptr() for x in routes))
+        need = C.c_size_t()
+        _check(lib.evo_route_rows_bytes(C.byref(p), C.byref(need)), where)
+        work = torch.empty(need.value, dtype=torch.uint8, device=device) if need.value else None
+        code = lib.evo_route_rows(C.byref(p), None if work is None else work.data_ptr(), need.value, st)
+    _check(code, where)
+    return routes
+
+
+def _row_sets(where: str, rows: torch.Tensor, sorted_rows: torch.Tensor, place: torch.Tensor, weights: Optional[torch.Tensor]) -> RowSets:
+    p = RowSets(C.sizeof(RowSets), TYPES[rows.dtype], place.shape[1] if place.dim() == 2 else 1, rows.shape[1], rows.shape[0], sorted_rows.shape[0],
+                place.data_ptr(), place.stride(0), None, 0, rows.data_ptr(), rows.stride(0), sorted_rows.data_ptr(), sorted_rows.stride(0))
+    if weights is not None:
+        p.d_weights, p.ld_weights = weights.data_ptr(), weights.stride(0)
+    return p
+
+
+def _check_rows(where: str, x: torch.Tensor, place: torch.Tensor, weights: Optional[torch.Tensor], rows: Optional[int]) -> None:
+    _require(x.is_cuda and x.dtype in TYPES and _rows(x, x.dtype, x.device) and x.shape[1] >= 1, where, "fp32, bf16 or fp16 rows on a GPU")
+    _require(_pairs(place, torch.int32, x.device) and (place.dim() == 1 or place.shape[1] >= 1) and (rows is None or place.shape[0] == rows), where,
+             "place: int32, [rows] or [rows, choices], as route_rows gives it")
+    _require(weights is None or _pairs(weights, torch.float32, x.device, place.shape), where, "weights: fp32, of place's shape")
+
+
+def take_rows(x: torch.Tensor, place: torch.Tensor, weights: Optional[torch.Tensor] = None, *, out: Optional[torch.Tensor] = None,
+              stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """``evo_take_rows``: ``out[place[r, j]] = weights[r, j] * x[r]`` (weights None: 1), the rows in sorted order.  Rows that no place names are left as
+    they are in ``out``, and undefined without one (which has a row for every pair).  The gradient of x is ``combine_rows(d_out, place, weights)``."""
+    lib, where, device = load_library(), "take_rows", x.device
+    _require_no_gradient(where, x, weights, out)
+    _check_rows(where, x, place, weights, x.shape[0])
+    with _On(device, stream, where) as st:
+        y = _out(out, x, place.numel() if out is None else out.shape[0], x.shape[1], where)
+        code = lib.evo_take_rows(C.byref(_row_sets(where, x, y, place, weights)), st)
+    _check(code, where)
+    return y
+
+
+def combine_rows(y: torch.Tensor, place: torch.Tensor, weights: Optional[torch.Tensor] = None, *, out: Optional[torch.Tensor] = None,
+                 stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """``evo_combine_rows``: ``out[r] = sum over j of weights[r, j] * y[place[r, j]]`` (weights None: 1), rows back from sorted order; zeros where
+    a row has no place."""
+    lib, where, device = load_library(), "combine_rows", y.device
+    _require_no_gradient(where, y, weights, out)
+    _check_rows(where, y, place, weights, None)
+    with _On(device, stream, where) as st:
+        x = _out(out, y, place.shape[0], y.shape[1], where)
+        code = lib.evo_combine_rows(C.byref(_row_sets(where, x, y, place, weights)), st)
+    _check(code, where)
+    return x
+
+
+def combine_rows_backward(d_out: torch.Tensor, y: torch.Tensor, place: torch.Tensor, weights: torch.Tensor, *, out: Optional[torch.Tensor] = None,
+                          stream: Optional[torch.cuda.Stream] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """``evo_combine_rows_backward``: the gradients (of y, of weights) of ``combine_rows(y, place, weights)`` for the gradient ``d_out`` of its result.
+    Rows of y that no place names are left as they are in ``out`` (the gradient of y), and undefined without one.  Without weights the gradient of y
+    is ``take_rows(d_out, place)``."""
+    lib, where, device = load_library(), "combine_rows_backward", y.device
+    _require_no_gradient(where, d_out, y, weights, out)
+    _check_rows(where, y, place, weights, None)
+    _require(weights is not None, where, "weights")
+    _require(_rows(d_out, y.dtype, device) and d_out.shape == (place.shape[0], y.shape[1]), where, "the gradient does not match")
+    with _On(device, stream, where) as st:
+        dy = _out(out, y, y.shape[0], y.shape[1], where)
+        dw = torch.empty(place.shape, dtype=torch.float32, device=device)
+        p = _row_sets(where, d_out, y, place, weights)
+        p.d_sorted_gradient, p.ld_sorted_gradient, p.d_weights_gradient, p.ld_weights_gradient = dy.data_ptr(), dy.stride(0), dw.data_ptr(), dw.stride(0)
+        code = lib.evo_combine_rows_backward(C.byref(p), st)
+    _check(code, where)
+    return dy, dw
+
+
+def grouped_linear_backward(dy: torch.Tensor, x: Optional[torch.Tensor], weight: torch.Tensor, offsets: torch.Tensor, y: Optional[torch.Tensor] = None, *,
+                            activation: str = "none", scale: float = 1.0, wanted: Tuple[bool, bool, bool] = (True, True, True),
+                            shared_bias: bool = False, out: Sequence[Optional[torch.Tensor]] = (None, None, None),
+                            stream: Optional[torch.cuda.Stream] = None) -> Tuple[Optional[torch.Tensor], ...]:
+    """``evo_grouped_linear_backward``: the gradients (of x, of weight, of the bias) of ``y = grouped_linear(x, weight, offsets, bias, activation=...,
+    scale=...)`` for the gradient ``dy`` of y; None where ``wanted`` says so.  y is needed with an activation, x for the gradient of weight.  Groups that share their weights (an
+    expanded weight, stride 0) or, with ``shared_bias``, their bias have one gradient, [1, ...], the sum over all groups.  ``out`` may give any of the
+    three a place, of any strides that keep rows apart: a layer's gradients inside rows like theta's.  Rows of x outside all groups are left as
+    they are in ``out``, and undefined without one."""
+    lib, where, device, dtype = load_library(), "grouped_linear_backward", dy.device, dy.dtype
+    _require(len(wanted) == 3 and len(out) == 3, where, "wanted and out are for x, weight and bias")
+    _require_no_gradient(where, dy, x, weight, y, *out)
+    _require(dy.is_cuda and dtype in TYPES and _rows(dy, dtype, device), where, "dy: fp32, bf16 or fp16 rows on a GPU")
+    _require(weight.device == device and weight.dtype == dtype and weight.dim() == 3, where, "weight does not match dy")
+    groups, n_out, n_in = weight.shape
+    rows = dy.shape[0]
+    stride, pitch, one = weight.stride()
+    _require(groups >= 1 and n_out >= 1 and n_in >= 1 and n_out == dy.shape[1] and (n_in == 1 or one == 1) and stride >= 0 and pitch >= 0, where,
+             "weight does not match dy")
+    _require(activation in ACTIVATIONS, where, "activation")
+    _require((y is not None or activation == "none") and (y is None or (_rows(y, dtype, device) and y.shape == dy.shape)), where, "y does not match")
+    _require((x is not None or not wanted[1]) and (x is None or (_rows(x, dtype, device) and x.shape == (rows, n_in))), where, "x does not match")
+    wide = _ragged(offsets, groups, device, where)
+    sets = [1 if groups > 1 and stride == 0 else groups, 1 if shared_bias else groups]
+    with _On(device, stream, where) as st:
+        dx = _out(out[0], dy, rows, n_in, where) if wanted[0] else None
+        dweight, dbias = out[1] if wanted[1] else None, out[2] if wanted[2] else None
+        if wanted[1] and dweight is None:
+            dweight = torch.empty((sets[0], n_out, n_in), dtype=dtype, device=device)
+        if wanted[2] and dbias is None:
+            dbias = torch.empty((sets[1], n_out), dtype=dtype, device=device)
+        _require(dweight is None or (dweight.device == device and dweight.dtype == dtype and dweight.shape == (sets[0], n_out, n_in) and
+                                     (n_in == 1 or dweight.stride(2) == 1)), where, "the gradient of weight does not match")
+        _require(dbias is None or (_rows(dbias, dtype, device) and dbias.shape == (sets[1], n_out)), where, "the gradient of the bias does not match")
+        f = Grouped(C.sizeof(Grouped), TYPES[dtype], groups, n_in, n_out, ACTIVATIONS[activation], scale, wide, rows)
+        f.d_weight, f.ld_weight, f.weight_stride, f.d_offsets = weight.data_ptr(), pitch if n_out > 1 else n_in, stride, offsets.data_ptr()
+        if x is not None:
+            f.d_x, f.ld_x = x.data_ptr(), x.stride(0)
+        if y is not None:
+            f.d_y, f.ld_y = y.data_ptr(), y.stride(0)
+        p = GroupedGradient(C.sizeof(GroupedGradient), 1 if sets[0] < groups else 0, 1 if sets[1] < groups else 0, dy.data_ptr(), dy.stride(0))
+        if dx is not None:
+            p.d_dx, p.ld_dx = dx.data_ptr(), dx.stride(0)
+        if dweight is not None:
+            p.d_dweight, p.ld_dweight, p.dweight_stride = dweight.data_ptr(), dweight.stride(1) if n_out > 1 else n_in, dweight.stride(0)
+        if dbias is not None:
+            p.d_dbias, p.dbias_stride = dbias.data_ptr(), dbias.stride(0)
+        need = C.c_size_t()
+        _check(lib.evo_grouped_linear_backward_bytes(C.byref(f), C.byref(p), C.byref(need)), where)
+        work = torch.empty(need.value, dtype=torch.uint8, device=device) if need.value else None
+        code = lib.evo_grouped_linear_backward(C.byref(f), C.byref(p), None if work is None else work.data_ptr(), need.value, st)
+    _check(code, where)
+    return dx, dweight, dbias
+
+
+class PolicyLoss(NamedTuple):
+    loss: torch.Tensor
+    logp: torch.Tensor
+    gradient: Optional[torch.Tensor]
+
+
+def policy_loss(logits: torch.Tensor, actions: torch.Tensor, old_logp: torch.Tensor, advantage: torch.Tensor, *, ref_logp: Optional[torch.Tensor] = None,
+                weights: Optional[torch.Tensor] = None, clip: Tuple[float, float] = (0.2, 0.2), kl: float = 0.0, gradient: bool = True,
+                out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> PolicyLoss:
+    """``evo_policy_loss``: the clipped policy loss (to be minimised) of rows of ``logits`` [rows, n] (fp32, bf16 or fp16) with ``kl`` times the estimate
+    ``exp(ref - logp) - (ref - logp) - 1`` of the divergence from a reference policy; its sum over the rows times ``weights`` (None: the mean), the log probability of every
+    row's action, and the gradient of the logits (``gradient`` False: None; ``out`` may be ``logits``).  ``clip``: how far a ratio may fall below and rise above 1.
+    actions int32 or int64; old_logp, advantage, ref_logp and weights fp32, [rows].  A row whose action is outside [0, n) or whose weight is 0
+    is padding.  Logits of minus infinity are forbidden actions."""
+    lib, where, device = load_library(), "policy_loss", logits.device
+    _require_no_gradient(where, logits, old_logp, advantage, ref_logp, weights, out)
+    _require(logits.is_cuda and logits.dtype in TYPES and _rows(logits, logits.dtype, device) and logits.shape[1] >= 1, where,
+             "logits: fp32, bf16 or fp16 rows on a GPU")
+    rows, n = logits.shape
+    _require(actions.device == device and actions.dtype in (torch.int32, torch.int64) and actions.shape == (rows,) and actions.is_contiguous(), where,
+             "actions: int32 or int64, one a row")
+    for x in (old_logp, advantage, ref_logp, weights):
+        _require(x is None or (x.device == device and x.dtype == torch.float32 and x.shape == (rows,) and x.is_contiguous()), where,
+                 "old_logp, advantage, ref_logp and weights: contiguous fp32, one a row")
+    _require(old_logp is not None and advantage is not None and (ref_logp is not None or kl == 0.0), where, "old_logp, advantage or ref_logp is missing")
+    _require(len(clip) == 2 and (out is None or gradient), where, "clip or out")
+    with _On(device, stream, where) as st:
+        d_logits = _out(out, logits, rows, n, where) if gradient else None
+        loss, logp = torch.empty((), dtype=torch.float32, device=device), torch.empty(rows, dtype=torch.float32, device=device)
+        p = PolicyRows(C.sizeof(PolicyRows), TYPES[logits.dtype], n, 1 if actions.dtype == torch.int64 else 0, rows, clip[0], clip[1], kl,
+                       logits.data_ptr(), logits.stride(0), actions.data_ptr(), old_logp.data_ptr(), advantage.data_ptr(),
+                       None if ref_logp is None else ref_logp.data_ptr(), None if weights is None else weights.data_ptr(), loss.data_ptr(), logp.data_ptr())
+        if d_logits is not None:
+            p.d_gradient, p.ld_gradient = d_logits.data_ptr(), d_logits.stride(0)
+        need = C.c_size_t()
+        _check(lib.evo_policy_loss_bytes(C.byref(p), C.byref(need)), where)
+        work = torch.empty(need.value, dtype=torch.uint8, device=device) if need.value else None
+        code = lib.evo_policy_loss(C.byref(p), None if work is None else work.data_ptr(), need.value, st)
+    _check(code, where)
+    return PolicyLoss(loss, logp, d_logits)
