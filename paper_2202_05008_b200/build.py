@@ -10,8 +10,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libevo.so")
 LIB_DEBUG = os.path.join(HERE, "libevo_debug.so")     # checked build: -DEVO_DEBUG (bounds checks, guard words)
-SOURCES = ["evo.cu", "solver_kernels.cu", "rollout_mlp.cu", "rollout_mlp_tiled.cu", "rollout_mlp2.cu", "rollout_mlp_deep.cu", "rollout_mlp_deep8.cu", "rollout_mlp_mma.cu", "rollout_cnn.cu", "rollout_cnn_tc.cu", "gradient_static.cu", "rollout_s2s.cu", "rollout_paint.cu", "newton_schulz_tiny.cu", "newton_schulz_small.cu", "newton_schulz_large.cu", "matrix_ops.cu", "grouped.cu", "grouped_tc.cu", "member_rows.cu", "grouped_ops.cu", "routing.cu", "rows.cu", "grouped_gradient.cu", "policy_loss.cu", "training_ops.cu"]
-HEADERS = ["internal.h", "noise.cuh", "tasks.cuh", "async.cuh", "umma.cuh", "fp32x2.cuh", "mma_split.cuh", "rollout_mlp_deep.cuh", "spread.h", "s2s_split.h", "mlp_choice.h", "newton_schulz.h", "newton_schulz.cuh", "matrix_ops.h", "grouped.h", "tma.h", "grouped_mma.cuh", "member_rows.h", "routing.h", "grouped_gradient.h", "policy_loss.h", os.path.join("..", "..", "include", "evo.h")]
+SOURCES = ["evo.cu", "solver_kernels.cu", "rollout_mlp.cu", "rollout_mlp_tiled.cu", "rollout_mlp2.cu", "rollout_mlp_deep.cu", "rollout_mlp_deep8.cu", "rollout_mlp_mma.cu", "rollout_cnn.cu", "rollout_cnn_tc.cu", "gradient_static.cu", "rollout_s2s.cu", "rollout_paint.cu", "newton_schulz_tiny.cu", "newton_schulz_small.cu", "newton_schulz_large.cu", "matrix_ops.cu", "grouped.cu", "grouped_tc.cu", "member_rows.cu", "grouped_ops.cu", "routing.cu", "rows.cu", "grouped_gradient.cu", "grouped_gradient_tc.cu", "policy_loss.cu", "training_ops.cu"]
+HEADERS = ["internal.h", "noise.cuh", "tasks.cuh", "async.cuh", "umma.cuh", "fp32x2.cuh", "mma_split.cuh", "rollout_mlp_deep.cuh", "spread.h", "s2s_split.h", "mlp_choice.h", "newton_schulz.h", "newton_schulz.cuh", "matrix_ops.h", "grouped.h", "tma.h", "grouped_mma.cuh", "member_rows.h", "routing.h", "grouped_gradient.h", "grouped_tc.cuh", "policy_loss.h", os.path.join("..", "..", "include", "evo.h")]
 
 
 def _nvcc() -> str:

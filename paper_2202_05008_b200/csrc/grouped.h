@@ -39,5 +39,10 @@ bool grouped_tc_addressable(uint32_t type, const GroupedArgs& a);
 bool grouped_tc_takes(uint32_t type, const GroupedArgs& a);
 size_t grouped_tc_bytes(uint32_t type, const GroupedArgs& a);
 int launch_grouped_tc(cudaStream_t st, uint32_t type, const GroupedArgs& a, void* work);
+// Pieces of it, for the gradients.  Rows laid out: their pitch (fp32: of one of three parts), and the launch for the weights or (rows) x.
+uint32_t grouped_tc_pitch(uint32_t type, uint32_t n);
+int lay_out(cudaStream_t st, uint32_t type, const GroupedArgs& a, bool rows, uint32_t pitch, uint16_t* to);
+// The product with weights [n_in][n_out], whose rows are the contracted index, of operands that TMA can address: `passes` 1; 2: x has two parts; 6: both three.
+int launch_grouped_tc_transposed(cudaStream_t st, uint32_t type, const GroupedArgs& a, uint32_t passes, uint32_t pitch_w, uint32_t pitch_x, uint64_t span_w, uint64_t span_x);
 
 }  // namespace evo

@@ -111,21 +111,6 @@ __global__ void __launch_bounds__(kThreads) k_rows(const __grid_constant__ Gradi
 }
 
 // ---- dW and db ----
-// Rows of a set (a group, or all of them together), of which split `s` of `splits` has its part, a multiple of 16 rows.
-__device__ __forceinline__ void set_rows(const GradientArgs& a, bool all, uint32_t set, uint32_t split, uint32_t splits, uint64_t* first, uint64_t* end)
-{
-    group_rows(a.f, set, first, end);
-    if (all) {
-        uint64_t p;
-        group_rows(a.f, a.f.groups - 1u, &p, end);
-        if (*end < *first) *end = *first;
-    }
-    const uint64_t per = ((*end - *first + splits - 1u) / splits + 15u) / 16u * 16u;
-    const uint64_t f = *first + split * per;
-    *end = min(*end, f + per);
-    *first = f;                                              // (behind the end: no rows)
-}
-
 struct WeightsArgs {
     GradientArgs a;
     uint32_t all, sets, splits, out_tiles, in_tiles;         // in_tiles 0: db alone, as one column of tiles
@@ -229,20 +214,32 @@ uint32_t splits_for(const GradientArgs& a, bool all, uint64_t tiles)
     const uint64_t most = 2u * kSms / blocks, want = rows / 128u;
     return static_cast<uint32_t>(want < 2u ? 1u : want < most ? want : most);
 }
+bool dx_on_tensor_cores(uint32_t type, const GradientArgs& a)
+{
+    return a.f.rows < (1ull << 31) && static_cast<uint64_t>(a.f.groups) * a.f.n_out < (1ull << 31) && a.f.rows >= 24ull * a.f.groups;
+}
+bool dw_on_tensor_cores(uint32_t type, const GradientArgs& a)
+{
+    return a.f.rows < (1ull << 31) && a.f.rows >= 24ull * (a.sum_w ? 1u : a.f.groups);
+}
 struct Plan {
-    bool both;                           // dW and db in one launch
+    TcPlan tc;
+    bool both;                           // dW and db in one launch of k_weights
     uint32_t w_splits, b_splits;
-    size_t w_bytes, b_bytes;
+    size_t tc_bytes, w_bytes, b_bytes;
 };
 size_t padded(size_t n) { return (n + 255u) / 256u * 256u; }
-Plan plan_for(const GradientArgs& a)
+Plan plan_for(uint32_t type, const GradientArgs& a, bool any_address)
 {
     Plan p;
     const uint64_t out_tiles = (a.f.n_out + kTile - 1u) / kTile, in_tiles = (a.f.n_in + kTile - 1u) / kTile;
-    p.both = a.dw && a.db && a.sum_w == a.sum_b;
-    p.w_splits = a.dw ? splits_for(a, a.sum_w, out_tiles * in_tiles) : 1u;
+    const bool dx = a.dx && a.f.rows && dx_on_tensor_cores(type, a), dw = a.dw && a.f.rows && dw_on_tensor_cores(type, a);
+    p.both = a.dw && !dw && a.db && a.sum_w == a.sum_b;
+    p.w_splits = !a.dw ? 1u : dw ? splits_for(a, a.sum_w, ((a.f.n_out + 127ull) / 128u) * ((a.f.n_in + 255ull) / 256u)) : splits_for(a, a.sum_w, out_tiles * in_tiles);
     p.b_splits = p.both ? p.w_splits : a.db ? splits_for(a, a.sum_b, out_tiles) : 1u;
+    p.tc = grouped_gradient_tc_plan(type, a, dx, dw, p.w_splits, any_address);
     const uint64_t w_sets = a.sum_w ? 1u : a.f.groups, b_sets = a.sum_b ? 1u : a.f.groups;
+    p.tc_bytes = padded(p.tc.bytes());
     p.w_bytes = p.w_splits > 1u ? padded(4u * p.w_splits * w_sets * a.f.n_out * a.f.n_in) : 0u;
     p.b_bytes = p.b_splits > 1u ? padded(4u * p.b_splits * b_sets * a.f.n_out) : 0u;
     return p;
@@ -264,6 +261,14 @@ int launch_rows(cudaStream_t st, const GradientArgs& a)
 }
 
 template <typename T>
+bool add_parts(cudaStream_t st, const float* part, uint32_t splits, uint32_t sets, uint32_t rows, uint32_t n, void* to, uint64_t stride, uint64_t ld)
+{
+    const uint64_t blocks = (static_cast<uint64_t>(sets) * rows * n + 255u) / 256u;
+    return launch_dependent(k_add_parts<T>, dim3(static_cast<uint32_t>(blocks < 8u * kSms ? blocks : 8u * kSms)), dim3(256), 0, st, part, splits, sets, rows, n, static_cast<T*>(to),
+                            stride, ld) == cudaSuccess;
+}
+
+template <typename T>
 int launch_weights(cudaStream_t st, const GradientArgs& in, bool weights, bool bias, uint32_t splits, float* part_w, float* part_b)
 {
     WeightsArgs p;
@@ -277,53 +282,60 @@ int launch_weights(cudaStream_t st, const GradientArgs& in, bool weights, bool b
     p.part_w = part_w; p.part_b = part_b;
     const uint64_t blocks = static_cast<uint64_t>(p.sets) * splits * p.out_tiles * (p.in_tiles ? p.in_tiles : 1u);
     if (blocks > 0x7FFFFFFFull) return -2;
-    if (launch_dependent(k_weights<T>, dim3(static_cast<uint32_t>(blocks)), dim3(256), 0, st, p) != cudaSuccess) return -1;
-    if (splits == 1u) return 1;
-    auto add = [&](const float* part, uint32_t rows, uint32_t n, void* to, uint64_t stride, uint64_t ld) {
-        const uint64_t count = (static_cast<uint64_t>(p.sets) * rows * n + 255u) / 256u;
-        return launch_dependent(k_add_parts<T>, dim3(static_cast<uint32_t>(count < 8u * kSms ? count : 8u * kSms)), dim3(256), 0, st, part, splits, p.sets, rows, n,
-                                static_cast<T*>(to), stride, ld) == cudaSuccess;
-    };
-    if (weights && !add(part_w, in.f.n_out, in.f.n_in, in.dw, in.stride_dw, in.ld_dw)) return -1;
-    if (bias && !add(part_b, 1u, in.f.n_out, in.db, in.stride_db, 0u)) return -1;
-    return 2;
+    return launch_dependent(k_weights<T>, dim3(static_cast<uint32_t>(blocks)), dim3(256), 0, st, p) == cudaSuccess ? 1 : -1;
 }
 
 template <typename T>
-int launch_type(cudaStream_t st, const GradientArgs& a, void* work)
+int launch_type(cudaStream_t st, uint32_t type, const GradientArgs& a, void* work)
 {
-    const Plan plan = plan_for(a);
-    float* const part_w = static_cast<float*>(work);
-    float* const part_b = reinterpret_cast<float*>(static_cast<uint8_t*>(work) + plan.w_bytes);
-    int n = 0;
-    if (a.dx && a.f.rows) {
+    const Plan plan = plan_for(type, a, false);
+    uint8_t* const at = static_cast<uint8_t*>(work);
+    float* const part_w = reinterpret_cast<float*>(at + plan.tc_bytes);
+    float* const part_b = reinterpret_cast<float*>(at + plan.tc_bytes + plan.w_bytes);
+    const uint32_t w_sets = a.sum_w ? 1u : a.f.groups, b_sets = a.sum_b ? 1u : a.f.groups;
+    int launches = 0, n = 0;
+    if (plan.tc.dx || plan.tc.dw) {
+        n = launch_grouped_gradient_tc(st, type, a, plan.tc, plan.w_splits, part_w, work);
+        if (n < 0) return n;
+        launches += n;
+    }
+    if (a.dx && a.f.rows && !plan.tc.dx) {
         n = launch_rows<T>(st, a);
         if (n < 0) return n;
+        launches += n;
     }
-    if (a.dw) {
-        const int k = launch_weights<T>(st, a, true, plan.both, plan.w_splits, part_w, part_b);
-        if (k < 0) return k;
-        n += k;
+    if (a.dw && !plan.tc.dw) {
+        n = launch_weights<T>(st, a, true, plan.both, plan.w_splits, part_w, part_b);
+        if (n < 0) return n;
+        launches += n;
     }
     if (a.db && !plan.both) {
-        const int k = launch_weights<T>(st, a, false, true, plan.b_splits, nullptr, part_b);
-        if (k < 0) return k;
-        n += k;
+        n = launch_weights<T>(st, a, false, true, plan.b_splits, nullptr, part_b);
+        if (n < 0) return n;
+        launches += n;
     }
-    return n;
+    if (plan.w_splits > 1u) {
+        if (!add_parts<T>(st, part_w, plan.w_splits, w_sets, a.f.n_out, a.f.n_in, a.dw, a.stride_dw, a.ld_dw)) return -1;
+        ++launches;
+    }
+    if (plan.b_splits > 1u) {
+        if (!add_parts<T>(st, part_b, plan.b_splits, b_sets, 1u, a.f.n_out, a.db, a.stride_db, 0u)) return -1;
+        ++launches;
+    }
+    return launches;
 }
 
 }  // namespace
 
-size_t grouped_gradient_bytes(uint32_t, const GradientArgs& a)
+size_t grouped_gradient_bytes(uint32_t type, const GradientArgs& a, bool any_address)
 {
-    const Plan p = plan_for(a);
-    return p.w_bytes + p.b_bytes;
+    const Plan p = plan_for(type, a, any_address);
+    return p.tc_bytes + p.w_bytes + p.b_bytes;
 }
 
 int launch_grouped_gradient(cudaStream_t st, uint32_t type, const GradientArgs& a, void* work)
 {
-    return type == EVO_F32 ? launch_type<float>(st, a, work) : type == EVO_BF16 ? launch_type<__nv_bfloat16>(st, a, work) : launch_type<__half>(st, a, work);
+    return type == EVO_F32 ? launch_type<float>(st, type, a, work) : type == EVO_BF16 ? launch_type<__nv_bfloat16>(st, type, a, work) : launch_type<__half>(st, type, a, work);
 }
 
 }  // namespace evo

@@ -21,7 +21,39 @@ __device__ __forceinline__ float dz_of(const GradientArgs& a, float dy, float y)
     return dy * scale;
 }
 
-size_t grouped_gradient_bytes(uint32_t type, const GradientArgs& a);   // workspace; with addresses of 0, enough for any
+// dz / scale: no larger than dy
+__device__ __forceinline__ float dz_unit(const GradientArgs& a, float dy, float y)
+{
+    if (a.f.activation == EVO_ACT_TANH) return dy * ((a.f.scale - y) * a.inverse) * ((a.f.scale + y) * a.inverse);
+    if (a.f.activation == EVO_ACT_RELU) return (a.f.scale > 0.f ? y > 0.f : y < 0.f) ? dy : 0.f;
+    return dy;
+}
+// Rows of a set (a group, or all of them together), of which split `split` of `splits` has its part, a multiple of 16 rows.
+__device__ __forceinline__ void set_rows(const GradientArgs& a, bool all, uint32_t set, uint32_t split, uint32_t splits, uint64_t* first, uint64_t* end)
+{
+    group_rows(a.f, set, first, end);
+    if (all) {
+        uint64_t p;
+        group_rows(a.f, a.f.groups - 1u, &p, end);
+        if (*end < *first) *end = *first;
+    }
+    const uint64_t per = ((*end - *first + splits - 1u) / splits + 15u) / 16u * 16u;
+    const uint64_t f = *first + split * per;
+    *end = min(*end, f + per);
+    *first = f;                                              // (behind the end: no rows)
+}
+
+size_t grouped_gradient_bytes(uint32_t type, const GradientArgs& a, bool any_address);      // workspace; any_address: enough wherever the inputs lie
 int launch_grouped_gradient(cudaStream_t st, uint32_t type, const GradientArgs& a, void* work);
+
+// grouped_gradient_tc.cu: dx and dW on tcgen05, and what has to be laid out in the workspace for that
+struct TcPlan {
+    bool dx, dw, lay_dz, lay_x, lay_w;
+    uint32_t dz_parts, pitch_dz, pitch, long_rows;
+    uint64_t dz_bytes, x_bytes, w_bytes, sum_bytes;
+    uint64_t bytes() const { return dz_bytes + x_bytes + w_bytes + sum_bytes; }
+};
+TcPlan grouped_gradient_tc_plan(uint32_t type, const GradientArgs& a, bool dx, bool dw, uint32_t splits, bool any_address);
+int launch_grouped_gradient_tc(cudaStream_t st, uint32_t type, const GradientArgs& a, const TcPlan& plan, uint32_t splits, float* part, void* work);
 
 }  // namespace evo

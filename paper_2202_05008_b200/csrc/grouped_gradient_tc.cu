@@ -1,0 +1,412 @@
+// Gradients of the products grouped by member on tcgen05.
+//
+// dW_g = scale sum_r dz[r] x[r]' over the group's rows: both operands lie with the contracted index, the rows, outermost, so TMA brings boxes of 64 columns x 64 (or 16)
+// rows as they are and the MMA takes both as MN-major; nothing is transposed.  A tile is 128 outputs x up to 256 inputs; blocks stay and walk over (set, split, 128 outputs,
+// inputs), the inputs of 128 outputs side by side, so that dz is read from L2.  One thread copies, one issues the MMAs, eight warps take the sums of one
+// tile out of tensor memory, through shared memory so that rows of a tile are written whole, while the next tile's are under way.  The last rows of a group end inside a box: the
+// rows behind them, another group's, are overwritten with zeros in shared memory (both operands: theirs may be infinities).
+// dx goes through the forward's kernel with the weights' rows as the contracted index.
+//
+// dz = dy act'(z) is laid out first where it is not dy itself, scale left to the end: fp32 as three bf16 parts like the rows (and weights), of 16-bit types with
+// tanh as two parts of the type (rounded once it would be off by as much as the result's own rounding); relu's is dy or 0.
+#include <cmath>
+
+#include "grouped_gradient.h"
+#include "grouped_tc.cuh"
+
+namespace evo {
+namespace {
+
+constexpr uint32_t kMostStages = 8, kThreads = 320, kMostColumns = 256;
+constexpr uint32_t kRing = 192u * 1024u, kStaging = 8u * 4096u, kSmem = kRing + kStaging + 1024u;
+
+// The tensor core cuts its sums off (2.7e-5 of 4,096 numbers of one sign).  fp32: the last pass, of the large products, is taken out every 8 chunks of 64 rows and added up in
+// fp32; 16-bit types: every 128.
+constexpr uint32_t kSegment = 8, kLongSegment = 128;
+
+struct DwArgs {
+    GradientArgs a;
+    CUtensorMap dz[2], x[2];                                 // boxes of 16 and of 64 rows
+    uint32_t all, sets, splits, out_tiles, in_tiles, columns, stages;
+    uint32_t passes, pitch_dz, pitch_x;
+    float* part;                                             // splits > 1: [splits][sets][n_out][n_in]
+    float* sums;                                             // 16-bit types: room for the sums of long sets, [first row / long_rows][n_out][n_in]
+    uint32_t long_rows, pieces;                              // pieces: 16-byte stores are possible
+};
+
+struct Item { uint32_t o0, i0, columns, set, split; uint64_t row, end; };
+__device__ __forceinline__ Item item_at(const DwArgs& p, uint32_t at)
+{
+    Item t;
+    t.i0 = static_cast<uint32_t>(at % p.in_tiles) * p.columns; at /= p.in_tiles;
+    t.columns = min(p.columns, (p.a.f.n_in - t.i0 + 15u) / 16u * 16u);
+    t.o0 = static_cast<uint32_t>(at % p.out_tiles) * 128u; at /= p.out_tiles;
+    t.split = at % p.splits; t.set = at / p.splits;
+    set_rows(p.a, p.all, t.set, t.split, p.splits, &t.row, &t.end);
+    if (t.end < t.row) t.end = t.row;
+    return t;
+}
+
+template <typename T, typename O>
+__global__ void __launch_bounds__(kThreads, 1) k_weights_tc(const __grid_constant__ DwArgs p)
+{
+    extern __shared__ uint8_t raw[];
+    __shared__ __align__(8) uint64_t full[kMostStages], empty[kMostStages], done[2], taken[2], drain;
+    __shared__ uint32_t slot, limit;
+    __shared__ volatile int abort_flag;
+    constexpr bool kFloat = std::is_same<O, float>::value;
+    const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31u;
+    const uint32_t smem = (smem_u32(raw) + 1023u) / 1024u * 1024u;
+    if (tid == 0) {
+        for (uint32_t s = 0; s < kMostStages; ++s) { mbar_init(smem_u32(&full[s]), 1); mbar_init(smem_u32(&empty[s]), 1); }
+        for (uint32_t b = 0; b < 2u; ++b) { mbar_init(smem_u32(&done[b]), 1); mbar_init(smem_u32(&taken[b]), 8); }
+        mbar_init(smem_u32(&drain), 1);
+        mbar_init_fence();
+        limit = 31u;
+        abort_flag = 0;
+    }
+    dep_wait();
+    dep_trigger();
+    if (warp == 1) tmem_alloc(smem_u32(&slot), 512);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = slot, stages = p.stages, boxes = (p.columns + 63u) / 64u, stage_bytes = (2u + boxes) * 8192u;
+    const uint32_t items = p.sets * p.splits * p.out_tiles * p.in_tiles;
+    auto wait = [&](uint64_t* bar, uint32_t parity) {
+        if (mbar_try_wait(smem_u32(bar), parity) || abort_flag) return;
+        if (!mbar_wait_bounded(smem_u32(bar), parity, &limit)) abort_flag = 1;
+    };
+    auto aborted = [&] { return __any_sync(0xffffffffu, abort_flag) != 0; };
+    auto chunks_of = [&](const Item& t) { return static_cast<uint32_t>((t.end - t.row + 63u) / 64u); };
+    // the step behind the part of a sum that begins at step k
+    auto part_end = [&](uint32_t k, uint32_t chunks) {
+        const uint32_t steps = chunks * p.passes;
+        return kFloat ? min(steps, max(k, steps - chunks) + kSegment) : min(steps, k + kLongSegment);
+    };
+    uint32_t stage = 0, phase = 0, acc = 0, acc_phase = 0, filled = 0;
+
+    if (warp == 0) {
+        Item next = blockIdx.x < items ? item_at(p, blockIdx.x) : Item{};
+        for (uint32_t at = blockIdx.x; at < items; at += gridDim.x) {
+            const Item t = next;
+            if (at + gridDim.x < items) next = item_at(p, at + gridDim.x);       // (its offsets are on their way meanwhile)
+            const uint32_t chunks = chunks_of(t), steps = chunks * p.passes, across = (t.columns + 63u) / 64u, high = t.o0 + 64u < p.a.f.n_out ? 2u : 1u;
+            uint32_t pass = 0, chunk = 0;
+            for (uint32_t k = 0; k < steps; ++k) {
+                wait(&empty[stage], phase ^ 1u);
+                if (aborted()) break;
+                if (lane == 0) {
+                    const uint32_t bar = smem_u32(&full[stage]), to = smem + stage * stage_bytes;
+                    const uint64_t row = t.row + chunk * 64ull;
+                    const uint32_t box = t.end - row > 16u ? 1u : 0u, bytes = box ? 8192u : 2048u;
+                    uint32_t c_dz = t.o0, c_x = t.i0;
+                    if (p.passes == 2u) c_dz += kPartTwo[pass] * p.pitch_dz;
+                    else if (p.passes > 1u) { c_dz += kPartW[pass] * p.pitch_dz; c_x += kPartX[pass] * p.pitch_x; }
+                    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" :: "r"(bar), "r"((high + across) * bytes) : "memory");
+                    for (uint32_t b = 0; b < high; ++b) copy2(to + b * bytes, &p.dz[box], c_dz + 64u * b, static_cast<uint32_t>(row), bar);
+                    for (uint32_t b = 0; b < across; ++b) copy2(to + (2u + b) * bytes, &p.x[box], c_x + 64u * b, static_cast<uint32_t>(row), bar);
+                }
+                if (++chunk == chunks) { chunk = 0; ++pass; }
+                __syncwarp();
+                ++filled;
+                if (++stage == stages) { stage = 0; phase ^= 1u; }
+            }
+            if (aborted()) break;
+        }
+        if (aborted())                                       // nothing may land after the block has gone
+            for (uint32_t s = 0; s < min(filled, stages); ++s) {
+                const uint32_t nth = filled - 1u - s;
+                mbar_wait_bounded(smem_u32(&full[nth % stages]), nth / stages & 1u, &limit);
+            }
+    } else if (warp == 1) {
+        Item next = blockIdx.x < items ? item_at(p, blockIdx.x) : Item{};
+        for (uint32_t at = blockIdx.x; at < items; at += gridDim.x) {
+            const Item t = next;
+            if (at + gridDim.x < items) next = item_at(p, at + gridDim.x);
+            const uint32_t chunks = chunks_of(t), steps = chunks * p.passes, across = (t.columns + 63u) / 64u, id = idesc<T, true, true>(t.columns);
+            uint32_t chunk = 0;
+            for (uint32_t k = 0; k < steps && !aborted();) {
+                const uint32_t d = tmem + acc * kMostColumns, first = k, end = part_end(k, chunks);
+                wait(&taken[acc], acc_phase ^ 1u);
+                for (; k < end; ++k) {
+                    wait(&full[stage], phase);
+                    tc_fence_after();
+                    if (aborted()) break;
+                    const uint32_t at_stage = smem + stage * stage_bytes;
+                    const uint64_t left = t.end - (t.row + chunk * 64ull);
+                    const uint32_t live = left < 64u ? static_cast<uint32_t>(left) : 64u, sixteens = (live + 15u) / 16u, bytes = left > 16u ? 8192u : 2048u;
+                    if (live & 15u) {                        // rows that are not the set's, as far as the MMAs reach (rows of a box are 128 bytes, whatever the swizzle)
+                        const uint32_t pieces = (sixteens * 16u - live) * 8u;
+                        for (uint32_t i = lane; i < pieces * (2u + across); i += 32u) {
+                            const uint32_t b = i / pieces;
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" :: "r"(at_stage + b * bytes + live * 128u + (i % pieces) * 16u), "r"(0u) : "memory");
+                        }
+                        fence_async_smem();
+                        __syncwarp();
+                    }
+                    if (lane == 0) {
+                        for (uint32_t s = 0; s < sixteens; ++s)
+                            umma_bf16(d, desc_sw128_mn(at_stage + s * 2048u, bytes), desc_sw128_mn(at_stage + 2u * bytes + s * 2048u, bytes), id, k - first + s != 0u);
+                        umma_commit(smem_u32(&empty[stage]));
+                        if (k + 1u == end) umma_commit(smem_u32(&done[acc]));
+                    }
+                    __syncwarp();
+                    if (++chunk == chunks) chunk = 0;
+                    if (++stage == stages) { stage = 0; phase ^= 1u; }
+                }
+                if (aborted()) break;
+                acc ^= 1u;
+                if (acc == 0u) acc_phase ^= 1u;
+            }
+            if (aborted()) break;
+        }
+        if (aborted()) {                                     // nor may an MMA write after its tensor memory is freed
+            if (lane == 0) umma_commit(smem_u32(&drain));
+            __syncwarp();
+            mbar_wait_bounded(smem_u32(&drain), 0u, &limit);
+        }
+    } else {
+        const uint32_t quarter = warp & 3u, half = (warp - 2u) >> 2, n_in = p.a.f.n_in, n_out = p.a.f.n_out;
+        const uint32_t staging = smem + kRing + (warp - 2u) * 4096u;
+        Item next = blockIdx.x < items ? item_at(p, blockIdx.x) : Item{};
+        for (uint32_t at = blockIdx.x; at < items; at += gridDim.x) {
+            const Item t = next;
+            if (at + gridDim.x < items) next = item_at(p, at + gridDim.x);
+            const uint32_t chunks = chunks_of(t), steps = chunks * p.passes, o0 = t.o0 + quarter * 32u;
+            // where the result goes, and where sums of several parts are kept meanwhile
+            O* const to = static_cast<O*>(p.a.dw) + static_cast<uint64_t>(t.set) * p.a.stride_dw;
+            float* sums = nullptr;
+            uint64_t ld_sums = n_in;
+            if (p.splits > 1u) sums = p.part + (static_cast<uint64_t>(t.split) * p.sets + t.set) * n_out * n_in;
+            else if constexpr (kFloat) { sums = reinterpret_cast<float*>(to); ld_sums = p.a.ld_dw; }
+            else if (steps > kLongSegment) sums = p.sums + t.row / p.long_rows * n_out * n_in;
+            for (uint32_t first = 0, end = 0; first == 0u || end < steps; first = end) {
+                if (steps) {
+                    end = part_end(first, chunks);
+                    wait(&done[acc], acc_phase);
+                    tc_fence_after();
+                }
+                const float scale = abort_flag ? __int_as_float(0x7FC00000) : p.a.f.scale;
+                const bool last = end >= steps;
+                for (uint32_t c = half * 32u; c < t.columns; c += 64u) {
+                    uint32_t u[4][8];
+                    if (steps) {
+                        tmem_ld32_issue(tmem + acc * kMostColumns + (quarter << 21) + c, u);
+                        tmem_ld8x4_fence(u[0], u[1], u[2], u[3]);
+                    } else {
+#pragma unroll
+                        for (uint32_t i = 0; i < 32u; ++i) u[i / 8u][i % 8u] = 0u;
+                    }
+                    // a row of 32 numbers a lane, its eight pieces of 16 bytes in an order that the lane's number turns: no bank is hit twice
+                    __syncwarp();
+#pragma unroll
+                    for (uint32_t i = 0; i < 8u; ++i)
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" :: "r"(staging + lane * 128u + ((i ^ lane) & 7u) * 16u), "r"(u[i / 2u][i % 2u * 4u]),
+                                     "r"(u[i / 2u][i % 2u * 4u + 1u]), "r"(u[i / 2u][i % 2u * 4u + 2u]), "r"(u[i / 2u][i % 2u * 4u + 3u]) : "memory");
+                    __syncwarp();
+                    const uint32_t column = t.i0 + c;
+                    if (p.pieces) {                          // eight lanes a row, four rows at a time
+                        const uint32_t k = column + (lane & 7u) * 4u;
+#pragma unroll
+                        for (uint32_t i = 0; i < 8u; ++i) {
+                            const uint32_t r = i * 4u + (lane >> 3), o = o0 + r;
+                            float4 v;
+                            asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+                                         : "r"(staging + r * 128u + ((lane ^ r) & 7u) * 16u) : "memory");
+                            if (o >= n_out || k >= n_in) continue;
+                            if (sums) {
+                                float4* const s = reinterpret_cast<float4*>(sums + o * ld_sums + k);
+                                if (first) { const float4 w = *s; v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w; }
+                                if (!last) { *s = v; continue; }
+                            }
+                            v.x *= scale; v.y *= scale; v.z *= scale; v.w *= scale;
+                            if (kFloat || p.splits > 1u) {
+                                *reinterpret_cast<float4*>((p.splits > 1u ? sums : reinterpret_cast<float*>(to)) + o * (p.splits > 1u ? ld_sums : p.a.ld_dw) + k) = v;
+                            } else {
+                                uint2 w;
+                                if constexpr (std::is_same<O, __half>::value) {
+                                    const __half2 a = __floats2half2_rn(v.x, v.y), b = __floats2half2_rn(v.z, v.w);
+                                    w = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+                                } else {
+                                    w = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
+                                }
+                                *reinterpret_cast<uint2*>(to + o * p.a.ld_dw + k) = w;
+                            }
+                        }
+                    } else {                                 // a number a lane, row by row
+                        const uint32_t k = column + lane;
+#pragma unroll 8
+                        for (uint32_t r = 0; r < 32u; ++r) {
+                            const uint32_t o = o0 + r;
+                            float v;
+                            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(staging + r * 128u + ((lane >> 2 ^ r) & 7u) * 16u + (lane & 3u) * 4u) : "memory");
+                            if (o >= n_out || k >= n_in) continue;
+                            if (sums) {
+                                float* const s = sums + o * ld_sums + k;
+                                if (first) v += *s;
+                                if (!last) { *s = v; continue; }
+                            }
+                            v *= scale;
+                            if (p.splits > 1u) sums[o * ld_sums + k] = v;
+                            else if constexpr (kFloat) to[o * p.a.ld_dw + k] = v;
+                            else if constexpr (std::is_same<O, __half>::value) to[o * p.a.ld_dw + k] = __float2half_rn(v);
+                            else to[o * p.a.ld_dw + k] = __float2bfloat16_rn(v);
+                        }
+                    }
+                }
+                if (!steps) break;
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&taken[acc]));
+                acc ^= 1u;
+                if (acc == 0u) acc_phase ^= 1u;
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        tc_fence_after();
+        tmem_dealloc(tmem, 512);
+    }
+}
+
+// dz / scale of every row, in parts `pitch` apart that are filled up with zeros; a warp a row.
+template <typename T, uint32_t PARTS>
+__global__ void __launch_bounds__(256) k_lay_dz(const __grid_constant__ GradientArgs a, uint16_t* __restrict__ to, uint32_t pitch)
+{
+    dep_wait();
+    dep_trigger();
+    const uint64_t row = static_cast<uint64_t>(blockIdx.x) * 8u + (threadIdx.x >> 5);
+    if (row >= a.f.rows) return;
+    const T* const dy = static_cast<const T*>(a.dy) + row * a.ld_dy;
+    const T* const y = static_cast<const T*>(a.f.y) + row * a.f.ld_y;
+    const bool act = a.f.activation != EVO_ACT_NONE;
+    uint16_t* const dst = to + row * PARTS * pitch;
+#pragma unroll 4
+    for (uint32_t k = threadIdx.x & 31u; k < pitch; k += 32u) {
+        const bool live = k < a.f.n_out;
+        if constexpr (std::is_same<T, float>::value) {
+            three_parts(live ? dz_unit(a, dy[k], act ? y[k] : 0.f) : 0.f, dst + k, dst + pitch + k, dst + 2u * pitch + k);
+        } else {
+            auto number = [](T x) { if constexpr (std::is_same<T, __half>::value) return __half2float(x); else return __bfloat162float(x); };
+            auto rounded = [](float x) { if constexpr (std::is_same<T, __half>::value) return __float2half_rn(x); else return __float2bfloat16_rn(x); };
+            const float x = live ? dz_unit(a, number(dy[k]), act ? number(y[k]) : 0.f) : 0.f;
+            const T first = rounded(x);
+            reinterpret_cast<T*>(dst)[k] = first;
+            if constexpr (PARTS == 2u) reinterpret_cast<T*>(dst)[pitch + k] = rounded(isfinite(number(first)) ? x - number(first) : 0.f);      // (an infinity has no second part)
+        }
+    }
+}
+
+bool addressable(const void* p, uint64_t ld, uint64_t rows) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0u && (ld & 7u) == 0u && ld < (1ull << 38) && rows < (1ull << 31); }
+uint64_t padded(uint64_t bytes) { return (bytes + 255u) / 256u * 256u; }
+
+}  // namespace
+
+TcPlan grouped_gradient_tc_plan(uint32_t type, const GradientArgs& a, bool dx, bool dw, uint32_t splits, bool any_address)
+{
+    TcPlan p;
+    const GroupedArgs& f = a.f;
+    const bool fp32 = type == EVO_F32, tanh = f.activation == EVO_ACT_TANH;
+    p.dx = dx; p.dw = dw;
+    p.dz_parts = fp32 ? 3u : tanh ? 2u : 1u;
+    p.lay_dz = (dx || dw) && (fp32 || f.activation != EVO_ACT_NONE || any_address || !addressable(a.dy, a.ld_dy, f.rows));
+    p.lay_x = dw && (fp32 || any_address || !addressable(f.x, f.ld_x, f.rows));
+    p.lay_w = dx && (fp32 || any_address || !addressable(f.w, f.ld_w | f.stride_w, 1u));
+    p.pitch_dz = (f.n_out + 63u) / 64u * 64u;
+    p.pitch = grouped_tc_pitch(type, f.n_in);
+    const uint64_t parts = fp32 ? 3u : 1u, sets = f.groups > 1u && f.stride_w == 0u ? 1u : f.groups, steps = dw && !fp32 && splits == 1u ? p.dz_parts : 0u;
+    p.long_rows = 64u * kLongSegment / p.dz_parts;
+    p.dz_bytes = p.lay_dz ? padded(2ull * f.rows * p.dz_parts * p.pitch_dz) : 0u;
+    p.x_bytes = p.lay_x ? padded(2ull * f.rows * parts * p.pitch) : 0u;
+    p.w_bytes = p.lay_w ? padded(2ull * sets * f.n_out * parts * p.pitch) : 0u;
+    p.sum_bytes = steps && f.rows > p.long_rows ? padded(4ull * (f.rows / p.long_rows + 1u) * f.n_out * f.n_in) : 0u;
+    return p;
+}
+
+int launch_grouped_gradient_tc(cudaStream_t st, uint32_t type, const GradientArgs& a, const TcPlan& plan, uint32_t splits, float* part, void* work)
+{
+    const GroupedArgs& f = a.f;
+    uint8_t* at = static_cast<uint8_t*>(work);
+    const bool fp32 = type == EVO_F32;
+    const uint32_t passes = fp32 ? 6u : plan.dz_parts;
+    int launches = 0;
+    const void* dz = a.dy; const void* x = f.x; const void* w = f.w;
+    uint64_t ld_dz = a.ld_dy, span_dz = f.n_out, ld_x = f.ld_x, span_x = f.n_in, ld_w = f.ld_w, span_w = f.n_in, stride_w = f.stride_w;
+    if (plan.lay_dz) {
+        const uint64_t blocks = (f.rows + 7u) / 8u;
+        if (blocks > 0x7FFFFFFFull) return -2;
+        uint16_t* const to = reinterpret_cast<uint16_t*>(at);
+        at += plan.dz_bytes;
+        auto kernel = fp32 ? k_lay_dz<float, 3> : type == EVO_F16 ? (plan.dz_parts == 2u ? k_lay_dz<__half, 2> : k_lay_dz<__half, 1>)
+                                                                  : (plan.dz_parts == 2u ? k_lay_dz<__nv_bfloat16, 2> : k_lay_dz<__nv_bfloat16, 1>);
+        if (launch_dependent(kernel, dim3(static_cast<uint32_t>(blocks)), dim3(256), 0, st, a, to, plan.pitch_dz) != cudaSuccess) return -1;
+        ++launches;
+        dz = to;
+        ld_dz = span_dz = static_cast<uint64_t>(plan.dz_parts) * plan.pitch_dz;
+    }
+    const uint64_t parts = fp32 ? 3u : 1u;
+    if (plan.lay_x) {
+        uint16_t* const to = reinterpret_cast<uint16_t*>(at);
+        at += plan.x_bytes;
+        const int n = lay_out(st, type, f, true, plan.pitch, to);
+        if (n < 0) return n;
+        launches += n;
+        x = to; ld_x = parts * plan.pitch; span_x = fp32 ? ld_x : f.n_in;
+    }
+    if (plan.lay_w) {
+        uint16_t* const to = reinterpret_cast<uint16_t*>(at);
+        at += plan.w_bytes;
+        const int n = lay_out(st, type, f, false, plan.pitch, to);
+        if (n < 0) return n;
+        launches += n;
+        w = to; ld_w = parts * plan.pitch; span_w = fp32 ? ld_w : f.n_in;
+        stride_w = f.groups > 1u && f.stride_w == 0u ? 0u : ld_w * f.n_out;
+    }
+    if (plan.dx) {
+        GroupedArgs t = f;
+        t.w = w; t.ld_w = ld_w; t.stride_w = stride_w; t.x = dz; t.ld_x = ld_dz; t.b = nullptr; t.y = a.dx; t.ld_y = a.ld_dx;
+        t.n_in = f.n_out; t.n_out = f.n_in; t.activation = EVO_ACT_NONE;
+        const int n = launch_grouped_tc_transposed(st, type, t, passes, plan.pitch, plan.pitch_dz, span_w, span_dz);
+        if (n < 0) return n;
+        launches += n;
+    }
+    if (!plan.dw) return launches;
+    const EncodeTiled encode = tensor_map_encoder();
+    if (!encode) return -1;
+    DwArgs p;
+    p.a = a;
+    p.all = a.sum_w; p.sets = a.sum_w ? 1u : f.groups; p.splits = splits;
+    p.out_tiles = (f.n_out + 127u) / 128u;
+    p.in_tiles = (f.n_in + kMostColumns - 1u) / kMostColumns;
+    // (several tiles are whole boxes wide: sums leave tensor memory 32 columns at a time)
+    p.columns = p.in_tiles > 1u ? ((f.n_in + p.in_tiles - 1u) / p.in_tiles + 63u) / 64u * 64u : (f.n_in + 15u) / 16u * 16u;
+    p.in_tiles = (f.n_in + p.columns - 1u) / p.columns;
+    const uint32_t stage_bytes = (2u + (p.columns + 63u) / 64u) * 8192u;
+    p.stages = kRing / stage_bytes < kMostStages ? kRing / stage_bytes : kMostStages;
+    p.passes = passes; p.pitch_dz = plan.pitch_dz; p.pitch_x = plan.pitch;
+    p.part = part;
+    p.sums = reinterpret_cast<float*>(at);
+    p.long_rows = plan.long_rows;
+    const uint32_t size = fp32 ? 4u : 2u;
+    p.pieces = f.n_in % 4u == 0u && (splits > 1u || (reinterpret_cast<uintptr_t>(a.dw) % (4u * size) == 0u && (a.ld_dw | a.stride_dw) % 4u == 0u));
+    const CUtensorMapDataType t = type == EVO_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+    for (uint32_t box = 0; box < 2u; ++box) {
+        const cuuint64_t dd[2] = { span_dz, f.rows }, ds[1] = { 2u * ld_dz }, xd[2] = { span_x, f.rows }, xs[1] = { 2u * ld_x };
+        const cuuint32_t size_of[2] = { 64u, box ? 64u : 16u }, one[2] = { 1u, 1u };
+        if (encode(&p.dz[box], t, 2, const_cast<void*>(dz), dd, ds, size_of, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS ||
+            encode(&p.x[box], t, 2, const_cast<void*>(x), xd, xs, size_of, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+            return -1;
+    }
+    const uint64_t items = static_cast<uint64_t>(p.sets) * splits * p.out_tiles * p.in_tiles;
+    if (items > 0x7FFFFFFFull) return -2;
+    auto kernel = fp32 ? k_weights_tc<__nv_bfloat16, float> : type == EVO_F16 ? k_weights_tc<__half, __half> : k_weights_tc<__nv_bfloat16, __nv_bfloat16>;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) != cudaSuccess) return -1;
+    return launch_dependent(kernel, dim3(items < kSms ? static_cast<uint32_t>(items) : kSms), dim3(kThreads), kSmem, st, p) == cudaSuccess ? launches + 1 : -1;
+}
+
+}  // namespace evo

@@ -11,13 +11,13 @@
 // issues the MMAs, eight warps take the sums of one tile out of tensor memory while the next tile's are under way.
 // 8,192 even rows of 4 groups, 4,096 -> 4,096: 225 us, 1,220 TFLOP/s; of 32 groups, 1,024 -> 4,096: 82 us (the weights alone are 41 from
 // memory).  What is left is the first loads, the last wave and, in ragged groups, tiles of few rows.
+//
+// TR: the weights' rows are the contracted index (the gradient of the rows, dx[r] = W_g' dz[r]): they come as boxes of 64 x 64, MN-major, and nothing is transposed.
 #include <cmath>
 #include <type_traits>
 
-#include "grouped.h"
 #include "grouped_mma.cuh"
-#include "tma.h"
-#include "umma.cuh"
+#include "grouped_tc.cuh"
 
 namespace evo {
 namespace {
@@ -40,35 +40,8 @@ struct TcArgs {
     CUtensorMap w, x[3];                                     // the rows in boxes of 32, 64 and 128
     uint32_t out_tiles, shared_w;                            // shared_w: one set of weights for all groups
     uint32_t most_rows, stages;                              // of a tile (a multiple of 32); as many as the ring has room for
-    uint32_t passes, pitch;                                  // passes through the contracted index; from one part of an operand to the next
+    uint32_t passes, pitch_w, pitch_x;                       // passes through the contracted index (1, 6, or TR 2); from one part of an operand to the next
 };
-// fp32: which parts (0 the largest) of the weights and of the rows a pass multiplies
-__constant__ uint8_t kPartW[6] = { 0, 2, 1, 0, 1, 0 }, kPartX[6] = { 2, 0, 1, 1, 0, 0 };
-
-// K-major operand of rows of 128 bytes with the 128-byte swizzle, groups of 8 rows side by side
-__device__ __forceinline__ uint64_t desc_sw128(uint32_t addr)
-{
-    return static_cast<uint64_t>((addr & 0x3FFFFu) >> 4) | static_cast<uint64_t>(1) << 16 | static_cast<uint64_t>(64) << 32 |
-           static_cast<uint64_t>(1) << 46 | static_cast<uint64_t>(2) << 61;
-}
-template <typename T>
-__device__ __forceinline__ uint32_t idesc(uint32_t n)
-{
-    const uint32_t type = std::is_same<T, __half>::value ? 0u : 1u;
-    return (1u << 4) | (type << 7) | (type << 10) | ((n >> 3) << 17) | ((128u >> 4) << 24);
-}
-
-__device__ __forceinline__ void copy2(uint32_t dst, const CUtensorMap* map, uint32_t c0, uint32_t c1, uint32_t bar)
-{
-    asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
-                 :: "r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1) : "memory");
-}
-__device__ __forceinline__ void copy3(uint32_t dst, const CUtensorMap* map, uint32_t c0, uint32_t c1, uint32_t c2, uint32_t bar)
-{
-    asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
-                 :: "r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2) : "memory");
-}
-
 // Walks a warp over the tiles of all groups.  Row tiles of a group: as few as can be, equal up to 16 rows.
 struct Walk {
     uint32_t base = 0;                                       // groups [base, base + 32): a lane each
@@ -113,7 +86,7 @@ struct Walk {
 };
 
 // T: type of the operands, O: of bias and result; LONG: a sum of 16-bit operands in several parts
-template <typename T, typename O, bool LONG>
+template <typename T, typename O, bool LONG, bool TR>
 __global__ void __launch_bounds__(kThreads, 1) k_grouped_tc(const __grid_constant__ TcArgs p)
 {
     extern __shared__ uint8_t raw[];
@@ -145,7 +118,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_grouped_tc(const __grid_constan
     };
     // the step behind the part of a sum that begins at step k
     const uint32_t small_steps = steps - chunks;
-    auto part_end = [&](uint32_t k) { return LONG ? min(steps, k + kLongSegment) : p.passes > 1u ? min(steps, max(k, small_steps) + kSegment) : steps; };
+    auto part_end = [&](uint32_t k) { return LONG ? min(steps, k + kLongSegment) : std::is_same<O, float>::value && p.passes > 1u ? min(steps, max(k, small_steps) + kSegment) : steps; };
     auto aborted = [&] { return __any_sync(0xffffffffu, abort_flag) != 0; };
     Walk walk;
     walk.fill(p);
@@ -163,8 +136,16 @@ __global__ void __launch_bounds__(kThreads, 1) k_grouped_tc(const __grid_constan
                 if (lane == 0) {
                     const uint32_t bar = smem_u32(&full[stage]), to = smem + stage * stage_bytes;
                     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" :: "r"(bar), "r"(kWBytes + read * 128u) : "memory");
-                    const uint32_t kw = chunk * 64u + (p.passes > 1u ? kPartW[pass] * p.pitch : 0u), kx = chunk * 64u + (p.passes > 1u ? kPartX[pass] * p.pitch : 0u);
-                    copy3(to, &p.w, kw, o0, p.shared_w ? 0u : group, bar);
+                    const uint32_t set = p.shared_w ? 0u : group;
+                    uint32_t at_w = 0, kx = chunk * 64u;     // (where the operands' parts begin)
+                    if (TR && p.passes == 2u) kx += kPartTwo[pass] * p.pitch_x;
+                    else if (p.passes > 1u) { at_w = kPartW[pass] * p.pitch_w; kx += kPartX[pass] * p.pitch_x; }
+                    if constexpr (TR) {
+                        copy3(to, &p.w, at_w + o0, chunk * 64u, set, bar);
+                        copy3(to + 8192u, &p.w, at_w + o0 + 64u, chunk * 64u, set, bar);
+                    } else {
+                        copy3(to, &p.w, at_w + chunk * 64u, o0, set, bar);
+                    }
                     // (as few copies as make up the rows: 8,192 of 4 groups, 4,096 -> 4,096, 323 us with 32 rows each, 242 with 128)
                     for (uint32_t b = 0; b < read;) {
                         const uint32_t box = read - b >= 128u ? 2u : read - b >= 64u ? 1u : 0u;
@@ -187,7 +168,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_grouped_tc(const __grid_constan
     } else if (warp == 1) {
         for (uint64_t at = blockIdx.x; walk.find(p, at / p.out_tiles, &group, &row, &rows); at += gridDim.x) {
             if (rows == 0u) continue;
-            const uint32_t id = idesc<T>((rows + 15u) / 16u * 16u);
+            const uint32_t id = idesc<T, TR>((rows + 15u) / 16u * 16u);
             for (uint32_t k = 0; k < steps && !aborted();) {
                 const uint32_t d = tmem + acc * kMostRows, first = k, end = part_end(k);
                 wait(&taken[acc], acc_phase ^ 1u);
@@ -198,7 +179,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_grouped_tc(const __grid_constan
                     if (lane == 0) {
                         const uint32_t w = smem + stage * stage_bytes;
 #pragma unroll
-                        for (uint32_t s = 0; s < 4u; ++s) umma_bf16(d, desc_sw128(w + s * 32u), desc_sw128(w + kWBytes + s * 32u), id, k - first + s != 0u);
+                        for (uint32_t s = 0; s < 4u; ++s) umma_bf16(d, TR ? desc_sw128_mn(w + s * 2048u, 8192u) : desc_sw128(w + s * 32u), desc_sw128(w + kWBytes + s * 32u), id, k - first + s != 0u);
                         umma_commit(smem_u32(&empty[stage]));
                         if (k + 1u == end) umma_commit(smem_u32(&done[acc]));
                     }
@@ -336,19 +317,11 @@ __global__ void __launch_bounds__(256) k_lay_out(const __grid_constant__ Grouped
         for (uint32_t k = 2u * lane; k < a.n_in; k += 64u)
             *reinterpret_cast<uint32_t*>(dst + k) = s[k] | (k + 1u < a.n_in ? static_cast<uint32_t>(s[k + 1u]) << 16 : 0u);
     } else {
-        // An infinity or a NaN has no further parts (the product of an infinity's with a zero would be NaN); a number that would round to an infinity, from 3.396e38 on, is
-        // cut off instead.  (Without branches, so that the loads of several numbers run ahead: 61 groups of 159 rows, 2,428 -> 5, 169 us, with them 197.)
+        // (Without branches: 61 groups of 159 rows, 2,428 -> 5, 169 us, with them 197.)
 #pragma unroll 4
         for (uint32_t k = lane; k < pitch; k += 32u) {
             const float x = k < a.n_in ? src[k] : 0.f;
-            uint32_t part = __bfloat16_as_ushort(__float2bfloat16_rn(x));
-            part -= (part & 0x7FFFu) == 0x7F80u && fabsf(x) <= 3.402823466e38f ? 1u : 0u;
-            const float back = __uint_as_float(part << 16);
-            const float rest = fabsf(back) <= 3.402823466e38f ? x - back : 0.f;
-            const __nv_bfloat16 second = __float2bfloat16_rn(rest);
-            dst[k] = static_cast<uint16_t>(part);
-            dst[pitch + k] = __bfloat16_as_ushort(second);
-            dst[2u * pitch + k] = __bfloat16_as_ushort(__float2bfloat16_rn(rest - __bfloat162float(second)));
+            three_parts(x, dst + k, dst + pitch + k, dst + 2u * pitch + k);
         }
     }
 }
@@ -383,7 +356,7 @@ bool grouped_tc_takes(uint32_t type, const GroupedArgs& a)
     return rows >= groups * (1000.0 / a.n_in + groups / 133.0 + 0.5 * (out_tiles * 128.0 / a.n_out - 1.0) + 24.0 * idle * idle * idle);
 }
 
-static uint32_t pitch_for(uint32_t type, uint32_t n_in) { return type == EVO_F32 ? (n_in + 63u) / 64u * 64u : (n_in + 7u) / 8u * 8u; }
+uint32_t grouped_tc_pitch(uint32_t type, uint32_t n_in) { return type == EVO_F32 ? (n_in + 63u) / 64u * 64u : (n_in + 7u) / 8u * 8u; }
 
 // Bytes for rows laid out anew where that pays (0: it does not): the weights are read, written and read again whatever the rows, so a group has to have some, and
 // more where its rows are short, where there are many groups to walk over, and where a tile for each 128 outputs leaves SMs without one.  16-bit operands, against loads of
@@ -395,7 +368,7 @@ static uint32_t pitch_for(uint32_t type, uint32_t n_in) { return type == EVO_F32
 // Over 1,100 drawn shapes (up to 4,096 -> 4,096, 4,096 groups, 300 rows a group) the choice takes 1.02 times the faster side's time in the geometric mean.
 size_t grouped_tc_bytes(uint32_t type, const GroupedArgs& a)
 {
-    const uint64_t pitch = pitch_for(type, a.n_in), parts = type == EVO_F32 ? 3u : 1u;
+    const uint64_t pitch = grouped_tc_pitch(type, a.n_in), parts = type == EVO_F32 ? 3u : 1u;
     const bool shared = a.groups > 1u && a.stride_w == 0u, fp32 = type == EVO_F32;
     const double least = (fp32 ? 24.0 : 4.0) + 1500.0 / a.n_in + std::fmin(a.groups, 400.0) / 50.0 + (fp32 ? 8.0 : 4.0) * idle_share(a);
     if (a.rows >= (1ull << 31) || static_cast<double>(a.rows) < least * a.groups || (shared ? 1ull : a.groups) * a.n_out >= (1ull << 31)) return 0;
@@ -419,46 +392,34 @@ static uint32_t rows_of_a_tile(const GroupedArgs& a, uint32_t out_tiles, uint32_
     return best;
 }
 
-int launch_grouped_tc(cudaStream_t st, uint32_t type, const GroupedArgs& in, void* work)
+// Weights of groups that have rows, or (rows) the rows of x, as TMA can address them.
+int lay_out(cudaStream_t st, uint32_t type, const GroupedArgs& a, bool rows, uint32_t pitch, uint16_t* to)
+{
+    const uint64_t sets = a.groups > 1u && a.stride_w == 0u ? 1u : a.groups;
+    const uint64_t blocks = rows ? (a.rows + 7u) / 8u : sets * ((a.n_out + 7u) / 8u), stride = rows ? 0u : a.stride_w, ld = rows ? a.ld_x : a.ld_w;
+    if (blocks > 0x7FFFFFFFull) return -2;
+    const void* const from = rows ? a.x : a.w;
+    const uint32_t n_out = rows ? 0u : a.n_out;
+    const dim3 grid(static_cast<uint32_t>(blocks));
+    const cudaError_t e = type == EVO_F32 ? launch_dependent(k_lay_out<float>, grid, dim3(256), 0, st, a, static_cast<const float*>(from), stride, ld, n_out, to, pitch)
+                                          : launch_dependent(k_lay_out<__half>, grid, dim3(256), 0, st, a, static_cast<const __half*>(from), stride, ld, n_out, to, pitch);
+    return e == cudaSuccess ? 1 : -1;
+}
+
+// The product with operands as they lie (or have been laid out): span_w and span_x numbers of a row of each can be addressed.
+static int launch_tiles(cudaStream_t st, uint32_t type, TcArgs& p, bool transposed, uint64_t span_w, uint64_t span_x)
 {
     const EncodeTiled f = tensor_map_encoder();
     if (!f) return -1;
-    TcArgs p;
-    p.g = in;
-    GroupedArgs& a = p.g;
+    const GroupedArgs& a = p.g;
     p.out_tiles = (a.n_out + 127u) / 128u;
     p.shared_w = a.groups > 1u && a.stride_w == 0u;
-    p.passes = type == EVO_F32 ? 6u : 1u;
-    p.pitch = pitch_for(type, a.n_in);
-    int launches = 1;
-    uint64_t span = a.n_in;                                  // of the contracted index, all parts
-    if (work) {
-        const uint32_t parts = type == EVO_F32 ? 3u : 1u, sets = p.shared_w ? 1u : a.groups;
-        uint16_t* const w = static_cast<uint16_t*>(work);
-        uint16_t* const x = w + (static_cast<uint64_t>(sets) * a.n_out * parts * p.pitch + 127u) / 128u * 128u;
-        const uint64_t w_blocks = static_cast<uint64_t>(sets) * ((a.n_out + 7u) / 8u), x_blocks = (a.rows + 7u) / 8u;
-        if (w_blocks > 0x7FFFFFFFull || x_blocks > 0x7FFFFFFFull) return -2;
-        cudaError_t e;
-        if (type == EVO_F32) {
-            e = launch_dependent(k_lay_out<float>, dim3(static_cast<uint32_t>(w_blocks)), dim3(256), 0, st, a, static_cast<const float*>(a.w), a.stride_w, a.ld_w, a.n_out, w, p.pitch);
-            if (e == cudaSuccess) e = launch_dependent(k_lay_out<float>, dim3(static_cast<uint32_t>(x_blocks)), dim3(256), 0, st, a, static_cast<const float*>(a.x), 0ull, a.ld_x, 0u, x, p.pitch);
-        } else {
-            e = launch_dependent(k_lay_out<__half>, dim3(static_cast<uint32_t>(w_blocks)), dim3(256), 0, st, a, static_cast<const __half*>(a.w), a.stride_w, a.ld_w, a.n_out, w, p.pitch);
-            if (e == cudaSuccess) e = launch_dependent(k_lay_out<__half>, dim3(static_cast<uint32_t>(x_blocks)), dim3(256), 0, st, a, static_cast<const __half*>(a.x), 0ull, a.ld_x, 0u, x, p.pitch);
-        }
-        if (e != cudaSuccess) return -1;
-        launches = 3;
-        a.w = w; a.x = x;
-        a.ld_w = a.ld_x = static_cast<uint64_t>(parts) * p.pitch;
-        a.stride_w = p.shared_w ? 0u : a.ld_w * a.n_out;
-        if (type == EVO_F32) span = a.ld_w;
-    }
     const CUtensorMapDataType t = type == EVO_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
     // (a pitch of 0 is one that is never taken: any valid one stands in for it)
-    const uint64_t own = (span + 7ull) / 8ull * 8ull;
-    const cuuint64_t wd[3] = { span, a.n_out, p.shared_w ? 1u : a.groups }, ws[2] = { 2u * (a.ld_w ? a.ld_w : own), 2u * (a.stride_w ? a.stride_w : own) };
-    const cuuint64_t xd[2] = { span, a.rows }, xs[1] = { 2u * (a.ld_x ? a.ld_x : own) };
-    const cuuint32_t wb[3] = { 64u, 128u, 1u }, xb[3][2] = { { 64u, 32u }, { 64u, 64u }, { 64u, 128u } }, one[3] = { 1u, 1u, 1u };
+    const uint64_t own_w = (span_w + 7ull) / 8ull * 8ull, own_x = (span_x + 7ull) / 8ull * 8ull;
+    const cuuint64_t wd[3] = { span_w, transposed ? a.n_in : a.n_out, p.shared_w ? 1u : a.groups }, ws[2] = { 2u * (a.ld_w ? a.ld_w : own_w), 2u * (a.stride_w ? a.stride_w : own_w) };
+    const cuuint64_t xd[2] = { span_x, a.rows }, xs[1] = { 2u * (a.ld_x ? a.ld_x : own_x) };
+    const cuuint32_t wb[3] = { 64u, transposed ? 64u : 128u, 1u }, xb[3][2] = { { 64u, 32u }, { 64u, 64u }, { 64u, 128u } }, one[3] = { 1u, 1u, 1u };
     if (f(&p.w, t, 3, const_cast<void*>(a.w), wd, ws, wb, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
           CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
         return -1;
@@ -466,16 +427,56 @@ int launch_grouped_tc(cudaStream_t st, uint32_t type, const GroupedArgs& in, voi
         if (f(&p.x[box], t, 2, const_cast<void*>(a.x), xd, xs, xb[box], one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
             return -1;
-    const bool parts_held = type != EVO_F32 && a.n_in > kLong;
+    const bool parts_held = type != EVO_F32 && static_cast<uint64_t>(a.n_in) * p.passes > kLong;
     p.most_rows = rows_of_a_tile(a, p.out_tiles, parts_held ? kLongRows : kMostRows);
     p.stages = kRing / (kWBytes + p.most_rows * 128u);
     if (p.stages > kMostStages) p.stages = kMostStages;
     const uint64_t used = a.rows < a.groups ? a.rows : a.groups, most = (a.rows / p.most_rows + used) * p.out_tiles;
-    auto kernel = type == EVO_F32 ? k_grouped_tc<__nv_bfloat16, float, false>
-                : type == EVO_F16 ? (parts_held ? k_grouped_tc<__half, __half, true> : k_grouped_tc<__half, __half, false>)
-                                  : (parts_held ? k_grouped_tc<__nv_bfloat16, __nv_bfloat16, true> : k_grouped_tc<__nv_bfloat16, __nv_bfloat16, false>);
+    using B = __nv_bfloat16;
+    auto kernel = transposed ? (type == EVO_F32 ? k_grouped_tc<B, float, false, true>
+                              : type == EVO_F16 ? (parts_held ? k_grouped_tc<__half, __half, true, true> : k_grouped_tc<__half, __half, false, true>)
+                                                : (parts_held ? k_grouped_tc<B, B, true, true> : k_grouped_tc<B, B, false, true>))
+                             : (type == EVO_F32 ? k_grouped_tc<B, float, false, false>
+                              : type == EVO_F16 ? (parts_held ? k_grouped_tc<__half, __half, true, false> : k_grouped_tc<__half, __half, false, false>)
+                                                : (parts_held ? k_grouped_tc<B, B, true, false> : k_grouped_tc<B, B, false, false>));
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) != cudaSuccess) return -1;
-    return launch_dependent(kernel, dim3(most < kSms ? static_cast<uint32_t>(most) : kSms), dim3(kThreads), kSmem, st, p) == cudaSuccess ? launches : -1;
+    return launch_dependent(kernel, dim3(most < kSms ? static_cast<uint32_t>(most) : kSms), dim3(kThreads), kSmem, st, p) == cudaSuccess ? 1 : -1;
+}
+
+int launch_grouped_tc(cudaStream_t st, uint32_t type, const GroupedArgs& in, void* work)
+{
+    TcArgs p;
+    p.g = in;
+    GroupedArgs& a = p.g;
+    p.passes = type == EVO_F32 ? 6u : 1u;
+    p.pitch_w = p.pitch_x = grouped_tc_pitch(type, a.n_in);
+    int launches = 0;
+    uint64_t span = a.n_in;                                  // of the contracted index, all parts
+    if (work) {
+        const bool shared = a.groups > 1u && a.stride_w == 0u;
+        const uint32_t parts = type == EVO_F32 ? 3u : 1u, pitch = p.pitch_x;
+        uint16_t* const w = static_cast<uint16_t*>(work);
+        uint16_t* const x = w + (static_cast<uint64_t>(shared ? 1u : a.groups) * a.n_out * parts * pitch + 127u) / 128u * 128u;
+        for (int rows = 0; rows < 2; ++rows) {
+            const int n = lay_out(st, type, a, rows != 0, pitch, rows ? x : w);
+            if (n < 0) return n;
+            launches += n;
+        }
+        a.w = w; a.x = x;
+        a.ld_w = a.ld_x = static_cast<uint64_t>(parts) * pitch;
+        a.stride_w = shared ? 0u : a.ld_w * a.n_out;
+        if (type == EVO_F32) span = a.ld_w;
+    }
+    const int n = launch_tiles(st, type, p, false, span, span);
+    return n < 0 ? n : launches + n;
+}
+
+int launch_grouped_tc_transposed(cudaStream_t st, uint32_t type, const GroupedArgs& a, uint32_t passes, uint32_t pitch_w, uint32_t pitch_x, uint64_t span_w, uint64_t span_x)
+{
+    TcArgs p;
+    p.g = a;
+    p.passes = passes; p.pitch_w = pitch_w; p.pitch_x = pitch_x;
+    return launch_tiles(st, type, p, true, span_w, span_x);
 }
 
 }  // namespace evo

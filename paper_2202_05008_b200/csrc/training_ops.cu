@@ -177,7 +177,9 @@ evo_status evo_grouped_linear_backward_bytes(const evo_grouped* forward, const e
 {
     GradientArgs a;
     if (!bytes || !gradient_args(forward, p, &a)) return EVO_ERR_INVALID_ARG;
-    *bytes = grouped_gradient_bytes(forward->type, a);
+    // (before the buffers exist: as much as they need wherever they lie)
+    const bool known = a.dy && (!a.dw || a.f.x) && (!a.dx || a.f.w);
+    *bytes = grouped_gradient_bytes(forward->type, a, !known);
     return EVO_OK;
 }
 
@@ -205,7 +207,7 @@ evo_status evo_grouped_linear_backward(const evo_grouped* forward, const evo_gro
     if ((a.dw && w_sets > 1u && a.stride_dw < set_dw) || (a.db && b_sets > 1u && a.stride_db < g.n_out)) return EVO_ERR_INVALID_ARG;
     const Span in[] = { dy, y, x, w, offsets }, rows[] = { dx }, weights[] = { dw }, biases[] = { db }, out[] = { dw, db };
     if (!apart(rows, in) || !apart(weights, in) || !apart(biases, in) || !apart(rows, out) || !interleaved(a, size, set_dw * size, w_sets, b_sets, dw, db)) return EVO_ERR_INVALID_ARG;
-    const evo_status st = check_workspace(grouped_gradient_bytes(forward->type, a), d_workspace, workspace_bytes);
+    const evo_status st = check_workspace(grouped_gradient_bytes(forward->type, a, false), d_workspace, workspace_bytes);
     return st != EVO_OK ? st : status_of(launch_grouped_gradient(static_cast<cudaStream_t>(cuda_stream), forward->type, a, d_workspace));
 }
 
