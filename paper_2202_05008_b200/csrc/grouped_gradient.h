@@ -28,19 +28,25 @@ __device__ __forceinline__ float dz_unit(const GradientArgs& a, float dy, float 
     if (a.f.activation == EVO_ACT_RELU) return (a.f.scale > 0.f ? y > 0.f : y < 0.f) ? dy : 0.f;
     return dy;
 }
-// Rows of a set (a group, or all of them together), of which split `split` of `splits` has its part, a multiple of 16 rows.
-__device__ __forceinline__ void set_rows(const GradientArgs& a, bool all, uint32_t set, uint32_t split, uint32_t splits, uint64_t* first, uint64_t* end)
+// Rows of a set (a group, or all of them together) between two offsets, inside [0, rows], of which split `split` of `splits` has its part, a multiple of 16 rows.
+__device__ __forceinline__ void split_rows(const GradientArgs& a, int64_t p, int64_t q, uint32_t split, uint32_t splits, uint64_t* first, uint64_t* end)
 {
-    group_rows(a.f, set, first, end);
-    if (all) {
-        uint64_t p;
-        group_rows(a.f, a.f.groups - 1u, &p, end);
-        if (*end < *first) *end = *first;
-    }
+    const int64_t top = static_cast<int64_t>(a.f.rows);
+    p = p < 0 ? 0 : p > top ? top : p;
+    q = q < p ? p : q > top ? top : q;
+    *first = static_cast<uint64_t>(p);
+    *end = static_cast<uint64_t>(q);
+    if (splits == 1u) return;
     const uint64_t per = ((*end - *first + splits - 1u) / splits + 15u) / 16u * 16u;
     const uint64_t f = *first + split * per;
     *end = min(*end, f + per);
     *first = f;                                              // (behind the end: no rows)
+}
+__device__ __forceinline__ void set_rows(const GradientArgs& a, bool all, uint32_t set, uint32_t split, uint32_t splits, uint64_t* first, uint64_t* end)
+{
+    const uint32_t behind = all ? a.f.groups : set + 1u;
+    if (a.f.wide_offsets) split_rows(a, static_cast<const int64_t*>(a.f.offsets)[set], static_cast<const int64_t*>(a.f.offsets)[behind], split, splits, first, end);
+    else split_rows(a, static_cast<const int32_t*>(a.f.offsets)[set], static_cast<const int32_t*>(a.f.offsets)[behind], split, splits, first, end);
 }
 
 size_t grouped_gradient_bytes(uint32_t type, const GradientArgs& a, bool any_address);      // workspace; any_address: enough wherever the inputs lie

@@ -17,7 +17,7 @@
 namespace evo {
 namespace {
 
-constexpr uint32_t kMostStages = 8, kThreads = 320, kMostColumns = 256;
+constexpr uint32_t kMostStages = 8, kThreads = 352, kMostColumns = 256;
 constexpr uint32_t kRing = 192u * 1024u, kStaging = 8u * 4096u, kSmem = kRing + kStaging + 1024u;
 
 // The tensor core cuts its sums off (2.7e-5 of 4,096 numbers of one sign).  fp32: the last pass, of the large products, is taken out every 8 chunks of 64 rows and added up in
@@ -26,23 +26,40 @@ constexpr uint32_t kSegment = 8, kLongSegment = 128;
 
 struct DwArgs {
     GradientArgs a;
-    CUtensorMap dz[2], x[2];                                 // boxes of 16 and of 64 rows
+    CUtensorMap dz[2], x[2], dw;                             // boxes of 16 and of 64 rows; of 32 outputs x 128 bytes
     uint32_t all, sets, splits, out_tiles, in_tiles, columns, stages;
     uint32_t passes, pitch_dz, pitch_x;
     float* part;                                             // splits > 1: [splits][sets][n_out][n_in]
     float* sums;                                             // 16-bit types: room for the sums of long sets, [first row / long_rows][n_out][n_in]
-    uint32_t long_rows, pieces;                              // pieces: 16-byte stores are possible
+    uint32_t long_rows, pieces, boxes;                       // pieces: 16-byte stores are possible; boxes: TMA can store the result
 };
 
+// A tile's set, and what it is of the set: the offsets are asked for a tile ahead and looked at when it is its turn.
 struct Item { uint32_t o0, i0, columns, set, split; uint64_t row, end; };
-__device__ __forceinline__ Item item_at(const DwArgs& p, uint32_t at)
+struct Asked { uint32_t o0, i0, set, split; int64_t from, to; };
+__device__ __forceinline__ Asked ask_for(const DwArgs& p, uint32_t at)
+{
+    Asked t;
+    t.i0 = at % p.in_tiles * p.columns; at /= p.in_tiles;
+    t.o0 = at % p.out_tiles * 128u; at /= p.out_tiles;
+    t.split = at % p.splits; t.set = at / p.splits;
+    const GroupedArgs& f = p.a.f;
+    const uint32_t behind = p.all ? f.groups : t.set + 1u;
+    if (f.wide_offsets) {
+        t.from = __ldg(static_cast<const long long*>(f.offsets) + t.set);
+        t.to = __ldg(static_cast<const long long*>(f.offsets) + behind);
+    } else {
+        t.from = __ldg(static_cast<const int*>(f.offsets) + t.set);
+        t.to = __ldg(static_cast<const int*>(f.offsets) + behind);
+    }
+    return t;
+}
+__device__ __forceinline__ Item item_of(const DwArgs& p, const Asked& a)
 {
     Item t;
-    t.i0 = static_cast<uint32_t>(at % p.in_tiles) * p.columns; at /= p.in_tiles;
+    t.o0 = a.o0; t.i0 = a.i0; t.set = a.set; t.split = a.split;
     t.columns = min(p.columns, (p.a.f.n_in - t.i0 + 15u) / 16u * 16u);
-    t.o0 = static_cast<uint32_t>(at % p.out_tiles) * 128u; at /= p.out_tiles;
-    t.split = at % p.splits; t.set = at / p.splits;
-    set_rows(p.a, p.all, t.set, t.split, p.splits, &t.row, &t.end);
+    split_rows(p.a, a.from, a.to, a.split, p.splits, &t.row, &t.end);
     if (t.end < t.row) t.end = t.row;
     return t;
 }
@@ -51,14 +68,14 @@ template <typename T, typename O>
 __global__ void __launch_bounds__(kThreads, 1) k_weights_tc(const __grid_constant__ DwArgs p)
 {
     extern __shared__ uint8_t raw[];
-    __shared__ __align__(8) uint64_t full[kMostStages], empty[kMostStages], done[2], taken[2], drain;
+    __shared__ __align__(8) uint64_t full[kMostStages], empty[kMostStages], cleared[kMostStages], done[2], taken[2], drain;
     __shared__ uint32_t slot, limit;
     __shared__ volatile int abort_flag;
     constexpr bool kFloat = std::is_same<O, float>::value;
     const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31u;
     const uint32_t smem = (smem_u32(raw) + 1023u) / 1024u * 1024u;
     if (tid == 0) {
-        for (uint32_t s = 0; s < kMostStages; ++s) { mbar_init(smem_u32(&full[s]), 1); mbar_init(smem_u32(&empty[s]), 1); }
+        for (uint32_t s = 0; s < kMostStages; ++s) { mbar_init(smem_u32(&full[s]), 1); mbar_init(smem_u32(&empty[s]), 1); mbar_init(smem_u32(&cleared[s]), 1); }
         for (uint32_t b = 0; b < 2u; ++b) { mbar_init(smem_u32(&done[b]), 1); mbar_init(smem_u32(&taken[b]), 8); }
         mbar_init(smem_u32(&drain), 1);
         mbar_init_fence();
@@ -73,11 +90,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_weights_tc(const __grid_constan
     tc_fence_after();
     const uint32_t tmem = slot, stages = p.stages, boxes = (p.columns + 63u) / 64u, stage_bytes = (2u + boxes) * 8192u;
     const uint32_t items = p.sets * p.splits * p.out_tiles * p.in_tiles;
+    // false: it, or another wait of the block, ran out
     auto wait = [&](uint64_t* bar, uint32_t parity) {
-        if (mbar_try_wait(smem_u32(bar), parity) || abort_flag) return;
-        if (!mbar_wait_bounded(smem_u32(bar), parity, &limit)) abort_flag = 1;
+        if (mbar_try_wait(smem_u32(bar), parity)) return true;
+        if (abort_flag) return false;
+        if (mbar_wait_bounded(smem_u32(bar), parity, &limit)) return true;
+        abort_flag = 1;
+        return false;
     };
-    auto aborted = [&] { return __any_sync(0xffffffffu, abort_flag) != 0; };
+    auto all_of = [](bool fine) { return __all_sync(0xffffffffu, fine) != 0; };
     auto chunks_of = [&](const Item& t) { return static_cast<uint32_t>((t.end - t.row + 63u) / 64u); };
     // the step behind the part of a sum that begins at step k
     auto part_end = [&](uint32_t k, uint32_t chunks) {
@@ -87,92 +108,121 @@ __global__ void __launch_bounds__(kThreads, 1) k_weights_tc(const __grid_constan
     uint32_t stage = 0, phase = 0, acc = 0, acc_phase = 0, filled = 0;
 
     if (warp == 0) {
-        Item next = blockIdx.x < items ? item_at(p, blockIdx.x) : Item{};
+        bool fine = true;
+        Asked next = blockIdx.x < items ? ask_for(p, blockIdx.x) : Asked{};
         for (uint32_t at = blockIdx.x; at < items; at += gridDim.x) {
-            const Item t = next;
-            if (at + gridDim.x < items) next = item_at(p, at + gridDim.x);       // (its offsets are on their way meanwhile)
+            const Item t = item_of(p, next);
+            if (at + gridDim.x < items) next = ask_for(p, at + gridDim.x);
             const uint32_t chunks = chunks_of(t), steps = chunks * p.passes, across = (t.columns + 63u) / 64u, high = t.o0 + 64u < p.a.f.n_out ? 2u : 1u;
             uint32_t pass = 0, chunk = 0;
             for (uint32_t k = 0; k < steps; ++k) {
-                wait(&empty[stage], phase ^ 1u);
-                if (aborted()) break;
-                if (lane == 0) {
-                    const uint32_t bar = smem_u32(&full[stage]), to = smem + stage * stage_bytes;
-                    const uint64_t row = t.row + chunk * 64ull;
-                    const uint32_t box = t.end - row > 16u ? 1u : 0u, bytes = box ? 8192u : 2048u;
-                    uint32_t c_dz = t.o0, c_x = t.i0;
-                    if (p.passes == 2u) c_dz += kPartTwo[pass] * p.pitch_dz;
-                    else if (p.passes > 1u) { c_dz += kPartW[pass] * p.pitch_dz; c_x += kPartX[pass] * p.pitch_x; }
-                    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" :: "r"(bar), "r"((high + across) * bytes) : "memory");
-                    for (uint32_t b = 0; b < high; ++b) copy2(to + b * bytes, &p.dz[box], c_dz + 64u * b, static_cast<uint32_t>(row), bar);
-                    for (uint32_t b = 0; b < across; ++b) copy2(to + (2u + b) * bytes, &p.x[box], c_x + 64u * b, static_cast<uint32_t>(row), bar);
+                fine = all_of(wait(&empty[stage], phase ^ 1u));
+                if (!fine) break;
+                const uint32_t bar = smem_u32(&full[stage]), to = smem + stage * stage_bytes;
+                const uint64_t row = t.row + chunk * 64ull;
+                const uint32_t box = t.end - row > 16u ? 1u : 0u, bytes = box ? 8192u : 2048u;
+                if (lane == 0) asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" :: "r"(bar), "r"((high + across) * bytes) : "memory");
+                __syncwarp();
+                // a box a lane: those of dz first
+                if (lane < 2u + across && (lane >= 2u || lane < high)) {
+                    const bool is_x = lane >= 2u;
+                    uint32_t c = is_x ? t.i0 + 64u * (lane - 2u) : t.o0 + 64u * lane;
+                    if (p.passes == 2u) c += is_x ? 0u : kPartTwo[pass] * p.pitch_dz;
+                    else if (p.passes > 1u) c += is_x ? kPartX[pass] * p.pitch_x : kPartW[pass] * p.pitch_dz;
+                    copy2(to + lane * bytes, (is_x ? p.x : p.dz) + box, c, static_cast<uint32_t>(row), bar);
                 }
                 if (++chunk == chunks) { chunk = 0; ++pass; }
                 __syncwarp();
                 ++filled;
                 if (++stage == stages) { stage = 0; phase ^= 1u; }
             }
-            if (aborted()) break;
+            if (!fine) break;
         }
-        if (aborted())                                       // nothing may land after the block has gone
+        if (!fine)                                           // nothing may land after the block has gone
             for (uint32_t s = 0; s < min(filled, stages); ++s) {
                 const uint32_t nth = filled - 1u - s;
                 mbar_wait_bounded(smem_u32(&full[nth % stages]), nth / stages & 1u, &limit);
             }
     } else if (warp == 1) {
-        Item next = blockIdx.x < items ? item_at(p, blockIdx.x) : Item{};
-        for (uint32_t at = blockIdx.x; at < items; at += gridDim.x) {
-            const Item t = next;
-            if (at + gridDim.x < items) next = item_at(p, at + gridDim.x);
-            const uint32_t chunks = chunks_of(t), steps = chunks * p.passes, across = (t.columns + 63u) / 64u, id = idesc<T, true, true>(t.columns);
-            uint32_t chunk = 0;
-            for (uint32_t k = 0; k < steps && !aborted();) {
-                const uint32_t d = tmem + acc * kMostColumns, first = k, end = part_end(k, chunks);
-                wait(&taken[acc], acc_phase ^ 1u);
-                for (; k < end; ++k) {
-                    wait(&full[stage], phase);
+        if (lane == 0) {                                     // (one thread: what it does between two MMAs is time that the tensor core has nothing to do)
+            bool fine = true;
+            uint32_t was_cleared = 0;                        // a bit a stage: the phase of its barrier
+            Asked next = blockIdx.x < items ? ask_for(p, blockIdx.x) : Asked{};
+            for (uint32_t at = blockIdx.x; at < items && fine; at += gridDim.x) {
+                const Item t = item_of(p, next);
+                if (at + gridDim.x < items) next = ask_for(p, at + gridDim.x);
+                const uint32_t chunks = chunks_of(t), steps = chunks * p.passes, id = idesc<T, true, true>(t.columns);
+                const uint32_t rest = static_cast<uint32_t>(t.end - t.row) - (chunks - 1u) * 64u;      // rows of the last chunk
+                uint32_t chunk = 0;
+                for (uint32_t k = 0; k < steps && fine;) {
+                    const uint32_t d = tmem + acc * kMostColumns, first = k, end = part_end(k, chunks);
+                    fine = wait(&taken[acc], acc_phase ^ 1u);
                     tc_fence_after();
-                    if (aborted()) break;
-                    const uint32_t at_stage = smem + stage * stage_bytes;
-                    const uint64_t left = t.end - (t.row + chunk * 64ull);
-                    const uint32_t live = left < 64u ? static_cast<uint32_t>(left) : 64u, sixteens = (live + 15u) / 16u, bytes = left > 16u ? 8192u : 2048u;
-                    if (live & 15u) {                        // rows that are not the set's, as far as the MMAs reach (rows of a box are 128 bytes, whatever the swizzle)
-                        const uint32_t pieces = (sixteens * 16u - live) * 8u;
-                        for (uint32_t i = lane; i < pieces * (2u + across); i += 32u) {
-                            const uint32_t b = i / pieces;
-                            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" :: "r"(at_stage + b * bytes + live * 128u + (i % pieces) * 16u), "r"(0u) : "memory");
+                    for (; k < end && fine; ++k) {
+                        const uint32_t at_stage = smem + stage * stage_bytes;
+                        if (chunk + 1u < chunks || rest == 64u) {
+                            fine = wait(&full[stage], phase);
+                            const uint64_t a = desc_sw128_mn(at_stage, 8192u), b = desc_sw128_mn(at_stage + 16384u, 8192u);
+#pragma unroll
+                            for (uint32_t s = 0; s < 4u; ++s) umma_bf16(d, a + s * 128u, b + s * 128u, id, k - first + s != 0u);
+                        } else {
+                            if (rest & 15u) {
+                                fine = wait(&cleared[stage], was_cleared >> stage & 1u);
+                                was_cleared ^= 1u << stage;
+                            } else {
+                                fine = wait(&full[stage], phase);
+                            }
+                            const uint32_t bytes = rest > 16u ? 8192u : 2048u;
+                            const uint64_t a = desc_sw128_mn(at_stage, bytes), b = desc_sw128_mn(at_stage + 2u * bytes, bytes);
+                            for (uint32_t s = 0; s * 16u < rest; ++s) umma_bf16(d, a + s * 128u, b + s * 128u, id, k - first + s != 0u);
                         }
-                        fence_async_smem();
-                        __syncwarp();
-                    }
-                    if (lane == 0) {
-                        for (uint32_t s = 0; s < sixteens; ++s)
-                            umma_bf16(d, desc_sw128_mn(at_stage + s * 2048u, bytes), desc_sw128_mn(at_stage + 2u * bytes + s * 2048u, bytes), id, k - first + s != 0u);
                         umma_commit(smem_u32(&empty[stage]));
-                        if (k + 1u == end) umma_commit(smem_u32(&done[acc]));
+                        if (++chunk == chunks) chunk = 0;
+                        if (++stage == stages) { stage = 0; phase ^= 1u; }
                     }
-                    __syncwarp();
-                    if (++chunk == chunks) chunk = 0;
-                    if (++stage == stages) { stage = 0; phase ^= 1u; }
+                    umma_commit(smem_u32(&done[acc]));
+                    acc ^= 1u;
+                    if (acc == 0u) acc_phase ^= 1u;
                 }
-                if (aborted()) break;
-                acc ^= 1u;
-                if (acc == 0u) acc_phase ^= 1u;
             }
-            if (aborted()) break;
+            if (!fine) {                                     // no MMA may write after its tensor memory is freed
+                umma_commit(smem_u32(&drain));
+                mbar_wait_bounded(smem_u32(&drain), 0u, &limit);
+            }
         }
-        if (aborted()) {                                     // nor may an MMA write after its tensor memory is freed
-            if (lane == 0) umma_commit(smem_u32(&drain));
-            __syncwarp();
-            mbar_wait_bounded(smem_u32(&drain), 0u, &limit);
+        __syncwarp();
+    } else if (warp == 10) {
+        // Rows of the last chunk's boxes that are not the set's, as far as the MMAs reach, become zeros (rows of a box are 128 bytes, whatever the swizzle).
+        bool fine = true;
+        Asked next = blockIdx.x < items ? ask_for(p, blockIdx.x) : Asked{};
+        for (uint32_t at = blockIdx.x; at < items && fine; at += gridDim.x) {
+            const Item t = item_of(p, next);
+            if (at + gridDim.x < items) next = ask_for(p, at + gridDim.x);
+            const uint32_t chunks = chunks_of(t), across = (t.columns + 63u) / 64u, rest = static_cast<uint32_t>(t.end - t.row) - (chunks - 1u) * 64u;
+            const uint32_t bytes = rest > 16u ? 8192u : 2048u, upto = (rest + 15u) / 16u * 16u;
+            uint32_t chunk = 0;
+            for (uint32_t k = 0; k < chunks * p.passes && fine; ++k) {
+                fine = all_of(wait(&full[stage], phase));    // (every one: a barrier tells apart two phases only)
+                const bool last = ++chunk == chunks;
+                if (last) chunk = 0;
+                if (last && (rest & 15u)) {
+                    for (uint32_t b = 0; b < 2u + across; ++b)
+                        for (uint32_t row = rest + (lane >> 3); row < upto; row += 4u)
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" :: "r"(smem + stage * stage_bytes + b * bytes + row * 128u + (lane & 7u) * 16u), "r"(0u) : "memory");
+                    fence_async_smem();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(smem_u32(&cleared[stage]));
+                }
+                if (++stage == stages) { stage = 0; phase ^= 1u; }
+            }
         }
     } else {
         const uint32_t quarter = warp & 3u, half = (warp - 2u) >> 2, n_in = p.a.f.n_in, n_out = p.a.f.n_out;
         const uint32_t staging = smem + kRing + (warp - 2u) * 4096u;
-        Item next = blockIdx.x < items ? item_at(p, blockIdx.x) : Item{};
+        Asked next = blockIdx.x < items ? ask_for(p, blockIdx.x) : Asked{};
         for (uint32_t at = blockIdx.x; at < items; at += gridDim.x) {
-            const Item t = next;
-            if (at + gridDim.x < items) next = item_at(p, at + gridDim.x);
+            const Item t = item_of(p, next);
+            if (at + gridDim.x < items) next = ask_for(p, at + gridDim.x);
             const uint32_t chunks = chunks_of(t), steps = chunks * p.passes, o0 = t.o0 + quarter * 32u;
             // where the result goes, and where sums of several parts are kept meanwhile
             O* const to = static_cast<O*>(p.a.dw) + static_cast<uint64_t>(t.set) * p.a.stride_dw;
@@ -189,7 +239,47 @@ __global__ void __launch_bounds__(kThreads, 1) k_weights_tc(const __grid_constan
                 }
                 const float scale = abort_flag ? __int_as_float(0x7FC00000) : p.a.f.scale;
                 const bool last = end >= steps;
-                for (uint32_t c = half * 32u; c < t.columns; c += 64u) {
+                if (p.boxes && first == 0u && last) {        // a sum in one part goes out as TMA has it: 128 bytes of 32 outputs
+                    constexpr uint32_t kWide = 128u / sizeof(O);
+                    for (uint32_t c = half * kWide; c < t.columns; c += 2u * kWide) {
+                        uint32_t u[kWide / 32u][4][8];
+                        if (steps) {
+#pragma unroll
+                            for (uint32_t i = 0; i < kWide / 32u; ++i) tmem_ld32_issue(tmem + acc * kMostColumns + (quarter << 21) + c + 32u * i, u[i]);
+#pragma unroll
+                            for (uint32_t i = 0; i < kWide / 32u; ++i) tmem_ld8x4_fence(u[i][0], u[i][1], u[i][2], u[i][3]);
+                        } else {
+#pragma unroll
+                            for (uint32_t i = 0; i < kWide; ++i) u[i / 32u][i / 8u % 4u][i % 8u] = 0u;
+                        }
+                        if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");      // (the box before has left)
+                        __syncwarp();
+#pragma unroll
+                        for (uint32_t i = 0; i < 8u; ++i) {
+                            uint32_t w[4];
+#pragma unroll
+                            for (uint32_t e = 0; e < 4u; ++e) {
+                                if constexpr (kFloat) {
+                                    w[e] = __float_as_uint(scale * __uint_as_float(u[0][i / 2u][i % 2u * 4u + e]));
+                                } else {
+                                    const uint32_t k = i * 8u + 2u * e;
+                                    const float x = scale * __uint_as_float(u[k / 32u][k / 8u % 4u][k % 8u]), y = scale * __uint_as_float(u[k / 32u][k / 8u % 4u][k % 8u + 1u]);
+                                    if constexpr (std::is_same<O, __half>::value) { const __half2 h = __floats2half2_rn(x, y); w[e] = *reinterpret_cast<const uint32_t*>(&h); }
+                                    else w[e] = pack_bf16(x, y);
+                                }
+                            }
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" :: "r"(staging + lane * 128u + ((i ^ lane) & 7u) * 16u), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3])
+                                         : "memory");
+                        }
+                        fence_async_smem();
+                        __syncwarp();
+                        if (lane == 0 && o0 < n_out) {
+                            asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];"
+                                         :: "l"(&p.dw), "r"(staging), "r"(t.i0 + c), "r"(o0), "r"(t.set) : "memory");
+                            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                        }
+                    }
+                } else for (uint32_t c = half * 32u; c < t.columns; c += 64u) {
                     uint32_t u[4][8];
                     if (steps) {
                         tmem_ld32_issue(tmem + acc * kMostColumns + (quarter << 21) + c, u);
@@ -199,6 +289,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_weights_tc(const __grid_constan
                         for (uint32_t i = 0; i < 32u; ++i) u[i / 8u][i % 8u] = 0u;
                     }
                     // a row of 32 numbers a lane, its eight pieces of 16 bytes in an order that the lane's number turns: no bank is hit twice
+                    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
                     __syncwarp();
 #pragma unroll
                     for (uint32_t i = 0; i < 8u; ++i)
@@ -263,6 +354,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_weights_tc(const __grid_constan
                 if (acc == 0u) acc_phase ^= 1u;
             }
         }
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
     tc_fence_before();
     __syncthreads();
@@ -399,6 +491,15 @@ int launch_grouped_gradient_tc(cudaStream_t st, uint32_t type, const GradientArg
         if (encode(&p.dz[box], t, 2, const_cast<void*>(dz), dd, ds, size_of, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                    CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS ||
             encode(&p.x[box], t, 2, const_cast<void*>(x), xd, xs, size_of, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+            return -1;
+    }
+    p.boxes = splits == 1u && reinterpret_cast<uintptr_t>(a.dw) % 16u == 0u && (a.ld_dw | a.stride_dw) * size % 16u == 0u && a.ld_dw < (1ull << 36) && a.stride_dw < (1ull << 36);
+    if (p.boxes) {
+        const uint64_t own = (f.n_in * size + 15ull) / 16ull * 16ull;
+        const cuuint64_t wd[3] = { f.n_in, f.n_out, p.sets }, ws[2] = { a.ld_dw * size, a.stride_dw ? a.stride_dw * size : own };
+        const cuuint32_t box[3] = { 128u / size, 32u, 1u }, one[3] = { 1u, 1u, 1u };
+        if (encode(&p.dw, fp32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : t, 3, a.dw, wd, ws, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
                    CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
             return -1;
     }
