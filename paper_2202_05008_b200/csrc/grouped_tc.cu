@@ -112,91 +112,91 @@ __global__ void __launch_bounds__(kThreads, 1) k_grouped_tc(const __grid_constan
     tc_fence_after();
     const uint32_t tmem = slot, chunks = (a.n_in + 63u) / 64u, steps = chunks * p.passes, stages = p.stages;
     const uint32_t stage_bytes = kWBytes + p.most_rows * 128u;
+    // false: it, or another wait of the block, ran out
     auto wait = [&](uint64_t* bar, uint32_t parity) {
-        if (mbar_try_wait(smem_u32(bar), parity) || abort_flag) return;
-        if (!mbar_wait_bounded(smem_u32(bar), parity, &limit)) abort_flag = 1;
+        if (mbar_try_wait(smem_u32(bar), parity)) return true;
+        if (abort_flag) return false;
+        if (mbar_wait_bounded(smem_u32(bar), parity, &limit)) return true;
+        abort_flag = 1;
+        return false;
     };
+    auto all_of = [](bool fine) { return __all_sync(0xffffffffu, fine) != 0; };
     // the step behind the part of a sum that begins at step k
     const uint32_t small_steps = steps - chunks;
     auto part_end = [&](uint32_t k) { return LONG ? min(steps, k + kLongSegment) : std::is_same<O, float>::value && p.passes > 1u ? min(steps, max(k, small_steps) + kSegment) : steps; };
-    auto aborted = [&] { return __any_sync(0xffffffffu, abort_flag) != 0; };
     Walk walk;
     walk.fill(p);
     uint32_t group, rows, stage = 0, phase = 0, acc = 0, acc_phase = 0, filled = 0;
     uint64_t row;
 
+    bool fine = true;
     if (warp == 0) {
-        for (uint64_t at = blockIdx.x; walk.find(p, at / p.out_tiles, &group, &row, &rows); at += gridDim.x) {
+        for (uint64_t at = blockIdx.x; fine && walk.find(p, at / p.out_tiles, &group, &row, &rows); at += gridDim.x) {
             if (rows == 0u) continue;
-            const uint32_t o0 = static_cast<uint32_t>(at % p.out_tiles) * 128u, read = (rows + 31u) / 32u * 32u;
+            const uint32_t o0 = static_cast<uint32_t>(at % p.out_tiles) * 128u, read = (rows + 31u) / 32u * 32u, set = p.shared_w ? 0u : group;
+            // a copy a lane: the weights' (TR: two boxes of 64 columns), then as few boxes of rows as make them up (8,192 of 4 groups, 4,096 -> 4,096, 323 us with 32 rows
+            // each, 242 with 128): whole 128s, a 64, a 32
+            constexpr uint32_t kBoxes = TR ? 2u : 1u;
+            const uint32_t nth = lane - kBoxes, whole = read / 128u, rest = read % 128u, copies = whole + (rest >= 64u) + (rest % 64u != 0u);
+            const uint32_t box = nth < whole ? 2u : nth == whole && rest >= 64u ? 1u : 0u;
+            const uint32_t before = nth <= whole ? nth * 128u : whole * 128u + 64u;
             uint32_t pass = 0, chunk = 0;
             for (uint32_t k = 0; k < steps; ++k) {
-                wait(&empty[stage], phase ^ 1u);
-                if (aborted()) break;
-                if (lane == 0) {
-                    const uint32_t bar = smem_u32(&full[stage]), to = smem + stage * stage_bytes;
-                    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" :: "r"(bar), "r"(kWBytes + read * 128u) : "memory");
-                    const uint32_t set = p.shared_w ? 0u : group;
-                    uint32_t at_w = 0, kx = chunk * 64u;     // (where the operands' parts begin)
-                    if (TR && p.passes == 2u) kx += kPartTwo[pass] * p.pitch_x;
-                    else if (p.passes > 1u) { at_w = kPartW[pass] * p.pitch_w; kx += kPartX[pass] * p.pitch_x; }
-                    if constexpr (TR) {
-                        copy3(to, &p.w, at_w + o0, chunk * 64u, set, bar);
-                        copy3(to + 8192u, &p.w, at_w + o0 + 64u, chunk * 64u, set, bar);
-                    } else {
-                        copy3(to, &p.w, at_w + chunk * 64u, o0, set, bar);
-                    }
-                    // (as few copies as make up the rows: 8,192 of 4 groups, 4,096 -> 4,096, 323 us with 32 rows each, 242 with 128)
-                    for (uint32_t b = 0; b < read;) {
-                        const uint32_t box = read - b >= 128u ? 2u : read - b >= 64u ? 1u : 0u;
-                        copy2(to + kWBytes + b * 128u, &p.x[box], kx, static_cast<uint32_t>(row) + b, bar);
-                        b += 32u << box;
-                    }
+                fine = all_of(wait(&empty[stage], phase ^ 1u));
+                if (!fine) break;
+                const uint32_t bar = smem_u32(&full[stage]), to = smem + stage * stage_bytes;
+                if (lane == 0) asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" :: "r"(bar), "r"(kWBytes + read * 128u) : "memory");
+                __syncwarp();
+                uint32_t at_w = 0, at_x = 0;                 // (where the operands' parts begin)
+                if (TR && p.passes == 2u) at_x = kPartTwo[pass] * p.pitch_x;
+                else if (p.passes > 1u) { at_w = kPartW[pass] * p.pitch_w; at_x = kPartX[pass] * p.pitch_x; }
+                if (lane < kBoxes) {
+                    if constexpr (TR) copy3(to + 8192u * lane, &p.w, at_w + o0 + 64u * lane, chunk * 64u, set, bar);
+                    else copy3(to, &p.w, at_w + chunk * 64u, o0, set, bar);
+                } else if (nth < copies) {
+                    copy2(to + kWBytes + before * 128u, &p.x[box], at_x + chunk * 64u, static_cast<uint32_t>(row) + before, bar);
                 }
                 if (++chunk == chunks) { chunk = 0; ++pass; }
                 __syncwarp();
                 ++filled;
                 if (++stage == stages) { stage = 0; phase ^= 1u; }
             }
-            if (aborted()) break;
         }
-        if (aborted())                                       // nothing may land after the block has gone
+        if (!fine)                                           // nothing may land after the block has gone
             for (uint32_t s = 0; s < min(filled, stages); ++s) {
                 const uint32_t nth = filled - 1u - s;
                 mbar_wait_bounded(smem_u32(&full[nth % stages]), nth / stages & 1u, &limit);
             }
     } else if (warp == 1) {
-        for (uint64_t at = blockIdx.x; walk.find(p, at / p.out_tiles, &group, &row, &rows); at += gridDim.x) {
+        for (uint64_t at = blockIdx.x; fine && walk.find(p, at / p.out_tiles, &group, &row, &rows); at += gridDim.x) {
             if (rows == 0u) continue;
-            const uint32_t id = idesc<T, TR>((rows + 15u) / 16u * 16u);
-            for (uint32_t k = 0; k < steps && !aborted();) {
-                const uint32_t d = tmem + acc * kMostRows, first = k, end = part_end(k);
-                wait(&taken[acc], acc_phase ^ 1u);
-                for (; k < end; ++k) {
-                    wait(&full[stage], phase);
+            if (lane == 0) {                                 // (one thread: what it does between two MMAs is time that the tensor core has nothing to do)
+                const uint32_t id = idesc<T, TR>((rows + 15u) / 16u * 16u);
+                for (uint32_t k = 0; k < steps && fine;) {
+                    const uint32_t d = tmem + acc * kMostRows, first = k, end = part_end(k);
+                    fine = wait(&taken[acc], acc_phase ^ 1u);
                     tc_fence_after();
-                    if (aborted()) break;
-                    if (lane == 0) {
+                    for (; k < end && fine; ++k) {
+                        fine = wait(&full[stage], phase);
                         const uint32_t w = smem + stage * stage_bytes;
+                        const uint64_t a = TR ? desc_sw128_mn(w, 8192u) : desc_sw128(w), b = desc_sw128(w + kWBytes);
 #pragma unroll
-                        for (uint32_t s = 0; s < 4u; ++s) umma_bf16(d, TR ? desc_sw128_mn(w + s * 2048u, 8192u) : desc_sw128(w + s * 32u), desc_sw128(w + kWBytes + s * 32u), id, k - first + s != 0u);
+                        for (uint32_t s = 0; s < 4u; ++s) umma_bf16(d, a + s * (TR ? 128u : 2u), b + s * 2u, id, k - first + s != 0u);
                         umma_commit(smem_u32(&empty[stage]));
-                        if (k + 1u == end) umma_commit(smem_u32(&done[acc]));
+                        if (++stage == stages) { stage = 0; phase ^= 1u; }
                     }
-                    __syncwarp();
-                    if (++stage == stages) { stage = 0; phase ^= 1u; }
+                    umma_commit(smem_u32(&done[acc]));
+                    acc ^= 1u;
+                    if (acc == 0u) acc_phase ^= 1u;
                 }
-                if (aborted()) break;
-                acc ^= 1u;
-                if (acc == 0u) acc_phase ^= 1u;
             }
-            if (aborted()) break;
+            fine = __shfl_sync(0xffffffffu, fine, 0);
         }
-        if (aborted()) {                                     // nor may an MMA write after its tensor memory is freed
-            if (lane == 0) umma_commit(smem_u32(&drain));
-            __syncwarp();
+        if (!fine && lane == 0) {                            // no MMA may write after its tensor memory is freed
+            umma_commit(smem_u32(&drain));
             mbar_wait_bounded(smem_u32(&drain), 0u, &limit);
         }
+        __syncwarp();
     } else {
         const uint32_t quarter = warp & 3u, half = (warp - 2u) >> 2;
         for (uint64_t at = blockIdx.x; walk.find(p, at / p.out_tiles, &group, &row, &rows); at += gridDim.x) {
