@@ -5,7 +5,7 @@
 // traffic is the bound for long rows, the launch for few short ones.  Rows of up to 256 actions are a part of a warp's, number by number; longer ones a warp's or a block's, in
 // pieces of 16 bytes from the row's first 16-byte boundary on (the ends in single numbers), where logits and gradient lie alike; other rows, and rows longer than a block's
 // registers hold, are read twice, the second time mostly from L2.
-// One thread has the row's scalars in fp64: the ratio may lie close to a border, and 1 - p of the chosen action is a difference.
+// One thread has the row's scalars.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -18,6 +18,7 @@ namespace evo {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr double kLn2 = 0.69314718055994530942;
 
 template <typename T> __device__ __forceinline__ float to_float(T x)
 {
@@ -39,6 +40,30 @@ __device__ __forceinline__ float exp_below(float x, float top)
     return y;
 }
 
+// Two at once: additions and products of pairs are one instruction.
+__device__ __forceinline__ float2 add2(float2 a, float2 b)
+{
+    float2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(*reinterpret_cast<unsigned long long*>(&r))
+        : "l"(*reinterpret_cast<const unsigned long long*>(&a)), "l"(*reinterpret_cast<const unsigned long long*>(&b)));
+    return r;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b)
+{
+    float2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(*reinterpret_cast<unsigned long long*>(&r))
+        : "l"(*reinterpret_cast<const unsigned long long*>(&a)), "l"(*reinterpret_cast<const unsigned long long*>(&b)));
+    return r;
+}
+__device__ __forceinline__ float2 exp_below2(float2 x, float top)
+{
+    const float2 y = mul2(add2(x, make_float2(-top, -top)), make_float2(kLog2e, kLog2e));
+    float2 r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r.x) : "f"(y.x));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r.y) : "f"(y.y));
+    return r;
+}
+
 struct Row { int64_t action; double weight; bool live; };
 __device__ __forceinline__ Row row_of(const PolicyArgs& a, uint64_t row)
 {
@@ -49,23 +74,35 @@ __device__ __forceinline__ Row row_of(const PolicyArgs& a, uint64_t row)
     return r;
 }
 
-// What follows from the row's maximum and s = sum of e^(x - top).  `all`: the factor of e^(x - top) in the gradient, `chosen`: the gradient of the action.
+// What follows from the row's maximum and s = sum of e^(x - top), 1 at least.  `all`: the factor of e^(x - top) in the gradient, `chosen`: the gradient of the action.
+// Differences are taken in fp64, functions of them in fp32: log s of its exponent and of a number close to 1, the ratio's borders as logarithms, 1 - p as an expm1,
+// e^d - 1 - d as its series where it is a small difference.
 __device__ __forceinline__ void finish_row(const PolicyArgs& a, uint64_t row, const Row& r, float chosen_logit, float top, float s, float* all, float* chosen)
 {
-    const double logp = static_cast<double>(chosen_logit) - static_cast<double>(top) - log(static_cast<double>(s));
-    const double adv = a.advantage[row], ratio = exp(logp - static_cast<double>(a.old_logp[row]));
-    const bool clipped = adv >= 0.0 ? ratio > 1.0 + a.clip_high : ratio < 1.0 - a.clip_low;
-    double loss = -adv * (clipped ? (adv >= 0.0 ? 1.0 + a.clip_high : 1.0 - a.clip_low) : ratio);
-    double c = clipped ? 0.0 : -adv * ratio;
-    if (!(ratio == ratio)) loss = c = ratio;                 // (a NaN compares as not clipped for either sign, but 0 times it is one too)
+    const uint32_t bits = __float_as_uint(s);
+    const int32_t exponent = static_cast<int32_t>(bits - 0x3F400000u) >> 23;      // s = m 2^exponent, m from 0.75 up to 1.5
+    const float m = __uint_as_float(bits - (static_cast<uint32_t>(exponent) << 23));
+    double logp = static_cast<double>(chosen_logit) - static_cast<double>(top) - fma(kLn2, static_cast<double>(exponent), static_cast<double>(logf(m)));
+    if (!(s >= 1.f)) logp = static_cast<double>(s);          // (a NaN)
+    const double log_ratio = logp - static_cast<double>(a.old_logp[row]);
+    const float adv = a.advantage[row], ratio = expf(static_cast<float>(log_ratio));
+    const bool clipped = adv >= 0.f ? log_ratio > a.log_high : log_ratio < a.log_low;
+    double loss = -static_cast<double>(adv) * (clipped ? (adv >= 0.f ? 1.0 + a.clip_high : 1.0 - a.clip_low) : static_cast<double>(ratio));
+    double c = clipped ? 0.0 : -static_cast<double>(adv) * static_cast<double>(ratio);
     if (a.ref_logp) {
-        const double d = static_cast<double>(a.ref_logp[row]) - logp, e = expm1(d);
-        loss += a.kl * (e - d);
-        c -= a.kl * e;
+        const float d = static_cast<float>(static_cast<double>(a.ref_logp[row]) - logp), e = expm1f(d);
+        float rest = e - d;
+        if (fabsf(d) < 0.5f) {                               // (what is left out is below 4e-8 of it)
+            float q = 1.f / 40320.f;
+            q = fmaf(q, d, 1.f / 5040.f); q = fmaf(q, d, 1.f / 720.f); q = fmaf(q, d, 1.f / 120.f); q = fmaf(q, d, 1.f / 24.f); q = fmaf(q, d, 1.f / 6.f); q = fmaf(q, d, 0.5f);
+            rest = d * d * q;
+        }
+        loss += a.kl * static_cast<double>(rest);
+        c -= a.kl * static_cast<double>(e);
     }
     c *= r.weight;
-    *all = static_cast<float>(-c / static_cast<double>(s));
-    *chosen = static_cast<float>(-c * expm1(logp));
+    *all = static_cast<float>(-c) / s;
+    *chosen = static_cast<float>(-c) * expm1f(static_cast<float>(logp));
     if (a.logp) a.logp[row] = static_cast<float>(logp);
     if (a.row_loss) a.row_loss[row] = r.weight * loss;
 }
@@ -75,165 +112,262 @@ __device__ __forceinline__ void padded_row(const PolicyArgs& a, uint64_t row)
     if (a.row_loss) a.row_loss[row] = 0.0;
 }
 
-// Up to L E actions: L lanes a row, E numbers each.
-template <typename T, uint32_t L, uint32_t E>
+// Up to L E actions: L lanes a row, E numbers each; a warp has R times 32 / L rows one behind the other, and a lane finishes each of them (a
+// row's scalars in fp64 cost more than its numbers: 4 million rows of 64 took 2,870 us with a row a time).
+template <typename T, uint32_t L, uint32_t E, uint32_t R>
 __global__ void __launch_bounds__(128) k_policy_short(const __grid_constant__ PolicyArgs a)
 {
+    constexpr uint32_t kAcross = 32u / L, kRows = kAcross * R;
+    static_assert(kRows <= 32u, "a lane a row");
     dep_wait();
     dep_trigger();
-    const uint64_t row = static_cast<uint64_t>(blockIdx.x) * (128u / L) + threadIdx.x / L;
-    const uint32_t lane = threadIdx.x % L;
+    const uint32_t all_lanes = threadIdx.x % 32u, lane = all_lanes % L, nth = all_lanes / L;
+    const uint64_t first = (static_cast<uint64_t>(blockIdx.x) * 4u + threadIdx.x / 32u) * kRows;
+    if (first >= a.rows) return;                             // (whole warps)
+    // the lane's own row
+    const uint64_t mine = first + all_lanes;
     Row r;
-    r.live = false;
-    if (row < a.rows) r = row_of(a, row);
-    const T* const x = static_cast<const T*>(a.logits) + (r.live ? row : 0u) * a.ld;
-    float v[E], top = -INFINITY;
-#pragma unroll
-    for (uint32_t i = 0; i < E; ++i) v[i] = r.live && lane + L * i < a.n ? to_float(x[lane + L * i]) : -INFINITY;
-    const float chosen_logit = r.live ? to_float(x[r.action]) : 0.f;
-#pragma unroll
-    for (uint32_t i = 0; i < E; ++i) top = fmaxf(top, v[i]);
-#pragma unroll
-    for (uint32_t d = L / 2u; d > 0u; d /= 2u) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-    float s = 0.f;
-#pragma unroll
-    for (uint32_t i = 0; i < E; ++i)
-        if (lane + L * i < a.n) {
-            v[i] = exp_below(v[i], top);
-            s += v[i];
-        }
-#pragma unroll
-    for (uint32_t d = L / 2u; d > 0u; d /= 2u) s += __shfl_xor_sync(0xffffffffu, s, d);
-    float all = 0.f, chosen = 0.f;
-    if (lane == 0u && row < a.rows) {
-        if (r.live) finish_row(a, row, r, chosen_logit, top, s, &all, &chosen);
-        else padded_row(a, row);
+    r.live = false; r.action = 0; r.weight = 0.0;
+    float chosen_logit = 0.f;
+    if (all_lanes < kRows && mine < a.rows) {
+        r = row_of(a, mine);
+        if (r.live) chosen_logit = to_float(static_cast<const T*>(a.logits)[mine * a.ld + r.action]);
     }
-    all = __shfl_sync(0xffffffffu, all, 0, L);
-    chosen = __shfl_sync(0xffffffffu, chosen, 0, L);
-    if (row >= a.rows || !a.gradient) return;
-    T* const g = static_cast<T*>(a.gradient) + row * a.ld_gradient;
+    float v[R][E], my_top = 0.f, my_sum = 1.f;
+    const uint32_t live = __ballot_sync(0xffffffffu, r.live);
 #pragma unroll
-    for (uint32_t i = 0; i < E; ++i) {
-        const uint32_t k = lane + L * i;
-        if (k < a.n) g[k] = from_float<T>(!r.live ? 0.f : k == static_cast<uint64_t>(r.action) ? chosen : all * v[i]);
+    for (uint32_t p = 0; p < R; ++p) {
+        const uint32_t row = p * kAcross + nth;
+        const T* const x = static_cast<const T*>(a.logits) + (first + row) * a.ld;
+#pragma unroll
+        for (uint32_t i = 0; i < E; ++i) v[p][i] = live >> row & 1u && lane + L * i < a.n ? to_float(x[lane + L * i]) : -INFINITY;
+    }
+#pragma unroll
+    for (uint32_t p = 0; p < R; ++p) {
+        float top = -INFINITY, s = 0.f;
+#pragma unroll
+        for (uint32_t i = 0; i < E; ++i) top = fmaxf(top, v[p][i]);
+#pragma unroll
+        for (uint32_t d = L / 2u; d > 0u; d /= 2u) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+#pragma unroll
+        for (uint32_t i = 0; i < E; ++i)
+            if (lane + L * i < a.n) {
+                v[p][i] = exp_below(v[p][i], top);
+                s += v[p][i];
+            }
+#pragma unroll
+        for (uint32_t d = L / 2u; d > 0u; d /= 2u) s += __shfl_xor_sync(0xffffffffu, s, d);
+        const float t = __shfl_sync(0xffffffffu, top, all_lanes % kAcross * L), u = __shfl_sync(0xffffffffu, s, all_lanes % kAcross * L);
+        if (all_lanes / kAcross == p) { my_top = t; my_sum = u; }
+    }
+    float all = 0.f, chosen = 0.f;
+    if (all_lanes < kRows && mine < a.rows) {
+        if (r.live) finish_row(a, mine, r, chosen_logit, my_top, my_sum, &all, &chosen);
+        else padded_row(a, mine);
+    }
+    if (!a.gradient) return;
+#pragma unroll
+    for (uint32_t p = 0; p < R; ++p) {
+        const uint32_t row = p * kAcross + nth;
+        const float f = __shfl_sync(0xffffffffu, all, row), c = __shfl_sync(0xffffffffu, chosen, row);
+        const uint32_t action = __shfl_sync(0xffffffffu, static_cast<uint32_t>(r.action), row);
+        if (first + row >= a.rows) continue;
+        T* const g = static_cast<T*>(a.gradient) + (first + row) * a.ld_gradient;
+#pragma unroll
+        for (uint32_t i = 0; i < E; ++i) {
+            const uint32_t k = lane + L * i;
+            if (k < a.n) g[k] = from_float<T>(!(live >> row & 1u) ? 0.f : k == action ? c : f * v[p][i]);
+        }
     }
 }
 
-// Maximum or sum over a block (one warp: no shared memory)
-template <uint32_t THREADS, bool MAX>
-__device__ __forceinline__ float over_block(float x, float* part)
+template <bool MAX>
+__device__ __forceinline__ float over_warp(float x)
 {
 #pragma unroll
     for (uint32_t d = 16u; d > 0u; d /= 2u) {
         const float y = __shfl_xor_sync(0xffffffffu, x, d);
         x = MAX ? fmaxf(x, y) : x + y;
     }
-    if constexpr (THREADS > 32u) {
-        if ((threadIdx.x & 31u) == 0u) part[threadIdx.x >> 5] = x;
-        __syncthreads();
-        x = part[threadIdx.x & 31u & (THREADS / 32u - 1u)];
+    return x;
+}
+// Maximum or sum over a block; `part` has room for its warps.
+template <uint32_t THREADS, bool MAX>
+__device__ __forceinline__ float over_block(float x, float* part)
+{
+    constexpr uint32_t kWarps = THREADS / 32u;
+    x = over_warp<MAX>(x);
+    if ((threadIdx.x & 31u) == 0u) part[threadIdx.x / 32u] = x;
+    __syncthreads();
+    x = part[threadIdx.x % kWarps];
 #pragma unroll
-        for (uint32_t d = THREADS / 64u; d > 0u; d /= 2u) {
-            const float y = __shfl_xor_sync(0xffffffffu, x, d);
-            x = MAX ? fmaxf(x, y) : x + y;
-        }
+    for (uint32_t d = kWarps / 2u; d > 0u; d /= 2u) {
+        const float y = __shfl_xor_sync(0xffffffffu, x, d);
+        x = MAX ? fmaxf(x, y) : x + y;
     }
     return x;
 }
 
+// 16 bytes of a row: kept as they were loaded, since numbers taken apart are twice the registers.
 template <typename T> struct Sixteen {
     static constexpr uint32_t N = 16u / sizeof(T);
-    T v[N];
-    __device__ __forceinline__ void load(const T* p) { const uint4 r = *reinterpret_cast<const uint4*>(p); memcpy(v, &r, 16); }
-    __device__ __forceinline__ void store(T* p) const { uint4 r; memcpy(&r, v, 16); *reinterpret_cast<uint4*>(p) = r; }
+    uint32_t w[4];
+    __device__ __forceinline__ void load(const T* p) { const uint4 r = *reinterpret_cast<const uint4*>(p); w[0] = r.x; w[1] = r.y; w[2] = r.z; w[3] = r.w; }
+    __device__ __forceinline__ void store(T* p) const { *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]); }
+    __device__ __forceinline__ void numbers(float2 (&f)[N / 2u]) const
+    {
+#pragma unroll
+        for (uint32_t i = 0; i < 4u; ++i) {
+            if constexpr (std::is_same<T, float>::value) (i % 2u ? f[i / 2u].y : f[i / 2u].x) = __uint_as_float(w[i]);
+            else if constexpr (std::is_same<T, __half>::value) f[i] = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+            else f[i] = make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xFFFF0000u));
+        }
+    }
+    __device__ __forceinline__ void round(const float2 (&f)[N / 2u])
+    {
+#pragma unroll
+        for (uint32_t i = 0; i < 4u; ++i) {
+            if constexpr (std::is_same<T, float>::value) {
+                w[i] = __float_as_uint(i % 2u ? f[i / 2u].y : f[i / 2u].x);
+            } else if constexpr (std::is_same<T, __half>::value) {
+                const __half2 two = __floats2half2_rn(f[i].x, f[i].y);
+                w[i] = *reinterpret_cast<const uint32_t*>(&two);
+            } else {
+                const __nv_bfloat162 two = __floats2bfloat162_rn(f[i].x, f[i].y);
+                w[i] = *reinterpret_cast<const uint32_t*>(&two);
+            }
+        }
+    }
+    // the larger of each pair of numbers, in the type itself (of a number and a NaN the number)
+    __device__ __forceinline__ void larger(const Sixteen& other)
+    {
+#pragma unroll
+        for (uint32_t i = 0; i < 4u; ++i) {
+            if constexpr (std::is_same<T, float>::value) {
+                w[i] = __float_as_uint(fmaxf(__uint_as_float(w[i]), __uint_as_float(other.w[i])));
+            } else if constexpr (std::is_same<T, __half>::value) {
+                const __half2 m = __hmax2(*reinterpret_cast<const __half2*>(&w[i]), *reinterpret_cast<const __half2*>(&other.w[i]));
+                w[i] = *reinterpret_cast<const uint32_t*>(&m);
+            } else {
+                const __nv_bfloat162 m = __hmax2(*reinterpret_cast<const __nv_bfloat162*>(&w[i]), *reinterpret_cast<const __nv_bfloat162*>(&other.w[i]));
+                w[i] = *reinterpret_cast<const uint32_t*>(&m);
+            }
+        }
+    }
+    __device__ __forceinline__ float largest() const
+    {
+        float2 f[N / 2u];
+        numbers(f);
+        float top = fmaxf(f[0].x, f[0].y);
+#pragma unroll
+        for (uint32_t i = 1; i < N / 2u; ++i) top = fmaxf(top, fmaxf(f[i].x, f[i].y));
+        return top;
+    }
+    // sum of e^(x - top)
+    __device__ __forceinline__ float sum_below(float top) const
+    {
+        float2 f[N / 2u], sum = make_float2(0.f, 0.f);
+        numbers(f);
+#pragma unroll
+        for (uint32_t i = 0; i < N / 2u; ++i) sum = add2(sum, exp_below2(f[i], top));
+        return sum.x + sum.y;
+    }
+    // every number to factor e^(x - top)
+    __device__ __forceinline__ void scale_below(float top, float factor)
+    {
+        float2 f[N / 2u];
+        numbers(f);
+#pragma unroll
+        for (uint32_t i = 0; i < N / 2u; ++i) f[i] = mul2(exp_below2(f[i], top), make_float2(factor, factor));
+        round(f);
+    }
 };
 
-// A row in the registers of THREADS threads, NV pieces of 16 bytes and one single number each.
-template <typename T, uint32_t THREADS, uint32_t NV>
-__global__ void __launch_bounds__(THREADS < 128u ? 128u : THREADS) k_policy_row(const __grid_constant__ PolicyArgs a)
+// A row in the registers of a warp, NV pieces of 16 bytes and one single number a lane; the scalars of a block's eight rows are finished by a warp side by side.
+template <typename T, uint32_t NV>
+__global__ void __launch_bounds__(256, 4) k_policy_row(const __grid_constant__ PolicyArgs a)
 {
-    constexpr uint32_t N = Sixteen<T>::N, kRows = THREADS < 128u ? 128u / THREADS : 1u;
-    __shared__ float part[2][32], factors[2];
+    constexpr uint32_t N = Sixteen<T>::N, THREADS = 32, kRows = 8;
+    __shared__ float tops[kRows], sums[kRows], alls[kRows], chosens[kRows];
     dep_wait();
     dep_trigger();
-    const uint64_t row = static_cast<uint64_t>(blockIdx.x) * kRows + threadIdx.x / THREADS;
-    const uint32_t t = threadIdx.x % THREADS;
-    if (row >= a.rows) return;                               // (whole warps)
-    const Row r = row_of(a, row);
+    const uint32_t t = threadIdx.x % THREADS, nth = threadIdx.x / THREADS;
+    const uint64_t first = static_cast<uint64_t>(blockIdx.x) * kRows, row = first + nth;
+    const bool exists = row < a.rows;
+    bool live = false;
+    uint32_t action = 0;
+    if (exists) {
+        const Row r = row_of(a, row);
+        live = r.live;
+        action = static_cast<uint32_t>(r.action);
+    }
     const T* const x = static_cast<const T*>(a.logits) + row * a.ld;
     T* const g = static_cast<T*>(a.gradient) + row * a.ld_gradient;
     // numbers in front of the first 16-byte boundary, pieces, and numbers behind them
     const uintptr_t address = reinterpret_cast<uintptr_t>(a.gradient ? static_cast<const void*>(g) : x);
     const uint32_t head = min(static_cast<uint32_t>((16u - (address & 15u)) & 15u) / static_cast<uint32_t>(sizeof(T)), a.n);
     const uint32_t pieces = (a.n - head) / N, tail = (a.n - head) % N;
-    const bool has_single = t < head + tail;
+    const bool has_single = exists && t < head + tail;
     const uint32_t single = t < head ? t : head + pieces * N + (t - head);
+    const uint32_t mine = live ? pieces : 0u;                // (of a row that is padding nothing is read)
     Sixteen<T> v[NV];
-    if (!r.live) {
-        if (t == 0u) padded_row(a, row);
-        if (!a.gradient) return;
-#pragma unroll
-        for (uint32_t e = 0; e < N; ++e) v[0].v[e] = from_float<T>(0.f);
-#pragma unroll
-        for (uint32_t i = 0; i < NV; ++i)
-            if (t + THREADS * i < pieces) v[0].store(g + head + (t + THREADS * i) * N);
-        if (has_single) g[single] = from_float<T>(0.f);
-        return;
-    }
 #pragma unroll
     for (uint32_t i = 0; i < NV; ++i)
-        if (t + THREADS * i < pieces) v[i].load(x + head + (t + THREADS * i) * N);
-    const float alone = has_single ? to_float(x[single]) : -INFINITY;
-    const float chosen_logit = t == 0u ? to_float(x[r.action]) : 0.f;
+        if (t + THREADS * i < mine) v[i].load(x + head + (t + THREADS * i) * N);
+    const float alone = has_single && live ? to_float(x[single]) : -INFINITY;
+    // the first warp has the rows' scalars, a lane each
+    Row r;
+    float chosen_logit = 0.f;
+    const bool finishes = threadIdx.x < kRows && first + threadIdx.x < a.rows;
+    if (finishes) {
+        r = row_of(a, first + threadIdx.x);
+        if (r.live) chosen_logit = to_float(static_cast<const T*>(a.logits)[(first + threadIdx.x) * a.ld + r.action]);
+    }
     float top = alone;
+    if (t < mine) {
+        Sixteen<T> most = v[0];
 #pragma unroll
-    for (uint32_t i = 0; i < NV; ++i)
-        if (t + THREADS * i < pieces)
-#pragma unroll
-            for (uint32_t e = 0; e < N; ++e) top = fmaxf(top, to_float(v[i].v[e]));
-    top = over_block<THREADS, true>(top, part[0]);
-    float s = has_single ? exp_below(alone, top) : 0.f;
-#pragma unroll
-    for (uint32_t i = 0; i < NV; ++i)
-        if (t + THREADS * i < pieces) {
-            float sum = 0.f;
-#pragma unroll
-            for (uint32_t e = 0; e < N; ++e) sum += exp_below(to_float(v[i].v[e]), top);
-            s += sum;
-        }
-    s = over_block<THREADS, false>(s, part[1]);
-    float all = 0.f, chosen = 0.f;
-    if (t == 0u) finish_row(a, row, r, chosen_logit, top, s, &all, &chosen);
-    if (!a.gradient) return;
-    if constexpr (THREADS > 32u) {
-        if (t == 0u) { factors[0] = all; factors[1] = chosen; }
-        __syncthreads();
-        all = factors[0]; chosen = factors[1];
-    } else {
-        all = __shfl_sync(0xffffffffu, all, 0);
-        chosen = __shfl_sync(0xffffffffu, chosen, 0);
+        for (uint32_t i = 1; i < NV; ++i)
+            if (t + THREADS * i < mine) most.larger(v[i]);
+        top = fmaxf(top, most.largest());
     }
+    top = over_warp<true>(top);
+    float s = has_single && live ? exp_below(alone, top) : 0.f;
+#pragma unroll
+    for (uint32_t i = 0; i < NV; ++i)
+        if (t + THREADS * i < mine) s += v[i].sum_below(top);
+    s = over_warp<false>(s);
+    if (t == 0u) { tops[nth] = top; sums[nth] = s; }
+    __syncthreads();
+    if (finishes) {
+        float all = 0.f, chosen = 0.f;
+        if (r.live) finish_row(a, first + threadIdx.x, r, chosen_logit, tops[threadIdx.x], sums[threadIdx.x], &all, &chosen);
+        else padded_row(a, first + threadIdx.x);
+        alls[threadIdx.x] = all;
+        chosens[threadIdx.x] = chosen;
+    }
+    if (!a.gradient) return;
+    __syncthreads();
+    if (!exists) return;
+    const float all = alls[nth], chosen = chosens[nth];
     // (the action's number is stored by the thread that has stored over it)
-    const uint32_t action = static_cast<uint32_t>(r.action);
-    bool mine = has_single && single == action;
+    bool own = has_single && single == action;
 #pragma unroll
     for (uint32_t i = 0; i < NV; ++i)
         if (t + THREADS * i < pieces) {
-            Sixteen<T> y;
-#pragma unroll
-            for (uint32_t e = 0; e < N; ++e) y.v[e] = from_float<T>(all * exp_below(to_float(v[i].v[e]), top));
-            y.store(g + head + (t + THREADS * i) * N);
-            mine = mine || (action >= head && (action - head) / N == t + THREADS * i);
+            if (live) v[i].scale_below(top, all);
+            else v[i].w[0] = v[i].w[1] = v[i].w[2] = v[i].w[3] = 0u;
+            v[i].store(g + head + (t + THREADS * i) * N);
+            own = own || (action >= head && (action - head) / N == t + THREADS * i);
         }
-    if (has_single) g[single] = from_float<T>(all * exp_below(alone, top));
-    if (mine) g[action] = from_float<T>(chosen);
+    if (has_single) g[single] = from_float<T>(live ? all * exp_below(alone, top) : 0.f);
+    if (own && live) g[action] = from_float<T>(chosen);
 }
 
-// Any length and alignment: a block a row, which is read twice, in pieces of N numbers (N 1: number by number).
-constexpr uint32_t kLongThreads = 512;
-template <typename T, bool PIECES>
-__global__ void __launch_bounds__(kLongThreads) k_policy_long(const __grid_constant__ PolicyArgs a)
+// Any length and alignment: a block a row, which is read twice, the second time from L2 as a rule (holding it in registers or shared memory leaves fewer rows in flight and
+// measured slower: 32,000 of bf16 230 us in registers, 198 like this), in pieces of 16 bytes or (PIECES false) number by number.
+template <typename T, bool PIECES, uint32_t THREADS>
+__global__ void __launch_bounds__(THREADS) k_policy_long(const __grid_constant__ PolicyArgs a)
 {
     constexpr uint32_t N = Sixteen<T>::N;
     __shared__ float part[2][32], factors[2];
@@ -251,44 +385,39 @@ __global__ void __launch_bounds__(kLongThreads) k_policy_long(const __grid_const
         if (t == 0u) padded_row(a, row);
         if (!a.gradient) return;
         Sixteen<T> zero;
-#pragma unroll
-        for (uint32_t e = 0; e < N; ++e) zero.v[e] = from_float<T>(0.f);
-        for (uint32_t i = t; i < pieces; i += kLongThreads) zero.store(g + head + i * N);
-        for (uint32_t k = t; k < head; k += kLongThreads) g[k] = zero.v[0];
-        for (uint32_t k = behind + t; k < a.n; k += kLongThreads) g[k] = zero.v[0];
+        zero.w[0] = zero.w[1] = zero.w[2] = zero.w[3] = 0u;
+        for (uint32_t i = t; i < pieces; i += THREADS) zero.store(g + head + i * N);
+        for (uint32_t k = t; k < head; k += THREADS) g[k] = from_float<T>(0.f);
+        for (uint32_t k = behind + t; k < a.n; k += THREADS) g[k] = from_float<T>(0.f);
         return;
     }
     const float chosen_logit = t == 0u ? to_float(x[r.action]) : 0.f;
     // the thread's maximum, and its sum with that taken off (0 while it has seen forbidden actions alone)
     float top = -INFINITY, s = 0.f;
-    auto add = [&](const float* v, uint32_t count) {
-        float most = v[0];
-        for (uint32_t e = 1; e < count; ++e) most = fmaxf(most, v[e]);
+    auto raise = [&](float most) {
         if (most > top) { s *= exp_below(top, most); top = most; }
-        const float off = top == -INFINITY ? 0.f : top;
-        float sum = 0.f;
-        for (uint32_t e = 0; e < count; ++e) sum += exp_below(v[e], off);
-        s += sum;
+        return top == -INFINITY ? 0.f : top;
     };
     constexpr uint32_t kAhead = 4;
-    for (uint32_t i = t; i < pieces; i += kLongThreads * kAhead) {
+    for (uint32_t i = t; i < pieces; i += THREADS * kAhead) {
         Sixteen<T> v[kAhead];
 #pragma unroll
         for (uint32_t k = 0; k < kAhead; ++k)
-            if (i + kLongThreads * k < pieces) v[k].load(x + head + (i + kLongThreads * k) * N);
+            if (i + THREADS * k < pieces) v[k].load(x + head + (i + THREADS * k) * N);
+        Sixteen<T> most = v[0];
+#pragma unroll
+        for (uint32_t k = 1; k < kAhead; ++k)
+            if (i + THREADS * k < pieces) most.larger(v[k]);
+        const float off = raise(most.largest());
 #pragma unroll
         for (uint32_t k = 0; k < kAhead; ++k)
-            if (i + kLongThreads * k < pieces) {
-                float f[N];
-#pragma unroll
-                for (uint32_t e = 0; e < N; ++e) f[e] = to_float(v[k].v[e]);
-                add(f, N);
-            }
+            if (i + THREADS * k < pieces) s += v[k].sum_below(off);
     }
-    for (uint32_t k = t; k < head; k += kLongThreads) { const float f = to_float(x[k]); add(&f, 1u); }
-    for (uint32_t k = behind + t; k < a.n; k += kLongThreads) { const float f = to_float(x[k]); add(&f, 1u); }
-    const float most = over_block<kLongThreads, true>(top, part[0]);
-    s = over_block<kLongThreads, false>(s * exp_below(top, most), part[1]);
+    auto add = [&](float x) { s += exp_below(x, raise(x)); };
+    for (uint32_t k = t; k < head; k += THREADS) add(to_float(x[k]));
+    for (uint32_t k = behind + t; k < a.n; k += THREADS) add(to_float(x[k]));
+    const float most = over_block<THREADS, true>(top, part[0]);
+    s = over_block<THREADS, false>(s * exp_below(top, most), part[1]);
     float all = 0.f, chosen = 0.f;
     if (t == 0u) finish_row(a, row, r, chosen_logit, most, s, &all, &chosen);
     if (!a.gradient) return;
@@ -296,36 +425,36 @@ __global__ void __launch_bounds__(kLongThreads) k_policy_long(const __grid_const
     __syncthreads();
     all = factors[0]; chosen = factors[1];
     const uint32_t action = static_cast<uint32_t>(r.action);
-    for (uint32_t i = t; i < pieces; i += kLongThreads * kAhead) {
+    for (uint32_t i = t; i < pieces; i += THREADS * kAhead) {
         Sixteen<T> v[kAhead];
 #pragma unroll
         for (uint32_t k = 0; k < kAhead; ++k)
-            if (i + kLongThreads * k < pieces) v[k].load(x + head + (i + kLongThreads * k) * N);
+            if (i + THREADS * k < pieces) v[k].load(x + head + (i + THREADS * k) * N);
 #pragma unroll
         for (uint32_t k = 0; k < kAhead; ++k)
-            if (i + kLongThreads * k < pieces) {
-                const uint32_t at = head + (i + kLongThreads * k) * N;
-                Sixteen<T> y;
-#pragma unroll
-                for (uint32_t e = 0; e < N; ++e) y.v[e] = from_float<T>(at + e == action ? chosen : all * exp_below(to_float(v[k].v[e]), most));
-                y.store(g + at);
+            if (i + THREADS * k < pieces) {
+                const uint32_t at = head + (i + THREADS * k) * N;
+                v[k].scale_below(most, all);
+                v[k].store(g + at);
+                if (action >= at && action - at < N) g[action] = from_float<T>(chosen);
             }
     }
-    for (uint32_t k = t; k < head; k += kLongThreads) g[k] = from_float<T>(k == action ? chosen : all * exp_below(to_float(x[k]), most));
-    for (uint32_t k = behind + t; k < a.n; k += kLongThreads) g[k] = from_float<T>(k == action ? chosen : all * exp_below(to_float(x[k]), most));
+    for (uint32_t k = t; k < head; k += THREADS) g[k] = from_float<T>(k == action ? chosen : all * exp_below(to_float(x[k]), most));
+    for (uint32_t k = behind + t; k < a.n; k += THREADS) g[k] = from_float<T>(k == action ? chosen : all * exp_below(to_float(x[k]), most));
 }
 
-// The sum over the rows: always the same parts in the same order.
-__global__ void __launch_bounds__(1024) k_policy_sum(const double* __restrict__ rows, uint64_t n, float* __restrict__ loss)
+// The sum over the rows, always of the same parts in the same order: a block's share of them to parts[block], or, of one block, the loss.
+__global__ void __launch_bounds__(1024) k_policy_sum(const double* __restrict__ rows, uint64_t n, uint64_t share, double* __restrict__ parts, float* __restrict__ loss)
 {
     __shared__ double part[32];
     dep_wait();
     dep_trigger();
+    const uint64_t first = blockIdx.x * share, end = min(first + share, n);
     double s[4] = {};
-    for (uint64_t i = threadIdx.x; i < n; i += 4096u)
+    for (uint64_t i = first + threadIdx.x; i < end; i += 4096u)
 #pragma unroll
         for (uint32_t k = 0; k < 4u; ++k)
-            if (i + 1024u * k < n) s[k] += rows[i + 1024u * k];
+            if (i + 1024u * k < end) s[k] += rows[i + 1024u * k];
     double sum = (s[0] + s[1]) + (s[2] + s[3]);
 #pragma unroll
     for (uint32_t d = 16u; d > 0u; d /= 2u) sum += __shfl_xor_sync(0xffffffffu, sum, d);
@@ -335,9 +464,14 @@ __global__ void __launch_bounds__(1024) k_policy_sum(const double* __restrict__ 
         sum = part[threadIdx.x];
 #pragma unroll
         for (uint32_t d = 16u; d > 0u; d /= 2u) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-        if (threadIdx.x == 0u) *loss = static_cast<float>(sum);
+        if (threadIdx.x == 0u) {
+            if (loss) *loss = static_cast<float>(sum);
+            else parts[blockIdx.x] = sum;
+        }
     }
 }
+// One block up to 8,192 rows, else 256 and one for their parts.
+constexpr uint64_t kOneBlock = 8192, kSumBlocks = 256;
 
 template <typename T>
 int launch_rows(cudaStream_t st, const PolicyArgs& a)
@@ -347,16 +481,26 @@ int launch_rows(cudaStream_t st, const PolicyArgs& a)
     uint32_t threads = 128, per = 1;
     const bool alike = !a.gradient || ((reinterpret_cast<uintptr_t>(a.logits) - reinterpret_cast<uintptr_t>(a.gradient)) % 16u == 0u &&
                                        (a.rows < 2u || (a.ld - a.ld_gradient) * sizeof(T) % 16u == 0u));
-    if (a.n <= 32u) { kernel = k_policy_short<T, 8, 4>; per = 16u; }
-    else if (a.n <= 256u) { kernel = k_policy_short<T, 32, 8>; per = 4u; }
-    else if (!alike) { kernel = k_policy_long<T, false>; threads = kLongThreads; }
-    else if (a.n <= 32u * 4u * N) { kernel = k_policy_row<T, 32, 4>; per = 4u; }
-    else if (a.n <= 128u * 4u * N) kernel = k_policy_row<T, 128, 4>;
-    else if (a.n <= 128u * 8u * N) kernel = k_policy_row<T, 128, 8>;
-    else if (a.n <= 512u * 4u * N) { kernel = k_policy_row<T, 512, 4>; threads = 512u; }
-    else if (a.n <= 512u * 8u * N) { kernel = k_policy_row<T, 512, 8>; threads = 512u; }
-    else if (a.n <= 512u * 16u * N) { kernel = k_policy_row<T, 512, 16>; threads = 512u; }
-    else { kernel = k_policy_long<T, true>; threads = kLongThreads; }
+    const uint32_t pieces = a.n / N;
+    if (a.n <= 32u) { kernel = k_policy_short<T, 8, 4, 8>; per = 128u; }
+    else if (a.n <= 64u) { kernel = k_policy_short<T, 16, 4, 8>; per = 64u; }
+    else if (a.n <= 128u) { kernel = k_policy_short<T, 32, 4, 8>; per = 32u; }
+    else if (a.n <= 256u) { kernel = k_policy_short<T, 32, 8, 4>; per = 16u; }
+    else if (!alike) { kernel = k_policy_long<T, false, 512>; threads = 512u; }
+    else if (pieces <= 64u) { kernel = k_policy_row<T, 2>; threads = 256u; per = 8u; }
+    else if (pieces <= 128u) { kernel = k_policy_row<T, 4>; threads = 256u; per = 8u; }
+    else if (pieces <= 256u) { kernel = k_policy_row<T, 8>; threads = 256u; per = 8u; }
+    else {
+        // 192 bytes a thread, more in rows that a block of 512 has no more threads for; 64 / 128 / 256 / 512 / 1,024 threads, us for half a GB of bf16: rows of 6,000
+        // 186 / 205 / 270, 12,000 224 / 182 / 208, 24,000 235 / 227 / 185 / 223, 48,000 - / - / 223 / 191 / 314, 130,000 - / - / 248 / 230 / 233; fp32, 130,000 - / - / - / 251 / 234.
+        // Few rows are spread over more threads.
+        const uint64_t bytes = static_cast<uint64_t>(a.n) * sizeof(T);
+        threads = 64u;
+        while (threads < 512u && (bytes > 192u * threads || a.rows * threads < 1024u * kSms)) threads *= 2u;
+        if (bytes > (200u << 10)) threads = 1024u;
+        kernel = threads == 64u ? k_policy_long<T, true, 64> : threads == 128u ? k_policy_long<T, true, 128> : threads == 256u ? k_policy_long<T, true, 256>
+               : threads == 512u ? k_policy_long<T, true, 512> : k_policy_long<T, true, 1024>;
+    }
     const uint64_t blocks = (a.rows + per - 1u) / per;
     if (blocks > 0x7FFFFFFFull) return -2;
     return launch_dependent(kernel, dim3(static_cast<uint32_t>(blocks)), dim3(threads), 0, st, a) == cudaSuccess ? 1 : -1;
@@ -372,7 +516,15 @@ int launch_policy_loss(cudaStream_t st, uint32_t type, const PolicyArgs& a)
         if (n < 0) return n;
     }
     if (!a.loss) return n;
-    return launch_dependent(k_policy_sum, dim3(1), dim3(1024), 0, st, a.row_loss, a.rows, a.loss) == cudaSuccess ? n + 1 : -1;
+    const dim3 one(1), threads(1024);
+    if (a.rows <= kOneBlock)
+        return launch_dependent(k_policy_sum, one, threads, 0, st, a.row_loss, a.rows, a.rows, static_cast<double*>(nullptr), a.loss) == cudaSuccess ? n + 1 : -1;
+    double* const parts = a.row_loss + a.rows;
+    const uint64_t share = (a.rows + kSumBlocks - 1u) / kSumBlocks;
+    if (launch_dependent(k_policy_sum, dim3(static_cast<uint32_t>(kSumBlocks)), threads, 0, st, a.row_loss, a.rows, share, parts, static_cast<float*>(nullptr)) != cudaSuccess) return -1;
+    return launch_dependent(k_policy_sum, one, threads, 0, st, parts, kSumBlocks, kSumBlocks, static_cast<double*>(nullptr), a.loss) == cudaSuccess ? n + 2 : -1;
 }
+
+size_t policy_loss_bytes(uint64_t rows) { return static_cast<size_t>((8u * (rows + (rows > kOneBlock ? kSumBlocks : 0u)) + 255u) / 256u * 256u); }
 
 }  // namespace evo

@@ -214,7 +214,7 @@ evo_status evo_grouped_linear_backward(const evo_grouped* forward, const evo_gro
 evo_status evo_policy_loss_bytes(const evo_policy_rows* p, size_t* bytes)
 {
     if (!p || !bytes || p->struct_size != sizeof(evo_policy_rows) || p->rows > kMost) return EVO_ERR_INVALID_ARG;
-    *bytes = p->d_loss ? static_cast<size_t>((8u * p->rows + 255u) / 256u * 256u) : 0u;
+    *bytes = p->d_loss ? policy_loss_bytes(p->rows) : 0u;
     return EVO_OK;
 }
 
@@ -248,6 +248,7 @@ evo_status evo_policy_loss(const evo_policy_rows* p, void* d_workspace, size_t w
     a.weights = p->d_weights; a.logp = p->d_logp; a.loss = p->d_loss; a.row_loss = need ? static_cast<double*>(d_workspace) : nullptr;
     a.rows = p->rows; a.ld = ld; a.ld_gradient = ld_gradient; a.n = p->actions; a.wide = p->actions_64;
     a.clip_low = p->clip_low; a.clip_high = p->clip_high; a.kl = p->kl; a.even = p->rows ? 1.0 / static_cast<double>(p->rows) : 0.0;
+    a.log_low = std::log1p(-p->clip_low); a.log_high = std::log1p(p->clip_high);      // (minus infinity for clip_low 1)
     if (!a.loss && !a.logp && !a.gradient) return EVO_OK;
     return status_of(launch_policy_loss(static_cast<cudaStream_t>(cuda_stream), p->type, a));
 }

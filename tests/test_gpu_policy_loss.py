@@ -2,7 +2,8 @@
 
 Tolerances.  With R the largest distance of a finite logit from the row's maximum, an exponential is off by E = 2^-22 + R (2 2^-24 + 2^-26) of itself (the
 instruction; its argument (x - max) log2 e: the difference's rounding, the product's, log2 e's own), the sum by another (terms of a thread's chain and of the tree) 2^-24; logp by both, D, plus
-R 2^-26.  With G = |A| ratio + kl e^(ref - logp) the factor c is off by D G and a probability by E + D; a number of the gradient is rounded once to fp32 and once to its type."""
+R 2^-26.  With G = |A| ratio + kl e^(ref - logp) the factor c is off by D G, and by 2^-21 G for the functions in fp32 that it is made of (each two units of 2^-23 at most, of
+arguments rounded to fp32, 2^-24 of the largest logarithm l), a probability by E + D; a number of the gradient is rounded once to fp32 and once to its type."""
 import math
 
 import pytest
@@ -34,7 +35,8 @@ def definition(logits, actions, old, adv, ref, weights, clip, kl):
     gradient.scatter_(1, a, (-(w * c) * torch.expm1(lp))[:, None])
     zero = torch.zeros((), dtype=torch.float64, device=logits.device)
     pick = lambda x: torch.where(live, x, zero)
-    return pick(w * loss).sum(), pick((w * loss).abs() + w.abs() * size).sum(), pick(lp), torch.where(live[:, None], gradient, zero), pick(w.abs() * size)
+    reach = torch.maximum((lp - old.double()).abs(), (ref.double() - lp).abs()) if kl else (lp - old.double()).abs()
+    return pick(w * loss).sum(), pick((w * loss).abs() + w.abs() * size).sum(), pick(lp), torch.where(live[:, None], gradient, zero), pick(w.abs() * size), pick(reach)
 
 
 def make(rows, n, dtype, seed=0, masked=0.0, spread=2.0, padded=0.2, wide=True):
@@ -61,21 +63,22 @@ def make(rows, n, dtype, seed=0, masked=0.0, spread=2.0, padded=0.2, wide=True):
 def check(logits, actions, old, adv, ref=None, weights=None, clip=(0.2, 0.3), kl=0.0, **kw):
     given = logits.clone()
     got = policy_loss(logits, actions, old, adv, ref_logp=ref, weights=weights, clip=clip, kl=kl, **kw)
-    loss, size, lp, gradient, g = definition(given, actions, old, adv, ref, weights, clip, kl)
+    loss, size, lp, gradient, g, far = definition(given, actions, old, adv, ref, weights, clip, kl)
     n = given.shape[1]
     x = given.double()
     reach = x.amax(1) - torch.where(x.isfinite(), x, torch.full_like(x, math.inf)).amin(1)
     e = 2.0 ** -22 + reach * 2.25 * 2.0 ** -24
     d = e + reach * 2.0 ** -26 + (min(n, 512) + n / 512 + 16) * 2.0 ** -24
     half = torch.finfo(logits.dtype).eps / 2
+    c = d + 2.0 ** -21 + far * 2.0 ** -24
     assert ((got.logp.double() - lp).abs() <= d + 2.0 ** -24 * (lp.abs() + d)).all()
-    assert abs(float(got.loss) - float(loss)) <= float((d * g).sum()) + 2.0 ** -24 * abs(float(loss)) + 1e-12 * float(size)
+    assert abs(float(got.loss) - float(loss)) <= float((c * g).sum()) + 2.0 ** -24 * abs(float(loss)) + 1e-12 * float(size)
     if got.gradient is not None:
         p = torch.softmax(x, 1)
         hot = torch.zeros_like(p)
         inside = (actions >= 0) & (actions < n)
         hot[inside, actions[inside].long()] = 1.0
-        off = g[:, None] * (d[:, None] * (hot - p).abs() + (e + d)[:, None] * p) + 2.0 ** -23 * gradient.abs()
+        off = g[:, None] * (c[:, None] * (hot - p).abs() + (e + d)[:, None] * p) + 2.0 ** -23 * gradient.abs()
         tiny = torch.finfo(logits.dtype).smallest_normal * torch.finfo(logits.dtype).eps + 2.0 ** -126
         bound = off + half * (gradient.abs() + off) + tiny
         err = (got.gradient.double() - gradient).abs()
