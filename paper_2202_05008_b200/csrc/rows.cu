@@ -196,7 +196,7 @@ __global__ void __launch_bounds__(kThreads) k_combine_backward(const __grid_cons
             dot[i] = 0.f;
         }
         if (w.live)
-#pragma unroll(JU > 4u ? 1 : JU > 2u ? 2 : 4)
+#pragma unroll(JU > 2u ? 2 : 4)
             for (uint32_t c = w.lane * N; c < a.cols; c += lanes * N) {
                 Piece<T, N> x, y[JU];
                 x.load(from + c);
@@ -418,8 +418,8 @@ int launch_combine(cudaStream_t st, uint32_t type, const RowSetArgs& a)
         const Way way = way_of(sizeof(T), a);
         if (way == kAny) return launch(st, k_combine_any<T>, a, lanes_for(a, N, 2u));
         if (way == kShort) return launch(st, k_combine<T, 1, 4, 1>, a, lanes_for(a, 1u, 1u));
-        return a.choices == 1u ? launch(st, k_combine<T, N, 1, 4>, a, lanes_for(a, N, 4u)) : a.choices == 2u ? launch(st, k_combine<T, N, 2, 4>, a, lanes_for(a, N, 4u))
-                               : launch(st, k_combine<T, N, 4, 2>, a, lanes_for(a, N, 2u));
+        return a.choices == 1u ? launch(st, k_combine<T, N, 1, 4>, a, lanes_for(a, N, 8u)) : a.choices == 2u ? launch(st, k_combine<T, N, 2, 4>, a, lanes_for(a, N, 8u))
+                               : launch(st, k_combine<T, N, 4, 2>, a, lanes_for(a, N, 8u));
     });
 }
 int launch_combine_backward(cudaStream_t st, uint32_t type, const RowSetArgs& a)
@@ -430,9 +430,8 @@ int launch_combine_backward(cudaStream_t st, uint32_t type, const RowSetArgs& a)
         const Way way = way_of(sizeof(T), a);
         if (way == kAny) return launch(st, k_combine_backward_any<T>, a, lanes_for(a, N, 2u));
         if (way == kShort) return launch(st, k_combine_backward<T, 1, 4>, a, lanes_for(a, 1u, 1u));
-        auto kernel = a.choices == 1u ? k_combine_backward<T, N, 1> : a.choices == 2u ? k_combine_backward<T, N, 2>
-                    : a.choices <= 4u ? k_combine_backward<T, N, 4> : k_combine_backward<T, N, 8>;
-        return launch(st, kernel, a, lanes_for(a, N, 4u));
+        auto kernel = a.choices == 1u ? k_combine_backward<T, N, 1> : a.choices == 2u ? k_combine_backward<T, N, 2> : k_combine_backward<T, N, 4>;
+        return launch(st, kernel, a, lanes_for(a, N, 8u));
     });
 }
 
