@@ -1,7 +1,7 @@
 // Gradients of the products grouped by member: dx[r] = W_g' dz[r], dW_g = sum_r dz[r] x[r]', db_g = sum_r dz[r]; any type, size, stride and alignment.
 //
 // A group of a population has few rows and weights of its own: dx is bound by the weights' way from memory, dW by its own way there.  k_rows reads
-// a group's weights once for up to 8 rows, which are multiplied in fp32 on the CUDA cores; k_weights makes tiles of 64 outputs x 64 or 128 inputs.  Where there are too few tiles for the
+// a group's weights once for up to 8 rows; k_weights makes tiles of 64 outputs x 64 or 128 inputs.  Where there are too few tiles for the
 // GPU and many rows, the rows are split and the parts added up in a fixed order.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -9,7 +9,9 @@
 #include <cstring>
 #include <type_traits>
 
+#include "async.cuh"
 #include "grouped_gradient.h"
+#include "grouped_mma.cuh"
 
 namespace evo {
 namespace {
@@ -26,23 +28,7 @@ template <typename T> __device__ __forceinline__ T from_float(float x)
     else if constexpr (std::is_same<T, __half>::value) return __float2half_rn(x);
     else return __float2bfloat16_rn(x);
 }
-template <typename T>
-__device__ __forceinline__ float dz_at(const GradientArgs& a, uint64_t row, uint32_t o)
-{
-    const float dy = to_float(static_cast<const T*>(a.dy)[row * a.ld_dy + o]);
-    return dz_of(a, dy, a.f.activation == EVO_ACT_NONE ? 0.f : to_float(static_cast<const T*>(a.f.y)[row * a.f.ld_y + o]));
-}
-
-// Four numbers that lie together, as fp32.
-template <typename T>
-__device__ __forceinline__ void load4(const T* p, float (&v)[4])
-{
-    T raw[4];
-    if constexpr (sizeof(T) == 4) { const uint4 u = __ldg(reinterpret_cast<const uint4*>(p)); memcpy(raw, &u, 16); }
-    else { const uint2 u = __ldg(reinterpret_cast<const uint2*>(p)); memcpy(raw, &u, 8); }
-#pragma unroll
-    for (uint32_t i = 0; i < 4u; ++i) v[i] = to_float(raw[i]);
-}
+// Four numbers that are stored together.
 template <typename T>
 __device__ __forceinline__ void store4(T* p, const float (&v)[4])
 {
@@ -54,93 +40,266 @@ __device__ __forceinline__ void store4(T* p, const float (&v)[4])
 }
 
 // ---- dx ----
-// 4 columns a thread, `wide` threads side by side and the others on other weight rows: their sums are added up at the end.  A thread asks for kAhead rows of
-// weights before it needs the first, and for the first ones before dz is there.
-constexpr uint32_t kRows = 8, kChunk = 256, kThreads = 256, kAhead = 8;
+// Warp-level products: the columns of the weights are the MMA's first operand, 16 bytes of them a lane (a warp has 32 of fp32, 64 of 16 bits), and 8 of a
+// group's rows the second.  A lane takes pieces of eight weight rows into what becomes operand registers; the order of the contracted index is free as
+// long as both operands share it.  fp32 numbers are two tf32 numbers each, dz of 16-bit types is one or two numbers (hi and lo), split once where it is staged in shared memory.
+// The tensor core cuts its sums off, so they are taken out every 64 (fp32) or 128 weight rows and added up in fp32.
+// What counts is that enough weights are under way: where they are aligned, 64 of their rows x 512 bytes are copied to shared memory asynchronously, five blocks an SM.
+// Where there are too few tiles for the GPU a block's warps share one and split the weight rows.
+constexpr uint32_t kRowWarps = 4, kStepK = 32;
 
+template <typename T> struct Tile {
+    static constexpr uint32_t kColumns = 16u / sizeof(T);             // of a lane
+    static constexpr uint32_t kTiles = kColumns / 2u;                 // 16 x 8 products side by side
+    static constexpr uint32_t kWarpColumns = 8u * kColumns;
+    static constexpr uint32_t kAcross = kWarpColumns * kRowWarps;     // 512 bytes
+    static constexpr uint32_t kPitch = sizeof(T) == 4 ? 144u : 160u;  // of a staged row: 16 words modulo 32, so that eight lanes' pieces meet no bank twice
+    static constexpr uint32_t kWeightPitch = kAcross + 32u / sizeof(T);      // of a staged weight row: 8 words modulo 32, the same for lanes of four rows
+    // Piece j of lane (g, q) is weight row `row_of(j)` of a step, and where a lane finds its rows of dz beside each other: the j-th of lane q at place `place_of(row)`.
+    static __device__ __forceinline__ constexpr uint32_t row_of(uint32_t j, uint32_t q) { return sizeof(T) == 4 ? 16u * (j / 4u) + 4u * (j % 4u) + q : 4u * j + q; }
+    static __device__ __forceinline__ constexpr uint32_t place_of(uint32_t row)
+    {
+        return sizeof(T) == 4 ? row / 16u * 16u + row % 4u * 4u + row / 4u % 4u : row / 32u * 32u + row % 4u * 8u + row / 4u % 8u;
+    }
+};
+
+// kStepK weight rows from k on, columns kColumns g ... of those from w on
 template <typename T, bool VEC>
-__global__ void __launch_bounds__(kThreads, 2) k_rows(const __grid_constant__ GradientArgs a, uint32_t wide)
+__device__ __forceinline__ void load_step(const T* w, uint64_t ld, uint32_t k, uint32_t end, uint32_t columns, uint4 (&v)[8])
 {
-    __shared__ __align__(16) float dz[kChunk][kRows];
-    __shared__ __align__(16) float sums[kThreads][4 * kRows];
-    dep_wait();
-    dep_trigger();
-    const GroupedArgs& f = a.f;
-    const uint32_t n_in = f.n_in, n_out = f.n_out, tiles = (n_in + 4u * wide - 1u) / (4u * wide);
-    const uint32_t group = blockIdx.x / tiles, c0 = blockIdx.x % tiles * 4u * wide, tx = threadIdx.x % wide, ty = threadIdx.x / wide, slices = kThreads / wide;
-    uint64_t first, end;
-    group_rows(f, group, &first, &end);
-    const T* const w = static_cast<const T*>(f.w) + group * f.stride_w + c0;
-    for (uint64_t r = first; r < end; r += kRows) {
-        const uint32_t rows = static_cast<uint32_t>(min(static_cast<uint64_t>(kRows), end - r));
-        float sum[4][kRows];
+    const uint32_t g = (threadIdx.x & 31u) >> 2, q = threadIdx.x & 3u;
+    constexpr uint32_t C = Tile<T>::kColumns;
 #pragma unroll
-        for (uint32_t i = 0; i < 4u; ++i)
+    for (uint32_t j = 0; j < 8u; ++j) {
+        const uint32_t row = k + Tile<T>::row_of(j, q);
+        v[j] = make_uint4(0u, 0u, 0u, 0u);
+        if (row >= end) continue;
+        const T* const from = w + static_cast<uint64_t>(row) * ld + C * g;
+        if constexpr (VEC) {
+            if (C * g < columns) v[j] = __ldg(reinterpret_cast<const uint4*>(from));
+        } else {
+            T n[C];
 #pragma unroll
-            for (uint32_t k = 0; k < kRows; ++k) sum[i][k] = 0.f;
-        for (uint32_t o0 = 0; o0 < n_out; o0 += kChunk) {
-            const uint32_t count = min(kChunk, n_out - o0);
-            float v[kAhead][4];
-            auto ask = [&](uint32_t o) {
-#pragma unroll
-                for (uint32_t j = 0; j < kAhead; ++j) {
-                    const uint32_t k = o + j * slices;
-                    const T* const from = w + static_cast<uint64_t>(o0 + k) * f.ld_w;
-                    if constexpr (VEC) {
-                        if (k < count && c0 + 4u * tx < n_in) load4(from + 4u * tx, v[j]);
-                        else v[j][0] = v[j][1] = v[j][2] = v[j][3] = 0.f;
-                    } else {
-#pragma unroll
-                        for (uint32_t i = 0; i < 4u; ++i) v[j][i] = k < count && c0 + tx + wide * i < n_in ? to_float(from[tx + wide * i]) : 0.f;
-                    }
-                }
-            };
-            ask(ty);
-            __syncthreads();
-            const uint32_t padded = (count + 31u) / 32u * 32u;              // (a warp's loads are one row's)
-#pragma unroll 2
-            for (uint32_t i = threadIdx.x; i < padded * kRows; i += kThreads) {
-                const uint32_t o = i % padded, row = i / padded;
-                dz[o][row] = o < count && row < rows ? dz_at<T>(a, r + row, o0 + o) : 0.f;
-            }
-            __syncthreads();
-            for (uint32_t o = ty; o < count; o += slices * kAhead) {
-                if (o != ty) ask(o);
-#pragma unroll
-                for (uint32_t j = 0; j < kAhead; ++j) {
-                    if (o + j * slices >= count) break;
-                    const float4 d0 = *reinterpret_cast<const float4*>(&dz[o + j * slices][0]), d1 = *reinterpret_cast<const float4*>(&dz[o + j * slices][4]);
-                    const float d[kRows] = { d0.x, d0.y, d0.z, d0.w, d1.x, d1.y, d1.z, d1.w };
-#pragma unroll
-                    for (uint32_t i = 0; i < 4u; ++i)
-#pragma unroll
-                        for (uint32_t k = 0; k < kRows; ++k) sum[i][k] = fmaf(v[j][i], d[k], sum[i][k]);
-                }
-            }
-        }
-        // sums[ty][row][column]
-        __syncthreads();
-        float* const flat = &sums[0][0];
-#pragma unroll
-        for (uint32_t k = 0; k < kRows; ++k)
-            if (k < rows) {
-                float* const to = flat + (ty * kRows + k) * 4u * wide;
-                if constexpr (VEC) {
-                    *reinterpret_cast<float4*>(to + 4u * tx) = make_float4(sum[0][k], sum[1][k], sum[2][k], sum[3][k]);
-                } else {
-#pragma unroll
-                    for (uint32_t i = 0; i < 4u; ++i) to[tx + wide * i] = sum[i][k];
-                }
-            }
-        __syncthreads();
-        for (uint32_t i = threadIdx.x; i < rows * 4u * wide; i += kThreads) {
-            const uint32_t c = i % (4u * wide), row = i / (4u * wide);
-            float s = 0.f;
-#pragma unroll 8
-            for (uint32_t y = 0; y < slices; ++y) s += flat[(y * kRows + row) * 4u * wide + c];
-            if (c0 + c < n_in) static_cast<T*>(a.dx)[(r + row) * a.ld_dx + c0 + c] = from_float<T>(s);
+            for (uint32_t i = 0; i < C; ++i) n[i] = C * g + i < columns ? from[i] : from_float<T>(0.f);
+            memcpy(&v[j], n, 16);
         }
     }
+}
+
+// c[tile]: columns (2 tile) and (2 tile + 1) of the lane's, rows 2q and 2q + 1
+template <typename T>
+struct Sums {
+    float c[Tile<T>::kTiles][4], small[std::is_same<T, float>::value ? Tile<T>::kTiles : 1u][4];
+
+    __device__ __forceinline__ void clear()
+    {
+#pragma unroll
+        for (uint32_t m = 0; m < Tile<T>::kTiles; ++m)
+#pragma unroll
+                for (uint32_t i = 0; i < 4u; ++i) {
+                    c[m][i] = 0.f;
+                    if constexpr (std::is_same<T, float>::value) small[m][i] = 0.f;
+                }
+    }
+    // weight rows [k, k + 32) of the chunk that is staged in `hi` and `lo`, added to part and small
+    __device__ __forceinline__ void step(const uint4 (&v)[8], const T* hi, const T* lo, bool two, uint32_t k, float (&part)[Tile<T>::kTiles][4])
+    {
+        const uint32_t g = (threadIdx.x & 31u) >> 2, q = threadIdx.x & 3u;
+        if constexpr (std::is_same<T, float>::value) {
+#pragma unroll
+            for (uint32_t s = 0; s < 2u; ++s) {
+                uint4 bh, bl;
+                {
+                    bh = *reinterpret_cast<const uint4*>(hi + g * Tile<T>::kPitch + k + 16u * s + 4u * q);
+                    bl = *reinterpret_cast<const uint4*>(lo + g * Tile<T>::kPitch + k + 16u * s + 4u * q);
+                }
+#pragma unroll
+                for (uint32_t h = 0; h < 2u; ++h) {          // weight rows 4q + 2h and 4q + 2h + 1
+                    const uint4 x = v[4u * s + 2u * h], y = v[4u * s + 2u * h + 1u];
+                    const uint32_t xs[4] = { x.x, x.y, x.z, x.w }, ys[4] = { y.x, y.y, y.z, y.w };
+#pragma unroll
+                    for (uint32_t m = 0; m < 2u; ++m) {
+                        uint32_t ah[4], al[4];
+                        gm::split(__uint_as_float(xs[2u * m]), ah[0], al[0]);
+                        gm::split(__uint_as_float(xs[2u * m + 1u]), ah[1], al[1]);
+                        gm::split(__uint_as_float(ys[2u * m]), ah[2], al[2]);
+                        gm::split(__uint_as_float(ys[2u * m + 1u]), ah[3], al[3]);
+                        {
+                            const uint32_t h0 = h ? bh.z : bh.x, h1 = h ? bh.w : bh.y, l0 = h ? bl.z : bl.x, l1 = h ? bl.w : bl.y;
+                            gm::mma_tf32(part[m], ah, h0, h1);
+                            gm::mma_tf32(small[m], ah, l0, l1);
+                            gm::mma_tf32(small[m], al, h0, h1);
+                        }
+                    }
+                }
+            }
+        } else {
+            uint4 bh, bl;
+            {
+                bh = *reinterpret_cast<const uint4*>(hi + g * Tile<T>::kPitch + k + 8u * q);
+                if (two) bl = *reinterpret_cast<const uint4*>(lo + g * Tile<T>::kPitch + k + 8u * q);
+            }
+#pragma unroll
+            for (uint32_t h = 0; h < 2u; ++h) {              // weight rows 8q + 4h ... 8q + 4h + 3
+                const uint32_t w[4][4] = { { v[4 * h].x, v[4 * h].y, v[4 * h].z, v[4 * h].w }, { v[4 * h + 1].x, v[4 * h + 1].y, v[4 * h + 1].z, v[4 * h + 1].w },
+                                           { v[4 * h + 2].x, v[4 * h + 2].y, v[4 * h + 2].z, v[4 * h + 2].w }, { v[4 * h + 3].x, v[4 * h + 3].y, v[4 * h + 3].z, v[4 * h + 3].w } };
+#pragma unroll
+                for (uint32_t m = 0; m < 4u; ++m) {
+                    // two rows' numbers of one column beside each other
+                    const uint32_t a[4] = { __byte_perm(w[0][m], w[1][m], 0x5410), __byte_perm(w[0][m], w[1][m], 0x7632), __byte_perm(w[2][m], w[3][m], 0x5410),
+                                            __byte_perm(w[2][m], w[3][m], 0x7632) };
+                    {
+                        gm::mma_16<T>(part[m], a, h ? bh.z : bh.x, h ? bh.w : bh.y);
+                        if (two) gm::mma_16<T>(part[m], a, h ? bl.z : bl.x, h ? bl.w : bl.y);
+                    }
+                }
+            }
+        }
+    }
+};
+
+// Rows [r, r + 8) of the group, as far as `end`.  STAGED: weights by way of shared memory (`stage`); SPLIT: the block's warps share a tile.
+template <typename T, bool VEC, bool STAGED, bool SPLIT>
+__device__ __forceinline__ void rows_tile(const GradientArgs& a, uint32_t group, uint32_t c0, uint64_t r, uint64_t end, T* hi, T* lo, T* stage, float (*share)[16][32])
+{
+    constexpr uint32_t kTiles = Tile<T>::kTiles, kPitch = Tile<T>::kPitch, C = Tile<T>::kColumns, kChunk = STAGED ? 64u : 128u, kThreads = 32u * kRowWarps;
+    const GroupedArgs& f = a.f;
+    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, g = lane >> 2, q = lane & 3u, n_out = f.n_out;
+    const uint32_t rows = static_cast<uint32_t>(min(static_cast<uint64_t>(8u), end - r));
+    const uint32_t mine = c0 + (SPLIT ? 0u : warp * Tile<T>::kWarpColumns), columns = mine < f.n_in ? f.n_in - mine : 0u;
+    const bool two = f.activation == EVO_ACT_TANH, act = f.activation != EVO_ACT_NONE;
+    const T* const w = static_cast<const T*>(f.w) + group * f.stride_w;
+    const uint32_t k0 = SPLIT ? warp * kStepK : 0u;
+    Sums<T> sums;
+    sums.clear();
+    float part[kTiles][4];
+    for (uint32_t o0 = 0; o0 < n_out; o0 += kChunk) {
+        const uint32_t count = min(kChunk, n_out - o0);
+        uint4 v[8];
+        if constexpr (STAGED) {
+            __syncthreads();
+#pragma unroll
+            for (uint32_t i = 0; i < kChunk * 32u / kThreads; ++i) {
+                const uint32_t row = threadIdx.x / 32u + i * (kThreads / 32u), c = threadIdx.x % 32u * C;
+                const bool there = row < count && c0 + c < f.n_in;
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;"
+                             :: "r"(smem_u32(stage + row * Tile<T>::kWeightPitch + c)), "l"(there ? w + static_cast<uint64_t>(o0 + row) * f.ld_w + c0 + c : w), "r"(there ? 16u : 0u)
+                             : "memory");
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        } else {
+            load_step<T, VEC>(w + (columns ? mine : 0u), f.ld_w, o0 + k0, n_out, columns, v);
+        }
+        {
+            // a weight row a thread: all its rows' dy and y are asked for together
+            constexpr uint32_t kEach = 8u * kChunk / kThreads;
+            const uint32_t k = threadIdx.x % kChunk, row0 = threadIdx.x / kChunk * kEach;
+            T dy[kEach], y[kEach];
+#pragma unroll
+            for (uint32_t i = 0; i < kEach; ++i)
+                if (k < count && row0 + i < rows) {
+                    dy[i] = static_cast<const T*>(a.dy)[(r + row0 + i) * a.ld_dy + o0 + k];
+                    if (act) y[i] = static_cast<const T*>(f.y)[(r + row0 + i) * f.ld_y + o0 + k];
+                }
+            if (!STAGED) __syncthreads();
+#pragma unroll
+            for (uint32_t i = 0; i < kEach; ++i) {
+                const float d = k < count && row0 + i < rows ? dz_unit(a, to_float(dy[i]), act ? to_float(y[i]) : 0.f) : 0.f;
+                const uint32_t at = (row0 + i) * kPitch + Tile<T>::place_of(k);
+                if constexpr (std::is_same<T, float>::value) {
+                    uint32_t h, l;
+                    gm::split(d, h, l);
+                    hi[at] = __uint_as_float(h);
+                    lo[at] = __uint_as_float(l);
+                } else {
+                    const T h = from_float<T>(d);
+                    hi[at] = h;
+                    if (two) lo[at] = from_float<T>(isfinite(to_float(h)) ? d - to_float(h) : 0.f);
+                }
+            }
+        }
+        if (STAGED) asm volatile("cp.async.wait_group 0;" ::: "memory");
+        __syncthreads();
+#pragma unroll
+        for (uint32_t n = 0; n < (SPLIT ? 1u : kChunk / kStepK); ++n) {
+            const uint32_t k = k0 + n * kStepK;
+            if (k >= count) break;
+            if (n == 0u || (sizeof(T) == 4 && n % 2u == 0u)) {
+#pragma unroll
+                for (uint32_t m = 0; m < kTiles; ++m)
+#pragma unroll
+                    for (uint32_t i = 0; i < 4u; ++i) {
+                        if (n) sums.c[m][i] += part[m][i];
+                        part[m][i] = 0.f;
+                    }
+            }
+            if constexpr (STAGED) {
+#pragma unroll
+                for (uint32_t j = 0; j < 8u; ++j)
+                    v[j] = *reinterpret_cast<const uint4*>(stage + (k + Tile<T>::row_of(j, q)) * Tile<T>::kWeightPitch + warp * Tile<T>::kWarpColumns + C * g);
+            } else {
+                if (n) load_step<T, VEC>(w + (columns ? mine : 0u), f.ld_w, o0 + k, n_out, columns, v);
+            }
+            sums.step(v, hi, lo, two, k, part);
+        }
+        if (k0 < count)
+#pragma unroll
+            for (uint32_t m = 0; m < kTiles; ++m)
+#pragma unroll
+                for (uint32_t i = 0; i < 4u; ++i) sums.c[m][i] += part[m][i];
+    }
+    if constexpr (std::is_same<T, float>::value)
+#pragma unroll
+        for (uint32_t m = 0; m < kTiles; ++m)
+#pragma unroll
+            for (uint32_t i = 0; i < 4u; ++i) sums.c[m][i] = gm::join(sums.c[m][i], sums.small[m][i]);
+    if (SPLIT) {
+        if (warp)
+#pragma unroll
+            for (uint32_t m = 0; m < kTiles; ++m)
+#pragma unroll
+                for (uint32_t i = 0; i < 4u; ++i) share[warp - 1u][m * 4u + i][lane] = sums.c[m][i];
+        __syncthreads();
+        if (warp == 0)
+#pragma unroll
+            for (uint32_t p = 0; p < kRowWarps - 1u; ++p)
+#pragma unroll
+                for (uint32_t m = 0; m < kTiles; ++m)
+#pragma unroll
+                    for (uint32_t i = 0; i < 4u; ++i) sums.c[m][i] += share[p][m * 4u + i][lane];
+        __syncthreads();
+        if (warp) return;
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < 2u; ++i) {
+        const uint32_t row = 2u * q + i;
+        if (row >= rows) continue;
+        T* const to = static_cast<T*>(a.dx) + (r + row) * a.ld_dx + mine + C * g;
+#pragma unroll
+        for (uint32_t e = 0; e < C; ++e)
+            if (C * g + e < columns) to[e] = from_float<T>(f.scale * sums.c[e / 2u][i + 2u * (e & 1u)]);
+    }
+}
+
+// layers 2: blocks of a first layer take the rows from the ninth on, so that long groups begin early
+template <typename T, bool VEC, bool SPLIT>
+__global__ void __launch_bounds__(32 * kRowWarps, 5) k_rows(const __grid_constant__ GradientArgs a, uint32_t layers)
+{
+    constexpr bool kStaged = VEC && !SPLIT;
+    constexpr uint32_t kWide = SPLIT ? Tile<T>::kWarpColumns : Tile<T>::kAcross;
+    __shared__ __align__(16) T hi[8 * Tile<T>::kPitch], lo[8 * Tile<T>::kPitch], stage[kStaged ? 64u * Tile<T>::kWeightPitch : 8u];
+    __shared__ float share[SPLIT ? kRowWarps - 1 : 1][16][32];
+    dep_begin(a);
+    const uint32_t across = (a.f.n_in + kWide - 1u) / kWide, per_layer = a.f.groups * across, layer = blockIdx.x / per_layer, at = blockIdx.x % per_layer;
+    const uint32_t group = at / across, c0 = at % across * kWide;
+    uint64_t r, end;
+    group_rows(a.f, group, &r, &end);
+    if (layers > 1u) {
+        if (layer == 0u) r += 8u;
+        else end = min(end, r + 8u);
+    }
+    for (; r < end; r += 8u) rows_tile<T, VEC, kStaged, SPLIT>(a, group, c0, r, end, hi, lo, stage, share);
+    dep_end(a);
 }
 
 // ---- dW and db ----
@@ -153,13 +312,12 @@ constexpr uint32_t kTile = 64, kStep = 16;                   // outputs of a til
 
 // Tiles of 64 outputs x TI inputs; a thread has 4 inputs (side by side with VEC, where four can be stored together) of TI / 16 outputs.
 template <typename T, uint32_t TI, bool VEC>
-__global__ void __launch_bounds__(256, 3) k_weights(const __grid_constant__ WeightsArgs p)
+__global__ void __launch_bounds__(256, 4) k_weights(const __grid_constant__ WeightsArgs p)
 {
     constexpr uint32_t kAcross = TI / 4u, kEach = TI / 16u;
     __shared__ __align__(16) float dz[kStep][kTile], xs[kStep][TI];
-    dep_wait();
-    dep_trigger();
     const GradientArgs& a = p.a;
+    dep_begin(a);
     const uint32_t n_in = a.f.n_in, n_out = a.f.n_out;
     uint32_t at = blockIdx.x;
     const uint32_t i0 = at % p.in_tiles * TI; at /= p.in_tiles;
@@ -171,30 +329,48 @@ __global__ void __launch_bounds__(256, 3) k_weights(const __grid_constant__ Weig
     const bool bias = a.db && i0 == 0u && threadIdx.x < kTile;
     float sum[kEach][4] = {}, sum_b = 0.f;
     for (; r < end; r += kStep) {
-        float d[4], x[TI / 16u];
+        const uint32_t rows = end - r < kStep ? static_cast<uint32_t>(end - r) : kStep;
+        // Rows are asked for, and put where the block's threads find them, 4 D at a time: no more than there are (with four of them, most of the instructions are
+        // those of the other twelve).
+        auto stage = [&](auto fours) {
+            constexpr uint32_t D = decltype(fours)::value;
+            T dy[D], y[D], x[D * TI / 64u];
+            const uint32_t o = o0 + threadIdx.x % kTile, i = i0 + threadIdx.x % TI;
 #pragma unroll
-        for (uint32_t k = 0; k < 4u; ++k) {
-            const uint32_t row = threadIdx.x / kTile + 4u * k, o = o0 + threadIdx.x % kTile;
-            d[k] = r + row < end && o < n_out ? dz_at<T>(a, r + row, o) : 0.f;
-        }
+            for (uint32_t k = 0; k < D; ++k) {
+                const uint32_t row = threadIdx.x / kTile + 4u * k;
+                if (row < rows && o < n_out) {
+                    dy[k] = static_cast<const T*>(a.dy)[(r + row) * a.ld_dy + o];
+                    if (a.f.activation != EVO_ACT_NONE) y[k] = static_cast<const T*>(a.f.y)[(r + row) * a.f.ld_y + o];
+                }
+            }
 #pragma unroll
-        for (uint32_t k = 0; k < TI / 16u; ++k) {
-            const uint32_t row = threadIdx.x / TI + 256u / TI * k, i = i0 + threadIdx.x % TI;
-            x[k] = r + row < end && i < n_in ? to_float(static_cast<const T*>(a.f.x)[(r + row) * a.f.ld_x + i]) : 0.f;
-        }
-        __syncthreads();
+            for (uint32_t k = 0; k < D * TI / 64u; ++k) {
+                const uint32_t row = threadIdx.x / TI + 256u / TI * k;
+                if (row < rows && i < n_in) x[k] = static_cast<const T*>(a.f.x)[(r + row) * a.f.ld_x + i];
+            }
+            __syncthreads();
 #pragma unroll
-        for (uint32_t k = 0; k < 4u; ++k) dz[threadIdx.x / kTile + 4u * k][threadIdx.x % kTile] = d[k];
+            for (uint32_t k = 0; k < D; ++k) {
+                const uint32_t row = threadIdx.x / kTile + 4u * k;
+                dz[row][threadIdx.x % kTile] = row < rows && o < n_out ? dz_of(a, to_float(dy[k]), a.f.activation == EVO_ACT_NONE ? 0.f : to_float(y[k])) : 0.f;
+            }
 #pragma unroll
-        for (uint32_t k = 0; k < TI / 16u; ++k) xs[threadIdx.x / TI + 256u / TI * k][threadIdx.x % TI] = x[k];
-        __syncthreads();
+            for (uint32_t k = 0; k < D * TI / 64u; ++k) {
+                const uint32_t row = threadIdx.x / TI + 256u / TI * k;
+                xs[row][threadIdx.x % TI] = row < rows && i < n_in ? to_float(x[k]) : 0.f;
+            }
+            __syncthreads();
+        };
+        if (rows <= 4u) stage(std::integral_constant<uint32_t, 1>());
+        else if (rows <= 8u) stage(std::integral_constant<uint32_t, 2>());
+        else stage(std::integral_constant<uint32_t, 4>());
         if (bias) {
             float s = 0.f;
 #pragma unroll
-            for (uint32_t k = 0; k < kStep; ++k) s += dz[k][threadIdx.x];
+            for (uint32_t k = 0; k < kStep; ++k) s += k < rows ? dz[k][threadIdx.x] : 0.f;
             sum_b += s;
         }
-        const uint32_t rows = end - r < kStep ? static_cast<uint32_t>(end - r) : kStep;
 #pragma unroll 4
         for (uint32_t k = 0; k < rows; ++k) {
             float xx[4];
@@ -243,6 +419,7 @@ __global__ void __launch_bounds__(256, 3) k_weights(const __grid_constant__ Weig
             }
         }
     }
+    dep_end(a);
 }
 
 // db alone: 32 threads side by side with N columns each, 8 rows at a time.
@@ -250,14 +427,15 @@ struct BiasArgs {
     GradientArgs a;
     uint32_t all, sets, splits, tiles;
     float* part;
+    const uint16_t* laid;                                    // dz as laid out for the tensor cores, or NULL
+    uint32_t parts, pitch;
 };
 template <typename T, uint32_t N>
 __global__ void __launch_bounds__(256) k_bias(const __grid_constant__ BiasArgs p)
 {
     __shared__ float sums[8][32 * N];
-    dep_wait();
-    dep_trigger();
     const GradientArgs& a = p.a;
+    dep_begin(a);
     uint32_t at = blockIdx.x;
     const uint32_t c0 = at % p.tiles * 32u * N; at /= p.tiles;
     const uint32_t split = at % p.splits, set = at / p.splits;
@@ -266,7 +444,23 @@ __global__ void __launch_bounds__(256) k_bias(const __grid_constant__ BiasArgs p
     const uint32_t c = c0 + threadIdx.x % 32u * N, n_out = a.f.n_out;
     const bool act = a.f.activation != EVO_ACT_NONE;
     float sum[N] = {};
-    if (c < n_out) {
+    if (p.laid) {                                            // dz / scale is there, in parts (N 8: aligned)
+        if (c < n_out)
+#pragma unroll 2
+            for (uint64_t r = first + threadIdx.x / 32u; r < end; r += 8u)
+                for (uint32_t part = 0; part < p.parts; ++part) {
+                    const uint4 u = __ldg(reinterpret_cast<const uint4*>(p.laid + (r * p.parts + part) * p.pitch + c));
+                    const uint32_t w[4] = { u.x, u.y, u.z, u.w };
+#pragma unroll
+                    for (uint32_t e = 0; e < N; ++e) {
+                        const uint16_t bits = static_cast<uint16_t>(w[e / 2u] >> (e % 2u * 16u));
+                        if constexpr (std::is_same<T, __half>::value) sum[e] += __half2float(__ushort_as_half(bits));
+                        else sum[e] += __uint_as_float(static_cast<uint32_t>(bits) << 16);
+                    }
+                }
+#pragma unroll
+        for (uint32_t e = 0; e < N; ++e) sum[e] *= a.f.scale;
+    } else if (c < n_out) {
         constexpr uint32_t kAsk = 4;
         for (uint64_t r = first + threadIdx.x / 32u; r < end; r += 8u * kAsk) {
             T dy[kAsk][N], y[kAsk][N];
@@ -276,7 +470,7 @@ __global__ void __launch_bounds__(256) k_bias(const __grid_constant__ BiasArgs p
                 if (row >= end) break;
                 const T* const from = static_cast<const T*>(a.dy) + row * a.ld_dy + c;
                 const T* const from_y = static_cast<const T*>(a.f.y) + row * a.f.ld_y + c;
-                if constexpr (N == 1u) {
+                if constexpr (N * sizeof(T) != 16u) {
                     dy[k][0] = from[0];
                     if (act) y[k][0] = from_y[0];
                 } else {
@@ -304,6 +498,7 @@ __global__ void __launch_bounds__(256) k_bias(const __grid_constant__ BiasArgs p
         if (p.splits > 1u) p.part[(static_cast<uint64_t>(split) * p.sets + set) * n_out + c0 + i] = s;
         else static_cast<T*>(a.db)[set * a.stride_db + c0 + i] = from_float<T>(s);
     }
+    dep_end(a);
 }
 
 // The splits' parts, added up in their order: rows of `n` numbers, `rows` of them a set.
@@ -367,15 +562,17 @@ template <typename T>
 int launch_rows(cudaStream_t st, const GradientArgs& a)
 {
     const GroupedArgs& f = a.f;
-    uint32_t wide = 8u;                                      // columns of a block: as the row needs, fewer where there are few groups
-    while (wide < 64u && wide * 4u < f.n_in) wide *= 2u;
+    const uint32_t wide = Tile<T>::kWarpColumns, all = Tile<T>::kAcross;
+    // groups that can have rows, and the blocks that they make without splitting the sums
     const uint64_t used = f.rows < f.groups ? f.rows : f.groups;
-    while (wide > 8u && used * ((f.n_in + 4u * wide - 1u) / (4u * wide)) < 2u * kSms) wide /= 2u;
-    const uint64_t blocks = static_cast<uint64_t>(f.groups) * ((f.n_in + 4u * wide - 1u) / (4u * wide));
+    const bool split = used * ((f.n_in + all - 1u) / all) < 4u * kSms && f.n_out > kStepK;
+    // (with two rows a group on average, few have nine, and the blocks that find none cost more)
+    const uint32_t layers = f.rows > 2ull * f.groups ? 2u : 1u;
+    const uint64_t blocks = static_cast<uint64_t>(f.groups) * (split ? (f.n_in + wide - 1u) / wide : (f.n_in + all - 1u) / all) * layers;
     if (blocks > 0x7FFFFFFFull) return -2;
-    const bool aligned = (reinterpret_cast<uintptr_t>(f.w) & (4u * sizeof(T) - 1u)) == 0u && ((f.n_in | f.ld_w | f.stride_w) & 3u) == 0u;
-    auto kernel = aligned ? k_rows<T, true> : k_rows<T, false>;
-    return launch_dependent(kernel, dim3(static_cast<uint32_t>(blocks)), dim3(kThreads), 0, st, a, wide) == cudaSuccess ? 1 : -1;
+    const bool aligned = (reinterpret_cast<uintptr_t>(f.w) & 15u) == 0u && (f.n_in | f.ld_w | f.stride_w) % Tile<T>::kColumns == 0u;
+    auto kernel = aligned ? (split ? k_rows<T, true, true> : k_rows<T, true, false>) : (split ? k_rows<T, false, true> : k_rows<T, false, false>);
+    return launch_dependent(kernel, dim3(static_cast<uint32_t>(blocks)), dim3(32 * kRowWarps), 0, st, a, layers) == cudaSuccess ? 1 : -1;
 }
 
 template <typename T>
@@ -416,16 +613,18 @@ uint32_t bias_columns(const GradientArgs& a)
     return address % 16u == 0u && (a.f.n_out | a.ld_dy | (act ? a.f.ld_y : 0u)) % N == 0u ? N : 1u;
 }
 template <typename T>
-int launch_bias(cudaStream_t st, const GradientArgs& in, uint32_t splits, float* part)
+int launch_bias(cudaStream_t st, const GradientArgs& in, uint32_t splits, float* part, const TcPlan& tc, const void* work)
 {
     BiasArgs p;
     p.a = in;
     p.all = in.sum_b; p.sets = p.all ? 1u : in.f.groups; p.splits = splits; p.part = part;
-    const uint32_t n = bias_columns<T>(in);
+    p.laid = tc.lay_dz ? static_cast<const uint16_t*>(work) : nullptr;      // (the first of the workspace)
+    p.parts = tc.dz_parts; p.pitch = tc.pitch_dz;
+    const uint32_t n = p.laid ? 8u : bias_columns<T>(in);
     p.tiles = (in.f.n_out + 32u * n - 1u) / (32u * n);
     const uint64_t blocks = static_cast<uint64_t>(p.sets) * splits * p.tiles;
     if (blocks > 0x7FFFFFFFull) return -2;
-    auto kernel = n == 1u ? k_bias<T, 1> : k_bias<T, 16u / sizeof(T)>;
+    auto kernel = n == 1u ? k_bias<T, 1> : n == 4u ? k_bias<T, 4> : k_bias<T, 8>;
     return launch_dependent(kernel, dim3(static_cast<uint32_t>(blocks)), dim3(256), 0, st, p) == cudaSuccess ? 1 : -1;
 }
 
@@ -438,23 +637,25 @@ int launch_type(cudaStream_t st, uint32_t type, const GradientArgs& a, void* wor
     float* const part_b = reinterpret_cast<float*>(at + plan.tc_bytes + plan.w_bytes);
     const uint32_t w_sets = a.sum_w ? 1u : a.f.groups, b_sets = a.sum_b ? 1u : a.f.groups;
     int launches = 0, n = 0;
+    // (the first kernel waits at its beginning)
+    auto late = [&](GradientArgs b) { b.late = launches > 0; return b; };
     if (plan.tc.dx || plan.tc.dw) {
         n = launch_grouped_gradient_tc(st, type, a, plan.tc, plan.w_splits, part_w, work);
         if (n < 0) return n;
         launches += n;
     }
     if (a.dx && a.f.rows && !plan.tc.dx) {
-        n = launch_rows<T>(st, a);
+        n = launch_rows<T>(st, late(a));
         if (n < 0) return n;
         launches += n;
     }
     if (a.dw && !plan.tc.dw) {
-        n = launch_weights<T>(st, a, plan.both, plan.w_splits, part_w, part_b);
+        n = launch_weights<T>(st, late(a), plan.both, plan.w_splits, part_w, part_b);
         if (n < 0) return n;
         launches += n;
     }
     if (a.db && !plan.both) {
-        n = launch_bias<T>(st, a, plan.b_splits, part_b);
+        n = launch_bias<T>(st, late(a), plan.b_splits, part_b, plan.tc, work);
         if (n < 0) return n;
         launches += n;
     }

@@ -10,7 +10,20 @@ struct GradientArgs {
     uint64_t ld_dy, ld_dx, ld_dw, stride_dw, stride_db;
     uint32_t sum_w, sum_b;               // one gradient for all groups together
     float inverse;                       // 1 / scale
+    uint32_t late;                       // see dep_begin
 };
+
+// dx, dW and db have nothing in common: a kernel that follows one of the others (which has waited for what both read before it let this one start) waits for it at its own
+// end only, so that it fills the SMs that the one before leaves.
+__device__ __forceinline__ void dep_begin(const GradientArgs& a)
+{
+    if (!a.late) dep_wait();
+    dep_trigger();
+}
+__device__ __forceinline__ void dep_end(const GradientArgs& a)
+{
+    if (a.late) dep_wait();
+}
 
 // dz = dy scale act'(z), from y = scale act(z).  scale - y is exact close to the ends of tanh.
 __device__ __forceinline__ float dz_of(const GradientArgs& a, float dy, float y)

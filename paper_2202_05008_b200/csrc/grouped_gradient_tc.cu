@@ -82,8 +82,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_weights_tc(const __grid_constan
         limit = 31u;
         abort_flag = 0;
     }
-    dep_wait();
-    dep_trigger();
+    dep_begin(p.a);
     if (warp == 1) tmem_alloc(smem_u32(&slot), 512);
     tc_fence_before();
     __syncthreads();
@@ -362,32 +361,43 @@ __global__ void __launch_bounds__(kThreads, 1) k_weights_tc(const __grid_constan
         tc_fence_after();
         tmem_dealloc(tmem, 512);
     }
+    dep_end(p.a);
 }
 
-// dz / scale of every row, in parts `pitch` apart that are filled up with zeros; a warp a row.
+// dz / scale of every row, in parts `pitch` apart that are filled up with zeros; 256 columns of a row a warp.
 template <typename T, uint32_t PARTS>
 __global__ void __launch_bounds__(256) k_lay_dz(const __grid_constant__ GradientArgs a, uint16_t* __restrict__ to, uint32_t pitch)
 {
     dep_wait();
     dep_trigger();
-    const uint64_t row = static_cast<uint64_t>(blockIdx.x) * 8u + (threadIdx.x >> 5);
+    const uint32_t across = (pitch + 255u) / 256u, at = blockIdx.x * 8u + (threadIdx.x >> 5), first = at % across * 256u + (threadIdx.x & 31u);
+    const uint64_t row = at / across;
     if (row >= a.f.rows) return;
     const T* const dy = static_cast<const T*>(a.dy) + row * a.ld_dy;
     const T* const y = static_cast<const T*>(a.f.y) + row * a.f.ld_y;
     const bool act = a.f.activation != EVO_ACT_NONE;
     uint16_t* const dst = to + row * PARTS * pitch;
-#pragma unroll 4
-    for (uint32_t k = threadIdx.x & 31u; k < pitch; k += 32u) {
+    T d[8], z[8];
+#pragma unroll
+    for (uint32_t i = 0; i < 8u; ++i)
+        if (first + 32u * i < a.f.n_out) {
+            d[i] = dy[first + 32u * i];
+            if (act) z[i] = y[first + 32u * i];
+        }
+#pragma unroll
+    for (uint32_t i = 0; i < 8u; ++i) {
+        const uint32_t k = first + 32u * i;
+        if (k >= pitch) break;
         const bool live = k < a.f.n_out;
         if constexpr (std::is_same<T, float>::value) {
-            three_parts(live ? dz_unit(a, dy[k], act ? y[k] : 0.f) : 0.f, dst + k, dst + pitch + k, dst + 2u * pitch + k);
+            three_parts(live ? dz_unit(a, d[i], act ? z[i] : 0.f) : 0.f, dst + k, dst + pitch + k, dst + 2u * pitch + k);
         } else {
             auto number = [](T x) { if constexpr (std::is_same<T, __half>::value) return __half2float(x); else return __bfloat162float(x); };
             auto rounded = [](float x) { if constexpr (std::is_same<T, __half>::value) return __float2half_rn(x); else return __float2bfloat16_rn(x); };
-            const float x = live ? dz_unit(a, number(dy[k]), act ? number(y[k]) : 0.f) : 0.f;
-            const T first = rounded(x);
-            reinterpret_cast<T*>(dst)[k] = first;
-            if constexpr (PARTS == 2u) reinterpret_cast<T*>(dst)[pitch + k] = rounded(isfinite(number(first)) ? x - number(first) : 0.f);      // (an infinity has no second part)
+            const float x = live ? dz_unit(a, number(d[i]), act ? number(z[i]) : 0.f) : 0.f;
+            const T whole = rounded(x);
+            reinterpret_cast<T*>(dst)[k] = whole;
+            if constexpr (PARTS == 2u) reinterpret_cast<T*>(dst)[pitch + k] = rounded(isfinite(number(whole)) ? x - number(whole) : 0.f);      // (an infinity has no second part)
         }
     }
 }
@@ -428,8 +438,8 @@ int launch_grouped_gradient_tc(cudaStream_t st, uint32_t type, const GradientArg
     const void* dz = a.dy; const void* x = f.x; const void* w = f.w;
     uint64_t ld_dz = a.ld_dy, span_dz = f.n_out, ld_x = f.ld_x, span_x = f.n_in, ld_w = f.ld_w, span_w = f.n_in, stride_w = f.stride_w;
     if (plan.lay_dz) {
-        const uint64_t blocks = (f.rows + 7u) / 8u;
-        if (blocks > 0x7FFFFFFFull) return -2;
+        const uint64_t blocks = (f.rows * ((plan.pitch_dz + 255u) / 256u) + 7u) / 8u;
+        if (blocks > 0x0FFFFFFFull) return -2;               // (warps are numbered with 32 bits)
         uint16_t* const to = reinterpret_cast<uint16_t*>(at);
         at += plan.dz_bytes;
         auto kernel = fp32 ? k_lay_dz<float, 3> : type == EVO_F16 ? (plan.dz_parts == 2u ? k_lay_dz<__half, 2> : k_lay_dz<__half, 1>)
@@ -470,6 +480,7 @@ int launch_grouped_gradient_tc(cudaStream_t st, uint32_t type, const GradientArg
     if (!encode) return -1;
     DwArgs p;
     p.a = a;
+    p.a.late = plan.dx;                                      // (what is laid out is behind dx's kernel)
     p.all = a.sum_w; p.sets = a.sum_w ? 1u : f.groups; p.splits = splits;
     p.out_tiles = (f.n_out + 127u) / 128u;
     p.in_tiles = (f.n_in + kMostColumns - 1u) / kMostColumns;

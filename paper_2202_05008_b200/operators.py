@@ -274,6 +274,13 @@ def _pairs(x: torch.Tensor, dtype: torch.dtype, device: torch.device, shape=None
         (shape is None or x.shape == shape)
 
 
+@lru_cache(maxsize=1024)
+def _route_bytes(groups: int, choices: int, rows: int) -> int:
+    need, p = C.c_size_t(), RoutePairs(C.sizeof(RoutePairs), groups, choices, 0, rows, None, choices)
+    _check(load_library().evo_route_rows_bytes(C.byref(p), C.byref(need)), "route_rows")
+    return need.value
+
+
 def route_rows(members: torch.Tensor, groups: int, *, stream: Optional[torch.cuda.Stream] = None) -> Routes:
     """``evo_route_rows``: the stable order by member of the pairs of ``members`` ([rows] or [rows, choices], int32 or int64).  Numbers outside
     [0, groups) are no member: padded rows, choices that were dropped."""
@@ -288,10 +295,9 @@ def route_rows(members: torch.Tensor, groups: int, *, stream: Optional[torch.cud
                         torch.empty(members.shape, dtype=torch.int32, device=device))
         p = RoutePairs(C.sizeof(RoutePairs), groups, choices, 1 if members.dtype == torch.int64 else 0, members.shape[0], members.data_ptr(),
                        members.stride(0), *(x.data_ptr() for x in routes))
-        need = C.c_size_t()
-        _check(lib.evo_route_rows_bytes(C.byref(p), C.byref(need)), where)
-        work = torch.empty(need.value, dtype=torch.uint8, device=device) if need.value else None
-        code = lib.evo_route_rows(C.byref(p), None if work is None else work.data_ptr(), need.value, st)
+        need = _route_bytes(groups, choices, members.shape[0])
+        work = torch.empty(need, dtype=torch.uint8, device=device) if need else None
+        code = lib.evo_route_rows(C.byref(p), None if work is None else work.data_ptr(), need, st)
     _check(code, where)
     return routes
 
@@ -420,6 +426,14 @@ class PolicyLoss(NamedTuple):
     gradient: Optional[torch.Tensor]
 
 
+@lru_cache(maxsize=1024)
+def _policy_bytes(rows: int) -> int:
+    need, p = C.c_size_t(), PolicyRows(C.sizeof(PolicyRows), 0, 1, 0, rows)
+    p.d_loss = 4
+    _check(load_library().evo_policy_loss_bytes(C.byref(p), C.byref(need)), "policy_loss")
+    return need.value
+
+
 def policy_loss(logits: torch.Tensor, actions: torch.Tensor, old_logp: torch.Tensor, advantage: torch.Tensor, *, ref_logp: Optional[torch.Tensor] = None,
                 weights: Optional[torch.Tensor] = None, clip: Tuple[float, float] = (0.2, 0.2), kl: float = 0.0, gradient: bool = True,
                 out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> PolicyLoss:
@@ -448,9 +462,8 @@ def policy_loss(logits: torch.Tensor, actions: torch.Tensor, old_logp: torch.Ten
                        None if ref_logp is None else ref_logp.data_ptr(), None if weights is None else weights.data_ptr(), loss.data_ptr(), logp.data_ptr())
         if d_logits is not None:
             p.d_gradient, p.ld_gradient = d_logits.data_ptr(), d_logits.stride(0)
-        need = C.c_size_t()
-        _check(lib.evo_policy_loss_bytes(C.byref(p), C.byref(need)), where)
-        work = torch.empty(need.value, dtype=torch.uint8, device=device) if need.value else None
-        code = lib.evo_policy_loss(C.byref(p), None if work is None else work.data_ptr(), need.value, st)
+        need = _policy_bytes(rows)
+        work = torch.empty(need, dtype=torch.uint8, device=device) if need else None
+        code = lib.evo_policy_loss(C.byref(p), None if work is None else work.data_ptr(), need, st)
     _check(code, where)
     return PolicyLoss(loss, logp, d_logits)
