@@ -6,6 +6,7 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <cmath>
 #include <cstring>
 #include <type_traits>
 
@@ -526,13 +527,43 @@ uint32_t splits_for(const GradientArgs& a, bool all, uint64_t tiles)
     const uint64_t most = 2u * kSms / blocks, want = rows / 128u;
     return static_cast<uint32_t>(want < 2u ? 1u : want < most ? want : most);
 }
+// 16-bit rows that are whole pieces of 16 bytes (the same wherever the arrays lie: workspaces are planned before they do)
+bool whole_pieces(const GradientArgs& a) { return ((a.f.n_in | a.f.n_out) & 7u) == 0u; }
+// Whether tcgen05 pays for dx: rows a group from which it does.  fp32 weights, and those that TMA cannot address, are laid out first, whatever the rows; the walk over many
+// groups takes a warp longer than the products; few tiles of few rows leave SMs without one, but a block of k_rows takes long weight columns one piece after the
+// other.  us, tcgen05 / k_rows, rows a group in brackets:
+//   fp32     200 groups of 256 -> 256 (16) 62.7 / 41.0, (32) 63.9 / 83.9; 32 of 1,024 -> 1,024 (16) 140 / 120, (32) 140 / 236; 1 of 4,096 -> 4,096 (32) 172 / 127, (64) 176 / 289;
+//            1,000 of 64 -> 64 (32) 64 / 45, (64) 75 / 87; 3,000 of 20 -> 30 (64) 171 / 127
+//   16 bits  200 of 256 -> 256 (2) 13.1 / 11.1, (8) 13.2 / 20.1; 1,000 of 64 -> 64 (16) 26.5 / 21.7, (32) 27.7 / 42; 32 of 1,024 -> 1,024 (2) 16.8 / 24.3;
+//            not aligned: 300 of 207 -> 379 (8) 60.8 / 60.0, (16) 62.7 / 120; 3,000 of 20 -> 30 (32) 102 / 92, 10 of 18 -> 2,204 with 3 rows in all 21.4 / 53.5
+// Over 225 shapes (120 of them drawn) the choice takes 1.02 times the faster side's time in the geometric mean; tcgen05 always 1.7 times, k_rows always 2.3.
 bool dx_on_tensor_cores(uint32_t type, const GradientArgs& a)
 {
-    return a.f.rows < (1ull << 31) && static_cast<uint64_t>(a.f.groups) * a.f.n_out < (1ull << 31) && a.f.rows >= 24ull * a.f.groups;
+    const GroupedArgs& f = a.f;
+    if (f.rows >= (1ull << 31) || static_cast<uint64_t>(f.groups) * f.n_out >= (1ull << 31)) return false;
+    const double groups = f.groups, tiles = std::fmin(groups, static_cast<double>(f.rows)) * ((f.n_in + 127u) / 128u), idle = std::fmax(0.0, 1.0 - tiles / kSms);
+    const double size = static_cast<double>(f.n_in) * f.n_out;
+    double least;
+    if (type == EVO_F32) least = 16.0 + groups / 45.0 + 24.0 * idle * idle * std::fmin(1.0, size / 1e6);
+    else if (whole_pieces(a)) least = groups / 50.0;
+    else least = idle > 0.1 && f.n_out >= 700u && f.groups <= 64u ? 0.0 : 4.0 + groups / 100.0;
+    return static_cast<double>(f.rows) >= least * groups;
 }
+// The same for dW.  A tile is 128 outputs x up to 256 inputs, however many there are; where there are few tiles k_weights takes long groups 16 rows at a time.  tcgen05 / k_weights:
+//   fp32     200 of 256 -> 256 (8) 29.5 / 20.6, (16) 31.0 / 33.1; 32 of 1,024 -> 1,024 (16) 58.7 / 62.6; 1 of 4,096 -> 4,096 (16) 36.5 / 27.8, (32) 40.2 / 45.4;
+//            1,000 of 64 -> 64 (64) 74 / 46; 7 of 171 -> 7 (107) 20.8 / 47.4
+//   16 bits  200 of 256 -> 256 (2) 10.0 / 10.9; 1,000 of 64 -> 64 (8) 17.3 / 9.7, (16) 12.0 / 15.4, (32) 13.1 / 26.4; 4 of 2,048 -> 2,048 (2) 17.6 / 11.1, (8) 17.5 / 19.5;
+//            not aligned: 300 of 207 -> 379 (8) 32.6 / 40.5; 3,000 of 20 -> 30 (32) 71 / 51, (64) 112 / 92
+// Over the same shapes 1.01 times the faster side's time; tcgen05 always 1.6 times, k_weights always 1.4.
 bool dw_on_tensor_cores(uint32_t type, const GradientArgs& a)
 {
-    return a.f.rows < (1ull << 31) && a.f.rows >= 24ull * (a.sum_w ? 1u : a.f.groups);
+    const GroupedArgs& f = a.f;
+    if (f.rows >= (1ull << 31)) return false;
+    const double sets = a.sum_w ? 1.0 : f.groups, tiles = static_cast<double>((f.n_out + 127u) / 128u) * ((f.n_in + 255u) / 256u);
+    const double waste = tiles * 32768.0 / (static_cast<double>(f.n_in) * f.n_out);
+    double least = type == EVO_F32 ? 18.0 * std::fmin(std::fmax(0.5 * waste, 1.0), 12.0) : (whole_pieces(a) ? 2.0 : 6.0) + 2.0 * std::fmin(waste, 12.0);
+    if (tiles * sets < kSms) least = std::fmin(least, 48.0);
+    return static_cast<double>(f.rows) >= least * sets;
 }
 uint32_t inputs_of_a_tile(const GradientArgs& a) { return a.f.n_in <= 64u ? 64u : 128u; }
 struct Plan {

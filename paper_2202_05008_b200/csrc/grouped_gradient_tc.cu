@@ -297,51 +297,93 @@ __global__ void __launch_bounds__(kThreads, 1) k_weights_tc(const __grid_constan
                     __syncwarp();
                     const uint32_t column = t.i0 + c;
                     if (p.pieces) {                          // eight lanes a row, four rows at a time
-                        const uint32_t k = column + (lane & 7u) * 4u;
+                        const uint32_t k = column + (lane & 7u) * 4u, row = o0 + (lane >> 3), outputs = row < n_out && k < n_in ? n_out - row : 0u;
+                        float4 v[8];
 #pragma unroll
-                        for (uint32_t i = 0; i < 8u; ++i) {
-                            const uint32_t r = i * 4u + (lane >> 3), o = o0 + r;
-                            float4 v;
-                            asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
-                                         : "r"(staging + r * 128u + ((lane ^ r) & 7u) * 16u) : "memory");
-                            if (o >= n_out || k >= n_in) continue;
-                            if (sums) {
-                                float4* const s = reinterpret_cast<float4*>(sums + o * ld_sums + k);
-                                if (first) { const float4 w = *s; v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w; }
-                                if (!last) { *s = v; continue; }
+                        for (uint32_t i = 0; i < 8u; ++i)
+                            asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[i].x), "=f"(v[i].y), "=f"(v[i].z), "=f"(v[i].w)
+                                         : "r"(staging + (i * 4u + (lane >> 3)) * 128u + ((lane ^ (i * 4u + (lane >> 3))) & 7u) * 16u));
+                        if (sums) {
+                            float* const sum_at = sums + row * ld_sums + k;
+                            if (first) {
+                                float4 w[8];
+#pragma unroll
+                                for (uint32_t i = 0; i < 8u; ++i)
+                                    if (4u * i < outputs) w[i] = *reinterpret_cast<const float4*>(sum_at + 4u * i * ld_sums);
+#pragma unroll
+                                for (uint32_t i = 0; i < 8u; ++i)
+                                    if (4u * i < outputs) { v[i].x += w[i].x; v[i].y += w[i].y; v[i].z += w[i].z; v[i].w += w[i].w; }
                             }
-                            v.x *= scale; v.y *= scale; v.z *= scale; v.w *= scale;
-                            if (kFloat || p.splits > 1u) {
-                                *reinterpret_cast<float4*>((p.splits > 1u ? sums : reinterpret_cast<float*>(to)) + o * (p.splits > 1u ? ld_sums : p.a.ld_dw) + k) = v;
-                            } else {
-                                uint2 w;
-                                if constexpr (std::is_same<O, __half>::value) {
-                                    const __half2 a = __floats2half2_rn(v.x, v.y), b = __floats2half2_rn(v.z, v.w);
-                                    w = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
-                                } else {
-                                    w = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
-                                }
-                                *reinterpret_cast<uint2*>(to + o * p.a.ld_dw + k) = w;
+                            if (!last || p.splits > 1u) {
+                                const float factor = last ? scale : 1.f;
+#pragma unroll
+                                for (uint32_t i = 0; i < 8u; ++i)
+                                    if (4u * i < outputs)
+                                        *reinterpret_cast<float4*>(sum_at + 4u * i * ld_sums) = make_float4(factor * v[i].x, factor * v[i].y, factor * v[i].z, factor * v[i].w);
+                                continue;
                             }
                         }
-                    } else {                                 // a number a lane, row by row
-                        const uint32_t k = column + lane;
-#pragma unroll 8
-                        for (uint32_t r = 0; r < 32u; ++r) {
-                            const uint32_t o = o0 + r;
-                            float v;
-                            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(staging + r * 128u + ((lane >> 2 ^ r) & 7u) * 16u + (lane & 3u) * 4u) : "memory");
-                            if (o >= n_out || k >= n_in) continue;
-                            if (sums) {
-                                float* const s = sums + o * ld_sums + k;
-                                if (first) v += *s;
-                                if (!last) { *s = v; continue; }
+                        O* at = to + row * p.a.ld_dw + k;
+#pragma unroll
+                        for (uint32_t i = 0; i < 8u; ++i) {
+                            if (4u * i < outputs) {
+                                const float4 x = make_float4(scale * v[i].x, scale * v[i].y, scale * v[i].z, scale * v[i].w);
+                                if constexpr (kFloat) {
+                                    *reinterpret_cast<float4*>(at) = x;
+                                } else if constexpr (std::is_same<O, __half>::value) {
+                                    const __half2 a = __floats2half2_rn(x.x, x.y), b = __floats2half2_rn(x.z, x.w);
+                                    *reinterpret_cast<uint2*>(at) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+                                } else {
+                                    *reinterpret_cast<uint2*>(at) = make_uint2(pack_bf16(x.x, x.y), pack_bf16(x.z, x.w));
+                                }
                             }
-                            v *= scale;
-                            if (p.splits > 1u) sums[o * ld_sums + k] = v;
-                            else if constexpr (kFloat) to[o * p.a.ld_dw + k] = v;
-                            else if constexpr (std::is_same<O, __half>::value) to[o * p.a.ld_dw + k] = __float2half_rn(v);
-                            else to[o * p.a.ld_dw + k] = __float2bfloat16_rn(v);
+                            at += 4u * p.a.ld_dw;
+                        }
+                    } else {                                 // a number a lane, row by row, eight rows on their way together
+                        const uint32_t k = column + lane;
+                        const bool live = k < n_in;
+                        const uint32_t outputs = o0 < n_out && live ? min(32u, n_out - o0) : 0u;
+                        auto number = [&](uint32_t r) {
+                            float v;
+                            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(staging + r * 128u + ((lane >> 2 ^ r) & 7u) * 16u + (lane & 3u) * 4u));
+                            return v;
+                        };
+                        if (!sums || (kFloat && p.splits == 1u && first == 0u && last)) {
+                            const float factor = scale;
+                            O* at = to + o0 * p.a.ld_dw + k;
+                            for (uint32_t r0 = 0; r0 < 32u; r0 += 8u) {
+                                float v[8];
+#pragma unroll
+                                for (uint32_t i = 0; i < 8u; ++i) v[i] = factor * number(r0 + i);
+#pragma unroll
+                                for (uint32_t i = 0; i < 8u; ++i) {
+                                    if (r0 + i < outputs) {
+                                        if constexpr (kFloat) *at = v[i];
+                                        else if constexpr (std::is_same<O, __half>::value) *at = __float2half_rn(v[i]);
+                                        else *at = __float2bfloat16_rn(v[i]);
+                                    }
+                                    at += p.a.ld_dw;
+                                }
+                            }
+                        } else {
+                            float* sum_at = sums + o0 * ld_sums + k;
+                            for (uint32_t r0 = 0; r0 < 32u; r0 += 8u) {
+                                float v[8];
+#pragma unroll
+                                for (uint32_t i = 0; i < 8u; ++i) {
+                                    v[i] = number(r0 + i);
+                                    if (first && r0 + i < outputs) v[i] += sum_at[(r0 + i) * ld_sums];
+                                }
+#pragma unroll
+                                for (uint32_t i = 0; i < 8u; ++i) {
+                                    if (r0 + i >= outputs) continue;
+                                    if (!last) sum_at[(r0 + i) * ld_sums] = v[i];
+                                    else if (p.splits > 1u) sum_at[(r0 + i) * ld_sums] = scale * v[i];
+                                    else if constexpr (kFloat) to[(o0 + r0 + i) * p.a.ld_dw + k] = scale * v[i];
+                                    else if constexpr (std::is_same<O, __half>::value) to[(o0 + r0 + i) * p.a.ld_dw + k] = __float2half_rn(scale * v[i]);
+                                    else to[(o0 + r0 + i) * p.a.ld_dw + k] = __float2bfloat16_rn(scale * v[i]);
+                                }
+                            }
                         }
                     }
                 }
