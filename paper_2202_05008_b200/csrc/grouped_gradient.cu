@@ -446,12 +446,17 @@ __global__ void __launch_bounds__(256) k_bias(const __grid_constant__ BiasArgs p
     const bool act = a.f.activation != EVO_ACT_NONE;
     float sum[N] = {};
     if (p.laid) {                                            // dz / scale is there, in parts (N 8: aligned)
+        constexpr uint32_t kAsk = 8;
+        const uint64_t rows = (end > first ? end - first : 0u) * p.parts;               // (the parts of a row lie one behind the other, like rows)
+        const uint16_t* const from = p.laid + first * p.parts * p.pitch + c;
         if (c < n_out)
-#pragma unroll 2
-            for (uint64_t r = first + threadIdx.x / 32u; r < end; r += 8u)
-                for (uint32_t part = 0; part < p.parts; ++part) {
-                    const uint4 u = __ldg(reinterpret_cast<const uint4*>(p.laid + (r * p.parts + part) * p.pitch + c));
-                    const uint32_t w[4] = { u.x, u.y, u.z, u.w };
+            for (uint64_t r = threadIdx.x / 32u; r < rows; r += 8u * kAsk) {
+                uint4 u[kAsk];
+#pragma unroll
+                for (uint32_t k = 0; k < kAsk; ++k) u[k] = r + 8u * k < rows ? __ldg(reinterpret_cast<const uint4*>(from + (r + 8u * k) * p.pitch)) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+                for (uint32_t k = 0; k < kAsk; ++k) {
+                    const uint32_t w[4] = { u[k].x, u[k].y, u[k].z, u[k].w };
 #pragma unroll
                     for (uint32_t e = 0; e < N; ++e) {
                         const uint16_t bits = static_cast<uint16_t>(w[e / 2u] >> (e % 2u * 16u));
@@ -459,10 +464,11 @@ __global__ void __launch_bounds__(256) k_bias(const __grid_constant__ BiasArgs p
                         else sum[e] += __uint_as_float(static_cast<uint32_t>(bits) << 16);
                     }
                 }
+            }
 #pragma unroll
         for (uint32_t e = 0; e < N; ++e) sum[e] *= a.f.scale;
     } else if (c < n_out) {
-        constexpr uint32_t kAsk = 4;
+        constexpr uint32_t kAsk = N == 1u ? 8u : 4u;
         for (uint64_t r = first + threadIdx.x / 32u; r < end; r += 8u * kAsk) {
             T dy[kAsk][N], y[kAsk][N];
 #pragma unroll
@@ -527,6 +533,14 @@ uint32_t splits_for(const GradientArgs& a, bool all, uint64_t tiles)
     const uint64_t most = 2u * kSms / blocks, want = rows / 128u;
     return static_cast<uint32_t>(want < 2u ? 1u : want < most ? want : most);
 }
+// db alone is read in little time, but a block's rows one after the other: no more than 64 rows a split on average, of up to 16, while the GPU has room.
+uint32_t bias_splits(const GradientArgs& a)
+{
+    const uint64_t sets = a.sum_b ? 1u : a.f.groups, blocks = sets * ((a.f.n_out + 255u) / 256u), rows = a.f.rows / sets;
+    uint32_t splits = 1;
+    while (splits < 16u && blocks * splits < 4u * kSms && rows > 64u * splits) splits *= 2u;
+    return splits;
+}
 // 16-bit rows that are whole pieces of 16 bytes (the same wherever the arrays lie: workspaces are planned before they do)
 bool whole_pieces(const GradientArgs& a) { return ((a.f.n_in | a.f.n_out) & 7u) == 0u; }
 // Whether tcgen05 pays for dx: rows a group from which it does.  fp32 weights, and those that TMA cannot address, are laid out first, whatever the rows; the walk over many
@@ -580,7 +594,7 @@ Plan plan_for(uint32_t type, const GradientArgs& a, bool any_address)
     const bool dx = a.dx && a.f.rows && dx_on_tensor_cores(type, a), dw = a.dw && a.f.rows && dw_on_tensor_cores(type, a);
     p.both = a.dw && !dw && a.db && a.sum_w == a.sum_b;
     p.w_splits = !a.dw ? 1u : dw ? splits_for(a, a.sum_w, ((a.f.n_out + 127ull) / 128u) * ((a.f.n_in + 255ull) / 256u)) : splits_for(a, a.sum_w, out_tiles * in_tiles);
-    p.b_splits = p.both ? p.w_splits : a.db ? splits_for(a, a.sum_b, (a.f.n_out + 127u) / 128u) : 1u;
+    p.b_splits = p.both ? p.w_splits : a.db ? bias_splits(a) : 1u;
     p.tc = grouped_gradient_tc_plan(type, a, dx, dw, p.w_splits, any_address);
     const uint64_t w_sets = a.sum_w ? 1u : a.f.groups, b_sets = a.sum_b ? 1u : a.f.groups;
     p.tc_bytes = padded(p.tc.bytes());

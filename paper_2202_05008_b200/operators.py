@@ -187,7 +187,7 @@ def _ragged(offsets: torch.Tensor, groups: int, device: torch.device, where: str
 
 def _out(out: Optional[torch.Tensor], x: torch.Tensor, rows: int, cols: int, where: str) -> torch.Tensor:
     if out is None:
-        return torch.empty((rows, cols), dtype=x.dtype, device=x.device)
+        return x.new_empty((rows, cols))
     _require(_rows(out, x.dtype, x.device) and out.shape == (rows, cols), where, "out does not match")
     return out
 
@@ -291,8 +291,8 @@ def route_rows(members: torch.Tensor, groups: int, *, stream: Optional[torch.cud
     _require(1 <= groups <= 1 << 20 and choices >= 1 and members.numel() < 1 << 31, where, "groups or members")
     with _On(device, stream, where) as st:
         n = members.numel()
-        routes = Routes(torch.empty(groups + 1, dtype=torch.int32, device=device), torch.empty(n, dtype=torch.int32, device=device),
-                        torch.empty(members.shape, dtype=torch.int32, device=device))
+        like = members if members.dtype == torch.int32 else torch.empty(0, dtype=torch.int32, device=device)
+        routes = Routes(like.new_empty(groups + 1), like.new_empty(n), like.new_empty(members.shape))
         p = RoutePairs(C.sizeof(RoutePairs), groups, choices, 1 if members.dtype == torch.int64 else 0, members.shape[0], members.data_ptr(),
                        members.stride(0), *(x.data_ptr() for x in routes))
         need = _route_bytes(groups, choices, members.shape[0])
@@ -357,7 +357,7 @@ def combine_rows_backward(d_out: torch.Tensor, y: torch.Tensor, place: torch.Ten
     _require(_rows(d_out, y.dtype, device) and d_out.shape == (place.shape[0], y.shape[1]), where, "the gradient does not match")
     with _On(device, stream, where) as st:
         dy = _out(out, y, y.shape[0], y.shape[1], where)
-        dw = torch.empty(place.shape, dtype=torch.float32, device=device)
+        dw = weights.new_empty(place.shape)
         p = _row_sets(where, d_out, y, place, weights)
         p.d_sorted_gradient, p.ld_sorted_gradient, p.d_weights_gradient, p.ld_weights_gradient = dy.data_ptr(), dy.stride(0), dw.data_ptr(), dw.stride(0)
         code = lib.evo_combine_rows_backward(C.byref(p), st)
@@ -393,9 +393,9 @@ def grouped_linear_backward(dy: torch.Tensor, x: Optional[torch.Tensor], weight:
         dx = _out(out[0], dy, rows, n_in, where) if wanted[0] else None
         dweight, dbias = out[1] if wanted[1] else None, out[2] if wanted[2] else None
         if wanted[1] and dweight is None:
-            dweight = torch.empty((sets[0], n_out, n_in), dtype=dtype, device=device)
+            dweight = dy.new_empty((sets[0], n_out, n_in))
         if wanted[2] and dbias is None:
-            dbias = torch.empty((sets[1], n_out), dtype=dtype, device=device)
+            dbias = dy.new_empty((sets[1], n_out))
         _require(dweight is None or (dweight.device == device and dweight.dtype == dtype and dweight.shape == (sets[0], n_out, n_in) and
                                      (n_in == 1 or dweight.stride(2) == 1)), where, "the gradient of weight does not match")
         _require(dbias is None or (_rows(dbias, dtype, device) and dbias.shape == (sets[1], n_out)), where, "the gradient of the bias does not match")
@@ -456,7 +456,7 @@ def policy_loss(logits: torch.Tensor, actions: torch.Tensor, old_logp: torch.Ten
     _require(len(clip) == 2 and (out is None or gradient), where, "clip or out")
     with _On(device, stream, where) as st:
         d_logits = _out(out, logits, rows, n, where) if gradient else None
-        loss, logp = torch.empty((), dtype=torch.float32, device=device), torch.empty(rows, dtype=torch.float32, device=device)
+        loss, logp = old_logp.new_empty(()), old_logp.new_empty(rows)
         p = PolicyRows(C.sizeof(PolicyRows), TYPES[logits.dtype], n, 1 if actions.dtype == torch.int64 else 0, rows, clip[0], clip[1], kl,
                        logits.data_ptr(), logits.stride(0), actions.data_ptr(), old_logp.data_ptr(), advantage.data_ptr(),
                        None if ref_logp is None else ref_logp.data_ptr(), None if weights is None else weights.data_ptr(), loss.data_ptr(), logp.data_ptr())

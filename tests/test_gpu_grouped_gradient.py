@@ -214,3 +214,38 @@ def test_refusals():
                  lambda: grouped_linear_backward(dy, x, w, off, wanted=(True, True))):
         with pytest.raises(EvoError):
             call()
+
+
+@pytest.mark.parametrize("dtype,act", [(BF16, "none"), (F16, "tanh"), (F32, "relu")])
+@pytest.mark.parametrize("n_in,n_out", [(264, 136), (20, 24), (130, 61)])
+def test_groups_of_more_rows_than_one_sum_may_have(dtype, act, n_in, n_out):
+    """Numbers of one sign, where what the tensor core cuts off adds up: 20,000 rows in one group, others around it."""
+    dy, x, w, off, y = make(3, [700, 20000, 300], n_in, n_out, dtype, act)
+    dy, x, w = dy.abs() * 0.05, x.abs(), w.abs()
+    check(dy, x, w, off, y, act, 1.0)
+    many = 40                                                    # (as many groups as fill the GPU: no split)
+    dy, x, w, off, y = make(many, [30] * 20 + [17000] + [50] * (many - 21), 264, 264, dtype, act)
+    dy, x, w = dy.abs() * 0.05, x.abs(), w.abs()
+    check(dy, x, w, off, y, act, 1.0)
+
+
+def test_the_same_bits_every_time():
+    for dtype, lengths, n_in, n_out in ((F32, [5, 3, 9] * 60, 72, 136), (BF16, [300, 10, 700], 136, 264), (F16, [4000], 40, 30), (F32, [900, 1300], 130, 70)):
+        args = make(len(lengths), lengths, n_in, n_out, dtype, "tanh")
+        dy, x, w, off, y = args
+        first = [t.clone() for t in grouped_linear_backward(dy, x, w, off, y, activation="tanh")]
+        for _ in range(5):
+            again = grouped_linear_backward(dy, x, w, off, y, activation="tanh")
+            assert all(torch.equal(a, b) for a, b in zip(first, again))
+
+
+def test_a_long_parameter_row_passes_32_bits():
+    """Groups 2^27 numbers apart: the last one's weights and gradients lie beyond 2^31 bytes and, with 17 groups, beyond 2^31 numbers."""
+    groups, pitch, n_in, n_out = 17, 1 << 27, 24, 40
+    room, gradient = torch.empty(groups * pitch, dtype=BF16, device="cuda"), torch.empty(groups * pitch, dtype=BF16, device="cuda")
+    theta, g = room.view(groups, pitch), gradient.view(groups, pitch)
+    dy, x, w, off, _ = make(groups, [3] * (groups - 1) + [60], n_in, n_out, BF16)
+    for at in (theta, g):
+        at[:, :n_in * n_out] = w.flatten(1)
+    weight, dw = theta[:, :n_in * n_out].unflatten(1, (n_out, n_in)), g[:, :n_in * n_out].unflatten(1, (n_out, n_in))
+    check(dy, x, weight, off, out=(None, dw, g[:, n_in * n_out:n_in * n_out + n_out]))
