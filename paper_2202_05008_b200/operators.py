@@ -50,6 +50,7 @@ def _require_no_gradient(where: str, *tensors: Optional[torch.Tensor]) -> None:
 
 
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)      # the handle without a Stream object (2 us)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 class _On:
@@ -65,7 +66,7 @@ class _On:
     def __enter__(self) -> int:
         if self.stream is not None:
             self.guard = torch.cuda.stream(self.stream)
-        elif self.device.index != torch.cuda.current_device():
+        elif self.device.index != _current_device():
             self.guard = torch.cuda.device(self.device)
         if self.guard is not None:
             self.guard.__enter__()
