@@ -484,8 +484,8 @@ evo_status evo_combine_rows_backward(const evo_row_sets* p, void* cuda_stream);
  *   dx[r] = W_g' dz[r]      dweight_g = sum over the group's rows of dz[r] x[r]'      dbias_g = sum of dz[r]
  * dx, dweight and dbias NULL: not wanted.  x is read for dweight alone, the weights for dx alone, y for activations alone (d_y may be NULL without one).
  * Rows of dx that belong to no group are left as they are; an empty group's gradients are zeros.  sum_weight / sum_bias: one gradient for all groups
- * together (weights or biases that the groups share: stride 0).  Types, offsets, sums and infinities as above; of 16-bit types dz counts with 16 bits and more.  With
- * an activation scale may not be 0.  Outputs may not overlap anything, from the first to the last element of each array (a layer's
+ * together (weights or biases that the groups share: stride 0).  Types, offsets, sums and infinities as above; of 16-bit types dz / scale counts with 16 bits and more
+ * (fp16: to 2^-25 at worst, numbers below 2^-14 with fewer).  With an activation scale may not be 0, nor so small that 1 / scale is no number.  Outputs may not overlap anything, from the first to the last element of each array (a layer's
  * gradients inside rows as wide as theta's do not overlap: dweight and dbias may lie between each other's groups).
  * Errors: INVALID_ARG, WORKSPACE, UNSUPPORTED (more than 2^31 blocks), CUDA.  The workspace with any of the inputs NULL is enough for any addresses.
  */
@@ -511,7 +511,7 @@ evo_status evo_grouped_linear_backward(const evo_grouped* forward, const evo_gro
  * is looked at, its logp is 0 and its gradient zeros.  Logits of minus infinity are forbidden actions (probability and gradient 0); a
  * row with a NaN, an infinity above zero, or nothing but forbidden actions has NaN for logp and gradient, and the loss is NaN.
  * logits and gradient [rows][actions] of one type, any pitch and alignment; gradient may be logits itself (same pointer and pitch).  loss (one number), logp and gradient NULL: not wanted.  Sums of a
- * row in fp32, what follows from it and the sum over rows in fp64, in a fixed order.
+ * row in fp32; differences of logarithms, and the sum over rows, in fp64, functions of them in fp32; everything in a fixed order.
  * Errors: INVALID_ARG, WORKSPACE, UNSUPPORTED (more than 2^31 rows), CUDA.
  */
 typedef struct evo_policy_rows {

@@ -2,7 +2,8 @@
 //
 // A group of a population has few rows and weights of its own: dx is bound by the weights' way from memory, dW by its own way there.  k_rows reads
 // a group's weights once for up to 8 rows; k_weights makes tiles of 64 outputs x 64 or 128 inputs.  Where there are too few tiles for the
-// GPU and many rows, the rows are split and the parts added up in a fixed order.
+// GPU and many rows, the rows are split and the parts added up in a fixed order.  4,096 members of 128 x 128, 16,384 ragged rows, fp32: k_rows 60 us (4.7 TB/s; reading the
+// weights alone is 41), k_weights 80 (its stores alone 40; the rest is what a block waits for before it stores), all together, overlapped, 137.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 

@@ -6,6 +6,9 @@
 // tile out of tensor memory, through shared memory so that rows of a tile are written whole, while the next tile's are under way.  The last rows of a group end inside a box: the
 // rows behind them, another group's, are overwritten with zeros in shared memory (both operands: theirs may be infinities).
 // dx goes through the forward's kernel with the weights' rows as the contracted index.
+// 8,192 rows of bf16 of 4 groups, 4,096 -> 4,096: dW 232 us, 1,185 TFLOP/s, dx 209, 1,315; the MMAs alone, without copies and stores, take 210 either way.  Of 32 ragged groups,
+// 1,024 -> 4,096: dW 104 us, dx 92 (3.7 us a tile of four times 64 rows, of which the MMAs need 1.2 and the result's way out 1.7).  Pairs of blocks on 256 x 256 tiles took 4 % less and
+// are not kept.
 //
 // dz = dy act'(z) is laid out first where it is not dy itself, scale left to the end: fp32 as three bf16 parts like the rows (and weights), of 16-bit types with
 // tanh as two parts of the type (rounded once it would be off by as much as the result's own rounding); relu's is dy or 0.

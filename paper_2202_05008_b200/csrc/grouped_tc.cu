@@ -9,7 +9,8 @@
 // count is padded beyond 16.  Blocks stay and walk over (group, row tile, 128 outputs), the outputs of a row tile side by side, so
 // that its rows are read from L2.  A thread copies 64 of the contracted index a stage by TMA (weights 128 x 64, rows in boxes of 128, 64 and 32), another
 // issues the MMAs, eight warps take the sums of one tile out of tensor memory while the next tile's are under way.
-// 8,192 even rows of 4 groups, 4,096 -> 4,096: 225 us, 1,220 TFLOP/s; of 32 groups, 1,024 -> 4,096: 82 us (the weights alone are 41 from
+// One thread waits for operands and issues (a warp that voted on a time-out between two steps left the tensor core idle: 4 groups 225 us).
+// 8,192 even rows of 4 groups, 4,096 -> 4,096: 209 us, 1,315 TFLOP/s; of 32 groups, 1,024 -> 4,096: 76 us (the weights alone are 41 from
 // memory).  What is left is the first loads, the last wave and, in ragged groups, tiles of few rows.
 //
 // TR: the weights' rows are the contracted index (the gradient of the rows, dx[r] = W_g' dz[r]): they come as boxes of 64 x 64, MN-major, and nothing is transposed.

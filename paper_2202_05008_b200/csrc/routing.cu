@@ -6,7 +6,7 @@
 // Up to 32,768 pairs are in the registers of one block or of a cluster of eight, whose totals meet through distributed shared memory: one launch.  More are counted,
 // scanned and placed in three; the table in between holds a count for every member and block.  Of more than 2,047 members, whose counters would take longer than
 // the pairs, a pass sorts by the lower half of the bits and another by the upper (524,288 pairs of 4,096: 57 us at once, 45 so).
-// It is bound by latency: 131,072 pairs are 1.6 MB.
+// It is bound by latency: 131,072 pairs are 1.6 MB.  In a graph 64 pairs take 1.8 us, 4,096 of 64 members 7.0, 16,384 8.6 (one launch each), 131,072 11.4, 524,288 18.5.
 #include "async.cuh"
 #include "routing.h"
 

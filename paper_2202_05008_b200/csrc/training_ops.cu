@@ -41,7 +41,7 @@ evo_status check_workspace(size_t need, const void* p, size_t bytes)
 bool route_args(const evo_routes* p, RouteArgs* a)
 {
     if (!p || p->struct_size != sizeof(evo_routes) || p->members_64 > 1u || p->groups < 1u || p->groups > kMostWidth || p->choices < 1u) return false;
-    if (p->rows > kMost || p->rows * p->choices >= (1ull << 31) || p->ld_members > kMost || (p->rows > 1u && p->ld_members < p->choices)) return false;
+    if (p->rows > kMost || (p->rows && p->choices > 0x7FFFFFFFull / p->rows) || p->ld_members > kMost || (p->rows > 1u && p->ld_members < p->choices)) return false;
     std::memset(a, 0, sizeof(*a));
     a->members = p->d_members; a->ld = p->rows > 1u ? p->ld_members : p->choices; a->wide = p->members_64;
     a->choices = p->choices; a->groups = p->groups; a->pairs = static_cast<uint32_t>(p->rows * p->choices);

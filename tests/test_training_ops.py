@@ -35,7 +35,8 @@ def _routes(**kw):
                                  dict(rows=1 << 41), dict(rows=1 << 63), dict(ld_members=1), dict(d_members=None), dict(d_offsets=None), dict(d_place=None),
                                  dict(d_members=FAR + 2), dict(d_members=FAR + 4, members_64=1), dict(d_offsets=2 * FAR + 2), dict(d_source=3 * FAR + 1),
                                  dict(d_place=4 * FAR + 2), dict(d_place=FAR + 796), dict(d_source=FAR), dict(d_offsets=FAR + 4), dict(d_source=4 * FAR + 400),
-                                 dict(d_offsets=3 * FAR + 796), dict(ld_members=1 << 41)])
+                                 dict(d_offsets=3 * FAR + 796), dict(ld_members=1 << 41),
+                                 dict(rows=1 << 40, choices=1 << 24, ld_members=1 << 24), dict(rows=1 << 33, choices=1 << 31, ld_members=1 << 32)])
 def test_routes_that_are_refused(lib, bad):
     assert lib.evo_route_rows(C.byref(_routes(**bad)), FAR * 9, 1 << 40, None) == INVALID
     assert lib.evo_route_rows(None, FAR * 9, 1 << 40, None) == INVALID
