@@ -160,10 +160,18 @@ struct Sums {
     }
 };
 
-// Rows [r, r + 8) of the group, as far as `end`.  STAGED: weights by way of shared memory (`stage`); SPLIT: the block's warps share a tile.
-template <typename T, bool VEC, bool STAGED, bool SPLIT>
-__device__ __forceinline__ void rows_tile(const GradientArgs& a, uint32_t group, uint32_t c0, uint64_t r, uint64_t end, T* hi, T* lo, T* stage, float (*share)[16][32])
+// COPY: bytes of a copy of weights to shared memory, 16, 4 or 0: they are loaded straight into operands.  SPLIT: the block's warps share a tile.
+struct RowsArgs {
+    GradientArgs a;
+    uint32_t layers, splits;             // blocks that share a group's rows, eight at a time; and the weight rows, a chunk at a time
+    float* part;                         // splits > 1: [splits][rows][n_in]
+};
+// Rows [r, r + 8) of the group, as far as `end`.
+template <typename T, uint32_t COPY, bool SPLIT>
+__device__ __forceinline__ void rows_tile(const RowsArgs& p, uint32_t group, uint32_t split, uint32_t c0, uint64_t r, uint64_t end, T* hi, T* lo, T* stage, float (*share)[16][32])
 {
+    constexpr bool STAGED = COPY != 0u && !SPLIT;
+    const GradientArgs& a = p.a;
     constexpr uint32_t kTiles = Tile<T>::kTiles, kPitch = Tile<T>::kPitch, C = Tile<T>::kColumns, kChunk = STAGED ? 64u : 128u, kThreads = 32u * kRowWarps;
     const GroupedArgs& f = a.f;
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, g = lane >> 2, q = lane & 3u, n_out = f.n_out;
@@ -175,22 +183,25 @@ __device__ __forceinline__ void rows_tile(const GradientArgs& a, uint32_t group,
     Sums<T> sums;
     sums.clear();
     float part[kTiles][4];
-    for (uint32_t o0 = 0; o0 < n_out; o0 += kChunk) {
+    for (uint32_t o0 = split * kChunk; o0 < n_out; o0 += p.splits * kChunk) {
         const uint32_t count = min(kChunk, n_out - o0);
         uint4 v[8];
         if constexpr (STAGED) {
             __syncthreads();
+            // (512 bytes of a weight row: 32 copies of 16 bytes, or 128 of 4)
+            constexpr uint32_t kCopies = 512u / COPY, kEach = COPY / sizeof(T), kMine = kChunk * kCopies / kThreads;
 #pragma unroll
-            for (uint32_t i = 0; i < kChunk * 32u / kThreads; ++i) {
-                const uint32_t row = threadIdx.x / 32u + i * (kThreads / 32u), c = threadIdx.x % 32u * C;
+            for (uint32_t i = 0; i < kMine; ++i) {
+                const uint32_t row = threadIdx.x / kCopies + i * (kThreads / kCopies), c = threadIdx.x % kCopies * kEach;
                 const bool there = row < count && c0 + c < f.n_in;
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;"
-                             :: "r"(smem_u32(stage + row * Tile<T>::kWeightPitch + c)), "l"(there ? w + static_cast<uint64_t>(o0 + row) * f.ld_w + c0 + c : w), "r"(there ? 16u : 0u)
-                             : "memory");
+                const uint32_t to = smem_u32(stage + row * Tile<T>::kWeightPitch + c), bytes = there ? COPY : 0u;
+                const T* const from = there ? w + static_cast<uint64_t>(o0 + row) * f.ld_w + c0 + c : w;
+                if constexpr (COPY == 16u) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(to), "l"(from), "r"(bytes) : "memory");
+                else asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" :: "r"(to), "l"(from), "r"(bytes) : "memory");
             }
             asm volatile("cp.async.commit_group;" ::: "memory");
         } else {
-            load_step<T, VEC>(w + (columns ? mine : 0u), f.ld_w, o0 + k0, n_out, columns, v);
+            load_step<T, COPY == 16u>(w + (columns ? mine : 0u), f.ld_w, o0 + k0, n_out, columns, v);
         }
         {
             // a weight row a thread: all its rows' dy and y are asked for together
@@ -240,7 +251,7 @@ __device__ __forceinline__ void rows_tile(const GradientArgs& a, uint32_t group,
                 for (uint32_t j = 0; j < 8u; ++j)
                     v[j] = *reinterpret_cast<const uint4*>(stage + (k + Tile<T>::row_of(j, q)) * Tile<T>::kWeightPitch + warp * Tile<T>::kWarpColumns + C * g);
             } else {
-                if (n) load_step<T, VEC>(w + (columns ? mine : 0u), f.ld_w, o0 + k, n_out, columns, v);
+                if (n) load_step<T, COPY == 16u>(w + (columns ? mine : 0u), f.ld_w, o0 + k, n_out, columns, v);
             }
             sums.step(v, hi, lo, two, k, part);
         }
@@ -276,32 +287,58 @@ __device__ __forceinline__ void rows_tile(const GradientArgs& a, uint32_t group,
     for (uint32_t i = 0; i < 2u; ++i) {
         const uint32_t row = 2u * q + i;
         if (row >= rows) continue;
-        T* const to = static_cast<T*>(a.dx) + (r + row) * a.ld_dx + mine + C * g;
+        if (p.splits > 1u) {
+            float* const to = p.part + (split * f.rows + r + row) * f.n_in + mine + C * g;
 #pragma unroll
-        for (uint32_t e = 0; e < C; ++e)
-            if (C * g + e < columns) to[e] = from_float<T>(f.scale * sums.c[e / 2u][i + 2u * (e & 1u)]);
+            for (uint32_t e = 0; e < C; ++e)
+                if (C * g + e < columns) to[e] = f.scale * sums.c[e / 2u][i + 2u * (e & 1u)];
+        } else {
+            T* const to = static_cast<T*>(a.dx) + (r + row) * a.ld_dx + mine + C * g;
+#pragma unroll
+            for (uint32_t e = 0; e < C; ++e)
+                if (C * g + e < columns) to[e] = from_float<T>(f.scale * sums.c[e / 2u][i + 2u * (e & 1u)]);
+        }
     }
 }
 
-// layers 2: blocks of a first layer take the rows from the ninth on, so that long groups begin early
-template <typename T, bool VEC, bool SPLIT>
-__global__ void __launch_bounds__(32 * kRowWarps, 5) k_rows(const __grid_constant__ GradientArgs a, uint32_t layers)
+template <typename T, uint32_t COPY, bool SPLIT>
+__global__ void __launch_bounds__(32 * kRowWarps, 5) k_rows(const __grid_constant__ RowsArgs p)
 {
-    constexpr bool kStaged = VEC && !SPLIT;
+    constexpr bool kStaged = COPY != 0u && !SPLIT;
     constexpr uint32_t kWide = SPLIT ? Tile<T>::kWarpColumns : Tile<T>::kAcross;
     __shared__ __align__(16) T hi[8 * Tile<T>::kPitch], lo[8 * Tile<T>::kPitch], stage[kStaged ? 64u * Tile<T>::kWeightPitch : 8u];
     __shared__ float share[SPLIT ? kRowWarps - 1 : 1][16][32];
-    dep_begin(a);
-    const uint32_t across = (a.f.n_in + kWide - 1u) / kWide, per_layer = a.f.groups * across, layer = blockIdx.x / per_layer, at = blockIdx.x % per_layer;
-    const uint32_t group = at / across, c0 = at % across * kWide;
-    uint64_t r, end;
-    group_rows(a.f, group, &r, &end);
-    if (layers > 1u) {
-        if (layer == 0u) r += 8u;
-        else end = min(end, r + 8u);
+    dep_begin(p.a);
+    const uint32_t across = (p.a.f.n_in + kWide - 1u) / kWide;
+    const uint32_t group = blockIdx.x / across, c0 = blockIdx.x % across * kWide;
+    // (the last rows first: few groups have them, and those take longest)
+    uint32_t split = 0, layer = gridDim.y - 1u - blockIdx.y;
+    if (p.splits > 1u) { split = layer % p.splits; layer /= p.splits; }
+    uint64_t first, end;
+    group_rows(p.a.f, group, &first, &end);
+    for (uint64_t r = first + 8u * layer; r < end; r += 8u * p.layers) rows_tile<T, COPY, SPLIT>(p, group, split, c0, r, end, hi, lo, stage, share);
+    dep_end(p.a);
+}
+
+// The parts of rows that belong to a group, added up in their order.
+template <typename T>
+__global__ void __launch_bounds__(256) k_add_rows(const __grid_constant__ RowsArgs p)
+{
+    dep_wait();
+    dep_trigger();
+    const GroupedArgs& f = p.a.f;
+    uint64_t first, end, skip;
+    group_rows(f, 0u, &first, &skip);
+    group_rows(f, f.groups - 1u, &skip, &end);
+    const uint64_t each = f.rows * f.n_in;
+    for (uint64_t i = static_cast<uint64_t>(blockIdx.x) * 256u + threadIdx.x; i < each; i += static_cast<uint64_t>(gridDim.x) * 256u) {
+        const uint64_t row = i / f.n_in;
+        if (row < first || row >= end) continue;
+        float s = 0.f;
+#pragma unroll 4
+        for (uint32_t k = 0; k < p.splits; ++k) s += p.part[k * each + i];
+        static_cast<T*>(p.a.dx)[row * p.a.ld_dx + i % f.n_in] = from_float<T>(s);
     }
-    for (; r < end; r += 8u) rows_tile<T, VEC, kStaged, SPLIT>(a, group, c0, r, end, hi, lo, stage, share);
-    dep_end(a);
 }
 
 // ---- dW and db ----
@@ -545,23 +582,20 @@ uint32_t bias_splits(const GradientArgs& a)
 // 16-bit rows that are whole pieces of 16 bytes (the same wherever the arrays lie: workspaces are planned before they do)
 bool whole_pieces(const GradientArgs& a) { return ((a.f.n_in | a.f.n_out) & 7u) == 0u; }
 // Whether tcgen05 pays for dx: rows a group from which it does.  fp32 weights, and those that TMA cannot address, are laid out first, whatever the rows; the walk over many
-// groups takes a warp longer than the products; few tiles of few rows leave SMs without one, but a block of k_rows takes long weight columns one piece after the
-// other.  us, tcgen05 / k_rows, rows a group in brackets:
-//   fp32     200 groups of 256 -> 256 (16) 62.7 / 41.0, (32) 63.9 / 83.9; 32 of 1,024 -> 1,024 (16) 140 / 120, (32) 140 / 236; 1 of 4,096 -> 4,096 (32) 172 / 127, (64) 176 / 289;
-//            1,000 of 64 -> 64 (32) 64 / 45, (64) 75 / 87; 3,000 of 20 -> 30 (64) 171 / 127
-//   16 bits  200 of 256 -> 256 (2) 13.1 / 11.1, (8) 13.2 / 20.1; 1,000 of 64 -> 64 (16) 26.5 / 21.7, (32) 27.7 / 42; 32 of 1,024 -> 1,024 (2) 16.8 / 24.3;
-//            not aligned: 300 of 207 -> 379 (8) 60.8 / 60.0, (16) 62.7 / 120; 3,000 of 20 -> 30 (32) 102 / 92, 10 of 18 -> 2,204 with 3 rows in all 21.4 / 53.5
-// Over 225 shapes (120 of them drawn) the choice takes 1.02 times the faster side's time in the geometric mean; tcgen05 always 1.7 times, k_rows always 2.3.
+// groups takes a warp longer than the products; few tiles leave SMs without one, which k_rows' splits do not; and a tile takes 128 inputs x 64 outputs at a time, however
+// few there are.  us, tcgen05 / k_rows, rows a group in brackets:
+//   fp32     200 groups of 256 -> 256 (16) 63.2 / 35.7, (32) 64.6 / 68.2; 32 of 1,024 -> 1,024 (32) 139 / 131, (64) 145 / 284; 1 of 4,096 -> 4,096 (32) 173 / 105, (64) 176 / 182;
+//            1,000 of 64 -> 64 (32) 66 / 37, (64) 74 / 61; 3,000 of 20 -> 30 (64) 172 / 102
+//   16 bits  200 of 256 -> 256 (2) 13.2 / 10.8, (8) 20.4 / 24.1; 1,000 of 64 -> 64 (16) 26.5 / 17.5, (32) 27.7 / 31.9; 32 of 1,024 -> 1,024 (2) 16.7 / 22.7, (8) 29 / 51;
+//            1 of 4,096 -> 4,096 (8) 25.9 / 19.3, (16) 26.1 / 38.9; not aligned: 300 of 207 -> 379 (2) 63.6 / 37.1, (8) 61.1 / 83.7; 3,000 of 20 -> 30 (16) 101 / 70, (32) 102 / 115
+// Over 225 shapes (120 of them drawn) the choice takes 1.02 times the faster side's time in the geometric mean; tcgen05 always 1.9 times, k_rows always 1.3.
 bool dx_on_tensor_cores(uint32_t type, const GradientArgs& a)
 {
     const GroupedArgs& f = a.f;
     if (f.rows >= (1ull << 31) || static_cast<uint64_t>(f.groups) * f.n_out >= (1ull << 31)) return false;
-    const double groups = f.groups, tiles = std::fmin(groups, static_cast<double>(f.rows)) * ((f.n_in + 127u) / 128u), idle = std::fmax(0.0, 1.0 - tiles / kSms);
-    const double size = static_cast<double>(f.n_in) * f.n_out;
-    double least;
-    if (type == EVO_F32) least = 16.0 + groups / 45.0 + 24.0 * idle * idle * std::fmin(1.0, size / 1e6);
-    else if (whole_pieces(a)) least = groups / 50.0;
-    else least = idle > 0.1 && f.n_out >= 700u && f.groups <= 64u ? 0.0 : 4.0 + groups / 100.0;
+    const double groups = f.groups, across = (f.n_in + 127u) / 128u, idle = std::fmax(0.0, 1.0 - std::fmin(groups, static_cast<double>(f.rows)) * across / kSms);
+    const double more = std::fmin(16.0, 8192.0 * across * ((f.n_out + 63u) / 64u) / (static_cast<double>(f.n_in) * f.n_out)) - 1.0;
+    const double least = type == EVO_F32 ? 18.0 + groups / 45.0 + 60.0 * idle * idle + 4.0 * more : whole_pieces(a) ? groups / 45.0 + 20.0 * idle * idle : 4.0 + 8.0 * idle * idle + more;
     return static_cast<double>(f.rows) >= least * groups;
 }
 // The same for dW.  A tile is 128 outputs x up to 256 inputs, however many there are; where there are few tiles k_weights takes long groups 16 rows at a time.  tcgen05 / k_weights:
@@ -581,11 +615,36 @@ bool dw_on_tensor_cores(uint32_t type, const GradientArgs& a)
     return static_cast<double>(f.rows) >= least * sets;
 }
 uint32_t inputs_of_a_tile(const GradientArgs& a) { return a.f.n_in <= 64u ? 64u : 128u; }
+// How dx is spread over blocks without tcgen05: the columns of a warp's tile shared by the block's warps (split), rows eight at a time over `layers`, weight rows a chunk at a time over
+// `splits`, as far as there is room on the GPU.
+struct RowsPlan { uint32_t split, layers, splits; };
+RowsPlan rows_plan(uint32_t type, const GradientArgs& a)
+{
+    const GroupedArgs& f = a.f;
+    const uint64_t all = type == EVO_F32 ? 128u : 256u, wide = all / kRowWarps, used = f.rows < f.groups ? f.rows : f.groups, passes = (f.rows / f.groups + 7u) / 8u;
+    RowsPlan p;
+    uint64_t blocks = used * ((f.n_in + all - 1u) / all);
+    // (with two rows a group on average few have nine, and the blocks that find none cost more)
+    const uint64_t most_layers = f.rows > 2ull * f.groups ? 2u * passes : 1u, room = 8u * kSms;
+    uint64_t layers = blocks ? room / blocks : 1u;
+    layers = layers < 2u ? 2u : layers;
+    layers = layers < most_layers ? layers : most_layers;
+    p.split = blocks * layers < 4u * kSms && f.n_out > kStepK;
+    if (p.split) blocks = used * ((f.n_in + wide - 1u) / wide);
+    const uint64_t chunks = (f.n_out + (p.split ? 127u : 63u)) / (p.split ? 128u : 64u);
+    uint64_t splits = 1;
+    if (blocks * layers < 2u * kSms && chunks > 2u) splits = 4u * kSms / (blocks * layers + 1u);
+    splits = splits > chunks / 2u ? chunks / 2u : splits;
+    p.layers = static_cast<uint32_t>(layers < 1u ? 1u : layers);
+    p.splits = static_cast<uint32_t>(splits < 2u ? 1u : splits > 32u ? 32u : splits);
+    return p;
+}
 struct Plan {
     TcPlan tc;
+    RowsPlan rows;
     bool both;                           // dW and db in one launch of k_weights
     uint32_t w_splits, b_splits;
-    size_t tc_bytes, w_bytes, b_bytes;
+    size_t tc_bytes, x_bytes, w_bytes, b_bytes;
 };
 size_t padded(size_t n) { return (n + 255u) / 256u * 256u; }
 Plan plan_for(uint32_t type, const GradientArgs& a, bool any_address)
@@ -599,26 +658,34 @@ Plan plan_for(uint32_t type, const GradientArgs& a, bool any_address)
     p.tc = grouped_gradient_tc_plan(type, a, dx, dw, p.w_splits, any_address);
     const uint64_t w_sets = a.sum_w ? 1u : a.f.groups, b_sets = a.sum_b ? 1u : a.f.groups;
     p.tc_bytes = padded(p.tc.bytes());
+    p.rows = rows_plan(type, a);
+    p.x_bytes = a.dx && a.f.rows && !dx && p.rows.splits > 1u ? padded(4u * p.rows.splits * a.f.rows * a.f.n_in) : 0u;
     p.w_bytes = p.w_splits > 1u ? padded(4u * p.w_splits * w_sets * a.f.n_out * a.f.n_in) : 0u;
     p.b_bytes = p.b_splits > 1u ? padded(4u * p.b_splits * b_sets * a.f.n_out) : 0u;
     return p;
 }
 
 template <typename T>
-int launch_rows(cudaStream_t st, const GradientArgs& a)
+int launch_rows(cudaStream_t st, const GradientArgs& a, const RowsPlan& plan, float* part)
 {
     const GroupedArgs& f = a.f;
-    const uint32_t wide = Tile<T>::kWarpColumns, all = Tile<T>::kAcross;
-    // groups that can have rows, and the blocks that they make without splitting the sums
-    const uint64_t used = f.rows < f.groups ? f.rows : f.groups;
-    const bool split = used * ((f.n_in + all - 1u) / all) < 4u * kSms && f.n_out > kStepK;
-    // (with two rows a group on average, few have nine, and the blocks that find none cost more)
-    const uint32_t layers = f.rows > 2ull * f.groups ? 2u : 1u;
-    const uint64_t blocks = static_cast<uint64_t>(f.groups) * (split ? (f.n_in + wide - 1u) / wide : (f.n_in + all - 1u) / all) * layers;
+    const uint32_t wide = plan.split ? Tile<T>::kWarpColumns : Tile<T>::kAcross;
+    const uint64_t blocks = static_cast<uint64_t>(f.groups) * ((f.n_in + wide - 1u) / wide);
     if (blocks > 0x7FFFFFFFull) return -2;
-    const bool aligned = (reinterpret_cast<uintptr_t>(f.w) & 15u) == 0u && (f.n_in | f.ld_w | f.stride_w) % Tile<T>::kColumns == 0u;
-    auto kernel = aligned ? (split ? k_rows<T, true, true> : k_rows<T, true, false>) : (split ? k_rows<T, false, true> : k_rows<T, false, false>);
-    return launch_dependent(kernel, dim3(static_cast<uint32_t>(blocks)), dim3(32 * kRowWarps), 0, st, a, layers) == cudaSuccess ? 1 : -1;
+    RowsArgs p;
+    p.a = a; p.layers = plan.layers; p.splits = plan.splits; p.part = part;
+    const uint64_t bits = reinterpret_cast<uintptr_t>(f.w) | (f.n_in | f.ld_w | f.stride_w) * sizeof(T);
+    auto kernel = bits % 16u == 0u ? (plan.split ? k_rows<T, 16, true> : k_rows<T, 16, false>)
+                : plan.split ? k_rows<T, 0, true> : bits % 4u == 0u ? k_rows<T, 4, false> : k_rows<T, 0, false>;
+    return launch_dependent(kernel, dim3(static_cast<uint32_t>(blocks), plan.layers * plan.splits), dim3(32 * kRowWarps), 0, st, p) == cudaSuccess ? 1 : -1;
+}
+template <typename T>
+bool add_rows(cudaStream_t st, const GradientArgs& a, const RowsPlan& plan, float* part)
+{
+    RowsArgs p;
+    p.a = a; p.layers = plan.layers; p.splits = plan.splits; p.part = part;
+    const uint64_t blocks = (a.f.rows * a.f.n_in + 255u) / 256u;
+    return launch_dependent(k_add_rows<T>, dim3(static_cast<uint32_t>(blocks < 8u * kSms ? blocks : 8u * kSms)), dim3(256), 0, st, p) == cudaSuccess;
 }
 
 template <typename T>
@@ -679,8 +746,9 @@ int launch_type(cudaStream_t st, uint32_t type, const GradientArgs& a, void* wor
 {
     const Plan plan = plan_for(type, a, false);
     uint8_t* const at = static_cast<uint8_t*>(work);
-    float* const part_w = reinterpret_cast<float*>(at + plan.tc_bytes);
-    float* const part_b = reinterpret_cast<float*>(at + plan.tc_bytes + plan.w_bytes);
+    float* const part_x = reinterpret_cast<float*>(at + plan.tc_bytes);
+    float* const part_w = reinterpret_cast<float*>(at + plan.tc_bytes + plan.x_bytes);
+    float* const part_b = reinterpret_cast<float*>(at + plan.tc_bytes + plan.x_bytes + plan.w_bytes);
     const uint32_t w_sets = a.sum_w ? 1u : a.f.groups, b_sets = a.sum_b ? 1u : a.f.groups;
     int launches = 0, n = 0;
     // (the first kernel waits at its beginning)
@@ -691,7 +759,7 @@ int launch_type(cudaStream_t st, uint32_t type, const GradientArgs& a, void* wor
         launches += n;
     }
     if (a.dx && a.f.rows && !plan.tc.dx) {
-        n = launch_rows<T>(st, late(a));
+        n = launch_rows<T>(st, late(a), plan.rows, part_x);
         if (n < 0) return n;
         launches += n;
     }
@@ -704,6 +772,10 @@ int launch_type(cudaStream_t st, uint32_t type, const GradientArgs& a, void* wor
         n = launch_bias<T>(st, late(a), plan.b_splits, part_b, plan.tc, work);
         if (n < 0) return n;
         launches += n;
+    }
+    if (plan.x_bytes) {
+        if (!add_rows<T>(st, a, plan.rows, part_x)) return -1;
+        ++launches;
     }
     if (plan.w_splits > 1u) {
         if (!add_parts<T>(st, part_w, plan.w_splits, w_sets, a.f.n_out, a.f.n_in, a.dw, a.stride_dw, a.ld_dw)) return -1;
@@ -721,7 +793,7 @@ int launch_type(cudaStream_t st, uint32_t type, const GradientArgs& a, void* wor
 size_t grouped_gradient_bytes(uint32_t type, const GradientArgs& a, bool any_address)
 {
     const Plan p = plan_for(type, a, any_address);
-    return p.tc_bytes + p.w_bytes + p.b_bytes;
+    return p.tc_bytes + p.x_bytes + p.w_bytes + p.b_bytes;
 }
 
 int launch_grouped_gradient(cudaStream_t st, uint32_t type, const GradientArgs& a, void* work)

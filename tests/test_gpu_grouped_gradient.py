@@ -102,6 +102,23 @@ def test_groups_of_every_part_of_a_tile(n_in, n_out, dtype):
         assert (dx[-3:] == 7).all()
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("groups,lengths,n_in,n_out", [
+    (1, [2], 200, 2000), (1, [1], 4097, 129), (2, [9, 0], 36, 700), (3, [30, 0, 47], 26, 300), (4, [3, 2, 0, 5], 300, 1031),    # few blocks: the weight rows are split
+    (2, [200, 7], 14, 260), (24, [0] * 23 + [150], 70, 66), (400, [3] * 398 + [90, 0], 50, 61),                               # one group has most of the rows
+    (400, [1] * 200 + [0] * 200, 137, 66), (300, [i % 7 for i in range(300)], 138, 200), (60, [1] * 60, 1001, 64),            # rows of weights that start on 2, 4 and 16 bytes
+])
+def test_few_rows_whatever_the_groups_and_the_alignment(dtype, groups, lengths, n_in, n_out):
+    for act, shift in (("none", 0), ("tanh", 1), ("relu", 2)):
+        dy, x, w, off, y = make(groups, lengths, n_in, n_out, dtype, act, lead=1, tail=2, seed=shift)
+        room = torch.full((groups, n_out * n_in + 8), float("nan"), dtype=dtype, device="cuda")         # (a NaN beside the weights would show)
+        weight = room[:, shift:shift + n_out * n_in].unflatten(1, (n_out, n_in))
+        weight.copy_(w)
+        wide = torch.full((x.shape[0], n_in + 3), 7.0, dtype=dtype, device="cuda")
+        check(dy, x, weight, off, y, act, 1.0, out=(wide[:, 1:n_in + 1], None, None))
+        assert (wide[0] == 7).all() and (wide[-2:] == 7).all() and (wide[:, 0] == 7).all() and (wide[:, n_in + 1:] == 7).all()
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("n_in,n_out,shift", [(64, 48, 0), (64, 48, 1), (61, 48, 0), (256, 136, 3), (256, 136, 8)])
 @pytest.mark.parametrize("lengths", [[3, 0, 20, 90, 1], [200, 64, 0, 130, 500]])
