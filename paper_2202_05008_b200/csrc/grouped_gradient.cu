@@ -55,7 +55,7 @@ template <typename T> struct Tile {
     static constexpr uint32_t kTiles = kColumns / 2u;                 // 16 x 8 products side by side
     static constexpr uint32_t kWarpColumns = 8u * kColumns;
     static constexpr uint32_t kAcross = kWarpColumns * kRowWarps;     // 512 bytes
-    static constexpr uint32_t kPitch = sizeof(T) == 4 ? 144u : 160u;  // of a staged row: 16 words modulo 32, so that eight lanes' pieces meet no bank twice
+    static __host__ __device__ constexpr uint32_t pitch(uint32_t chunk) { return chunk + 64u / sizeof(T); }      // of a staged row: 16 words modulo 32, so that eight lanes' pieces meet no bank twice
     static constexpr uint32_t kWeightPitch = kAcross + 32u / sizeof(T);      // of a staged weight row: 8 words modulo 32, the same for lanes of four rows
     // Piece j of lane (g, q) is weight row `row_of(j)` of a step, and where a lane finds its rows of dz beside each other: the j-th of lane q at place `place_of(row)`.
     static __device__ __forceinline__ constexpr uint32_t row_of(uint32_t j, uint32_t q) { return sizeof(T) == 4 ? 16u * (j / 4u) + 4u * (j % 4u) + q : 4u * j + q; }
@@ -91,74 +91,91 @@ __device__ __forceinline__ void load_step(const T* w, uint64_t ld, uint32_t k, u
 // c[tile]: columns (2 tile) and (2 tile + 1) of the lane's, rows 2q and 2q + 1
 template <typename T>
 struct Sums {
-    float c[Tile<T>::kTiles][4], small[std::is_same<T, float>::value ? Tile<T>::kTiles : 1u][4];
+    float c[Tile<T>::kTiles][4], part[Tile<T>::kTiles][4], small[std::is_same<T, float>::value ? Tile<T>::kTiles : 1u][4];
 
     __device__ __forceinline__ void clear()
     {
 #pragma unroll
         for (uint32_t m = 0; m < Tile<T>::kTiles; ++m)
 #pragma unroll
-                for (uint32_t i = 0; i < 4u; ++i) {
-                    c[m][i] = 0.f;
-                    if constexpr (std::is_same<T, float>::value) small[m][i] = 0.f;
-                }
+            for (uint32_t i = 0; i < 4u; ++i) {
+                c[m][i] = part[m][i] = 0.f;
+                if constexpr (std::is_same<T, float>::value) small[m][i] = 0.f;
+            }
     }
-    // weight rows [k, k + 32) of the chunk that is staged in `hi` and `lo`, added to part and small
-    __device__ __forceinline__ void step(const uint4 (&v)[8], const T* hi, const T* lo, bool two, uint32_t k, float (&part)[Tile<T>::kTiles][4])
+    __device__ __forceinline__ void take_out()
     {
-        const uint32_t g = (threadIdx.x & 31u) >> 2, q = threadIdx.x & 3u;
-        if constexpr (std::is_same<T, float>::value) {
 #pragma unroll
-            for (uint32_t s = 0; s < 2u; ++s) {
-                uint4 bh, bl;
-                {
-                    bh = *reinterpret_cast<const uint4*>(hi + g * Tile<T>::kPitch + k + 16u * s + 4u * q);
-                    bl = *reinterpret_cast<const uint4*>(lo + g * Tile<T>::kPitch + k + 16u * s + 4u * q);
-                }
+        for (uint32_t m = 0; m < Tile<T>::kTiles; ++m)
 #pragma unroll
-                for (uint32_t h = 0; h < 2u; ++h) {          // weight rows 4q + 2h and 4q + 2h + 1
-                    const uint4 x = v[4u * s + 2u * h], y = v[4u * s + 2u * h + 1u];
-                    const uint32_t xs[4] = { x.x, x.y, x.z, x.w }, ys[4] = { y.x, y.y, y.z, y.w };
-#pragma unroll
-                    for (uint32_t m = 0; m < 2u; ++m) {
-                        uint32_t ah[4], al[4];
-                        gm::split(__uint_as_float(xs[2u * m]), ah[0], al[0]);
-                        gm::split(__uint_as_float(xs[2u * m + 1u]), ah[1], al[1]);
-                        gm::split(__uint_as_float(ys[2u * m]), ah[2], al[2]);
-                        gm::split(__uint_as_float(ys[2u * m + 1u]), ah[3], al[3]);
-                        {
-                            const uint32_t h0 = h ? bh.z : bh.x, h1 = h ? bh.w : bh.y, l0 = h ? bl.z : bl.x, l1 = h ? bl.w : bl.y;
-                            gm::mma_tf32(part[m], ah, h0, h1);
-                            gm::mma_tf32(small[m], ah, l0, l1);
-                            gm::mma_tf32(small[m], al, h0, h1);
-                        }
-                    }
-                }
+            for (uint32_t i = 0; i < 4u; ++i) {
+                c[m][i] += part[m][i];
+                part[m][i] = 0.f;
             }
-        } else {
-            uint4 bh, bl;
-            {
-                bh = *reinterpret_cast<const uint4*>(hi + g * Tile<T>::kPitch + k + 8u * q);
-                if (two) bl = *reinterpret_cast<const uint4*>(lo + g * Tile<T>::kPitch + k + 8u * q);
+    }
+};
+// weight rows [k, k + 32) of the chunk whose dz is staged in `hi` and `lo`, added to the parts of 8 rows, or of EIGHTS times as many where there are more
+template <typename T, uint32_t EIGHTS>
+__device__ __forceinline__ void step(const uint4 (&v)[8], const T* hi, const T* lo, uint32_t pitch, bool two, bool more, uint32_t k, Sums<T> (&sums)[EIGHTS])
+{
+    const uint32_t g = (threadIdx.x & 31u) >> 2, q = threadIdx.x & 3u;
+    if constexpr (std::is_same<T, float>::value) {
+#pragma unroll
+        for (uint32_t s = 0; s < 2u; ++s) {
+            uint4 bh[EIGHTS], bl[EIGHTS];
+#pragma unroll
+            for (uint32_t e = 0; e < EIGHTS; ++e) {
+                bh[e] = *reinterpret_cast<const uint4*>(hi + (8u * e + g) * pitch + k + 16u * s + 4u * q);
+                bl[e] = *reinterpret_cast<const uint4*>(lo + (8u * e + g) * pitch + k + 16u * s + 4u * q);
             }
 #pragma unroll
-            for (uint32_t h = 0; h < 2u; ++h) {              // weight rows 8q + 4h ... 8q + 4h + 3
-                const uint32_t w[4][4] = { { v[4 * h].x, v[4 * h].y, v[4 * h].z, v[4 * h].w }, { v[4 * h + 1].x, v[4 * h + 1].y, v[4 * h + 1].z, v[4 * h + 1].w },
-                                           { v[4 * h + 2].x, v[4 * h + 2].y, v[4 * h + 2].z, v[4 * h + 2].w }, { v[4 * h + 3].x, v[4 * h + 3].y, v[4 * h + 3].z, v[4 * h + 3].w } };
+            for (uint32_t h = 0; h < 2u; ++h) {              // weight rows 4q + 2h and 4q + 2h + 1
+                const uint4 x = v[4u * s + 2u * h], y = v[4u * s + 2u * h + 1u];
+                const uint32_t xs[4] = { x.x, x.y, x.z, x.w }, ys[4] = { y.x, y.y, y.z, y.w };
 #pragma unroll
-                for (uint32_t m = 0; m < 4u; ++m) {
-                    // two rows' numbers of one column beside each other
-                    const uint32_t a[4] = { __byte_perm(w[0][m], w[1][m], 0x5410), __byte_perm(w[0][m], w[1][m], 0x7632), __byte_perm(w[2][m], w[3][m], 0x5410),
-                                            __byte_perm(w[2][m], w[3][m], 0x7632) };
-                    {
-                        gm::mma_16<T>(part[m], a, h ? bh.z : bh.x, h ? bh.w : bh.y);
-                        if (two) gm::mma_16<T>(part[m], a, h ? bl.z : bl.x, h ? bl.w : bl.y);
+                for (uint32_t m = 0; m < 2u; ++m) {
+                    uint32_t ah[4], al[4];
+                    gm::split(__uint_as_float(xs[2u * m]), ah[0], al[0]);
+                    gm::split(__uint_as_float(xs[2u * m + 1u]), ah[1], al[1]);
+                    gm::split(__uint_as_float(ys[2u * m]), ah[2], al[2]);
+                    gm::split(__uint_as_float(ys[2u * m + 1u]), ah[3], al[3]);
+#pragma unroll
+                    for (uint32_t e = 0; e < EIGHTS; ++e) {
+                        if (e && !more) continue;
+                        const uint32_t h0 = h ? bh[e].z : bh[e].x, h1 = h ? bh[e].w : bh[e].y, l0 = h ? bl[e].z : bl[e].x, l1 = h ? bl[e].w : bl[e].y;
+                        gm::mma_tf32(sums[e].part[m], ah, h0, h1);
+                        gm::mma_tf32(sums[e].small[m], ah, l0, l1);
+                        gm::mma_tf32(sums[e].small[m], al, h0, h1);
                     }
                 }
             }
         }
+    } else {
+        uint4 bh[EIGHTS], bl[EIGHTS];
+#pragma unroll
+        for (uint32_t e = 0; e < EIGHTS; ++e) {
+            bh[e] = *reinterpret_cast<const uint4*>(hi + (8u * e + g) * pitch + k + 8u * q);
+            if (two) bl[e] = *reinterpret_cast<const uint4*>(lo + (8u * e + g) * pitch + k + 8u * q);
+        }
+#pragma unroll
+        for (uint32_t h = 0; h < 2u; ++h) {                  // weight rows 8q + 4h ... 8q + 4h + 3
+            const uint32_t w[4][4] = { { v[4 * h].x, v[4 * h].y, v[4 * h].z, v[4 * h].w }, { v[4 * h + 1].x, v[4 * h + 1].y, v[4 * h + 1].z, v[4 * h + 1].w },
+                                       { v[4 * h + 2].x, v[4 * h + 2].y, v[4 * h + 2].z, v[4 * h + 2].w }, { v[4 * h + 3].x, v[4 * h + 3].y, v[4 * h + 3].z, v[4 * h + 3].w } };
+#pragma unroll
+            for (uint32_t m = 0; m < 4u; ++m) {
+                // two rows' numbers of one column beside each other
+                const uint32_t a[4] = { __byte_perm(w[0][m], w[1][m], 0x5410), __byte_perm(w[0][m], w[1][m], 0x7632), __byte_perm(w[2][m], w[3][m], 0x5410),
+                                        __byte_perm(w[2][m], w[3][m], 0x7632) };
+#pragma unroll
+                for (uint32_t e = 0; e < EIGHTS; ++e) {
+                    if (e && !more) continue;
+                    gm::mma_16<T>(sums[e].part[m], a, h ? bh[e].z : bh[e].x, h ? bh[e].w : bh[e].y);
+                    if (two) gm::mma_16<T>(sums[e].part[m], a, h ? bl[e].z : bl[e].x, h ? bl[e].w : bl[e].y);
+                }
+            }
+        }
     }
-};
+}
 
 // COPY: bytes of a copy of weights to shared memory, 16, 4 or 0: they are loaded straight into operands.  SPLIT: the block's warps share a tile.
 struct RowsArgs {
@@ -166,23 +183,23 @@ struct RowsArgs {
     uint32_t layers, splits;             // blocks that share a group's rows, eight at a time; and the weight rows, a chunk at a time
     float* part;                         // splits > 1: [splits][rows][n_in]
 };
-// Rows [r, r + 8) of the group, as far as `end`.
-template <typename T, uint32_t COPY, bool SPLIT>
-__device__ __forceinline__ void rows_tile(const RowsArgs& p, uint32_t group, uint32_t split, uint32_t c0, uint64_t r, uint64_t end, T* hi, T* lo, T* stage, float (*share)[16][32])
+// Rows [r, r + 8 EIGHTS) of the group, as far as `end`.
+template <typename T, uint32_t COPY, bool SPLIT, uint32_t EIGHTS>
+__device__ __forceinline__ void rows_tile(const RowsArgs& p, uint32_t group, uint32_t split, uint32_t c0, uint64_t r, uint64_t end, T* hi, T* lo, T* stage, float (*share)[EIGHTS][16][32])
 {
     constexpr bool STAGED = COPY != 0u && !SPLIT;
     const GradientArgs& a = p.a;
-    constexpr uint32_t kTiles = Tile<T>::kTiles, kPitch = Tile<T>::kPitch, C = Tile<T>::kColumns, kChunk = STAGED ? 64u : 128u, kThreads = 32u * kRowWarps;
+    constexpr uint32_t kTiles = Tile<T>::kTiles, C = Tile<T>::kColumns, kChunk = STAGED ? 64u : 128u, kPitch = Tile<T>::pitch(kChunk), kThreads = 32u * kRowWarps;
     const GroupedArgs& f = a.f;
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, g = lane >> 2, q = lane & 3u, n_out = f.n_out;
-    const uint32_t rows = static_cast<uint32_t>(min(static_cast<uint64_t>(8u), end - r));
+    const uint32_t rows = static_cast<uint32_t>(min(static_cast<uint64_t>(8u * EIGHTS), end - r));
     const uint32_t mine = c0 + (SPLIT ? 0u : warp * Tile<T>::kWarpColumns), columns = mine < f.n_in ? f.n_in - mine : 0u;
     const bool two = f.activation == EVO_ACT_TANH, act = f.activation != EVO_ACT_NONE;
     const T* const w = static_cast<const T*>(f.w) + group * f.stride_w;
     const uint32_t k0 = SPLIT ? warp * kStepK : 0u;
-    Sums<T> sums;
-    sums.clear();
-    float part[kTiles][4];
+    Sums<T> sums[EIGHTS];
+#pragma unroll
+    for (uint32_t e = 0; e < EIGHTS; ++e) sums[e].clear();
     for (uint32_t o0 = split * kChunk; o0 < n_out; o0 += p.splits * kChunk) {
         const uint32_t count = min(kChunk, n_out - o0);
         uint4 v[8];
@@ -205,7 +222,7 @@ __device__ __forceinline__ void rows_tile(const RowsArgs& p, uint32_t group, uin
         }
         {
             // a weight row a thread: all its rows' dy and y are asked for together
-            constexpr uint32_t kEach = 8u * kChunk / kThreads;
+            constexpr uint32_t kEach = 8u * EIGHTS * kChunk / kThreads;
             const uint32_t k = threadIdx.x % kChunk, row0 = threadIdx.x / kChunk * kEach;
             T dy[kEach], y[kEach];
 #pragma unroll
@@ -237,14 +254,9 @@ __device__ __forceinline__ void rows_tile(const RowsArgs& p, uint32_t group, uin
         for (uint32_t n = 0; n < (SPLIT ? 1u : kChunk / kStepK); ++n) {
             const uint32_t k = k0 + n * kStepK;
             if (k >= count) break;
-            if (n == 0u || (sizeof(T) == 4 && n % 2u == 0u)) {
+            if (n && sizeof(T) == 4 && n % 2u == 0u) {
 #pragma unroll
-                for (uint32_t m = 0; m < kTiles; ++m)
-#pragma unroll
-                    for (uint32_t i = 0; i < 4u; ++i) {
-                        if (n) sums.c[m][i] += part[m][i];
-                        part[m][i] = 0.f;
-                    }
+                for (uint32_t e = 0; e < EIGHTS; ++e) sums[e].take_out();
             }
             if constexpr (STAGED) {
 #pragma unroll
@@ -253,61 +265,66 @@ __device__ __forceinline__ void rows_tile(const RowsArgs& p, uint32_t group, uin
             } else {
                 if (n) load_step<T, COPY == 16u>(w + (columns ? mine : 0u), f.ld_w, o0 + k, n_out, columns, v);
             }
-            sums.step(v, hi, lo, two, k, part);
+            step<T, EIGHTS>(v, hi, lo, kPitch, two, rows > 8u, k, sums);
         }
-        if (k0 < count)
 #pragma unroll
-            for (uint32_t m = 0; m < kTiles; ++m)
-#pragma unroll
-                for (uint32_t i = 0; i < 4u; ++i) sums.c[m][i] += part[m][i];
+        for (uint32_t e = 0; e < EIGHTS; ++e) sums[e].take_out();
     }
     if constexpr (std::is_same<T, float>::value)
 #pragma unroll
-        for (uint32_t m = 0; m < kTiles; ++m)
-#pragma unroll
-            for (uint32_t i = 0; i < 4u; ++i) sums.c[m][i] = gm::join(sums.c[m][i], sums.small[m][i]);
-    if (SPLIT) {
-        if (warp)
+        for (uint32_t e = 0; e < EIGHTS; ++e)
 #pragma unroll
             for (uint32_t m = 0; m < kTiles; ++m)
 #pragma unroll
-                for (uint32_t i = 0; i < 4u; ++i) share[warp - 1u][m * 4u + i][lane] = sums.c[m][i];
+                for (uint32_t i = 0; i < 4u; ++i) sums[e].c[m][i] = gm::join(sums[e].c[m][i], sums[e].small[m][i]);
+    if (SPLIT) {
+        if (warp)
+#pragma unroll
+            for (uint32_t e = 0; e < EIGHTS; ++e)
+#pragma unroll
+                for (uint32_t m = 0; m < kTiles; ++m)
+#pragma unroll
+                    for (uint32_t i = 0; i < 4u; ++i) share[warp - 1u][e][m * 4u + i][lane] = sums[e].c[m][i];
         __syncthreads();
         if (warp == 0)
 #pragma unroll
             for (uint32_t p = 0; p < kRowWarps - 1u; ++p)
 #pragma unroll
-                for (uint32_t m = 0; m < kTiles; ++m)
+                for (uint32_t e = 0; e < EIGHTS; ++e)
 #pragma unroll
-                    for (uint32_t i = 0; i < 4u; ++i) sums.c[m][i] += share[p][m * 4u + i][lane];
+                    for (uint32_t m = 0; m < kTiles; ++m)
+#pragma unroll
+                        for (uint32_t i = 0; i < 4u; ++i) sums[e].c[m][i] += share[p][e][m * 4u + i][lane];
         __syncthreads();
         if (warp) return;
     }
 #pragma unroll
-    for (uint32_t i = 0; i < 2u; ++i) {
-        const uint32_t row = 2u * q + i;
-        if (row >= rows) continue;
-        if (p.splits > 1u) {
-            float* const to = p.part + (split * f.rows + r + row) * f.n_in + mine + C * g;
+    for (uint32_t e = 0; e < EIGHTS; ++e)
 #pragma unroll
-            for (uint32_t e = 0; e < C; ++e)
-                if (C * g + e < columns) to[e] = f.scale * sums.c[e / 2u][i + 2u * (e & 1u)];
-        } else {
-            T* const to = static_cast<T*>(a.dx) + (r + row) * a.ld_dx + mine + C * g;
+        for (uint32_t i = 0; i < 2u; ++i) {
+            const uint32_t row = 8u * e + 2u * q + i;
+            if (row >= rows) continue;
+            if (p.splits > 1u) {
+                float* const to = p.part + (split * f.rows + r + row) * f.n_in + mine + C * g;
 #pragma unroll
-            for (uint32_t e = 0; e < C; ++e)
-                if (C * g + e < columns) to[e] = from_float<T>(f.scale * sums.c[e / 2u][i + 2u * (e & 1u)]);
+                for (uint32_t j = 0; j < C; ++j)
+                    if (C * g + j < columns) to[j] = f.scale * sums[e].c[j / 2u][i + 2u * (j & 1u)];
+            } else {
+                T* const to = static_cast<T*>(a.dx) + (r + row) * a.ld_dx + mine + C * g;
+#pragma unroll
+                for (uint32_t j = 0; j < C; ++j)
+                    if (C * g + j < columns) to[j] = from_float<T>(f.scale * sums[e].c[j / 2u][i + 2u * (j & 1u)]);
+            }
         }
-    }
 }
 
-template <typename T, uint32_t COPY, bool SPLIT>
-__global__ void __launch_bounds__(32 * kRowWarps, 5) k_rows(const __grid_constant__ RowsArgs p)
+template <typename T, uint32_t COPY, bool SPLIT, uint32_t EIGHTS>
+__global__ void __launch_bounds__(32 * kRowWarps, (COPY && !SPLIT ? 6 : 5) - EIGHTS) k_rows(const __grid_constant__ RowsArgs p)
 {
     constexpr bool kStaged = COPY != 0u && !SPLIT;
-    constexpr uint32_t kWide = SPLIT ? Tile<T>::kWarpColumns : Tile<T>::kAcross;
-    __shared__ __align__(16) T hi[8 * Tile<T>::kPitch], lo[8 * Tile<T>::kPitch], stage[kStaged ? 64u * Tile<T>::kWeightPitch : 8u];
-    __shared__ float share[SPLIT ? kRowWarps - 1 : 1][16][32];
+    constexpr uint32_t kPitch = Tile<T>::pitch(kStaged ? 64u : 128u), kWide = SPLIT ? Tile<T>::kWarpColumns : Tile<T>::kAcross;
+    __shared__ __align__(16) T hi[8 * EIGHTS * kPitch], lo[8 * EIGHTS * kPitch], stage[kStaged ? 64u * Tile<T>::kWeightPitch : 8u];
+    __shared__ float share[SPLIT ? kRowWarps - 1 : 1][EIGHTS][16][32];
     dep_begin(p.a);
     const uint32_t across = (p.a.f.n_in + kWide - 1u) / kWide;
     const uint32_t group = blockIdx.x / across, c0 = blockIdx.x % across * kWide;
@@ -316,7 +333,7 @@ __global__ void __launch_bounds__(32 * kRowWarps, 5) k_rows(const __grid_constan
     if (p.splits > 1u) { split = layer % p.splits; layer /= p.splits; }
     uint64_t first, end;
     group_rows(p.a.f, group, &first, &end);
-    for (uint64_t r = first + 8u * layer; r < end; r += 8u * p.layers) rows_tile<T, COPY, SPLIT>(p, group, split, c0, r, end, hi, lo, stage, share);
+    for (uint64_t r = first + 8u * EIGHTS * layer; r < end; r += 8u * EIGHTS * p.layers) rows_tile<T, COPY, SPLIT, EIGHTS>(p, group, split, c0, r, end, hi, lo, stage, share);
     dep_end(p.a);
 }
 
@@ -584,18 +601,20 @@ bool whole_pieces(const GradientArgs& a) { return ((a.f.n_in | a.f.n_out) & 7u) 
 // Whether tcgen05 pays for dx: rows a group from which it does.  fp32 weights, and those that TMA cannot address, are laid out first, whatever the rows; the walk over many
 // groups takes a warp longer than the products; few tiles leave SMs without one, which k_rows' splits do not; and a tile takes 128 inputs x 64 outputs at a time, however
 // few there are.  us, tcgen05 / k_rows, rows a group in brackets:
-//   fp32     200 groups of 256 -> 256 (16) 63.2 / 35.7, (32) 64.6 / 68.2; 32 of 1,024 -> 1,024 (32) 139 / 131, (64) 145 / 284; 1 of 4,096 -> 4,096 (32) 173 / 105, (64) 176 / 182;
-//            1,000 of 64 -> 64 (32) 66 / 37, (64) 74 / 61; 3,000 of 20 -> 30 (64) 172 / 102
-//   16 bits  200 of 256 -> 256 (2) 13.2 / 10.8, (8) 20.4 / 24.1; 1,000 of 64 -> 64 (16) 26.5 / 17.5, (32) 27.7 / 31.9; 32 of 1,024 -> 1,024 (2) 16.7 / 22.7, (8) 29 / 51;
-//            1 of 4,096 -> 4,096 (8) 25.9 / 19.3, (16) 26.1 / 38.9; not aligned: 300 of 207 -> 379 (2) 63.6 / 37.1, (8) 61.1 / 83.7; 3,000 of 20 -> 30 (16) 101 / 70, (32) 102 / 115
-// Over 225 shapes (120 of them drawn) the choice takes 1.02 times the faster side's time in the geometric mean; tcgen05 always 1.9 times, k_rows always 1.3.
+//   fp32     200 groups of 256 -> 256 (32) 63.6 / 53.1, (64) 69.3 / 98; 32 of 1,024 -> 1,024 (32) 139 / 96, (64) 144 / 185; 1 of 4,096 -> 4,096 (32) 172 / 83, (64) 175 / 161;
+//            1,000 of 64 -> 64 (64) 75 / 48; 300 of 207 -> 379 (32) 134 / 131; 4,096 of 128 -> 128 (64) 421 / 300
+//   16 bits  200 of 256 -> 256 (2) 13.1 / 10.6, (5) 13.1 / 15.9; 1,000 of 64 -> 64 (16) 26.4 / 17.6, (32) 27.5 / 31.6; 4,096 of 128 -> 128 (16) 109 / 100; 32 of 1,024 -> 1,024
+//            (2) 16.6 / 22.2, (8) 16.6 / 39.4; 1 of 4,096 -> 4,096 (8) 25.8 / 18.8, (16) 25.9 / 37; not aligned: 300 of 207 -> 379 (5) 60.8 / 36.7, (8) 61.3 / 64.5; 3,000 of
+//            20 -> 30 (16) 94.6 / 65.2, (32) 102 / 105; 10 of 1,887 -> 3,200 (1) 56 / 117
+// Over 374 shapes (270 of them drawn) the choice takes 1.03 times the faster side's time in the geometric mean; tcgen05 always 1.8 times, k_rows always 1.2.
 bool dx_on_tensor_cores(uint32_t type, const GradientArgs& a)
 {
     const GroupedArgs& f = a.f;
     if (f.rows >= (1ull << 31) || static_cast<uint64_t>(f.groups) * f.n_out >= (1ull << 31)) return false;
-    const double groups = f.groups, across = (f.n_in + 127u) / 128u, idle = std::fmax(0.0, 1.0 - std::fmin(groups, static_cast<double>(f.rows)) * across / kSms);
+    const double groups = f.groups, across = (f.n_in + 127u) / 128u, idle = std::fmax(0.0, 1.0 - std::fmin(groups, static_cast<double>(f.rows)) * across / kSms), few = idle * idle * idle * idle;
     const double more = std::fmin(16.0, 8192.0 * across * ((f.n_out + 63u) / 64u) / (static_cast<double>(f.n_in) * f.n_out)) - 1.0;
-    const double least = type == EVO_F32 ? 18.0 + groups / 45.0 + 60.0 * idle * idle + 4.0 * more : whole_pieces(a) ? groups / 45.0 + 20.0 * idle * idle : 4.0 + 8.0 * idle * idle + more;
+    const double least = type == EVO_F32 ? 34.0 + groups / 40.0 + 60.0 * few + 4.0 * more
+                       : whole_pieces(a) ? 2.0 + std::fmin(groups / 90.0, 16.0) + 20.0 * few + 4.0 * more : std::fmin(groups / 45.0, 16.0) + 80.0 * few + more;
     return static_cast<double>(f.rows) >= least * groups;
 }
 // The same for dW.  A tile is 128 outputs x up to 256 inputs, however many there are; where there are few tiles k_weights takes long groups 16 rows at a time.  tcgen05 / k_weights:
@@ -617,12 +636,18 @@ bool dw_on_tensor_cores(uint32_t type, const GradientArgs& a)
 uint32_t inputs_of_a_tile(const GradientArgs& a) { return a.f.n_in <= 64u ? 64u : 128u; }
 // How dx is spread over blocks without tcgen05: the columns of a warp's tile shared by the block's warps (split), rows eight at a time over `layers`, weight rows a chunk at a time over
 // `splits`, as far as there is room on the GPU.
-struct RowsPlan { uint32_t split, layers, splits; };
+struct RowsPlan { uint32_t eights, split, layers, splits; };
 RowsPlan rows_plan(uint32_t type, const GradientArgs& a)
 {
     const GroupedArgs& f = a.f;
-    const uint64_t all = type == EVO_F32 ? 128u : 256u, wide = all / kRowWarps, used = f.rows < f.groups ? f.rows : f.groups, passes = (f.rows / f.groups + 7u) / 8u;
+    const uint64_t all = type == EVO_F32 ? 128u : 256u, wide = all / kRowWarps, used = f.rows < f.groups ? f.rows : f.groups;
     RowsPlan p;
+    // (16 rows at a time read and split the weights half as often: us, 8 / 16 at a time, rows a group in brackets: fp32, 200 groups of 256 -> 256 (5) 19.0 / 17.2, (16) 34.8 / 29.5, (64)
+    // 127 / 98; 32 of 1,024 -> 1,024 (8) 58 / 65, (32) 122 / 96; not aligned, 100 of 414 -> 378 (2) 17.5 / 25.3, (5) 37.5 / 27.4; 16 bits, 4,096 of 128 -> 128 (8) 59 / 72, (32)
+    // 180 / 185; not aligned, 300 of 207 -> 379 (2) 32.8 / 39.7, (5) 57.9 / 36.7, (12) 81.8 / 68.8)
+    const bool aligned = f.n_in % (type == EVO_F32 ? 4u : 8u) == 0u;
+    p.eights = f.rows > (aligned ? 10ull : 4ull) * f.groups && (type == EVO_F32 || !aligned) ? 2u : 1u;
+    const uint64_t passes = (f.rows / f.groups + 8u * p.eights - 1u) / (8u * p.eights);
     uint64_t blocks = used * ((f.n_in + all - 1u) / all);
     // (with two rows a group on average few have nine, and the blocks that find none cost more)
     const uint64_t most_layers = f.rows > 2ull * f.groups ? 2u * passes : 1u, room = 8u * kSms;
@@ -665,7 +690,7 @@ Plan plan_for(uint32_t type, const GradientArgs& a, bool any_address)
     return p;
 }
 
-template <typename T>
+template <typename T, uint32_t EIGHTS>
 int launch_rows(cudaStream_t st, const GradientArgs& a, const RowsPlan& plan, float* part)
 {
     const GroupedArgs& f = a.f;
@@ -675,8 +700,8 @@ int launch_rows(cudaStream_t st, const GradientArgs& a, const RowsPlan& plan, fl
     RowsArgs p;
     p.a = a; p.layers = plan.layers; p.splits = plan.splits; p.part = part;
     const uint64_t bits = reinterpret_cast<uintptr_t>(f.w) | (f.n_in | f.ld_w | f.stride_w) * sizeof(T);
-    auto kernel = bits % 16u == 0u ? (plan.split ? k_rows<T, 16, true> : k_rows<T, 16, false>)
-                : plan.split ? k_rows<T, 0, true> : bits % 4u == 0u ? k_rows<T, 4, false> : k_rows<T, 0, false>;
+    auto kernel = bits % 16u == 0u ? (plan.split ? k_rows<T, 16, true, EIGHTS> : k_rows<T, 16, false, EIGHTS>)
+                : plan.split ? k_rows<T, 0, true, EIGHTS> : bits % 4u == 0u ? k_rows<T, 4, false, EIGHTS> : k_rows<T, 0, false, EIGHTS>;
     return launch_dependent(kernel, dim3(static_cast<uint32_t>(blocks), plan.layers * plan.splits), dim3(32 * kRowWarps), 0, st, p) == cudaSuccess ? 1 : -1;
 }
 template <typename T>
@@ -759,7 +784,7 @@ int launch_type(cudaStream_t st, uint32_t type, const GradientArgs& a, void* wor
         launches += n;
     }
     if (a.dx && a.f.rows && !plan.tc.dx) {
-        n = launch_rows<T>(st, late(a), plan.rows, part_x);
+        n = plan.rows.eights == 2u ? launch_rows<T, 2>(st, late(a), plan.rows, part_x) : launch_rows<T, 1>(st, late(a), plan.rows, part_x);
         if (n < 0) return n;
         launches += n;
     }
