@@ -364,25 +364,25 @@ struct WeightsArgs {
     uint32_t all, sets, splits, out_tiles, in_tiles;
     float* part_w; float* part_b;                            // [splits][sets][n_out][n_in], [splits][sets][n_out]
 };
-constexpr uint32_t kTile = 64, kStep = 16;                   // outputs of a tile, rows at a time
+constexpr uint32_t kStep = 16;                               // rows at a time
 
-// Tiles of 64 outputs x TI inputs; a thread has 4 inputs (side by side with VEC, where four can be stored together) of TI / 16 outputs.
-template <typename T, uint32_t TI, bool VEC>
+// Tiles of TO outputs x TI inputs; a thread has 4 inputs (side by side with VEC, where four can be stored together) of TO TI / 1,024 outputs.
+template <typename T, uint32_t TO, uint32_t TI, bool VEC>
 __global__ void __launch_bounds__(256, 4) k_weights(const __grid_constant__ WeightsArgs p)
 {
-    constexpr uint32_t kAcross = TI / 4u, kEach = TI / 16u;
-    __shared__ __align__(16) float dz[kStep][kTile], xs[kStep][TI];
+    constexpr uint32_t kAcross = TI / 4u, kEach = TO * TI / 1024u;
+    __shared__ __align__(16) float dz[kStep][TO], xs[kStep][TI];
     const GradientArgs& a = p.a;
     dep_begin(a);
     const uint32_t n_in = a.f.n_in, n_out = a.f.n_out;
     uint32_t at = blockIdx.x;
     const uint32_t i0 = at % p.in_tiles * TI; at /= p.in_tiles;
-    const uint32_t o0 = at % p.out_tiles * kTile; at /= p.out_tiles;
+    const uint32_t o0 = at % p.out_tiles * TO; at /= p.out_tiles;
     const uint32_t split = at % p.splits, set = at / p.splits;
     uint64_t r, end;
     set_rows(a, p.all, set, split, p.splits, &r, &end);
     const uint32_t tx = threadIdx.x % kAcross, ty = threadIdx.x / kAcross;
-    const bool bias = a.db && i0 == 0u && threadIdx.x < kTile;
+    const bool bias = a.db && i0 == 0u && threadIdx.x < TO;
     float sum[kEach][4] = {}, sum_b = 0.f;
     for (; r < end; r += kStep) {
         const uint32_t rows = end - r < kStep ? static_cast<uint32_t>(end - r) : kStep;
@@ -390,29 +390,30 @@ __global__ void __launch_bounds__(256, 4) k_weights(const __grid_constant__ Weig
         // those of the other twelve).
         auto stage = [&](auto fours) {
             constexpr uint32_t D = decltype(fours)::value;
-            T dy[D], y[D], x[D * TI / 64u];
-            const uint32_t o = o0 + threadIdx.x % kTile, i = i0 + threadIdx.x % TI;
+            constexpr uint32_t kZ = (4u * D * TO + 255u) / 256u, kX = (4u * D * TI + 255u) / 256u;
+            T dy[kZ], y[kZ], x[kX];
+            const uint32_t o = o0 + threadIdx.x % TO, i = i0 + threadIdx.x % TI;
 #pragma unroll
-            for (uint32_t k = 0; k < D; ++k) {
-                const uint32_t row = threadIdx.x / kTile + 4u * k;
+            for (uint32_t k = 0; k < kZ; ++k) {
+                const uint32_t row = threadIdx.x / TO + 256u / TO * k;
                 if (row < rows && o < n_out) {
                     dy[k] = static_cast<const T*>(a.dy)[(r + row) * a.ld_dy + o];
                     if (a.f.activation != EVO_ACT_NONE) y[k] = static_cast<const T*>(a.f.y)[(r + row) * a.f.ld_y + o];
                 }
             }
 #pragma unroll
-            for (uint32_t k = 0; k < D * TI / 64u; ++k) {
+            for (uint32_t k = 0; k < kX; ++k) {
                 const uint32_t row = threadIdx.x / TI + 256u / TI * k;
                 if (row < rows && i < n_in) x[k] = static_cast<const T*>(a.f.x)[(r + row) * a.f.ld_x + i];
             }
             __syncthreads();
 #pragma unroll
-            for (uint32_t k = 0; k < D; ++k) {
-                const uint32_t row = threadIdx.x / kTile + 4u * k;
-                dz[row][threadIdx.x % kTile] = row < rows && o < n_out ? dz_of(a, to_float(dy[k]), a.f.activation == EVO_ACT_NONE ? 0.f : to_float(y[k])) : 0.f;
+            for (uint32_t k = 0; k < kZ; ++k) {
+                const uint32_t row = threadIdx.x / TO + 256u / TO * k;
+                dz[row][threadIdx.x % TO] = row < rows && o < n_out ? dz_of(a, to_float(dy[k]), a.f.activation == EVO_ACT_NONE ? 0.f : to_float(y[k])) : 0.f;
             }
 #pragma unroll
-            for (uint32_t k = 0; k < D * TI / 64u; ++k) {
+            for (uint32_t k = 0; k < kX; ++k) {
                 const uint32_t row = threadIdx.x / TI + 256u / TI * k;
                 xs[row][threadIdx.x % TI] = row < rows && i < n_in ? to_float(x[k]) : 0.f;
             }
@@ -478,7 +479,7 @@ __global__ void __launch_bounds__(256, 4) k_weights(const __grid_constant__ Weig
     dep_end(a);
 }
 
-// db alone: 32 threads side by side with N columns each, 8 rows at a time.
+// db alone: 256 / R threads side by side with N columns each, R rows at a time.
 struct BiasArgs {
     GradientArgs a;
     uint32_t all, sets, splits, tiles;
@@ -486,18 +487,19 @@ struct BiasArgs {
     const uint16_t* laid;                                    // dz as laid out for the tensor cores, or NULL
     uint32_t parts, pitch;
 };
-template <typename T, uint32_t N>
+template <typename T, uint32_t N, uint32_t R>
 __global__ void __launch_bounds__(256) k_bias(const __grid_constant__ BiasArgs p)
 {
-    __shared__ float sums[8][32 * N];
+    constexpr uint32_t kWide = 256u / R;
+    __shared__ float sums[R][kWide * N];
     const GradientArgs& a = p.a;
     dep_begin(a);
     uint32_t at = blockIdx.x;
-    const uint32_t c0 = at % p.tiles * 32u * N; at /= p.tiles;
+    const uint32_t c0 = at % p.tiles * kWide * N; at /= p.tiles;
     const uint32_t split = at % p.splits, set = at / p.splits;
     uint64_t first, end;
     set_rows(a, p.all, set, split, p.splits, &first, &end);
-    const uint32_t c = c0 + threadIdx.x % 32u * N, n_out = a.f.n_out;
+    const uint32_t c = c0 + threadIdx.x % kWide * N, n_out = a.f.n_out;
     const bool act = a.f.activation != EVO_ACT_NONE;
     float sum[N] = {};
     if (p.laid) {                                            // dz / scale is there, in parts (N 8: aligned)
@@ -505,10 +507,10 @@ __global__ void __launch_bounds__(256) k_bias(const __grid_constant__ BiasArgs p
         const uint64_t rows = (end > first ? end - first : 0u) * p.parts;               // (the parts of a row lie one behind the other, like rows)
         const uint16_t* const from = p.laid + first * p.parts * p.pitch + c;
         if (c < n_out)
-            for (uint64_t r = threadIdx.x / 32u; r < rows; r += 8u * kAsk) {
+            for (uint64_t r = threadIdx.x / kWide; r < rows; r += R * kAsk) {
                 uint4 u[kAsk];
 #pragma unroll
-                for (uint32_t k = 0; k < kAsk; ++k) u[k] = r + 8u * k < rows ? __ldg(reinterpret_cast<const uint4*>(from + (r + 8u * k) * p.pitch)) : make_uint4(0u, 0u, 0u, 0u);
+                for (uint32_t k = 0; k < kAsk; ++k) u[k] = r + R * k < rows ? __ldg(reinterpret_cast<const uint4*>(from + (r + R * k) * p.pitch)) : make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
                 for (uint32_t k = 0; k < kAsk; ++k) {
                     const uint32_t w[4] = { u[k].x, u[k].y, u[k].z, u[k].w };
@@ -524,11 +526,11 @@ __global__ void __launch_bounds__(256) k_bias(const __grid_constant__ BiasArgs p
         for (uint32_t e = 0; e < N; ++e) sum[e] *= a.f.scale;
     } else if (c < n_out) {
         constexpr uint32_t kAsk = N == 1u ? 8u : 4u;
-        for (uint64_t r = first + threadIdx.x / 32u; r < end; r += 8u * kAsk) {
+        for (uint64_t r = first + threadIdx.x / kWide; r < end; r += R * kAsk) {
             T dy[kAsk][N], y[kAsk][N];
 #pragma unroll
             for (uint32_t k = 0; k < kAsk; ++k) {
-                const uint64_t row = r + 8u * k;
+                const uint64_t row = r + R * k;
                 if (row >= end) break;
                 const T* const from = static_cast<const T*>(a.dy) + row * a.ld_dy + c;
                 const T* const from_y = static_cast<const T*>(a.f.y) + row * a.f.ld_y + c;
@@ -543,20 +545,20 @@ __global__ void __launch_bounds__(256) k_bias(const __grid_constant__ BiasArgs p
             }
 #pragma unroll
             for (uint32_t k = 0; k < kAsk; ++k) {
-                if (r + 8u * k >= end) break;
+                if (r + R * k >= end) break;
 #pragma unroll
                 for (uint32_t e = 0; e < N; ++e) sum[e] += dz_of(a, to_float(dy[k][e]), act ? to_float(y[k][e]) : 0.f);
             }
         }
     }
 #pragma unroll
-    for (uint32_t e = 0; e < N; ++e) sums[threadIdx.x / 32u][threadIdx.x % 32u * N + e] = sum[e];
+    for (uint32_t e = 0; e < N; ++e) sums[threadIdx.x / kWide][threadIdx.x % kWide * N + e] = sum[e];
     __syncthreads();
-    for (uint32_t i = threadIdx.x; i < 32u * N; i += 256u) {
+    for (uint32_t i = threadIdx.x; i < kWide * N; i += 256u) {
         if (c0 + i >= n_out) break;
         float s = 0.f;
 #pragma unroll
-        for (uint32_t k = 0; k < 8u; ++k) s += sums[k][i];
+        for (uint32_t k = 0; k < R; ++k) s += sums[k][i];
         if (p.splits > 1u) p.part[(static_cast<uint64_t>(split) * p.sets + set) * n_out + c0 + i] = s;
         else static_cast<T*>(a.db)[set * a.stride_db + c0 + i] = from_float<T>(s);
     }
@@ -622,7 +624,7 @@ bool dx_on_tensor_cores(uint32_t type, const GradientArgs& a)
 //            1,000 of 64 -> 64 (64) 74 / 46; 7 of 171 -> 7 (107) 20.8 / 47.4
 //   16 bits  200 of 256 -> 256 (2) 10.0 / 10.9; 1,000 of 64 -> 64 (8) 17.3 / 9.7, (16) 12.0 / 15.4, (32) 13.1 / 26.4; 4 of 2,048 -> 2,048 (2) 17.6 / 11.1, (8) 17.5 / 19.5;
 //            not aligned: 300 of 207 -> 379 (8) 32.6 / 40.5; 3,000 of 20 -> 30 (32) 71 / 51, (64) 112 / 92
-// Over the same shapes 1.01 times the faster side's time; tcgen05 always 1.6 times, k_weights always 1.4.
+// Over the same shapes 1.02 times the faster side's time; tcgen05 always 1.7 times, k_weights always 1.3.
 bool dw_on_tensor_cores(uint32_t type, const GradientArgs& a)
 {
     const GroupedArgs& f = a.f;
@@ -633,7 +635,17 @@ bool dw_on_tensor_cores(uint32_t type, const GradientArgs& a)
     if (tiles * sets < kSms) least = std::fmin(least, 48.0);
     return static_cast<double>(f.rows) >= least * sets;
 }
-uint32_t inputs_of_a_tile(const GradientArgs& a) { return a.f.n_in <= 64u ? 64u : 128u; }
+// A tile of k_weights: where there are few outputs (a policy's actions) or few inputs, most of a square one would be nothing.  fp32, us, square / narrow: 320
+// groups of 137 -> 7, 9,292 rows 30.7 / 16.9; 1,000 of 256 -> 16, 32,000 rows 58.5 / 27.2; 2,000 of 16 -> 256, a row each 24.9 / 10.8; but long groups are better served by more
+// tiles: 64 of 4 -> 128, 60,000 rows 170 / 286.
+struct Shape { uint32_t outputs, inputs; };
+Shape tile_of(const GradientArgs& a)
+{
+    if (a.f.n_out <= 16u && a.f.n_in > 64u) return { 16u, 256u };
+    if (a.f.n_in <= 16u && a.f.n_out > 64u && a.f.rows <= 16ull * a.f.groups) return { 256u, 16u };
+    return { 64u, a.f.n_in <= 64u ? 64u : 128u };
+}
+uint64_t tiles_of(uint64_t n, uint32_t each) { return (n + each - 1u) / each; }
 // How dx is spread over blocks without tcgen05: the columns of a warp's tile shared by the block's warps (split), rows eight at a time over `layers`, weight rows a chunk at a time over
 // `splits`, as far as there is room on the GPU.
 struct RowsPlan { uint32_t eights, split, layers, splits; };
@@ -675,10 +687,10 @@ size_t padded(size_t n) { return (n + 255u) / 256u * 256u; }
 Plan plan_for(uint32_t type, const GradientArgs& a, bool any_address)
 {
     Plan p;
-    const uint64_t out_tiles = (a.f.n_out + kTile - 1u) / kTile, in_tiles = (a.f.n_in + inputs_of_a_tile(a) - 1u) / inputs_of_a_tile(a);
+    const Shape tile = tile_of(a);
     const bool dx = a.dx && a.f.rows && dx_on_tensor_cores(type, a), dw = a.dw && a.f.rows && dw_on_tensor_cores(type, a);
     p.both = a.dw && !dw && a.db && a.sum_w == a.sum_b;
-    p.w_splits = !a.dw ? 1u : dw ? splits_for(a, a.sum_w, ((a.f.n_out + 127ull) / 128u) * ((a.f.n_in + 255ull) / 256u)) : splits_for(a, a.sum_w, out_tiles * in_tiles);
+    p.w_splits = !a.dw ? 1u : dw ? splits_for(a, a.sum_w, ((a.f.n_out + 127ull) / 128u) * ((a.f.n_in + 255ull) / 256u)) : splits_for(a, a.sum_w, tiles_of(a.f.n_out, tile.outputs) * tiles_of(a.f.n_in, tile.inputs));
     p.b_splits = p.both ? p.w_splits : a.db ? bias_splits(a) : 1u;
     p.tc = grouped_gradient_tc_plan(type, a, dx, dw, p.w_splits, any_address);
     const uint64_t w_sets = a.sum_w ? 1u : a.f.groups, b_sets = a.sum_b ? 1u : a.f.groups;
@@ -730,14 +742,16 @@ int launch_weights(cudaStream_t st, const GradientArgs& in, bool bias, uint32_t 
     p.all = in.sum_w;
     p.sets = p.all ? 1u : in.f.groups;
     p.splits = splits;
-    p.out_tiles = (in.f.n_out + kTile - 1u) / kTile;
-    const uint32_t wide = inputs_of_a_tile(in);
-    p.in_tiles = (in.f.n_in + wide - 1u) / wide;
+    const Shape tile = tile_of(in);
+    p.out_tiles = static_cast<uint32_t>(tiles_of(in.f.n_out, tile.outputs));
+    p.in_tiles = static_cast<uint32_t>(tiles_of(in.f.n_in, tile.inputs));
     p.part_w = part_w; p.part_b = part_b;
     const uint64_t blocks = static_cast<uint64_t>(p.sets) * splits * p.out_tiles * p.in_tiles;
     if (blocks > 0x7FFFFFFFull) return -2;
     const bool four = in.f.n_in % 4u == 0u && (splits > 1u || (reinterpret_cast<uintptr_t>(in.dw) % (4u * sizeof(T)) == 0u && (in.ld_dw | in.stride_dw) % 4u == 0u));
-    auto kernel = wide == 64u ? (four ? k_weights<T, 64, true> : k_weights<T, 64, false>) : (four ? k_weights<T, 128, true> : k_weights<T, 128, false>);
+    auto kernel = tile.outputs == 16u ? (four ? k_weights<T, 16, 256, true> : k_weights<T, 16, 256, false>)
+                : tile.outputs == 256u ? (four ? k_weights<T, 256, 16, true> : k_weights<T, 256, 16, false>)
+                : tile.inputs == 64u ? (four ? k_weights<T, 64, 64, true> : k_weights<T, 64, 64, false>) : (four ? k_weights<T, 64, 128, true> : k_weights<T, 64, 128, false>);
     return launch_dependent(kernel, dim3(static_cast<uint32_t>(blocks)), dim3(256), 0, st, p) == cudaSuccess ? 1 : -1;
 }
 
@@ -759,10 +773,12 @@ int launch_bias(cudaStream_t st, const GradientArgs& in, uint32_t splits, float*
     p.laid = tc.lay_dz ? static_cast<const uint16_t*>(work) : nullptr;      // (the first of the workspace)
     p.parts = tc.dz_parts; p.pitch = tc.pitch_dz;
     const uint32_t n = p.laid ? 8u : bias_columns<T>(in);
-    p.tiles = (in.f.n_out + 32u * n - 1u) / (32u * n);
+    // (many groups of few rows: wide rows one at a time: 1,095 of 1,597, 17 rows in all 62 -> 10.6 us, 4,096 of 512, a row each 31 -> 10.6)
+    const bool one = splits == 1u && in.f.rows <= 4ull * p.sets && in.f.n_out > 32u * n;
+    p.tiles = static_cast<uint32_t>(tiles_of(in.f.n_out, (one ? 256u : 32u) * n));
     const uint64_t blocks = static_cast<uint64_t>(p.sets) * splits * p.tiles;
     if (blocks > 0x7FFFFFFFull) return -2;
-    auto kernel = n == 1u ? k_bias<T, 1> : n == 4u ? k_bias<T, 4> : k_bias<T, 8>;
+    auto kernel = one ? (n == 1u ? k_bias<T, 1, 1> : n == 4u ? k_bias<T, 4, 1> : k_bias<T, 8, 1>) : n == 1u ? k_bias<T, 1, 8> : n == 4u ? k_bias<T, 4, 8> : k_bias<T, 8, 8>;
     return launch_dependent(kernel, dim3(static_cast<uint32_t>(blocks)), dim3(256), 0, st, p) == cudaSuccess ? 1 : -1;
 }
 

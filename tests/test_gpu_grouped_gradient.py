@@ -119,6 +119,19 @@ def test_few_rows_whatever_the_groups_and_the_alignment(dtype, groups, lengths, 
         assert (wide[0] == 7).all() and (wide[-2:] == 7).all() and (wide[:, 0] == 7).all() and (wide[:, n_in + 1:] == 7).all()
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("n_in,n_out", [(300, 7), (65, 16), (512, 1), (137, 15), (12, 300), (16, 65), (1, 520), (7, 257)])
+@pytest.mark.parametrize("lengths", [[i % 4 for i in range(40)], [0] * 30 + [2], [17, 40, 0, 3], [2000, 5]])
+def test_few_outputs_and_few_inputs(dtype, n_in, n_out, lengths):
+    for act, scale in (("none", -1.5), ("tanh", 1.0)):
+        dy, x, w, off, y = make(len(lengths), lengths, n_in, n_out, dtype, act, scale, lead=3)
+        check(dy, x, w, off, y, act, scale)
+        _, _, db = grouped_linear_backward(dy, None, w, off, y, activation=act, scale=scale, wanted=(False, False, True))       # (by itself: not a part of dW's kernel)
+        edges = off.tolist()
+        (_, _), (_, _), (eb, sb) = exact(dy, x, w, off, y, act, scale)
+        close(db, eb, sb, max(q - p for p, q in zip(edges[:-1], edges[1:])))
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("n_in,n_out,shift", [(64, 48, 0), (64, 48, 1), (61, 48, 0), (256, 136, 3), (256, 136, 8)])
 @pytest.mark.parametrize("lengths", [[3, 0, 20, 90, 1], [200, 64, 0, 130, 500]])
