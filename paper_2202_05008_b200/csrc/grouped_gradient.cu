@@ -603,20 +603,21 @@ bool whole_pieces(const GradientArgs& a) { return ((a.f.n_in | a.f.n_out) & 7u) 
 // Whether tcgen05 pays for dx: rows a group from which it does.  fp32 weights, and those that TMA cannot address, are laid out first, whatever the rows; the walk over many
 // groups takes a warp longer than the products; few tiles leave SMs without one, which k_rows' splits do not; and a tile takes 128 inputs x 64 outputs at a time, however
 // few there are.  us, tcgen05 / k_rows, rows a group in brackets:
-//   fp32     200 groups of 256 -> 256 (32) 63.6 / 53.1, (64) 69.3 / 98; 32 of 1,024 -> 1,024 (32) 139 / 96, (64) 144 / 185; 1 of 4,096 -> 4,096 (32) 172 / 83, (64) 175 / 161;
+//   fp32     200 groups of 256 -> 256 (32) 63.6 / 53.1, (64) 69.3 / 98; 32 of 1,024 -> 1,024 (32) 139 / 88, (64) 144 / 163; 1 of 4,096 -> 4,096 (64) 175 / 127;
 //            1,000 of 64 -> 64 (64) 75 / 48; 300 of 207 -> 379 (32) 134 / 131; 4,096 of 128 -> 128 (64) 421 / 300
 //   16 bits  200 of 256 -> 256 (2) 13.1 / 10.6, (5) 13.1 / 15.9; 1,000 of 64 -> 64 (16) 26.4 / 17.6, (32) 27.5 / 31.6; 4,096 of 128 -> 128 (16) 109 / 100; 32 of 1,024 -> 1,024
-//            (2) 16.6 / 22.2, (8) 16.6 / 39.4; 1 of 4,096 -> 4,096 (8) 25.8 / 18.8, (16) 25.9 / 37; not aligned: 300 of 207 -> 379 (5) 60.8 / 36.7, (8) 61.3 / 64.5; 3,000 of
+//            (2) 16.6 / 22.2, (8) 16.6 / 39.4; 1 of 4,096 -> 4,096 (10) 25.8 / 24.1, (64) 26 / 75; not aligned: 300 of 207 -> 379 (5) 60.8 / 36.7, (8) 61.3 / 64.5; 3,000 of
 //            20 -> 30 (16) 94.6 / 65.2, (32) 102 / 105; 10 of 1,887 -> 3,200 (1) 56 / 117
-// Over 374 shapes (270 of them drawn) the choice takes 1.03 times the faster side's time in the geometric mean; tcgen05 always 1.8 times, k_rows always 1.2.
+// Over 374 shapes (270 of them drawn) the choice takes 1.03 times the faster side's time in the geometric mean; tcgen05 always 1.8 times, k_rows always 1.16.
 bool dx_on_tensor_cores(uint32_t type, const GradientArgs& a)
 {
     const GroupedArgs& f = a.f;
     if (f.rows >= (1ull << 31) || static_cast<uint64_t>(f.groups) * f.n_out >= (1ull << 31)) return false;
     const double groups = f.groups, across = (f.n_in + 127u) / 128u, idle = std::fmax(0.0, 1.0 - std::fmin(groups, static_cast<double>(f.rows)) * across / kSms), few = idle * idle * idle * idle;
-    const double more = std::fmin(16.0, 8192.0 * across * ((f.n_out + 63u) / 64u) / (static_cast<double>(f.n_in) * f.n_out)) - 1.0;
-    const double least = type == EVO_F32 ? 34.0 + groups / 40.0 + 60.0 * few + 4.0 * more
-                       : whole_pieces(a) ? 2.0 + std::fmin(groups / 90.0, 16.0) + 20.0 * few + 4.0 * more : std::fmin(groups / 45.0, 16.0) + 80.0 * few + more;
+    const double size = static_cast<double>(f.n_in) * f.n_out, more = std::fmin(16.0, 8192.0 * across * ((f.n_out + 63u) / 64u) / size) - 1.0;
+    const double least = type == EVO_F32 ? 34.0 + groups / 40.0 + 120.0 * few + 4.0 * more
+                       : whole_pieces(a) ? 2.0 + std::fmin(groups / 60.0, 16.0) + 80.0 * few + more
+                       : 8.0 * std::fmin(1.0, 3e5 / size) + std::fmin(groups / 60.0, 16.0) + 160.0 * few * std::fmin(1.0, 1e5 / size) + 2.0 * more;
     return static_cast<double>(f.rows) >= least * groups;
 }
 // The same for dW.  A tile is 128 outputs x up to 256 inputs, however many there are; where there are few tiles k_weights takes long groups 16 rows at a time.  tcgen05 / k_weights:
@@ -670,7 +671,9 @@ RowsPlan rows_plan(uint32_t type, const GradientArgs& a)
     if (p.split) blocks = used * ((f.n_in + wide - 1u) / wide);
     const uint64_t chunks = (f.n_out + (p.split ? 127u : 63u)) / (p.split ? 128u : 64u);
     uint64_t splits = 1;
-    if (blocks * layers < 2u * kSms && chunks > 2u) splits = 4u * kSms / (blocks * layers + 1u);
+    // (a block waits most of the time, for one chunk after the other: more of them than fit at a time, us with 4 / 8 / 16 an SM: fp32, 10 groups of 1,887 -> 3,200, 23 rows each
+    // 387 / 383 / 195; 32 of 1,024 -> 1,024, 10 rows each 54 / 54 / 43; 1 of 4,096 -> 4,096, 10 rows 61 / 39 / 39)
+    if (chunks > 2u) splits = 16u * kSms / (blocks * layers + 1u);
     splits = splits > chunks / 2u ? chunks / 2u : splits;
     p.layers = static_cast<uint32_t>(layers < 1u ? 1u : layers);
     p.splits = static_cast<uint32_t>(splits < 2u ? 1u : splits > 32u ? 32u : splits);
