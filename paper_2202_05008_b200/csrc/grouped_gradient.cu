@@ -1,9 +1,9 @@
 // Gradients of the products grouped by member: dx[r] = W_g' dz[r], dW_g = sum_r dz[r] x[r]', db_g = sum_r dz[r]; any type, size, stride and alignment.
 //
 // A group of a population has few rows and weights of its own: dx is bound by the weights' way from memory, dW by its own way there.  k_rows reads
-// a group's weights once for up to 8 rows; k_weights makes tiles of 64 outputs x 64 or 128 inputs.  Where there are too few tiles for the
-// GPU and many rows, the rows are split and the parts added up in a fixed order.  4,096 members of 128 x 128, 16,384 ragged rows, fp32: k_rows 60 us (4.7 TB/s; reading the
-// weights alone is 41), k_weights 80 (its stores alone 40; the rest is what a block waits for before it stores), all together, overlapped, 137.
+// a group's weights once for up to 8 or 16 rows; k_weights makes tiles of 64 outputs x 64 or 128 inputs, or narrow ones.  Where there are too few tiles for the
+// GPU, what is summed over (dx: weight rows, dW and db: rows) is split and the parts added up in a fixed order.  4,096 members of 128 x 128, 16,384 ragged rows, fp32: k_rows 60 us (4.7 TB/s; reading the
+// weights alone is 41), k_weights 80 (its stores alone 40; the rest is what a block waits for before it stores), all together, overlapped, 138.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -42,11 +42,12 @@ __device__ __forceinline__ void store4(T* p, const float (&v)[4])
 }
 
 // ---- dx ----
-// Warp-level products: the columns of the weights are the MMA's first operand, 16 bytes of them a lane (a warp has 32 of fp32, 64 of 16 bits), and 8 of a
+// Warp-level products: the columns of the weights are the MMA's first operand, 16 bytes of them a lane (a warp has 32 of fp32, 64 of 16 bits), and 8 or 16 of a
 // group's rows the second.  A lane takes pieces of eight weight rows into what becomes operand registers; the order of the contracted index is free as
 // long as both operands share it.  fp32 numbers are two tf32 numbers each, dz of 16-bit types is one or two numbers (hi and lo), split once where it is staged in shared memory.
 // The tensor core cuts its sums off, so they are taken out every 64 (fp32) or 128 weight rows and added up in fp32.
-// What counts is that enough weights are under way: where they are aligned, 64 of their rows x 512 bytes are copied to shared memory asynchronously, five blocks an SM.
+// What counts is that enough weights are under way: where they are aligned, 64 of their rows x 512 bytes are copied to shared memory asynchronously, five blocks an SM (four
+// with 16 rows at a time).  Further rows are other blocks' (layers), and so are, in a group of few tiles, parts of a long column of weights (splits).
 // Where there are too few tiles for the GPU a block's warps share one and split the weight rows.
 constexpr uint32_t kRowWarps = 4, kStepK = 32;
 
