@@ -150,6 +150,16 @@ def test_one_action_that_is_allowed_and_extremes(n):
     assert (got.logp + math.log(n)).abs().max() < 1e-5 and got.gradient.isfinite().all()
 
 
+@pytest.mark.parametrize("n,each", [(12, 128), (50, 64), (100, 32), (200, 16)])
+def test_rows_of_one_block_of_a_cluster_of_them_and_more(n, each):
+    for rows in (1, each - 1, each, each + 1, 2 * each + 1, 4 * each, 5 * each + 3, 8 * each - 1, 8 * each, 8 * each + 1, 9 * each):
+        logits, actions, old, adv, ref, weights = make(rows, n, F32, wide=rows % 2 == 0)
+        got = check(logits, actions, old, adv, ref, weights, kl=0.05)
+        again = policy_loss(logits, actions, old, adv, ref_logp=ref, weights=weights, clip=(0.2, 0.3), kl=0.05, gradient=False)
+        assert torch.equal(got.loss, again.loss) and torch.equal(got.logp, again.logp)
+        check(logits, actions, old, adv)
+
+
 def test_no_rows_and_one():
     empty = torch.zeros(0, 9, device="cuda")
     none = torch.zeros(0, device="cuda")
