@@ -3,8 +3,8 @@
 // All three go by the rows of the unsorted side, so that each of them is read or written once, and the sorted rows that it has are found by
 // their places.  A row is `lanes` threads' (a power of two up to a block), each with every lanes-th piece of 16 bytes.  Bound by memory: no number is moved twice.
 // Rows of bf16: take of 32,768 x 2,048 for four choices 101 us, 6.5 TB/s; combine of 40,000 x 2,048, two choices, 86 us, 5.6 TB/s; its gradient, 16,384 x 1,024, eight
-// choices, 99 us, 5.7 TB/s; fp16, 5,003 x 1,001, three choices, where no two rows begin alike, 18.5 us,
-// 3.6 TB/s.
+// choices, 99 us, 5.7 TB/s; fp16, 5,003 x 1,001, three choices, where no two rows begin alike, 17.1 us,
+// 3.9 TB/s.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -372,7 +372,7 @@ __global__ void __launch_bounds__(kThreads) k_combine_backward_any(const __grid_
 
 // ---- choices ----
 // kPieces: 16 bytes everywhere; kShort: rows of less than 128 bytes, a number a thread; kAny (5,003 rows of 1,001 numbers of fp16, three choices: take 11.1 us number by number, 9.6 so; combine 26.3, 11.4; its
-// gradient 37.7, 18.5)
+// gradient 37.7, 17.1)
 enum Way { kPieces, kShort, kAny };
 Way way_of(uint32_t size, const RowSetArgs& a)
 {
@@ -432,7 +432,8 @@ int launch_combine_backward(cudaStream_t st, uint32_t type, const RowSetArgs& a)
         using T = decltype(t);
         constexpr uint32_t N = 16u / sizeof(T);
         const Way way = way_of(sizeof(T), a);
-        if (way == kAny) return launch(st, k_combine_backward_any<T>, a, lanes_for(a, N, 2u));
+        // (2 / 4 / 8 pieces a thread, each of two or three loads: 5,003 x 1,001 of fp16, three choices 19.1 / 17.1 / 23 us, 20,000 x 333 of fp32, two 52.6 / 39.1 / 37.8)
+        if (way == kAny) return launch(st, k_combine_backward_any<T>, a, lanes_for(a, N, 4u));
         if (way == kShort) return launch(st, k_combine_backward<T, 1, 4>, a, lanes_for(a, 1u, 1u));
         auto kernel = a.choices == 1u ? k_combine_backward<T, N, 1> : a.choices == 2u ? k_combine_backward<T, N, 2> : k_combine_backward<T, N, 4>;
         return launch(st, kernel, a, lanes_for(a, N, 8u));
