@@ -31,6 +31,7 @@ from .binding import (EVO_MAX_LAYERS, Actions, EvoError, Grouped, GroupedGradien
 
 TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 INVALID_ARG = 1
+_ROW_SETS, _GROUPED, _GROUPED_GRADIENT = C.sizeof(RowSets), C.sizeof(Grouped), C.sizeof(GroupedGradient)
 ACTIVATIONS = {"none": 0, "tanh": 1, "relu": 2}
 COEFFICIENTS = (3.4445, -4.7750, 2.0315)
 _LEAST = math.ulp(0.0)
@@ -303,19 +304,22 @@ def route_rows(members: torch.Tensor, groups: int, *, stream: Optional[torch.cud
     return routes
 
 
-def _row_sets(where: str, rows: torch.Tensor, sorted_rows: torch.Tensor, place: torch.Tensor, weights: Optional[torch.Tensor]) -> RowSets:
-    p = RowSets(C.sizeof(RowSets), TYPES[rows.dtype], place.shape[1] if place.dim() == 2 else 1, rows.shape[1], rows.shape[0], sorted_rows.shape[0],
-                place.data_ptr(), place.stride(0), None, 0, rows.data_ptr(), rows.stride(0), sorted_rows.data_ptr(), sorted_rows.stride(0))
-    if weights is not None:
-        p.d_weights, p.ld_weights = weights.data_ptr(), weights.stride(0)
-    return p
+def _row_sets(rows: torch.Tensor, sorted_rows: torch.Tensor, place: torch.Tensor, weights: Optional[torch.Tensor]) -> RowSets:
+    count, cols = rows.shape
+    at, pitch = (None, 0) if weights is None else (weights.data_ptr(), weights.stride(0))
+    return RowSets(_ROW_SETS, TYPES[rows.dtype], place.shape[1] if place.dim() == 2 else 1, cols, count, sorted_rows.shape[0], place.data_ptr(), place.stride(0), at, pitch,
+                   rows.data_ptr(), rows.stride(0), sorted_rows.data_ptr(), sorted_rows.stride(0))
 
 
 def _check_rows(where: str, x: torch.Tensor, place: torch.Tensor, weights: Optional[torch.Tensor], rows: Optional[int]) -> None:
-    _require(x.is_cuda and x.dtype in TYPES and _rows(x, x.dtype, x.device) and x.shape[1] >= 1, where, "fp32, bf16 or fp16 rows on a GPU")
-    _require(_pairs(place, torch.int32, x.device) and (place.dim() == 1 or place.shape[1] >= 1) and (rows is None or place.shape[0] == rows), where,
+    device = x.device
+    _require(x.is_cuda and x.dtype in TYPES and x.dim() == 2 and x.shape[1] >= 1 and (x.stride(1) == 1 or x.shape[1] == 1), where, "fp32, bf16 or fp16 rows on a GPU")
+    shape = place.shape
+    _require(place.device == device and place.dtype == torch.int32 and
+             (len(shape) == 1 or (len(shape) == 2 and shape[1] >= 1 and (place.stride(1) == 1 or shape[1] == 1))) and (rows is None or shape[0] == rows), where,
              "place: int32, [rows] or [rows, choices], as route_rows gives it")
-    _require(weights is None or _pairs(weights, torch.float32, x.device, place.shape), where, "weights: fp32, of place's shape")
+    _require(weights is None or (weights.device == device and weights.dtype == torch.float32 and weights.shape == shape and
+                                 (len(shape) == 1 or weights.stride(1) == 1 or shape[1] == 1)), where, "weights: fp32, of place's shape")
 
 
 def take_rows(x: torch.Tensor, place: torch.Tensor, weights: Optional[torch.Tensor] = None, *, out: Optional[torch.Tensor] = None,
@@ -327,7 +331,7 @@ def take_rows(x: torch.Tensor, place: torch.Tensor, weights: Optional[torch.Tens
     _check_rows(where, x, place, weights, x.shape[0])
     with _On(device, stream, where) as st:
         y = _out(out, x, place.numel() if out is None else out.shape[0], x.shape[1], where)
-        code = lib.evo_take_rows(C.byref(_row_sets(where, x, y, place, weights)), st)
+        code = lib.evo_take_rows(C.byref(_row_sets(x, y, place, weights)), st)
     _check(code, where)
     return y
 
@@ -341,7 +345,7 @@ def combine_rows(y: torch.Tensor, place: torch.Tensor, weights: Optional[torch.T
     _check_rows(where, y, place, weights, None)
     with _On(device, stream, where) as st:
         x = _out(out, y, place.shape[0], y.shape[1], where)
-        code = lib.evo_combine_rows(C.byref(_row_sets(where, x, y, place, weights)), st)
+        code = lib.evo_combine_rows(C.byref(_row_sets(x, y, place, weights)), st)
     _check(code, where)
     return x
 
@@ -359,7 +363,7 @@ def combine_rows_backward(d_out: torch.Tensor, y: torch.Tensor, place: torch.Ten
     with _On(device, stream, where) as st:
         dy = _out(out, y, y.shape[0], y.shape[1], where)
         dw = weights.new_empty(place.shape)
-        p = _row_sets(where, d_out, y, place, weights)
+        p = _row_sets(d_out, y, place, weights)
         p.d_sorted_gradient, p.ld_sorted_gradient, p.d_weights_gradient, p.ld_weights_gradient = dy.data_ptr(), dy.stride(0), dw.data_ptr(), dw.stride(0)
         code = lib.evo_combine_rows_backward(C.byref(p), st)
     _check(code, where)
@@ -393,26 +397,22 @@ def grouped_linear_backward(dy: torch.Tensor, x: Optional[torch.Tensor], weight:
     with _On(device, stream, where) as st:
         dx = _out(out[0], dy, rows, n_in, where) if wanted[0] else None
         dweight, dbias = out[1] if wanted[1] else None, out[2] if wanted[2] else None
-        if wanted[1] and dweight is None:
-            dweight = dy.new_empty((sets[0], n_out, n_in))
-        if wanted[2] and dbias is None:
-            dbias = dy.new_empty((sets[1], n_out))
-        _require(dweight is None or (dweight.device == device and dweight.dtype == dtype and dweight.shape == (sets[0], n_out, n_in) and
-                                     (n_in == 1 or dweight.stride(2) == 1)), where, "the gradient of weight does not match")
-        _require(dbias is None or (_rows(dbias, dtype, device) and dbias.shape == (sets[1], n_out)), where, "the gradient of the bias does not match")
-        f = Grouped(C.sizeof(Grouped), TYPES[dtype], groups, n_in, n_out, ACTIVATIONS[activation], scale, wide, rows)
-        f.d_weight, f.ld_weight, f.weight_stride, f.d_offsets = weight.data_ptr(), pitch if n_out > 1 else n_in, stride, offsets.data_ptr()
-        if x is not None:
-            f.d_x, f.ld_x = x.data_ptr(), x.stride(0)
-        if y is not None:
-            f.d_y, f.ld_y = y.data_ptr(), y.stride(0)
-        p = GroupedGradient(C.sizeof(GroupedGradient), 1 if sets[0] < groups else 0, 1 if sets[1] < groups else 0, dy.data_ptr(), dy.stride(0))
-        if dx is not None:
-            p.d_dx, p.ld_dx = dx.data_ptr(), dx.stride(0)
         if dweight is not None:
-            p.d_dweight, p.ld_dweight, p.dweight_stride = dweight.data_ptr(), dweight.stride(1) if n_out > 1 else n_in, dweight.stride(0)
+            _require(dweight.device == device and dweight.dtype == dtype and dweight.shape == (sets[0], n_out, n_in) and (n_in == 1 or dweight.stride(2) == 1), where,
+                     "the gradient of weight does not match")
+        elif wanted[1]:
+            dweight = dy.new_empty((sets[0], n_out, n_in))
         if dbias is not None:
-            p.d_dbias, p.dbias_stride = dbias.data_ptr(), dbias.stride(0)
+            _require(_rows(dbias, dtype, device) and dbias.shape == (sets[1], n_out), where, "the gradient of the bias does not match")
+        elif wanted[2]:
+            dbias = dy.new_empty((sets[1], n_out))
+        no = (None, 0)
+        f = Grouped(_GROUPED, TYPES[dtype], groups, n_in, n_out, ACTIVATIONS[activation], scale, wide, rows, *(no if x is None else (x.data_ptr(), x.stride(0))),
+                    weight.data_ptr(), pitch if n_out > 1 else n_in, stride, None, 0, offsets.data_ptr(), *(no if y is None else (y.data_ptr(), y.stride(0))))
+        apart, down = (0, 0) if dweight is None else dweight.stride()[:2]
+        p = GroupedGradient(_GROUPED_GRADIENT, 1 if sets[0] < groups else 0, 1 if sets[1] < groups else 0, dy.data_ptr(), dy.stride(0),
+                            *(no if dx is None else (dx.data_ptr(), dx.stride(0))), None if dweight is None else dweight.data_ptr(), down if n_out > 1 else n_in, apart,
+                            *(no if dbias is None else (dbias.data_ptr(), dbias.stride(0))))
         need = C.c_size_t()
         _check(lib.evo_grouped_linear_backward_bytes(C.byref(f), C.byref(p), C.byref(need)), where)
         work = torch.empty(need.value, dtype=torch.uint8, device=device) if need.value else None
@@ -451,7 +451,7 @@ def policy_loss(logits: torch.Tensor, actions: torch.Tensor, old_logp: torch.Ten
     _require(actions.device == device and actions.dtype in (torch.int32, torch.int64) and actions.shape == (rows,) and actions.is_contiguous(), where,
              "actions: int32 or int64, one a row")
     for x in (old_logp, advantage, ref_logp, weights):
-        _require(x is None or (x.device == device and x.dtype == torch.float32 and x.shape == (rows,) and x.is_contiguous()), where,
+        _require(x is None or (x.device == device and x.dtype == torch.float32 and x.shape == actions.shape and x.is_contiguous()), where,
                  "old_logp, advantage, ref_logp and weights: contiguous fp32, one a row")
     _require(old_logp is not None and advantage is not None and (ref_logp is not None or kl == 0.0), where, "old_logp, advantage or ref_logp is missing")
     _require(len(clip) == 2 and (out is None or gradient), where, "clip or out")
