@@ -201,6 +201,24 @@ def test_infinities_and_nan_stay_in_their_groups_and_rows(dtype, lengths, n_in, 
     assert bad[a - 1].all() and bad[b].all() and int(bad.sum()) == 2 * n_in
 
 
+@pytest.mark.parametrize("lengths,n_in,n_out", [([2, 0, 3, 1] * 8, 200, 136), ([22, 5, 31] * 30, 159, 902), ([40, 300, 17], 264, 128)])
+def test_fp16_numbers_whose_second_part_has_few_bits(lengths, n_in, n_out):
+    """dz / scale is two numbers of fp16: where it is small the second is a multiple of 2^-24, off by half of that at most, whatever dz is.  So a sum of products is off by
+    another 2^-25 |scale| times the sum of the other operand's sizes."""
+    scale = 2.0
+    dy, x, w, off, y = make(len(lengths), lengths, n_in, n_out, F16, "tanh", scale)
+    y = (scale * torch.tanh(2.5 * torch.atanh((y / scale).double().clamp(-0.99, 0.99)))).half()         # saturated
+    dy = (dy.double() * 2.0 ** -6).half()
+    got = grouped_linear_backward(dy, x, w, off, y, activation="tanh", scale=scale)
+    for which, (want, s) in enumerate(exact(dy, x, w, off, y, "tanh", scale)):
+        ones = torch.ones_like(dy)
+        more = exact(ones, x, w, off, None, "none", 1.0)[which][1]       # sums of |weights|, |x|, 1
+        k = n_out if which == 0 else max(lengths)
+        off_by = slack(F16, k) * s + 2.0 ** -25 * scale * more
+        err, bound = (got[which].double() - want).abs(), off_by + 2.0 ** -11 * (want.abs() + off_by) + 2.0 ** -24
+        assert (err <= bound).all(), (which, float((err / bound).max()))
+
+
 def test_offsets_that_fall_or_leave_the_rows_touch_nothing_outside():
     dy, x, w, off, _ = make(4, [40, 30, 20, 10], 72, 40, F32)
     for edges in ([-5, 40, 30, 200, 100], [100, 0, 50, 10, 100], [2 ** 31 - 1] * 5, [-2 ** 31] * 5):
