@@ -27,6 +27,10 @@ constexpr uint32_t kRing = 192u * 1024u, kStaging = 8u * 4096u, kSmem = kRing + 
 // fp32; 16-bit types: every 128.
 constexpr uint32_t kSegment = 8, kLongSegment = 128;
 
+// What a stage waits for before it is filled anew: its MMAs, and the warp that clears rows, which looks at every stage.  (With the MMAs alone that warp could be overtaken by a
+// turn of the ring, whose phase a barrier's parity does not tell from the one it waits for.)
+constexpr uint32_t kEmptyArrivals = 2;
+
 struct DwArgs {
     GradientArgs a;
     CUtensorMap dz[2], x[2], dw;                             // boxes of 16 and of 64 rows; of 32 outputs x 128 bytes
@@ -78,7 +82,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_weights_tc(const __grid_constan
     const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31u;
     const uint32_t smem = (smem_u32(raw) + 1023u) / 1024u * 1024u;
     if (tid == 0) {
-        for (uint32_t s = 0; s < kMostStages; ++s) { mbar_init(smem_u32(&full[s]), 1); mbar_init(smem_u32(&empty[s]), 1); mbar_init(smem_u32(&cleared[s]), 1); }
+        for (uint32_t s = 0; s < kMostStages; ++s) { mbar_init(smem_u32(&full[s]), 1); mbar_init(smem_u32(&empty[s]), kEmptyArrivals); mbar_init(smem_u32(&cleared[s]), 1); }
         for (uint32_t b = 0; b < 2u; ++b) { mbar_init(smem_u32(&done[b]), 1); mbar_init(smem_u32(&taken[b]), 8); }
         mbar_init(smem_u32(&drain), 1);
         mbar_init_fence();
@@ -204,7 +208,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_weights_tc(const __grid_constan
             const uint32_t bytes = rest > 16u ? 8192u : 2048u, upto = (rest + 15u) / 16u * 16u;
             uint32_t chunk = 0;
             for (uint32_t k = 0; k < chunks * p.passes && fine; ++k) {
-                fine = all_of(wait(&full[stage], phase));    // (every one: a barrier tells apart two phases only)
+                fine = all_of(wait(&full[stage], phase));
+                if (!fine) break;
                 const bool last = ++chunk == chunks;
                 if (last) chunk = 0;
                 if (last && (rest & 15u)) {
@@ -215,6 +220,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_weights_tc(const __grid_constan
                     __syncwarp();
                     if (lane == 0) mbar_arrive(smem_u32(&cleared[stage]));
                 }
+                if (lane == 0) mbar_arrive(smem_u32(&empty[stage]));
                 if (++stage == stages) { stage = 0; phase ^= 1u; }
             }
         }
