@@ -19,6 +19,7 @@ constexpr uint32_t kItems = kSmallCols * kSmallRows / 8u / kThreads;       // ei
 
 __device__ __forceinline__ void cluster_sync()
 {
+    __syncwarp();                                            // (.aligned: a warp comes to it as one)
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 __device__ __forceinline__ uint32_t in_block(uint32_t addr, uint32_t rank)

@@ -22,6 +22,7 @@ __device__ __forceinline__ uint32_t turned(uint32_t x)
 }
 __device__ __forceinline__ void cluster_sync_all()
 {
+    __syncwarp();                                            // (.aligned: a warp comes to it as one)
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 template <typename T>

@@ -127,7 +127,10 @@ __global__ void __launch_bounds__(128) k_policy_short(const __grid_constant__ Po
     static_assert(kRows <= 32u, "a lane a row");
     dep_wait();
     dep_trigger();
-    if constexpr (ONE) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");         // (that the first block has begun)
+    if constexpr (ONE) {
+        __syncwarp();                                        // (.aligned: a warp comes to it as one)
+        asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");         // (that the first block has begun)
+    }
     const uint32_t all_lanes = threadIdx.x % 32u, lane = all_lanes % L, nth = all_lanes / L;
     const uint64_t first = (static_cast<uint64_t>(blockIdx.x) * 4u + threadIdx.x / 32u) * kRows;
     if (!ONE && first >= a.rows) return;                     // (whole warps)
@@ -178,6 +181,7 @@ __global__ void __launch_bounds__(128) k_policy_short(const __grid_constant__ Po
 #pragma unroll
         for (uint32_t d = 16u; d > 0u; d /= 2u) loss += __shfl_xor_sync(0xffffffffu, loss, d);
         if (all_lanes == 0u) warps[threadIdx.x / 32u] = loss;
+        __syncwarp();
         asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
         __syncthreads();
         if (threadIdx.x == 0u) {
@@ -186,8 +190,7 @@ __global__ void __launch_bounds__(128) k_policy_short(const __grid_constant__ Po
             asm volatile("st.shared::cluster.f64 [%0], %1;" :: "r"(there), "d"((warps[0] + warps[1]) + (warps[2] + warps[3])) : "memory");
         }
         __syncwarp();
-        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+        asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
         if (blockIdx.x == 0u && threadIdx.x == 0u) {
             loss = 0.0;
             for (uint32_t k = 0; k < gridDim.x; ++k) loss += blocks[k];

@@ -144,6 +144,7 @@ __global__ void __launch_bounds__(1024) k_route_once(const __grid_constant__ Pas
         if (CTAS == 1u) base[b] = sum;
     }
     if constexpr (CTAS > 1u) {
+        __syncwarp();                                        // (.aligned: a warp comes to it as one, from loops that its lanes leave at different turns)
         asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
         // the sum over the blocks, and what the blocks before this one have (added to the first warp's counts and so on below)
         for (uint32_t b = threadIdx.x; b < p.bins; b += blockDim.x) {
@@ -159,6 +160,7 @@ __global__ void __launch_bounds__(1024) k_route_once(const __grid_constant__ Pas
             base[b] = sum;
             for (uint32_t w = 0; w < p.counting; ++w) counts[w * p.bins + b] += before;
         }
+        __syncwarp();
         asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");       // (waited for at the end: the others may still be reading)
     }
     __syncthreads();
@@ -171,7 +173,10 @@ __global__ void __launch_bounds__(1024) k_route_once(const __grid_constant__ Pas
         const uint32_t bin = member[i] >> p.shift & p.mask;
         put(p, pair[i], member[i], base[bin] + mine[bin] + rank[i]);
     }
-    if constexpr (CTAS > 1u) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    if constexpr (CTAS > 1u) {
+        __syncwarp();
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    }
 }
 
 // ---- three launches ----
