@@ -14,7 +14,7 @@ namespace evo {
 namespace {
 
 constexpr uint32_t kMostBins = 2048, kMostBlocks = 592;
-constexpr uint32_t kSmem = 200u * 1024u;
+constexpr uint32_t kSmem = 200u * 1024u, kOwn = 32u * 4u;      // of counters at most; beside them (warp_sums)
 
 struct Pass {
     RouteArgs a;
@@ -325,11 +325,17 @@ Plan plan_for(const RouteArgs& a)
     return p;
 }
 
+// (48 KB without asking, what a kernel has beside its counters included)
+bool has_room(void (*kernel)(Pass), size_t smem)
+{
+    return smem + kOwn <= 48u * 1024u || cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSmem)) == cudaSuccess;
+}
+
 template <uint32_t CTAS>
 cudaError_t launch_once(cudaStream_t st, uint32_t it, uint32_t threads, size_t smem, const Pass& p)
 {
     auto kernel = it == 1u ? k_route_once<CTAS, 1> : k_route_once<CTAS, 4>;
-    if (smem > 48u * 1024u && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSmem)) != cudaSuccess) return cudaErrorInvalidValue;
+    if (!has_room(kernel, smem)) return cudaErrorInvalidValue;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(CTAS); cfg.blockDim = dim3(threads); cfg.dynamicSmemBytes = smem; cfg.stream = st;
     cudaLaunchAttribute attr[2];
@@ -382,7 +388,7 @@ int launch_route(cudaStream_t st, const RouteArgs& a, void* work)
         const uint32_t helping = p.bins > 2048u ? 32u : p.bins > 256u ? 8u : 1u, warps = p.counting > helping ? p.counting : helping;
         const size_t smem = 4u * static_cast<size_t>(p.counting + 2u) * p.bins;
         auto launch = [&](void (*kernel)(Pass), uint32_t blocks) {
-            if (smem > 48u * 1024u && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSmem)) != cudaSuccess) return false;
+            if (!has_room(kernel, smem)) return false;
             ++launches;
             return launch_dependent(kernel, dim3(blocks), dim3(warps * 32u), smem, st, p) == cudaSuccess;
         };
