@@ -485,7 +485,7 @@ evo_status evo_combine_rows_backward(const evo_row_sets* p, void* cuda_stream);
  * dx, dweight and dbias NULL: not wanted.  x is read for dweight alone, the weights for dx alone, y for activations alone (d_y may be NULL without one).
  * Rows of dx that belong to no group are left as they are; an empty group's gradients are zeros.  sum_weight / sum_bias: one gradient for all groups
  * together (weights or biases that the groups share: stride 0).  Types, offsets, sums and infinities as above; of 16-bit types dz / scale counts with 16 bits and more
- * (fp16: to 2^-25 at worst, numbers below 2^-14 with fewer).  With an activation scale may not be 0, nor so small that 1 / scale is no number.  Outputs may not overlap anything, from the first to the last element of each array (a layer's
+ * (fp16: with 22, numbers below 2^-14 to 2^-36).  With an activation scale may not be 0, nor so small that 1 / scale is no number.  Outputs may not overlap anything, from the first to the last element of each array (a layer's
  * gradients inside rows as wide as theta's do not overlap: dweight and dbias may lie between each other's groups).
  * Errors: INVALID_ARG, WORKSPACE, UNSUPPORTED (more than 2^31 blocks), CUDA.  The workspace with any of the inputs NULL is enough for any addresses.
  */

@@ -171,7 +171,15 @@ __device__ __forceinline__ void step(const uint4 (&v)[8], const T* hi, const T* 
                 for (uint32_t e = 0; e < EIGHTS; ++e) {
                     if (e && !more) continue;
                     gm::mma_16<T>(sums[e].part[m], a, h ? bh[e].z : bh[e].x, h ? bh[e].w : bh[e].y);
-                    if (two) gm::mma_16<T>(sums[e].part[m], a, h ? bl[e].z : bl[e].x, h ? bl[e].w : bl[e].y);
+                    if (!two) continue;
+                    if constexpr (std::is_same<T, __half>::value) {
+                        float second[4] = {};
+                        gm::mma_16<T>(second, a, h ? bl[e].z : bl[e].x, h ? bl[e].w : bl[e].y);
+#pragma unroll
+                        for (uint32_t i = 0; i < 4u; ++i) sums[e].part[m][i] = fmaf(kDown<T>, second[i], sums[e].part[m][i]);
+                    } else {
+                        gm::mma_16<T>(sums[e].part[m], a, h ? bl[e].z : bl[e].x, h ? bl[e].w : bl[e].y);
+                    }
                 }
             }
         }
@@ -245,7 +253,7 @@ __device__ __forceinline__ void rows_tile(const RowsArgs& p, uint32_t group, uin
                 } else {
                     const T h = from_float<T>(d);
                     hi[at] = h;
-                    if (two) lo[at] = from_float<T>(isfinite(to_float(h)) ? d - to_float(h) : 0.f);
+                    if (two) lo[at] = from_float<T>(isfinite(to_float(h)) ? kUp<T> * (d - to_float(h)) : 0.f);
                 }
             }
         }
@@ -515,10 +523,11 @@ __global__ void __launch_bounds__(256) k_bias(const __grid_constant__ BiasArgs p
 #pragma unroll
                 for (uint32_t k = 0; k < kAsk; ++k) {
                     const uint32_t w[4] = { u[k].x, u[k].y, u[k].z, u[k].w };
+                    const float factor = std::is_same<T, __half>::value && p.parts == 2u && ((r + R * k) & 1u) ? kDown<T> : 1.f;      // (a second part)
 #pragma unroll
                     for (uint32_t e = 0; e < N; ++e) {
                         const uint16_t bits = static_cast<uint16_t>(w[e / 2u] >> (e % 2u * 16u));
-                        if constexpr (std::is_same<T, __half>::value) sum[e] += __half2float(__ushort_as_half(bits));
+                        if constexpr (std::is_same<T, __half>::value) sum[e] = fmaf(factor, __half2float(__ushort_as_half(bits)), sum[e]);
                         else sum[e] += __uint_as_float(static_cast<uint32_t>(bits) << 16);
                     }
                 }

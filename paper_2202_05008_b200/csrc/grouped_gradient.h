@@ -1,5 +1,9 @@
 // Arguments and launchers of the gradients of the products grouped by member (grouped_gradient.cu).
 #pragma once
+#include <cuda_fp16.h>
+
+#include <type_traits>
+
 #include "grouped.h"
 
 namespace evo {
@@ -41,6 +45,12 @@ __device__ __forceinline__ float dz_unit(const GradientArgs& a, float dy, float 
     if (a.f.activation == EVO_ACT_RELU) return (a.f.scale > 0.f ? y > 0.f : y < 0.f) ? dy : 0.f;
     return dy;
 }
+// dz / scale of 16-bit types in two numbers of the type, where it is not dy or 0: the second is what the first leaves, of fp16 times 2^kSecondUp, since what is left of small
+// numbers lies below fp16's own (without that dz was off by up to 2^-25 whatever its size; so by 2^-22 of itself, or 2^-36).  Sums of second numbers are taken down again before those
+// of the first ones join them.
+constexpr uint32_t kSecondUp = 11;
+template <typename T> constexpr float kUp = std::is_same<T, __half>::value ? static_cast<float>(1u << kSecondUp) : 1.f;
+template <typename T> constexpr float kDown = 1.f / kUp<T>;
 // Rows of a set (a group, or all of them together) between two offsets, inside [0, rows], of which split `split` of `splits` has its part, a multiple of 16 rows.
 __device__ __forceinline__ void split_rows(const GradientArgs& a, int64_t p, int64_t q, uint32_t split, uint32_t splits, uint64_t* first, uint64_t* end)
 {

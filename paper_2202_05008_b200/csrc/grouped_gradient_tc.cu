@@ -11,7 +11,7 @@
 // are not kept.
 //
 // dz = dy act'(z) is laid out first where it is not dy itself, scale left to the end: fp32 as three bf16 parts like the rows (and weights), of 16-bit types with
-// tanh as two parts of the type (rounded once it would be off by as much as the result's own rounding); relu's is dy or 0.
+// tanh as two parts of the type (rounded once it would be off by as much as the result's own rounding), of fp16 the second 2^11 times as large (kSecondUp); relu's is dy or 0.
 #include <cmath>
 
 #include "grouped_gradient.h"
@@ -105,6 +105,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_weights_tc(const __grid_constan
         return false;
     };
     auto all_of = [](bool fine) { return __all_sync(0xffffffffu, fine) != 0; };
+    // fp16 in two parts: the step at which the sums of second parts end (0: there are none), the first of whose MMAs takes the sum so far down
+    auto turn_of = [&](uint32_t chunks) { return std::is_same<T, __half>::value && p.passes == 2u ? chunks : 0u; };
     auto chunks_of = [&](const Item& t) { return static_cast<uint32_t>((t.end - t.row + 63u) / 64u); };
     // the step behind the part of a sum that begins at step k
     auto part_end = [&](uint32_t k, uint32_t chunks) {
@@ -157,7 +159,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_weights_tc(const __grid_constan
             for (uint32_t at = blockIdx.x; at < items && fine; at += gridDim.x) {
                 const Item t = item_of(p, next);
                 if (at + gridDim.x < items) next = ask_for(p, at + gridDim.x);
-                const uint32_t chunks = chunks_of(t), steps = chunks * p.passes, id = idesc<T, true, true>(t.columns);
+                const uint32_t chunks = chunks_of(t), steps = chunks * p.passes, turn = turn_of(chunks), id = idesc<T, true, true>(t.columns);
                 const uint32_t rest = static_cast<uint32_t>(t.end - t.row) - (chunks - 1u) * 64u;      // rows of the last chunk
                 uint32_t chunk = 0;
                 for (uint32_t k = 0; k < steps && fine;) {
@@ -165,12 +167,17 @@ __global__ void __launch_bounds__(kThreads, 1) k_weights_tc(const __grid_constan
                     fine = wait(&taken[acc], acc_phase ^ 1u);
                     tc_fence_after();
                     for (; k < end && fine; ++k) {
+                        const bool down = k == turn && k != first;
+                        auto multiply = [&](uint64_t a, uint64_t b, uint32_t s) {
+                            if (std::is_same<T, __half>::value && s == 0u && down) umma_scaling_down<kSecondUp>(d, a, b, id);
+                            else umma_bf16(d, a + s * 128u, b + s * 128u, id, k - first + s != 0u);
+                        };
                         const uint32_t at_stage = smem + stage * stage_bytes;
                         if (chunk + 1u < chunks || rest == 64u) {
                             fine = wait(&full[stage], phase);
                             const uint64_t a = desc_sw128_mn(at_stage, 8192u), b = desc_sw128_mn(at_stage + 16384u, 8192u);
 #pragma unroll
-                            for (uint32_t s = 0; s < 4u; ++s) umma_bf16(d, a + s * 128u, b + s * 128u, id, k - first + s != 0u);
+                            for (uint32_t s = 0; s < 4u; ++s) multiply(a, b, s);
                         } else {
                             if (rest & 15u) {
                                 fine = wait(&cleared[stage], was_cleared >> stage & 1u);
@@ -180,7 +187,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_weights_tc(const __grid_constan
                             }
                             const uint32_t bytes = rest > 16u ? 8192u : 2048u;
                             const uint64_t a = desc_sw128_mn(at_stage, bytes), b = desc_sw128_mn(at_stage + 2u * bytes, bytes);
-                            for (uint32_t s = 0; s * 16u < rest; ++s) umma_bf16(d, a + s * 128u, b + s * 128u, id, k - first + s != 0u);
+                            for (uint32_t s = 0; s * 16u < rest; ++s) multiply(a, b, s);
                         }
                         umma_commit(smem_u32(&empty[stage]));
                         if (++chunk == chunks) chunk = 0;
@@ -296,6 +303,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_weights_tc(const __grid_constan
 #pragma unroll
                         for (uint32_t i = 0; i < 32u; ++i) u[i / 8u][i % 8u] = 0u;
                     }
+                    if (std::is_same<T, __half>::value && end <= turn_of(chunks))          // (a part of second numbers alone)
+#pragma unroll
+                        for (uint32_t i = 0; i < 32u; ++i) u[i / 8u][i % 8u] = __float_as_uint(kDown<T> * __uint_as_float(u[i / 8u][i % 8u]));
                     // a row of 32 numbers a lane, its eight pieces of 16 bytes in an order that the lane's number turns: no bank is hit twice
                     if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
                     __syncwarp();
@@ -448,7 +458,7 @@ __global__ void __launch_bounds__(256) k_lay_dz(const __grid_constant__ Gradient
             const float x = live ? dz_unit(a, number(d[i]), act ? number(z[i]) : 0.f) : 0.f;
             const T whole = rounded(x);
             reinterpret_cast<T*>(dst)[k] = whole;
-            if constexpr (PARTS == 2u) reinterpret_cast<T*>(dst)[pitch + k] = rounded(isfinite(number(whole)) ? x - number(whole) : 0.f);      // (an infinity has no second part)
+            if constexpr (PARTS == 2u) reinterpret_cast<T*>(dst)[pitch + k] = rounded(isfinite(number(whole)) ? kUp<T> * (x - number(whole)) : 0.f);      // (an infinity has no second part)
         }
     }
 }

@@ -17,6 +17,7 @@
 #include <cmath>
 #include <type_traits>
 
+#include "grouped_gradient.h"
 #include "grouped_mma.cuh"
 #include "grouped_tc.cuh"
 
@@ -125,6 +126,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_grouped_tc(const __grid_constan
     // the step behind the part of a sum that begins at step k
     const uint32_t small_steps = steps - chunks;
     auto part_end = [&](uint32_t k) { return LONG ? min(steps, k + kLongSegment) : std::is_same<O, float>::value && p.passes > 1u ? min(steps, max(k, small_steps) + kSegment) : steps; };
+    // rows of fp16 in two parts: the step at which the sums of second parts end (0: there are none), the first of whose MMAs takes the sum so far down
+    constexpr bool kHalfRows = TR && std::is_same<T, __half>::value;
+    const uint32_t turn = kHalfRows && p.passes == 2u ? chunks : 0u;
     Walk walk;
     walk.fill(p);
     uint32_t group, rows, stage = 0, phase = 0, acc = 0, acc_phase = 0, filled = 0;
@@ -182,7 +186,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_grouped_tc(const __grid_constan
                         const uint32_t w = smem + stage * stage_bytes;
                         const uint64_t a = TR ? desc_sw128_mn(w, 8192u) : desc_sw128(w), b = desc_sw128(w + kWBytes);
 #pragma unroll
-                        for (uint32_t s = 0; s < 4u; ++s) umma_bf16(d, a + s * (TR ? 128u : 2u), b + s * 2u, id, k - first + s != 0u);
+                        for (uint32_t s = 0; s < 4u; ++s) {
+                            if (kHalfRows && s == 0u && k == turn && k != first) umma_scaling_down<kSecondUp>(d, a, b, id);
+                            else umma_bf16(d, a + s * (TR ? 128u : 2u), b + s * 2u, id, k - first + s != 0u);
+                        }
                         umma_commit(smem_u32(&empty[stage]));
                         if (++stage == stages) { stage = 0; phase ^= 1u; }
                     }
@@ -228,6 +235,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_grouped_tc(const __grid_constan
 #pragma unroll
                     for (uint32_t i = 0; i < 32u; ++i) v[i] = __uint_as_float(u[i / 8u][i % 8u]);
                     if constexpr (LONG) {
+                        if (kHalfRows && end <= turn)        // (a part of second numbers alone)
+#pragma unroll
+                            for (uint32_t i = 0; i < 32u; ++i) v[i] *= kDown<__half>;
 #pragma unroll
                         for (uint32_t i = 0; i < 32u; ++i) so_far[i] = v[i] = first ? so_far[i] + v[i] : v[i];
                         if (end != steps) return;
