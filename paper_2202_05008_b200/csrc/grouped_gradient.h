@@ -29,11 +29,11 @@ __device__ __forceinline__ void dep_end(const GradientArgs& a)
     if (a.late) dep_wait();
 }
 
-// dz = dy scale act'(z), from y = scale act(z).  scale - y is exact close to the ends of tanh.
+// dz = dy scale act'(z), from y = scale act(z).  scale - y is exact close to the ends of tanh; scale + y is divided by scale before the two meet, since scale squared may be no number.
 __device__ __forceinline__ float dz_of(const GradientArgs& a, float dy, float y)
 {
     const float scale = a.f.scale;
-    if (a.f.activation == EVO_ACT_TANH) return dy * ((scale - y) * (scale + y) * a.inverse);
+    if (a.f.activation == EVO_ACT_TANH) return dy * ((scale - y) * ((scale + y) * a.inverse));
     if (a.f.activation == EVO_ACT_RELU) return (scale > 0.f ? y > 0.f : y < 0.f) ? dy * scale : 0.f;
     return dy * scale;
 }
