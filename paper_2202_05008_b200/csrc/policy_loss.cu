@@ -34,7 +34,9 @@ template <typename T> __device__ __forceinline__ T from_float(float x)
     else if constexpr (std::is_same<T, __half>::value) return __float2half_rn(x);
     else return __float2bfloat16_rn(x);
 }
-// e^(x - top), 1 for the maximum itself.  (The difference first: x log2 e may leave fp32's range, and all of a row may be the type's lowest number.)
+// e^(x - top), 1 for the maximum itself.  (The difference first: x log2 e may leave fp32's range, and all of a row may be the type's lowest number.)  The difference and the product are
+// rounded to fp32, so that it is off by up to 2.25 2^-24 (top - x) of itself, and numbers below 2^-126 are 0: what that is of is as small against the row's largest, and the two or three
+// instructions more that would keep the product's second part are a fifth of a long row's time (it is bound by issue beside memory).
 __device__ __forceinline__ float exp_below(float x, float top)
 {
     float y;
@@ -76,6 +78,15 @@ __device__ __forceinline__ Row row_of(const PolicyArgs& a, uint64_t row)
     return r;
 }
 
+// e^x in fp32's precision and fp64's range: its product with a weight or an advantage may be an fp32 number where it is none itself.
+__device__ __forceinline__ double exp_far(double x)
+{
+    if (fabs(x) < 80.0) return static_cast<double>(expf(static_cast<float>(x)));
+    if (!(fabs(x) < 700.0)) return x > 0.0 ? static_cast<double>(INFINITY) : x < 0.0 ? 0.0 : x;      // (a NaN)
+    const double k = rint(x * static_cast<double>(kLog2e));
+    return scalbn(static_cast<double>(expf(static_cast<float>(fma(-kLn2, k, x)))), static_cast<int>(k));
+}
+
 // What follows from the row's maximum and s = sum of e^(x - top), 1 at least.  `all`: the factor of e^(x - top) in the gradient, `chosen`: the gradient of the action.
 // Differences are taken in fp64, functions of them in fp32: log s of its exponent and of a number close to 1, the ratio's borders as logarithms, 1 - p as an expm1,
 // e^d - 1 - d as its series where it is a small difference.  Returns the row's share of the loss.
@@ -87,20 +98,25 @@ __device__ __forceinline__ double finish_row(const PolicyArgs& a, uint64_t row, 
     double logp = static_cast<double>(chosen_logit) - static_cast<double>(top) - fma(kLn2, static_cast<double>(exponent), static_cast<double>(logf(m)));
     if (!(s >= 1.f)) logp = static_cast<double>(s);          // (a NaN)
     const double log_ratio = logp - static_cast<double>(a.old_logp[row]);
-    const float adv = a.advantage[row], ratio = expf(static_cast<float>(log_ratio));
+    const float adv = a.advantage[row];
+    const double ratio = exp_far(log_ratio);
     const bool clipped = adv >= 0.f ? log_ratio > a.log_high : log_ratio < a.log_low;
-    double loss = -static_cast<double>(adv) * (clipped ? (adv >= 0.f ? 1.0 + a.clip_high : 1.0 - a.clip_low) : static_cast<double>(ratio));
-    double c = clipped ? 0.0 : -static_cast<double>(adv) * static_cast<double>(ratio);
+    double loss = -static_cast<double>(adv) * (clipped ? (adv >= 0.f ? 1.0 + a.clip_high : 1.0 - a.clip_low) : ratio);
+    double c = clipped ? 0.0 : -static_cast<double>(adv) * ratio;
     if (a.ref_logp) {
-        const float d = static_cast<float>(static_cast<double>(a.ref_logp[row]) - logp), e = expm1f(d);
-        float rest = e - d;
-        if (fabsf(d) < 0.5f) {                               // (what is left out is below 4e-8 of it)
+        const double far = static_cast<double>(a.ref_logp[row]) - logp;
+        const float d = static_cast<float>(far), near = expm1f(d);
+        double e = near, rest = near - d;
+        if (d >= 80.f) {
+            e = exp_far(far) - 1.0;
+            rest = e - far;
+        } else if (fabsf(d) < 0.5f) {                        // (what is left out is below 4e-8 of it)
             float q = 1.f / 40320.f;
             q = fmaf(q, d, 1.f / 5040.f); q = fmaf(q, d, 1.f / 720.f); q = fmaf(q, d, 1.f / 120.f); q = fmaf(q, d, 1.f / 24.f); q = fmaf(q, d, 1.f / 6.f); q = fmaf(q, d, 0.5f);
             rest = d * d * q;
         }
-        loss += a.kl * static_cast<double>(rest);
-        c -= a.kl * static_cast<double>(e);
+        loss += a.kl * rest;
+        c -= a.kl * e;
     }
     c *= r.weight;
     *all = static_cast<float>(-c) / s;
