@@ -512,7 +512,8 @@ evo_status evo_grouped_linear_backward(const evo_grouped* forward, const evo_gro
  * row with a NaN, an infinity above zero, or nothing but forbidden actions has NaN for logp and gradient, and the loss is NaN.
  * logits and gradient [rows][actions] of one type, any pitch and alignment; gradient may be logits itself (same pointer and pitch).  loss (one number), logp and gradient NULL: not wanted.  Sums of a
  * row in fp32; differences of logarithms, and the sum over rows, in fp64, functions of them with fp32's bits (and fp64's range: a ratio that is no fp32 number may have a product that is
- * one); everything in a fixed order.  A probability R below the row's largest in its logarithm is off by up to R 2^-22.8 of itself, and 0 below 2^-126.
+ * one); everything in a fixed order.  A probability whose logarithm is R below the row's largest is off by up to R 2^-24 of itself beside what its sum is
+ * (of 16-bit types R 2^-22.8), and 0 below 2^-126.
  * Errors: INVALID_ARG, WORKSPACE, UNSUPPORTED (more than 2^31 rows), CUDA.
  */
 typedef struct evo_policy_rows {

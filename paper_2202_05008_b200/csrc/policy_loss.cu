@@ -19,7 +19,7 @@ namespace evo {
 namespace {
 
 constexpr uint32_t kMostBlocks = 8;          // of a cluster
-constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLog2e = 1.4426950408889634f, kLog2eRest = static_cast<float>(1.4426950408889634 - static_cast<double>(kLog2e)), kLn2f = 0.69314718055994530942f;
 constexpr double kLn2 = 0.69314718055994530942;
 
 template <typename T> __device__ __forceinline__ float to_float(T x)
@@ -34,16 +34,6 @@ template <typename T> __device__ __forceinline__ T from_float(float x)
     else if constexpr (std::is_same<T, __half>::value) return __float2half_rn(x);
     else return __float2bfloat16_rn(x);
 }
-// e^(x - top), 1 for the maximum itself.  (The difference first: x log2 e may leave fp32's range, and all of a row may be the type's lowest number.)  The difference and the product are
-// rounded to fp32, so that it is off by up to 2.25 2^-24 (top - x) of itself, and numbers below 2^-126 are 0: what that is of is as small against the row's largest, and the two or three
-// instructions more that would keep the product's second part are a fifth of a long row's time (it is bound by issue beside memory).
-__device__ __forceinline__ float exp_below(float x, float top)
-{
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"((x - top) * kLog2e));
-    return y;
-}
-
 // Two at once: additions and products of pairs are one instruction.
 __device__ __forceinline__ float2 add2(float2 a, float2 b)
 {
@@ -59,13 +49,49 @@ __device__ __forceinline__ float2 mul2(float2 a, float2 b)
         : "l"(*reinterpret_cast<const unsigned long long*>(&a)), "l"(*reinterpret_cast<const unsigned long long*>(&b)));
     return r;
 }
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
+{
+    float2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(*reinterpret_cast<unsigned long long*>(&r))
+        : "l"(*reinterpret_cast<const unsigned long long*>(&a)), "l"(*reinterpret_cast<const unsigned long long*>(&b)), "l"(*reinterpret_cast<const unsigned long long*>(&c)));
+    return r;
+}
+__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
+__device__ __forceinline__ float power2(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// what has a power that is 0 anyway is cut off (an infinite difference has no rest); a NaN stays one
+__device__ __forceinline__ float no_less(float t)
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(t), "f"(-256.f));
+    return r;
+}
+
+// e^(x - top), 1 for the maximum itself; numbers below 2^-126 are 0.  (The difference first: x log2 e may leave fp32's range, and all of a row may be the type's lowest number.)
+// y = (x - top) log2 e is rounded, which of a large difference R is R 1.25 2^-24 of the result.  WHOLE (fp32): what y leaves is put right, e^(x - top) = 2^y (1 + ln 2 rest), so that
+// the difference's own rounding is what is left.  Numbers of 16 bits do without: R would have to be in the hundreds to be seen in them, and a long row of bf16 is bound by issue (8,192 of
+// 32,000: 197 us without, 264 with; of fp32 4,096 of 32,000 200 and 202, 100,000 of 900 150 and 158, 1,000,000 of 12 63).
+template <typename T> constexpr bool kWhole = std::is_same<T, float>::value;
+template <bool WHOLE>
+__device__ __forceinline__ float exp_below(float x, float top)
+{
+    if constexpr (!WHOLE) return power2((x - top) * kLog2e);
+    const float t = no_less(x - top), y = t * kLog2e, r = power2(y);
+    return fmaf(r * kLn2f, fmaf(t, kLog2eRest, fmaf(t, kLog2e, -y)), r);
+}
+template <bool WHOLE>
 __device__ __forceinline__ float2 exp_below2(float2 x, float top)
 {
-    const float2 y = mul2(add2(x, make_float2(-top, -top)), make_float2(kLog2e, kLog2e));
-    float2 r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r.x) : "f"(y.x));
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r.y) : "f"(y.y));
-    return r;
+    float2 t = add2(x, both(-top));
+    if constexpr (WHOLE) t = make_float2(no_less(t.x), no_less(t.y));
+    const float2 y = mul2(t, both(kLog2e)), r = make_float2(power2(y.x), power2(y.y));
+    if constexpr (!WHOLE) return r;
+    return fma2(mul2(r, both(kLn2f)), fma2(t, both(kLog2eRest), fma2(t, both(kLog2e), make_float2(-y.x, -y.y))), r);
 }
 
 struct Row { int64_t action; double weight; bool live; };
@@ -176,11 +202,13 @@ __global__ void __launch_bounds__(128) k_policy_short(const __grid_constant__ Po
 #pragma unroll
         for (uint32_t d = L / 2u; d > 0u; d /= 2u) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
 #pragma unroll
-        for (uint32_t i = 0; i < E; ++i)
-            if (lane + L * i < a.n) {
-                v[p][i] = exp_below(v[p][i], top);
-                s += v[p][i];
-            }
+        for (uint32_t i = 0; i < E; i += 2u) {               // (behind the row's end minus infinity)
+            const float2 e = exp_below2<kWhole<T>>(make_float2(v[p][i], v[p][i + 1u]), top);
+            v[p][i] = e.x;
+            v[p][i + 1u] = e.y;
+            s += e.x;
+            s += e.y;
+        }
 #pragma unroll
         for (uint32_t d = L / 2u; d > 0u; d /= 2u) s += __shfl_xor_sync(0xffffffffu, s, d);
         const float t = __shfl_sync(0xffffffffu, top, all_lanes % kAcross * L), u = __shfl_sync(0xffffffffu, s, all_lanes % kAcross * L);
@@ -317,7 +345,7 @@ template <typename T> struct Sixteen {
         float2 f[N / 2u], sum = make_float2(0.f, 0.f);
         numbers(f);
 #pragma unroll
-        for (uint32_t i = 0; i < N / 2u; ++i) sum = add2(sum, exp_below2(f[i], top));
+        for (uint32_t i = 0; i < N / 2u; ++i) sum = add2(sum, exp_below2<kWhole<T>>(f[i], top));
         return sum.x + sum.y;
     }
     // every number to factor e^(x - top)
@@ -326,7 +354,7 @@ template <typename T> struct Sixteen {
         float2 f[N / 2u];
         numbers(f);
 #pragma unroll
-        for (uint32_t i = 0; i < N / 2u; ++i) f[i] = mul2(exp_below2(f[i], top), make_float2(factor, factor));
+        for (uint32_t i = 0; i < N / 2u; ++i) f[i] = mul2(exp_below2<kWhole<T>>(f[i], top), make_float2(factor, factor));
         round(f);
     }
 };
@@ -380,7 +408,7 @@ __global__ void __launch_bounds__(256, 4) k_policy_row(const __grid_constant__ P
         top = fmaxf(top, most.largest());
     }
     top = over_warp<true>(top);
-    float s = has_single && live ? exp_below(alone, top) : 0.f;
+    float s = has_single && live ? exp_below<kWhole<T>>(alone, top) : 0.f;
 #pragma unroll
     for (uint32_t i = 0; i < NV; ++i)
         if (t + THREADS * i < mine) s += v[i].sum_below(top);
@@ -408,7 +436,7 @@ __global__ void __launch_bounds__(256, 4) k_policy_row(const __grid_constant__ P
             v[i].store(g + head + (t + THREADS * i) * N);
             own = own || (action >= head && (action - head) / N == t + THREADS * i);
         }
-    if (has_single) g[single] = from_float<T>(live ? all * exp_below(alone, top) : 0.f);
+    if (has_single) g[single] = from_float<T>(live ? all * exp_below<kWhole<T>>(alone, top) : 0.f);
     if (own && live) g[action] = from_float<T>(chosen);
 }
 
@@ -443,7 +471,7 @@ __global__ void __launch_bounds__(THREADS) k_policy_long(const __grid_constant__
     // the thread's maximum, and its sum with that taken off (0 while it has seen forbidden actions alone)
     float top = -INFINITY, s = 0.f;
     auto raise = [&](float most) {
-        if (most > top) { s *= exp_below(top, most); top = most; }
+        if (most > top) { s *= exp_below<kWhole<T>>(top, most); top = most; }
         return top == -INFINITY ? 0.f : top;
     };
     constexpr uint32_t kAhead = 4;
@@ -461,11 +489,11 @@ __global__ void __launch_bounds__(THREADS) k_policy_long(const __grid_constant__
         for (uint32_t k = 0; k < kAhead; ++k)
             if (i + THREADS * k < pieces) s += v[k].sum_below(off);
     }
-    auto add = [&](float x) { s += exp_below(x, raise(x)); };
+    auto add = [&](float x) { s += exp_below<kWhole<T>>(x, raise(x)); };
     for (uint32_t k = t; k < head; k += THREADS) add(to_float(x[k]));
     for (uint32_t k = behind + t; k < a.n; k += THREADS) add(to_float(x[k]));
     const float most = over_block<THREADS, true>(top, part[0]);
-    s = over_block<THREADS, false>(s * exp_below(top, most), part[1]);
+    s = over_block<THREADS, false>(s * exp_below<kWhole<T>>(top, most), part[1]);
     float all = 0.f, chosen = 0.f;
     if (t == 0u) finish_row(a, row, r, chosen_logit, most, s, &all, &chosen);
     if (!a.gradient) return;
@@ -487,8 +515,8 @@ __global__ void __launch_bounds__(THREADS) k_policy_long(const __grid_constant__
                 if (action >= at && action - at < N) g[action] = from_float<T>(chosen);
             }
     }
-    for (uint32_t k = t; k < head; k += THREADS) g[k] = from_float<T>(k == action ? chosen : all * exp_below(to_float(x[k]), most));
-    for (uint32_t k = behind + t; k < a.n; k += THREADS) g[k] = from_float<T>(k == action ? chosen : all * exp_below(to_float(x[k]), most));
+    for (uint32_t k = t; k < head; k += THREADS) g[k] = from_float<T>(k == action ? chosen : all * exp_below<kWhole<T>>(to_float(x[k]), most));
+    for (uint32_t k = behind + t; k < a.n; k += THREADS) g[k] = from_float<T>(k == action ? chosen : all * exp_below<kWhole<T>>(to_float(x[k]), most));
 }
 
 // The sum over the rows, always of the same parts in the same order: a block's share of them to parts[block], or, of one block, the loss.

@@ -68,3 +68,24 @@ def test_a_ratio_exactly_on_the_border_is_not_clipped(n):
     assert (got.logp == 0).all()
     assert (got.gradient[[0, 1, 4, 5], 1] != 0).all() and (got.gradient[[2, 3]] == 0).all()
     assert got.gradient[0, 1] > 0 > got.gradient[1, 1]       # descending it takes from the other actions where the first did well
+
+
+@pytest.mark.parametrize("n", [7, 40, 100, 200, 300, 1029, 5000, 40000])
+@pytest.mark.parametrize("shift", [0, 1])
+def test_small_probabilities_of_fp32_logits_have_their_bits(n, shift):
+    """One logit far above the others, all of them multiples of 2^-10 below 2^7: differences are exact, the sum is 1 to the last bit (n e^-50 is below 2^-25), the action's log probability is
+    exact, and with the old one equal to it the ratio is 1.  A number of the gradient is then an exponential, off by 2^-22 (the instruction) and four roundings of its correction (2^-24 each),
+    times a weight, with two roundings more."""
+    gen = torch.Generator(device="cuda").manual_seed(n)
+    logits = -torch.randint(50 << 10, 85 << 10, (4, n), generator=gen, device="cuda").float() / 1024
+    at = torch.randint(1, n, (4,), generator=gen, device="cuda")
+    logits[torch.arange(4, device="cuda"), at] = 0.0
+    actions = torch.zeros(4, dtype=torch.int64, device="cuda")
+    old = logits[:, 0].clone()
+    adv, weights = torch.tensor([1.0, -2.0, 4.0, -0.5], device="cuda"), torch.tensor([1.0, 0.5, 2.0, 0.25], device="cuda")
+    out = torch.empty(4, n + shift, device="cuda")[:, shift:]          # (1: rows of the gradient that do not lie like the logits')
+    got = policy_loss(logits, actions, old, adv, weights=weights, clip=(0.2, 0.2), out=out)
+    assert torch.equal(got.logp, old)
+    want = (weights * adv).double()[:, None] * torch.exp(logits.double())
+    want[:, 0] = -(weights * adv).double() * -torch.expm1(old.double())
+    assert ((got.gradient.double() - want).abs() <= (2.0 ** -22 + 6 * 2.0 ** -24) * want.abs()).all()
