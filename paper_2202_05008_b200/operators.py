@@ -4,7 +4,7 @@ All of them enqueue their work on ``stream`` (the current stream of the tensors'
 outputs and workspaces through torch on that stream, and return without waiting.  Where that is not the stream on which an argument
 was made, ordering the two and keeping the argument until the work is done are the caller's.  Arguments that the library cannot
 take raise ``EvoError``; there is no fallback.  None of them has a backward pass that torch records: while torch records gradients, tensors that require one are
-refused (detach them, or call under ``torch.no_grad()``).  Gradients are calls of their own: a training step of a mixture of members (or experts) is
+refused (detach them, or call under ``torch.no_grad()``), and so are dual tensors of forward mode, whose tangent would be lost.  Gradients are calls of their own: a training step of a mixture of members (or experts) is
 
     routes = route_rows(members, groups)                    # members [rows, choices], gates [rows, choices]
     xs = take_rows(x, routes.place)
@@ -25,6 +25,7 @@ from functools import lru_cache
 from typing import NamedTuple, Optional, Sequence, Tuple
 
 import torch
+from torch.autograd import forward_ad
 
 from .binding import (EVO_MAX_LAYERS, Actions, EvoError, Grouped, GroupedGradient, Matrices, Matrix, Muon, NewtonSchulz, PolicyRows, RoutePairs, RowSets, _check,
                       load_library)
@@ -48,6 +49,9 @@ def _require_no_gradient(where: str, *tensors: Optional[torch.Tensor]) -> None:
     for x in tensors:
         if x is not None and x.requires_grad and torch.is_grad_enabled():
             _require(False, where, "a tensor requires a gradient, and there is no backward pass")
+    if forward_ad._current_level >= 0:
+        for x in tensors:
+            _require(x is None or forward_ad.unpack_dual(x).tangent is None, where, "a dual tensor, and no tangent is carried on")
 
 
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)      # the handle without a Stream object (2 us)
