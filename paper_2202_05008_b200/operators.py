@@ -332,7 +332,8 @@ def take_rows(x: torch.Tensor, place: torch.Tensor, weights: Optional[torch.Tens
     they are in ``out``, and undefined without one (which has a row for every pair).  The gradient of x is ``combine_rows(d_out, place, weights)``."""
     lib, where, device = load_library(), "take_rows", x.device
     _require_no_gradient(where, x, weights, out)
-    _check_rows(where, x, place, weights, x.shape[0])
+    _check_rows(where, x, place, weights, x.shape[0] if x.dim() else 0)
+    _require(out is None or out.dim() == 2, where, "out does not match")
     with _On(device, stream, where) as st:
         y = _out(out, x, place.numel() if out is None else out.shape[0], x.shape[1], where)
         code = lib.evo_take_rows(C.byref(_row_sets(x, y, place, weights)), st)
