@@ -262,6 +262,14 @@ evo_status evo_sync_status(evo_solver* s);
  */
 evo_status evo_debug_check(evo_solver* s, int32_t* damaged_region, uint32_t* bounds_site, uint64_t* bounds_index);
 
+/*
+ * Checked build only, for tests of what follows a wait that runs out: until the next such call, the waits inside the tensor-core kernels of
+ * evo_grouped_linear and evo_grouped_linear_backward give up after some 2^wait_cycles_log2 SM clocks (10 .. 31, 31 without this call; those for copies and products in flight keep to
+ * 31), and with drop_completion the first block of a launch leaves out the first completion that another of its warps waits for.  Such a block leaves NaN in what it still has
+ * to write.  The normal build returns EVO_ERR_UNSUPPORTED.  Errors: INVALID_ARG.
+ */
+evo_status evo_debug_grouped_waits(uint32_t wait_cycles_log2, uint32_t drop_completion);
+
 /* Number of kernels the library has launched for this solver so far. */
 evo_status evo_launch_count(evo_solver* s, uint64_t* launches);
 

@@ -105,6 +105,8 @@ def load_library(debug: bool = False):
         getattr(L, name).restype = C.c_int
     L.evo_debug_check.argtypes = [vp, C.POINTER(C.c_int32), u32p, C.POINTER(C.c_uint64)]
     L.evo_debug_check.restype = C.c_int
+    L.evo_debug_grouped_waits.argtypes = [C.c_uint32, C.c_uint32]
+    L.evo_debug_grouped_waits.restype = C.c_int
     L.evo_orthogonalize_bytes.argtypes = [C.c_uint32, C.c_uint32, C.c_uint32, szp]
     L.evo_orthogonalize.argtypes = [vp, vp, vp, vp, C.c_size_t, vp]
     L.evo_muon_bytes.argtypes = [vp, C.c_uint32, C.c_uint64, szp]

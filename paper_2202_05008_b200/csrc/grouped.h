@@ -32,6 +32,11 @@ __device__ __forceinline__ void group_rows(const GroupedArgs& a, uint32_t g, uin
     *end = static_cast<uint64_t>(q);
 }
 
+// The limit of a wait inside the kernels on tcgen05, and whether the first block leaves out a completion (evo_debug_grouped_waits): 31 and no but in the checked build.
+struct Waits { uint32_t cycles_log2, drop; };
+Waits grouped_waits();
+constexpr uint32_t kLongestWait = 31;
+
 size_t grouped_bytes(uint32_t type, const GroupedArgs& a);             // workspace
 int launch_grouped(cudaStream_t st, uint32_t type, const GroupedArgs& a, void* work);
 // grouped_tc.cu: 16-bit types whose rows TMA can address as they lie, where that pays, or (work) rows that are laid out for it first

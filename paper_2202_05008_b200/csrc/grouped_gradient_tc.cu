@@ -36,6 +36,7 @@ struct DwArgs {
     CUtensorMap dz[2], x[2], dw;                             // boxes of 16 and of 64 rows; of 32 outputs x 128 bytes
     uint32_t all, sets, splits, out_tiles, in_tiles, columns, stages;
     uint32_t passes, pitch_dz, pitch_x;
+    Waits waits;
     float* part;                                             // splits > 1: [splits][sets][n_out][n_in]
     float* sums;                                             // 16-bit types: room for the sums of long sets, [first row / long_rows][n_out][n_in]
     uint32_t long_rows, pieces, boxes;                       // pieces: 16-byte stores are possible; boxes: TMA can store the result
@@ -76,7 +77,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_weights_tc(const __grid_constan
 {
     extern __shared__ uint8_t raw[];
     __shared__ __align__(8) uint64_t full[kMostStages], empty[kMostStages], cleared[kMostStages], done[2], taken[2], drain;
-    __shared__ uint32_t slot, limit;
+    __shared__ uint32_t slot, limit, longest;
     __shared__ volatile int abort_flag;
     constexpr bool kFloat = std::is_same<O, float>::value;
     const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31u;
@@ -86,7 +87,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_weights_tc(const __grid_constan
         for (uint32_t b = 0; b < 2u; ++b) { mbar_init(smem_u32(&done[b]), 1); mbar_init(smem_u32(&taken[b]), 8); }
         mbar_init(smem_u32(&drain), 1);
         mbar_init_fence();
-        limit = 31u;
+        limit = p.waits.cycles_log2;
+        longest = kLongestWait;
         abort_flag = 0;
     }
     dep_begin(p.a);
@@ -149,7 +151,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_weights_tc(const __grid_constan
         if (!fine)                                           // nothing may land after the block has gone
             for (uint32_t s = 0; s < min(filled, stages); ++s) {
                 const uint32_t nth = filled - 1u - s;
-                mbar_wait_bounded(smem_u32(&full[nth % stages]), nth / stages & 1u, &limit);
+                mbar_wait_bounded(smem_u32(&full[nth % stages]), nth / stages & 1u, &longest);
             }
     } else if (warp == 1) {
         if (lane == 0) {                                     // (one thread: what it does between two MMAs is time that the tensor core has nothing to do)
@@ -189,6 +191,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_weights_tc(const __grid_constan
                             const uint64_t a = desc_sw128_mn(at_stage, bytes), b = desc_sw128_mn(at_stage + 2u * bytes, bytes);
                             for (uint32_t s = 0; s * 16u < rest; ++s) multiply(a, b, s);
                         }
+#ifdef EVO_DEBUG
+                        if (!p.waits.drop || at != 0u || k != 0u)
+#endif
                         umma_commit(smem_u32(&empty[stage]));
                         if (++chunk == chunks) chunk = 0;
                         if (++stage == stages) { stage = 0; phase ^= 1u; }
@@ -200,7 +205,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_weights_tc(const __grid_constan
             }
             if (!fine) {                                     // no MMA may write after its tensor memory is freed
                 umma_commit(smem_u32(&drain));
-                mbar_wait_bounded(smem_u32(&drain), 0u, &limit);
+                mbar_wait_bounded(smem_u32(&drain), 0u, &longest);
             }
         }
         __syncwarp();
@@ -250,6 +255,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_weights_tc(const __grid_constan
                 if (steps) {
                     end = part_end(first, chunks);
                     wait(&done[acc], acc_phase);
+                    __syncwarp();
                     tc_fence_after();
                 }
                 const float scale = abort_flag ? __int_as_float(0x7FC00000) : p.a.f.scale;
@@ -541,6 +547,7 @@ int launch_grouped_gradient_tc(cudaStream_t st, uint32_t type, const GradientArg
     if (!encode) return -1;
     DwArgs p;
     p.a = a;
+    p.waits = grouped_waits();
     p.a.late = plan.dx;                                      // (what is laid out is behind dx's kernel)
     p.all = a.sum_w; p.sets = a.sum_w ? 1u : f.groups; p.splits = splits;
     p.out_tiles = (f.n_out + 127u) / 128u;

@@ -1,4 +1,5 @@
 // C entry points of the products grouped by member and of the policy's actions.
+#include <atomic>
 #include <cmath>
 #include <cstring>
 
@@ -10,6 +11,10 @@ using namespace evo;
 namespace {
 
 constexpr uint64_t kMost = 1ull << 40;       // elements of a pitch or a stride, and rows
+
+#ifdef EVO_DEBUG
+std::atomic<uint32_t> test_waits { kLongestWait }, test_drop { 0u };
+#endif
 
 // the layers of a policy as the kernel for rows and layers takes them
 void policy_layers(const evo_actions& p, MemberArgs* a)
@@ -65,7 +70,25 @@ evo_status check_actions(const evo_actions* a)
 
 }  // namespace
 
+#ifdef EVO_DEBUG
+evo::Waits evo::grouped_waits() { return { test_waits.load(), test_drop.load() }; }
+#else
+evo::Waits evo::grouped_waits() { return { kLongestWait, 0u }; }
+#endif
+
 extern "C" {
+
+evo_status evo_debug_grouped_waits(uint32_t wait_cycles_log2, uint32_t drop_completion)
+{
+    if (wait_cycles_log2 < 10u || wait_cycles_log2 > kLongestWait || drop_completion > 1u) return EVO_ERR_INVALID_ARG;
+#ifdef EVO_DEBUG
+    test_waits = wait_cycles_log2;
+    test_drop = drop_completion;
+    return EVO_OK;
+#else
+    return EVO_ERR_UNSUPPORTED;
+#endif
+}
 
 static evo_status check_grouped(const evo_grouped* p)
 {

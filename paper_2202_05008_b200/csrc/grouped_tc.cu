@@ -42,6 +42,7 @@ struct TcArgs {
     CUtensorMap w, x[3];                                     // the rows in boxes of 32, 64 and 128
     uint32_t out_tiles, shared_w;                            // shared_w: one set of weights for all groups
     uint32_t most_rows, stages;                              // of a tile (a multiple of 32); as many as the ring has room for
+    Waits waits;
     uint32_t passes, pitch_w, pitch_x;                       // passes through the contracted index (1, 6, or TR 2); from one part of an operand to the next
 };
 // Walks a warp over the tiles of all groups.  Row tiles of a group: as few as can be, equal up to 16 rows.
@@ -93,7 +94,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_grouped_tc(const __grid_constan
 {
     extern __shared__ uint8_t raw[];
     __shared__ __align__(8) uint64_t full[kMostStages], empty[kMostStages], done[2], taken[2], drain;
-    __shared__ uint32_t slot, limit;
+    __shared__ uint32_t slot, limit, longest;
     __shared__ volatile int abort_flag;
     const GroupedArgs& a = p.g;
     const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31u;
@@ -103,7 +104,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_grouped_tc(const __grid_constan
         for (uint32_t b = 0; b < 2u; ++b) { mbar_init(smem_u32(&done[b]), 1); mbar_init(smem_u32(&taken[b]), 8); }
         mbar_init(smem_u32(&drain), 1);
         mbar_init_fence();
-        limit = 31u;
+        limit = p.waits.cycles_log2;
+        longest = kLongestWait;
         abort_flag = 0;
     }
     dep_wait();
@@ -170,7 +172,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_grouped_tc(const __grid_constan
         if (!fine)                                           // nothing may land after the block has gone
             for (uint32_t s = 0; s < min(filled, stages); ++s) {
                 const uint32_t nth = filled - 1u - s;
-                mbar_wait_bounded(smem_u32(&full[nth % stages]), nth / stages & 1u, &limit);
+                mbar_wait_bounded(smem_u32(&full[nth % stages]), nth / stages & 1u, &longest);
             }
     } else if (warp == 1) {
         for (uint64_t at = blockIdx.x; fine && walk.find(p, at / p.out_tiles, &group, &row, &rows); at += gridDim.x) {
@@ -190,6 +192,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_grouped_tc(const __grid_constan
                             if (kHalfRows && s == 0u && k == turn && k != first) umma_scaling_down<kSecondUp>(d, a, b, id);
                             else umma_bf16(d, a + s * (TR ? 128u : 2u), b + s * 2u, id, k - first + s != 0u);
                         }
+#ifdef EVO_DEBUG
+                        if (!p.waits.drop || blockIdx.x != 0u || at != 0u || k != 0u)
+#endif
                         umma_commit(smem_u32(&empty[stage]));
                         if (++stage == stages) { stage = 0; phase ^= 1u; }
                     }
@@ -202,7 +207,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_grouped_tc(const __grid_constan
         }
         if (!fine && lane == 0) {                            // no MMA may write after its tensor memory is freed
             umma_commit(smem_u32(&drain));
-            mbar_wait_bounded(smem_u32(&drain), 0u, &limit);
+            mbar_wait_bounded(smem_u32(&drain), 0u, &longest);
         }
         __syncwarp();
     } else {
@@ -223,6 +228,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_grouped_tc(const __grid_constan
             for (uint32_t first = 0, end = 0; end < steps; first = end) {
                 end = part_end(first);
                 wait(&done[acc], acc_phase);
+                __syncwarp();
                 tc_fence_after();
                 const float scale = abort_flag ? __int_as_float(0x7FC00000) : a.scale;
                 auto take = [&](uint32_t c, float (&so_far)[32]) {
@@ -423,6 +429,7 @@ static int launch_tiles(cudaStream_t st, uint32_t type, TcArgs& p, bool transpos
     const EncodeTiled f = tensor_map_encoder();
     if (!f) return -1;
     const GroupedArgs& a = p.g;
+    p.waits = grouped_waits();
     p.out_tiles = (a.n_out + 127u) / 128u;
     p.shared_w = a.groups > 1u && a.stride_w == 0u;
     const CUtensorMapDataType t = type == EVO_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;

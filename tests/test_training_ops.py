@@ -177,3 +177,9 @@ def test_tensors_that_want_a_gradient_are_refused():
         with torch.no_grad(), pytest.raises(EvoError) as e:         # (these are not on a GPU, which is the next thing that is looked at)
             call(lambda t: t.clone().requires_grad_())
         assert "backward pass" not in str(e.value)
+
+
+def test_waits_can_be_made_short_in_the_checked_build_alone(lib):
+    for bad in ((9, 0), (32, 0), (20, 2)):
+        assert lib.evo_debug_grouped_waits(*bad) == INVALID
+    assert lib.evo_debug_grouped_waits(20, 1) == 7           # EVO_ERR_UNSUPPORTED
