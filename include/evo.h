@@ -465,8 +465,8 @@ evo_status evo_route_rows(const evo_routes* p, void* d_workspace, size_t workspa
  *   combine_backward, rows being the gradient of what combine returned:
  *                      sorted_gradient[place[r][j]] = weights[r][j] rows[r]
  *                      weights_gradient[r][j] = rows[r] . sorted[place[r][j]]      (no place: 0)
- * Sorted rows that no place names are left as they are.  Two pairs with the same place leave one of the two rows there (route_rows
- * makes none).  Sums in fp32 in the choices' order, weights fp32, all other numbers of one type, any pitch and alignment.  A weight of 0 takes
+ * Sorted rows that no place names are left as they are.  Two pairs with the same place leave numbers of either there, in take as in
+ * combine_backward, where the gradient would be their sum (route_rows makes none).  Sums in fp32 in the choices' order, weights fp32, all other numbers of one type, any pitch and alignment.  A weight of 0 takes
  * infinities and NaN of its row along as NaN; a place that is none takes nothing.  Outputs may not overlap anything, from the first to the last element of
  * each array.
  * Errors: INVALID_ARG, UNSUPPORTED (more than 2^31 blocks), CUDA.

@@ -3,7 +3,7 @@
 // A group of a population has few rows and weights of its own: dx is bound by the weights' way from memory, dW by its own way there.  k_rows reads
 // a group's weights once for up to 8 or 16 rows; k_weights makes tiles of 64 outputs x 64 or 128 inputs, or narrow ones.  Where there are too few tiles for the
 // GPU, what is summed over (dx: weight rows, dW and db: rows) is split and the parts added up in a fixed order.  4,096 members of 128 x 128, 16,384 ragged rows, fp32: k_rows 60 us (4.7 TB/s; reading the
-// weights alone is 41), k_weights 80 (its stores alone 40; the rest is what a block waits for before it stores), all together, overlapped, 138.
+// weights alone is 41), k_weights 80 (its stores alone 40; the rest is what a block waits for before it stores), all together, overlapped, 135.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -618,7 +618,9 @@ bool whole_pieces(const GradientArgs& a) { return ((a.f.n_in | a.f.n_out) & 7u) 
 //   16 bits  200 of 256 -> 256 (2) 13.1 / 10.6, (5) 13.1 / 15.9; 1,000 of 64 -> 64 (16) 26.4 / 17.6, (32) 27.5 / 31.6; 4,096 of 128 -> 128 (16) 109 / 100; 32 of 1,024 -> 1,024
 //            (2) 16.6 / 22.2, (8) 16.6 / 39.4; 1 of 4,096 -> 4,096 (10) 25.8 / 24.1, (64) 26 / 75; not aligned: 300 of 207 -> 379 (5) 60.8 / 36.7, (8) 61.3 / 64.5; 3,000 of
 //            20 -> 30 (16) 94.6 / 65.2, (32) 102 / 105; 10 of 1,887 -> 3,200 (1) 56 / 117
-// Over 374 shapes (270 of them drawn) the choice takes 1.03 times the faster side's time in the geometric mean; tcgen05 always 1.8 times, k_rows always 1.16.
+// Over 374 shapes (270 of them drawn) the choice takes 1.03 times the faster side's time in the geometric mean; tcgen05 always 1.8 times, k_rows always 1.16.  It is a fit, and the lines above
+// are not all on its side: 1,000 of 64 -> 64 fp32 go to tcgen05 from 63 rows on (75 us for 48), 32 of 1,024 -> 1,024 fp32 from 35 on, where the two meet near 54, and 16 bits from 2.5 (2 rows: 22.2 us for
+// 16.6).
 bool dx_on_tensor_cores(uint32_t type, const GradientArgs& a)
 {
     const GroupedArgs& f = a.f;

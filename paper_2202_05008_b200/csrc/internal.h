@@ -176,6 +176,8 @@ int launch_rollout_paint(cudaStream_t st, const float* theta, uint32_t ldD, uint
 // return): that waits for the predecessor to have completed, and so, one after the other, for
 // everything before it.  A kernel lets its successor be set up with dep_trigger().  After a kernel that
 // never triggers, or after a copy, the launch is an ordinary one.
+// One exception: a kernel of a call that neither reads nor writes over what its predecessors in the same call write or read may wait at its end instead (every thread, before any return), if the first of
+// them has waited before it triggered.  What came before the call is then complete when it starts, and what follows it still finds everything complete (dep_begin and dep_end of the grouped products' gradients).
 // ------------------------------------------------------------------------------------------
 // Dynamic shared memory for a grid of `blocks` that fits the SMs at fewer blocks each than could be resident (see spread_bytes).
 // Without it the blocks of a grid that becomes resident while the kernel before it still occupies some SMs crowd the others

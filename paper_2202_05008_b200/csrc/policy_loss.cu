@@ -1,11 +1,12 @@
-// Clipped policy loss of rows of logits and its gradient, one pass over the logits.
+// Clipped policy loss of rows of logits and its gradient.
 //
 //   e_v = exp(x_v - max), s = sum e_v, logp = x_a - max - log s;  gradient_v = w c ([v = a] - e_v / s)
-// A row stays in registers between its two uses (the sum and the gradient), so that it is read once and its gradient written once: that
-// traffic is the bound for long rows, the launch for few short ones.  Rows of up to 256 actions are a part of a warp's, number by number; longer ones a warp's or a block's, in
-// pieces of 16 bytes from the row's first 16-byte boundary on (the ends in single numbers), where logits and gradient lie alike; other rows, and rows longer than a block's
-// registers hold, are read twice, the second time mostly from L2.
-// One thread has the row's scalars.
+// Rows of up to 256 actions are a part of a warp's, number by number, and rows of up to 4 KB a warp's, in pieces of 16 bytes from the row's first 16-byte boundary on (the ends in single
+// numbers): they stay in registers between their two uses, the sum and the gradient.  Longer rows are a block's and are read twice, the second time mostly from L2.  So are all rows above 256
+// actions whose logits and gradient do not begin alike modulo 16 bytes, number by number.  A lane, or one thread of a block, has a row's scalars.
+// Many short rows are bound by those and by issue (4,000,000 of 64: fp32 470 us, 4.4 TB/s, bf16 586; 100,000 of 300 bf16 83, of 900 106, of 2,000 158, 5.1 TB/s), long ones by memory and the
+// exponentials (8,192 of 32,000 bf16 196 to 211), few by the launch and by a row's way through one block (1 to 148 rows of 130,000 bf16 20 us a call).  Rows that do not lie alike take
+// two to six times as long: bf16 of pitch 50,304, 4,096 of 50,257 340 us against 165, 100,000 of 300 in a pitch of 304 509 against 83.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -159,7 +160,7 @@ __device__ __forceinline__ void padded_row(const PolicyArgs& a, uint64_t row)
 }
 
 // Up to L E actions: L lanes a row, E numbers each; a warp has R times 32 / L rows one behind the other, and a lane finishes each of them (a
-// row's scalars in fp64 cost more than its numbers: 4 million rows of 64 took 2,870 us with a row a time).
+// row's scalars in fp64 cost more than its numbers: 4 million rows of 64 took 2,870 us with a row a time, fp32 470 and bf16 586 so).
 // ONE: the grid is one cluster, whose blocks' shares of the loss meet in the first one's shared memory, added up in their order: no second launch (1,024 rows of 12: a call
 // from Python 21 -> 18.7 us, on the device 5.4 -> 4.7).
 template <typename T, uint32_t L, uint32_t E, uint32_t R, bool ONE>

@@ -358,7 +358,8 @@ def combine_rows(y: torch.Tensor, place: torch.Tensor, weights: Optional[torch.T
 def combine_rows_backward(d_out: torch.Tensor, y: torch.Tensor, place: torch.Tensor, weights: torch.Tensor, *, out: Optional[torch.Tensor] = None,
                           stream: Optional[torch.cuda.Stream] = None) -> Tuple[torch.Tensor, torch.Tensor]:
     """``evo_combine_rows_backward``: the gradients (of y, of weights) of ``combine_rows(y, place, weights)`` for the gradient ``d_out`` of its result.
-    Rows of y that no place names are left as they are in ``out`` (the gradient of y), and undefined without one.  Without weights the gradient of y
+    Rows of y that no place names are left as they are in ``out`` (the gradient of y), and undefined without one; a row that two places name, which route_rows never gives, has
+    numbers of either's gradient and not their sum.  Without weights the gradient of y
     is ``take_rows(d_out, place)``."""
     lib, where, device = load_library(), "combine_rows_backward", y.device
     _require_no_gradient(where, d_out, y, weights, out)
@@ -445,7 +446,8 @@ def policy_loss(logits: torch.Tensor, actions: torch.Tensor, old_logp: torch.Ten
                 out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> PolicyLoss:
     """``evo_policy_loss``: the clipped policy loss (to be minimised) of rows of ``logits`` [rows, n] (fp32, bf16 or fp16) with ``kl`` times the estimate
     ``exp(ref - logp) - (ref - logp) - 1`` of the divergence from a reference policy; its sum over the rows times ``weights`` (None: the mean), the log probability of every
-    row's action, and the gradient of the logits (``gradient`` False: None; ``out`` may be ``logits``).  ``clip``: how far a ratio may fall below and rise above 1.
+    row's action, and the gradient of the logits (``gradient`` False: None; ``out`` may be ``logits``; for rows of logits inside wider ones, an ``out`` of the same pitch takes half
+    the time or less).  ``clip``: how far a ratio may fall below and rise above 1.
     actions int32 or int64; old_logp, advantage, ref_logp and weights fp32, [rows].  A row whose action is outside [0, n) or whose weight is 0
     is padding.  Logits of minus infinity are forbidden actions."""
     lib, where, device = load_library(), "policy_loss", logits.device
